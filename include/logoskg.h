@@ -467,6 +467,159 @@ logoskg_status logoskg_paths_static(logoskg_graph *g, const logoskg_result *r, c
                                     const int32_t *target, int64_t n_pairs, int32_t max_paths,
                                     int32_t *path_count, int32_t *path_edges, void *stream);
 
+/* ---------------------------------------------------------------- reading */
+
+/*
+ * What a language model does with a retrieval.  None of these calls belongs to a
+ * graph: they take device arrays, launch on `stream` of `device`, allocate
+ * nothing, do not synchronise and may be captured.  A batch is ragged: row i of
+ * document d stands at off[d] + i.  Offsets are device int64[n + 1], ascending;
+ * what they say outside the arrays they index is not read (each is taken into
+ * [0, length of the array]).
+ */
+typedef enum { LOGOSKG_F32 = 0, LOGOSKG_BF16 = 1, LOGOSKG_F16 = 2 } logoskg_dtype;
+
+#define LOGOSKG_MAX_BUCKETS 64      /* buckets of a learned distance bias                    */
+#define LOGOSKG_MAX_DISTANCE 1024   /* largest distance that has a bucket of its own         */
+#define LOGOSKG_BIAS_PLACES 16384   /* heads / kv_heads * (2 max_distance + 1) at most       */
+
+/*
+ * How scores are made of products, for every call below: with z = scale q.k,
+ *     u = cap tanh(z / cap)   (cap = 0: u = z)
+ *     y = u + bias[head][buckets[clamp(k_pos - q_pos, -M, M) + M]],  M = max_distance
+ * and the softmax over the visible keys' y.  bias has the type of q; NULL = none.
+ */
+typedef struct {
+    float scale, cap;
+    const void *bias;         /* device [heads][num_buckets]                                */
+    const int32_t *buckets;   /* device [2 max_distance + 1], entries in [0, num_buckets)   */
+    int32_t num_buckets, max_distance;
+} logoskg_score;
+
+typedef struct {
+    uint32_t struct_size;     /* sizeof(logoskg_attention)                                   */
+    int32_t device;
+    int32_t dtype;            /* of q, k, v, out and the bias: LOGOSKG_BF16 or LOGOSKG_F16   */
+    int32_t num_docs;
+    int32_t heads, kv_heads;  /* head h reads key head h / (heads / kv_heads)                */
+    int32_t dim;              /* of a head: a multiple of 8, at most 128                     */
+    int32_t causal;
+    int64_t num_rows, num_keys;      /* rows of q / of k and v, all documents together       */
+    const int64_t *q_off, *k_off;    /* device int64[num_docs + 1]                           */
+    const void *q, *k, *v;           /* device, rows of heads of dim consecutive elements    */
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head; /* strides, in elements: multiples of 8
+                                        (the arrays are 16-byte aligned)                     */
+    const int32_t *prefix;    /* device int32[num_docs] or NULL (no prefix)                  */
+    const int32_t *q_pos;     /* device int32[num_rows] or NULL: row i stands at i + keys - rows
+                                 of its document                                             */
+    const int32_t *k_pos;     /* device int32[num_keys] or NULL: key j stands at j           */
+    logoskg_score score;
+    void *out;                /* device [num_rows][heads][dim]                               */
+    float *lse;               /* device [num_rows][heads]: log of the sum of exp(y)          */
+    void *stream;             /* hipStream_t                                                 */
+} logoskg_attention;
+
+/*
+ * Attention of a ragged batch.  Row i of a document with R rows and K keys sees
+ * all K keys, or with `causal` the keys j < prefix and j <= i + K - R (the
+ * retrieved entities in front, then the text up to the row itself).  A row that
+ * sees nothing gets zeros and lse = -inf.
+ */
+logoskg_status logoskg_attend(const logoskg_attention *a);
+
+typedef struct {
+    uint32_t struct_size;     /* sizeof(logoskg_attention_grad)                              */
+    int32_t reserved;
+    const void *dout;         /* device [num_rows][heads][dim]: gradient of out              */
+    void *dq;                 /* device [num_rows][heads][dim]                               */
+    void *dk, *dv;            /* device [num_keys][kv_heads][dim], summed over the heads that
+                                 share a key head                                            */
+    void *dbias;              /* device [heads][num_buckets], NULL without a bias            */
+    void *workspace;          /* device, logoskg_attend_backward_bytes bytes, 16-byte aligned */
+    int64_t workspace_bytes;
+} logoskg_attention_grad;
+
+/*
+ * Gradients of logoskg_attend with respect to q, k, v and the bias, for out and
+ * lse as that call has left them.  Sums are taken in a fixed order: the same
+ * inputs give the same bits.
+ */
+int64_t logoskg_attend_backward_bytes(const logoskg_attention *a);
+logoskg_status logoskg_attend_backward(const logoskg_attention *a, const logoskg_attention_grad *g);
+
+typedef struct {
+    uint32_t struct_size;     /* sizeof(logoskg_entity_read)                                 */
+    int32_t device;
+    int32_t dtype;            /* of q, keys, values, out and the bias                        */
+    int32_t num_queries;
+    int32_t tokens;           /* rows of q per query                                         */
+    int32_t heads, kv_heads, dim;
+    int64_t num_entries;      /* length of entity and hop                                    */
+    int64_t num_entities;     /* rows of keys and values                                     */
+    const int64_t *off;       /* device int64[num_queries + 1]                               */
+    const int32_t *entity;    /* device int32[num_entries]: rows of keys and values; entries outside
+                                 [0, num_entities) are left out.  NULL: entry i reads row i  */
+    const uint8_t *hop;       /* device uint8[num_entries] or NULL (all 0): position of the entries */
+    const int32_t *q_pos;     /* device int32[num_queries] or NULL (all 0): position of the tokens  */
+    const void *q;            /* device [num_queries][tokens][heads][dim]                    */
+    const void *keys, *values; /* device, rows of kv_heads x dim                             */
+    int64_t key_row, key_head, value_row, value_head; /* strides, in elements: multiples of 8 */
+    logoskg_score score;
+    void *out;                /* device [num_queries][tokens][heads][dim]                    */
+    float *lse;               /* device [num_queries][tokens][heads]                         */
+    void *workspace;          /* device, logoskg_read_entities_bytes bytes, 16-byte aligned  */
+    int64_t workspace_bytes;
+    void *stream;
+} logoskg_entity_read;
+
+/*
+ * The serving form: the few tokens of each query attend to all entries of its
+ * list (off, entity and hop as logoskg_result_offsets and logoskg_result_fetch
+ * give them), whose keys and values lie in a table by entity.  A query with no
+ * entry gets zeros and lse = -inf.
+ */
+int64_t logoskg_read_entities_bytes(const logoskg_entity_read *r);
+logoskg_status logoskg_read_entities(const logoskg_entity_read *r);
+
+/*
+ * The lists as bit masks in the layout of logoskg_query_batch.rel_mask:
+ * mask = device uint64[num_queries][ceil(num_ids / 64)], bit i % 64 of word
+ * i / 64 set for every id of the query's list.  Ids outside [0, num_ids) are
+ * left out; order and repeats do not matter.
+ */
+logoskg_status logoskg_entity_mask(int32_t device, const int64_t *off, const int32_t *ids, int64_t num_entries,
+                                   int32_t num_queries, int64_t num_ids, uint64_t *mask, void *stream);
+
+typedef struct {
+    uint32_t struct_size;     /* sizeof(logoskg_logits)                                      */
+    int32_t device;
+    int32_t dtype;            /* of logits and out                                           */
+    int32_t num_rows;
+    int64_t vocab;
+    int64_t row;              /* stride of the rows of logits and of out, in elements        */
+    const void *logits;       /* device                                                      */
+    void *out;                /* device; may be `logits`                                     */
+    const int64_t *history_off; /* device int64[num_rows + 1], with history; NULL = none     */
+    const int32_t *history;   /* device int32[num_history]: ids said so far, repeats count; ids
+                                 outside [0, vocab) pad                                      */
+    int64_t num_history;
+    const float *repetition, *presence, *frequency; /* device float[num_rows] each, or NULL   */
+    const int64_t *bias_off;  /* device int64[num_rows + 1], with bias_id and bias_value; NULL = none */
+    const int32_t *bias_id;   /* device int32[num_bias]; of repeated ids the last entry counts */
+    const float *bias_value;  /* device float[num_bias]                                      */
+    int64_t num_bias;
+    const uint64_t *mask;     /* device uint64[num_rows][ceil(vocab / 64)] or NULL           */
+    void *stream;
+} logoskg_logits;
+
+/*
+ * A step's logits, in this order: an id that its row's history holds c > 0 times
+ * is divided by `repetition` where it is positive and multiplied by it where it
+ * is not, then loses presence + c frequency; biases are added; ids whose mask bit
+ * is 0 become -inf, whatever stood there.
+ */
+logoskg_status logoskg_constrain_logits(const logoskg_logits *l);
+
 const char *logoskg_last_error(void);
 const char *logoskg_version(void);
 

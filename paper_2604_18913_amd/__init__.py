@@ -6,6 +6,8 @@ names.  PyTorch is used only for device buffers and the stream handle.
 """
 from .binding import (Graph, Result, LogosKGError, logoskg_build, logoskg_khop, logoskg_paths,
                       library_path, version)
+from .reading import (attend, attend_backward, constrain_logits, distance_buckets, entity_mask, read_entities)
 
 __all__ = ["Graph", "Result", "LogosKGError", "logoskg_build", "logoskg_khop", "logoskg_paths",
-           "library_path", "version"]
+           "library_path", "version", "attend", "attend_backward", "constrain_logits", "distance_buckets",
+           "entity_mask", "read_entities"]

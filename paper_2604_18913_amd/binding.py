@@ -145,6 +145,17 @@ def _load():
     lib.logoskg_profile_enable.argtypes = [P, I32]
     lib.logoskg_profile_read.restype = ctypes.c_int
     lib.logoskg_profile_read.argtypes = [P, P, I32, ctypes.POINTER(I32)]
+    for name in ("attend", "attend_backward", "read_entities", "entity_mask", "constrain_logits"):
+        getattr(lib, "logoskg_" + name).restype = ctypes.c_int
+    lib.logoskg_attend.argtypes = [P]
+    lib.logoskg_attend_backward.argtypes = [P, P]
+    lib.logoskg_attend_backward_bytes.restype = I64
+    lib.logoskg_attend_backward_bytes.argtypes = [P]
+    lib.logoskg_read_entities.argtypes = [P]
+    lib.logoskg_read_entities_bytes.restype = I64
+    lib.logoskg_read_entities_bytes.argtypes = [P]
+    lib.logoskg_entity_mask.argtypes = [I32, P, P, I64, I32, I64, P, P]
+    lib.logoskg_constrain_logits.argtypes = [P]
     lib.logoskg_last_error.restype = ctypes.c_char_p
     lib.logoskg_version.restype = ctypes.c_char_p
     _lib = lib

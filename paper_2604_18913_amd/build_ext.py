@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblogoskg.so")
-SOURCES = ["build.hip", "build_device.hip", "khop.hip", "small.hip", "result.hip", "paths.hip", "shards.hip", "triples.hip", "walks.hip"]
+SOURCES = ["build.hip", "build_device.hip", "khop.hip", "small.hip", "result.hip", "paths.hip", "shards.hip", "triples.hip", "walks.hip",
+           "attend.hip", "attend_backward.hip", "read.hip", "answers.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -19,7 +20,8 @@ FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
 def _stale(obj: str, src: str) -> bool:
     if not os.path.exists(obj):
         return True
-    deps = [src, os.path.join(CSRC, "common.h"), os.path.join(ROOT, "include", "logoskg.h")]
+    deps = [src, os.path.join(ROOT, "include", "logoskg.h")]
+    deps += [os.path.join(CSRC, h) for h in ("common.h", "reading.h", "attend.h")]
     return any(os.path.getmtime(d) > os.path.getmtime(obj) for d in deps)
 
 

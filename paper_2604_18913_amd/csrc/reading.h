@@ -1,0 +1,167 @@
+// Device helpers of the calls that read a retrieval into a language model (attend*.hip, read.hip, answers.hip).
+#pragma once
+
+#include "common.h"
+
+namespace lkg {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLowest = -1e30f;  // running maximum of a row that has seen nothing: below any score, and no infinity
+
+// The two 16-bit types: eight values as a matrix instruction takes them, and that instruction on 32 x 32 x 16.
+// Lane l holds A[l % 32][8 (l / 32) ..] and B[8 (l / 32) ..][l % 32]; C's element r is row 8 (r / 4) + 4 (l / 32) + r % 4
+// of column l % 32.  So C = rows x columns puts a column into a lane (and its partner in the other half), which makes
+// softmax sums a loop over registers and one exchange, and C's elements 8 s .. 8 s + 7 are the B of the next product's
+// step s as they are, if its A takes the 16 places of the step in the same order: 4 h .. 4 h + 3 and 8 + 4 h .. 8 + 4 h + 3
+// in half h, which is what two transposing LDS reads give.
+template <class E> struct Vec8 { typedef E type __attribute__((ext_vector_type(8))); };
+template <class E> struct Vec4 { typedef E type __attribute__((ext_vector_type(4))); };
+typedef __bf16 bf16;
+typedef _Float16 fp16;
+
+__device__ __forceinline__ f32x16 mfma(Vec8<bf16>::type a, Vec8<bf16>::type b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mfma(Vec8<fp16>::type a, Vec8<fp16>::type b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+template <class E> __device__ __forceinline__ typename Vec8<E>::type as8(u32x4 x) { return __builtin_bit_cast(typename Vec8<E>::type, x); }
+
+__device__ __forceinline__ f32x16 zero16() {
+    f32x16 z;
+#pragma unroll
+    for (int i = 0; i < 16; i++) z[i] = 0.f;
+    return z;
+}
+
+// eight elements of a C as the B of the next product, each rounded once to E (nearest even): the operands of a matrix
+// instruction have 16 bits, and the products are summed in 32
+template <class E, int S> __device__ __forceinline__ typename Vec8<E>::type rounded8(const f32x16 &c) {
+    typename Vec8<E>::type r;
+#pragma unroll
+    for (int i = 0; i < 8; i++) r[i] = (E)c[8 * S + i];
+    return r;
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }  // 1 ulp, 0 below 2^-126
+__device__ __forceinline__ float rcp_fast(float x) { return __builtin_amdgcn_rcpf(x); }    // 1 ulp
+
+// x of this lane and of its partner in the other half of the wavefront.  (The exchange gets two registers: of one given
+// twice the compiler takes both results to be the same.)
+__device__ __forceinline__ void both_halves(float x, float &lo, float &hi) {
+    unsigned a = __builtin_bit_cast(unsigned, x), b = a;
+    asm("" : "+v"(b));
+    auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+    lo = __builtin_bit_cast(float, (unsigned)r[0]);
+    hi = __builtin_bit_cast(float, (unsigned)r[1]);
+}
+__device__ __forceinline__ float halves_max(float x) {
+    float lo, hi;
+    both_halves(x, lo, hi);
+    return fmaxf(lo, hi);
+}
+__device__ __forceinline__ float halves_sum(float x) {
+    float lo, hi;
+    both_halves(x, lo, hi);
+    return lo + hi;
+}
+
+// what the wavefront's lanes have written to LDS is there for its other lanes (LDS runs a wavefront's accesses in order)
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// A tile in LDS: rows of DP 16-bit values in 16-byte chunks, chunk c of row r at place c ^ spread(r), so that neither the
+// 16 rows x one chunk that a row-wise read asks for at a time nor the 4 rows x 64 bytes of a transposing read share banks.
+template <int DP> __device__ __forceinline__ int spread(int r) {
+    if (DP == 128) return ((r & 3) << 2) | ((r >> 2) & 3);
+    return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+}
+
+// A[row of the tile][16 kk + 8 (l / 32) ..]: rows at r0 + l % 32
+template <class E, int DP> __device__ __forceinline__ typename Vec8<E>::type tile_rows(const char *tile, int r0, int kk, int lane) {
+    int r = r0 + (lane & 31), c = 2 * kk + (lane >> 5);
+    return as8<E>(*(const u32x4 *)(tile + r * (DP * 2) + ((c ^ spread<DP>(r)) << 4)));
+}
+
+// A = the tile's transpose: lane l gets column 32 dt + l % 32 of the rows r0 + 4 (l / 32) .. + 3 and r0 + 8 + 4 (l / 32) .. + 3
+template <class E, int DP> __device__ __forceinline__ typename Vec8<E>::type tile_columns(const char *tile, int r0, int dt, int lane) {
+    typedef __attribute__((address_space(3))) s16x4 lds4;
+    int r = r0 + ((lane & 15) >> 2) + 4 * (lane >> 5), c = 4 * dt + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(tile + r * (DP * 2) + ((c ^ spread<DP>(r)) << 4) + (lane & 1) * 8));
+    r += 8;
+    s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(tile + r * (DP * 2) + ((c ^ spread<DP>(r)) << 4) + (lane & 1) * 8));
+    struct { s16x4 a, b; } both = {lo, hi};
+    return __builtin_bit_cast(typename Vec8<E>::type, both);
+}
+
+// ---------------------------------------------------------------- ragged batches
+__device__ __forceinline__ long long taken_into(long long x, long long hi) { return x < 0 ? 0 : x > hi ? hi : x; }
+
+// Blocks of 2^shift rows over the documents of a ragged array, without a pass over their lengths: document d has the
+// blocks (off[d] mult >> shift) + d up to those of d + 1, at least as many as it needs.  The document of a block by a
+// search of the whole wavefront, two rounds for 4,096 documents.
+__device__ __forceinline__ long long first_block(const int64_t *off, int d, long long total, int mult, int shift) {
+    return (taken_into(off[d], total) * mult >> shift) + d;
+}
+__device__ __forceinline__ int document_of(const int64_t *off, int n, long long total, int mult, int shift, long long block, int lane) {
+    int lo = 0, span = n;
+    while (span > 1) {
+        int step = (span + 63) >> 6, at = lane * step;
+        bool below = at < span && first_block(off, lo + at, total, mult, shift) <= block;
+        int count = __popcll(__ballot(below));
+        int skip = (count > 0 ? count - 1 : 0) * step;
+        lo += skip;
+        span = span - skip < step ? span - skip : step;
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// ---------------------------------------------------------------- scores
+// What the kernels make of logoskg_score, in units of log 2: y = cap: c - 2 c / (2^(z k) + 1), c = cap log2 e, which is
+// c tanh(z / cap) for k = 2 log2 e scale / cap (2^.. may be infinite or 0: +c or -c); else z k, k = scale log2 e.
+struct ScoreArgs {
+    float k, c;
+    const void *bias;
+    const int32_t *buckets;
+    int num_buckets, max_distance;
+};
+
+inline ScoreArgs score_args(const logoskg_score &s) {
+    ScoreArgs a;
+    a.k = s.cap > 0 ? 2.f * kLog2e * s.scale / s.cap : s.scale * kLog2e;
+    a.c = s.cap > 0 ? s.cap * kLog2e : 0.f;
+    a.bias = s.bias;
+    a.buckets = s.buckets;
+    a.num_buckets = s.num_buckets;
+    a.max_distance = s.max_distance;
+    return a;
+}
+
+// Biases of the heads h0 .. h0 + group - 1 by distance, times log2 e, in LDS: [group][2 M + 1]
+template <class E> __device__ __forceinline__ void bias_to_lds(float *table, const ScoreArgs &s, int h0, int group, int tid, int threads) {
+    const E *bias = (const E *)s.bias;
+    int places = 2 * s.max_distance + 1;
+    for (int i = tid; i < places; i += threads) {
+        int b = s.buckets[i];
+        b = b < 0 ? 0 : b >= s.num_buckets ? s.num_buckets - 1 : b;
+        for (int g = 0; g < group; g++) table[g * places + i] = (float)bias[(long long)(h0 + g) * s.num_buckets + b] * kLog2e;
+    }
+}
+
+__device__ __forceinline__ int distance_place(int k_pos, int q_pos, int M) {
+    int d = __builtin_elementwise_sub_sat(k_pos, q_pos);
+    return (d < -M ? -M : d > M ? M : d) + M;
+}
+
+const char *bad_score(const logoskg_score &s, int heads, int kv_heads);  // read.hip: why a call refuses it, or NULL
+const char *bad_heads(int dtype, int heads, int kv_heads, int dim);
+
+}  // namespace lkg
