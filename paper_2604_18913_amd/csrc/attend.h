@@ -9,6 +9,7 @@ constexpr int kAttThreads = 256;  // four wavefronts
 constexpr int kAttRowsShift = 7;  // a block's rows: 4 x 32
 constexpr int kAttRows = 1 << kAttRowsShift;
 constexpr long long kMostRows = (1ll << 31) - (1 << 16);  // of a batch: places in a document are 32-bit, with room for a tile
+constexpr long long kMostStride = 1 << 23;                // between rows, in elements: a tile's rows within 2^31 bytes
 constexpr int kMostGroup = 128;                           // heads that share a key head
 
 struct AttArgs {
@@ -24,9 +25,10 @@ struct AttArgs {
     // backward
     const void *dout;
     void *dq, *dk, *dv, *dbias;
-    float *delta;      // [num_rows][heads] sum of dout out
-    float *bias_part;  // [blocks of the dq kernel][heads][num_buckets]
+    float *delta;      // [num_rows][heads] sum of dout out, then of p dP
+    float *bias_part;  // [key_blocks][heads][num_buckets]
     float scale;
+    float curve;       // .. of scale (1 - tanh^2) = scale + curve y^2, y = c tanh in units of log 2
     float slope;       // with a cap: 4 scale, of scale (1 - tanh^2) = 4 scale r (1 - r), r = 1 / (2^(z k) + 1)
     long long row_blocks, key_blocks;
 };
@@ -54,27 +56,41 @@ __device__ __forceinline__ AttDoc att_doc(const AttArgs &a, int d) {
     return o;
 }
 
-__device__ const u32x4 kZeroChunk = {0, 0, 0, 0};
+// A window of memory from `base` on: reads behind `bytes` give zeros (and touch nothing).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t window(const void *base, long long bytes) {
+    bytes = bytes < 0 ? 0 : bytes > 0x7ffffff0 ? 0x7ffffff0 : bytes;
+    return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)bytes, 0x00027000);  // raw bytes
+}
+__device__ __forceinline__ u32x4 window_chunk(__amdgpu_buffer_rsrc_t w, unsigned offset) {
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(w, offset, 0, 0));
+}
+constexpr unsigned kNowhere = 0x80000000u;  // behind every window
 
-// Reads rows [r0, r0 + N) of a ragged array's head (row strides in elements) into registers, N x DP values over the block's
-// threads, zeros outside [0, rows) and behind dim.
+// Moves N rows x DP values of a ragged array's head into a tile through registers, spread over the block's threads: rows
+// [r0, r0 + N) of a matrix of `rows` rows with `row_bytes` between them, zeros behind the last row and behind dim.
 template <int N, int DP> struct TileLoad {
-    static constexpr int kChunks = N * DP / 8 / kAttThreads;
+    static constexpr int kChunks = N * DP / 8 / kAttThreads, kStep = kAttThreads / (DP / 8);  // rows between a thread's chunks
+    unsigned from, to;
     u32x4 x[kChunks];
-    __device__ __forceinline__ void load(const void *base, long long row_stride, int r0, int rows, int dim, int tid) {
-#pragma unroll
-        for (int i = 0; i < kChunks; i++) {
-            int at = i * kAttThreads + tid, r = r0 + at / (DP / 8), c = at % (DP / 8);
-            bool in = r < rows && c * 8 < dim;
-            x[i] = in ? *(const u32x4 *)((const char *)base + (r * row_stride + c * 8) * 2) : u32x4{0, 0, 0, 0};
-        }
+    __device__ __forceinline__ void begin(unsigned row_bytes, int dim, int tid) {
+        int r = tid / (DP / 8), c = tid % (DP / 8);
+        from = c * 8 < dim ? r * row_bytes + c * 16 : kNowhere;
+        to = r * (DP * 2) + ((c ^ spread<DP>(r)) << 4);
     }
-    __device__ __forceinline__ void store(char *tile, int tid) const {
+    __device__ __forceinline__ void load(const char *base, unsigned row_bytes, int r0, int rows, int dim) {
+        const __amdgpu_buffer_rsrc_t w = window(base + (long long)r0 * row_bytes, rows > r0 ? (long long)(rows - r0 - 1) * row_bytes + dim * 2 : 0);
 #pragma unroll
-        for (int i = 0; i < kChunks; i++) {
-            int at = i * kAttThreads + tid, r = at / (DP / 8), c = at % (DP / 8);
-            *(u32x4 *)(tile + r * (DP * 2) + ((c ^ spread<DP>(r)) << 4)) = x[i];
-        }
+        for (int i = 0; i < kChunks; i++) x[i] = window_chunk(w, from + i * kStep * row_bytes);
+    }
+    __device__ __forceinline__ void clear(unsigned tile) const {
+        typedef __attribute__((address_space(3))) u32x4 chunk;
+#pragma unroll
+        for (int i = 0; i < kChunks; i++) *(chunk *)(uintptr_t)(tile + to + i * kStep * DP * 2) = u32x4{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ void store(unsigned tile) const {  // (kStep is a multiple of 16 rows, over which the spread repeats)
+        typedef __attribute__((address_space(3))) u32x4 chunk;
+#pragma unroll
+        for (int i = 0; i < kChunks; i++) *(chunk *)(uintptr_t)(tile + to + i * kStep * DP * 2) = x[i];
     }
 };
 

@@ -5,17 +5,24 @@ namespace lkg {
 
 // One block: 128 rows of (document, key head), where a row is a (row of q, head of the group) pair, so that the heads that
 // share a key head share its tiles.  A wavefront holds 32 rows: lane l works for row l % 32 and half of the keys, so a row's
-// maximum and sum are its own registers and one exchange with the other half.  Keys pass in tiles of 64 through two
-// buffers in LDS; S^T = K Q^T, p = 2^(y - m), O^T += V^T P^T with m the running maximum.
-constexpr int kKeys = 64;
+// maximum and sum are its own registers and one exchange with the other half.  Keys pass in tiles of 32 through a ring of
+// four buffers in LDS: S^T = K Q^T, p = 2^(y - m), O^T += V^T P^T with m the running maximum.
+//
+// The vector units bound this: a score costs them about twelve issue slots (a tanh among them), its products four.  So the
+// products of the next tile's scores and of the last tile's values are issued between the exponentials of this one, one
+// matrix instruction a step, and a tile is spared what costs most when nothing special is asked of it: all its keys are visible, all
+// its distances read one bias (text far from the row, which is most of a long document), the scores are in the range of the
+// tanh's polynomial, and the maximum does not move by more than 2^8.  m need not be the true maximum: p stays below 2^8 and
+// is summed in 32 bits.  Other tiles get their y - m first, with m the maximum again.
+constexpr int kKeys = 32;
 
 template <class E, int DP, bool CAP, bool BIAS>
 __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
+    typedef typename Vec8<E>::type Chunk;
     constexpr int kTile = kKeys * DP * 2, kSteps = DP / 16, kOut = DP / 32;
-    char *tiles = lds;                                 // [2][K, V]
-    int *kpos = (int *)(lds + 4 * kTile);              // [2][kKeys]
-    float *table = (float *)(lds + 4 * kTile + 2 * kKeys * 4);
+    int *kpos = (int *)(lds + 8 * kTile);              // [4][kKeys]
+    float *table = (float *)(kpos + 4 * kKeys);        // [group][2 M + 1]
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int head = blockIdx.x % a.kv_heads;
     const long long block = a.row_blocks - 1 - blockIdx.x / a.kv_heads;  // the last rows of a document see most: first
@@ -27,7 +34,8 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
 
     const long long vr = first + wave * 32 + (lane & 31);
     const bool mine = vr < vrows;
-    const int row = mine ? (int)(vr / a.group) : 0, g = mine ? (int)(vr % a.group) : 0;
+    const long long vr_in = mine ? vr : vrows - 1;
+    const int row = (int)(vr_in / a.group), g = (int)(vr_in % a.group);
     const int seen = mine ? doc.seen(row, a.causal) : 0;
     // of the block's first and last row
     const int least = doc.seen((int)(first / a.group), a.causal);
@@ -36,83 +44,163 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
 
     const int h = head * a.group + g;
     const E *qrow = (const E *)a.q + (doc.row0 + row) * a.q_row + (long long)h * a.q_head;
-    typename Vec8<E>::type q[kSteps];
+    Chunk q[kSteps];
 #pragma unroll
     for (int kk = 0; kk < kSteps; kk++) q[kk] = row_chunk<E>(qrow, mine, kk, a.dim, lane);
-    const int q_pos = !mine ? 0 : a.q_pos ? a.q_pos[doc.row0 + row] : row + doc.keys - doc.rows;
     const int M = a.score.max_distance;
     const float *my_table = table + g * (2 * M + 1);
-    if (BIAS) bias_to_lds<E>(table, a.score, head * a.group, a.group, tid, kAttThreads);
+    int q_pos = 0, q_low = 0, q_high = 0;  // of the row, and the wavefront's lowest and highest
+    if (BIAS) {
+        q_pos = a.q_pos ? a.q_pos[doc.row0 + row] : row + doc.keys - doc.rows;
+        q_low = wave_min(q_pos);
+        q_high = wave_max(q_pos);
+        bias_to_lds<E>(table, a.score, head * a.group, a.group, tid, kAttThreads);
+    }
 
     const char *kbase = (const char *)a.k + (doc.key0 * a.k_row + (long long)head * a.k_head) * 2;
     const char *vbase = (const char *)a.v + (doc.key0 * a.v_row + (long long)head * a.v_head) * 2;
-    f32x16 o[kOut];
+    f32x16 o[kOut], s = zero16();
+    Chunk p0 = as8<E>(u32x4{0, 0, 0, 0}), p1 = p0;  // of the last tile
 #pragma unroll
     for (int i = 0; i < kOut; i++) o[i] = zero16();
-    float m = kLowest, l = 0.f;
+    float m = kLowest, l = 0.f, size = 0.f;  // size: the largest product of the tile, without its sign
 
     TileLoad<kKeys, DP> kload, vload;
+    const unsigned k_bytes = (unsigned)a.k_row * 2, v_bytes = (unsigned)a.v_row * 2;
+    kload.begin(k_bytes, a.dim, tid);
+    vload.begin(v_bytes, a.dim, tid);
+    const unsigned tiles = lds_place(lds), my_rows = rows_place<DP>(lane) + tiles, my_columns = columns_place<DP>(lane) + tiles + kTile;
+    auto buffer = [](int t) { return (unsigned)(t & 3) * 2 * kTile; };
     int kp = 0;
     const int tiles_n = (most + kKeys - 1) / kKeys;
     auto fetch = [&](int t) {
-        kload.load(kbase, a.k_row, t * kKeys, doc.keys, a.dim, tid);
-        vload.load(vbase, a.v_row, t * kKeys, doc.keys, a.dim, tid);
-        int j = t * kKeys + tid;
-        if (BIAS && tid < kKeys) kp = a.k_pos && j < doc.keys ? a.k_pos[doc.key0 + j] : j;
-    };
-    if (tiles_n > 0) fetch(0);
-    for (int t = 0; t < tiles_n; t++) {
-        char *kt = tiles + (t & 1) * 2 * kTile, *vt = kt + kTile;
-        int *kpt = kpos + (t & 1) * kKeys;
-        kload.store(kt, tid);
-        vload.store(vt, tid);
-        if (BIAS && tid < kKeys) kpt[tid] = kp;
-        __syncthreads();  // (the buffer's last readers are behind the barrier of the round before)
-        if (t + 1 < tiles_n) fetch(t + 1);
-
-        f32x16 s[2];
-#pragma unroll
-        for (int u = 0; u < 2; u++) {
-            s[u] = zero16();
-#pragma unroll
-            for (int kk = 0; kk < kSteps; kk++) s[u] = mfma(tile_rows<E, DP>(kt, 32 * u, kk, lane), q[kk], s[u]);
+        kload.load(kbase, k_bytes, t * kKeys, doc.keys, a.dim);
+        vload.load(vbase, v_bytes, t * kKeys, doc.keys, a.dim);
+        if (BIAS && tid < kKeys) {
+            int j = t * kKeys + tid;
+            j = j < doc.keys ? j : doc.keys - 1;
+            kp = a.k_pos && doc.keys > 0 ? a.k_pos[doc.key0 + j] : j;
         }
-        const bool edge = (t + 1) * kKeys > least;  // some row does not see all of the tile
-        float top = kLowest;
+    };
+    auto stage = [&](int t) {
+        kload.store(tiles + buffer(t));
+        vload.store(tiles + buffer(t) + kTile);
+        if (BIAS && tid < kKeys) kpos[(t & 3) * kKeys + tid] = kp;
+    };
+    auto scores = [&](int t) {
+        const unsigned kt = my_rows + buffer(t);
+        f32x16 x = zero16();
 #pragma unroll
-        for (int u = 0; u < 2; u++)
+        for (int kk = 0; kk < kSteps; kk++) x = mfma(rows_chunk<E>(kt, kk), q[kk], x);
+        return x;
+    };
+
+    if (tiles_n > 0) {
+        fetch(0);
+        stage(0);
+        if (tiles_n > 1) fetch(1), stage(1);
+        if (tiles_n > 2) fetch(2);
+        vload.clear(tiles + buffer(3) + kTile);  // (round 0 multiplies it with zeros)
+        __syncthreads();
+        s = scores(0);
+#pragma unroll
+        for (int r = 0; r < 16; r++) size = fmaxf(size, __builtin_fabsf(s[r]));
+    }
+    for (int t = 0; t < tiles_n; t++) {
+        if (t + 2 < tiles_n) stage(t + 2);  // (its buffer was read last in round t - 1: values of t - 2)
+        if (t + 3 < tiles_n) fetch(t + 3);
+        bool plain = (t + 1) * kKeys <= least;
+        float b = 0.f;
+        if (BIAS) {  // one bias for all distances of the tile?
+            int pos = kpos[(t & 3) * kKeys + (lane & 31)];
+            int x = distance_place(pos, q_high, M), y = distance_place(pos, q_low, M), x0 = __builtin_amdgcn_readfirstlane(x);
+            plain = plain && !wave_any(x != x0 || y != x0);
+            b = my_table[x0];
+        }
+        plain = plain && !wave_any(size > a.score.most || __builtin_fmaf(size, a.score.slope, b) > m + 8.f);
+        // p = 2^(w + shift), w = z times the polynomial of `near` (CAP) or z near[0]; the other way leaves y - m in z
+        float shift = b - m, near0 = CAP ? a.score.near[0] : a.score.k, near1 = a.score.near[1], near2 = a.score.near[2], near3 = a.score.near[3];
+        float shrink = 1.f;
+        if (!plain) {
+            const bool edge = (t + 1) * kKeys > least;  // some row does not see all of the tile
+            const int *kpt = kpos + (t & 3) * kKeys;
+            float top = kLowest;
 #pragma unroll
             for (int r = 0; r < 16; r++) {
+                const int at = 8 * (r / 4) + 4 * half + r % 4;
                 float y;
-                if (CAP) y = __builtin_fmaf(-2.f * a.score.c, rcp_fast(exp2_fast(s[u][r] * a.score.k) + 1.f), a.score.c);
-                else y = s[u][r] * a.score.k;
-                int at = 32 * u + 8 * (r / 4) + 4 * half + r % 4;
+                if (CAP) y = __builtin_fmaf(-2.f * a.score.c, rcp_fast(exp2_fast(s[r] * a.score.k) + 1.f), a.score.c);
+                else y = s[r] * a.score.k;
                 if (BIAS) y += my_table[distance_place(kpt[at], q_pos, M)];
                 if (edge) y = t * kKeys + at < seen ? y : -INFINITY;
-                s[u][r] = y;
+                s[r] = y;
                 top = fmaxf(top, y);
             }
-        top = halves_max(top);
-        if (wave_any(top > m)) {
-            float up = fmaxf(m, top), shrink = exp2_fast(m - up);
+            top = halves_max(top);
+            const float up = fmaxf(m, top);
+            shrink = exp2_fast(m - up);
             m = up;
             l *= shrink;
 #pragma unroll
+            for (int r = 0; r < 16; r++) {  // (2^-1e15 is 0; its square is finite, where that of the infinity of a hidden key is not)
+                s[r] -= m;
+                if (CAP) s[r] = s[r] < -1e15f ? -1e15f : s[r];
+            }
+            shift = 0.f, near0 = 1.f, near1 = near2 = near3 = 0.f;
+        }
+        const unsigned kt = my_rows + buffer(t + 1), vt = my_columns + buffer(t - 1);
+        constexpr int kAll = 2 * kSteps, kAhead = 3, kEach = 16 / kAll;
+        Chunk piece[4];
+        auto piece_of = [&](int at) {
+            return at < kSteps ? rows_chunk<E>(kt, at) : columns_chunk<E, DP>(vt, ((at - kSteps) & 1) * 16, (at - kSteps) >> 1);
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; i++) piece[i] = piece_of(i);
+        f32x16 next = zero16();
+        float top = 0.f;
+#pragma unroll
+        for (int at = 0; at < kAll; at++) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (at + kAhead < kAll) piece[(at + kAhead) & 3] = piece_of(at + kAhead);
+            if (at < kSteps) next = mfma(piece[at & 3], q[at], next);  // (behind the last tile: of what the buffer holds, not used)
+            else o[(at - kSteps) >> 1] = mfma(piece[at & 3], (at - kSteps) & 1 ? p1 : p0, o[(at - kSteps) >> 1]);
+#pragma unroll
+            for (int e = at * kEach; e < (at + 1) * kEach; e++) {
+                const float z = s[e];
+                float y;
+                if (CAP) {
+                    float zz = z * z;
+                    y = __builtin_fmaf(zz, near3, near2);
+                    y = __builtin_fmaf(zz, y, near1);
+                    y = __builtin_fmaf(zz, y, near0);
+                    y = __builtin_fmaf(z, y, shift);
+                } else y = __builtin_fmaf(z, near0, shift);
+                s[e] = exp2_fast(y);
+                l += s[e];
+            }
+            constexpr int kFrom = kSteps + kSteps / 4, kPer = (16 + kAll - kFrom - 1) / (kAll - kFrom);
+            if (at >= kFrom) {
+#pragma unroll
+                for (int e = (at - kFrom) * kPer; e < (at - kFrom + 1) * kPer && e < 16; e++) top = fmaxf(top, __builtin_fabsf(next[e]));
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (wave_any(shrink != 1.f)) {
+#pragma unroll
             for (int i = 0; i < kOut; i++) o[i] *= shrink;
         }
+        size = top;
+        p0 = rounded8<E, 0>(s);
+        p1 = rounded8<E, 1>(s);
+        s = next;
+        __syncthreads();
+    }
+    if (tiles_n > 0) {
+        const unsigned vt = my_columns + buffer(tiles_n - 1);
 #pragma unroll
-        for (int u = 0; u < 2; u++) {
-#pragma unroll
-            for (int r = 0; r < 16; r++) {
-                s[u][r] = exp2_fast(s[u][r] - m);
-                l += s[u][r];
-            }
-            typename Vec8<E>::type p0 = rounded8<E, 0>(s[u]), p1 = rounded8<E, 1>(s[u]);
-#pragma unroll
-            for (int i = 0; i < kOut; i++) {
-                o[i] = mfma(tile_columns<E, DP>(vt, 32 * u, i, lane), p0, o[i]);
-                o[i] = mfma(tile_columns<E, DP>(vt, 32 * u + 16, i, lane), p1, o[i]);
-            }
+        for (int i = 0; i < kOut; i++) {
+            o[i] = mfma(columns_chunk<E, DP>(vt, 0, i), p0, o[i]);
+            o[i] = mfma(columns_chunk<E, DP>(vt, 16, i), p1, o[i]);
         }
     }
     l = halves_sum(l);
@@ -164,6 +252,7 @@ logoskg_status attend_args(const logoskg_attention *a, AttArgs *o, const char *c
     if (!why && a->num_docs > 0 && (!a->q_off || !a->k_off)) why = "offsets are NULL";
     if (!why && a->num_rows && (!a->q || !a->out || !a->lse)) why = "q, out or lse is NULL";
     if (!why && a->num_keys && (!a->k || !a->v)) why = "k or v is NULL";
+    if (!why && (a->k_row < 0 || a->v_row < 0 || a->k_row >= kMostStride || a->v_row >= kMostStride || a->q_row >= kMostStride)) why = "a row stride is negative or too large";
     if (!why && (odd_place(a->q, a->q_row, a->q_head) || odd_place(a->k, a->k_row, a->k_head) || odd_place(a->v, a->v_row, a->v_head) || odd_place(a->out, 0, 0)))
         why = "an array is not 16-byte aligned, or a stride no multiple of 8";
     if (why) { set_error("%s: %s", call, why); return LOGOSKG_EINVAL; }
@@ -176,14 +265,16 @@ logoskg_status attend_args(const logoskg_attention *a, AttArgs *o, const char *c
     o->score = score_args(a->score);
     o->out = a->out; o->lse = a->lse;
     o->row_blocks = (a->num_rows * o->group >> kAttRowsShift) + a->num_docs;
+    o->key_blocks = (a->num_keys >> kAttRowsShift) + a->num_docs;
     o->scale = a->score.scale;
+    o->curve = o->score.c > 0 ? -a->score.scale / (o->score.c * o->score.c) : 0.f;
     o->slope = 4.f * a->score.scale;
     if (o->row_blocks * a->kv_heads >= (1ll << 31)) { set_error("%s: too many rows", call); return LOGOSKG_EINVAL; }
     return LOGOSKG_OK;
 }
 
 template <class E, int DP, bool CAP, bool BIAS> static logoskg_status launch_attend(const AttArgs &a, hipStream_t st) {
-    size_t bytes = 4 * kKeys * DP * 2 + 2 * kKeys * 4 + (BIAS ? (size_t)a.group * (2 * a.score.max_distance + 1) * 4 : 0);
+    size_t bytes = 8 * kKeys * DP * 2 + 4 * kKeys * 4 + (BIAS ? (size_t)a.group * (2 * a.score.max_distance + 1) * 4 : 0);
     LKG_TRY(allow_lds(k_attend<E, DP, CAP, BIAS>, bytes));
     k_attend<E, DP, CAP, BIAS><<<dim3((unsigned)(a.row_blocks * a.kv_heads)), kAttThreads, bytes, st>>>(a);
     LKG_HIP(hipGetLastError());

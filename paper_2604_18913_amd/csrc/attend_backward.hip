@@ -1,10 +1,17 @@
 // Gradients of the attention of a ragged batch (logoskg_attend_backward).
 //
-// With p = 2^(y - lse), dP = dO V^T and delta = sum of dO O of a row (= sum of p dP), the gradient of the score y is
+// With p = 2^(y - lse), dP = dO V^T and delta = sum of p dP of a row (= dO . O), the gradient of the score y is
 // dy = p (dP - delta), that of the product z: dz = dy scale (1 - tanh^2); dV = p^T dO, dK = dz^T Q, dQ = dz K, and a
-// bucket's bias gets the sum of its dy.  Two kernels make p and dP again, one that keeps keys in registers and passes over
-// the rows that see them (dK, dV), one that keeps rows and passes over their keys (dQ, biases): seven products for five, and
+// bucket's bias gets the sum of its dy.  Two kernels make p and dP again: first one that keeps rows and passes over their
+// keys (dQ), then one that keeps keys and passes over the rows that see them (dK, dV, biases): seven products for five, and
 // in return no sum depends on the order in which blocks arrive, and none is kept in memory in between.
+//
+// O comes in 16 bits, and dO . O carries its rounding: the first kernel adds up a row's dy, which is what delta lacks, and
+// leaves delta with it to the second (a bucket's sum of many dy would show it most).
+//
+// Both kernels work as the forward does: products of the next and of the last tile between the elements of this one, and
+// tiles that ask for nothing special (all visible, one bias, scores in the range of the tanh's polynomial) are spared the
+// rest.  A special tile's elements are made beforehand in a form that the common steps leave as they are.
 #include "attend.h"
 
 namespace lkg {
@@ -26,50 +33,301 @@ template <class E> __global__ __launch_bounds__(256) void k_att_delta(AttArgs a)
     if (in && c == 0) a.delta[at] = sum;
 }
 
-// ---------------------------------------------------------------- dK, dV
-// One block: 128 keys of (document, key head), 32 per wavefront, key = lane, K and V in registers as the B of S = Q K^T and
-// dP = dO V^T.  Rows (all heads of the group) pass in tiles of 64 through LDS, where they are read by rows for these two
-// products and by columns for dV^T += dO^T p and dK^T += Q^T dz.
-constexpr int kGradRows = 64;
-
-struct RowInfo {  // of a row in LDS
-    float lse, delta;  // lse in units of log 2, +infinite for rows that see nothing: p = 0
-    int seen, pos;
+// What an element's steps take, from its products z and dP: w = z times the polynomial (or z near0), p = 2^(w + fma(lse, lse_share,
+// b)), dy = p (dP - delta_share delta), dz = dy (curve w^2 + slope).  Special tiles come with w + shift in z and with
+// (dP - delta) slope in dP.
+struct Steps {
+    float near0, near1, near2, near3, b, lse_share, delta_share, curve, slope;
 };
+template <bool CAP> __device__ __forceinline__ Steps plain_steps(const AttArgs &a, float b) {
+    Steps x;
+    x.near0 = CAP ? a.score.near[0] : a.score.k, x.near1 = a.score.near[1], x.near2 = a.score.near[2], x.near3 = a.score.near[3];
+    x.b = b, x.lse_share = -1.f, x.delta_share = 1.f, x.curve = CAP ? a.curve : 0.f, x.slope = a.scale;
+    return x;
+}
+__device__ __forceinline__ Steps special_steps() { return Steps{1.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 1.f}; }
 
+template <bool CAP> __device__ __forceinline__ float element_w(const Steps &x, float z) {
+    if (!CAP) return z;
+    const float zz = z * z;
+    float w = __builtin_fmaf(zz, x.near3, x.near2);
+    w = __builtin_fmaf(zz, w, x.near1);
+    w = __builtin_fmaf(zz, w, x.near0);
+    return z * w;
+}
+template <bool CAP> __device__ __forceinline__ float element_p(const Steps &x, float w, float lse) {
+    const float shift = __builtin_fmaf(lse, x.lse_share, x.b);
+    return exp2_fast(CAP ? w + shift : __builtin_fmaf(w, x.near0, shift));
+}
+template <bool CAP> __device__ __forceinline__ float element_dy(const Steps &x, float p, float dp, float delta) {
+    return p * __builtin_fmaf(delta, -x.delta_share, dp);
+}
+template <bool CAP> __device__ __forceinline__ float element_dz(const Steps &x, float dy, float w) {
+    return dy * (CAP ? __builtin_fmaf(w * w, x.curve, x.slope) : x.slope);
+}
+
+// A special element: y and its slope from the product, by the exact tanh
+template <bool CAP> __device__ __forceinline__ void exact_score(const AttArgs &a, float z, float &y, float &slope) {
+    if (CAP) {
+        const float w = rcp_fast(exp2_fast(z * a.score.k) + 1.f);
+        y = __builtin_fmaf(-2.f * a.score.c, w, a.score.c);
+        slope = a.slope * (w * (1.f - w));
+    } else {
+        y = z * a.score.k;
+        slope = a.scale;
+    }
+}
+constexpr float kHidden = -1e15f;      // 2^this is 0, and its square finite
+constexpr float kHiddenLse = 1e30f;    // of a row that sees nothing: p = 0
+
+// ---------------------------------------------------------------- dQ
+// One block: 128 rows as in the forward, keys in tiles of 32 through a ring of four buffers.
+constexpr int kGradTile = 32;
+
+template <class E, int DP, bool CAP, bool BIAS>
+__global__ __launch_bounds__(kAttThreads, DP == 128 ? 1 : 2) void k_att_dq(AttArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    typedef typename Vec8<E>::type Chunk;
+    constexpr int kTile = kGradTile * DP * 2, kSteps = DP / 16, kOut = DP / 32;
+    int *kpos = (int *)(lds + 8 * kTile);       // [4][kGradTile]
+    float *table = (float *)(kpos + 4 * kGradTile);
+    const int M = a.score.max_distance, G = a.group;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    const int head = blockIdx.x % a.kv_heads;
+    const long long block = a.row_blocks - 1 - blockIdx.x / a.kv_heads;
+    const int d = document_of(a.q_off, a.num_docs, a.num_rows, G, kAttRowsShift, block, lane);
+    const AttDoc doc = att_doc(a, d);
+    const long long first = (block - first_block(a.q_off, d, a.num_rows, G, kAttRowsShift)) << kAttRowsShift;
+    const long long vrows = (long long)doc.rows * G;
+    if (first >= vrows || first < 0) return;
+
+    const long long vr = first + wave * 32 + (lane & 31);
+    const bool mine = vr < vrows;
+    const long long vr_in = mine ? vr : vrows - 1;
+    const int row = (int)(vr_in / G), g = (int)(vr_in % G), h = head * G + g;
+    const int seen = mine ? doc.seen(row, a.causal) : 0;
+    const int least = doc.seen((int)(first / G), a.causal);
+    const long long last_v = first + kAttRows < vrows ? first + kAttRows - 1 : vrows - 1;
+    const int most = doc.seen((int)(last_v / G), a.causal);
+    const long long place = (doc.row0 + row) * a.heads + h;
+    const E *qrow = (const E *)a.q + (doc.row0 + row) * a.q_row + (long long)h * a.q_head;
+    const E *orow = (const E *)a.dout + place * a.dim;
+    Chunk q[kSteps], o[kSteps];
+#pragma unroll
+    for (int kk = 0; kk < kSteps; kk++) {
+        q[kk] = row_chunk<E>(qrow, mine, kk, a.dim, lane);
+        o[kk] = row_chunk<E>(orow, mine, kk, a.dim, lane);
+    }
+    float lse = mine ? a.lse[place] : -INFINITY;
+    lse = lse == -INFINITY ? kHiddenLse : lse * kLog2e;
+    const float delta = mine ? a.delta[place] : 0.f;
+    const float *my_table = table + g * (2 * M + 1);
+    int q_pos = 0, q_low = 0, q_high = 0;
+    if (BIAS) {
+        q_pos = a.q_pos ? a.q_pos[doc.row0 + row] : row + doc.keys - doc.rows;
+        q_low = wave_min(q_pos);
+        q_high = wave_max(q_pos);
+        bias_to_lds<E>(table, a.score, head * G, G, tid, kAttThreads);
+    }
+    const char *kbase = (const char *)a.k + (doc.key0 * a.k_row + (long long)head * a.k_head) * 2;
+    const char *vbase = (const char *)a.v + (doc.key0 * a.v_row + (long long)head * a.v_head) * 2;
+    f32x16 dq[kOut], s = zero16(), dp = zero16();
+#pragma unroll
+    for (int i = 0; i < kOut; i++) dq[i] = zero16();
+    Chunk z0 = as8<E>(u32x4{0, 0, 0, 0}), z1 = z0;
+    float size = 0.f, lacks = 0.f;
+
+    TileLoad<kGradTile, DP> kload, vload;
+    const unsigned k_bytes = (unsigned)a.k_row * 2, v_bytes = (unsigned)a.v_row * 2;
+    kload.begin(k_bytes, a.dim, tid);
+    vload.begin(v_bytes, a.dim, tid);
+    const unsigned tiles = lds_place(lds), my_rows = rows_place<DP>(lane) + tiles, my_columns = columns_place<DP>(lane) + tiles;
+    auto buffer = [](int t) { return (unsigned)(t & 3) * 2 * kTile; };
+    int kp = 0;
+    auto fetch = [&](int t) {
+        kload.load(kbase, k_bytes, t * kGradTile, doc.keys, a.dim);
+        vload.load(vbase, v_bytes, t * kGradTile, doc.keys, a.dim);
+        if (BIAS && tid < kGradTile) {
+            int j = t * kGradTile + tid;
+            j = j < doc.keys ? j : doc.keys - 1;
+            kp = a.k_pos && doc.keys > 0 ? a.k_pos[doc.key0 + j] : j;
+        }
+    };
+    auto stage = [&](int t) {
+        kload.store(tiles + buffer(t));
+        vload.store(tiles + buffer(t) + kTile);
+        if (BIAS && tid < kGradTile) kpos[(t & 3) * kGradTile + tid] = kp;
+    };
+    const int tiles_n = (most + kGradTile - 1) / kGradTile;
+    if (tiles_n > 0) {
+        fetch(0);
+        stage(0);
+        if (tiles_n > 1) fetch(1), stage(1);
+        if (tiles_n > 2) fetch(2);
+        kload.clear(tiles + buffer(3));  // (round 0 multiplies it with zeros)
+        __syncthreads();
+#pragma unroll
+        for (int kk = 0; kk < kSteps; kk++) {
+            s = mfma(rows_chunk<E>(my_rows, kk), q[kk], s);
+            dp = mfma(rows_chunk<E>(my_rows + kTile, kk), o[kk], dp);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; r++) size = fmaxf(size, __builtin_fabsf(s[r]));
+    }
+    for (int t = 0; t < tiles_n; t++) {
+        if (t + 2 < tiles_n) stage(t + 2);
+        if (t + 3 < tiles_n) fetch(t + 3);
+        bool plain = (t + 1) * kGradTile <= least && !wave_any(size > a.score.most);
+        float b = 0.f;
+        if (BIAS) {
+            int pos = kpos[(t & 3) * kGradTile + (lane & 31)];
+            int x = distance_place(pos, q_high, M), y = distance_place(pos, q_low, M), x0 = __builtin_amdgcn_readfirstlane(x);
+            plain = plain && !wave_any(x != x0 || y != x0);
+            b = my_table[x0];
+        }
+        Steps x = plain_steps<CAP>(a, b);
+        if (!plain) {
+            const bool edge = (t + 1) * kGradTile > least;
+            const int *kpt = kpos + (t & 3) * kGradTile;
+#pragma unroll
+            for (int r = 0; r < 16; r++) {
+                const int at = 8 * (r / 4) + 4 * half + r % 4;
+                float y, slope;
+                exact_score<CAP>(a, s[r], y, slope);
+                if (BIAS) y += my_table[distance_place(kpt[at], q_pos, M)];
+                y -= lse;
+                float away = dp[r] - delta;
+                if (edge && t * kGradTile + at >= seen) y = kHidden, away = 0.f;
+                lacks = __builtin_fmaf(exp2_fast(y), away, lacks);
+                dp[r] = away * slope;
+                s[r] = y < kHidden ? kHidden : y;
+            }
+            x = special_steps();
+        }
+        const unsigned kt = my_rows + buffer(t + 1), ct = my_columns + buffer(t - 1);
+        constexpr int kAll = 3 * kSteps, kAhead = 3;
+        Chunk piece[4];
+        auto piece_of = [&](int at) {
+            return at < kSteps ? rows_chunk<E>(kt, at) : at < 2 * kSteps ? rows_chunk<E>(kt + kTile, at - kSteps)
+                                                                         : columns_chunk<E, DP>(ct, ((at - 2 * kSteps) & 1) * 16, (at - 2 * kSteps) >> 1);
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; i++) piece[i] = piece_of(i);
+        f32x16 next_s = zero16(), next_dp = zero16();
+        float top = 0.f, sum = 0.f;
+#pragma unroll
+        for (int at = 0; at < kAll; at++) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (at + kAhead < kAll) piece[(at + kAhead) & 3] = piece_of(at + kAhead);
+            if (at < kSteps) next_s = mfma(piece[at & 3], q[at], next_s);
+            else if (at < 2 * kSteps) next_dp = mfma(piece[at & 3], o[at - kSteps], next_dp);
+            else dq[(at - 2 * kSteps) >> 1] = mfma(piece[at & 3], (at & 1) ? z1 : z0, dq[(at - 2 * kSteps) >> 1]);
+#pragma unroll
+            for (int e = 16 * at / kAll; e < 16 * (at + 1) / kAll; e++) {
+                const float w = element_w<CAP>(x, s[e]), p = element_p<CAP>(x, w, lse), dy = element_dy<CAP>(x, p, dp[e], delta);
+                sum += dy;
+                dp[e] = element_dz<CAP>(x, dy, w);
+            }
+            constexpr int kFrom = 2 * kSteps, kPer = 16 / kSteps;
+            if (at >= kFrom) {
+#pragma unroll
+                for (int e = (at - kFrom) * kPer; e < (at - kFrom + 1) * kPer; e++) top = fmaxf(top, __builtin_fabsf(next_s[e]));
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (plain) lacks += sum;
+        size = top;
+        z0 = rounded8<E, 0>(dp);
+        z1 = rounded8<E, 1>(dp);
+        s = next_s;
+        dp = next_dp;
+        __syncthreads();
+    }
+    if (tiles_n > 0) {
+        const unsigned ct = my_columns + buffer(tiles_n - 1);
+#pragma unroll
+        for (int i = 0; i < kOut; i++) {
+            dq[i] = mfma(columns_chunk<E, DP>(ct, 0, i), z0, dq[i]);
+            dq[i] = mfma(columns_chunk<E, DP>(ct, 16, i), z1, dq[i]);
+        }
+    }
+    lacks = halves_sum(lacks);
+    if (!mine) return;
+    if (half == 0) a.delta[place] = delta + lacks;
+    E *out = (E *)a.dq + place * a.dim;
+#pragma unroll
+    for (int i = 0; i < kOut; i++)
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+            int c = 32 * i + 8 * r + 4 * half;
+            if (c >= a.dim) continue;
+            typename Vec4<E>::type x;
+#pragma unroll
+            for (int e = 0; e < 4; e++) x[e] = (E)dq[i][4 * r + e];
+            *(typename Vec4<E>::type *)(out + c) = x;
+        }
+}
+
+// ---------------------------------------------------------------- dK, dV, biases
+// One block: 128 keys of (document, key head), 32 per wavefront, key = lane, K and V in registers as the B of S = Q K^T and
+// dP = dO V^T.  The rows that see them pass in tiles of 32 of one head, one head of the group after the other, through a
+// ring of four buffers in LDS, where they are read by rows for these two products and by columns for dV^T += dO^T p and
+// dK^T += Q^T dz.  A lane adds its dy to its own column of [buckets][64] in LDS (no two lanes share an address, so the sums
+// have an order), a tile of one bias all at once; a head's columns are added up when its rows are through.
 template <class E, int DP, bool CAP, bool BIAS>
 __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    constexpr int kTile = kGradRows * DP * 2, kSteps = DP / 16, kOut = DP / 32, kChunks = kGradRows * DP / 8 / kAttThreads;
-    char *tiles = lds;  // [2][Q, dO]
-    RowInfo *info = (RowInfo *)(lds + 4 * kTile);          // [2][kGradRows]
-    int *row_table = (int *)(info + 2 * kGradRows);        // [2][kGradRows] where the row's head begins in the table
-    float *table = (float *)(row_table + 2 * kGradRows);
+    typedef typename Vec8<E>::type Chunk;
+    constexpr int kTile = kGradTile * DP * 2, kSteps = DP / 16, kOut = DP / 32;
+    const int G = a.group, M = a.score.max_distance, places = 2 * M + 1, nb = a.score.num_buckets;
+    float *lses = (float *)(lds + 8 * kTile), *deltas = lses + 4 * kGradTile;  // [4][kGradTile] of the rows
+    int *qpos = (int *)(deltas + 4 * kGradTile);
+    float *sums = (float *)(qpos + 4 * kGradTile);           // [4 wavefronts][nb][64]
+    int *column = (int *)(sums + (BIAS ? 4 * nb * 64 : 0));  // [places] where a distance's bucket begins
+    float *table = (float *)(column + (BIAS ? places : 0));  // [group][places]
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int head = blockIdx.x % a.kv_heads;
-    const long long block = blockIdx.x / a.kv_heads;
+    const long long block = blockIdx.x / a.kv_heads;  // the first keys of a document are seen by most rows: first
     const int d = document_of(a.k_off, a.num_docs, a.num_keys, 1, kAttRowsShift, block, lane);
     const AttDoc doc = att_doc(a, d);
     const long long kb = (block - first_block(a.k_off, d, a.num_keys, 1, kAttRowsShift)) << kAttRowsShift;
-    if (kb >= doc.keys || kb < 0) return;
+    float *part = BIAS ? a.bias_part + (block * a.heads + head * G) * nb : nullptr;
+    if (kb >= doc.keys || kb < 0) {
+        if (BIAS)
+            for (int i = tid; i < G * nb; i += kAttThreads) part[i] = 0.f;
+        return;
+    }
 
-    const int G = a.group, places = 2 * a.score.max_distance + 1, magic = (65536 + G - 1) / G;
     const int key = (int)kb + wave * 32 + (lane & 31);
     const bool mine = key < doc.keys;
     const E *krow = (const E *)a.k + (doc.key0 + key) * a.k_row + (long long)head * a.k_head;
     const E *vrow = (const E *)a.v + (doc.key0 + key) * a.v_row + (long long)head * a.v_head;
-    typename Vec8<E>::type k[kSteps], v[kSteps];
+    Chunk k[kSteps], v[kSteps];
 #pragma unroll
     for (int kk = 0; kk < kSteps; kk++) {
         k[kk] = row_chunk<E>(krow, mine, kk, a.dim, lane);
         v[kk] = row_chunk<E>(vrow, mine, kk, a.dim, lane);
     }
-    const int k_pos = !mine ? 0 : a.k_pos ? a.k_pos[doc.key0 + key] : key;
-    if (BIAS) bias_to_lds<E>(table, a.score, head * G, G, tid, kAttThreads);
+    int k_pos = 0, k_low = 0, k_high = 0;
+    float *my_sums = sums + wave * nb * 64 + lane;
+    if (BIAS) {
+        const int in = mine ? key : doc.keys - 1;
+        k_pos = a.k_pos ? a.k_pos[doc.key0 + in] : in;
+        k_low = wave_min(k_pos);
+        k_high = wave_max(k_pos);
+        bias_to_lds<E>(table, a.score, head * G, G, tid, kAttThreads);
+        for (int i = tid; i < places; i += kAttThreads) {
+            int b = a.score.buckets[i];
+            column[i] = (b < 0 ? 0 : b >= nb ? nb - 1 : b) * 64;
+        }
+        for (int i = tid; i < 4 * nb * 64; i += kAttThreads) sums[i] = 0.f;
+    }
 
-    f32x16 dk[kOut], dv[kOut];
+    f32x16 dk[kOut], dv[kOut], s = zero16(), dp = zero16();
 #pragma unroll
     for (int i = 0; i < kOut; i++) dk[i] = zero16(), dv[i] = zero16();
+    Chunk p0 = as8<E>(u32x4{0, 0, 0, 0}), p1 = p0, z0 = p0, z1 = p0;
+    float size = 0.f;
 
     const int kend = doc.keys < kb + kAttRows ? doc.keys : (int)kb + kAttRows;
     int from = 0;  // first row that sees one of the keys
@@ -77,91 +335,190 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
         long long i = kb - ((long long)doc.keys - doc.rows);
         from = i < 0 ? 0 : i > doc.rows ? doc.rows : (int)i;
     }
-    const long long vrows = (long long)doc.rows * G;
-    const long long v0 = (long long)from * G;
-    const int tiles_n = (int)((vrows - v0 + kGradRows - 1) / kGradRows);
+    const int per = (doc.rows - from + kGradTile - 1) / kGradTile, tiles_n = per * G;  // tiles of a head, of all
 
-    u32x4 qx[kChunks], ox[kChunks];
-    RowInfo my_info;
-    int my_table = 0;
-    auto fetch = [&](int t) {
-        const long long base = v0 + (long long)t * kGradRows;
-        const int i0 = (int)(base / G), g0 = (int)(base - (long long)i0 * G);
-#pragma unroll
-        for (int i = 0; i < kChunks; i++) {
-            int at = i * kAttThreads + tid, r = at / (DP / 8), c = (at % (DP / 8)) * 8;
-            int up = ((g0 + r) * magic) >> 16, row = i0 + up, g = g0 + r - up * G;
-            bool in = row < doc.rows && c < a.dim;
-            const E *qp = (const E *)a.q + (doc.row0 + row) * a.q_row + (long long)(head * G + g) * a.q_head + c;
-            const E *op = (const E *)a.dout + ((doc.row0 + row) * a.heads + head * G + g) * a.dim + c;
-            qx[i] = in ? *(const u32x4 *)qp : u32x4{0, 0, 0, 0};
-            ox[i] = in ? *(const u32x4 *)op : u32x4{0, 0, 0, 0};
+    TileLoad<kGradTile, DP> qload, oload;
+    const unsigned q_bytes = (unsigned)a.q_row * 2, o_bytes = (unsigned)a.heads * a.dim * 2;
+    qload.begin(q_bytes, a.dim, tid);
+    oload.begin(o_bytes, a.dim, tid);
+    const unsigned tiles = lds_place(lds), my_rows = rows_place<DP>(lane) + tiles, my_columns = columns_place<DP>(lane) + tiles;
+    auto buffer = [](int t) { return (unsigned)(t & 3) * 2 * kTile; };
+    float my_lse = 0.f, my_delta = 0.f;
+    int my_pos = 0, fetch_g = 0, fetch_at = 0;
+    auto fetch = [&]() {  // the next tile
+        const int h = head * G + fetch_g, r0 = from + fetch_at * kGradTile;
+        qload.load((const char *)a.q + (doc.row0 * a.q_row + (long long)h * a.q_head) * 2, q_bytes, r0, doc.rows, a.dim);
+        oload.load((const char *)a.dout + (doc.row0 * a.heads + h) * a.dim * 2, o_bytes, r0, doc.rows, a.dim);
+        if (tid < kGradTile) {
+            const int row = r0 + tid;
+            const bool in = row < doc.rows;
+            const long long at = in ? (doc.row0 + row) * a.heads + h : 0;
+            const float lse = in ? a.lse[at] : -INFINITY;
+            my_lse = lse == -INFINITY ? kHiddenLse : lse * kLog2e;
+            my_delta = in ? a.delta[at] : 0.f;
+            if (BIAS) {
+                const int near = in ? row : doc.rows - 1;
+                my_pos = a.q_pos ? a.q_pos[doc.row0 + near] : near + doc.keys - doc.rows;
+            }
         }
-        if (tid < kGradRows) {
-            int up = ((g0 + tid) * magic) >> 16, row = i0 + up, g = g0 + tid - up * G;
-            bool in = row < doc.rows;
-            long long at = in ? (doc.row0 + row) * a.heads + head * G + g : 0;
-            float lse = in ? a.lse[at] : -INFINITY;
-            my_info.lse = lse == -INFINITY ? INFINITY : lse * kLog2e;
-            my_info.delta = in ? a.delta[at] : 0.f;
-            my_info.seen = in ? doc.seen(row, a.causal) : 0;
-            my_info.pos = !in ? 0 : a.q_pos ? a.q_pos[doc.row0 + row] : row + doc.keys - doc.rows;
-            my_table = g * places;
+        if (++fetch_at == per) fetch_at = 0, fetch_g++;
+    };
+    auto stage = [&](int t) {
+        qload.store(tiles + buffer(t));
+        oload.store(tiles + buffer(t) + kTile);
+        if (tid < kGradTile) {
+            const int at = (t & 3) * kGradTile + tid;
+            lses[at] = my_lse;
+            deltas[at] = my_delta;
+            if (BIAS) qpos[at] = my_pos;
         }
     };
-    if (tiles_n > 0) fetch(0);
-    for (int t = 0; t < tiles_n; t++) {
-        char *qt = tiles + (t & 1) * 2 * kTile, *ot = qt + kTile;
-        const RowInfo *inf = info + (t & 1) * kGradRows;
-        const int *rt = row_table + (t & 1) * kGradRows;
-#pragma unroll
-        for (int i = 0; i < kChunks; i++) {
-            int at = i * kAttThreads + tid, r = at / (DP / 8), c = at % (DP / 8), place = r * (DP * 2) + ((c ^ spread<DP>(r)) << 4);
-            *(u32x4 *)(qt + place) = qx[i];
-            *(u32x4 *)(ot + place) = ox[i];
-        }
-        if (tid < kGradRows) {
-            info[(t & 1) * kGradRows + tid] = my_info;
-            row_table[(t & 1) * kGradRows + tid] = my_table;
+    // the columns of a head that is through: a bucket's 256 sums by 256 / nb threads, their parts by one
+    auto finish = [&](int g) {
+        __syncthreads();
+        int strands = kAttThreads / nb;
+        strands = strands > 16 ? 16 : strands;
+        const int b = tid % nb, st = tid / nb, n = 256 / strands;
+        float sum = 0.f;
+        if (st < strands)
+            for (int i = 0; i < n; i++) {  // (rotated by the bucket, so that neighbouring threads read other banks)
+                const int c = st * n + ((i + b) % n), w = c >> 6;
+                sum += sums[(w * nb + b) * 64 + (c & 63)];
+            }
+        if (st == strands - 1)
+            for (int c = strands * n; c < 256; c++) sum += sums[((c >> 6) * nb + b) * 64 + (c & 63)];
+        __syncthreads();
+        for (int i = tid; i < 4 * nb * 64; i += kAttThreads) sums[i] = 0.f;
+        __syncthreads();
+        if (st < strands) sums[tid] = sum;
+        __syncthreads();
+        if (tid < nb) {
+            for (int i = 1; i < strands; i++) sum += sums[i * nb + tid];
+            part[g * nb + tid] = sum;
         }
         __syncthreads();
-        if (t + 1 < tiles_n) fetch(t + 1);
-        const bool edge = doc.seen((int)((v0 + (long long)t * kGradRows) / G), a.causal) < kend;
-
+        if (st < strands) sums[tid] = 0.f;
+        __syncthreads();
+    };
+    if (tiles_n > 0) {
+        fetch();
+        stage(0);
+        if (tiles_n > 1) fetch(), stage(1);
+        if (tiles_n > 2) fetch();
+        qload.clear(tiles + buffer(3));  // (round 0 multiplies them with zeros)
+        oload.clear(tiles + buffer(3) + kTile);
+        __syncthreads();
 #pragma unroll
-        for (int u = 0; u < 2; u++) {
-            f32x16 s = zero16(), dp = zero16();
+        for (int kk = 0; kk < kSteps; kk++) {
+            s = mfma(rows_chunk<E>(my_rows, kk), k[kk], s);
+            dp = mfma(rows_chunk<E>(my_rows + kTile, kk), v[kk], dp);
+        }
 #pragma unroll
-            for (int kk = 0; kk < kSteps; kk++) {
-                s = mfma(tile_rows<E, DP>(qt, 32 * u, kk, lane), k[kk], s);
-                dp = mfma(tile_rows<E, DP>(ot, 32 * u, kk, lane), v[kk], dp);
-            }
+        for (int r = 0; r < 16; r++) size = fmaxf(size, __builtin_fabsf(s[r]));
+    }
+    int g = 0, at_tile = 0;  // of the tile in work
+    for (int t = 0; t < tiles_n; t++) {
+        if (t + 2 < tiles_n) stage(t + 2);
+        if (t + 3 < tiles_n) fetch();
+        const int r0 = from + at_tile * kGradTile;
+        const bool edge = doc.seen(r0, a.causal) < kend;
+        const float *lse = lses + (t & 3) * kGradTile, *delta = deltas + (t & 3) * kGradTile;
+        const int *pos = qpos + (t & 3) * kGradTile;
+        bool plain = !edge && !wave_any(size > a.score.most);
+        float b = 0.f;
+        int x0 = 0;
+        const float *my_table = table + g * places;
+        if (BIAS) {
+            const int p = pos[lane & 31], x = distance_place(k_low, p, M), y = distance_place(k_high, p, M);
+            x0 = __builtin_amdgcn_readfirstlane(x);
+            plain = plain && !wave_any(x != x0 || y != x0);
+            b = my_table[x0];
+        }
+        Steps x = plain_steps<CAP>(a, b);
+        if (!plain) {
 #pragma unroll
             for (int r = 0; r < 16; r++) {
-                const int at = 32 * u + 8 * (r / 4) + 4 * half + r % 4;
-                const RowInfo ri = inf[at];
-                float y, w = 0.f;
-                if (CAP) {
-                    w = rcp_fast(exp2_fast(s[r] * a.score.k) + 1.f);
-                    y = __builtin_fmaf(-2.f * a.score.c, w, a.score.c);
-                } else y = s[r] * a.score.k;
-                if (BIAS) y += table[rt[at] + distance_place(k_pos, ri.pos, a.score.max_distance)];
-                float p = exp2_fast(y - ri.lse);
-                if (edge) p = key < ri.seen ? p : 0.f;
-                float dy = p * (dp[r] - ri.delta);
-                if (edge) dy = key < ri.seen ? dy : 0.f;
-                s[r] = p;
-                dp[r] = CAP ? dy * a.slope * (w * (1.f - w)) : dy * a.scale;
+                const int at = 8 * (r / 4) + 4 * half + r % 4;
+                float y, slope;
+                exact_score<CAP>(a, s[r], y, slope);
+                int apart = 0;
+                if (BIAS) {
+                    apart = distance_place(k_pos, pos[at], M);
+                    y += my_table[apart];
+                }
+                y -= lse[at];
+                float away = dp[r] - delta[at];
+                if (edge && key >= doc.seen(r0 + at, a.causal)) y = kHidden, away = 0.f;
+                if (BIAS && mine) __hip_atomic_fetch_add(my_sums + column[apart], exp2_fast(y) * away, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                dp[r] = away * slope;
+                s[r] = y < kHidden ? kHidden : y;
             }
-            typename Vec8<E>::type p0 = rounded8<E, 0>(s), p1 = rounded8<E, 1>(s), z0 = rounded8<E, 0>(dp), z1 = rounded8<E, 1>(dp);
+            x = special_steps();
+        }
+        const unsigned rt = my_rows + buffer(t + 1), ct = my_columns + buffer(t - 1);
+        constexpr int kAll = 4 * kSteps, kAhead = 3;
+        Chunk piece[4];
+        auto piece_of = [&](int at) {
+            return at < kSteps ? rows_chunk<E>(rt, at) : at < 2 * kSteps ? rows_chunk<E>(rt + kTile, at - kSteps)
+                 : at < 3 * kSteps ? columns_chunk<E, DP>(ct + kTile, ((at - 2 * kSteps) & 1) * 16, (at - 2 * kSteps) >> 1)
+                                   : columns_chunk<E, DP>(ct, ((at - 3 * kSteps) & 1) * 16, (at - 3 * kSteps) >> 1);
+        };
 #pragma unroll
-            for (int i = 0; i < kOut; i++) {
-                dv[i] = mfma(tile_columns<E, DP>(ot, 32 * u, i, lane), p0, dv[i]);
-                dv[i] = mfma(tile_columns<E, DP>(ot, 32 * u + 16, i, lane), p1, dv[i]);
-                dk[i] = mfma(tile_columns<E, DP>(qt, 32 * u, i, lane), z0, dk[i]);
-                dk[i] = mfma(tile_columns<E, DP>(qt, 32 * u + 16, i, lane), z1, dk[i]);
+        for (int i = 0; i < kAhead; i++) piece[i] = piece_of(i);
+        f32x16 next_s = zero16(), next_dp = zero16();
+        float top = 0.f, sum = 0.f;
+        f32x4 l4 = {0, 0, 0, 0}, d4 = {0, 0, 0, 0};
+#pragma unroll
+        for (int at = 0; at < kAll; at++) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (at + kAhead < kAll) piece[(at + kAhead) & 3] = piece_of(at + kAhead);
+            if (at % (kAll / 4) == 0) {
+                l4 = *(const f32x4 *)(lse + 8 * (4 * at / kAll) + 4 * half);
+                d4 = *(const f32x4 *)(delta + 8 * (4 * at / kAll) + 4 * half);
+            }
+            if (at < kSteps) next_s = mfma(piece[at & 3], k[at], next_s);
+            else if (at < 2 * kSteps) next_dp = mfma(piece[at & 3], v[at - kSteps], next_dp);
+            else if (at < 3 * kSteps) dv[(at - 2 * kSteps) >> 1] = mfma(piece[at & 3], (at & 1) ? p1 : p0, dv[(at - 2 * kSteps) >> 1]);
+            else dk[(at - 3 * kSteps) >> 1] = mfma(piece[at & 3], (at & 1) ? z1 : z0, dk[(at - 3 * kSteps) >> 1]);
+#pragma unroll
+            for (int e = 16 * at / kAll; e < 16 * (at + 1) / kAll; e++) {
+                const float w = element_w<CAP>(x, s[e]), p = element_p<CAP>(x, w, l4[e % 4]), dy = element_dy<CAP>(x, p, dp[e], d4[e % 4]);
+                if (BIAS) sum += dy;
+                dp[e] = element_dz<CAP>(x, dy, w);
+                s[e] = p;
+            }
+            constexpr int kFrom = 2 * kSteps, kPer = 8 / kSteps;
+            if (at >= kFrom) {
+#pragma unroll
+                for (int e = (at - kFrom) * kPer; e < (at - kFrom + 1) * kPer; e++) top = fmaxf(top, __builtin_fabsf(next_s[e]));
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
+        if (BIAS && plain && mine) __hip_atomic_fetch_add(my_sums + column[x0], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        size = top;
+        p0 = rounded8<E, 0>(s);
+        p1 = rounded8<E, 1>(s);
+        z0 = rounded8<E, 0>(dp);
+        z1 = rounded8<E, 1>(dp);
+        s = next_s;
+        dp = next_dp;
+        __syncthreads();
+        if (++at_tile == per) {
+            if (BIAS) finish(g);
+            at_tile = 0, g++;
+        }
+    }
+    if (tiles_n > 0) {
+        const unsigned ct = my_columns + buffer(tiles_n - 1);
+#pragma unroll
+        for (int i = 0; i < kOut; i++) {
+            dv[i] = mfma(columns_chunk<E, DP>(ct + kTile, 0, i), p0, dv[i]);
+            dv[i] = mfma(columns_chunk<E, DP>(ct + kTile, 16, i), p1, dv[i]);
+            dk[i] = mfma(columns_chunk<E, DP>(ct, 0, i), z0, dk[i]);
+            dk[i] = mfma(columns_chunk<E, DP>(ct, 16, i), z1, dk[i]);
+        }
+    } else if (BIAS) {
+        for (int i = tid; i < G * nb; i += kAttThreads) part[i] = 0.f;
     }
     if (!mine) return;
     const long long place = ((doc.key0 + key) * a.kv_heads + head) * a.dim;
@@ -179,157 +536,13 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
         }
 }
 
-// ---------------------------------------------------------------- dQ, biases
-// One block: 128 rows as in the forward, keys in tiles of 32.  A lane adds its dy to its own column of [buckets][64] in LDS:
-// no two lanes share an address, so the sums have an order.
-constexpr int kGradKeys = 32;
-
-template <class E, int DP, bool CAP, bool BIAS>
-__global__ __launch_bounds__(kAttThreads, 2) void k_att_dq(AttArgs a) {
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    constexpr int kTile = kGradKeys * DP * 2, kSteps = DP / 16, kOut = DP / 32;
-    char *tiles = lds;                               // [2][K, V]
-    int *kpos = (int *)(lds + 4 * kTile);            // [2][kGradKeys]
-    float *sums = (float *)(kpos + 2 * kGradKeys);   // [4 wavefronts][num_buckets][64]
-    const int nb = a.score.num_buckets, M = a.score.max_distance, places = 2 * M + 1, G = a.group;
-    int *column = (int *)(sums + (BIAS ? 4 * nb * 64 : 0));  // [places] where a distance's bucket begins
-    float *table = (float *)(column + (BIAS ? places : 0));
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
-    const int head = blockIdx.x % a.kv_heads;
-    const long long block = a.row_blocks - 1 - blockIdx.x / a.kv_heads;
-    const int d = document_of(a.q_off, a.num_docs, a.num_rows, G, kAttRowsShift, block, lane);
-    const AttDoc doc = att_doc(a, d);
-    const long long first = (block - first_block(a.q_off, d, a.num_rows, G, kAttRowsShift)) << kAttRowsShift;
-    const long long vrows = (long long)doc.rows * G;
-    float *part = BIAS ? a.bias_part + (block * a.heads + head * G) * nb : nullptr;
-    if (first >= vrows || first < 0) {
-        if (BIAS)
-            for (int i = tid; i < G * nb; i += kAttThreads) part[i] = 0.f;
-        return;
-    }
-
-    const long long vr = first + wave * 32 + (lane & 31);
-    const bool mine = vr < vrows;
-    const int row = mine ? (int)(vr / G) : 0, g = mine ? (int)(vr % G) : 0, h = head * G + g;
-    const int seen = mine ? doc.seen(row, a.causal) : 0;
-    const int least = doc.seen((int)(first / G), a.causal);
-    const long long last_v = first + kAttRows < vrows ? first + kAttRows - 1 : vrows - 1;
-    const int most = doc.seen((int)(last_v / G), a.causal);
-    const long long place = (doc.row0 + row) * a.heads + h;
-    const E *qrow = (const E *)a.q + (doc.row0 + row) * a.q_row + (long long)h * a.q_head;
-    const E *orow = (const E *)a.dout + place * a.dim;
-    typename Vec8<E>::type q[kSteps], o[kSteps];
-#pragma unroll
-    for (int kk = 0; kk < kSteps; kk++) {
-        q[kk] = row_chunk<E>(qrow, mine, kk, a.dim, lane);
-        o[kk] = row_chunk<E>(orow, mine, kk, a.dim, lane);
-    }
-    float lse = mine ? a.lse[place] : -INFINITY;
-    lse = lse == -INFINITY ? INFINITY : lse * kLog2e;
-    const float delta = mine ? a.delta[place] : 0.f;
-    const int q_pos = !mine ? 0 : a.q_pos ? a.q_pos[doc.row0 + row] : row + doc.keys - doc.rows;
-    const float *my_table = table + g * places;
-    float *my_sums = sums + wave * nb * 64 + lane;
-    if (BIAS) {
-        bias_to_lds<E>(table, a.score, head * G, G, tid, kAttThreads);
-        for (int i = tid; i < places; i += kAttThreads) {
-            int b = a.score.buckets[i];
-            column[i] = (b < 0 ? 0 : b >= nb ? nb - 1 : b) * 64;
-        }
-        for (int i = tid; i < 4 * nb * 64; i += kAttThreads) sums[i] = 0.f;
-    }
-    const char *kbase = (const char *)a.k + (doc.key0 * a.k_row + (long long)head * a.k_head) * 2;
-    const char *vbase = (const char *)a.v + (doc.key0 * a.v_row + (long long)head * a.v_head) * 2;
-    f32x16 dq[kOut];
-#pragma unroll
-    for (int i = 0; i < kOut; i++) dq[i] = zero16();
-
-    TileLoad<kGradKeys, DP> kload, vload;
-    int kp = 0;
-    auto fetch = [&](int t) {
-        kload.load(kbase, a.k_row, t * kGradKeys, doc.keys, a.dim, tid);
-        vload.load(vbase, a.v_row, t * kGradKeys, doc.keys, a.dim, tid);
-        int j = t * kGradKeys + tid;
-        if (BIAS && tid < kGradKeys) kp = a.k_pos && j < doc.keys ? a.k_pos[doc.key0 + j] : j;
-    };
-    const int tiles_n = (most + kGradKeys - 1) / kGradKeys;
-    if (tiles_n > 0) fetch(0);
-    for (int t = 0; t < tiles_n; t++) {
-        char *kt = tiles + (t & 1) * 2 * kTile, *vt = kt + kTile;
-        int *kpt = kpos + (t & 1) * kGradKeys;
-        kload.store(kt, tid);
-        vload.store(vt, tid);
-        if (BIAS && tid < kGradKeys) kpt[tid] = kp;
-        __syncthreads();
-        if (t + 1 < tiles_n) fetch(t + 1);
-        f32x16 s = zero16(), dp = zero16();
-#pragma unroll
-        for (int kk = 0; kk < kSteps; kk++) {
-            s = mfma(tile_rows<E, DP>(kt, 0, kk, lane), q[kk], s);
-            dp = mfma(tile_rows<E, DP>(vt, 0, kk, lane), o[kk], dp);
-        }
-        const bool edge = (t + 1) * kGradKeys > least;
-#pragma unroll
-        for (int r = 0; r < 16; r++) {
-            const int at = 8 * (r / 4) + 4 * half + r % 4;
-            float y, w = 0.f;
-            if (CAP) {
-                w = rcp_fast(exp2_fast(s[r] * a.score.k) + 1.f);
-                y = __builtin_fmaf(-2.f * a.score.c, w, a.score.c);
-            } else y = s[r] * a.score.k;
-            int apart = 0;
-            if (BIAS) {
-                apart = distance_place(kpt[at], q_pos, M);
-                y += my_table[apart];
-            }
-            float dy = exp2_fast(y - lse) * (dp[r] - delta);
-            if (edge) dy = t * kGradKeys + at < seen ? dy : 0.f;
-            if (BIAS) __hip_atomic_fetch_add(my_sums + column[apart], dy, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-            dp[r] = CAP ? dy * a.slope * (w * (1.f - w)) : dy * a.scale;
-        }
-        typename Vec8<E>::type z0 = rounded8<E, 0>(dp), z1 = rounded8<E, 1>(dp);
-#pragma unroll
-        for (int i = 0; i < kOut; i++) {
-            dq[i] = mfma(tile_columns<E, DP>(kt, 0, i, lane), z0, dq[i]);
-            dq[i] = mfma(tile_columns<E, DP>(kt, 16, i, lane), z1, dq[i]);
-        }
-    }
-    if (mine) {
-        E *out = (E *)a.dq + place * a.dim;
-#pragma unroll
-        for (int i = 0; i < kOut; i++)
-#pragma unroll
-            for (int r = 0; r < 4; r++) {
-                int c = 32 * i + 8 * r + 4 * half;
-                if (c >= a.dim) continue;
-                typename Vec4<E>::type x;
-#pragma unroll
-                for (int e = 0; e < 4; e++) x[e] = (E)dq[i][4 * r + e];
-                *(typename Vec4<E>::type *)(out + c) = x;
-            }
-    }
-    if (BIAS) {  // the columns of a head's rows, rotated by the bucket so that neighbouring threads read other banks
-        __syncthreads();
-        for (int i = tid; i < G * nb; i += kAttThreads) {
-            const int gg = i / nb, b = i % nb;
-            float sum = 0.f;
-            for (int w = 0; w < 4; w++)
-                for (int e = 0; e < 64; e++) {
-                    int l = (e + b) & 63;
-                    if ((int)((first + w * 32 + (l & 31)) % G) == gg) sum += sums[(w * nb + b) * 64 + l];
-                }
-            part[i] = sum;
-        }
-    }
-}
-
 // dbias[head][bucket] = the blocks' parts, one after the other in 1024 / num_buckets strands
 template <class E> __global__ __launch_bounds__(1024) void k_att_dbias(AttArgs a) {
     __shared__ float strand[1024];
     const int nb = a.score.num_buckets, h = blockIdx.x, strands = 1024 / nb, b = threadIdx.x % nb, s = threadIdx.x / nb;
     float sum = 0.f;
     if (s < strands)
-        for (long long i = s; i < a.row_blocks; i += strands) sum += a.bias_part[(i * a.heads + h) * nb + b];
+        for (long long i = s; i < a.key_blocks; i += strands) sum += a.bias_part[(i * a.heads + h) * nb + b];
     strand[threadIdx.x] = sum;
     __syncthreads();
     if (s != 0) return;
@@ -339,22 +552,21 @@ template <class E> __global__ __launch_bounds__(1024) void k_att_dbias(AttArgs a
 
 static int64_t delta_bytes(const AttArgs &a) { return (a.num_rows * a.heads * 4 + 15) / 16 * 16; }
 static int64_t backward_bytes(const AttArgs &a) {
-    return delta_bytes(a) + (a.score.bias ? a.row_blocks * a.heads * (int64_t)a.score.num_buckets * 4 : 0);
+    return delta_bytes(a) + (a.score.bias ? a.key_blocks * a.heads * (int64_t)a.score.num_buckets * 4 : 0);
 }
 
 template <class E, int DP, bool CAP, bool BIAS> static logoskg_status launch_backward(const AttArgs &a, hipStream_t st) {
-    const size_t table = BIAS ? (size_t)a.group * (2 * a.score.max_distance + 1) * 4 : 0;
-    if (a.num_keys) {
-        size_t bytes = 4 * kGradRows * DP * 2 + 2 * kGradRows * (sizeof(RowInfo) + 4) + table;
-        LKG_TRY(allow_lds(k_att_dkdv<E, DP, CAP, BIAS>, bytes));
-        k_att_dkdv<E, DP, CAP, BIAS><<<dim3((unsigned)(a.key_blocks * a.kv_heads)), kAttThreads, bytes, st>>>(a);
-        LKG_HIP(hipGetLastError());
-    }
+    const size_t places = BIAS ? 2 * a.score.max_distance + 1 : 0, table = a.group * places * 4;
     if (a.num_rows) {
-        size_t bytes = 4 * kGradKeys * DP * 2 + 2 * kGradKeys * 4 + table;
-        if (BIAS) bytes += (size_t)4 * a.score.num_buckets * 64 * 4 + (size_t)(2 * a.score.max_distance + 1) * 4;
+        size_t bytes = 8 * kGradTile * DP * 2 + 4 * kGradTile * 4 + table;
         LKG_TRY(allow_lds(k_att_dq<E, DP, CAP, BIAS>, bytes));
         k_att_dq<E, DP, CAP, BIAS><<<dim3((unsigned)(a.row_blocks * a.kv_heads)), kAttThreads, bytes, st>>>(a);
+        LKG_HIP(hipGetLastError());
+    }
+    if (a.num_keys) {
+        size_t bytes = 8 * kGradTile * DP * 2 + 3 * 4 * kGradTile * 4 + table + places * 4 + (BIAS ? 4 * a.score.num_buckets * 64 * 4 : 0);
+        LKG_TRY(allow_lds(k_att_dkdv<E, DP, CAP, BIAS>, bytes));
+        k_att_dkdv<E, DP, CAP, BIAS><<<dim3((unsigned)(a.key_blocks * a.kv_heads)), kAttThreads, bytes, st>>>(a);
         LKG_HIP(hipGetLastError());
     }
     return LOGOSKG_OK;
@@ -404,9 +616,8 @@ extern "C" logoskg_status logoskg_attend_backward(const logoskg_attention *in, c
     a.dout = g->dout; a.dq = g->dq; a.dk = g->dk; a.dv = g->dv; a.dbias = g->dbias;
     a.delta = (float *)g->workspace;
     a.bias_part = (float *)((char *)g->workspace + delta_bytes(a));
-    a.key_blocks = (a.num_keys >> kAttRowsShift) + a.num_docs;
     if (a.key_blocks * a.kv_heads >= (1ll << 31) || (a.num_rows * a.heads + 15) / 16 >= (1ll << 31)) { set_error("logoskg_attend_backward: too many rows"); return LOGOSKG_EINVAL; }
-    if (a.num_rows == 0) a.row_blocks = 0;
+    if (a.num_keys == 0) a.key_blocks = 0;
     LKG_HIP(hipSetDevice(in->device));
     return in->dtype == LOGOSKG_BF16 ? backward<bf16>(a, (hipStream_t)in->stream) : backward<fp16>(a, (hipStream_t)in->stream);
 }

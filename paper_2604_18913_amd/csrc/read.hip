@@ -32,6 +32,7 @@ __global__ __launch_bounds__(256, 2) void k_read(ReadArgs a) {
     float *table = (float *)(lds + 4 * kTile);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     char *vt = lds + wave * kTile;
+    const unsigned my_columns = columns_place<DP>(lane) + lds_place(vt);
     __shared__ int ids[4][kReadTile], hops[4][kReadTile];
     __shared__ float wave_m[4][32], wave_l[4][32];
     const int head = blockIdx.x % a.kv_heads;
@@ -130,8 +131,8 @@ __global__ __launch_bounds__(256, 2) void k_read(ReadArgs a) {
         wave_sync();
 #pragma unroll
         for (int i = 0; i < kOut; i++) {
-            o[i] = mfma(tile_columns<E, DP>(vt, 0, i, lane), p0, o[i]);
-            o[i] = mfma(tile_columns<E, DP>(vt, 16, i, lane), p1, o[i]);
+            o[i] = mfma(columns_chunk<E, DP>(my_columns, 0, i), p0, o[i]);
+            o[i] = mfma(columns_chunk<E, DP>(my_columns, 16, i), p1, o[i]);
         }
         wave_sync();
     }

@@ -9,6 +9,8 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -1e30f;  // running maximum of a row that has seen nothing: below any score, and no infinity
 
@@ -85,20 +87,32 @@ template <int DP> __device__ __forceinline__ int spread(int r) {
     return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
 }
 
-// A[row of the tile][16 kk + 8 (l / 32) ..]: rows at r0 + l % 32
-template <class E, int DP> __device__ __forceinline__ typename Vec8<E>::type tile_rows(const char *tile, int r0, int kk, int lane) {
-    int r = r0 + (lane & 31), c = 2 * kk + (lane >> 5);
-    return as8<E>(*(const u32x4 *)(tile + r * (DP * 2) + ((c ^ spread<DP>(r)) << 4)));
+// Places in LDS are 32-bit offsets: a lane's place in a tile is made once, the chunk's part of it is flipped into it (the
+// tiles begin at multiples of 8 KiB, so that no flipped bit meets another).
+typedef __attribute__((address_space(3))) char lds_char;
+__device__ __forceinline__ unsigned lds_place(const void *p) { return (unsigned)(uintptr_t)(lds_char *)p; }
+
+// A[row][16 kk + 8 (l / 32) ..] of the 32 rows at a tile's begin: rows_place of the lane, then a chunk per kk
+template <int DP> __device__ __forceinline__ unsigned rows_place(int lane) {
+    int r = lane & 31;
+    return r * (DP * 2) + (((lane >> 5) ^ spread<DP>(r)) << 4);
+}
+template <class E> __device__ __forceinline__ typename Vec8<E>::type rows_chunk(unsigned place, int kk) {
+    typedef __attribute__((address_space(3))) const u32x4 chunk;
+    return as8<E>(*(chunk *)(uintptr_t)(place ^ (kk << 5)));
 }
 
-// A = the tile's transpose: lane l gets column 32 dt + l % 32 of the rows r0 + 4 (l / 32) .. + 3 and r0 + 8 + 4 (l / 32) .. + 3
-template <class E, int DP> __device__ __forceinline__ typename Vec8<E>::type tile_columns(const char *tile, int r0, int dt, int lane) {
+// A = the tile's transpose: lane l gets column 32 dt + l % 32 of the rows r0 + 4 (l / 32) .. + 3 and r0 + 8 + 4 (l / 32) .. + 3,
+// r0 = 0 or 16: columns_place of the lane, then a chunk per (r0, dt)
+template <int DP> __device__ __forceinline__ unsigned columns_place(int lane) {
+    int r = ((lane & 15) >> 2) + 4 * (lane >> 5), c = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    return r * (DP * 2) + ((c ^ spread<DP>(r)) << 4) + (lane & 1) * 8;
+}
+template <class E, int DP> __device__ __forceinline__ typename Vec8<E>::type columns_chunk(unsigned place, int r0, int dt) {
     typedef __attribute__((address_space(3))) s16x4 lds4;
-    int r = r0 + ((lane & 15) >> 2) + 4 * (lane >> 5), c = 4 * dt + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-    s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(tile + r * (DP * 2) + ((c ^ spread<DP>(r)) << 4) + (lane & 1) * 8));
-    r += 8;
-    s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(tile + r * (DP * 2) + ((c ^ spread<DP>(r)) << 4) + (lane & 1) * 8));
-    struct { s16x4 a, b; } both = {lo, hi};
+    struct { s16x4 a, b; } both;
+    both.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(uintptr_t)((place ^ (dt << 6)) + r0 * (DP * 2)));
+    both.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(uintptr_t)((place ^ (dt << 6) ^ 32) + (r0 + 8) * (DP * 2)));
     return __builtin_bit_cast(typename Vec8<E>::type, both);
 }
 
@@ -125,10 +139,15 @@ __device__ __forceinline__ int document_of(const int64_t *off, int n, long long 
 }
 
 // ---------------------------------------------------------------- scores
-// What the kernels make of logoskg_score, in units of log 2: y = cap: c - 2 c / (2^(z k) + 1), c = cap log2 e, which is
-// c tanh(z / cap) for k = 2 log2 e scale / cap (2^.. may be infinite or 0: +c or -c); else z k, k = scale log2 e.
+// What the kernels make of logoskg_score, in units of log 2.  Without a cap y = z k, k = scale log2 e.  With one
+// y = c - 2 c / (2^(z k) + 1), c = cap log2 e, which is c tanh(z scale / cap) for k = 2 log2 e scale / cap (2^.. may be
+// infinite or 0: +c or -c); for products up to `most`, where tanh's argument is below 1/2, also y = z times a polynomial in
+// z^2 (near), which costs five instructions instead of an exponential, a reciprocal and three, and is as exact.
 struct ScoreArgs {
     float k, c;
+    float slope;    // |y| <= |z| slope
+    float most;     // largest |z| that the near form holds for (no cap: any)
+    float near[4];
     const void *bias;
     const int32_t *buckets;
     int num_buckets, max_distance;
@@ -136,13 +155,39 @@ struct ScoreArgs {
 
 inline ScoreArgs score_args(const logoskg_score &s) {
     ScoreArgs a;
-    a.k = s.cap > 0 ? 2.f * kLog2e * s.scale / s.cap : s.scale * kLog2e;
+    const float lin = s.scale * kLog2e;
+    a.k = s.cap > 0 ? 2.f * kLog2e * s.scale / s.cap : lin;
     a.c = s.cap > 0 ? s.cap * kLog2e : 0.f;
+    a.slope = lin < 0 ? -lin : lin;
+    a.most = INFINITY;
+    // tanh(x) / x on |x| <= 1/2 as a polynomial in x^2: smallest largest relative error, 5.5e-7 (Remez exchange on [0, 1/4])
+    const double fit[4] = {0.999999463558197, -0.33326318860054016, 0.13190296292304993, -0.04440222680568695};
+    const double w = s.cap > 0 ? (double)s.scale / s.cap : 0.0;
+    double f = lin;
+    for (int i = 0; i < 4; i++, f *= w * w) a.near[i] = (float)(fit[i] * f);
+    if (s.cap > 0 && w != 0.0) a.most = (float)(0.5 / (w < 0 ? -w : w));
     a.bias = s.bias;
     a.buckets = s.buckets;
     a.num_buckets = s.num_buckets;
     a.max_distance = s.max_distance;
     return a;
+}
+
+__device__ __forceinline__ int wave_min(int x) {
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) {
+        int y = __shfl_xor(x, s);
+        x = y < x ? y : x;
+    }
+    return x;
+}
+__device__ __forceinline__ int wave_max(int x) {
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) {
+        int y = __shfl_xor(x, s);
+        x = y > x ? y : x;
+    }
+    return x;
 }
 
 // Biases of the heads h0 .. h0 + group - 1 by distance, times log2 e, in LDS: [group][2 M + 1]
