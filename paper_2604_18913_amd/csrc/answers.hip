@@ -6,6 +6,47 @@ namespace lkg {
 
 typedef unsigned long long u64;
 
+constexpr int kMostMaskPieces = 96, kMostMaskList = 1 << 16;  // of a query (entries: on average): made in LDS up to these
+
+// Masks come out in one of two ways.  Where a list can be looked through once for every piece of its mask, a block makes a
+// piece in LDS and writes it once (k_mask_piece): no cleared memory and no atomics on it.  Else the masks are cleared and
+// the ids set by atomics (k_mask_clear, k_mask_set).
+__global__ __launch_bounds__(1024) void k_mask_piece(const int64_t *off, const int32_t *ids, long long n, long long num_ids, long long words, int pieces, int piece_words, u64 *mask) {
+    extern __shared__ u64 bits[];
+    const int tid = threadIdx.x, q = blockIdx.x / pieces;
+    const long long w0 = (long long)(blockIdx.x % pieces) * piece_words;
+    const int count = (int)(words - w0 < piece_words ? words - w0 : piece_words);
+    for (int i = tid; i < count; i += 1024) bits[i] = 0;
+    const long long e0 = taken_into(off[q], n), e1 = taken_into(off[q + 1], n), lo = w0 * 64;
+    const unsigned size = (unsigned)(lo + (long long)count * 64 < num_ids ? (long long)count * 64 : num_ids - lo);
+    auto set = [&](int id) {
+        const unsigned at = (unsigned)id - (unsigned)lo;  // (ids and lo are below 2^31: one compare for both ends)
+        if (at < size) atomicOr(&((unsigned *)bits)[at >> 5], 1u << (at & 31));
+    };
+    __syncthreads();
+    // sixteen ids of a thread at a time: whole 16-byte chunks of the list, what lies before and behind them alone
+    const long long a0 = e0 + ((16 - ((uintptr_t)(ids + e0) & 15)) & 15) / 4, chunks = e1 > a0 ? (e1 - a0) / 4 : 0, a1 = a0 + chunks * 4;
+    if (chunks == 0) {
+        if (e0 + tid < e1) set(ids[e0 + tid]);
+    } else {
+        if (e0 + tid < a0) set(ids[e0 + tid]);
+        if (a1 + tid < e1) set(ids[a1 + tid]);
+        const int4 *list = (const int4 *)(ids + a0);
+        long long i = tid;
+        for (; i + 3 * 1024 < chunks; i += 4 * 1024) {
+            const int4 x[4] = {list[i], list[i + 1024], list[i + 2048], list[i + 3072]};
+#pragma unroll
+            for (int u = 0; u < 4; u++) set(x[u].x), set(x[u].y), set(x[u].z), set(x[u].w);
+        }
+        for (; i < chunks; i += 1024) {
+            const int4 x = list[i];
+            set(x.x), set(x.y), set(x.z), set(x.w);
+        }
+    }
+    __syncthreads();
+    for (int i = tid; i < count; i += 1024) mask[q * words + w0 + i] = bits[i];
+}
+
 __global__ __launch_bounds__(256) void k_mask_clear(ulonglong2 *mask, long long pairs, u64 *last) {
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < pairs; i += (long long)gridDim.x * 256) mask[i] = ulonglong2{0, 0};
     if (last && blockIdx.x == 0 && threadIdx.x == 0) *last = 0;
@@ -51,7 +92,7 @@ __global__ __launch_bounds__(256) void k_mask_set(const int64_t *off, const int3
 // ---------------------------------------------------------------- logits
 struct LogitArgs {
     int num_rows;
-    long long vocab, row, words, num_history, num_bias;
+    long long vocab, row, words, num_history, num_bias, pieces;  // pieces of a row
     const void *logits;
     void *out;
     const int64_t *history_off, *bias_off;
@@ -60,48 +101,145 @@ struct LogitArgs {
     const u64 *mask;
 };
 
-constexpr int kPiece = 8192;  // ids of a block
+constexpr int kBiasHits = 512;  // of a piece: listed in LDS
 
-// One block: a piece of a row.  The row's history is counted into LDS for the ids of the piece, its biases' last entries are
-// found the same way, and the piece passes once through registers.  Whole numbers only are added up by atomics.
-template <class T> __global__ __launch_bounds__(512) void k_logits(LogitArgs a) {
-    __shared__ int count[kPiece];
-    __shared__ int which[kPiece];
+// One block: a piece of 16 ids per thread of a row.  The row's history is counted in LDS for the ids of the piece, in 16 bits
+// (32 where the history is so long that a count might not fit, for half of the ids at a time); its biases that fall
+// into the piece are marked, and listed as (id, place in the list), of which the last place counts.  Whole numbers only are
+// added up by atomics.  The logits pass once through registers, in 16-byte chunks from the first whole one of the row on,
+// where logits and out lie alike; else one by one.
+template <class T, int THREADS> __global__ __launch_bounds__(THREADS) void k_logits(LogitArgs a) {
+    constexpr int kPiece = 16 * THREADS, kChunk = 16 / sizeof(T), kChunks = 16 / kChunk;  // ids of a chunk; chunks of a thread
+    typedef T chunk __attribute__((ext_vector_type(kChunk)));
+    __shared__ __attribute__((aligned(16))) unsigned count[kPiece / 2 + kChunk];
+    __shared__ unsigned marked[kPiece / 32 + 1];
+    __shared__ int hit_id[kBiasHits], hit_at[kBiasHits], hits;
     const int tid = threadIdx.x;
-    const long long pieces = (a.vocab + kPiece - 1) / kPiece, b = blockIdx.x / pieces, v0 = (blockIdx.x % pieces) * kPiece;
-    const int n = (int)(a.vocab - v0 < kPiece ? a.vocab - v0 : kPiece);
+    const long long b = blockIdx.x / a.pieces;
+    const T *in = (const T *)a.logits + b * a.row;
+    T *out = (T *)a.out + b * a.row;
+    // ids of the row before its first whole chunk; pieces begin there, the first one with what lies before
+    const int lead = (int)((16 - ((uintptr_t)in & 15)) & 15) / (int)sizeof(T);
+    const bool alike = (((uintptr_t)in ^ (uintptr_t)out) & 15) == 0;
+    const long long piece = blockIdx.x % a.pieces, v0 = piece * kPiece + lead - kChunk;  // a chunk more than the ids that may lie before
+    const long long lo = piece == 0 ? 0 : v0, hi = v0 + kPiece < a.vocab ? v0 + kPiece : a.vocab;
+    if (lo >= hi) return;
+    chunk x[kChunks];
+    if (alike) {
+#pragma unroll
+        for (int i = 0; i < kChunks; i++) {
+            const long long v = v0 + (long long)(i * THREADS + tid) * kChunk;
+            if (v >= lo && v + kChunk <= hi) x[i] = *(const chunk *)(in + v);
+        }
+    }
     long long h0 = 0, h1 = 0, s0 = 0, s1 = 0;
     if (a.history_off) h0 = taken_into(a.history_off[b], a.num_history), h1 = taken_into(a.history_off[b + 1], a.num_history);
     if (a.bias_off) s0 = taken_into(a.bias_off[b], a.num_bias), s1 = taken_into(a.bias_off[b + 1], a.num_bias);
-    const bool said = h1 > h0, biased = s1 > s0;
-    if (said)
-        for (int i = tid; i < n; i += 512) count[i] = 0;
-    if (biased)
-        for (int i = tid; i < n; i += 512) which[i] = -1;
-    if (said || biased) __syncthreads();
-    for (long long i = h0 + tid; i < h1; i += 512) {
-        long long id = a.history[i] - v0;
-        if (a.history[i] >= 0 && id >= 0 && id < n) atomicAdd(&count[id], 1);
-    }
-    for (long long i = s0 + tid; i < s1; i += 512) {
-        long long id = a.bias_id[i] - v0;
-        if (a.bias_id[i] >= 0 && id >= 0 && id < n) atomicMax(&which[id], (int)(i - s0));
-    }
-    if (said || biased) __syncthreads();
+    const bool said = h1 > h0, biased = s1 > s0, wide = h1 - h0 > 65535;
     const float rep = a.repetition ? a.repetition[b] : 1.f, pres = a.presence ? a.presence[b] : 0.f, freq = a.frequency ? a.frequency[b] : 0.f;
-    const T *in = (const T *)a.logits + b * a.row + v0;
-    T *out = (T *)a.out + b * a.row + v0;
-    const u64 *mask = a.mask ? a.mask + b * a.words + (v0 >> 6) : nullptr;
-    for (int i = tid; i < n; i += 512) {
-        float x = (float)in[i];
-        if (said) {
-            int c = count[i];
-            if (c > 0) x = (x > 0.f ? x / rep : x * rep) - (freq * c + pres);
+    const u64 *mask = a.mask ? a.mask + b * a.words : nullptr;
+    if (biased) {
+        for (int i = tid; i < kPiece / 32 + 1; i += THREADS) marked[i] = 0;
+        if (tid == 0) hits = 0;
+        __syncthreads();
+        for (long long i = s0 + tid; i < s1; i += THREADS) {
+            const long long id = a.bias_id[i];
+            if (id >= lo && id < hi) {
+                atomicOr(&marked[(int)(id - v0) >> 5], 1u << ((id - v0) & 31));
+                const int n = atomicAdd(&hits, 1);
+                if (n < kBiasHits) hit_id[n] = (int)(id - v0), hit_at[n] = (int)(i - s0);
+            }
         }
-        if (biased && which[i] >= 0) x += a.bias_value[s0 + which[i]];
-        if (mask && !(mask[i >> 6] >> (i & 63) & 1)) x = -INFINITY;
-        out[i] = (T)x;
+        __syncthreads();
     }
+
+    auto one = [&](float y, long long v, unsigned c, bool allowed) {  // id v, said c times
+        if (c > 0) y = (y > 0.f ? y / rep : y * rep) - (freq * (float)c + pres);
+        const int at = (int)(v - v0);
+        if (biased && (marked[at >> 5] >> (at & 31) & 1)) {
+            int last = -1;
+            if (hits <= kBiasHits) {
+                for (int i = 0; i < hits; i++)
+                    if (hit_id[i] == at && hit_at[i] > last) last = hit_at[i];
+            } else {
+                for (long long i = s1 - 1; i >= s0 && last < 0; i--)
+                    if (a.bias_id[i] == v) last = (int)(i - s0);
+            }
+            y += a.bias_value[s0 + last];
+        }
+        return allowed ? y : -INFINITY;
+    };
+    auto allowed = [&](long long v) { return !mask || (mask[v >> 6] >> (v & 63) & 1); };
+    const int rounds = wide ? 2 : 1;
+    for (int round = 0; round < rounds; round++) {  // of a wide history: half of the ids each
+        const long long w0 = v0 + round * (kPiece / 2), from = lo > w0 ? lo : w0, to = wide && round == 0 && w0 + kPiece / 2 < hi ? w0 + kPiece / 2 : hi;
+        if (said) {
+            if (round > 0) __syncthreads();
+            for (int i = tid; i < (int)(sizeof(count) / 16); i += THREADS) ((u32x4 *)count)[i] = u32x4{0, 0, 0, 0};
+            __syncthreads();
+            for (long long i = h0 + tid; i < h1; i += THREADS) {
+                const long long id = a.history[i];
+                if (id < from || id >= to) continue;
+                if (wide) atomicAdd(&count[(int)(id - w0)], 1u);
+                else atomicAdd(&count[(int)(id - v0) >> 1], (id - v0) & 1 ? 65536u : 1u);
+            }
+            __syncthreads();
+        }
+        auto count_of = [&](long long v) {
+            const int at = (int)(v - w0);
+            return !said ? 0u : wide ? count[at] : count[at >> 1] >> (16 * (at & 1)) & 65535u;
+        };
+        if (!alike) {
+            for (long long v = from + tid; v < to; v += THREADS) out[v] = (T)one((float)in[v], v, count_of(v), allowed(v));
+            continue;
+        }
+#pragma unroll
+        for (int i = 0; i < kChunks; i++) {
+            if (wide && i / (kChunks / 2) != round) continue;
+            const long long v = v0 + (long long)(i * THREADS + tid) * kChunk;
+            if (v >= lo && v + kChunk <= hi) {
+                const int at = (int)(v - v0);
+                unsigned bits = ~0u, marks = 0, counts[kChunk / 2] = {};
+                if (mask) {
+                    const int sh = (int)(v & 63);
+                    u64 w = mask[v >> 6] >> sh;
+                    if (sh > 64 - kChunk) w |= mask[(v >> 6) + 1] << (64 - sh);
+                    bits = (unsigned)w;
+                }
+                if (said && !wide) {
+#pragma unroll
+                    for (int e = 0; e < kChunk / 2; e++) counts[e] = count[(at >> 1) + e];
+                }
+                if (biased) marks = marked[at >> 5] >> (at & 31);
+                unsigned any = marks & ((1u << kChunk) - 1);
+#pragma unroll
+                for (int e = 0; e < kChunk / 2; e++) any |= counts[e];
+                if (any || wide) {
+#pragma unroll
+                    for (int e = 0; e < kChunk; e++)
+                        x[i][e] = (T)one((float)x[i][e], v + e, wide ? count_of(v + e) : counts[e / 2] >> (16 * (e & 1)) & 65535u, bits >> e & 1);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < kChunk; e++) x[i][e] = bits >> e & 1 ? x[i][e] : (T)-INFINITY;
+                }
+                *(chunk *)(out + v) = x[i];
+            } else {
+                for (long long w = v < lo ? lo : v; w < v + kChunk && w < hi; w++) out[w] = (T)one((float)in[w], w, count_of(w), allowed(w));
+            }
+        }
+    }
+}
+
+// Pieces of 16,384 ids where there are 512 of them, of 4,096 for less.  (A piece looks through the row's whole history.)
+template <class T> static logoskg_status launch_logits(LogitArgs a, hipStream_t st) {
+    a.pieces = (a.vocab + 16384 + 15) / 16384;
+    const bool large = a.pieces * a.num_rows >= 512;
+    if (!large) a.pieces = (a.vocab + 4096 + 15) / 4096;
+    if (a.pieces * a.num_rows >= (1ll << 31)) { set_error("logoskg_constrain_logits: too many rows"); return LOGOSKG_EINVAL; }
+    if (large) k_logits<T, 1024><<<dim3((unsigned)(a.pieces * a.num_rows)), 1024, 0, st>>>(a);
+    else k_logits<T, 256><<<dim3((unsigned)(a.pieces * a.num_rows)), 256, 0, st>>>(a);
+    LKG_HIP(hipGetLastError());
+    return LOGOSKG_OK;
 }
 
 }  // namespace lkg
@@ -113,13 +251,23 @@ extern "C" logoskg_status logoskg_entity_mask(int32_t device, const int64_t *off
     const char *why = nullptr;
     if (num_entries < 0 || num_queries < 0 || num_ids < 0 || num_ids > (1ll << 31) || num_entries >= (1ll << 40)) why = "a count is out of range";
     else if (num_queries && num_ids && !mask) why = "mask is NULL";
-    else if (num_entries && num_queries && (!off || !ids)) why = "off or ids is NULL";
+    else if (num_queries && num_ids && (!off || (num_entries && !ids))) why = "off or ids is NULL";
     else if ((uintptr_t)mask & 15) why = "mask is not 16-byte aligned";
     if (why) { set_error("logoskg_entity_mask: %s", why); return LOGOSKG_EINVAL; }
     const long long words = (num_ids + 63) / 64, all = words * num_queries;
     if (all == 0) return LOGOSKG_OK;
     LKG_HIP(hipSetDevice(device));
     hipStream_t st = (hipStream_t)stream;
+    // Pieces of up to 16,384 words (128 KiB of LDS), smaller ones down to 512 where there are fewer than 512 of them.
+    int piece_words = 16384;
+    while (piece_words > 512 && (words + piece_words - 1) / piece_words * num_queries < 512) piece_words /= 2;
+    const long long pieces = (words + piece_words - 1) / piece_words;
+    if (pieces <= kMostMaskPieces && num_entries / num_queries <= kMostMaskList && pieces * num_queries < (1ll << 31)) {
+        LKG_TRY(allow_lds(k_mask_piece, (size_t)piece_words * 8));
+        k_mask_piece<<<dim3((unsigned)(pieces * num_queries)), 1024, piece_words * 8, st>>>(off, ids, num_entries, num_ids, words, (int)pieces, piece_words, (u64 *)mask);
+        LKG_HIP(hipGetLastError());
+        return LOGOSKG_OK;
+    }
     const long long blocks = (all / 2 + 255) / 256;
     k_mask_clear<<<dim3((unsigned)(blocks < 1 ? 1 : blocks > 8192 ? 8192 : blocks)), 256, 0, st>>>((ulonglong2 *)mask, all / 2, all & 1 ? (u64 *)mask + all - 1 : nullptr);
     LKG_HIP(hipGetLastError());
@@ -149,13 +297,8 @@ extern "C" logoskg_status logoskg_constrain_logits(const logoskg_logits *l) {
     a.history_off = l->history_off; a.history = l->history; a.bias_off = l->bias_off; a.bias_id = l->bias_id;
     a.bias_value = l->bias_value; a.repetition = l->repetition; a.presence = l->presence; a.frequency = l->frequency;
     a.mask = (const u64 *)l->mask;
-    const long long blocks = (l->vocab + kPiece - 1) / kPiece * l->num_rows;
-    if (blocks >= (1ll << 31)) { set_error("logoskg_constrain_logits: too many rows"); return LOGOSKG_EINVAL; }
     LKG_HIP(hipSetDevice(l->device));
     hipStream_t st = (hipStream_t)l->stream;
-    if (l->dtype == LOGOSKG_F32) k_logits<float><<<dim3((unsigned)blocks), 512, 0, st>>>(a);
-    else if (l->dtype == LOGOSKG_BF16) k_logits<bf16><<<dim3((unsigned)blocks), 512, 0, st>>>(a);
-    else k_logits<fp16><<<dim3((unsigned)blocks), 512, 0, st>>>(a);
-    LKG_HIP(hipGetLastError());
-    return LOGOSKG_OK;
+    if (l->dtype == LOGOSKG_F32) return launch_logits<float>(a, st);
+    return l->dtype == LOGOSKG_BF16 ? launch_logits<bf16>(a, st) : launch_logits<fp16>(a, st);
 }

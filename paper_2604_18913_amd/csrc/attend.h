@@ -104,9 +104,4 @@ template <class E> __device__ __forceinline__ typename Vec8<E>::type row_chunk(c
 
 logoskg_status attend_args(const logoskg_attention *a, AttArgs *o, const char *call);
 
-template <class F> logoskg_status allow_lds(F *kernel, size_t bytes) {
-    if (bytes > (64 << 10)) LKG_HIP(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
-    return LOGOSKG_OK;
-}
-
 }  // namespace lkg

@@ -175,13 +175,17 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
                     y = __builtin_fmaf(zz, y, near0);
                     y = __builtin_fmaf(z, y, shift);
                 } else y = __builtin_fmaf(z, near0, shift);
-                s[e] = exp2_fast(y);
-                l += s[e];
+                y = exp2_fast(y);
+                here(y);
+                s[e] = y;
+                l += y;
             }
+            here(l);
             constexpr int kFrom = kSteps + kSteps / 4, kPer = (16 + kAll - kFrom - 1) / (kAll - kFrom);
             if (at >= kFrom) {
 #pragma unroll
                 for (int e = (at - kFrom) * kPer; e < (at - kFrom + 1) * kPer && e < 16; e++) top = fmaxf(top, __builtin_fabsf(next[e]));
+                here(top);
             }
         }
         __builtin_amdgcn_sched_barrier(0);

@@ -226,12 +226,16 @@ __global__ __launch_bounds__(kAttThreads, DP == 128 ? 1 : 2) void k_att_dq(AttAr
             for (int e = 16 * at / kAll; e < 16 * (at + 1) / kAll; e++) {
                 const float w = element_w<CAP>(x, s[e]), p = element_p<CAP>(x, w, lse), dy = element_dy<CAP>(x, p, dp[e], delta);
                 sum += dy;
-                dp[e] = element_dz<CAP>(x, dy, w);
+                float dz = element_dz<CAP>(x, dy, w);
+                here(dz);
+                dp[e] = dz;
             }
+            here(sum);
             constexpr int kFrom = 2 * kSteps, kPer = 16 / kSteps;
             if (at >= kFrom) {
 #pragma unroll
                 for (int e = (at - kFrom) * kPer; e < (at - kFrom + 1) * kPer; e++) top = fmaxf(top, __builtin_fabsf(next_s[e]));
+                here(top);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -482,15 +486,21 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
             else dk[(at - 3 * kSteps) >> 1] = mfma(piece[at & 3], (at & 1) ? z1 : z0, dk[(at - 3 * kSteps) >> 1]);
 #pragma unroll
             for (int e = 16 * at / kAll; e < 16 * (at + 1) / kAll; e++) {
-                const float w = element_w<CAP>(x, s[e]), p = element_p<CAP>(x, w, l4[e % 4]), dy = element_dy<CAP>(x, p, dp[e], d4[e % 4]);
+                const float w = element_w<CAP>(x, s[e]);
+                float p = element_p<CAP>(x, w, l4[e % 4]), dy = element_dy<CAP>(x, p, dp[e], d4[e % 4]);
                 if (BIAS) sum += dy;
-                dp[e] = element_dz<CAP>(x, dy, w);
+                float dz = element_dz<CAP>(x, dy, w);
+                here(p);
+                here(dz);
+                dp[e] = dz;
                 s[e] = p;
             }
+            if (BIAS) here(sum);
             constexpr int kFrom = 2 * kSteps, kPer = 8 / kSteps;
             if (at >= kFrom) {
 #pragma unroll
                 for (int e = (at - kFrom) * kPer; e < (at - kFrom + 1) * kPer; e++) top = fmaxf(top, __builtin_fabsf(next_s[e]));
+                here(top);
             }
         }
         __builtin_amdgcn_sched_barrier(0);

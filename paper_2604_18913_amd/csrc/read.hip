@@ -35,8 +35,12 @@ __global__ __launch_bounds__(256, 2) void k_read(ReadArgs a) {
     const unsigned my_columns = columns_place<DP>(lane) + lds_place(vt);
     __shared__ int ids[4][kReadTile], hops[4][kReadTile];
     __shared__ float wave_m[4][32], wave_l[4][32];
-    const int head = blockIdx.x % a.kv_heads;
-    const long long block = blockIdx.x / a.kv_heads;
+    // the key heads of a block's entries one behind the other on one of the card's eight dies, which blocks take turns with:
+    // their rows lie side by side
+    const unsigned turn = blockIdx.x >> 3;
+    const int head = turn % a.kv_heads;
+    const long long block = (long long)(turn / a.kv_heads) * 8 + (blockIdx.x & 7);
+    if (block >= a.blocks) return;
     const int d = document_of(a.off, a.num_queries, a.num_entries, 1, a.shift, block, lane);
     const long long b0 = first_block(a.off, d, a.num_entries, 1, a.shift);
     const long long e0 = taken_into(a.off[d], a.num_entries), e1 = taken_into(a.off[d + 1], a.num_entries);
@@ -68,21 +72,17 @@ __global__ __launch_bounds__(256, 2) void k_read(ReadArgs a) {
     const E *keys = (const E *)a.keys + (long long)head * a.key_head, *values = (const E *)a.values + (long long)head * a.value_head;
     auto id_of = [&](int t) {  // row of the table of this lane's entry of tile t, -1 for none
         int at = t * kReadTile + (lane & 31);
-        if (at >= n) return -1ll;
+        if (at >= n) return -1;
         long long id = entity ? entity[at] : e0 + from + at;
-        return id >= 0 && id < a.num_entities ? id : -1ll;
+        return id >= 0 && id < a.num_entities ? (int)id : -1;
     };
-    const int tiles_n = (n + kReadTile - 1) / kReadTile;
-    for (int t = wave; t < tiles_n; t += 4) {
-        const long long id = id_of(t);
-        const unsigned seen = (unsigned)__ballot(id >= 0);
-        if (lane < 32) {
-            ids[wave][lane] = (int)id;
-            if (BIAS) hops[wave][lane] = hop && id >= 0 ? hop[t * kReadTile + lane] : 0;
-        }
-        wave_sync();
-        const E *krow = keys + (id < 0 ? 0 : id) * a.key_row;
-        u32x4 k[kSteps], v[DP / 16];
+    auto hop_of = [&](int t) {
+        int at = t * kReadTile + (lane & 31);
+        return hop && at < n ? (int)hop[at] : 0;
+    };
+    u32x4 k[kSteps], v[DP / 16];
+    auto fetch = [&](int id) {  // keys and values of a tile, once its rows stand in ids
+        const E *krow = keys + (long long)(id < 0 ? 0 : id) * a.key_row;
 #pragma unroll
         for (int kk = 0; kk < kSteps; kk++) {
             int c = 16 * kk + 8 * half;
@@ -94,6 +94,18 @@ __global__ __launch_bounds__(256, 2) void k_read(ReadArgs a) {
             long long vid = ids[wave][r];
             v[i] = vid >= 0 && c < a.dim ? *(const u32x4 *)(values + vid * a.value_row + c) : u32x4{0, 0, 0, 0};
         }
+    };
+    // A tile's rows of the table are known two rounds, its keys and values asked for one round ahead.
+    const int tiles_n = (n + kReadTile - 1) / kReadTile;
+    int id = id_of(wave), next_id = id_of(wave + 4), next_hop = 0, now_hop = 0;
+    if (BIAS) now_hop = hop_of(wave), next_hop = hop_of(wave + 4);
+    if (wave < tiles_n) {
+        if (lane < 32) ids[wave][lane] = id;
+        wave_sync();
+        fetch(id);
+    }
+    for (int t = wave; t < tiles_n; t += 4) {
+        const unsigned seen = (unsigned)__ballot(id >= 0);
         f32x16 s = zero16();
 #pragma unroll
         for (int kk = 0; kk < kSteps; kk++) s = mfma(as8<E>(k[kk]), q[kk], s);
@@ -102,6 +114,16 @@ __global__ __launch_bounds__(256, 2) void k_read(ReadArgs a) {
             int at = i * 64 + lane, r = at / kRow, c = at % kRow;
             *(u32x4 *)(vt + r * (DP * 2) + ((c ^ spread<DP>(r)) << 4)) = v[i];
         }
+        if (lane < 32) {
+            ids[wave][lane] = next_id;
+            if (BIAS) hops[wave][lane] = now_hop;
+        }
+        wave_sync();
+        id = next_id;
+        now_hop = next_hop;
+        if (t + 4 < tiles_n) fetch(id);
+        next_id = id_of(t + 8);
+        if (BIAS) next_hop = hop_of(t + 8);
         float top = kLowest;
 #pragma unroll
         for (int r = 0; r < 16; r++) {
@@ -128,7 +150,6 @@ __global__ __launch_bounds__(256, 2) void k_read(ReadArgs a) {
             l += s[r];
         }
         typename Vec8<E>::type p0 = rounded8<E, 0>(s), p1 = rounded8<E, 1>(s);
-        wave_sync();
 #pragma unroll
         for (int i = 0; i < kOut; i++) {
             o[i] = mfma(columns_chunk<E, DP>(my_columns, 0, i), p0, o[i]);
@@ -268,7 +289,7 @@ static logoskg_status read_args(const logoskg_entity_read *r, ReadArgs *a, const
     a->shift = kReadLeastShift;
     while (a->shift < 12 && (a->num_entries >> a->shift) * a->kv_heads * row_groups > 2048) a->shift++;
     a->blocks = (a->num_entries >> a->shift) + a->num_queries;
-    if (a->blocks * a->kv_heads >= (1ll << 31) || row_groups > 65535 || (long long)a->num_queries * a->tokens * a->heads >= (1ll << 32)) { set_error("%s: too many rows", call); return LOGOSKG_EINVAL; }
+    if ((a->blocks + 8) * a->kv_heads >= (1ll << 31) || row_groups > 65535 || (long long)a->num_queries * a->tokens * a->heads >= (1ll << 32)) { set_error("%s: too many rows", call); return LOGOSKG_EINVAL; }
     return LOGOSKG_OK;
 }
 
@@ -279,7 +300,7 @@ static int64_t part_bytes(const ReadArgs &a) {  // one block per list: nothing t
 template <class E, int DP, bool CAP, bool BIAS> static logoskg_status launch_read(const ReadArgs &a, hipStream_t st) {
     size_t bytes = 4 * kReadTile * DP * 2 + (BIAS ? (size_t)a.group * (2 * a.score.max_distance + 1) * 4 : 0);
     LKG_TRY(allow_lds(k_read<E, DP, CAP, BIAS>, bytes));
-    k_read<E, DP, CAP, BIAS><<<dim3((unsigned)(a.blocks * a.kv_heads), (unsigned)((a.rows + 31) / 32)), 256, bytes, st>>>(a);
+    k_read<E, DP, CAP, BIAS><<<dim3((unsigned)((a.blocks + 7) / 8 * 8 * a.kv_heads), (unsigned)((a.rows + 31) / 32)), 256, bytes, st>>>(a);
     LKG_HIP(hipGetLastError());
     return LOGOSKG_OK;
 }

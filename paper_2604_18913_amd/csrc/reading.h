@@ -80,6 +80,9 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// Keeps what makes x in its place among the matrix instructions: the compiler would gather it behind them.
+__device__ __forceinline__ void here(float &x) { asm volatile("" : "+v"(x)); }
+
 // A tile in LDS: rows of DP 16-bit values in 16-byte chunks, chunk c of row r at place c ^ spread(r), so that neither the
 // 16 rows x one chunk that a row-wise read asks for at a time nor the 4 rows x 64 bytes of a transposing read share banks.
 template <int DP> __device__ __forceinline__ int spread(int r) {
@@ -204,6 +207,11 @@ template <class E> __device__ __forceinline__ void bias_to_lds(float *table, con
 __device__ __forceinline__ int distance_place(int k_pos, int q_pos, int M) {
     int d = __builtin_elementwise_sub_sat(k_pos, q_pos);
     return (d < -M ? -M : d > M ? M : d) + M;
+}
+
+template <class F> logoskg_status allow_lds(F *kernel, size_t bytes) {
+    if (bytes > (64 << 10)) LKG_HIP(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    return LOGOSKG_OK;
 }
 
 const char *bad_score(const logoskg_score &s, int heads, int kv_heads);  // read.hip: why a call refuses it, or NULL
