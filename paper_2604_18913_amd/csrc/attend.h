@@ -66,31 +66,41 @@ __device__ __forceinline__ u32x4 window_chunk(__amdgpu_buffer_rsrc_t w, unsigned
 }
 constexpr unsigned kNowhere = 0x80000000u;  // behind every window
 
-// Moves N rows x DP values of a ragged array's head into a tile through registers, spread over the block's threads: rows
-// [r0, r0 + N) of a matrix of `rows` rows with `row_bytes` between them, zeros behind the last row and behind dim.
+// Moves N rows x DP values of a ragged array's head into a tile through registers, spread over the block's threads: tile after
+// tile of a matrix of `rows` rows, zeros behind the last row and behind dim.
 template <int N, int DP> struct TileLoad {
     static constexpr int kChunks = N * DP / 8 / kAttThreads, kStep = kAttThreads / (DP / 8);  // rows between a thread's chunks
-    unsigned from, to;
-    u32x4 x[kChunks];
-    __device__ __forceinline__ void begin(unsigned row_bytes, int dim, int tid) {
-        int r = tid / (DP / 8), c = tid % (DP / 8);
-        from = c * 8 < dim ? r * row_bytes + c * 16 : kNowhere;
+    const char *at;  // the next tile
+    long long left;  // bytes from there to the end of the last row
+    unsigned row_bytes, from, to;
+    __device__ __forceinline__ void begin(const char *base, unsigned bytes, int row, int rows, int dim, int tid) {
+        const int r = tid / (DP / 8), c = tid % (DP / 8);
+        row_bytes = bytes;
+        go_to(base, row, rows, dim);
+        from = c * 8 < dim ? r * bytes + c * 16 : kNowhere;
         to = r * (DP * 2) + ((c ^ spread<DP>(r)) << 4);
     }
-    __device__ __forceinline__ void load(const char *base, unsigned row_bytes, int r0, int rows, int dim) {
-        const __amdgpu_buffer_rsrc_t w = window(base + (long long)r0 * row_bytes, rows > r0 ? (long long)(rows - r0 - 1) * row_bytes + dim * 2 : 0);
+    __device__ __forceinline__ void go_to(const char *base, int row, int rows, int dim) {
+        at = base + (long long)row * row_bytes;
+        left = (long long)(rows - row - 1) * row_bytes + dim * 2;
+    }
+    __device__ __forceinline__ void load(u32x4 (&x)[kChunks]) {
+        const __amdgpu_buffer_rsrc_t w = window(at, left);
 #pragma unroll
         for (int i = 0; i < kChunks; i++) x[i] = window_chunk(w, from + i * kStep * row_bytes);
+        at += (long long)N * row_bytes;
+        left -= (long long)N * row_bytes;
     }
-    __device__ __forceinline__ void clear(unsigned tile) const {
-        typedef __attribute__((address_space(3))) u32x4 chunk;
-#pragma unroll
-        for (int i = 0; i < kChunks; i++) *(chunk *)(uintptr_t)(tile + to + i * kStep * DP * 2) = u32x4{0, 0, 0, 0};
-    }
-    __device__ __forceinline__ void store(unsigned tile) const {  // (kStep is a multiple of 16 rows, over which the spread repeats)
+    __device__ __forceinline__ void store(unsigned tile, const u32x4 (&x)[kChunks]) const {  // (kStep is a multiple of 16 rows, over which the spread repeats)
         typedef __attribute__((address_space(3))) u32x4 chunk;
 #pragma unroll
         for (int i = 0; i < kChunks; i++) *(chunk *)(uintptr_t)(tile + to + i * kStep * DP * 2) = x[i];
+    }
+    __device__ __forceinline__ void clear(unsigned tile) const {
+        u32x4 x[kChunks];
+#pragma unroll
+        for (int i = 0; i < kChunks; i++) x[i] = u32x4{0, 0, 0, 0};
+        store(tile, x);
     }
 };
 

@@ -5,8 +5,8 @@ namespace lkg {
 
 // One block: 128 rows of (document, key head), where a row is a (row of q, head of the group) pair, so that the heads that
 // share a key head share its tiles.  A wavefront holds 32 rows: lane l works for row l % 32 and half of the keys, so a row's
-// maximum and sum are its own registers and one exchange with the other half.  Keys pass in tiles of 32 through a ring of
-// four buffers in LDS: S^T = K Q^T, p = 2^(y - m), O^T += V^T P^T with m the running maximum.
+// maximum and sum are its own registers and one exchange with the other half.  Keys pass in tiles of 64 through two buffers
+// for K and two for V in LDS: S^T = K Q^T, p = 2^(y - m), O^T += V^T P^T with m the running maximum.
 //
 // The vector units bound this: a score costs them about twelve issue slots (a tanh among them), its products four.  So the
 // products of the next tile's scores and of the last tile's values are issued between the exponentials of this one, one
@@ -14,15 +14,15 @@ namespace lkg {
 // its distances read one bias (text far from the row, which is most of a long document), the scores are in the range of the
 // tanh's polynomial, and the maximum does not move by more than 2^8.  m need not be the true maximum: p stays below 2^8 and
 // is summed in 32 bits.  Other tiles get their y - m first, with m the maximum again.
-constexpr int kKeys = 32;
+constexpr int kKeys = 64;
 
 template <class E, int DP, bool CAP, bool BIAS>
 __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     typedef typename Vec8<E>::type Chunk;
     constexpr int kTile = kKeys * DP * 2, kSteps = DP / 16, kOut = DP / 32;
-    int *kpos = (int *)(lds + 8 * kTile);              // [4][kKeys]
-    float *table = (float *)(kpos + 4 * kKeys);        // [group][2 M + 1]
+    int *kpos = (int *)(lds + 4 * kTile);              // [2][kKeys]  (LDS begins with K, K, V, V)
+    float *table = (float *)(kpos + 2 * kKeys);        // [group][2 M + 1]
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int head = blockIdx.x % a.kv_heads;
     const long long block = a.row_blocks - 1 - blockIdx.x / a.kv_heads;  // the last rows of a document see most: first
@@ -59,63 +59,63 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
 
     const char *kbase = (const char *)a.k + (doc.key0 * a.k_row + (long long)head * a.k_head) * 2;
     const char *vbase = (const char *)a.v + (doc.key0 * a.v_row + (long long)head * a.v_head) * 2;
-    f32x16 o[kOut], s = zero16();
-    Chunk p0 = as8<E>(u32x4{0, 0, 0, 0}), p1 = p0;  // of the last tile
+    f32x16 o[kOut], s[2] = {zero16(), zero16()};
+    Chunk p[4];  // of the last tile, 16 keys each
+#pragma unroll
+    for (int i = 0; i < 4; i++) p[i] = as8<E>(u32x4{0, 0, 0, 0});
 #pragma unroll
     for (int i = 0; i < kOut; i++) o[i] = zero16();
     float m = kLowest, l = 0.f, size = 0.f;  // size: the largest product of the tile, without its sign
 
     TileLoad<kKeys, DP> kload, vload;
-    const unsigned k_bytes = (unsigned)a.k_row * 2, v_bytes = (unsigned)a.v_row * 2;
-    kload.begin(k_bytes, a.dim, tid);
-    vload.begin(v_bytes, a.dim, tid);
-    const unsigned tiles = lds_place(lds), my_rows = rows_place<DP>(lane) + tiles, my_columns = columns_place<DP>(lane) + tiles + kTile;
-    auto buffer = [](int t) { return (unsigned)(t & 3) * 2 * kTile; };
+    kload.begin(kbase, (unsigned)a.k_row * 2, 0, doc.keys, a.dim, tid);
+    vload.begin(vbase, (unsigned)a.v_row * 2, 0, doc.keys, a.dim, tid);
+    const unsigned tiles = lds_place(lds), my_rows = rows_place<DP>(lane) + tiles, my_columns = columns_place<DP>(lane) + tiles + 2 * kTile;
+    auto buffer = [](int t) { return (unsigned)(t & 1) * kTile; };
+    u32x4 x[TileLoad<kKeys, DP>::kChunks];
     int kp = 0;
     const int tiles_n = (most + kKeys - 1) / kKeys;
-    auto fetch = [&](int t) {
-        kload.load(kbase, k_bytes, t * kKeys, doc.keys, a.dim);
-        vload.load(vbase, v_bytes, t * kKeys, doc.keys, a.dim);
+    auto fetch_pos = [&](int t) {
         if (BIAS && tid < kKeys) {
             int j = t * kKeys + tid;
             j = j < doc.keys ? j : doc.keys - 1;
             kp = a.k_pos && doc.keys > 0 ? a.k_pos[doc.key0 + j] : j;
         }
     };
-    auto stage = [&](int t) {
-        kload.store(tiles + buffer(t));
-        vload.store(tiles + buffer(t) + kTile);
-        if (BIAS && tid < kKeys) kpos[(t & 3) * kKeys + tid] = kp;
+    auto stage_pos = [&](int t) {
+        if (BIAS && tid < kKeys) kpos[(t & 1) * kKeys + tid] = kp;
     };
-    auto scores = [&](int t) {
-        const unsigned kt = my_rows + buffer(t);
-        f32x16 x = zero16();
-#pragma unroll
-        for (int kk = 0; kk < kSteps; kk++) x = mfma(rows_chunk<E>(kt, kk), q[kk], x);
-        return x;
-    };
-
+    // Round t makes the scores of tile t + 1 and the output of tile t - 1.  K of tile t + 2 and V of tile t come in meanwhile,
+    // one after the other through the same registers.
     if (tiles_n > 0) {
-        fetch(0);
-        stage(0);
-        if (tiles_n > 1) fetch(1), stage(1);
-        if (tiles_n > 2) fetch(2);
-        vload.clear(tiles + buffer(3) + kTile);  // (round 0 multiplies it with zeros)
+        kload.load(x);
+        kload.store(tiles, x);
+        fetch_pos(0);
+        stage_pos(0);
+        kload.load(x);
+        kload.store(tiles + kTile, x);
+        fetch_pos(1);
+        stage_pos(1);
+        kload.load(x);
+        fetch_pos(2);
+        vload.clear(tiles + 2 * kTile + buffer(1));  // (round 0 multiplies it with zeros)
         __syncthreads();
-        s = scores(0);
 #pragma unroll
-        for (int r = 0; r < 16; r++) size = fmaxf(size, __builtin_fabsf(s[r]));
+        for (int kk = 0; kk < kSteps; kk++)
+#pragma unroll
+            for (int u = 0; u < 2; u++) s[u] = mfma(rows_chunk<E>(my_rows + u * 32 * DP * 2, kk), q[kk], s[u]);
+#pragma unroll
+        for (int r = 0; r < 32; r++) size = fmaxf(size, __builtin_fabsf(s[r / 16][r % 16]));
+        __syncthreads();
     }
     for (int t = 0; t < tiles_n; t++) {
-        if (t + 2 < tiles_n) stage(t + 2);  // (its buffer was read last in round t - 1: values of t - 2)
-        if (t + 3 < tiles_n) fetch(t + 3);
         bool plain = (t + 1) * kKeys <= least;
         float b = 0.f;
         if (BIAS) {  // one bias for all distances of the tile?
-            int pos = kpos[(t & 3) * kKeys + (lane & 31)];
-            int x = distance_place(pos, q_high, M), y = distance_place(pos, q_low, M), x0 = __builtin_amdgcn_readfirstlane(x);
-            plain = plain && !wave_any(x != x0 || y != x0);
-            b = my_table[x0];
+            int pos = kpos[(t & 1) * kKeys + lane];
+            int y = distance_place(pos, q_high, M), z = distance_place(pos, q_low, M), y0 = __builtin_amdgcn_readfirstlane(y);
+            plain = plain && !wave_any(y != y0 || z != y0);
+            b = my_table[y0];
         }
         plain = plain && !wave_any(size > a.score.most || __builtin_fmaf(size, a.score.slope, b) > m + 8.f);
         // p = 2^(w + shift), w = z times the polynomial of `near` (CAP) or z near[0]; the other way leaves y - m in z
@@ -123,50 +123,56 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
         float shrink = 1.f;
         if (!plain) {
             const bool edge = (t + 1) * kKeys > least;  // some row does not see all of the tile
-            const int *kpt = kpos + (t & 3) * kKeys;
+            const int *kpt = kpos + (t & 1) * kKeys;
             float top = kLowest;
 #pragma unroll
-            for (int r = 0; r < 16; r++) {
-                const int at = 8 * (r / 4) + 4 * half + r % 4;
-                float y;
-                if (CAP) y = __builtin_fmaf(-2.f * a.score.c, rcp_fast(exp2_fast(s[r] * a.score.k) + 1.f), a.score.c);
-                else y = s[r] * a.score.k;
-                if (BIAS) y += my_table[distance_place(kpt[at], q_pos, M)];
-                if (edge) y = t * kKeys + at < seen ? y : -INFINITY;
-                s[r] = y;
-                top = fmaxf(top, y);
-            }
+            for (int u = 0; u < 2; u++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) {
+                    const int at = 32 * u + 8 * (r / 4) + 4 * half + r % 4;
+                    float y;
+                    if (CAP) y = __builtin_fmaf(-2.f * a.score.c, rcp_fast(exp2_fast(s[u][r] * a.score.k) + 1.f), a.score.c);
+                    else y = s[u][r] * a.score.k;
+                    if (BIAS) y += my_table[distance_place(kpt[at], q_pos, M)];
+                    if (edge) y = t * kKeys + at < seen ? y : -INFINITY;
+                    s[u][r] = y;
+                    top = fmaxf(top, y);
+                }
             top = halves_max(top);
             const float up = fmaxf(m, top);
             shrink = exp2_fast(m - up);
             m = up;
             l *= shrink;
 #pragma unroll
-            for (int r = 0; r < 16; r++) {  // (2^-1e15 is 0; its square is finite, where that of the infinity of a hidden key is not)
-                s[r] -= m;
-                if (CAP) s[r] = s[r] < -1e15f ? -1e15f : s[r];
-            }
+            for (int u = 0; u < 2; u++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) {  // (2^-1e15 is 0; its square is finite, where that of the infinity of a hidden key is not)
+                    s[u][r] -= m;
+                    if (CAP) s[u][r] = s[u][r] < -1e15f ? -1e15f : s[u][r];
+                }
             shift = 0.f, near0 = 1.f, near1 = near2 = near3 = 0.f;
         }
         const unsigned kt = my_rows + buffer(t + 1), vt = my_columns + buffer(t - 1);
-        constexpr int kAll = 2 * kSteps, kAhead = 3, kEach = 16 / kAll;
+        constexpr int kAll = 4 * kSteps, kAhead = 3, kEach = 32 / kAll;
         Chunk piece[4];
         auto piece_of = [&](int at) {
-            return at < kSteps ? rows_chunk<E>(kt, at) : columns_chunk<E, DP>(vt, ((at - kSteps) & 1) * 16, (at - kSteps) >> 1);
+            if (at < 2 * kSteps) return rows_chunk<E>(kt + (at & 1) * 32 * DP * 2, at >> 1);
+            const int i = at - 2 * kSteps;
+            return columns_chunk<E, DP>(vt, 16 * (i / kOut), i % kOut);
         };
 #pragma unroll
         for (int i = 0; i < kAhead; i++) piece[i] = piece_of(i);
-        f32x16 next = zero16();
+        f32x16 next[2] = {zero16(), zero16()};
         float top = 0.f;
 #pragma unroll
         for (int at = 0; at < kAll; at++) {
             __builtin_amdgcn_sched_barrier(0);
             if (at + kAhead < kAll) piece[(at + kAhead) & 3] = piece_of(at + kAhead);
-            if (at < kSteps) next = mfma(piece[at & 3], q[at], next);  // (behind the last tile: of what the buffer holds, not used)
-            else o[(at - kSteps) >> 1] = mfma(piece[at & 3], (at - kSteps) & 1 ? p1 : p0, o[(at - kSteps) >> 1]);
+            if (at < 2 * kSteps) next[at & 1] = mfma(piece[at & 3], q[at >> 1], next[at & 1]);  // (behind the last tile: of what the buffer holds, not used)
+            else o[(at - 2 * kSteps) % kOut] = mfma(piece[at & 3], p[(at - 2 * kSteps) / kOut], o[(at - 2 * kSteps) % kOut]);
 #pragma unroll
             for (int e = at * kEach; e < (at + 1) * kEach; e++) {
-                const float z = s[e];
+                const float z = s[e / 16][e % 16];
                 float y;
                 if (CAP) {
                     float zz = z * z;
@@ -177,15 +183,23 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
                 } else y = __builtin_fmaf(z, near0, shift);
                 y = exp2_fast(y);
                 here(y);
-                s[e] = y;
+                s[e / 16][e % 16] = y;
                 l += y;
             }
             here(l);
-            constexpr int kFrom = kSteps + kSteps / 4, kPer = (16 + kAll - kFrom - 1) / (kAll - kFrom);
+            constexpr int kFrom = 2 * kSteps + kSteps / 2, kPer = (32 + kAll - kFrom - 1) / (kAll - kFrom);
             if (at >= kFrom) {
 #pragma unroll
-                for (int e = (at - kFrom) * kPer; e < (at - kFrom + 1) * kPer && e < 16; e++) top = fmaxf(top, __builtin_fabsf(next[e]));
+                for (int e = (at - kFrom) * kPer; e < (at - kFrom + 1) * kPer && e < 32; e++) top = fmaxf(top, __builtin_fabsf(next[e / 16][e % 16]));
                 here(top);
+            }
+            if (at == 0) {
+                kload.store(tiles + buffer(t), x);  // K of t + 2, where that of t was (read in the last round)
+                vload.load(x);
+            }
+            if (at == kAll / 2 + 2) {
+                vload.store(tiles + 2 * kTile + buffer(t), x);  // V of t, where that of t - 2 was
+                kload.load(x);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -194,18 +208,22 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
             for (int i = 0; i < kOut; i++) o[i] *= shrink;
         }
         size = top;
-        p0 = rounded8<E, 0>(s);
-        p1 = rounded8<E, 1>(s);
-        s = next;
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            p[2 * u] = rounded8<E, 0>(s[u]);
+            p[2 * u + 1] = rounded8<E, 1>(s[u]);
+            s[u] = next[u];
+        }
         __syncthreads();
+        if (BIAS) {
+            stage_pos(t + 2);  // (tile t's have been read; seen from the barrier of the next round on)
+            fetch_pos(t + 3);
+        }
     }
     if (tiles_n > 0) {
         const unsigned vt = my_columns + buffer(tiles_n - 1);
 #pragma unroll
-        for (int i = 0; i < kOut; i++) {
-            o[i] = mfma(columns_chunk<E, DP>(vt, 0, i), p0, o[i]);
-            o[i] = mfma(columns_chunk<E, DP>(vt, 16, i), p1, o[i]);
-        }
+        for (int i = 0; i < 4 * kOut; i++) o[i % kOut] = mfma(columns_chunk<E, DP>(vt, 16 * (i / kOut), i % kOut), p[i / kOut], o[i % kOut]);
     }
     l = halves_sum(l);
     if (!mine) return;
@@ -278,7 +296,7 @@ logoskg_status attend_args(const logoskg_attention *a, AttArgs *o, const char *c
 }
 
 template <class E, int DP, bool CAP, bool BIAS> static logoskg_status launch_attend(const AttArgs &a, hipStream_t st) {
-    size_t bytes = 8 * kKeys * DP * 2 + 4 * kKeys * 4 + (BIAS ? (size_t)a.group * (2 * a.score.max_distance + 1) * 4 : 0);
+    size_t bytes = 4 * kKeys * DP * 2 + 2 * kKeys * 4 + (BIAS ? (size_t)a.group * (2 * a.score.max_distance + 1) * 4 : 0);
     LKG_TRY(allow_lds(k_attend<E, DP, CAP, BIAS>, bytes));
     k_attend<E, DP, CAP, BIAS><<<dim3((unsigned)(a.row_blocks * a.kv_heads)), kAttThreads, bytes, st>>>(a);
     LKG_HIP(hipGetLastError());

@@ -138,15 +138,15 @@ __global__ __launch_bounds__(kAttThreads, DP == 128 ? 1 : 2) void k_att_dq(AttAr
     float size = 0.f, lacks = 0.f;
 
     TileLoad<kGradTile, DP> kload, vload;
-    const unsigned k_bytes = (unsigned)a.k_row * 2, v_bytes = (unsigned)a.v_row * 2;
-    kload.begin(k_bytes, a.dim, tid);
-    vload.begin(v_bytes, a.dim, tid);
+    kload.begin(kbase, (unsigned)a.k_row * 2, 0, doc.keys, a.dim, tid);
+    vload.begin(vbase, (unsigned)a.v_row * 2, 0, doc.keys, a.dim, tid);
+    u32x4 kx[TileLoad<kGradTile, DP>::kChunks], vx[TileLoad<kGradTile, DP>::kChunks];
     const unsigned tiles = lds_place(lds), my_rows = rows_place<DP>(lane) + tiles, my_columns = columns_place<DP>(lane) + tiles;
     auto buffer = [](int t) { return (unsigned)(t & 3) * 2 * kTile; };
     int kp = 0;
     auto fetch = [&](int t) {
-        kload.load(kbase, k_bytes, t * kGradTile, doc.keys, a.dim);
-        vload.load(vbase, v_bytes, t * kGradTile, doc.keys, a.dim);
+        kload.load(kx);
+        vload.load(vx);
         if (BIAS && tid < kGradTile) {
             int j = t * kGradTile + tid;
             j = j < doc.keys ? j : doc.keys - 1;
@@ -154,8 +154,8 @@ __global__ __launch_bounds__(kAttThreads, DP == 128 ? 1 : 2) void k_att_dq(AttAr
         }
     };
     auto stage = [&](int t) {
-        kload.store(tiles + buffer(t));
-        vload.store(tiles + buffer(t) + kTile);
+        kload.store(tiles + buffer(t), kx);
+        vload.store(tiles + buffer(t) + kTile, vx);
         if (BIAS && tid < kGradTile) kpos[(t & 3) * kGradTile + tid] = kp;
     };
     const int tiles_n = (most + kGradTile - 1) / kGradTile;
@@ -343,16 +343,21 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
 
     TileLoad<kGradTile, DP> qload, oload;
     const unsigned q_bytes = (unsigned)a.q_row * 2, o_bytes = (unsigned)a.heads * a.dim * 2;
-    qload.begin(q_bytes, a.dim, tid);
-    oload.begin(o_bytes, a.dim, tid);
+    qload.begin((const char *)a.q, q_bytes, 0, 0, a.dim, tid);
+    oload.begin((const char *)a.dout, o_bytes, 0, 0, a.dim, tid);
+    u32x4 qx[TileLoad<kGradTile, DP>::kChunks], ox[TileLoad<kGradTile, DP>::kChunks];
     const unsigned tiles = lds_place(lds), my_rows = rows_place<DP>(lane) + tiles, my_columns = columns_place<DP>(lane) + tiles;
     auto buffer = [](int t) { return (unsigned)(t & 3) * 2 * kTile; };
     float my_lse = 0.f, my_delta = 0.f;
     int my_pos = 0, fetch_g = 0, fetch_at = 0;
     auto fetch = [&]() {  // the next tile
         const int h = head * G + fetch_g, r0 = from + fetch_at * kGradTile;
-        qload.load((const char *)a.q + (doc.row0 * a.q_row + (long long)h * a.q_head) * 2, q_bytes, r0, doc.rows, a.dim);
-        oload.load((const char *)a.dout + (doc.row0 * a.heads + h) * a.dim * 2, o_bytes, r0, doc.rows, a.dim);
+        if (fetch_at == 0) {
+            qload.go_to((const char *)a.q + (doc.row0 * a.q_row + (long long)h * a.q_head) * 2, r0, doc.rows, a.dim);
+            oload.go_to((const char *)a.dout + (doc.row0 * a.heads + h) * a.dim * 2, r0, doc.rows, a.dim);
+        }
+        qload.load(qx);
+        oload.load(ox);
         if (tid < kGradTile) {
             const int row = r0 + tid;
             const bool in = row < doc.rows;
@@ -368,8 +373,8 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
         if (++fetch_at == per) fetch_at = 0, fetch_g++;
     };
     auto stage = [&](int t) {
-        qload.store(tiles + buffer(t));
-        oload.store(tiles + buffer(t) + kTile);
+        qload.store(tiles + buffer(t), qx);
+        oload.store(tiles + buffer(t) + kTile, ox);
         if (tid < kGradTile) {
             const int at = (t & 3) * kGradTile + tid;
             lses[at] = my_lse;
