@@ -21,9 +21,9 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     typedef typename Vec8<E>::type Chunk;
     constexpr int kTile = kKeys * DP * 2, kSteps = DP / 16, kOut = DP / 32;
-    int *kpos = (int *)(lds + 4 * kTile);              // [2][kKeys]  (LDS begins with K, K, V, V)
-    float *table = (float *)(kpos + 2 * kKeys);        // [group][2 M + 1]
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    int *kpos = (int *)(lds + 4 * kTile);              // [4][kKeys]  (LDS begins with K, K, V, V)
+    float *table = (float *)(kpos + 4 * kKeys);        // [group][2 M + 1]
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
     const int head = blockIdx.x % a.kv_heads;
     const long long block = a.row_blocks - 1 - blockIdx.x / a.kv_heads;  // the last rows of a document see most: first
     const int d = document_of(a.q_off, a.num_docs, a.num_rows, a.group, kAttRowsShift, block, lane);
@@ -49,11 +49,13 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
     for (int kk = 0; kk < kSteps; kk++) q[kk] = row_chunk<E>(qrow, mine, kk, a.dim, lane);
     const int M = a.score.max_distance;
     const float *my_table = table + g * (2 * M + 1);
-    int q_pos = 0, q_low = 0, q_high = 0;  // of the row, and the wavefront's lowest and highest
+    int q_low = 0, q_high = 0;  // the wavefront's lowest and highest position
+    Places places = {0, 0, 0};
     if (BIAS) {
-        q_pos = a.q_pos ? a.q_pos[doc.row0 + row] : row + doc.keys - doc.rows;
-        q_low = wave_min(q_pos);
-        q_high = wave_max(q_pos);
+        const int q_pos = a.q_pos ? a.q_pos[doc.row0 + row] : row + doc.keys - doc.rows;
+        places = places_of_keys(q_pos, M, lds_place(my_table));
+        q_low = __builtin_amdgcn_readfirstlane(wave_min(q_pos));
+        q_high = __builtin_amdgcn_readfirstlane(wave_max(q_pos));
         bias_to_lds<E>(table, a.score, head * a.group, a.group, tid, kAttThreads);
     }
 
@@ -83,7 +85,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
         }
     };
     auto stage_pos = [&](int t) {
-        if (BIAS && tid < kKeys) kpos[(t & 1) * kKeys + tid] = kp;
+        if (BIAS && tid < kKeys) kpos[(t & 3) * kKeys + tid] = kp;
     };
     // Round t makes the scores of tile t + 1 and the output of tile t - 1.  K of tile t + 2 and V of tile t come in meanwhile,
     // one after the other through the same registers.
@@ -98,6 +100,8 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
         stage_pos(1);
         kload.load(x);
         fetch_pos(2);
+        stage_pos(2);
+        fetch_pos(3);
         vload.clear(tiles + 2 * kTile + buffer(1));  // (round 0 multiplies it with zeros)
         __syncthreads();
 #pragma unroll
@@ -108,68 +112,98 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
         for (int r = 0; r < 32; r++) size = fmaxf(size, __builtin_fabsf(s[r / 16][r % 16]));
         __syncthreads();
     }
+    // one bias for all distances of a tile? (the wavefront's keys, a lane each, from its lowest and its highest row)
+    bool varied = false;
+    float b = 0.f;
+    auto look_at = [&](int pos) {
+        const int y = distance_place(pos, q_high, M), z = distance_place(pos, q_low, M), y0 = __builtin_amdgcn_readfirstlane(y);
+        varied = wave_any(y != y0 || z != y0);
+        b = my_table[y0];
+    };
+    if (BIAS && tiles_n > 0) look_at(kpos[lane]);
     for (int t = 0; t < tiles_n; t++) {
-        bool plain = (t + 1) * kKeys <= least;
-        float b = 0.f;
-        if (BIAS) {  // one bias for all distances of the tile?
-            int pos = kpos[(t & 1) * kKeys + lane];
-            int y = distance_place(pos, q_high, M), z = distance_place(pos, q_low, M), y0 = __builtin_amdgcn_readfirstlane(y);
-            plain = plain && !wave_any(y != y0 || z != y0);
-            b = my_table[y0];
-        }
-        plain = plain && !wave_any(size > a.score.most || __builtin_fmaf(size, a.score.slope, b) > m + 8.f);
+        const bool edge = (t + 1) * kKeys > least;  // some row does not see all of the tile
+        const bool far = wave_any(size > a.score.most);
+        const bool plain = !edge && !far && !varied && !wave_any(__builtin_fmaf(size, a.score.slope, b) > m + 8.f);
         // p = 2^(w + shift), w = z times the polynomial of `near` (CAP) or z near[0]; the other way leaves y - m in z
         float shift = b - m, near0 = CAP ? a.score.near[0] : a.score.k, near1 = a.score.near[1], near2 = a.score.near[2], near3 = a.score.near[3];
         float shrink = 1.f;
         if (!plain) {
-            const bool edge = (t + 1) * kKeys > least;  // some row does not see all of the tile
-            const int *kpt = kpos + (t & 1) * kKeys;
+            const int *kpt = kpos + (t & 3) * kKeys;
             float top = kLowest;
+            if (!edge && !far) {
 #pragma unroll
-            for (int u = 0; u < 2; u++)
+                for (int u = 0; u < 2; u++)
 #pragma unroll
-                for (int r = 0; r < 16; r++) {
-                    const int at = 32 * u + 8 * (r / 4) + 4 * half + r % 4;
-                    float y;
-                    if (CAP) y = __builtin_fmaf(-2.f * a.score.c, rcp_fast(exp2_fast(s[u][r] * a.score.k) + 1.f), a.score.c);
-                    else y = s[u][r] * a.score.k;
-                    if (BIAS) y += my_table[distance_place(kpt[at], q_pos, M)];
-                    if (edge) y = t * kKeys + at < seen ? y : -INFINITY;
-                    s[u][r] = y;
-                    top = fmaxf(top, y);
-                }
+                    for (int r = 0; r < 16; r++) {
+                        float y = BIAS ? float_at(place_of_key(places, kpt[32 * u + 8 * (r / 4) + 4 * half + r % 4])) : 0.f;
+                        const float z = s[u][r];
+                        if (CAP) {
+                            const float zz = z * z;
+                            float w = __builtin_fmaf(zz, near3, near2);
+                            w = __builtin_fmaf(zz, w, near1);
+                            w = __builtin_fmaf(zz, w, near0);
+                            y = __builtin_fmaf(z, w, y);
+                        } else y = __builtin_fmaf(z, near0, y);
+                        s[u][r] = y;
+                        top = fmaxf(top, y);
+                    }
+            } else {
+#pragma unroll
+                for (int u = 0; u < 2; u++)
+#pragma unroll
+                    for (int r = 0; r < 16; r++) {
+                        const int at = 32 * u + 8 * (r / 4) + 4 * half + r % 4;
+                        float y;
+                        if (CAP) y = __builtin_fmaf(-2.f * a.score.c, rcp_fast(exp2_fast(s[u][r] * a.score.k) + 1.f), a.score.c);
+                        else y = s[u][r] * a.score.k;
+                        if (BIAS) y += float_at(place_of_key(places, kpt[at]));
+                        y = t * kKeys + at < seen ? y : -INFINITY;
+                        s[u][r] = y;
+                        top = fmaxf(top, y);
+                    }
+            }
             top = halves_max(top);
-            const float up = fmaxf(m, top);
-            shrink = exp2_fast(m - up);
-            m = up;
-            l *= shrink;
+            if (wave_any(top > m + 8.f)) {
+                const float up = fmaxf(m, top);
+                shrink = exp2_fast(m - up);
+                m = up;
+                l *= shrink;
+            }
 #pragma unroll
             for (int u = 0; u < 2; u++)
 #pragma unroll
-                for (int r = 0; r < 16; r++) {  // (2^-1e15 is 0; its square is finite, where that of the infinity of a hidden key is not)
-                    s[u][r] -= m;
-                    if (CAP) s[u][r] = s[u][r] < -1e15f ? -1e15f : s[u][r];
-                }
+                for (int r = 0; r < 16; r++) s[u][r] -= m;
+            if (CAP && (edge || far)) {  // (2^-1e15 is 0; its square is finite, where that of the infinity of a hidden key is not)
+#pragma unroll
+                for (int u = 0; u < 2; u++)
+#pragma unroll
+                    for (int r = 0; r < 16; r++) s[u][r] = s[u][r] < -1e15f ? -1e15f : s[u][r];
+            }
             shift = 0.f, near0 = 1.f, near1 = near2 = near3 = 0.f;
         }
         const unsigned kt = my_rows + buffer(t + 1), vt = my_columns + buffer(t - 1);
+        // First the output, whose weights' registers then take the new ones of the tile's first half, and the scores of the
+        // next tile those of this one's: everything fits 256 registers, two wavefronts to a unit.
         constexpr int kAll = 4 * kSteps, kAhead = 3, kEach = 32 / kAll;
         Chunk piece[4];
         auto piece_of = [&](int at) {
-            if (at < 2 * kSteps) return rows_chunk<E>(kt + (at & 1) * 32 * DP * 2, at >> 1);
-            const int i = at - 2 * kSteps;
-            return columns_chunk<E, DP>(vt, 16 * (i / kOut), i % kOut);
+            if (at < 2 * kSteps) return columns_chunk<E, DP>(vt, 16 * (at / kOut), at % kOut);
+            return rows_chunk<E>(kt + (at & 1) * 32 * DP * 2, (at - 2 * kSteps) >> 1);
         };
 #pragma unroll
         for (int i = 0; i < kAhead; i++) piece[i] = piece_of(i);
         f32x16 next[2] = {zero16(), zero16()};
-        float top = 0.f;
 #pragma unroll
         for (int at = 0; at < kAll; at++) {
             __builtin_amdgcn_sched_barrier(0);
+            if (at == 2 * kSteps) {
+                p[0] = rounded8<E, 0>(s[0]);
+                p[1] = rounded8<E, 1>(s[0]);
+            }
             if (at + kAhead < kAll) piece[(at + kAhead) & 3] = piece_of(at + kAhead);
-            if (at < 2 * kSteps) next[at & 1] = mfma(piece[at & 3], q[at >> 1], next[at & 1]);  // (behind the last tile: of what the buffer holds, not used)
-            else o[(at - 2 * kSteps) % kOut] = mfma(piece[at & 3], p[(at - 2 * kSteps) / kOut], o[(at - 2 * kSteps) % kOut]);
+            if (at < 2 * kSteps) o[at % kOut] = mfma(piece[at & 3], p[at / kOut], o[at % kOut]);
+            else next[at & 1] = mfma(piece[at & 3], q[(at - 2 * kSteps) >> 1], next[at & 1]);  // (behind the last tile: of what the buffer holds, not used)
 #pragma unroll
             for (int e = at * kEach; e < (at + 1) * kEach; e++) {
                 const float z = s[e / 16][e % 16];
@@ -187,12 +221,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
                 l += y;
             }
             here(l);
-            constexpr int kFrom = 2 * kSteps + kSteps / 2, kPer = (32 + kAll - kFrom - 1) / (kAll - kFrom);
-            if (at >= kFrom) {
-#pragma unroll
-                for (int e = (at - kFrom) * kPer; e < (at - kFrom + 1) * kPer && e < 32; e++) top = fmaxf(top, __builtin_fabsf(next[e / 16][e % 16]));
-                here(top);
-            }
+            if (BIAS && at == kAll / 4) look_at(kpos[((t + 1) & 3) * kKeys + lane]);
             if (at == 0) {
                 kload.store(tiles + buffer(t), x);  // K of t + 2, where that of t was (read in the last round)
                 vload.load(x);
@@ -207,17 +236,17 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
 #pragma unroll
             for (int i = 0; i < kOut; i++) o[i] *= shrink;
         }
-        size = top;
+        p[2] = rounded8<E, 0>(s[1]);
+        p[3] = rounded8<E, 1>(s[1]);
+        s[0] = next[0];
+        s[1] = next[1];
+        size = 0.f;
 #pragma unroll
-        for (int u = 0; u < 2; u++) {
-            p[2 * u] = rounded8<E, 0>(s[u]);
-            p[2 * u + 1] = rounded8<E, 1>(s[u]);
-            s[u] = next[u];
-        }
+        for (int r = 0; r < 32; r++) size = fmaxf(size, __builtin_fabsf(s[r / 16][r % 16]));
         __syncthreads();
         if (BIAS) {
-            stage_pos(t + 2);  // (tile t's have been read; seen from the barrier of the next round on)
-            fetch_pos(t + 3);
+            stage_pos(t + 3);  // (seen from the barrier of the next round on)
+            fetch_pos(t + 4);
         }
     }
     if (tiles_n > 0) {
@@ -296,7 +325,7 @@ logoskg_status attend_args(const logoskg_attention *a, AttArgs *o, const char *c
 }
 
 template <class E, int DP, bool CAP, bool BIAS> static logoskg_status launch_attend(const AttArgs &a, hipStream_t st) {
-    size_t bytes = 4 * kKeys * DP * 2 + 2 * kKeys * 4 + (BIAS ? (size_t)a.group * (2 * a.score.max_distance + 1) * 4 : 0);
+    size_t bytes = 4 * kKeys * DP * 2 + 4 * kKeys * 4 + (BIAS ? (size_t)a.group * (2 * a.score.max_distance + 1) * 4 : 0);
     LKG_TRY(allow_lds(k_attend<E, DP, CAP, BIAS>, bytes));
     k_attend<E, DP, CAP, BIAS><<<dim3((unsigned)(a.row_blocks * a.kv_heads)), kAttThreads, bytes, st>>>(a);
     LKG_HIP(hipGetLastError());

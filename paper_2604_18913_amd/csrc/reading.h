@@ -204,10 +204,28 @@ template <class E> __device__ __forceinline__ void bias_to_lds(float *table, con
     }
 }
 
-__device__ __forceinline__ int distance_place(int k_pos, int q_pos, int M) {
-    int d = __builtin_elementwise_sub_sat(k_pos, q_pos);
-    return (d < -M ? -M : d > M ? M : d) + M;
+// Where a distance's entry stands in a table of 2 M + 1 words: one end of the distance is fixed (pos), the other, x, counts
+// with `sign`; clamped first, so that no difference leaves 32 bits.
+struct Places {
+    int lo, hi;     // x is taken into these
+    unsigned base;  // of a table of words in LDS: the entry of x is at base + 4 x (wrapping)
+};
+__device__ __forceinline__ int added(int a, int b) { return __builtin_elementwise_add_sat(a, b); }
+// of keys, for a row at q_pos: distance x - q_pos
+__device__ __forceinline__ Places places_of_keys(int q_pos, int M, unsigned table) {
+    return Places{added(q_pos, -M), added(q_pos, M), table + 4u * ((unsigned)M - (unsigned)q_pos)};
 }
+__device__ __forceinline__ int clamped(int x, int lo, int hi) { return __builtin_elementwise_min(__builtin_elementwise_max(x, lo), hi); }
+__device__ __forceinline__ unsigned place_of_key(const Places &p, int x) { return p.base + 4u * (unsigned)clamped(x, p.lo, p.hi); }
+// of rows, for a key at k_pos: distance k_pos - x
+__device__ __forceinline__ Places places_of_rows(int k_pos, int M, unsigned table) {
+    return Places{added(k_pos, -M), added(k_pos, M), table + 4u * ((unsigned)M + (unsigned)k_pos)};
+}
+__device__ __forceinline__ unsigned place_of_row(const Places &p, int x) { return p.base - 4u * (unsigned)clamped(x, p.lo, p.hi); }
+__device__ __forceinline__ float float_at(unsigned place) { return *(__attribute__((address_space(3))) const float *)(uintptr_t)place; }
+__device__ __forceinline__ int int_at(unsigned place) { return *(__attribute__((address_space(3))) const int *)(uintptr_t)place; }
+
+__device__ __forceinline__ int distance_place(int k_pos, int q_pos, int M) { return clamped(__builtin_elementwise_sub_sat(k_pos, q_pos), -M, M) + M; }
 
 template <class F> logoskg_status allow_lds(F *kernel, size_t bytes) {
     if (bytes > (64 << 10)) LKG_HIP(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
