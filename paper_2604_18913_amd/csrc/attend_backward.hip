@@ -78,21 +78,22 @@ template <bool CAP> __device__ __forceinline__ void exact_score(const AttArgs &a
     }
 }
 constexpr float kHidden = -1e15f;      // 2^this is 0, and its square finite
-constexpr float kHiddenLse = 1e30f;    // of a row that sees nothing: p = 0
+constexpr float kHiddenLse = 1e15f;    // of a row that sees nothing, or is none: p = 0 the same way
 
 // ---------------------------------------------------------------- dQ
-// One block: 128 rows as in the forward, keys in tiles of 32 through a ring of four buffers.
-constexpr int kGradTile = 32;
+// One block: 128 rows as in the forward, keys in tiles of 64: K through a ring of four buffers (read by rows for the next
+// tile's scores, by columns for the last tile's dQ), V through two.
+constexpr int kGradTile = 64;
 
 template <class E, int DP, bool CAP, bool BIAS>
-__global__ __launch_bounds__(kAttThreads, DP == 128 ? 1 : 2) void k_att_dq(AttArgs a) {
+__global__ __launch_bounds__(kAttThreads, 1) void k_att_dq(AttArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     typedef typename Vec8<E>::type Chunk;
-    constexpr int kTile = kGradTile * DP * 2, kSteps = DP / 16, kOut = DP / 32;
-    int *kpos = (int *)(lds + 8 * kTile);       // [4][kGradTile]
+    constexpr int kTile = kGradTile * DP * 2, kSteps = DP / 16, kOut = DP / 32, kUnder = 32 * DP * 2;  // kUnder: to a tile's second 32 rows
+    int *kpos = (int *)(lds + 6 * kTile);       // [4][kGradTile]  (LDS begins with four buffers of K, two of V)
     float *table = (float *)(kpos + 4 * kGradTile);
     const int M = a.score.max_distance, G = a.group;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
     const int head = blockIdx.x % a.kv_heads;
     const long long block = a.row_blocks - 1 - blockIdx.x / a.kv_heads;
     const int d = document_of(a.q_off, a.num_docs, a.num_rows, G, kAttRowsShift, block, lane);
@@ -122,19 +123,23 @@ __global__ __launch_bounds__(kAttThreads, DP == 128 ? 1 : 2) void k_att_dq(AttAr
     lse = lse == -INFINITY ? kHiddenLse : lse * kLog2e;
     const float delta = mine ? a.delta[place] : 0.f;
     const float *my_table = table + g * (2 * M + 1);
-    int q_pos = 0, q_low = 0, q_high = 0;
+    int q_low = 0, q_high = 0;
+    Places places = {0, 0, 0};
     if (BIAS) {
-        q_pos = a.q_pos ? a.q_pos[doc.row0 + row] : row + doc.keys - doc.rows;
-        q_low = wave_min(q_pos);
-        q_high = wave_max(q_pos);
+        const int q_pos = a.q_pos ? a.q_pos[doc.row0 + row] : row + doc.keys - doc.rows;
+        places = places_of_keys(q_pos, M, lds_place(my_table));
+        q_low = __builtin_amdgcn_readfirstlane(wave_min(q_pos));
+        q_high = __builtin_amdgcn_readfirstlane(wave_max(q_pos));
         bias_to_lds<E>(table, a.score, head * G, G, tid, kAttThreads);
     }
     const char *kbase = (const char *)a.k + (doc.key0 * a.k_row + (long long)head * a.k_head) * 2;
     const char *vbase = (const char *)a.v + (doc.key0 * a.v_row + (long long)head * a.v_head) * 2;
-    f32x16 dq[kOut], s = zero16(), dp = zero16();
+    f32x16 dq[kOut], s[2] = {zero16(), zero16()}, dp[2] = {zero16(), zero16()};
 #pragma unroll
     for (int i = 0; i < kOut; i++) dq[i] = zero16();
-    Chunk z0 = as8<E>(u32x4{0, 0, 0, 0}), z1 = z0;
+    Chunk z[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) z[i] = as8<E>(u32x4{0, 0, 0, 0});
     float size = 0.f, lacks = 0.f;
 
     TileLoad<kGradTile, DP> kload, vload;
@@ -142,118 +147,140 @@ __global__ __launch_bounds__(kAttThreads, DP == 128 ? 1 : 2) void k_att_dq(AttAr
     vload.begin(vbase, (unsigned)a.v_row * 2, 0, doc.keys, a.dim, tid);
     u32x4 kx[TileLoad<kGradTile, DP>::kChunks], vx[TileLoad<kGradTile, DP>::kChunks];
     const unsigned tiles = lds_place(lds), my_rows = rows_place<DP>(lane) + tiles, my_columns = columns_place<DP>(lane) + tiles;
-    auto buffer = [](int t) { return (unsigned)(t & 3) * 2 * kTile; };
+    auto k_buffer = [](int t) { return (unsigned)(t & 3) * kTile; };
+    auto v_buffer = [](int t) { return (unsigned)(4 + (t & 1)) * kTile; };
     int kp = 0;
     auto fetch = [&](int t) {
         kload.load(kx);
         vload.load(vx);
-        if (BIAS && tid < kGradTile) {
-            int j = t * kGradTile + tid;
+        if (BIAS && wave == 0) {
+            int j = t * kGradTile + lane;
             j = j < doc.keys ? j : doc.keys - 1;
             kp = a.k_pos && doc.keys > 0 ? a.k_pos[doc.key0 + j] : j;
         }
     };
     auto stage = [&](int t) {
-        kload.store(tiles + buffer(t), kx);
-        vload.store(tiles + buffer(t) + kTile, vx);
-        if (BIAS && tid < kGradTile) kpos[(t & 3) * kGradTile + tid] = kp;
+        kload.store(tiles + k_buffer(t), kx);
+        vload.store(tiles + v_buffer(t), vx);
+        if (BIAS && wave == 0) kpos[(t & 3) * kGradTile + lane] = kp;
+    };
+    bool varied = false;
+    float b = 0.f;
+    auto look_at = [&](int pos) {  // one bias for all distances of a tile?
+        const int y = distance_place(pos, q_high, M), w = distance_place(pos, q_low, M), y0 = __builtin_amdgcn_readfirstlane(y);
+        varied = wave_any(y != y0 || w != y0);
+        b = my_table[y0];
     };
     const int tiles_n = (most + kGradTile - 1) / kGradTile;
     if (tiles_n > 0) {
         fetch(0);
         stage(0);
-        if (tiles_n > 1) fetch(1), stage(1);
-        if (tiles_n > 2) fetch(2);
-        kload.clear(tiles + buffer(3));  // (round 0 multiplies it with zeros)
+        fetch(1);
+        stage(1);
+        fetch(2);
+        kload.clear(tiles + k_buffer(3));  // (round 0 multiplies it with zeros)
         __syncthreads();
 #pragma unroll
-        for (int kk = 0; kk < kSteps; kk++) {
-            s = mfma(rows_chunk<E>(my_rows, kk), q[kk], s);
-            dp = mfma(rows_chunk<E>(my_rows + kTile, kk), o[kk], dp);
+        for (int i = 0; i < 2 * kSteps; i++) {
+            s[i & 1] = mfma(rows_chunk<E>(my_rows + (i & 1) * kUnder, i >> 1), q[i >> 1], s[i & 1]);
+            dp[i & 1] = mfma(rows_chunk<E>(my_rows + v_buffer(0) + (i & 1) * kUnder, i >> 1), o[i >> 1], dp[i & 1]);
         }
 #pragma unroll
-        for (int r = 0; r < 16; r++) size = fmaxf(size, __builtin_fabsf(s[r]));
+        for (int r = 0; r < 32; r++) size = fmaxf(size, __builtin_fabsf(s[r / 16][r % 16]));
+        if (BIAS) look_at(kpos[lane]);
+        __syncthreads();
     }
     for (int t = 0; t < tiles_n; t++) {
-        if (t + 2 < tiles_n) stage(t + 2);
-        if (t + 3 < tiles_n) fetch(t + 3);
-        bool plain = (t + 1) * kGradTile <= least && !wave_any(size > a.score.most);
-        float b = 0.f;
-        if (BIAS) {
-            int pos = kpos[(t & 3) * kGradTile + (lane & 31)];
-            int x = distance_place(pos, q_high, M), y = distance_place(pos, q_low, M), x0 = __builtin_amdgcn_readfirstlane(x);
-            plain = plain && !wave_any(x != x0 || y != x0);
-            b = my_table[x0];
-        }
+        const bool edge = (t + 1) * kGradTile > least, far = wave_any(size > a.score.most), plain = !edge && !far && !varied;
         Steps x = plain_steps<CAP>(a, b);
         if (!plain) {
-            const bool edge = (t + 1) * kGradTile > least;
             const int *kpt = kpos + (t & 3) * kGradTile;
+            if (!edge && !far) {
 #pragma unroll
-            for (int r = 0; r < 16; r++) {
-                const int at = 8 * (r / 4) + 4 * half + r % 4;
-                float y, slope;
-                exact_score<CAP>(a, s[r], y, slope);
-                if (BIAS) y += my_table[distance_place(kpt[at], q_pos, M)];
-                y -= lse;
-                float away = dp[r] - delta;
-                if (edge && t * kGradTile + at >= seen) y = kHidden, away = 0.f;
-                lacks = __builtin_fmaf(exp2_fast(y), away, lacks);
-                dp[r] = away * slope;
-                s[r] = y < kHidden ? kHidden : y;
+                for (int u = 0; u < 2; u++)
+#pragma unroll
+                    for (int r = 0; r < 16; r++) {
+                        float y = float_at(place_of_key(places, kpt[32 * u + 8 * (r / 4) + 4 * half + r % 4])) - lse;
+                        const float away = dp[u][r] - delta, w = element_w<CAP>(x, s[u][r]);
+                        y = CAP ? y + w : __builtin_fmaf(w, x.near0, y);
+                        lacks = __builtin_fmaf(exp2_fast(y), away, lacks);
+                        dp[u][r] = element_dz<CAP>(x, away, w);
+                        s[u][r] = y;
+                    }
+            } else {
+#pragma unroll
+                for (int u = 0; u < 2; u++)
+#pragma unroll
+                    for (int r = 0; r < 16; r++) {
+                        const int at = 32 * u + 8 * (r / 4) + 4 * half + r % 4;
+                        float y, slope;
+                        exact_score<CAP>(a, s[u][r], y, slope);
+                        if (BIAS) y += float_at(place_of_key(places, kpt[at]));
+                        y -= lse;
+                        float away = dp[u][r] - delta;
+                        if (t * kGradTile + at >= seen) y = kHidden, away = 0.f;
+                        lacks = __builtin_fmaf(exp2_fast(y), away, lacks);
+                        dp[u][r] = away * slope;
+                        s[u][r] = y < kHidden ? kHidden : y;
+                    }
             }
             x = special_steps();
         }
-        const unsigned kt = my_rows + buffer(t + 1), ct = my_columns + buffer(t - 1);
-        constexpr int kAll = 3 * kSteps, kAhead = 3;
-        Chunk piece[4];
+        const unsigned kt = my_rows + k_buffer(t + 1), vt = my_rows + v_buffer(t + 1), ct = my_columns + k_buffer(t - 1);
+        constexpr int kAll = 6 * kSteps, kAhead = 4;
+        Chunk piece[8];
         auto piece_of = [&](int at) {
-            return at < kSteps ? rows_chunk<E>(kt, at) : at < 2 * kSteps ? rows_chunk<E>(kt + kTile, at - kSteps)
-                                                                         : columns_chunk<E, DP>(ct, ((at - 2 * kSteps) & 1) * 16, (at - 2 * kSteps) >> 1);
+            if (at < 2 * kSteps) return columns_chunk<E, DP>(ct, 16 * (at / kOut), at % kOut);
+            const int i = at - 2 * kSteps;  // four chains, one after the other: scores and dP of either half
+            return rows_chunk<E>((i & 1 ? vt : kt) + (i >> 1 & 1) * kUnder, i >> 2);
         };
 #pragma unroll
         for (int i = 0; i < kAhead; i++) piece[i] = piece_of(i);
-        f32x16 next_s = zero16(), next_dp = zero16();
-        float top = 0.f, sum = 0.f;
-#pragma unroll
-        for (int at = 0; at < kAll; at++) {
+        f32x16 next_s[2] = {zero16(), zero16()}, next_dp[2] = {zero16(), zero16()};
+        float sum = 0.f;
+        in_turn<kAll>([&](auto step) __attribute__((always_inline)) {
+            constexpr int at = decltype(step)::value;
             __builtin_amdgcn_sched_barrier(0);
-            if (at + kAhead < kAll) piece[(at + kAhead) & 3] = piece_of(at + kAhead);
-            if (at < kSteps) next_s = mfma(piece[at & 3], q[at], next_s);
-            else if (at < 2 * kSteps) next_dp = mfma(piece[at & 3], o[at - kSteps], next_dp);
-            else dq[(at - 2 * kSteps) >> 1] = mfma(piece[at & 3], (at & 1) ? z1 : z0, dq[(at - 2 * kSteps) >> 1]);
+            if (at + kAhead < kAll) piece[(at + kAhead) & 7] = piece_of(at + kAhead);
+            if (at < 2 * kSteps) dq[at % kOut] = mfma(piece[at & 7], z[at / kOut], dq[at % kOut]);
+            else {
+                const int i = at - 2 * kSteps, u = i >> 1 & 1;
+                if (i & 1) next_dp[u] = mfma(piece[at & 7], o[i >> 2], next_dp[u]);
+                else next_s[u] = mfma(piece[at & 7], q[i >> 2], next_s[u]);
+            }
 #pragma unroll
-            for (int e = 16 * at / kAll; e < 16 * (at + 1) / kAll; e++) {
-                const float w = element_w<CAP>(x, s[e]), p = element_p<CAP>(x, w, lse), dy = element_dy<CAP>(x, p, dp[e], delta);
+            for (int e = 32 * at / kAll; e < 32 * (at + 1) / kAll; e++) {
+                const float w = element_w<CAP>(x, s[e / 16][e % 16]), p = element_p<CAP>(x, w, lse), dy = element_dy<CAP>(x, p, dp[e / 16][e % 16], delta);
                 sum += dy;
                 float dz = element_dz<CAP>(x, dy, w);
                 here(dz);
-                dp[e] = dz;
+                dp[e / 16][e % 16] = dz;
             }
             here(sum);
-            constexpr int kFrom = 2 * kSteps, kPer = 16 / kSteps;
-            if (at >= kFrom) {
-#pragma unroll
-                for (int e = (at - kFrom) * kPer; e < (at - kFrom + 1) * kPer; e++) top = fmaxf(top, __builtin_fabsf(next_s[e]));
-                here(top);
+            if (BIAS && at == kAll / 4) look_at(kpos[((t + 1) & 3) * kGradTile + lane]);
+            if (at == kAll / 2) {
+                stage(t + 2);  // (its buffers: of K of t - 2, of V of t, read last in the round before)
+                fetch(t + 3);
             }
-        }
+        });
         __builtin_amdgcn_sched_barrier(0);
         if (plain) lacks += sum;
-        size = top;
-        z0 = rounded8<E, 0>(dp);
-        z1 = rounded8<E, 1>(dp);
-        s = next_s;
-        dp = next_dp;
+        size = 0.f;
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            z[2 * u] = rounded8<E, 0>(dp[u]);
+            z[2 * u + 1] = rounded8<E, 1>(dp[u]);
+            s[u] = next_s[u];
+            dp[u] = next_dp[u];
+        }
+#pragma unroll
+        for (int r = 0; r < 32; r++) size = fmaxf(size, __builtin_fabsf(s[r / 16][r % 16]));
         __syncthreads();
     }
     if (tiles_n > 0) {
-        const unsigned ct = my_columns + buffer(tiles_n - 1);
+        const unsigned ct = my_columns + k_buffer(tiles_n - 1);
 #pragma unroll
-        for (int i = 0; i < kOut; i++) {
-            dq[i] = mfma(columns_chunk<E, DP>(ct, 0, i), z0, dq[i]);
-            dq[i] = mfma(columns_chunk<E, DP>(ct, 16, i), z1, dq[i]);
-        }
+        for (int i = 0; i < 4 * kOut; i++) dq[i % kOut] = mfma(columns_chunk<E, DP>(ct, 16 * (i / kOut), i % kOut), z[i / kOut], dq[i % kOut]);
     }
     lacks = halves_sum(lacks);
     if (!mine) return;
@@ -265,31 +292,32 @@ __global__ __launch_bounds__(kAttThreads, DP == 128 ? 1 : 2) void k_att_dq(AttAr
         for (int r = 0; r < 4; r++) {
             int c = 32 * i + 8 * r + 4 * half;
             if (c >= a.dim) continue;
-            typename Vec4<E>::type x;
+            typename Vec4<E>::type y;
 #pragma unroll
-            for (int e = 0; e < 4; e++) x[e] = (E)dq[i][4 * r + e];
-            *(typename Vec4<E>::type *)(out + c) = x;
+            for (int e = 0; e < 4; e++) y[e] = (E)dq[i][4 * r + e];
+            *(typename Vec4<E>::type *)(out + c) = y;
         }
 }
 
 // ---------------------------------------------------------------- dK, dV, biases
 // One block: 128 keys of (document, key head), 32 per wavefront, key = lane, K and V in registers as the B of S = Q K^T and
-// dP = dO V^T.  The rows that see them pass in tiles of 32 of one head, one head of the group after the other, through a
-// ring of four buffers in LDS, where they are read by rows for these two products and by columns for dV^T += dO^T p and
-// dK^T += Q^T dz.  A lane adds its dy to its own column of [buckets][64] in LDS (no two lanes share an address, so the sums
-// have an order), a tile of one bias all at once; a head's columns are added up when its rows are through.
+// dP = dO V^T.  The rows that see them pass in tiles of 64 of one head, one head of the group after the other, through three
+// buffers in LDS, where they are read by rows for these two products and by columns for dV^T += dO^T p and dK^T += Q^T dz;
+// a round's first half is the last tile's columns, whose buffer then takes the tile after the next.  A key adds its dy to its
+// own column of [buckets][32] in LDS (no two lanes add to an address at a time, so the sums have an order), those of a tile
+// of one bias all at once; a head's columns are added up when its rows are through.
 template <class E, int DP, bool CAP, bool BIAS>
 __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     typedef typename Vec8<E>::type Chunk;
-    constexpr int kTile = kGradTile * DP * 2, kSteps = DP / 16, kOut = DP / 32;
-    const int G = a.group, M = a.score.max_distance, places = 2 * M + 1, nb = a.score.num_buckets;
-    float *lses = (float *)(lds + 8 * kTile), *deltas = lses + 4 * kGradTile;  // [4][kGradTile] of the rows
+    constexpr int kTile = kGradTile * DP * 2, kSteps = DP / 16, kOut = DP / 32, kUnder = 32 * DP * 2;
+    const int G = a.group, M = a.score.max_distance, places_n = 2 * M + 1, nb = a.score.num_buckets;
+    float *lses = (float *)(lds + 6 * kTile), *deltas = lses + 4 * kGradTile;  // [4][kGradTile] of the rows  (LDS begins with three times Q, dO)
     int *qpos = (int *)(deltas + 4 * kGradTile);
-    float *sums = (float *)(qpos + 4 * kGradTile);           // [4 wavefronts][nb][64]
-    int *column = (int *)(sums + (BIAS ? 4 * nb * 64 : 0));  // [places] where a distance's bucket begins
-    float *table = (float *)(column + (BIAS ? places : 0));  // [group][places]
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    float *sums = (float *)(qpos + 4 * kGradTile);           // [4 wavefronts][nb][32]
+    int *column = (int *)(sums + (BIAS ? 4 * nb * 32 : 0));  // [places_n] where a distance's bucket begins, in bytes
+    float *table = (float *)(column + (BIAS ? places_n : 0));  // [group][places_n]
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
     const int head = blockIdx.x % a.kv_heads;
     const long long block = blockIdx.x / a.kv_heads;  // the first keys of a document are seen by most rows: first
     const int d = document_of(a.k_off, a.num_docs, a.num_keys, 1, kAttRowsShift, block, lane);
@@ -312,25 +340,31 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
         k[kk] = row_chunk<E>(krow, mine, kk, a.dim, lane);
         v[kk] = row_chunk<E>(vrow, mine, kk, a.dim, lane);
     }
-    int k_pos = 0, k_low = 0, k_high = 0;
-    float *my_sums = sums + wave * nb * 64 + lane;
+    int k_low = 0, k_high = 0;
+    Places places = {0, 0, 0};  // in `column`; a head's biases lie the same way
+    const unsigned to_table = (unsigned)((char *)table - (char *)column), my_sums = lds_place(sums) + (wave * nb * 32 + (lane & 31)) * 4;
     if (BIAS) {
-        const int in = mine ? key : doc.keys - 1;
-        k_pos = a.k_pos ? a.k_pos[doc.key0 + in] : in;
-        k_low = wave_min(k_pos);
-        k_high = wave_max(k_pos);
+        const int in = mine ? key : doc.keys - 1, k_pos = a.k_pos ? a.k_pos[doc.key0 + in] : in;
+        places = places_of_rows(k_pos, M, lds_place(column));
+        k_low = __builtin_amdgcn_readfirstlane(wave_min(k_pos));
+        k_high = __builtin_amdgcn_readfirstlane(wave_max(k_pos));
         bias_to_lds<E>(table, a.score, head * G, G, tid, kAttThreads);
-        for (int i = tid; i < places; i += kAttThreads) {
+        for (int i = tid; i < places_n; i += kAttThreads) {
             int b = a.score.buckets[i];
-            column[i] = (b < 0 ? 0 : b >= nb ? nb - 1 : b) * 64;
+            column[i] = (b < 0 ? 0 : b >= nb ? nb - 1 : b) * 128;
         }
-        for (int i = tid; i < 4 * nb * 64; i += kAttThreads) sums[i] = 0.f;
+        for (int i = tid; i < 4 * nb * 32; i += kAttThreads) sums[i] = 0.f;
     }
+    auto add_at = [&](int bucket, float x) {
+        __hip_atomic_fetch_add((__attribute__((address_space(3))) float *)(uintptr_t)(my_sums + bucket), x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    };
 
-    f32x16 dk[kOut], dv[kOut], s = zero16(), dp = zero16();
+    f32x16 dk[kOut], dv[kOut], s[2] = {zero16(), zero16()}, dp[2] = {zero16(), zero16()};
 #pragma unroll
     for (int i = 0; i < kOut; i++) dk[i] = zero16(), dv[i] = zero16();
-    Chunk p0 = as8<E>(u32x4{0, 0, 0, 0}), p1 = p0, z0 = p0, z1 = p0;
+    Chunk p[4], z[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) p[i] = z[i] = as8<E>(u32x4{0, 0, 0, 0});
     float size = 0.f;
 
     const int kend = doc.keys < kb + kAttRows ? doc.keys : (int)kb + kAttRows;
@@ -342,24 +376,22 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
     const int per = (doc.rows - from + kGradTile - 1) / kGradTile, tiles_n = per * G;  // tiles of a head, of all
 
     TileLoad<kGradTile, DP> qload, oload;
-    const unsigned q_bytes = (unsigned)a.q_row * 2, o_bytes = (unsigned)a.heads * a.dim * 2;
-    qload.begin((const char *)a.q, q_bytes, 0, 0, a.dim, tid);
-    oload.begin((const char *)a.dout, o_bytes, 0, 0, a.dim, tid);
+    qload.begin((const char *)a.q, (unsigned)a.q_row * 2, 0, 0, a.dim, tid);
+    oload.begin((const char *)a.dout, (unsigned)a.heads * a.dim * 2, 0, 0, a.dim, tid);
     u32x4 qx[TileLoad<kGradTile, DP>::kChunks], ox[TileLoad<kGradTile, DP>::kChunks];
     const unsigned tiles = lds_place(lds), my_rows = rows_place<DP>(lane) + tiles, my_columns = columns_place<DP>(lane) + tiles;
-    auto buffer = [](int t) { return (unsigned)(t & 3) * 2 * kTile; };
     float my_lse = 0.f, my_delta = 0.f;
     int my_pos = 0, fetch_g = 0, fetch_at = 0;
-    auto fetch = [&]() {  // the next tile
-        const int h = head * G + fetch_g, r0 = from + fetch_at * kGradTile;
+    auto fetch = [&]() {  // the next tile (behind the last head's: rows that there are none of)
+        const int h = head * G + (fetch_g < G ? fetch_g : G - 1), r0 = fetch_g < G ? from + fetch_at * kGradTile : doc.rows;
         if (fetch_at == 0) {
             qload.go_to((const char *)a.q + (doc.row0 * a.q_row + (long long)h * a.q_head) * 2, r0, doc.rows, a.dim);
             oload.go_to((const char *)a.dout + (doc.row0 * a.heads + h) * a.dim * 2, r0, doc.rows, a.dim);
         }
         qload.load(qx);
         oload.load(ox);
-        if (tid < kGradTile) {
-            const int row = r0 + tid;
+        if (wave == 0) {
+            const int row = r0 + lane;
             const bool in = row < doc.rows;
             const long long at = in ? (doc.row0 + row) * a.heads + h : 0;
             const float lse = in ? a.lse[at] : -INFINITY;
@@ -372,32 +404,30 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
         }
         if (++fetch_at == per) fetch_at = 0, fetch_g++;
     };
-    auto stage = [&](int t) {
-        qload.store(tiles + buffer(t), qx);
-        oload.store(tiles + buffer(t) + kTile, ox);
-        if (tid < kGradTile) {
-            const int at = (t & 3) * kGradTile + tid;
+    auto stage = [&](int t, unsigned buffer) {
+        qload.store(tiles + buffer, qx);
+        oload.store(tiles + buffer + kTile, ox);
+        if (wave == 0) {
+            const int at = (t & 3) * kGradTile + lane;
             lses[at] = my_lse;
             deltas[at] = my_delta;
             if (BIAS) qpos[at] = my_pos;
         }
     };
-    // the columns of a head that is through: a bucket's 256 sums by 256 / nb threads, their parts by one
+    // the columns of a head that is through: a bucket's 128 sums by 256 / nb threads, their parts by one
     auto finish = [&](int g) {
         __syncthreads();
         int strands = kAttThreads / nb;
-        strands = strands > 16 ? 16 : strands;
-        const int b = tid % nb, st = tid / nb, n = 256 / strands;
+        strands = strands >= 16 ? 16 : strands >= 8 ? 8 : 4;
+        const int b = tid % nb, st = tid / nb, n = 128 / strands;
         float sum = 0.f;
         if (st < strands)
             for (int i = 0; i < n; i++) {  // (rotated by the bucket, so that neighbouring threads read other banks)
-                const int c = st * n + ((i + b) % n), w = c >> 6;
-                sum += sums[(w * nb + b) * 64 + (c & 63)];
+                const int c = st * n + ((i + b) & (n - 1));
+                sum += sums[((c >> 5) * nb + b) * 32 + (c & 31)];
             }
-        if (st == strands - 1)
-            for (int c = strands * n; c < 256; c++) sum += sums[((c >> 6) * nb + b) * 64 + (c & 63)];
         __syncthreads();
-        for (int i = tid; i < 4 * nb * 64; i += kAttThreads) sums[i] = 0.f;
+        for (int i = tid; i < 4 * nb * 32; i += kAttThreads) sums[i] = 0.f;
         __syncthreads();
         if (st < strands) sums[tid] = sum;
         __syncthreads();
@@ -409,114 +439,164 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
         if (st < strands) sums[tid] = 0.f;
         __syncthreads();
     };
+    bool varied = false;
+    float b = 0.f;
+    int bucket = 0;
+    auto look_at = [&](int pos, int g) {  // one bias for all distances of a tile? (rows of a head, a lane each)
+        const int y = distance_place(k_low, pos, M), w = distance_place(k_high, pos, M), y0 = __builtin_amdgcn_readfirstlane(y);
+        varied = wave_any(y != y0 || w != y0);
+        b = table[g * places_n + y0];
+        bucket = column[y0];
+    };
+    unsigned last = 4 * kTile, now = 0, after = 2 * kTile;  // buffers of the tiles t - 1, t, t + 1
     if (tiles_n > 0) {
         fetch();
-        stage(0);
-        if (tiles_n > 1) fetch(), stage(1);
-        if (tiles_n > 2) fetch();
-        qload.clear(tiles + buffer(3));  // (round 0 multiplies them with zeros)
-        oload.clear(tiles + buffer(3) + kTile);
+        stage(0, now);
+        fetch();
+        stage(1, after);
+        fetch();
+        qload.clear(tiles + last);  // (round 0 multiplies them with zeros)
+        oload.clear(tiles + last + kTile);
         __syncthreads();
 #pragma unroll
-        for (int kk = 0; kk < kSteps; kk++) {
-            s = mfma(rows_chunk<E>(my_rows, kk), k[kk], s);
-            dp = mfma(rows_chunk<E>(my_rows + kTile, kk), v[kk], dp);
+        for (int i = 0; i < 2 * kSteps; i++) {
+            s[i & 1] = mfma(rows_chunk<E>(my_rows + (i & 1) * kUnder, i >> 1), k[i >> 1], s[i & 1]);
+            dp[i & 1] = mfma(rows_chunk<E>(my_rows + kTile + (i & 1) * kUnder, i >> 1), v[i >> 1], dp[i & 1]);
         }
 #pragma unroll
-        for (int r = 0; r < 16; r++) size = fmaxf(size, __builtin_fabsf(s[r]));
+        for (int r = 0; r < 32; r++) size = fmaxf(size, __builtin_fabsf(s[r / 16][r % 16]));
+        if (BIAS) look_at(qpos[lane], 0);
+        __syncthreads();
     }
     int g = 0, at_tile = 0;  // of the tile in work
     for (int t = 0; t < tiles_n; t++) {
-        if (t + 2 < tiles_n) stage(t + 2);
-        if (t + 3 < tiles_n) fetch();
         const int r0 = from + at_tile * kGradTile;
-        const bool edge = doc.seen(r0, a.causal) < kend;
+        const bool edge = doc.seen(r0, a.causal) < kend, far = wave_any(size > a.score.most), plain = !edge && !far && !varied;
         const float *lse = lses + (t & 3) * kGradTile, *delta = deltas + (t & 3) * kGradTile;
-        const int *pos = qpos + (t & 3) * kGradTile;
-        bool plain = !edge && !wave_any(size > a.score.most);
-        float b = 0.f;
-        int x0 = 0;
-        const float *my_table = table + g * places;
-        if (BIAS) {
-            const int p = pos[lane & 31], x = distance_place(k_low, p, M), y = distance_place(k_high, p, M);
-            x0 = __builtin_amdgcn_readfirstlane(x);
-            plain = plain && !wave_any(x != x0 || y != x0);
-            b = my_table[x0];
-        }
+        const int bucket_now = bucket;
         Steps x = plain_steps<CAP>(a, b);
         if (!plain) {
+            const int *pos = qpos + (t & 3) * kGradTile;
+            const unsigned to_head = to_table + g * places_n * 4;
+            if (!edge && !far) {
 #pragma unroll
-            for (int r = 0; r < 16; r++) {
-                const int at = 8 * (r / 4) + 4 * half + r % 4;
-                float y, slope;
-                exact_score<CAP>(a, s[r], y, slope);
-                int apart = 0;
-                if (BIAS) {
-                    apart = distance_place(k_pos, pos[at], M);
-                    y += my_table[apart];
-                }
-                y -= lse[at];
-                float away = dp[r] - delta[at];
-                if (edge && key >= doc.seen(r0 + at, a.causal)) y = kHidden, away = 0.f;
-                if (BIAS && mine) __hip_atomic_fetch_add(my_sums + column[apart], exp2_fast(y) * away, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                dp[r] = away * slope;
-                s[r] = y < kHidden ? kHidden : y;
+                for (int u = 0; u < 2; u++)
+#pragma unroll
+                    for (int r = 0; r < 16; r++) {
+                        const int at = 32 * u + 8 * (r / 4) + 4 * half + r % 4;
+                        const unsigned place = place_of_row(places, pos[at]);
+                        float y = float_at(place + to_head) - lse[at];
+                        const float away = dp[u][r] - delta[at], w = element_w<CAP>(x, s[u][r]);
+                        y = CAP ? y + w : __builtin_fmaf(w, x.near0, y);
+                        const float dy = exp2_fast(y) * away;
+                        const int c = int_at(place);
+                        if (mine && half == 0) add_at(c, dy);
+                        if (mine && half == 1) add_at(c, dy);
+                        dp[u][r] = element_dz<CAP>(x, away, w);
+                        s[u][r] = y;
+                    }
+            } else {
+#pragma unroll
+                for (int u = 0; u < 2; u++)
+#pragma unroll
+                    for (int r = 0; r < 16; r++) {
+                        const int at = 32 * u + 8 * (r / 4) + 4 * half + r % 4;
+                        const unsigned place = BIAS ? place_of_row(places, pos[at]) : 0;
+                        float y, slope;
+                        exact_score<CAP>(a, s[u][r], y, slope);
+                        if (BIAS) y += float_at(place + to_head);
+                        y -= lse[at];
+                        float away = dp[u][r] - delta[at];
+                        if (key >= doc.seen(r0 + at, a.causal)) y = kHidden, away = 0.f;
+                        if (BIAS) {
+                            const float dy = exp2_fast(y) * away;
+                            const int c = int_at(place);
+                            if (mine && half == 0) add_at(c, dy);
+                            if (mine && half == 1) add_at(c, dy);
+                        }
+                        dp[u][r] = away * slope;
+                        s[u][r] = y < kHidden ? kHidden : y;
+                    }
             }
             x = special_steps();
         }
-        const unsigned rt = my_rows + buffer(t + 1), ct = my_columns + buffer(t - 1);
-        constexpr int kAll = 4 * kSteps, kAhead = 3;
-        Chunk piece[4];
+        const unsigned rt = my_rows + after, ct = my_columns + last;
+        constexpr int kAll = 8 * kSteps, kAhead = 4;
+        Chunk piece[8];
         auto piece_of = [&](int at) {
-            return at < kSteps ? rows_chunk<E>(rt, at) : at < 2 * kSteps ? rows_chunk<E>(rt + kTile, at - kSteps)
-                 : at < 3 * kSteps ? columns_chunk<E, DP>(ct + kTile, ((at - 2 * kSteps) & 1) * 16, (at - 2 * kSteps) >> 1)
-                                   : columns_chunk<E, DP>(ct, ((at - 3 * kSteps) & 1) * 16, (at - 3 * kSteps) >> 1);
+            if (at < 4 * kSteps) return columns_chunk<E, DP>(ct + (at & 1 ? 0 : kTile), 16 * (at / 2 / kOut), at / 2 % kOut);  // dO and Q in turn
+            const int i = at - 4 * kSteps;
+            return rows_chunk<E>(rt + (i & 1 ? kTile : 0) + (i >> 1 & 1) * kUnder, i >> 2);
         };
-#pragma unroll
-        for (int i = 0; i < kAhead; i++) piece[i] = piece_of(i);
-        f32x16 next_s = zero16(), next_dp = zero16();
-        float top = 0.f, sum = 0.f;
+        f32x16 next_s[2] = {zero16(), zero16()}, next_dp[2] = {zero16(), zero16()};
+        float sum = 0.f;
         f32x4 l4 = {0, 0, 0, 0}, d4 = {0, 0, 0, 0};
-#pragma unroll
-        for (int at = 0; at < kAll; at++) {
+        in_turn<kAll>([&](auto step) __attribute__((always_inline)) {
+            constexpr int at = decltype(step)::value;
             __builtin_amdgcn_sched_barrier(0);
-            if (at + kAhead < kAll) piece[(at + kAhead) & 3] = piece_of(at + kAhead);
-            if (at % (kAll / 4) == 0) {
-                l4 = *(const f32x4 *)(lse + 8 * (4 * at / kAll) + 4 * half);
-                d4 = *(const f32x4 *)(delta + 8 * (4 * at / kAll) + 4 * half);
-            }
-            if (at < kSteps) next_s = mfma(piece[at & 3], k[at], next_s);
-            else if (at < 2 * kSteps) next_dp = mfma(piece[at & 3], v[at - kSteps], next_dp);
-            else if (at < 3 * kSteps) dv[(at - 2 * kSteps) >> 1] = mfma(piece[at & 3], (at & 1) ? p1 : p0, dv[(at - 2 * kSteps) >> 1]);
-            else dk[(at - 3 * kSteps) >> 1] = mfma(piece[at & 3], (at & 1) ? z1 : z0, dk[(at - 3 * kSteps) >> 1]);
+            if (at % (kAll / 2) == 0) {
+                if (at > 0) {
+                    __syncthreads();  // the last tile's columns are read
+                    stage(t + 2, last);
+                    fetch();
 #pragma unroll
-            for (int e = 16 * at / kAll; e < 16 * (at + 1) / kAll; e++) {
-                const float w = element_w<CAP>(x, s[e]);
-                float p = element_p<CAP>(x, w, l4[e % 4]), dy = element_dy<CAP>(x, p, dp[e], d4[e % 4]);
+                    for (int i = 0; i < 2; i++) {
+                        p[i] = i ? rounded8<E, 1>(s[0]) : rounded8<E, 0>(s[0]);
+                        z[i] = i ? rounded8<E, 1>(dp[0]) : rounded8<E, 0>(dp[0]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < kAhead; i++) piece[(at + i) & 7] = piece_of(at + i);
+            }
+            if ((at + kAhead) % (kAll / 2) >= kAhead) piece[(at + kAhead) & 7] = piece_of(at + kAhead);
+            if (at % (kAll / 8) == 0) {
+                l4 = *(const f32x4 *)(lse + 8 * (8 * at / kAll) + 4 * half);
+                d4 = *(const f32x4 *)(delta + 8 * (8 * at / kAll) + 4 * half);
+            }
+            if (at < 4 * kSteps) {
+                const int i = at / 2;
+                if (at & 1) dk[i % kOut] = mfma(piece[at & 7], z[i / kOut], dk[i % kOut]);
+                else dv[i % kOut] = mfma(piece[at & 7], p[i / kOut], dv[i % kOut]);
+            } else {
+                const int i = at - 4 * kSteps, u = i >> 1 & 1;
+                if (i & 1) next_dp[u] = mfma(piece[at & 7], v[i >> 2], next_dp[u]);
+                else next_s[u] = mfma(piece[at & 7], k[i >> 2], next_s[u]);
+            }
+#pragma unroll
+            for (int e = 32 * at / kAll; e < 32 * (at + 1) / kAll; e++) {
+                const float w = element_w<CAP>(x, s[e / 16][e % 16]);
+                float pe = element_p<CAP>(x, w, l4[e % 4]), dy = element_dy<CAP>(x, pe, dp[e / 16][e % 16], d4[e % 4]);
                 if (BIAS) sum += dy;
                 float dz = element_dz<CAP>(x, dy, w);
-                here(p);
+                here(pe);
                 here(dz);
-                dp[e] = dz;
-                s[e] = p;
+                dp[e / 16][e % 16] = dz;
+                s[e / 16][e % 16] = pe;
             }
             if (BIAS) here(sum);
-            constexpr int kFrom = 2 * kSteps, kPer = 8 / kSteps;
-            if (at >= kFrom) {
-#pragma unroll
-                for (int e = (at - kFrom) * kPer; e < (at - kFrom + 1) * kPer; e++) top = fmaxf(top, __builtin_fabsf(next_s[e]));
-                here(top);
-            }
-        }
+            if (BIAS && at == kAll / 4) look_at(qpos[((t + 1) & 3) * kGradTile + lane], at_tile + 1 < per ? g : g + 1 < G ? g + 1 : g);
+        });
         __builtin_amdgcn_sched_barrier(0);
-        if (BIAS && plain && mine) __hip_atomic_fetch_add(my_sums + column[x0], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-        size = top;
-        p0 = rounded8<E, 0>(s);
-        p1 = rounded8<E, 1>(s);
-        z0 = rounded8<E, 0>(dp);
-        z1 = rounded8<E, 1>(dp);
-        s = next_s;
-        dp = next_dp;
+        if (BIAS && plain) {
+            sum = halves_sum(sum);
+            if (mine && half == 0) add_at(bucket_now, sum);
+        }
+        p[2] = rounded8<E, 0>(s[1]);
+        p[3] = rounded8<E, 1>(s[1]);
+        z[2] = rounded8<E, 0>(dp[1]);
+        z[3] = rounded8<E, 1>(dp[1]);
+        size = 0.f;
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            s[u] = next_s[u];
+            dp[u] = next_dp[u];
+        }
+#pragma unroll
+        for (int r = 0; r < 32; r++) size = fmaxf(size, __builtin_fabsf(s[r / 16][r % 16]));
+        const unsigned free_now = last;
+        last = now;
+        now = after;
+        after = free_now;
         __syncthreads();
         if (++at_tile == per) {
             if (BIAS) finish(g);
@@ -524,13 +604,11 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
         }
     }
     if (tiles_n > 0) {
-        const unsigned ct = my_columns + buffer(tiles_n - 1);
+        const unsigned ct = my_columns + last;
 #pragma unroll
-        for (int i = 0; i < kOut; i++) {
-            dv[i] = mfma(columns_chunk<E, DP>(ct + kTile, 0, i), p0, dv[i]);
-            dv[i] = mfma(columns_chunk<E, DP>(ct + kTile, 16, i), p1, dv[i]);
-            dk[i] = mfma(columns_chunk<E, DP>(ct, 0, i), z0, dk[i]);
-            dk[i] = mfma(columns_chunk<E, DP>(ct, 16, i), z1, dk[i]);
+        for (int i = 0; i < 4 * kOut; i++) {
+            dv[i % kOut] = mfma(columns_chunk<E, DP>(ct + kTile, 16 * (i / kOut), i % kOut), p[i / kOut], dv[i % kOut]);
+            dk[i % kOut] = mfma(columns_chunk<E, DP>(ct, 16 * (i / kOut), i % kOut), z[i / kOut], dk[i % kOut]);
         }
     } else if (BIAS) {
         for (int i = tid; i < G * nb; i += kAttThreads) part[i] = 0.f;
@@ -573,13 +651,13 @@ static int64_t backward_bytes(const AttArgs &a) {
 template <class E, int DP, bool CAP, bool BIAS> static logoskg_status launch_backward(const AttArgs &a, hipStream_t st) {
     const size_t places = BIAS ? 2 * a.score.max_distance + 1 : 0, table = a.group * places * 4;
     if (a.num_rows) {
-        size_t bytes = 8 * kGradTile * DP * 2 + 4 * kGradTile * 4 + table;
+        size_t bytes = 6 * kGradTile * DP * 2 + 4 * kGradTile * 4 + table;
         LKG_TRY(allow_lds(k_att_dq<E, DP, CAP, BIAS>, bytes));
         k_att_dq<E, DP, CAP, BIAS><<<dim3((unsigned)(a.row_blocks * a.kv_heads)), kAttThreads, bytes, st>>>(a);
         LKG_HIP(hipGetLastError());
     }
     if (a.num_keys) {
-        size_t bytes = 8 * kGradTile * DP * 2 + 3 * 4 * kGradTile * 4 + table + places * 4 + (BIAS ? 4 * a.score.num_buckets * 64 * 4 : 0);
+        size_t bytes = 6 * kGradTile * DP * 2 + 3 * 4 * kGradTile * 4 + table + places * 4 + (BIAS ? 4 * a.score.num_buckets * 32 * 4 : 0);
         LKG_TRY(allow_lds(k_att_dkdv<E, DP, CAP, BIAS>, bytes));
         k_att_dkdv<E, DP, CAP, BIAS><<<dim3((unsigned)(a.key_blocks * a.kv_heads)), kAttThreads, bytes, st>>>(a);
         LKG_HIP(hipGetLastError());

@@ -3,6 +3,8 @@
 
 #include "common.h"
 
+#include <utility>
+
 namespace lkg {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -79,6 +81,13 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
+
+// f(0), f(1), .. f(N - 1), each with its number as a constant: loops that must be unrolled whatever their size, since registers
+// are picked by it.
+template <class F, int... I> __device__ __forceinline__ void in_turn(F &f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F> __device__ __forceinline__ void in_turn(F f) { in_turn(f, std::make_integer_sequence<int, N>{}); }
 
 // Keeps what makes x in its place among the matrix instructions: the compiler would gather it behind them.
 __device__ __forceinline__ void here(float &x) { asm volatile("" : "+v"(x)); }
