@@ -147,6 +147,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
                         } else y = __builtin_fmaf(z, near0, y);
                         s[u][r] = y;
                         top = fmaxf(top, y);
+                        if (r % 8 == 7) __builtin_amdgcn_sched_barrier(0);  // (no more in registers than these)
                     }
             } else {
 #pragma unroll
@@ -161,6 +162,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
                         y = t * kKeys + at < seen ? y : -INFINITY;
                         s[u][r] = y;
                         top = fmaxf(top, y);
+                        if (r % 8 == 7) __builtin_amdgcn_sched_barrier(0);  // (no more in registers than these)
                     }
             }
             top = halves_max(top);
@@ -183,42 +185,53 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
             shift = 0.f, near0 = 1.f, near1 = near2 = near3 = 0.f;
         }
         const unsigned kt = my_rows + buffer(t + 1), vt = my_columns + buffer(t - 1);
-        // First the output, whose weights' registers then take the new ones of the tile's first half, and the scores of the
-        // next tile those of this one's: everything fits 256 registers, two wavefronts to a unit.
-        constexpr int kAll = 4 * kSteps, kAhead = 3, kEach = 32 / kAll;
+        // First the output, whose weights' registers then take the new ones, and the scores of the next tile those of this
+        // one's: everything fits 256 registers, two wavefronts to a unit.
+        constexpr int kAll = 4 * kSteps, kAhead = 3, kStages = 4;
         Chunk piece[4];
-        auto piece_of = [&](int at) {
+        auto piece_of = [&](int at) __attribute__((always_inline)) {
             if (at < 2 * kSteps) return columns_chunk<E, DP>(vt, 16 * (at / kOut), at % kOut);
             return rows_chunk<E>(kt + (at & 1) * 32 * DP * 2, (at - 2 * kSteps) >> 1);
         };
 #pragma unroll
         for (int i = 0; i < kAhead; i++) piece[i] = piece_of(i);
         f32x16 next[2] = {zero16(), zero16()};
-#pragma unroll
-        for (int at = 0; at < kAll; at++) {
+        float square[32], w[32];  // (few of them at a time)
+        unsigned packed[16];
+        in_turn<kAll + kStages - 1>([&](auto step) __attribute__((always_inline)) {
+            constexpr int at = decltype(step)::value;
             __builtin_amdgcn_sched_barrier(0);
-            if (at == 2 * kSteps) {
-                p[0] = rounded8<E, 0>(s[0]);
-                p[1] = rounded8<E, 1>(s[0]);
-            }
             if (at + kAhead < kAll) piece[(at + kAhead) & 3] = piece_of(at + kAhead);
-            if (at < 2 * kSteps) o[at % kOut] = mfma(piece[at & 3], p[at / kOut], o[at % kOut]);
-            else next[at & 1] = mfma(piece[at & 3], q[(at - 2 * kSteps) >> 1], next[at & 1]);  // (behind the last tile: of what the buffer holds, not used)
+            if (at < 2 * kSteps) o[at % kOut] = mfma(piece[at & 3], p[at / kOut & 3], o[at % kOut]);
+            else if (at < kAll) next[at & 1] = mfma(piece[at & 3], q[(at - 2 * kSteps) >> 1], next[at & 1]);  // (behind the last tile: of what the buffer holds, not used)
 #pragma unroll
-            for (int e = at * kEach; e < (at + 1) * kEach; e++) {
+            for (int e = first_of<kAll>(at); e < first_of<kAll>(at + 1); e++) {
                 const float z = s[e / 16][e % 16];
-                float y;
                 if (CAP) {
-                    float zz = z * z;
-                    y = __builtin_fmaf(zz, near3, near2);
-                    y = __builtin_fmaf(zz, y, near1);
-                    y = __builtin_fmaf(zz, y, near0);
-                    y = __builtin_fmaf(z, y, shift);
-                } else y = __builtin_fmaf(z, near0, shift);
-                y = exp2_fast(y);
-                here(y);
-                s[e / 16][e % 16] = y;
-                l += y;
+                    square[e] = z * z;
+                    w[e] = __builtin_fmaf(square[e], near3, near2);
+                    here(w[e]);
+                }
+            }
+#pragma unroll
+            for (int e = first_of<kAll>(at - 1); e < first_of<kAll>(at); e++)
+                if (CAP) {
+                    w[e] = __builtin_fmaf(square[e], w[e], near1);
+                    w[e] = __builtin_fmaf(square[e], w[e], near0);
+                    here(w[e]);
+                }
+#pragma unroll
+            for (int e = first_of<kAll>(at - 2); e < first_of<kAll>(at - 1); e++) {
+                w[e] = exp2_fast(__builtin_fmaf(s[e / 16][e % 16], CAP ? w[e] : near0, shift));
+                here(w[e]);
+            }
+#pragma unroll
+            for (int e = first_of<kAll>(at - 3); e < first_of<kAll>(at - 2); e++) {
+                l += w[e];
+                if (e & 1) {
+                    packed[e / 2] = rounded2<E>(w[e - 1], w[e]);
+                    here(packed[e / 2]);
+                }
             }
             here(l);
             if (BIAS && at == kAll / 4) look_at(kpos[((t + 1) & 3) * kKeys + lane]);
@@ -230,14 +243,14 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
                 vload.store(tiles + 2 * kTile + buffer(t), x);  // V of t, where that of t - 2 was
                 kload.load(x);
             }
-        }
+        });
         __builtin_amdgcn_sched_barrier(0);
         if (wave_any(shrink != 1.f)) {
 #pragma unroll
             for (int i = 0; i < kOut; i++) o[i] *= shrink;
         }
-        p[2] = rounded8<E, 0>(s[1]);
-        p[3] = rounded8<E, 1>(s[1]);
+#pragma unroll
+        for (int i = 0; i < 4; i++) p[i] = as8<E>(u32x4{packed[4 * i], packed[4 * i + 1], packed[4 * i + 2], packed[4 * i + 3]});
         s[0] = next[0];
         s[1] = next[1];
         size = 0.f;

@@ -227,7 +227,7 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dq(AttArgs a) {
             x = special_steps();
         }
         const unsigned kt = my_rows + k_buffer(t + 1), vt = my_rows + v_buffer(t + 1), ct = my_columns + k_buffer(t - 1);
-        constexpr int kAll = 6 * kSteps, kAhead = 4;
+        constexpr int kAll = 6 * kSteps, kAhead = 7;
         Chunk piece[8];
         auto piece_of = [&](int at) {
             if (at < 2 * kSteps) return columns_chunk<E, DP>(ct, 16 * (at / kOut), at % kOut);
@@ -521,7 +521,7 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
             x = special_steps();
         }
         const unsigned rt = my_rows + after, ct = my_columns + last;
-        constexpr int kAll = 8 * kSteps, kAhead = 4;
+        constexpr int kAll = 8 * kSteps, kAhead = 7;
         Chunk piece[8];
         auto piece_of = [&](int at) {
             if (at < 4 * kSteps) return columns_chunk<E, DP>(ct + (at & 1 ? 0 : kTile), 16 * (at / 2 / kOut), at / 2 % kOut);  // dO and Q in turn

@@ -89,6 +89,19 @@ template <class F, int... I> __device__ __forceinline__ void in_turn(F &f, std::
 }
 template <int N, class F> __device__ __forceinline__ void in_turn(F f) { in_turn(f, std::make_integer_sequence<int, N>{}); }
 
+// A round's 32 elements go through their stages, one a step, while its `all` matrix instructions are issued: element e begins at
+// step e all / 32, so that a step holds one stage each of some neighbouring elements.  A vector instruction that
+// waits for the one before it takes twice as long as one that does not (8 clocks for 4 to 5): chains of one element alone
+// would leave the units idle half of the time.  The elements whose stage `s` falls on step `at`: [first, behind).
+template <int ALL> constexpr int first_of(int at) { return at < 0 ? 0 : at >= ALL ? 32 : (at * 32 + ALL - 1) / ALL; }
+
+template <class E> struct Pair { typedef E type __attribute__((ext_vector_type(2))); };
+template <class E> __device__ __forceinline__ unsigned rounded2(float a, float b) {  // nearest even, as rounded8
+    typename Pair<E>::type r = {(E)a, (E)b};
+    return __builtin_bit_cast(unsigned, r);
+}
+__device__ __forceinline__ void here(unsigned &x) { asm volatile("" : "+v"(x)); }
+
 // Keeps what makes x in its place among the matrix instructions: the compiler would gather it behind them.
 __device__ __forceinline__ void here(float &x) { asm volatile("" : "+v"(x)); }
 
