@@ -8,6 +8,7 @@ namespace lkg {
 constexpr int kAttThreads = 256;  // four wavefronts
 constexpr int kAttRowsShift = 7;  // a block's rows: 4 x 32
 constexpr int kAttRows = 1 << kAttRowsShift;
+constexpr size_t kLds = 160 << 10;                        // of a compute unit
 constexpr long long kMostRows = (1ll << 31) - (1 << 16);  // of a batch: places in a document are 32-bit, with room for a tile
 constexpr long long kMostStride = 1 << 23;                // between rows, in elements: a tile's rows within 2^31 bytes
 constexpr int kMostGroup = 128;                           // heads that share a key head
@@ -31,6 +32,7 @@ struct AttArgs {
     float curve;       // .. of scale (1 - tanh^2) = scale + curve y^2, y = c tanh in units of log 2
     float slope;       // with a cap: 4 scale, of scale (1 - tanh^2) = 4 scale r (1 - r), r = 1 / (2^(z k) + 1)
     long long row_blocks, key_blocks;
+    int bias_columns;  // 64, or 32 where LDS has no room for them
 };
 
 struct AttDoc {  // a document: where its rows and keys begin, and how many there are

@@ -55,15 +55,50 @@ template <bool CAP> __device__ __forceinline__ float element_w(const Steps &x, f
     w = __builtin_fmaf(zz, w, x.near0);
     return z * w;
 }
-template <bool CAP> __device__ __forceinline__ float element_p(const Steps &x, float w, float lse) {
-    const float shift = __builtin_fmaf(lse, x.lse_share, x.b);
-    return exp2_fast(CAP ? w + shift : __builtin_fmaf(w, x.near0, shift));
-}
-template <bool CAP> __device__ __forceinline__ float element_dy(const Steps &x, float p, float dp, float delta) {
-    return p * __builtin_fmaf(delta, -x.delta_share, dp);
-}
 template <bool CAP> __device__ __forceinline__ float element_dz(const Steps &x, float dy, float w) {
     return dy * (CAP ? __builtin_fmaf(w * w, x.curve, x.slope) : x.slope);
+}
+
+// An element on its way through the steps (first_of): w, p, dy, dz, a stage each step
+constexpr int kStages = 6;
+struct Element {
+    float square, w, p, dz;
+    template <bool CAP> __device__ __forceinline__ void step(int stage, const Steps &x, float z, float dp, float shift, float delta, float &sum) {
+        if (stage == 0 && CAP) {
+            square = z * z;
+            w = __builtin_fmaf(square, x.near3, x.near2);
+            here(w);
+        }
+        if (stage == 1 && CAP) {
+            w = __builtin_fmaf(square, w, x.near1);
+            w = __builtin_fmaf(square, w, x.near0);
+            here(w);
+        }
+        if (stage == 2) {
+            if (CAP) w *= z;
+            p = CAP ? w + shift : __builtin_fmaf(z, x.near0, shift);
+            here(p);
+        }
+        if (stage == 3) {
+            p = exp2_fast(p);
+            dz = __builtin_fmaf(delta, -x.delta_share, dp);
+            here(p);
+            here(dz);
+        }
+        if (stage == 4) {
+            dz *= p;  // (dy)
+            square = CAP ? w * w : 0.f;
+            here(dz);
+        }
+        if (stage == 5) {
+            sum += dz;
+            dz *= CAP ? __builtin_fmaf(square, x.curve, x.slope) : x.slope;
+            here(dz);
+        }
+    }
+};
+template <class E> __device__ __forceinline__ typename Vec8<E>::type chunk_of(const unsigned *pairs) {
+    return as8<E>(u32x4{pairs[0], pairs[1], pairs[2], pairs[3]});
 }
 
 // A special element: y and its slope from the product, by the exact tanh
@@ -194,40 +229,41 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dq(AttArgs a) {
         const bool edge = (t + 1) * kGradTile > least, far = wave_any(size > a.score.most), plain = !edge && !far && !varied;
         Steps x = plain_steps<CAP>(a, b);
         if (!plain) {
-            const int *kpt = kpos + (t & 3) * kGradTile;
-            if (!edge && !far) {
 #pragma unroll
-                for (int u = 0; u < 2; u++)
+            for (int u = 0; u < 2; u++) {
+                float bias[16];
 #pragma unroll
-                    for (int r = 0; r < 16; r++) {
-                        float y = float_at(place_of_key(places, kpt[32 * u + 8 * (r / 4) + 4 * half + r % 4])) - lse;
-                        const float away = dp[u][r] - delta, w = element_w<CAP>(x, s[u][r]);
+                for (int j = 0; j < 4; j++) {
+                    const u32x4 p4 = BIAS ? *(const u32x4 *)(kpos + (t & 3) * kGradTile + 32 * u + 8 * j + 4 * half) : u32x4{0, 0, 0, 0};
+#pragma unroll
+                    for (int e = 0; e < 4; e++) bias[4 * j + e] = BIAS ? float_at(place_of_key(places, (int)p4[e])) : 0.f;
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int r = 0; r < 16; r++) {
+                    float away = dp[u][r] - delta;
+                    if (!edge && !far) {
+                        const float w = element_w<CAP>(x, s[u][r]);
+                        float y = bias[r] - lse;
                         y = CAP ? y + w : __builtin_fmaf(w, x.near0, y);
-                        lacks = __builtin_fmaf(exp2_fast(y), away, lacks);
-                        dp[u][r] = element_dz<CAP>(x, away, w);
                         s[u][r] = y;
-                    }
-            } else {
-#pragma unroll
-                for (int u = 0; u < 2; u++)
-#pragma unroll
-                    for (int r = 0; r < 16; r++) {
-                        const int at = 32 * u + 8 * (r / 4) + 4 * half + r % 4;
+                        dp[u][r] = element_dz<CAP>(x, away, w);
+                    } else {
                         float y, slope;
                         exact_score<CAP>(a, s[u][r], y, slope);
-                        if (BIAS) y += float_at(place_of_key(places, kpt[at]));
-                        y -= lse;
-                        float away = dp[u][r] - delta;
-                        if (t * kGradTile + at >= seen) y = kHidden, away = 0.f;
-                        lacks = __builtin_fmaf(exp2_fast(y), away, lacks);
-                        dp[u][r] = away * slope;
+                        y += bias[r] - lse;
+                        if (t * kGradTile + 32 * u + 8 * (r / 4) + 4 * half + r % 4 >= seen) y = kHidden, away = 0.f;
                         s[u][r] = y < kHidden ? kHidden : y;
+                        dp[u][r] = away * slope;
                     }
+                    lacks = __builtin_fmaf(exp2_fast(s[u][r]), away, lacks);
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
             x = special_steps();
         }
         const unsigned kt = my_rows + k_buffer(t + 1), vt = my_rows + v_buffer(t + 1), ct = my_columns + k_buffer(t - 1);
-        constexpr int kAll = 6 * kSteps, kAhead = 7;
+        constexpr int kAll = 6 * kSteps, kAhead = 6;
         Chunk piece[8];
         auto piece_of = [&](int at) {
             if (at < 2 * kSteps) return columns_chunk<E, DP>(ct, 16 * (at / kOut), at % kOut);
@@ -238,24 +274,29 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dq(AttArgs a) {
         for (int i = 0; i < kAhead; i++) piece[i] = piece_of(i);
         f32x16 next_s[2] = {zero16(), zero16()}, next_dp[2] = {zero16(), zero16()};
         float sum = 0.f;
-        in_turn<kAll>([&](auto step) __attribute__((always_inline)) {
+        Element el[32];
+        unsigned dz_pair[16];
+        const float shift = __builtin_fmaf(lse, x.lse_share, x.b);
+        in_turn<kAll + kStages - 1>([&](auto step) __attribute__((always_inline)) {
             constexpr int at = decltype(step)::value;
             __builtin_amdgcn_sched_barrier(0);
             if (at + kAhead < kAll) piece[(at + kAhead) & 7] = piece_of(at + kAhead);
-            if (at < 2 * kSteps) dq[at % kOut] = mfma(piece[at & 7], z[at / kOut], dq[at % kOut]);
-            else {
-                const int i = at - 2 * kSteps, u = i >> 1 & 1;
+            if (at < 2 * kSteps) dq[at % kOut] = mfma(piece[at & 7], z[at / kOut & 3], dq[at % kOut]);
+            else if (at < kAll) {
+                constexpr int i = at - 2 * kSteps, u = i >> 1 & 1;
                 if (i & 1) next_dp[u] = mfma(piece[at & 7], o[i >> 2], next_dp[u]);
                 else next_s[u] = mfma(piece[at & 7], q[i >> 2], next_s[u]);
             }
 #pragma unroll
-            for (int e = 32 * at / kAll; e < 32 * (at + 1) / kAll; e++) {
-                const float w = element_w<CAP>(x, s[e / 16][e % 16]), p = element_p<CAP>(x, w, lse), dy = element_dy<CAP>(x, p, dp[e / 16][e % 16], delta);
-                sum += dy;
-                float dz = element_dz<CAP>(x, dy, w);
-                here(dz);
-                dp[e / 16][e % 16] = dz;
-            }
+            for (int stage = 0; stage < kStages; stage++)
+#pragma unroll
+                for (int e = first_of<kAll>(at - stage); e < first_of<kAll>(at - stage + 1); e++) {
+                    el[e].step<CAP>(stage, x, s[e / 16][e % 16], dp[e / 16][e % 16], shift, delta, sum);
+                    if (stage == kStages - 1 && (e & 1)) {
+                        dz_pair[e / 2] = rounded2<E>(el[e - 1].dz, el[e].dz);
+                        here(dz_pair[e / 2]);
+                    }
+                }
             here(sum);
             if (BIAS && at == kAll / 4) look_at(kpos[((t + 1) & 3) * kGradTile + lane]);
             if (at == kAll / 2) {
@@ -268,11 +309,11 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dq(AttArgs a) {
         size = 0.f;
 #pragma unroll
         for (int u = 0; u < 2; u++) {
-            z[2 * u] = rounded8<E, 0>(dp[u]);
-            z[2 * u + 1] = rounded8<E, 1>(dp[u]);
             s[u] = next_s[u];
             dp[u] = next_dp[u];
         }
+#pragma unroll
+        for (int i = 0; i < 4; i++) z[i] = chunk_of<E>(dz_pair + 4 * i);
 #pragma unroll
         for (int r = 0; r < 32; r++) size = fmaxf(size, __builtin_fabsf(s[r / 16][r % 16]));
         __syncthreads();
@@ -303,9 +344,10 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dq(AttArgs a) {
 // One block: 128 keys of (document, key head), 32 per wavefront, key = lane, K and V in registers as the B of S = Q K^T and
 // dP = dO V^T.  The rows that see them pass in tiles of 64 of one head, one head of the group after the other, through three
 // buffers in LDS, where they are read by rows for these two products and by columns for dV^T += dO^T p and dK^T += Q^T dz;
-// a round's first half is the last tile's columns, whose buffer then takes the tile after the next.  A key adds its dy to its
-// own column of [buckets][32] in LDS (no two lanes add to an address at a time, so the sums have an order), those of a tile
-// of one bias all at once; a head's columns are added up when its rows are through.
+// a round's first half is the last tile's columns, whose buffer then takes the tile after the next.  A lane adds its dy to its
+// own column of [buckets][64] in LDS ([buckets][32] and one half of the wavefront after the other where there is no room: no
+// two lanes add to an address at a time, so the sums have an order), those of a tile of one bias all at once; a head's
+// columns are added up when its rows are through.
 template <class E, int DP, bool CAP, bool BIAS>
 __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -314,8 +356,10 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
     const int G = a.group, M = a.score.max_distance, places_n = 2 * M + 1, nb = a.score.num_buckets;
     float *lses = (float *)(lds + 6 * kTile), *deltas = lses + 4 * kGradTile;  // [4][kGradTile] of the rows  (LDS begins with three times Q, dO)
     int *qpos = (int *)(deltas + 4 * kGradTile);
-    float *sums = (float *)(qpos + 4 * kGradTile);           // [4 wavefronts][nb][32]
-    int *column = (int *)(sums + (BIAS ? 4 * nb * 32 : 0));  // [places_n] where a distance's bucket begins, in bytes
+    const int cols = a.bias_columns;
+    float *sums = (float *)(qpos + 4 * kGradTile);            // [4 wavefronts][nb][cols]
+    float *aside = sums + (BIAS ? 4 * nb * cols : 0);         // [4 wavefronts][64]
+    int *column = (int *)(aside + (BIAS ? 256 : 0));          // [places_n] where a distance's bucket begins, in bytes
     float *table = (float *)(column + (BIAS ? places_n : 0));  // [group][places_n]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
     const int head = blockIdx.x % a.kv_heads;
@@ -342,7 +386,7 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
     }
     int k_low = 0, k_high = 0;
     Places places = {0, 0, 0};  // in `column`; a head's biases lie the same way
-    const unsigned to_table = (unsigned)((char *)table - (char *)column), my_sums = lds_place(sums) + (wave * nb * 32 + (lane & 31)) * 4;
+    const unsigned to_table = (unsigned)((char *)table - (char *)column), my_sums = lds_place(sums) + (wave * nb * cols + (lane & (cols - 1))) * 4;
     if (BIAS) {
         const int in = mine ? key : doc.keys - 1, k_pos = a.k_pos ? a.k_pos[doc.key0 + in] : in;
         places = places_of_rows(k_pos, M, lds_place(column));
@@ -351,12 +395,21 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
         bias_to_lds<E>(table, a.score, head * G, G, tid, kAttThreads);
         for (int i = tid; i < places_n; i += kAttThreads) {
             int b = a.score.buckets[i];
-            column[i] = (b < 0 ? 0 : b >= nb ? nb - 1 : b) * 128;
+            column[i] = (b < 0 ? 0 : b >= nb ? nb - 1 : b) * cols * 4;
         }
-        for (int i = tid; i < 4 * nb * 32; i += kAttThreads) sums[i] = 0.f;
+        for (int i = tid; i < 4 * nb * cols; i += kAttThreads) sums[i] = 0.f;
     }
-    auto add_at = [&](int bucket, float x) {
-        __hip_atomic_fetch_add((__attribute__((address_space(3))) float *)(uintptr_t)(my_sums + bucket), x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    auto add_at = [&](unsigned place, float x) {
+        __hip_atomic_fetch_add((__attribute__((address_space(3))) float *)(uintptr_t)place, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    };
+    // keys that are none (and where halves go one after the other, the other half) add to a place of their own that nobody reads
+    const unsigned my_aside = lds_place(aside) + tid * 4;
+    auto add_each = [&](int bucket, float x) {
+        if (cols == 64) add_at(mine ? my_sums + bucket : my_aside, x);
+        else {
+            add_at(mine && half == 0 ? my_sums + bucket : my_aside, x);
+            add_at(mine && half == 1 ? my_sums + bucket : my_aside, x);
+        }
     };
 
     f32x16 dk[kOut], dv[kOut], s[2] = {zero16(), zero16()}, dp[2] = {zero16(), zero16()};
@@ -414,20 +467,20 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
             if (BIAS) qpos[at] = my_pos;
         }
     };
-    // the columns of a head that is through: a bucket's 128 sums by 256 / nb threads, their parts by one
+    // the columns of a head that is through: a bucket's sums by 256 / nb threads, their parts by one
     auto finish = [&](int g) {
         __syncthreads();
         int strands = kAttThreads / nb;
         strands = strands >= 16 ? 16 : strands >= 8 ? 8 : 4;
-        const int b = tid % nb, st = tid / nb, n = 128 / strands;
+        const int b = tid % nb, st = tid / nb, n = 4 * cols / strands;
         float sum = 0.f;
         if (st < strands)
             for (int i = 0; i < n; i++) {  // (rotated by the bucket, so that neighbouring threads read other banks)
-                const int c = st * n + ((i + b) & (n - 1));
-                sum += sums[((c >> 5) * nb + b) * 32 + (c & 31)];
+                const int c = st * n + ((i + b) & (n - 1)), w = c / cols;
+                sum += sums[(w * nb + b) * cols + c - w * cols];
             }
         __syncthreads();
-        for (int i = tid; i < 4 * nb * 32; i += kAttThreads) sums[i] = 0.f;
+        for (int i = tid; i < 4 * nb * cols; i += kAttThreads) sums[i] = 0.f;
         __syncthreads();
         if (st < strands) sums[tid] = sum;
         __syncthreads();
@@ -476,52 +529,62 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
         const int bucket_now = bucket;
         Steps x = plain_steps<CAP>(a, b);
         if (!plain) {
-            const int *pos = qpos + (t & 3) * kGradTile;
             const unsigned to_head = to_table + g * places_n * 4;
-            if (!edge && !far) {
 #pragma unroll
-                for (int u = 0; u < 2; u++)
+            for (int part = 0; part < 4; part++) {
+                // eight rows' look-ups, then their elements, then their additions: one wait each
+                const int u = part >> 1, j0 = 2 * (part & 1);
+                unsigned place[8];
+                float bias[8], dy[8];
+                int bucket_of[8];
 #pragma unroll
-                    for (int r = 0; r < 16; r++) {
-                        const int at = 32 * u + 8 * (r / 4) + 4 * half + r % 4;
-                        const unsigned place = place_of_row(places, pos[at]);
-                        float y = float_at(place + to_head) - lse[at];
-                        const float away = dp[u][r] - delta[at], w = element_w<CAP>(x, s[u][r]);
-                        y = CAP ? y + w : __builtin_fmaf(w, x.near0, y);
-                        const float dy = exp2_fast(y) * away;
-                        const int c = int_at(place);
-                        if (mine && half == 0) add_at(c, dy);
-                        if (mine && half == 1) add_at(c, dy);
-                        dp[u][r] = element_dz<CAP>(x, away, w);
-                        s[u][r] = y;
-                    }
-            } else {
+                for (int j = 0; j < 2; j++) {
+                    if (!BIAS) break;
+                    const u32x4 p4 = *(const u32x4 *)(qpos + (t & 3) * kGradTile + 32 * u + 8 * (j0 + j) + 4 * half);
 #pragma unroll
-                for (int u = 0; u < 2; u++)
+                    for (int e = 0; e < 4; e++) place[4 * j + e] = place_of_row(places, (int)p4[e]);
+                }
 #pragma unroll
-                    for (int r = 0; r < 16; r++) {
-                        const int at = 32 * u + 8 * (r / 4) + 4 * half + r % 4;
-                        const unsigned place = BIAS ? place_of_row(places, pos[at]) : 0;
-                        float y, slope;
-                        exact_score<CAP>(a, s[u][r], y, slope);
-                        if (BIAS) y += float_at(place + to_head);
-                        y -= lse[at];
-                        float away = dp[u][r] - delta[at];
-                        if (key >= doc.seen(r0 + at, a.causal)) y = kHidden, away = 0.f;
-                        if (BIAS) {
-                            const float dy = exp2_fast(y) * away;
-                            const int c = int_at(place);
-                            if (mine && half == 0) add_at(c, dy);
-                            if (mine && half == 1) add_at(c, dy);
+                for (int i = 0; i < 8; i++) {
+                    bias[i] = BIAS ? float_at(place[i] + to_head) : 0.f;
+                    if (BIAS) bucket_of[i] = int_at(place[i]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int j = 0; j < 2; j++) {
+                    const int at = 32 * u + 8 * (j0 + j) + 4 * half;
+                    const f32x4 lse4 = *(const f32x4 *)(lse + at), delta4 = *(const f32x4 *)(delta + at);
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        const int r = 4 * (j0 + j) + e;
+                        float away = dp[u][r] - delta4[e];
+                        if (!edge && !far) {
+                            const float w = element_w<CAP>(x, s[u][r]);
+                            float y = bias[4 * j + e] - lse4[e];
+                            y = CAP ? y + w : __builtin_fmaf(w, x.near0, y);
+                            s[u][r] = y;
+                            dp[u][r] = element_dz<CAP>(x, away, w);
+                        } else {
+                            float y, slope;
+                            exact_score<CAP>(a, s[u][r], y, slope);
+                            y += bias[4 * j + e] - lse4[e];
+                            if (key >= doc.seen(r0 + at + e, a.causal)) y = kHidden, away = 0.f;
+                            s[u][r] = y < kHidden ? kHidden : y;
+                            dp[u][r] = away * slope;
                         }
-                        dp[u][r] = away * slope;
-                        s[u][r] = y < kHidden ? kHidden : y;
+                        dy[4 * j + e] = exp2_fast(s[u][r]) * away;
                     }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    if (BIAS) add_each(bucket_of[i], dy[i]);
+                __builtin_amdgcn_sched_barrier(0);
             }
             x = special_steps();
         }
         const unsigned rt = my_rows + after, ct = my_columns + last;
-        constexpr int kAll = 8 * kSteps, kAhead = 7;
+        constexpr int kAll = 8 * kSteps, kAhead = 6;
         Chunk piece[8];
         auto piece_of = [&](int at) {
             if (at < 4 * kSteps) return columns_chunk<E, DP>(ct + (at & 1 ? 0 : kTile), 16 * (at / 2 / kOut), at / 2 % kOut);  // dO and Q in turn
@@ -530,61 +593,55 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
         };
         f32x16 next_s[2] = {zero16(), zero16()}, next_dp[2] = {zero16(), zero16()};
         float sum = 0.f;
-        f32x4 l4 = {0, 0, 0, 0}, d4 = {0, 0, 0, 0};
-        in_turn<kAll>([&](auto step) __attribute__((always_inline)) {
+        f32x4 l4[2], d4[2];  // of four rows, and the four before them
+        Element el[32];
+        unsigned p_pair[16], dz_pair[16];
+        in_turn<kAll + kStages - 1>([&](auto step) __attribute__((always_inline)) {
             constexpr int at = decltype(step)::value;
             __builtin_amdgcn_sched_barrier(0);
-            if (at % (kAll / 2) == 0) {
+            if (at % (kAll / 2) == 0 && at < kAll) {
                 if (at > 0) {
                     __syncthreads();  // the last tile's columns are read
                     stage(t + 2, last);
                     fetch();
-#pragma unroll
-                    for (int i = 0; i < 2; i++) {
-                        p[i] = i ? rounded8<E, 1>(s[0]) : rounded8<E, 0>(s[0]);
-                        z[i] = i ? rounded8<E, 1>(dp[0]) : rounded8<E, 0>(dp[0]);
-                    }
                 }
 #pragma unroll
                 for (int i = 0; i < kAhead; i++) piece[(at + i) & 7] = piece_of(at + i);
             }
-            if ((at + kAhead) % (kAll / 2) >= kAhead) piece[(at + kAhead) & 7] = piece_of(at + kAhead);
-            if (at % (kAll / 8) == 0) {
-                l4 = *(const f32x4 *)(lse + 8 * (8 * at / kAll) + 4 * half);
-                d4 = *(const f32x4 *)(delta + 8 * (8 * at / kAll) + 4 * half);
+            if (at + kAhead < kAll && (at + kAhead) % (kAll / 2) >= kAhead) piece[(at + kAhead) & 7] = piece_of(at + kAhead);
+            if (at % (kAll / 8) == 0 && at < kAll) {
+                l4[at / (kAll / 8) & 1] = *(const f32x4 *)(lse + 8 * (8 * at / kAll) + 4 * half);
+                d4[at / (kAll / 8) & 1] = *(const f32x4 *)(delta + 8 * (8 * at / kAll) + 4 * half);
             }
             if (at < 4 * kSteps) {
-                const int i = at / 2;
-                if (at & 1) dk[i % kOut] = mfma(piece[at & 7], z[i / kOut], dk[i % kOut]);
-                else dv[i % kOut] = mfma(piece[at & 7], p[i / kOut], dv[i % kOut]);
-            } else {
-                const int i = at - 4 * kSteps, u = i >> 1 & 1;
+                constexpr int i = at / 2;
+                if (at & 1) dk[i % kOut] = mfma(piece[at & 7], z[i / kOut & 3], dk[i % kOut]);
+                else dv[i % kOut] = mfma(piece[at & 7], p[i / kOut & 3], dv[i % kOut]);
+            } else if (at < kAll) {
+                constexpr int i = at - 4 * kSteps, u = i >> 1 & 1;
                 if (i & 1) next_dp[u] = mfma(piece[at & 7], v[i >> 2], next_dp[u]);
                 else next_s[u] = mfma(piece[at & 7], k[i >> 2], next_s[u]);
             }
 #pragma unroll
-            for (int e = 32 * at / kAll; e < 32 * (at + 1) / kAll; e++) {
-                const float w = element_w<CAP>(x, s[e / 16][e % 16]);
-                float pe = element_p<CAP>(x, w, l4[e % 4]), dy = element_dy<CAP>(x, pe, dp[e / 16][e % 16], d4[e % 4]);
-                if (BIAS) sum += dy;
-                float dz = element_dz<CAP>(x, dy, w);
-                here(pe);
-                here(dz);
-                dp[e / 16][e % 16] = dz;
-                s[e / 16][e % 16] = pe;
-            }
+            for (int stage = 0; stage < kStages; stage++)
+#pragma unroll
+                for (int e = first_of<kAll>(at - stage); e < first_of<kAll>(at - stage + 1); e++) {
+                    const float shift = stage == 2 ? __builtin_fmaf(l4[e / 4 & 1][e % 4], x.lse_share, x.b) : 0.f;
+                    el[e].step<CAP>(stage, x, s[e / 16][e % 16], dp[e / 16][e % 16], shift, d4[e / 4 & 1][e % 4], sum);
+                    if (stage == kStages - 1 && (e & 1)) {
+                        p_pair[e / 2] = rounded2<E>(el[e - 1].p, el[e].p);
+                        dz_pair[e / 2] = rounded2<E>(el[e - 1].dz, el[e].dz);
+                        here(p_pair[e / 2]);
+                        here(dz_pair[e / 2]);
+                    }
+                }
             if (BIAS) here(sum);
             if (BIAS && at == kAll / 4) look_at(qpos[((t + 1) & 3) * kGradTile + lane], at_tile + 1 < per ? g : g + 1 < G ? g + 1 : g);
         });
         __builtin_amdgcn_sched_barrier(0);
-        if (BIAS && plain) {
-            sum = halves_sum(sum);
-            if (mine && half == 0) add_at(bucket_now, sum);
-        }
-        p[2] = rounded8<E, 0>(s[1]);
-        p[3] = rounded8<E, 1>(s[1]);
-        z[2] = rounded8<E, 0>(dp[1]);
-        z[3] = rounded8<E, 1>(dp[1]);
+        if (BIAS && plain) add_each(bucket_now, sum);
+#pragma unroll
+        for (int i = 0; i < 4; i++) p[i] = chunk_of<E>(p_pair + 4 * i), z[i] = chunk_of<E>(dz_pair + 4 * i);
         size = 0.f;
 #pragma unroll
         for (int u = 0; u < 2; u++) {
@@ -657,9 +714,12 @@ template <class E, int DP, bool CAP, bool BIAS> static logoskg_status launch_bac
         LKG_HIP(hipGetLastError());
     }
     if (a.num_keys) {
-        size_t bytes = 6 * kGradTile * DP * 2 + 3 * 4 * kGradTile * 4 + table + places * 4 + (BIAS ? 4 * a.score.num_buckets * 32 * 4 : 0);
+        AttArgs b = a;
+        size_t bytes = 6 * kGradTile * DP * 2 + 3 * 4 * kGradTile * 4 + table + places * 4 + (BIAS ? 1024 : 0);
+        b.bias_columns = bytes + (size_t)4 * a.score.num_buckets * 64 * 4 <= kLds ? 64 : 32;
+        if (BIAS) bytes += (size_t)4 * a.score.num_buckets * b.bias_columns * 4;
         LKG_TRY(allow_lds(k_att_dkdv<E, DP, CAP, BIAS>, bytes));
-        k_att_dkdv<E, DP, CAP, BIAS><<<dim3((unsigned)(a.key_blocks * a.kv_heads)), kAttThreads, bytes, st>>>(a);
+        k_att_dkdv<E, DP, CAP, BIAS><<<dim3((unsigned)(a.key_blocks * a.kv_heads)), kAttThreads, bytes, st>>>(b);
         LKG_HIP(hipGetLastError());
     }
     return LOGOSKG_OK;
