@@ -212,7 +212,6 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dq(AttArgs a) {
         stage(0);
         fetch(1);
         stage(1);
-        fetch(2);
         kload.clear(tiles + k_buffer(3));  // (round 0 multiplies it with zeros)
         __syncthreads();
 #pragma unroll
@@ -263,8 +262,8 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dq(AttArgs a) {
             x = special_steps();
         }
         const unsigned kt = my_rows + k_buffer(t + 1), vt = my_rows + v_buffer(t + 1), ct = my_columns + k_buffer(t - 1);
-        constexpr int kAll = 6 * kSteps, kAhead = 6;
-        Chunk piece[8];
+        constexpr int kAll = 6 * kSteps, kAhead = 4, kRing = 5;
+        Chunk piece[kRing];
         auto piece_of = [&](int at) {
             if (at < 2 * kSteps) return columns_chunk<E, DP>(ct, 16 * (at / kOut), at % kOut);
             const int i = at - 2 * kSteps;  // four chains, one after the other: scores and dP of either half
@@ -280,12 +279,12 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dq(AttArgs a) {
         in_turn<kAll + kStages - 1>([&](auto step) __attribute__((always_inline)) {
             constexpr int at = decltype(step)::value;
             __builtin_amdgcn_sched_barrier(0);
-            if (at + kAhead < kAll) piece[(at + kAhead) & 7] = piece_of(at + kAhead);
-            if (at < 2 * kSteps) dq[at % kOut] = mfma(piece[at & 7], z[at / kOut & 3], dq[at % kOut]);
+            if (at + kAhead < kAll) piece[(at + kAhead) % kRing] = piece_of(at + kAhead);
+            if (at < 2 * kSteps) dq[at % kOut] = mfma(piece[at % kRing], z[at / kOut & 3], dq[at % kOut]);
             else if (at < kAll) {
                 constexpr int i = at - 2 * kSteps, u = i >> 1 & 1;
-                if (i & 1) next_dp[u] = mfma(piece[at & 7], o[i >> 2], next_dp[u]);
-                else next_s[u] = mfma(piece[at & 7], q[i >> 2], next_s[u]);
+                if (i & 1) next_dp[u] = mfma(piece[at % kRing], o[i >> 2], next_dp[u]);
+                else next_s[u] = mfma(piece[at % kRing], q[i >> 2], next_s[u]);
             }
 #pragma unroll
             for (int stage = 0; stage < kStages; stage++)
@@ -299,10 +298,8 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dq(AttArgs a) {
                 }
             here(sum);
             if (BIAS && at == kAll / 4) look_at(kpos[((t + 1) & 3) * kGradTile + lane]);
-            if (at == kAll / 2) {
-                stage(t + 2);  // (its buffers: of K of t - 2, of V of t, read last in the round before)
-                fetch(t + 3);
-            }
+            if (at == 0) fetch(t + 2);
+            if (at == kAll / 2) stage(t + 2);  // (its buffers: of K of t - 2, of V of t, read last in the round before)
         });
         __builtin_amdgcn_sched_barrier(0);
         if (plain) lacks += sum;
@@ -399,8 +396,11 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
         }
         for (int i = tid; i < 4 * nb * cols; i += kAttThreads) sums[i] = 0.f;
     }
+    // (Read, added and written: nobody else has the address meanwhile.  An atomic addition of 64 floats keeps LDS busy for 192 clocks.)
     auto add_at = [&](unsigned place, float x) {
-        __hip_atomic_fetch_add((__attribute__((address_space(3))) float *)(uintptr_t)place, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        typedef __attribute__((address_space(3))) float lds_float;
+        lds_float *at = (lds_float *)(uintptr_t)place;
+        *at = *at + x;
     };
     // keys that are none (and where halves go one after the other, the other half) add to a place of their own that nobody reads
     const unsigned my_aside = lds_place(aside) + tid * 4;
@@ -507,7 +507,6 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
         stage(0, now);
         fetch();
         stage(1, after);
-        fetch();
         qload.clear(tiles + last);  // (round 0 multiplies them with zeros)
         oload.clear(tiles + last + kTile);
         __syncthreads();
@@ -584,8 +583,8 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
             x = special_steps();
         }
         const unsigned rt = my_rows + after, ct = my_columns + last;
-        constexpr int kAll = 8 * kSteps, kAhead = 6;
-        Chunk piece[8];
+        constexpr int kAll = 8 * kSteps, kAhead = 4, kRing = 5;
+        Chunk piece[kRing];
         auto piece_of = [&](int at) {
             if (at < 4 * kSteps) return columns_chunk<E, DP>(ct + (at & 1 ? 0 : kTile), 16 * (at / 2 / kOut), at / 2 % kOut);  // dO and Q in turn
             const int i = at - 4 * kSteps;
@@ -600,27 +599,27 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
             constexpr int at = decltype(step)::value;
             __builtin_amdgcn_sched_barrier(0);
             if (at % (kAll / 2) == 0 && at < kAll) {
-                if (at > 0) {
+                if (at == 0) fetch();  // (tile t + 2)
+                else {
                     __syncthreads();  // the last tile's columns are read
                     stage(t + 2, last);
-                    fetch();
                 }
 #pragma unroll
-                for (int i = 0; i < kAhead; i++) piece[(at + i) & 7] = piece_of(at + i);
+                for (int i = 0; i < kAhead; i++) piece[(at + i) % kRing] = piece_of(at + i);
             }
-            if (at + kAhead < kAll && (at + kAhead) % (kAll / 2) >= kAhead) piece[(at + kAhead) & 7] = piece_of(at + kAhead);
+            if (at + kAhead < kAll && (at + kAhead) % (kAll / 2) >= kAhead) piece[(at + kAhead) % kRing] = piece_of(at + kAhead);
             if (at % (kAll / 8) == 0 && at < kAll) {
                 l4[at / (kAll / 8) & 1] = *(const f32x4 *)(lse + 8 * (8 * at / kAll) + 4 * half);
                 d4[at / (kAll / 8) & 1] = *(const f32x4 *)(delta + 8 * (8 * at / kAll) + 4 * half);
             }
             if (at < 4 * kSteps) {
                 constexpr int i = at / 2;
-                if (at & 1) dk[i % kOut] = mfma(piece[at & 7], z[i / kOut & 3], dk[i % kOut]);
-                else dv[i % kOut] = mfma(piece[at & 7], p[i / kOut & 3], dv[i % kOut]);
+                if (at & 1) dk[i % kOut] = mfma(piece[at % kRing], z[i / kOut & 3], dk[i % kOut]);
+                else dv[i % kOut] = mfma(piece[at % kRing], p[i / kOut & 3], dv[i % kOut]);
             } else if (at < kAll) {
                 constexpr int i = at - 4 * kSteps, u = i >> 1 & 1;
-                if (i & 1) next_dp[u] = mfma(piece[at & 7], v[i >> 2], next_dp[u]);
-                else next_s[u] = mfma(piece[at & 7], k[i >> 2], next_s[u]);
+                if (i & 1) next_dp[u] = mfma(piece[at % kRing], v[i >> 2], next_dp[u]);
+                else next_s[u] = mfma(piece[at % kRing], k[i >> 2], next_s[u]);
             }
 #pragma unroll
             for (int stage = 0; stage < kStages; stage++)
