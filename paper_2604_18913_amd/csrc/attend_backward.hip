@@ -121,7 +121,7 @@ constexpr float kHiddenLse = 1e15f;    // of a row that sees nothing, or is none
 constexpr int kGradTile = 64;
 
 template <class E, int DP, bool CAP, bool BIAS>
-__global__ __launch_bounds__(kAttThreads, 1) void k_att_dq(AttArgs a) {
+__global__ __launch_bounds__(kAttThreads, DP == 64 ? 2 : 1) void k_att_dq(AttArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     typedef typename Vec8<E>::type Chunk;
     constexpr int kTile = kGradTile * DP * 2, kSteps = DP / 16, kOut = DP / 32, kUnder = 32 * DP * 2;  // kUnder: to a tile's second 32 rows
@@ -227,7 +227,7 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dq(AttArgs a) {
     for (int t = 0; t < tiles_n; t++) {
         const bool edge = (t + 1) * kGradTile > least, far = wave_any(size > a.score.most), plain = !edge && !far && !varied;
         Steps x = plain_steps<CAP>(a, b);
-        if (!plain) {
+        auto special = [&](auto exact) __attribute__((always_inline)) {
 #pragma unroll
             for (int u = 0; u < 2; u++) {
                 float bias[16];
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dq(AttArgs a) {
 #pragma unroll
                 for (int r = 0; r < 16; r++) {
                     float away = dp[u][r] - delta;
-                    if (!edge && !far) {
+                    if (!decltype(exact)::value) {
                         const float w = element_w<CAP>(x, s[u][r]);
                         float y = bias[r] - lse;
                         y = CAP ? y + w : __builtin_fmaf(w, x.near0, y);
@@ -259,6 +259,10 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dq(AttArgs a) {
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
+        };
+        if (!plain) {
+            if (!BIAS || edge || far) special(std::true_type{});
+            else special(std::false_type{});
             x = special_steps();
         }
         const unsigned kt = my_rows + k_buffer(t + 1), vt = my_rows + v_buffer(t + 1), ct = my_columns + k_buffer(t - 1);
@@ -527,7 +531,7 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
         const float *lse = lses + (t & 3) * kGradTile, *delta = deltas + (t & 3) * kGradTile;
         const int bucket_now = bucket;
         Steps x = plain_steps<CAP>(a, b);
-        if (!plain) {
+        auto special = [&](auto exact) __attribute__((always_inline)) {
             const unsigned to_head = to_table + g * places_n * 4;
 #pragma unroll
             for (int part = 0; part < 4; part++) {
@@ -557,7 +561,7 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
                     for (int e = 0; e < 4; e++) {
                         const int r = 4 * (j0 + j) + e;
                         float away = dp[u][r] - delta4[e];
-                        if (!edge && !far) {
+                        if (!decltype(exact)::value) {
                             const float w = element_w<CAP>(x, s[u][r]);
                             float y = bias[4 * j + e] - lse4[e];
                             y = CAP ? y + w : __builtin_fmaf(w, x.near0, y);
@@ -580,6 +584,10 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
                     if (BIAS) add_each(bucket_of[i], dy[i]);
                 __builtin_amdgcn_sched_barrier(0);
             }
+        };
+        if (!plain) {
+            if (!BIAS || edge || far) special(std::true_type{});
+            else special(std::false_type{});
             x = special_steps();
         }
         const unsigned rt = my_rows + after, ct = my_columns + last;
