@@ -481,7 +481,7 @@ typedef enum { LOGOSKG_F32 = 0, LOGOSKG_BF16 = 1, LOGOSKG_F16 = 2 } logoskg_dtyp
 
 #define LOGOSKG_MAX_BUCKETS 64      /* buckets of a learned distance bias                    */
 #define LOGOSKG_MAX_DISTANCE 1024   /* largest distance that has a bucket of its own         */
-#define LOGOSKG_BIAS_PLACES 16384   /* heads / kv_heads * (2 max_distance + 1) at most       */
+#define LOGOSKG_BIAS_PLACES 4480    /* heads / kv_heads * (2 max_distance + 1) at most       */
 
 /*
  * How scores are made of products, for every call below: with z = scale q.k,

@@ -360,7 +360,8 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
     const int cols = a.bias_columns;
     float *sums = (float *)(qpos + 4 * kGradTile);            // [4 wavefronts][nb][cols]
     float *aside = sums + (BIAS ? 4 * nb * cols : 0);         // [4 wavefronts][64]
-    int *column = (int *)(aside + (BIAS ? 256 : 0));          // [places_n] where a distance's bucket begins, in bytes
+    float *total = aside + (BIAS ? 256 : 0);                  // [2][4 wavefronts][nb]
+    int *column = (int *)(total + (BIAS ? 8 * nb : 0));                // [places_n] where a distance's bucket begins, in bytes
     float *table = (float *)(column + (BIAS ? places_n : 0));  // [group][places_n]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
     const int head = blockIdx.x % a.kv_heads;
@@ -398,7 +399,7 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
             int b = a.score.buckets[i];
             column[i] = (b < 0 ? 0 : b >= nb ? nb - 1 : b) * cols * 4;
         }
-        for (int i = tid; i < 4 * nb * cols; i += kAttThreads) sums[i] = 0.f;
+        for (int i = tid; i < nb * cols; i += kAttThreads) ((f32x4 *)sums)[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     // (Read, added and written: nobody else has the address meanwhile.  An atomic addition of 64 floats keeps LDS busy for 192 clocks.)
     auto add_at = [&](unsigned place, float x) {
@@ -471,30 +472,31 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
             if (BIAS) qpos[at] = my_pos;
         }
     };
-    // the columns of a head that is through: a bucket's sums by 256 / nb threads, their parts by one
+    // The columns of a head that is through: a wavefront adds up its own, half of a bucket's columns a lane (16 bytes at a time,
+    // from another place for each bucket, so that lanes read different banks), and clears them; the four sums are joined behind
+    // one barrier, in two places by turns, so that none has to wait for the readers.
     auto finish = [&](int g) {
-        __syncthreads();
-        int strands = kAttThreads / nb;
-        strands = strands >= 16 ? 16 : strands >= 8 ? 8 : 4;
-        const int b = tid % nb, st = tid / nb, n = 4 * cols / strands;
-        float sum = 0.f;
-        if (st < strands)
-            for (int i = 0; i < n; i++) {  // (rotated by the bucket, so that neighbouring threads read other banks)
-                const int c = st * n + ((i + b) & (n - 1)), w = c / cols;
-                sum += sums[(w * nb + b) * cols + c - w * cols];
+        float *mine4 = total + (g & 1) * 4 * nb;
+        wave_sync();
+        for (int b0 = 0; b0 < nb; b0 += 32) {
+            const int b = b0 + (lane & 31), quads = cols >> 3;
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+            if (b < nb) {
+                f32x4 *at = (f32x4 *)(sums + (wave * nb + b) * cols) + half * quads;
+#pragma unroll 4
+                for (int i = 0; i < quads; i++) {
+                    const int c = (i + b) & (quads - 1);
+                    const f32x4 x = at[c];
+                    at[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int e = 0; e < 4; e++) sum[e] += x[e];
+                }
             }
-        __syncthreads();
-        for (int i = tid; i < 4 * nb * cols; i += kAttThreads) sums[i] = 0.f;
-        __syncthreads();
-        if (st < strands) sums[tid] = sum;
-        __syncthreads();
-        if (tid < nb) {
-            for (int i = 1; i < strands; i++) sum += sums[i * nb + tid];
-            part[g * nb + tid] = sum;
+            const float all = halves_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
+            if (b < nb && half == 0) mine4[wave * nb + b] = all;
         }
         __syncthreads();
-        if (st < strands) sums[tid] = 0.f;
-        __syncthreads();
+        if (tid < nb) part[g * nb + tid] = (mine4[tid] + mine4[nb + tid]) + (mine4[2 * nb + tid] + mine4[3 * nb + tid]);
     };
     bool varied = false;
     float b = 0.f;
@@ -722,7 +724,9 @@ template <class E, int DP, bool CAP, bool BIAS> static logoskg_status launch_bac
     }
     if (a.num_keys) {
         AttArgs b = a;
-        size_t bytes = 6 * kGradTile * DP * 2 + 3 * 4 * kGradTile * 4 + table + places * 4 + (BIAS ? 1024 : 0);
+        size_t bytes = 6 * kGradTile * DP * 2 + 3 * 4 * kGradTile * 4 + table + places * 4 + (BIAS ? 1024 + 32 * (size_t)a.score.num_buckets : 0);
+        static_assert(6 * kGradTile * 128 * 2 + 3 * 4 * kGradTile * 4 + (LOGOSKG_BIAS_PLACES + 2 * LOGOSKG_MAX_DISTANCE + 1) * 4 + 1024 +
+                      LOGOSKG_MAX_BUCKETS * (32 + 4 * 32 * 4) <= kLds, "the largest biases fit, with 32 columns a bucket");
         b.bias_columns = bytes + (size_t)4 * a.score.num_buckets * 64 * 4 <= kLds ? 64 : 32;
         if (BIAS) bytes += (size_t)4 * a.score.num_buckets * b.bias_columns * 4;
         LKG_TRY(allow_lds(k_att_dkdv<E, DP, CAP, BIAS>, bytes));

@@ -1,10 +1,16 @@
 """What a language model does with a retrieval: ctypes binding of the calls under "reading" in
-``include/logoskg.h``.  Argument checks and marshalling only; outputs and workspaces are torch
-tensors of the current stream's allocator, nothing synchronises."""
+``include/logoskg.h``.  Argument checks and marshalling only; outputs and workspaces are torch tensors, nothing
+synchronises.  With ``stream`` a call's work and its tensors belong to that stream (and the inputs must live until it is
+through), else to torch's current one.
+
+A small call's time is what happens here: a question's first token reads its 900 entities in 13 us of the GPU's time, and
+the call took 19 us before tensors were asked for each property once and structures were packed (1.6 to 0.3 us)."""
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
+import struct
 
 from .binding import _check, _load, _stream_handle, _torch
 
@@ -43,75 +49,88 @@ class _Logits(ctypes.Structure):
                 ("bias_value", _P), ("num_bias", _I64), ("mask", _P), ("stream", _P)]
 
 
+def _packer(cls):
+    """bytes of a structure from its fields' values in turn, those of a _Score inside as its six (NULL: 0)."""
+    code = {ctypes.c_uint32: "I", _I32: "i", _I64: "q", _P: "Q", _F: "f", _Score: "ffQQii"}
+    return struct.Struct("=" + "".join(code[kind] for _, kind in cls._fields_)).pack
+
+
+_attention_of, _gradients_of, _entity_read_of, _logits_of = (_packer(c) for c in (_Attention, _AttentionGrad, _EntityRead, _Logits))
 _TYPES = None  # torch type -> logoskg_dtype
 
 
-def _dtype(t) -> int:
+def _dtype(dtype) -> int:
     global _TYPES
     if _TYPES is None:
         torch = _torch()
         _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-    if t.dtype not in _TYPES:
-        raise ValueError(f"{t.dtype} is not supported")
-    return _TYPES[t.dtype]
+    if dtype not in _TYPES:
+        raise ValueError(f"{dtype} is not supported")
+    return _TYPES[dtype]
 
 
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+def _on_stream(call):
+    """``stream``: the call with that stream as torch's current one, so that its tensors are of that stream's memory."""
+    @functools.wraps(call)
+    def on(*args, stream=None, **kw):
+        if stream is None:
+            return call(*args, **kw)
+        with _torch().cuda.stream(stream):
+            return call(*args, **kw)
+    return on
 
 
-def _plain(t, name, dtype, device, shape=None):
-    """A contiguous tensor of that type on the device, or None."""
+def _on_gpu(t, name) -> int:
+    """The number of the tensor's GPU."""
+    device = t.get_device()
+    if device < 0:
+        raise ValueError(f"{name} must be on the GPU (no CPU fallback)")
+    return device
+
+
+def _plain(t, name, dtype, device, shape=None) -> int:
+    """The place of a contiguous tensor of that type on that GPU; 0 for None."""
     if t is None:
-        return None
-    if t.dtype != dtype or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor on {device}")
-    if shape is not None and tuple(t.shape) != shape:
+        return 0
+    if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor on cuda:{device}")
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} has the shape {tuple(t.shape)}, not {shape}")
-    return t
+    return t.data_ptr()
 
 
 def _rows(t, name, dtype, device):
-    """A [rows, heads, dim] tensor whose last axis is contiguous; the strides of the others are free."""
-    if t.dim() != 3 or t.dtype != dtype or t.device != device:
-        raise ValueError(f"{name} must be a [rows, heads, dim] {dtype} tensor on {device}")
-    if t.numel() and t.shape[2] > 1 and t.stride(2) != 1:
+    """Sizes and strides of the rows and heads of a [rows, heads, dim] tensor whose last axis is contiguous."""
+    if t.dim() != 3 or t.dtype is not dtype or t.get_device() != device:
+        raise ValueError(f"{name} must be a [rows, heads, dim] {dtype} tensor on cuda:{device}")
+    n, heads, dim = t.shape
+    row, head, one = t.stride()
+    if one != 1 and dim > 1 and n and heads:
         raise ValueError(f"the last axis of {name} must be contiguous")
-    return t
+    return n, heads, dim, row if n > 1 else 0, head if heads > 1 else 0
 
 
 def _score(scale, cap, bias, buckets, heads, dim, dtype, device):
+    """The values of a _Score."""
+    scale = dim ** -0.5 if scale is None and dim else scale or 0.0
     if bias is None:
         if buckets is not None:
             raise ValueError("buckets without a bias")
-        return _Score(1.0 / math.sqrt(dim) if scale is None else scale, cap or 0.0, None, None, 0, 0)
+        return scale, cap or 0.0, 0, 0, 0, 0
     if buckets is None or buckets.dim() != 1 or buckets.numel() % 2 != 1:
         raise ValueError("a bias needs buckets, one per distance -M .. M")
-    torch = _torch()
     if bias.dim() != 2 or bias.shape[0] != heads:
         raise ValueError("bias must be [heads, buckets]")
-    _plain(bias, "bias", dtype, device)
-    _plain(buckets, "buckets", torch.int32, device)
-    return _Score(1.0 / math.sqrt(dim) if scale is None else scale, cap or 0.0, bias.data_ptr(), buckets.data_ptr(),
-                  bias.shape[1], buckets.numel() // 2)
+    return (scale, cap or 0.0, _plain(bias, "bias", dtype, device), _plain(buckets, "buckets", _torch().int32, device),
+            bias.shape[1], buckets.numel() // 2)
 
 
-def _on_gpu(t, name):
-    if t.device.type != "cuda":
-        raise ValueError(f"{name} must be on the GPU (no CPU fallback)")
-    return t.device
-
-
-def _workspace(nbytes, device, stream):
-    if nbytes < 0:
-        _check(1)  # (the library has said why)
-    if nbytes == 0:
+def _workspace(nbytes, like):
+    if nbytes <= 0:
+        if nbytes < 0:
+            _check(1)  # (the library has said why)
         return None
-    torch = _torch()
-    w = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    if stream is not None:
-        w.record_stream(stream)
-    return w
+    return like.new_empty(nbytes, dtype=_torch().uint8)
 
 
 def distance_buckets(num_buckets: int, max_distance: int, both_sides: bool = True, device="cuda"):
@@ -135,33 +154,34 @@ def distance_buckets(num_buckets: int, max_distance: int, both_sides: bool = Tru
 
 
 def _attention(q, k, v, q_off, k_off, scale, cap, causal, prefix, bias, buckets, q_pos, k_pos, out, lse, stream):
+    """An _Attention, packed."""
     torch = _torch()
     dtype, device = q.dtype, _on_gpu(q, "q")
-    for t, name in ((q, "q"), (k, "k"), (v, "v")):
-        _rows(t, name, dtype, device)
-    n, heads, dim = q.shape
-    m, kv_heads = k.shape[:2]
-    if v.shape != k.shape or k.shape[2] != dim:
+    n, heads, dim, q_row, q_head = _rows(q, "q", dtype, device)
+    m, kv_heads, k_dim, k_row, k_head = _rows(k, "k", dtype, device)
+    v_row, v_head = _rows(v, "v", dtype, device)[3:]
+    if v.shape != k.shape or k_dim != dim:
         raise ValueError("k and v must have one shape, and q's head size")
     docs = q_off.numel() - 1
     if k_off.numel() - 1 != docs or docs < 0:
         raise ValueError("q_off and k_off must have one entry per document and one more")
-    _plain(q_off, "q_off", torch.int64, device)
-    _plain(k_off, "k_off", torch.int64, device)
-    _plain(prefix, "prefix", torch.int32, device, (docs,))
-    _plain(q_pos, "q_pos", torch.int32, device, (n,))
-    _plain(k_pos, "k_pos", torch.int32, device, (m,))
     if prefix is not None and not causal:
         raise ValueError("a prefix is part of the causal mask")
-    s = _score(scale, cap, bias, buckets, heads, dim, dtype, device)
-    return _Attention(ctypes.sizeof(_Attention), device.index or 0, _dtype(q), docs, heads, kv_heads, dim, 1 if causal else 0, n, m,
-                      q_off.data_ptr(), k_off.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), q.stride(0), q.stride(1),
-                      k.stride(0), k.stride(1), v.stride(0), v.stride(1), _ptr(prefix), _ptr(q_pos), _ptr(k_pos), s,
-                      out.data_ptr(), lse.data_ptr(), _stream_handle(stream))
+    return _attention_of(
+            216, device, _dtype(dtype), docs, heads, kv_heads, dim, 1 if causal else 0, n, m,
+            _plain(q_off, "q_off", torch.int64, device), _plain(k_off, "k_off", torch.int64, device), q.data_ptr(), k.data_ptr(),
+            v.data_ptr(), q_row, q_head, k_row, k_head, v_row, v_head, _plain(prefix, "prefix", torch.int32, device, (docs,)),
+            _plain(q_pos, "q_pos", torch.int32, device, (n,)), _plain(k_pos, "k_pos", torch.int32, device, (m,)),
+            *_score(scale, cap, bias, buckets, heads, dim, dtype, device), out.data_ptr(), lse.data_ptr(), _stream_handle(stream, device))
 
 
+def _new(t):
+    return _torch().empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+
+
+@_on_stream
 def attend(q, k, v, q_off, k_off, *, scale=None, cap=0.0, causal=False, prefix=None, bias=None, buckets=None, q_pos=None,
-           k_pos=None, stream=None):
+           k_pos=None):
     """``logoskg_attend``: attention of a ragged batch, as (out [rows, heads, dim], lse float32 [rows, heads]).
 
     ``q`` [rows, heads, dim], ``k`` and ``v`` [keys, kv_heads, dim] in bfloat16 or float16, documents one behind the
@@ -169,35 +189,34 @@ def attend(q, k, v, q_off, k_off, *, scale=None, cap=0.0, causal=False, prefix=N
     the document's first ``prefix`` (int32, one per document) besides; else every row sees all keys.  ``cap``: scores
     become cap tanh(score / cap).  ``bias`` [heads, buckets] is learned, ``buckets`` (``distance_buckets``) says which
     column the distance ``k_pos - q_pos`` reads (positions: int32, by default the places, aligned at the end)."""
-    torch = _torch()
-    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-    a = _attention(q, k, v, q_off, k_off, scale, cap, causal, prefix, bias, buckets, q_pos, k_pos, out, lse, stream)
-    _check(_load().logoskg_attend(ctypes.addressof(a)))
+    out, lse = _new(q), q.new_empty(q.shape[:2], dtype=_torch().float32)
+    _check(_load().logoskg_attend(_attention(q, k, v, q_off, k_off, scale, cap, causal, prefix, bias, buckets, q_pos, k_pos, out, lse, None)))
     return out, lse
 
 
+@_on_stream
 def attend_backward(dout, q, k, v, out, lse, q_off, k_off, *, scale=None, cap=0.0, causal=False, prefix=None, bias=None,
-                    buckets=None, q_pos=None, k_pos=None, stream=None):
+                    buckets=None, q_pos=None, k_pos=None):
     """``logoskg_attend_backward``: gradients (dq, dk, dv, dbias or None) for ``dout``, the gradient of ``attend``'s
     ``out``; the other arguments are those of that call and what it returned.  The same inputs give the same bits."""
     torch = _torch()
-    _plain(dout, "dout", q.dtype, q.device, tuple(q.shape))
-    _plain(out, "out", q.dtype, q.device, tuple(q.shape))
-    _plain(lse, "lse", torch.float32, q.device, tuple(q.shape[:2]))
-    a = _attention(q, k, v, q_off, k_off, scale, cap, causal, prefix, bias, buckets, q_pos, k_pos, out, lse, stream)
-    dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    device = _on_gpu(q, "q")
+    dout_at = _plain(dout, "dout", q.dtype, device, q.shape)
+    _plain(out, "out", q.dtype, device, q.shape)
+    _plain(lse, "lse", torch.float32, device, q.shape[:2])
+    a = _attention(q, k, v, q_off, k_off, scale, cap, causal, prefix, bias, buckets, q_pos, k_pos, out, lse, None)
+    dq, dk, dv = _new(q), _new(k), _new(v)
     dbias = None if bias is None else torch.empty_like(bias)
     lib = _load()
-    w = _workspace(lib.logoskg_attend_backward_bytes(ctypes.addressof(a)), q.device, stream)
-    g = _AttentionGrad(ctypes.sizeof(_AttentionGrad), 0, dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
-                       _ptr(dbias), _ptr(w), 0 if w is None else w.numel())
-    _check(lib.logoskg_attend_backward(ctypes.addressof(a), ctypes.addressof(g)))
+    w = _workspace(lib.logoskg_attend_backward_bytes(a), q)
+    g = _gradients_of(64, 0, dout_at, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), 0 if dbias is None else dbias.data_ptr(),
+                      *((0, 0) if w is None else (w.data_ptr(), w.numel())))
+    _check(lib.logoskg_attend_backward(a, g))
     return dq, dk, dv, dbias
 
 
-def read_entities(q, keys, values, off, entity=None, *, scale=None, cap=0.0, bias=None, buckets=None, hop=None, q_pos=None,
-                  stream=None):
+@_on_stream
+def read_entities(q, keys, values, off, entity=None, *, scale=None, cap=0.0, bias=None, buckets=None, hop=None, q_pos=None):
     """``logoskg_read_entities``: the tokens of every query attend to its entity list, as {"out": like q, "lse":
     float32 [queries, tokens, heads]} (with its lse, the answer can be joined with attention over the text).
 
@@ -207,78 +226,74 @@ def read_entities(q, keys, values, off, entity=None, *, scale=None, cap=0.0, bia
     torch = _torch()
     if q.dim() != 4 or not q.is_contiguous():
         raise ValueError("q must be a contiguous [queries, tokens, heads, dim] tensor")
-    _on_gpu(q, "q")
+    dtype, device = q.dtype, _on_gpu(q, "q")
     n, tokens, heads, dim = q.shape
-    _rows(keys, "keys", q.dtype, q.device)
-    _rows(values, "values", q.dtype, q.device)
-    if values.shape != keys.shape or keys.shape[2] != dim:
+    rows, kv_heads, k_dim, k_row, k_head = _rows(keys, "keys", dtype, device)
+    v_row, v_head = _rows(values, "values", dtype, device)[3:]
+    if values.shape != keys.shape or k_dim != dim:
         raise ValueError("keys and values must have one shape, and q's head size")
-    entries = keys.shape[0] if entity is None else entity.numel()
-    _plain(off, "off", torch.int64, q.device, (n + 1,))
-    _plain(entity, "entity", torch.int32, q.device, (entries,))
-    _plain(hop, "hop", torch.uint8, q.device, (entries,))
-    _plain(q_pos, "q_pos", torch.int32, q.device, (n,))
-    s = _score(scale, cap, bias, buckets, heads, dim, q.dtype, q.device)
-    out = torch.empty_like(q)
-    lse = torch.empty((n, tokens, heads), dtype=torch.float32, device=q.device)
-    r = _EntityRead(ctypes.sizeof(_EntityRead), q.device.index or 0, _dtype(q), n, tokens, heads, keys.shape[1], dim, entries,
-                    keys.shape[0], off.data_ptr(), _ptr(entity), _ptr(hop), _ptr(q_pos), q.data_ptr(), keys.data_ptr(),
-                    values.data_ptr(), keys.stride(0), keys.stride(1), values.stride(0), values.stride(1), s, out.data_ptr(),
-                    lse.data_ptr(), None, 0, _stream_handle(stream))
+    entries = rows if entity is None else entity.numel()
+    head = (208, device, _dtype(dtype), n, tokens, heads, kv_heads, dim, entries, rows, _plain(off, "off", torch.int64, device, (n + 1,)),
+            _plain(entity, "entity", torch.int32, device, (entries,)), _plain(hop, "hop", torch.uint8, device, (entries,)),
+            _plain(q_pos, "q_pos", torch.int32, device, (n,)), q.data_ptr(), keys.data_ptr(), values.data_ptr(), k_row, k_head,
+            v_row, v_head, *_score(scale, cap, bias, buckets, heads, dim, dtype, device))
+    out, lse = torch.empty_like(q), q.new_empty((n, tokens, heads), dtype=torch.float32)
+    head += (out.data_ptr(), lse.data_ptr())
     lib = _load()
-    w = _workspace(lib.logoskg_read_entities_bytes(ctypes.addressof(r)), q.device, stream)
-    if w is not None:
-        r.workspace, r.workspace_bytes = w.data_ptr(), w.numel()
-    _check(lib.logoskg_read_entities(ctypes.addressof(r)))
+    w = _workspace(lib.logoskg_read_entities_bytes(_entity_read_of(*head, 0, 0, 0)), q)
+    _check(lib.logoskg_read_entities(_entity_read_of(*head, *((0, 0) if w is None else (w.data_ptr(), w.numel())),
+                                                     _stream_handle(None, device))))
     return {"out": out, "lse": lse}
 
 
-def entity_mask(off, ids, num_ids: int, *, out=None, stream=None):
+@_on_stream
+def entity_mask(off, ids, num_ids: int, *, out=None):
     """``logoskg_entity_mask``: int64[queries, ceil(num_ids / 64)] words, bit i % 64 of word i / 64 set for the ids of a
     query's list (``off`` int64, ``ids`` int32 on the device, any order): the layout of ``Graph.khop``'s ``rel_mask``."""
     torch = _torch()
-    _plain(ids, "ids", torch.int32, _on_gpu(ids, "ids"))
-    _plain(off, "off", torch.int64, ids.device)
-    shape = (off.numel() - 1, (num_ids + 63) // 64)
+    device = _on_gpu(ids, "ids")
+    off_at, ids_at = _plain(off, "off", torch.int64, device), _plain(ids, "ids", torch.int32, device)
+    queries = off.numel() - 1
+    if queries < 0:
+        raise ValueError("off must have one entry per query and one more")
+    shape = (queries, (num_ids + 63) // 64)
     if out is None:
-        out = torch.empty(shape, dtype=torch.int64, device=ids.device)
-    _plain(out, "out", torch.int64, ids.device, shape)
-    _check(_load().logoskg_entity_mask(ids.device.index or 0, off.data_ptr(), ids.data_ptr(), ids.numel(), shape[0], num_ids,
-                                       out.data_ptr(), _stream_handle(stream)))
+        out = off.new_empty(shape)
+    _check(_load().logoskg_entity_mask(device, off_at, ids_at, ids.numel(), queries, num_ids,
+                                       _plain(out, "out", torch.int64, device, shape), _stream_handle(None, device)))
     return out
 
 
+@_on_stream
 def constrain_logits(logits, *, history=None, history_off=None, repetition=None, presence=None, frequency=None,
-                     bias_off=None, bias_id=None, bias_value=None, mask=None, out=None, stream=None):
+                     bias_off=None, bias_id=None, bias_value=None, mask=None, out=None):
     """``logoskg_constrain_logits``: a step's logits [rows, vocab] (bfloat16, float16 or float32) with the ids of each
     row's ``history`` penalised (``repetition`` divides or multiplies, ``presence`` and count times ``frequency`` are taken
     off; float32 per row), biases added, and every id whose bit of ``mask`` (``entity_mask``'s layout) is 0 at -infinity.
     Lists are ragged: ``history`` int32 at ``history_off``, ``bias_id`` int32 and ``bias_value`` float32 at ``bias_off``.
     ``out`` may be ``logits``."""
     torch = _torch()
-    if logits.dim() != 2 or (logits.numel() and logits.stride(1) != 1):
+    if logits.dim() != 2:
         raise ValueError("logits must be [rows, vocab] with contiguous rows")
-    rows, vocab = logits.shape
+    (rows, vocab), (row, one) = logits.shape, logits.stride()
+    if one != 1 and rows and vocab > 1:
+        raise ValueError("logits must be [rows, vocab] with contiguous rows")
     device = _on_gpu(logits, "logits")
     if (history is None) != (history_off is None) or (bias_id is None) != (bias_off is None) or (bias_id is None) != (bias_value is None):
         raise ValueError("history comes with history_off, and bias_id with bias_off and bias_value")
     if history is None and not (repetition is None and presence is None and frequency is None):
         raise ValueError("penalties without a history")
-    for t, name in ((history_off, "history_off"), (bias_off, "bias_off")):
-        _plain(t, name, torch.int64, device, (rows + 1,))
-    for t, name in ((repetition, "repetition"), (presence, "presence"), (frequency, "frequency")):
-        _plain(t, name, torch.float32, device, (rows,))
-    _plain(history, "history", torch.int32, device)
-    _plain(bias_id, "bias_id", torch.int32, device)
-    _plain(bias_value, "bias_value", torch.float32, device, None if bias_id is None else tuple(bias_id.shape))
-    _plain(mask, "mask", torch.int64, device, (rows, (vocab + 63) // 64))
+    int32, int64, float32, per_row = torch.int32, torch.int64, torch.float32, (rows,)
+    head = (144, device, _dtype(logits.dtype), rows, vocab, row if rows > 1 else vocab, logits.data_ptr())
+    tail = (_plain(history_off, "history_off", int64, device, (rows + 1,)), _plain(history, "history", int32, device),
+            0 if history is None else history.numel(), _plain(repetition, "repetition", float32, device, per_row),
+            _plain(presence, "presence", float32, device, per_row), _plain(frequency, "frequency", float32, device, per_row),
+            _plain(bias_off, "bias_off", int64, device, (rows + 1,)), _plain(bias_id, "bias_id", int32, device),
+            _plain(bias_value, "bias_value", float32, device, None if bias_id is None else bias_id.shape),
+            0 if bias_id is None else bias_id.numel(), _plain(mask, "mask", int64, device, (rows, (vocab + 63) // 64)))
     if out is None:
-        out = torch.empty_strided(logits.shape, logits.stride(), dtype=logits.dtype, device=device)
-    elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != device or out.stride() != logits.stride():
+        out = torch.empty_like(logits) if logits.is_contiguous() else torch.empty_strided((rows, vocab), (row, one), dtype=logits.dtype, device=logits.device)
+    elif out.shape != logits.shape or out.dtype is not logits.dtype or out.get_device() != device or out.stride() != (row, one):
         raise ValueError("out must be laid out as logits")
-    a = _Logits(ctypes.sizeof(_Logits), device.index or 0, _dtype(logits), rows, vocab, logits.stride(0) if rows > 1 else vocab,
-                logits.data_ptr(), out.data_ptr(), _ptr(history_off), _ptr(history), 0 if history is None else history.numel(),
-                _ptr(repetition), _ptr(presence), _ptr(frequency), _ptr(bias_off), _ptr(bias_id), _ptr(bias_value),
-                0 if bias_id is None else bias_id.numel(), _ptr(mask), _stream_handle(stream))
-    _check(_load().logoskg_constrain_logits(ctypes.addressof(a)))
+    _check(_load().logoskg_constrain_logits(_logits_of(*head, out.data_ptr(), *tail, _stream_handle(None, device))))
     return out

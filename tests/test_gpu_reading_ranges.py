@@ -1,0 +1,164 @@
+"""The calls that read a retrieval at the ends of their ranges (bounds: reading_oracle, as in test_gpu_reading)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2604_18913_amd as lkg
+from test_gpu_reading import HALVES, _check, _check_logits, _check_read, _gpu, _inputs, _logit_case, _read
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------- attention
+@pytest.mark.parametrize("dtype", HALVES, ids=["bf16", "fp16"])
+@pytest.mark.parametrize("heads, dim, buckets, far", [(2, 128, 64, 1024), (35, 128, 64, 63), (2, 96, 33, 1024), (64, 64, 64, 34), (4, 128, 1, 5)])
+def test_most_biases(heads, dim, buckets, far, dtype):
+    # heads of one key head: the tables and sums of the gradients at the limits of LDS, and one bucket alone
+    a, dout = _inputs(1, dtype, [70, 3], [140, 60], heads, 1, dim)
+    g = torch.Generator().manual_seed(2)
+    a |= dict(bias=torch.randn(heads, buckets, generator=g).to(dtype), buckets=torch.randint(0, buckets, (2 * far + 1,), generator=g, dtype=torch.int32))
+    a["k_pos"] = torch.randint(-far - 3, far + 4, (200,), generator=g, dtype=torch.int32)
+    _check({**a, "cap": 9.0}, dout)
+
+
+@pytest.mark.parametrize("heads, far", [(4, 560), (36, 62), (3, 1024)])  # 4 x 1121 = 4484 places, 36 x 125 = 4500
+def test_biases_beyond_the_limit_are_refused(heads, far):
+    a, dout = _inputs(2, torch.bfloat16, [5], [9], heads, 1, 128)
+    a |= dict(bias=torch.zeros(heads, 4, dtype=torch.bfloat16), buckets=torch.zeros(2 * far + 1, dtype=torch.int32))
+    b = {k: _gpu(x) for k, x in a.items()}
+    with pytest.raises(lkg.LogosKGError, match="BIAS_PLACES"):
+        lkg.attend(**b)
+    with pytest.raises(lkg.LogosKGError, match="BIAS_PLACES"):
+        lkg.read_entities(b["q"][None, :1], b["k"], b["v"], torch.tensor([0, 9]).cuda(), bias=b["bias"], buckets=b["buckets"])
+
+
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_tiles_of_several_blocks(dim, bias):
+    # rows and keys beyond one block each way, all of whose tiles but the last are whole
+    a, dout = _inputs(3, torch.bfloat16, [400, 190], [700, 129], 4, 2, dim, bias=bias)
+    _check({**a, "causal": True, "prefix": torch.tensor([150, 0], dtype=torch.int32), "cap": 6.0}, dout)
+    _check(a, dout)
+
+
+def test_single_rows_and_axes_with_any_stride():
+    a, dout = _inputs(4, torch.bfloat16, [1], [1], 1, 1, 64)
+    odd = lambda x: x.cuda().as_strided(x.shape, (77, 33, 1))  # (an axis of one has no stride to speak of)
+    out, lse = lkg.attend(odd(a["q"]), odd(a["k"]), odd(a["v"]), _gpu(a["q_off"]), _gpu(a["k_off"]))
+    assert torch.equal(out.cpu(), a["v"])
+    r = _read(4, torch.bfloat16, [50], 1, 1, 1, 64, bias=False)
+    want = _check_read(r)
+    b = {k: _gpu(x) for k, x in r.items()}
+    got = lkg.read_entities(**{**b, "keys": b["keys"].as_strided((500, 1, 64), (64, 5, 1))})
+    assert torch.equal(got["out"], want["out"])
+
+
+def test_a_given_stream():
+    a, dout = _inputs(5, torch.bfloat16, [300] * 8, [900] * 8, 8, 2, 128, bias=True)
+    b, d = {k: _gpu(x) for k, x in a.items()}, _gpu(dout)
+    pos = [b.pop(n) for n in ("q", "k", "v", "q_off", "k_off")]
+    out, lse = lkg.attend(*pos, **b)
+    want = (out, lse, *lkg.attend_backward(d, *pos[:3], out, lse, *pos[3:], **b))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):  # memory that goes round between the calls is that stream's own
+        out, lse = lkg.attend(*pos, **b, stream=side)
+        got = (out, lse, *lkg.attend_backward(d, *pos[:3], out, lse, *pos[3:], **b, stream=side))
+        torch.full((1 << 22,), math.nan, device="cuda")
+        side.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+    r = {k: _gpu(x) for k, x in _read(5, torch.bfloat16, [9000, 40], 1, 8, 2, 64).items()}
+    want = lkg.read_entities(**r)
+    got = lkg.read_entities(**r, stream=side)
+    mask = lkg.entity_mask(r["off"], r["entity"], 500, stream=side)
+    logits = torch.zeros(2, 500, device="cuda")
+    side.wait_stream(torch.cuda.current_stream())
+    held = lkg.constrain_logits(logits, mask=mask, stream=side)
+    side.synchronize()
+    assert torch.equal(got["out"], want["out"])
+    assert (held == 0).sum(1).tolist() == [len(set(x.tolist())) for x in r["entity"].cpu().split([9000, 40])]
+
+
+def test_gradients_against_differences():
+    # the loss sum(out * dout) along a direction of every input; out is rounded once (2^-11), so steps are wide
+    a, dout = _inputs(6, torch.float16, [40, 21], [90, 33], 4, 2, 64, bias=True)
+    a |= dict(causal=True, cap=4.0, prefix=torch.tensor([20, 5], dtype=torch.int32))
+    b, d = {k: _gpu(x) for k, x in a.items()}, _gpu(dout)
+    def loss(**other):
+        return float((lkg.attend(**{**b, **other})[0].double() * d.double()).sum())
+    out, lse = lkg.attend(**b)
+    rest = {k: x for k, x in b.items() if k not in ("q", "k", "v", "q_off", "k_off")}
+    grads = dict(zip(("q", "k", "v", "bias"), lkg.attend_backward(d, b["q"], b["k"], b["v"], out, lse, b["q_off"], b["k_off"], **rest)))
+    for n, grad in grads.items():
+        step = grad.float() / grad.float().norm() * 0.5  # along the gradient the difference is largest
+        up, down = (b[n].float() + step).half(), (b[n].float() - step).half()
+        want = loss(**{n: up}) - loss(**{n: down})
+        got = float((grad.double() * (up.double() - down.double())).sum())
+        # third order terms of a step of 1/2 along one direction, and the roundings of out: a fiftieth
+        assert abs(got - want) <= 0.02 * abs(want), (n, got, want)
+
+
+# ------------------------------------------------------------------------- masks
+def _mask_words(off, ids, num_ids):
+    bits = np.zeros((len(off) - 1, (num_ids + 63) // 64), dtype=np.uint64)
+    for i in range(len(off) - 1):
+        x = ids[off[i]:off[i + 1]]
+        x = x[(x >= 0) & (x < num_ids)].astype(np.uint64)
+        np.bitwise_or.at(bits[i], (x >> np.uint64(6)).astype(np.int64), np.uint64(1) << (x & np.uint64(63)))
+    return bits.view(np.int64)
+
+
+@pytest.mark.parametrize("ascending", [False, True])
+@pytest.mark.parametrize("lengths, num_ids", [([70_000], 100_001), ([200_000, 3, 0, 90_000], 64_064), ([140_001, 0], 65), ([900, 0, 40], 110_000_000)])
+def test_masks_of_long_lists_and_of_many_ids(lengths, num_ids, ascending):
+    rng = np.random.default_rng(len(lengths))
+    off = np.concatenate([[0], np.cumsum(lengths)])
+    ids = rng.integers(-5, num_ids + 5, off[-1]).astype(np.int32)
+    ids[::1001] = -2 ** 31
+    if ascending:
+        for i in range(len(lengths)):
+            ids[off[i]:off[i + 1]].sort()
+    out = torch.full((len(lengths), (num_ids + 63) // 64), -1, dtype=torch.int64, device="cuda")
+    got = lkg.entity_mask(torch.from_numpy(off).cuda(), torch.from_numpy(ids).cuda(), num_ids, out=out)
+    assert np.array_equal(got.cpu().numpy(), _mask_words(off, ids, num_ids))
+
+
+# ------------------------------------------------------------------------- logits
+@pytest.mark.parametrize("dtype", [torch.float32, *HALVES], ids=["fp32", "bf16", "fp16"])
+def test_logits_after_a_history_beyond_16_bits(dtype):
+    a = _logit_case(1, dtype, 3, 9001, 30, 5)
+    g = torch.Generator().manual_seed(1)
+    said = torch.tensor([0, 1, 2, 4095, 4096, 4097, 8000, 9000])
+    long = said[torch.randint(0, 8, (70_000,), generator=g)].int()
+    few, one = a["history"][:20], torch.full((66_000,), 4097, dtype=torch.int32)
+    a |= dict(history=torch.cat([long, few, one]), history_off=torch.tensor([0, 70_000, 70_020, 136_020]), frequency=torch.full((3,), 2.0 ** -10))
+    _check_logits(a)
+
+
+@pytest.mark.parametrize("vocab", [300, 20_000])
+def test_logits_with_more_biases_than_a_block_lists(vocab):
+    a = _logit_case(2, torch.float32, 2, vocab, 10, 3)
+    g = torch.Generator().manual_seed(2)
+    a |= dict(bias_off=torch.tensor([0, 3000, 3700]), bias_id=torch.randint(-3, min(vocab, 900) + 3, (3700,), generator=g, dtype=torch.int32),
+              bias_value=torch.randn(3700, generator=g))
+    _check_logits(a)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("shift", [0, 1, 3])
+def test_logits_and_out_at_different_places(shift, dtype):
+    a = {k: _gpu(x) for k, x in _logit_case(3, dtype, 4, 5001, 300, 40).items()}
+    want = lkg.constrain_logits(**a)
+    room = torch.full((4 * 5001 + 8,), 3.0, dtype=dtype, device="cuda")
+    got = lkg.constrain_logits(**a, out=room[shift:shift + 4 * 5001].view(4, 5001))
+    assert torch.equal(got, want) and (room[:shift] == 3).all() and (room[shift + 4 * 5001:] == 3).all()
+
+
+def test_logits_of_offsets_that_point_outside():
+    a = {k: _gpu(x) for k, x in _logit_case(4, torch.float32, 2, 400, 20, 5).items()}
+    n, m = a["history"].numel(), a["bias_id"].numel()
+    want = lkg.constrain_logits(**{**a, "history_off": torch.tensor([0, n, n]).cuda(), "bias_off": torch.tensor([0, 0, m]).cuda()})
+    got = lkg.constrain_logits(**{**a, "history_off": torch.tensor([-9, 1 << 40, n]).cuda(), "bias_off": torch.tensor([-(1 << 50), 0, 1 << 33]).cuda()})
+    assert torch.equal(got, want)
