@@ -8,6 +8,7 @@ namespace lkg {
 constexpr int kAttThreads = 256;  // four wavefronts
 constexpr int kAttRowsShift = 7;  // a block's rows: 4 x 32
 constexpr int kAttRows = 1 << kAttRowsShift;
+constexpr int kFewShift = 5;       // rows of a block where there are few: 32
 constexpr size_t kLds = 160 << 10;                        // of a compute unit
 constexpr long long kMostRows = (1ll << 31) - (1 << 16);  // of a batch: places in a document are 32-bit, with room for a tile
 constexpr long long kMostStride = 1 << 23;                // between rows, in elements: a tile's rows within 2^31 bytes
@@ -32,6 +33,7 @@ struct AttArgs {
     float curve;       // .. of scale (1 - tanh^2) = scale + curve y^2, y = c tanh in units of log 2
     float slope;       // with a cap: 4 scale, of scale (1 - tanh^2) = 4 scale r (1 - r), r = 1 / (2^(z k) + 1)
     long long row_blocks, key_blocks;
+    long long few_blocks;  // of 32 rows
     int bias_columns;  // 64, or 32 where LDS has no room for them
 };
 
@@ -41,7 +43,7 @@ struct AttDoc {  // a document: where its rows and keys begin, and how many ther
     // keys that row i sees: the first seen(i)
     __device__ __forceinline__ int seen(int i, int causal) const {
         if (!causal) return keys;
-        int n = i + keys - rows + 1;  // (rows and keys below 2^31)
+        int n = i + (keys - rows) + 1;  // (rows and keys below 2^31: their sum may not be)
         n = n < prefix ? prefix : n;
         return n < 0 ? 0 : n > keys ? keys : n;
     }
@@ -112,6 +114,64 @@ template <class E> __device__ __forceinline__ typename Vec8<E>::type row_chunk(c
     u32x4 x = {0, 0, 0, 0};
     if (in && c < dim) x = *(const u32x4 *)(row + c);
     return as8<E>(x);
+}
+
+// A row's output, O^T in the layout of the matrix instruction's result, times `by`.
+template <class E, int DP> __device__ __forceinline__ void write_row(const f32x16 (&o)[DP / 32], float by, E *out, int dim, int half) {
+#pragma unroll
+    for (int i = 0; i < DP / 32; i++)
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+            int c = 32 * i + 8 * r + 4 * half;
+            if (c >= dim) continue;
+            typename Vec4<E>::type x;
+#pragma unroll
+            for (int e = 0; e < 4; e++) x[e] = (E)(o[i][4 * r + e] * by);
+            *(typename Vec4<E>::type *)(out + c) = x;
+        }
+}
+
+// Four wavefronts' maxima, sums and outputs of the same 32 rows joined at the largest of their maxima: `top` and `sum` in all,
+// the output in the first one's o.  The block's LDS from `lds` on (DP 256 bytes) is free for it behind the first barrier.
+struct Joined { float top, sum; };
+template <int DP> __device__ __forceinline__ Joined join_wavefronts(f32x16 (&o)[DP / 32], float m, float l, char *lds, float (&wave_m)[4][32], float (&wave_l)[4][32], int wave, int lane) {
+    constexpr int kOut = DP / 32;
+    const int half = lane >> 5, r31 = lane & 31;
+    l = halves_sum(l);
+    if (half == 0) wave_m[wave][lane] = m, wave_l[wave][lane] = l;
+    __syncthreads();
+    const float top = fmaxf(fmaxf(wave_m[0][r31], wave_m[1][r31]), fmaxf(wave_m[2][r31], wave_m[3][r31]));
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; w++) sum += wave_l[w][r31] * exp2_fast(wave_m[w][r31] - top);
+    const float shrink = exp2_fast(m - top);
+#pragma unroll
+    for (int i = 0; i < kOut; i++) o[i] *= shrink;
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    f32x4 *box = (f32x4 *)lds;  // [wavefront][DP / 4][32 rows] (the tiles are read)
+#pragma unroll
+    for (int round = 2; round > 0; round >>= 1) {
+        if (wave >= round && wave < 2 * round) {
+#pragma unroll
+            for (int i = 0; i < kOut; i++)
+#pragma unroll
+                for (int r = 0; r < 4; r++)
+                    box[((wave - round) * (DP / 4) + 8 * i + 2 * r + half) * 32 + r31] = f32x4{o[i][4 * r], o[i][4 * r + 1], o[i][4 * r + 2], o[i][4 * r + 3]};
+        }
+        __syncthreads();
+        if (wave < round) {
+#pragma unroll
+            for (int i = 0; i < kOut; i++)
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    f32x4 x = box[(wave * (DP / 4) + 8 * i + 2 * r + half) * 32 + r31];
+#pragma unroll
+                    for (int e = 0; e < 4; e++) o[i][4 * r + e] += x[e];
+                }
+        }
+        __syncthreads();
+    }
+    return Joined{top, sum};
 }
 
 logoskg_status attend_args(const logoskg_attention *a, AttArgs *o, const char *call);

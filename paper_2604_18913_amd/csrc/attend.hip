@@ -52,7 +52,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
     int q_low = 0, q_high = 0;  // the wavefront's lowest and highest position
     Places places = {0, 0, 0};
     if (BIAS) {
-        const int q_pos = a.q_pos ? a.q_pos[doc.row0 + row] : row + doc.keys - doc.rows;
+        const int q_pos = a.q_pos ? a.q_pos[doc.row0 + row] : row + (doc.keys - doc.rows);
         places = places_of_keys(q_pos, M, lds_place(my_table));
         q_low = __builtin_amdgcn_readfirstlane(wave_min(q_pos));
         q_high = __builtin_amdgcn_readfirstlane(wave_max(q_pos));
@@ -271,19 +271,136 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
     if (!mine) return;
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;  // (a NaN stays one)
     const long long place = (doc.row0 + row) * a.heads + h;
-    E *out = (E *)a.out + place * a.dim;
-#pragma unroll
-    for (int i = 0; i < kOut; i++)
-#pragma unroll
-        for (int r = 0; r < 4; r++) {
-            int c = 32 * i + 8 * r + 4 * half;
-            if (c >= a.dim) continue;
-            typename Vec4<E>::type x;
-#pragma unroll
-            for (int e = 0; e < 4; e++) x[e] = (E)(o[i][4 * r + e] * inv);
-            *(typename Vec4<E>::type *)(out + c) = x;
-        }
+    write_row<E, DP>(o, inv, (E *)a.out + place * a.dim, a.dim, half);
     if (half == 0) a.lse[place] = l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2;
+}
+
+// Few rows: one block is 32 rows of (document, key head), and its four wavefronts take every fourth tile of 32 keys and
+// join at the end, so that a short prompt before many keys is spread over four times the units and each of them does a
+// quarter of the keys.  As in the read of entity lists, keys go from memory into the registers that the matrix
+// instruction reads and values through the wavefront's own piece of LDS; no wavefront waits for another.
+constexpr int kFewKeys = 32;
+
+template <class E, int DP, bool CAP, bool BIAS>
+__global__ __launch_bounds__(kAttThreads, 2) void k_attend_few(AttArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    constexpr int kTile = kFewKeys * DP * 2, kSteps = DP / 16, kOut = DP / 32, kRow = DP / 8;  // kRow: chunks of a row
+    float *table = (float *)(lds + 4 * kTile);  // [group][2 M + 1]
+    __shared__ __attribute__((aligned(16))) int kpos[4][kFewKeys];
+    __shared__ float wave_m[4][32], wave_l[4][32];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
+    const int head = blockIdx.x % a.kv_heads;
+    const long long block = a.few_blocks - 1 - blockIdx.x / a.kv_heads;  // the last rows of a document see most: first
+    const int d = document_of(a.q_off, a.num_docs, a.num_rows, a.group, kFewShift, block, lane);
+    const AttDoc doc = att_doc(a, d);
+    const long long first = (block - first_block(a.q_off, d, a.num_rows, a.group, kFewShift)) << kFewShift;
+    const long long vrows = (long long)doc.rows * a.group;
+    if (first >= vrows || first < 0) return;
+
+    const long long vr = first + (lane & 31);
+    const bool mine = vr < vrows;
+    const long long vr_in = mine ? vr : vrows - 1;
+    const int row = (int)(vr_in / a.group), g = (int)(vr_in % a.group), h = head * a.group + g;
+    const int seen = mine ? doc.seen(row, a.causal) : 0;
+    const int least = doc.seen((int)(first / a.group), a.causal);  // of the block's first row, and of its last
+    const int most = doc.seen((int)((first + 31 < vrows ? first + 31 : vrows - 1) / a.group), a.causal);
+    const int tiles_n = (most + kFewKeys - 1) / kFewKeys;
+
+    const E *keys = (const E *)a.k + doc.key0 * a.k_row + (long long)head * a.k_head;
+    const E *values = (const E *)a.v + doc.key0 * a.v_row + (long long)head * a.v_head;
+    u32x4 k[kSteps], v[kSteps];
+    int kp = 0;
+    auto fetch = [&](int t) {
+        const long long j = (long long)t * kFewKeys + (lane & 31);
+        const E *krow = keys + j * a.k_row;
+#pragma unroll
+        for (int kk = 0; kk < kSteps; kk++) k[kk] = __builtin_bit_cast(u32x4, row_chunk<E>(krow, j < doc.keys, kk, a.dim, lane));
+#pragma unroll
+        for (int i = 0; i < kSteps; i++) {
+            const int at = i * 64 + lane, c = (at % kRow) * 8;
+            const long long r = (long long)t * kFewKeys + at / kRow;
+            v[i] = r < doc.keys && c < a.dim ? *(const u32x4 *)(values + r * a.v_row + c) : u32x4{0, 0, 0, 0};
+        }
+        if (BIAS) {
+            const int in = j < doc.keys ? (int)j : doc.keys - 1;
+            kp = a.k_pos ? a.k_pos[doc.key0 + in] : in;
+        }
+    };
+    if (wave < tiles_n) fetch(wave);
+    const E *qrow = (const E *)a.q + (doc.row0 + row) * a.q_row + (long long)h * a.q_head;
+    typename Vec8<E>::type q[kSteps];
+#pragma unroll
+    for (int kk = 0; kk < kSteps; kk++) q[kk] = row_chunk<E>(qrow, mine, kk, a.dim, lane);
+    Places places = {0, 0, 0};
+    if (BIAS) {
+        const int M = a.score.max_distance;
+        places = places_of_keys(a.q_pos ? a.q_pos[doc.row0 + row] : row + (doc.keys - doc.rows), M, lds_place(table + g * (2 * M + 1)));
+        bias_to_lds<E>(table, a.score, head * a.group, a.group, tid, kAttThreads);
+        __syncthreads();
+    }
+    f32x16 o[kOut];
+#pragma unroll
+    for (int i = 0; i < kOut; i++) o[i] = zero16();
+    float m = kLowest, l = 0.f;
+    char *vt = lds + wave * kTile;
+    const unsigned my_columns = columns_place<DP>(lane) + lds_place(vt);
+
+    for (int t = wave; t < tiles_n; t += 4) {
+        f32x16 s = zero16();
+#pragma unroll
+        for (int kk = 0; kk < kSteps; kk++) s = mfma(as8<E>(k[kk]), q[kk], s);
+#pragma unroll
+        for (int i = 0; i < kSteps; i++) {
+            const int at = i * 64 + lane, r = at / kRow, c = at % kRow;
+            *(u32x4 *)(vt + r * (DP * 2) + ((c ^ spread<DP>(r)) << 4)) = v[i];
+        }
+        if (BIAS && lane < kFewKeys) kpos[wave][lane] = kp;
+        wave_sync();
+        if (t + 4 < tiles_n) fetch(t + 4);
+        const bool edge = (t + 1) * kFewKeys > least;
+        float top = kLowest;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const u32x4 p4 = BIAS ? *(const u32x4 *)(kpos[wave] + 8 * j + 4 * half) : u32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const int r = 4 * j + e;
+                float y;
+                if (CAP) y = __builtin_fmaf(-2.f * a.score.c, rcp_fast(exp2_fast(s[r] * a.score.k) + 1.f), a.score.c);
+                else y = s[r] * a.score.k;
+                if (BIAS) y += float_at(place_of_key(places, (int)p4[e]));
+                if (edge) y = t * kFewKeys + 8 * j + 4 * half + e < seen ? y : -INFINITY;
+                s[r] = y;
+                top = fmaxf(top, y);
+            }
+        }
+        top = halves_max(top);
+        if (wave_any(top > m)) {
+            const float up = fmaxf(m, top), shrink = exp2_fast(m - up);
+            m = up;
+            l *= shrink;
+#pragma unroll
+            for (int i = 0; i < kOut; i++) o[i] *= shrink;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+            s[r] = exp2_fast(s[r] - m);
+            l += s[r];
+        }
+        typename Vec8<E>::type p0 = rounded8<E, 0>(s), p1 = rounded8<E, 1>(s);
+#pragma unroll
+        for (int i = 0; i < kOut; i++) {
+            o[i] = mfma(columns_chunk<E, DP>(my_columns, 0, i), p0, o[i]);
+            o[i] = mfma(columns_chunk<E, DP>(my_columns, 16, i), p1, o[i]);
+        }
+        wave_sync();
+    }
+    const Joined all = join_wavefronts<DP>(o, m, l, lds, wave_m, wave_l, wave, lane);
+    if (wave != 0 || !mine) return;
+    const long long place = (doc.row0 + row) * a.heads + h;
+    const float inv = all.sum > 0.f || all.sum != all.sum ? 1.f / all.sum : 0.f;
+    write_row<E, DP>(o, inv, (E *)a.out + place * a.dim, a.dim, half);
+    if (half == 0) a.lse[place] = all.sum == 0.f ? -INFINITY : (all.top + __log2f(all.sum)) * kLn2;
 }
 
 const char *bad_heads(int dtype, int heads, int kv_heads, int dim) {
@@ -329,6 +446,7 @@ logoskg_status attend_args(const logoskg_attention *a, AttArgs *o, const char *c
     o->score = score_args(a->score);
     o->out = a->out; o->lse = a->lse;
     o->row_blocks = (a->num_rows * o->group >> kAttRowsShift) + a->num_docs;
+    o->few_blocks = (a->num_rows * o->group >> kFewShift) + a->num_docs;
     o->key_blocks = (a->num_keys >> kAttRowsShift) + a->num_docs;
     o->scale = a->score.scale;
     o->curve = o->score.c > 0 ? -a->score.scale / (o->score.c * o->score.c) : 0.f;
@@ -337,8 +455,23 @@ logoskg_status attend_args(const logoskg_attention *a, AttArgs *o, const char *c
     return LOGOSKG_OK;
 }
 
+// Blocks of 128 rows x key heads up to which rows are few (k_attend / k_attend_few, us, with cap and bias and without):
+//   heads of 128   16 blocks: 33 rows before 300 entities 24.4 / 12.8 and 14.3 / 10.5, before 5,000 198 / 74 and 94 / 59
+//                  128: 500 rows before 300 entities 34 / 26 and 23.6 / 23.2, before 2,000 92 / 63 and 54 / 58
+//                  168: 16 documents of 24 rows before 1,000 48 / 31 and 26.0 / 28.7; 256: 1,000 rows before 2,000 98 / 119, 70 / 107
+//   heads of 64    192: 3,000 rows before 300 entities 74 / 61 and 49 / 42; 432: 32 documents of 200 rows 31 / 25 and 17.2 / 18.4
+constexpr long long few_blocks_most(int DP) { return DP == 64 ? 256 : 128; }
+
 template <class E, int DP, bool CAP, bool BIAS> static logoskg_status launch_attend(const AttArgs &a, hipStream_t st) {
-    size_t bytes = 4 * kKeys * DP * 2 + 4 * kKeys * 4 + (BIAS ? (size_t)a.group * (2 * a.score.max_distance + 1) * 4 : 0);
+    const size_t table = BIAS ? (size_t)a.group * (2 * a.score.max_distance + 1) * 4 : 0;
+    if (a.row_blocks * a.kv_heads <= few_blocks_most(DP)) {
+        const size_t few = 4 * kFewKeys * DP * 2 + table;
+        LKG_TRY(allow_lds(k_attend_few<E, DP, CAP, BIAS>, few));
+        k_attend_few<E, DP, CAP, BIAS><<<dim3((unsigned)(a.few_blocks * a.kv_heads)), kAttThreads, few, st>>>(a);
+        LKG_HIP(hipGetLastError());
+        return LOGOSKG_OK;
+    }
+    size_t bytes = 4 * kKeys * DP * 2 + 4 * kKeys * 4 + table;
     LKG_TRY(allow_lds(k_attend<E, DP, CAP, BIAS>, bytes));
     k_attend<E, DP, CAP, BIAS><<<dim3((unsigned)(a.row_blocks * a.kv_heads)), kAttThreads, bytes, st>>>(a);
     LKG_HIP(hipGetLastError());

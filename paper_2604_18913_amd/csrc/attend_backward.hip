@@ -161,7 +161,7 @@ __global__ __launch_bounds__(kAttThreads, DP == 64 ? 2 : 1) void k_att_dq(AttArg
     int q_low = 0, q_high = 0;
     Places places = {0, 0, 0};
     if (BIAS) {
-        const int q_pos = a.q_pos ? a.q_pos[doc.row0 + row] : row + doc.keys - doc.rows;
+        const int q_pos = a.q_pos ? a.q_pos[doc.row0 + row] : row + (doc.keys - doc.rows);
         places = places_of_keys(q_pos, M, lds_place(my_table));
         q_low = __builtin_amdgcn_readfirstlane(wave_min(q_pos));
         q_high = __builtin_amdgcn_readfirstlane(wave_max(q_pos));
@@ -327,18 +327,7 @@ __global__ __launch_bounds__(kAttThreads, DP == 64 ? 2 : 1) void k_att_dq(AttArg
     lacks = halves_sum(lacks);
     if (!mine) return;
     if (half == 0) a.delta[place] = delta + lacks;
-    E *out = (E *)a.dq + place * a.dim;
-#pragma unroll
-    for (int i = 0; i < kOut; i++)
-#pragma unroll
-        for (int r = 0; r < 4; r++) {
-            int c = 32 * i + 8 * r + 4 * half;
-            if (c >= a.dim) continue;
-            typename Vec4<E>::type y;
-#pragma unroll
-            for (int e = 0; e < 4; e++) y[e] = (E)dq[i][4 * r + e];
-            *(typename Vec4<E>::type *)(out + c) = y;
-        }
+    write_row<E, DP>(dq, 1.f, (E *)a.dq + place * a.dim, a.dim, half);
 }
 
 // ---------------------------------------------------------------- dK, dV, biases
@@ -457,7 +446,7 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
             my_delta = in ? a.delta[at] : 0.f;
             if (BIAS) {
                 const int near = in ? row : doc.rows - 1;
-                my_pos = a.q_pos ? a.q_pos[doc.row0 + near] : near + doc.keys - doc.rows;
+                my_pos = a.q_pos ? a.q_pos[doc.row0 + near] : near + (doc.keys - doc.rows);
             }
         }
         if (++fetch_at == per) fetch_at = 0, fetch_g++;

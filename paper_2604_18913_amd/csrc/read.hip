@@ -157,59 +157,15 @@ __global__ __launch_bounds__(256, 2) void k_read(ReadArgs a) {
         }
         wave_sync();
     }
-    // join: the wavefronts' sums at the largest of their maxima
-    l = halves_sum(l);
-    if (half == 0) wave_m[wave][lane] = m, wave_l[wave][lane] = l;
-    __syncthreads();
-    const int r31 = lane & 31;
-    const float top = fmaxf(fmaxf(wave_m[0][r31], wave_m[1][r31]), fmaxf(wave_m[2][r31], wave_m[3][r31]));
-    float sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; w++) sum += wave_l[w][r31] * exp2_fast(wave_m[w][r31] - top);
-    const float shrink = exp2_fast(m - top);
-#pragma unroll
-    for (int i = 0; i < kOut; i++) o[i] *= shrink;
-    typedef float f32x4 __attribute__((ext_vector_type(4)));
-    f32x4 *box = (f32x4 *)lds;  // [wavefront][DP / 4][32 rows] (the tiles are read)
-#pragma unroll
-    for (int round = 2; round > 0; round >>= 1) {
-        if (wave >= round && wave < 2 * round) {
-#pragma unroll
-            for (int i = 0; i < kOut; i++)
-#pragma unroll
-                for (int r = 0; r < 4; r++)
-                    box[((wave - round) * (DP / 4) + 8 * i + 2 * r + half) * 32 + r31] = f32x4{o[i][4 * r], o[i][4 * r + 1], o[i][4 * r + 2], o[i][4 * r + 3]};
-        }
-        __syncthreads();
-        if (wave < round) {
-#pragma unroll
-            for (int i = 0; i < kOut; i++)
-#pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    f32x4 x = box[(wave * (DP / 4) + 8 * i + 2 * r + half) * 32 + r31];
-#pragma unroll
-                    for (int e = 0; e < 4; e++) o[i][4 * r + e] += x[e];
-                }
-        }
-        __syncthreads();
-    }
+    const Joined all = join_wavefronts<DP>(o, m, l, lds, wave_m, wave_l, wave, lane);
+    const float top = all.top, sum = all.sum;
     if (wave != 0 || !mine) return;
     if (alone) {
         const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-        E *out = (E *)a.out + place * a.dim;
-#pragma unroll
-        for (int i = 0; i < kOut; i++)
-#pragma unroll
-            for (int r = 0; r < 4; r++) {
-                int c = 32 * i + 8 * r + 4 * half;
-                if (c >= a.dim) continue;
-                typename Vec4<E>::type x;
-#pragma unroll
-                for (int e = 0; e < 4; e++) x[e] = (E)(o[i][4 * r + e] * inv);
-                *(typename Vec4<E>::type *)(out + c) = x;
-            }
+        write_row<E, DP>(o, inv, (E *)a.out + place * a.dim, a.dim, half);
         if (half == 0) a.lse[place] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * kLn2;
     } else {
+        typedef float f32x4 __attribute__((ext_vector_type(4)));
         const long long at = (block * a.tokens + token) * a.heads + head * a.group + g;
 #pragma unroll
         for (int i = 0; i < kOut; i++)

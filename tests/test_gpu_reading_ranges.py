@@ -6,7 +6,8 @@ import pytest
 import torch
 
 import paper_2604_18913_amd as lkg
-from test_gpu_reading import HALVES, _check, _check_logits, _check_read, _gpu, _inputs, _logit_case, _read
+import reading_oracle as oracle
+from test_gpu_reading import HALVES, LENGTHS, _attend, _check, _check_logits, _check_read, _gpu, _inputs, _logit_case, _read
 
 pytestmark = pytest.mark.gpu
 
@@ -162,3 +163,82 @@ def test_logits_of_offsets_that_point_outside():
     want = lkg.constrain_logits(**{**a, "history_off": torch.tensor([0, n, n]).cuda(), "bias_off": torch.tensor([0, 0, m]).cuda()})
     got = lkg.constrain_logits(**{**a, "history_off": torch.tensor([-9, 1 << 40, n]).cuda(), "bias_off": torch.tensor([-(1 << 50), 0, 1 << 33]).cuda()})
     assert torch.equal(got, want)
+
+
+# ------------------------------------------------------------------------- attention on either side of the rule for few rows
+@pytest.mark.parametrize("dtype", HALVES, ids=["bf16", "fp16"])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("heads, kv_heads, dim", [(32, 8, 128), (8, 8, 64), (24, 3, 96)])
+def test_few_rows_and_many(heads, kv_heads, dim, bias, dtype):
+    # 1,100 rows fill more blocks than the rule for few rows allows, their first 37 do not; both see the same keys, and rows
+    # between 32 and 64 keys of both masks' ends
+    a, _ = _inputs(21, dtype, [1100], [1130], heads, kv_heads, dim, bias=bias)
+    if heads == 8:
+        a["q"], a["q_off"] = a["q"].repeat(8, 1, 1)[:4500], torch.tensor([0, 4500])
+        a["k"], a["v"], a["k_off"] = a["k"].repeat(5, 1, 1)[:4530], a["v"].repeat(5, 1, 1)[:4530], torch.tensor([0, 4530])
+    n, m = a["q"].shape[0], a["k"].shape[0]
+    kw = dict(causal=True, cap=5.0, prefix=torch.tensor([45], dtype=torch.int32).cuda(), **({"bias": a["bias"].cuda(), "buckets": a["buckets"].cuda()} if bias else {}))
+    q, k, v = (a[x].cuda() for x in "qkv")
+    many, many_lse = lkg.attend(q, k, v, a["q_off"].cuda(), a["k_off"].cuda(), **kw)
+    few, few_lse = lkg.attend(q[:37], k[:67], v[:67], torch.tensor([0, 37]).cuda(), torch.tensor([0, 67]).cuda(), **kw)
+    # the same rows of the same keys: each within the oracle's bound of the same value
+    small = {**a, "q": a["q"][:37], "k": a["k"][:67], "v": a["v"][:67], "q_off": torch.tensor([0, 37]), "k_off": torch.tensor([0, 67]),
+             "causal": True, "cap": 5.0, "prefix": torch.tensor([45], dtype=torch.int32)}
+    assert m - n == 30
+    res, tol = oracle.attention(**small)
+    for got, lse in ((few, few_lse), (many[:37], many_lse[:37])):
+        oracle.check(got, res["out"], tol["out"], "out")
+        oracle.check(lse, res["lse"], tol["lse"], "lse")
+
+
+@pytest.mark.parametrize("lengths", [([1], [1]), ([31, 1, 0, 33], [31, 33, 5, 0]), ([40], [2000]), ([3] * 9, [1, 0, 129, 128, 127, 32, 33, 5, 400])])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dim", [40, 128])
+def test_few_rows(dim, causal, lengths):
+    a, dout = _inputs(22, torch.float16, *lengths, 4, 1, dim, bias=True, far=30)
+    if causal:
+        a["prefix"] = torch.tensor([(5 * i + 1) % 40 for i in range(len(lengths[0]))], dtype=torch.int32)
+    _check({**a, "causal": causal}, dout)
+
+
+# heads so many that a document of one row is over the rule's limit: the form for many rows at lengths where it can go wrong
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("lengths", [n for n in LENGTHS if n != "many"])
+def test_lengths_under_many_heads(lengths, causal):
+    rows, keys = LENGTHS[lengths]
+    a, dout = _inputs(len(rows), torch.bfloat16, rows, keys, 264, 264, 16, bias=True)
+    if causal:
+        a["prefix"] = torch.tensor([(7 * i) % 50 for i in range(len(rows))], dtype=torch.int32)
+    _check({**a, "causal": causal, "cap": 4.0}, dout, lengths)
+
+
+@pytest.mark.parametrize("dtype", HALVES, ids=["bf16", "fp16"])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("cap", [0.0, 3.0, 50.0])
+@pytest.mark.parametrize("heads, kv_heads, dim", [(132, 132, 128), (264, 132, 96), (260, 260, 64), (520, 260, 40)])
+def test_many_heads_types_and_scores(heads, kv_heads, dim, cap, bias, dtype):
+    a, dout = _inputs(7, dtype, [37, 2, 90], [50, 140, 90], heads, kv_heads, dim, bias=bias)
+    got = lkg.attend(**{k: _gpu(x) for k, x in {**a, "causal": True, "cap": cap, "prefix": torch.tensor([30, 0, 11], dtype=torch.int32)}.items()})
+    res, tol = oracle.attention(**a, causal=True, cap=cap, prefix=torch.tensor([30, 0, 11], dtype=torch.int32))
+    for x, n in zip(got, ("out", "lse")):
+        oracle.check(x, res[n], tol[n], n)
+
+
+def test_many_heads_rows_that_see_nothing_far_positions_and_other_documents():
+    a, dout = _inputs(12, torch.bfloat16, [40, 8, 30], [10, 0, 70], 260, 260, 16, bias=True)
+    got = _check({**a, "causal": True}, dout)
+    assert (got["out"][:30] == 0).all() and (got["lse"][:30] == -math.inf).all() and (got["out"][40:48] == 0).all()
+    g = torch.Generator().manual_seed(1)
+    k_pos, q_pos = -1 - torch.randint(0, 4, (80,), generator=g, dtype=torch.int32), torch.arange(78, dtype=torch.int32)
+    k_pos[::3], q_pos[::2] = 2 ** 31 - 1, -2 ** 31
+    want = _check({**a, "q_pos": q_pos, "k_pos": k_pos}, dout)
+    a["q"][:40], a["k"][:10], a["v"][:10] = math.nan, math.inf, math.nan
+    got = _attend({**a, "q_pos": q_pos, "k_pos": k_pos}, dout)
+    assert all(torch.equal(got[n][40:], want[n][40:]) for n in ("out", "lse", "dq"))
+
+
+def test_many_heads_large_scores():
+    a, dout = _inputs(11, torch.bfloat16, [50], [200], 260, 260, 64, spread=6.0)
+    res, _ = oracle.attention(**a)
+    got = lkg.attend(**{k: _gpu(x) for k, x in a.items()})
+    assert torch.allclose(got[1].cpu().double(), res["lse"], rtol=2e-5)  # (as with few heads)
