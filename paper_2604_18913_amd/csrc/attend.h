@@ -27,7 +27,7 @@ struct AttArgs {
     // backward
     const void *dout;
     void *dq, *dk, *dv, *dbias;
-    float *delta;      // [num_rows][heads] sum of dout out, then of p dP
+    float *delta;      // [num_rows][heads] sum of p dP, from the first kernel to the second
     float *bias_part;  // [key_blocks][heads][num_buckets]
     float scale;
     float curve;       // .. of scale (1 - tanh^2) = scale + curve y^2, y = c tanh in units of log 2

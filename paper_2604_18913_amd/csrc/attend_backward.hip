@@ -6,8 +6,11 @@
 // keys (dQ), then one that keeps keys and passes over the rows that see them (dK, dV, biases): seven products for five, and
 // in return no sum depends on the order in which blocks arrive, and none is kept in memory in between.
 //
-// O comes in 16 bits, and dO . O carries its rounding: the first kernel adds up a row's dy, which is what delta lacks, and
-// leaves delta with it to the second (a bucket's sum of many dy would show it most).
+// O comes in 16 bits, and dO . O carries its rounding: the first kernel, which begins with dO . O of its rows, adds up a row's
+// dy, which is what delta lacks, and leaves delta with it to the second (a bucket's sum of many dy would show it most).
+// p and dz are rounded to the 16 bits that the matrix instructions take, sums are held in 32: dQ, dK and dV carry two
+// roundings, this one of every term and their own, sqrt 2 of what rounding the exact gradient alone gives (bfloat16: 0.0025 for
+// 0.0017 of the norm).  In float16 a dz below 2^-14 loses bits and one below 2^-25 all: losses are scaled, as that type asks.
 //
 // Both kernels work as the forward does: products of the next and of the last tile between the elements of this one, and
 // tiles that ask for nothing special (all visible, one bias, scores in the range of the tanh's polynomial) are spared the
@@ -15,23 +18,6 @@
 #include "attend.h"
 
 namespace lkg {
-
-// delta[row][head]: 16 lanes per (row, head), 8 values each
-template <class E> __global__ __launch_bounds__(256) void k_att_delta(AttArgs a) {
-    const long long at = ((long long)blockIdx.x * 256 + threadIdx.x) >> 4;
-    const int c = (threadIdx.x & 15) * 8;
-    float sum = 0.f;
-    const bool in = at < a.num_rows * a.heads;
-    if (in && c < a.dim) {
-        typename Vec8<E>::type x = as8<E>(*(const u32x4 *)((const E *)a.out + at * a.dim + c));
-        typename Vec8<E>::type y = as8<E>(*(const u32x4 *)((const E *)a.dout + at * a.dim + c));
-#pragma unroll
-        for (int i = 0; i < 8; i++) sum = __builtin_fmaf((float)x[i], (float)y[i], sum);
-    }
-#pragma unroll
-    for (int s = 8; s > 0; s >>= 1) sum += __shfl_xor(sum, s);
-    if (in && c == 0) a.delta[at] = sum;
-}
 
 // What an element's steps take, from its products z and dP: w = z times the polynomial (or z near0), p = 2^(w + fma(lse, lse_share,
 // b)), dy = p (dP - delta_share delta), dz = dy (curve w^2 + slope).  Special tiles come with w + shift in z and with
@@ -154,9 +140,16 @@ __global__ __launch_bounds__(kAttThreads, DP == 64 ? 2 : 1) void k_att_dq(AttArg
         q[kk] = row_chunk<E>(qrow, mine, kk, a.dim, lane);
         o[kk] = row_chunk<E>(orow, mine, kk, a.dim, lane);
     }
+    float delta = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < kSteps; kk++) {
+        const Chunk x = row_chunk<E>((const E *)a.out + place * a.dim, mine, kk, a.dim, lane);
+#pragma unroll
+        for (int i = 0; i < 8; i++) delta = __builtin_fmaf((float)x[i], (float)o[kk][i], delta);
+    }
+    delta = halves_sum(delta);
     float lse = mine ? a.lse[place] : -INFINITY;
     lse = lse == -INFINITY ? kHiddenLse : lse * kLog2e;
-    const float delta = mine ? a.delta[place] : 0.f;
     const float *my_table = table + g * (2 * M + 1);
     int q_low = 0, q_high = 0;
     Places places = {0, 0, 0};
@@ -726,11 +719,6 @@ template <class E, int DP, bool CAP, bool BIAS> static logoskg_status launch_bac
 }
 
 template <class E> static logoskg_status backward(const AttArgs &a, hipStream_t st) {
-    if (a.num_rows) {
-        long long n = a.num_rows * a.heads;
-        k_att_delta<E><<<dim3((unsigned)((n + 15) / 16)), 256, 0, st>>>(a);
-        LKG_HIP(hipGetLastError());
-    }
     const bool cap = a.score.c > 0, bias = a.score.bias != nullptr, wide = a.dim > 64;
     if (wide) LKG_TRY((cap ? bias ? launch_backward<E, 128, true, true>(a, st) : launch_backward<E, 128, true, false>(a, st)
                            : bias ? launch_backward<E, 128, false, true>(a, st) : launch_backward<E, 128, false, false>(a, st)));
@@ -769,7 +757,7 @@ extern "C" logoskg_status logoskg_attend_backward(const logoskg_attention *in, c
     a.dout = g->dout; a.dq = g->dq; a.dk = g->dk; a.dv = g->dv; a.dbias = g->dbias;
     a.delta = (float *)g->workspace;
     a.bias_part = (float *)((char *)g->workspace + delta_bytes(a));
-    if (a.key_blocks * a.kv_heads >= (1ll << 31) || (a.num_rows * a.heads + 15) / 16 >= (1ll << 31)) { set_error("logoskg_attend_backward: too many rows"); return LOGOSKG_EINVAL; }
+    if (a.key_blocks * a.kv_heads >= (1ll << 31)) { set_error("logoskg_attend_backward: too many rows"); return LOGOSKG_EINVAL; }
     if (a.num_keys == 0) a.key_blocks = 0;
     LKG_HIP(hipSetDevice(in->device));
     return in->dtype == LOGOSKG_BF16 ? backward<bf16>(a, (hipStream_t)in->stream) : backward<fp16>(a, (hipStream_t)in->stream);
