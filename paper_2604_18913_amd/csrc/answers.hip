@@ -108,16 +108,18 @@ struct LogitArgs {
 
 constexpr int kBiasHits = 512;  // of a piece: listed in LDS
 
-// One block: a piece of 16 ids per thread of a row.  The row's history is counted in LDS for the ids of the piece, in 16 bits
-// (32 where the history is so long that a count might not fit, for half of the ids at a time); its biases that fall
-// into the piece are marked, and listed with their places in the row's list, of which the last counts.  Whole numbers only
-// are added up by atomics.  The logits pass once through registers, in 16-byte chunks from the first whole one of the row on,
-// where logits and out lie alike; else one by one.
+// One block: a piece of 16 ids per thread of a row.  The logits pass once through registers under the mask, in 16-byte chunks
+// from the first whole one of the row on, where logits and out lie alike; else one by one.  What the lists ask for is few
+// ids, and comes behind: the row's history is counted in LDS for the ids of the piece, in 16 bits (32 where the history is so long
+// that a count might not fit, for half of the ids at a time); its biases that fall into the piece are marked, and listed with
+// their places in the row's list, of which the last counts; then every thread looks through 16 neighbouring ids and writes
+// those again that a list holds and the mask allows.  (A chunk that looks after its own ids has some instructions for each of
+// its eight as soon as one lane of the wavefront has one.)  Whole numbers only are added up by atomics.
 template <class T, int THREADS> __global__ __launch_bounds__(THREADS) void k_logits(LogitArgs a) {
     constexpr int kPiece = 16 * THREADS, kChunk = 16 / sizeof(T), kChunks = 16 / kChunk;  // ids of a chunk; chunks of a thread
     typedef T chunk __attribute__((ext_vector_type(kChunk)));
-    __shared__ __attribute__((aligned(16))) unsigned count[kPiece / 2 + kChunk];
-    __shared__ unsigned marked[kPiece / 32 + 1];
+    __shared__ __attribute__((aligned(16))) unsigned count[kPiece / 2];
+    __shared__ unsigned marked[kPiece / 32];
     __shared__ int hit_id[kBiasHits], hit_at[kBiasHits], hits;
     __shared__ float hit_value[kBiasHits];
     const int tid = threadIdx.x;
@@ -131,6 +133,7 @@ template <class T, int THREADS> __global__ __launch_bounds__(THREADS) void k_log
     const long long lo = piece == 0 ? 0 : v0, hi = v0 + kPiece < a.vocab ? v0 + kPiece : a.vocab;
     if (lo >= hi) return;
     const u64 *mask = a.mask ? a.mask + b * a.words : nullptr;
+    auto allowed = [&](long long v) { return !mask || (mask[v >> 6] >> (v & 63) & 1); };
     chunk x[kChunks];
     u64 word[kChunks], behind[kChunks];  // of the mask: that of a chunk's first id, and the next where the chunk goes on into it
     if (alike) {
@@ -168,94 +171,106 @@ template <class T, int THREADS> __global__ __launch_bounds__(THREADS) void k_log
         }
         return 0.f;
     };
-    auto one = [&](float y, long long v, unsigned c, bool allowed) {  // id v, said c times
-        y = penalised(y, c);
-        const int at = (int)(v - v0);
-        if (biased && (marked[at >> 5] >> (at & 31) & 1)) y += bias_of(v);
-        return allowed ? y : -INFINITY;
+    auto from_of = [&](int round) { return round == 0 ? lo : lo > v0 + kPiece / 2 ? lo : v0 + kPiece / 2; };  // ids of a round
+    auto to_of = [&](int round) { return wide && round == 0 && v0 + kPiece / 2 < hi ? v0 + kPiece / 2 : hi; };
+    auto clear = [&] {
+        for (int i = tid; i < (int)(sizeof(count) / 16); i += THREADS) ((u32x4 *)count)[i] = u32x4{0, 0, 0, 0};
     };
-    auto allowed = [&](long long v) { return !mask || (mask[v >> 6] >> (v & 63) & 1); };
-    const int rounds = wide ? 2 : 1;
-    for (int round = 0; round < rounds; round++) {  // of a wide history: half of the ids each
-        const long long w0 = v0 + round * (kPiece / 2), from = lo > w0 ? lo : w0, to = wide && round == 0 && w0 + kPiece / 2 < hi ? w0 + kPiece / 2 : hi;
-        if (said || biased) {
-            if (round > 0) __syncthreads();
-            else {
-                for (int i = tid; i < kPiece / 32 + 1; i += THREADS) marked[i] = 0;
-                if (tid == 0) hits = 0;
+    auto count_history = [&](int round) {
+        const long long w0 = v0 + round * (kPiece / 2), from = from_of(round), to = to_of(round);
+        const unsigned base = (unsigned)w0, skip = (unsigned)(from - w0), size = to > from ? (unsigned)(to - from) : 0;
+        for_entries<THREADS>(a.history, h0, h1, tid, [&](int id) {
+            const unsigned at = (unsigned)id - base;
+            if (at - skip >= size) return;
+            if (wide) atomicAdd(&count[at], 1u);
+            else atomicAdd(&count[at >> 1], at & 1 ? 65536u : 1u);
+        });
+    };
+    const bool listed = said || biased;
+    u64 allow[2] = {~0ull, ~0ull};  // of the ids that this thread looks through in a round
+    auto look_up = [&](int round) {
+        const long long v = v0 + (wide ? 8 * tid + round * (kPiece / 2) : 16 * tid);
+        for (int i = 0; i < 2; i++) {
+            const long long w = (v >> 6) + i;
+            if (mask) allow[i] = w >= 0 && w < a.words ? mask[w] : 0;
+        }
+    };
+    // (the logits themselves are written: in place, an allowed one still stands as it came)
+    auto write_again = [&](int round) {
+        const int mine = wide ? 8 : 16, at0 = mine * tid, all0 = at0 + round * (kPiece / 2);
+        const long long first = v0 + all0;
+        const int sh = (int)(first & 63);
+        unsigned again = biased ? marked[all0 >> 5] >> (all0 & 31) : 0;
+        if (said) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const unsigned c = count[8 * tid + i];
+                again |= wide ? (unsigned)(c != 0) << i : (unsigned)((c & 65535u) != 0) << 2 * i | (unsigned)(c >> 16 != 0) << (2 * i + 1);
             }
-            for (int i = tid; i < (int)(sizeof(count) / 16); i += THREADS) ((u32x4 *)count)[i] = u32x4{0, 0, 0, 0};
-            __syncthreads();
-            const int base = (int)w0;
-            const unsigned skip = (unsigned)(from - w0), size = to > from ? (unsigned)(to - from) : 0;
-            if (round == 0)
-                for (long long i = s0 + tid; i < s1; i += THREADS) {
-                    const long long id = a.bias_id[i];
-                    if (id >= lo && id < hi) {
-                        atomicOr(&marked[(int)(id - v0) >> 5], 1u << ((id - v0) & 31));
-                        const int n = atomicAdd(&hits, 1);
-                        if (n < kBiasHits) hit_id[n] = (int)(id - v0), hit_at[n] = (int)(i - s0), hit_value[n] = a.bias_value[i];
-                    }
-                }
-            for_entries<THREADS>(a.history, h0, h1, tid, [&](int id) {
-                const unsigned at = (unsigned)id - (unsigned)base;
-                if (at - skip >= size) return;
-                if (wide) atomicAdd(&count[at], 1u);
-                else atomicAdd(&count[at >> 1], at & 1 ? 65536u : 1u);
-            });
-            __syncthreads();
         }
-        auto count_of = [&](long long v) {
-            const int at = (int)(v - w0);
-            return !said ? 0u : wide ? count[at] : count[at >> 1] >> (16 * (at & 1)) & 65535u;
-        };
-        if (!alike) {
-            for (long long v = from + tid; v < to; v += THREADS) out[v] = (T)one((float)in[v], v, count_of(v), allowed(v));
-            continue;
+        again &= (unsigned)(allow[0] >> sh | allow[1] << 1 << (63 - sh)) & ((1u << mine) - 1);
+        if (!again) return;
+        float next = (float)in[first + __ffs(again) - 1];
+        while (again) {
+            const int e = __ffs(again) - 1, at = at0 + e;
+            float y = next;
+            again &= again - 1;
+            if (again) next = (float)in[first + __ffs(again) - 1];
+            y = penalised(y, !said ? 0u : wide ? count[at] : count[at >> 1] >> (16 * (at & 1)) & 65535u);
+            if (biased && (marked[(all0 + e) >> 5] >> ((all0 + e) & 31) & 1)) y += bias_of(first + e);
+            out[first + e] = (T)y;
         }
+    };
+    if (listed) {
+        for (int i = tid; i < kPiece / 32; i += THREADS) marked[i] = 0;
+        if (tid == 0) hits = 0;
+        clear();
+        __syncthreads();
+        for (long long i = s0 + tid; i < s1; i += THREADS) {
+            const long long id = a.bias_id[i];
+            if (id >= lo && id < hi) {
+                atomicOr(&marked[(int)(id - v0) >> 5], 1u << ((id - v0) & 31));
+                const int n = atomicAdd(&hits, 1);
+                if (n < kBiasHits) hit_id[n] = (int)(id - v0), hit_at[n] = (int)(i - s0), hit_value[n] = a.bias_value[i];
+            }
+        }
+        count_history(0);
+        look_up(0);
+    }
+    if (alike) {
 #pragma unroll
         for (int i = 0; i < kChunks; i++) {
-            if (wide && i / (kChunks / 2) != round) continue;
             const long long v = v0 + (long long)(i * THREADS + tid) * kChunk;
             if (v >= lo && v + kChunk <= hi) {
-                const int at = (int)(v - v0);
                 const int sh = (int)(v & 63);
                 const unsigned bits = (unsigned)(word[i] >> sh | behind[i] << 1 << (63 - sh));
-                unsigned marks = 0, counts[kChunk / 2] = {};
-                if (said && !wide) {
-#pragma unroll
-                    for (int e = 0; e < kChunk / 2; e++) counts[e] = count[(at >> 1) + e];
-                }
-                if (biased) marks = marked[at >> 5] >> (at & 31);
-                marks &= (1u << kChunk) - 1;
-                unsigned any = marks;
-#pragma unroll
-                for (int e = 0; e < kChunk / 2; e++) any |= counts[e];
-                if (any || wide) {
-                    float y[kChunk];
-#pragma unroll
-                    for (int e = 0; e < kChunk; e++) y[e] = penalised((float)x[i][e], wide ? count_of(v + e) : counts[e / 2] >> (16 * (e & 1)) & 65535u);
-                    if (marks) {
-#pragma unroll
-                        for (int e = 0; e < kChunk; e++)
-                            if (marks >> e & 1) y[e] += bias_of(v + e);
-                    }
-#pragma unroll
-                    for (int e = 0; e < kChunk; e++) x[i][e] = (T)y[e];
-                }
 #pragma unroll
                 for (int e = 0; e < kChunk; e++) x[i][e] = bits >> e & 1 ? x[i][e] : (T)-INFINITY;
                 *(chunk *)(out + v) = x[i];
             } else {
-                for (long long w = v < lo ? lo : v; w < v + kChunk && w < hi; w++) out[w] = (T)one((float)in[w], w, count_of(w), allowed(w));
+                for (long long w = v < lo ? lo : v; w < v + kChunk && w < hi; w++) out[w] = allowed(w) ? in[w] : (T)-INFINITY;
             }
         }
+    } else {
+        for (long long v = lo + tid; v < hi; v += THREADS) out[v] = allowed(v) ? in[v] : (T)-INFINITY;
     }
+    if (!listed) return;
+    __syncthreads();
+    write_again(0);
+    if (!wide) return;
+    __syncthreads();
+    clear();
+    __syncthreads();
+    count_history(1);
+    look_up(1);
+    __syncthreads();
+    write_again(1);
 }
 
 template <class T> static logoskg_status launch_logits(LogitArgs a, hipStream_t st) {
-    // Pieces of 4,096 ids: 256 rows of 150,001 logits take 77 us without / 34 us without lists, with pieces of 16,384 153 / 49 us.
-    // (Only where histories are longer than pieces do larger ones pay, by an eighth at 4,700 entries a row.)
+    // Pieces of 4,096 ids, 256 threads: 256 rows of 150,001 bfloat16 logits with histories of up to 4,000 ids and 300 biases take 44 us
+    // (3.6 TB/s; a copy of the logits and masks 33), with next to no lists 29; pieces of 2,048 take 49 and 29, of 8,192
+    // 48 and 29, of 16,384 73 and 45 us.  (256 rows of 32,000 float32 logits with 8,000 ids each: 26, 28, 24, 22 us.)
     a.pieces = (a.vocab + 4096 + 15) / 4096;
     if (a.pieces * a.num_rows >= (1ll << 31)) { set_error("logoskg_constrain_logits: too many rows"); return LOGOSKG_EINVAL; }
     k_logits<T, 256><<<dim3((unsigned)(a.pieces * a.num_rows)), 256, 0, st>>>(a);
