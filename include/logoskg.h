@@ -481,7 +481,8 @@ typedef enum { LOGOSKG_F32 = 0, LOGOSKG_BF16 = 1, LOGOSKG_F16 = 2 } logoskg_dtyp
 
 #define LOGOSKG_MAX_BUCKETS 64      /* buckets of a learned distance bias                    */
 #define LOGOSKG_MAX_DISTANCE 1024   /* largest distance that has a bucket of its own         */
-#define LOGOSKG_BIAS_PLACES 4480    /* heads / kv_heads * (2 max_distance + 1) at most       */
+#define LOGOSKG_BIAS_PLACES 4480    /* heads / kv_heads * (2 max_distance + 1) at most: what
+                                       the gradients' tables and sums leave room for in LDS  */
 
 /*
  * How scores are made of products, for every call below: with z = scale q.k,
@@ -523,7 +524,9 @@ typedef struct {
  * Attention of a ragged batch.  Row i of a document with R rows and K keys sees
  * all K keys, or with `causal` the keys j < prefix and j <= i + K - R (the
  * retrieved entities in front, then the text up to the row itself).  A row that
- * sees nothing gets zeros and lse = -inf.
+ * sees nothing gets zeros and lse = -inf.  Other documents' values never matter;
+ * keys of its own document that a row does not see are weighted with 0, so that an
+ * infinity or NaN there may still reach it.
  */
 logoskg_status logoskg_attend(const logoskg_attention *a);
 
@@ -584,7 +587,7 @@ logoskg_status logoskg_read_entities(const logoskg_entity_read *r);
 /*
  * The lists as bit masks in the layout of logoskg_query_batch.rel_mask:
  * mask = device uint64[num_queries][ceil(num_ids / 64)], bit i % 64 of word
- * i / 64 set for every id of the query's list.  Ids outside [0, num_ids) are
+ * i / 64 set for every id of the query's list (mask is 16-byte aligned).  Ids outside [0, num_ids) are
  * left out; order and repeats do not matter.
  */
 logoskg_status logoskg_entity_mask(int32_t device, const int64_t *off, const int32_t *ids, int64_t num_entries,

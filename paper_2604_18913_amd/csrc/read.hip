@@ -25,6 +25,10 @@ constexpr int kReadLeastShift = 7;  // four wavefronts, a tile each
 // tile of 32 entries and join at the end.  The bytes of the entries are all that counts (a row of the matrix instructions
 // may well be empty): keys go from memory into the registers that the instruction reads, values through the wavefront's
 // own piece of LDS, where they are read by columns; no wavefront waits for another.
+//
+// Memory bounds it: 64 lists of up to 20,000 entities of a table of 407,000 (8 key heads of 128, float16) 597 us, 4.5 TB/s of the
+// rows read, a copy's rate 4.85; 1,024 lists of up to 3,000 of 3 M (8 of 64, four tokens) 812 us, 3.9 TB/s: a key head's piece
+// of a row is one line of 128 bytes.  One list of 900: 10 us and 4 for the join, both chains of loads.
 template <class E, int DP, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_read(ReadArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
