@@ -522,7 +522,7 @@ typedef struct {
 
 /*
  * Attention of a ragged batch.  Row i of a document with R rows and K keys sees
- * all K keys, or with `causal` the keys j < prefix and j <= i + K - R (the
+ * all K keys, or with `causal` the keys j < prefix and those j <= i + K - R (the
  * retrieved entities in front, then the text up to the row itself).  A row that
  * sees nothing gets zeros and lse = -inf.  Other documents' values never matter;
  * keys of its own document that a row does not see are weighted with 0, so that an
