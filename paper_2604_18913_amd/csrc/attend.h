@@ -34,6 +34,7 @@ struct AttArgs {
     float slope;       // with a cap: 4 scale, of scale (1 - tanh^2) = 4 scale r (1 - r), r = 1 / (2^(z k) + 1)
     long long row_blocks, key_blocks;
     long long few_blocks;  // of 32 rows
+    int *row_order, *key_order;  // blocks in the order of their work, or NULL
     int bias_columns;  // 64, or 32 where LDS has no room for them
 };
 

@@ -101,6 +101,70 @@ template <bool CAP> __device__ __forceinline__ void exact_score(const AttArgs &a
 constexpr float kHidden = -1e15f;      // 2^this is 0, and its square finite
 constexpr float kHiddenLse = 1e15f;    // of a row that sees nothing, or is none: p = 0 the same way
 
+// the first row that sees one of the keys from kb on
+__device__ __forceinline__ int first_row(const AttArgs &a, const AttDoc &doc, long long kb) {
+    if (!a.causal || kb < doc.prefix) return 0;
+    const long long i = kb - ((long long)doc.keys - doc.rows);
+    return i < 0 ? 0 : i > doc.rows ? doc.rows : (int)i;
+}
+
+// ---------------------------------------------------------------- order
+// Blocks by their work, most first, for k_att_dkdv (key blocks) and k_att_dq (row blocks): where there are more of them than
+// units, long ones that begin late leave the others idle.  One block each; a wavefront goes over a document's blocks, three
+// times: the largest, how many of each of 512 classes, and each into its class's places (in whichever order: what a block
+// computes does not depend on its turn).  Offsets that do not ascend may name a block twice or never, but none outside.
+__global__ __launch_bounds__(1024) void k_att_order(AttArgs a) {
+    constexpr int kBins = 512;
+    __shared__ unsigned bins[kBins];
+    __shared__ int largest;
+    const bool of_rows = blockIdx.x != 0;
+    const int64_t *off = of_rows ? a.q_off : a.k_off;
+    const long long total = of_rows ? a.num_rows : a.num_keys, n = of_rows ? a.row_blocks : a.key_blocks;
+    const int mult = of_rows ? a.group : 1, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int *order = of_rows ? a.row_order : a.key_order;
+    const float by_group = 1.f / a.group;  // (a row or two off is no matter here)
+    if (tid < kBins) bins[tid] = 0;
+    if (tid == 0) largest = 1;
+    for (long long i = tid; i < n; i += 1024) order[i] = (int)i;
+    __syncthreads();
+    auto each = [&](auto f) {
+        for (int d = wave; d < a.num_docs; d += 16) {
+            const AttDoc doc = att_doc(a, d);
+            const long long base = first_block(off, d, total, mult, kAttRowsShift), end = d + 1 == a.num_docs ? n : first_block(off, d + 1, total, mult, kAttRowsShift);
+            for (long long b = (d == 0 ? 0 : base) + lane; b < end && b < n; b += 64) {
+                const long long x = (b - base) << kAttRowsShift, rows = (long long)doc.rows * a.group;
+                int tiles = 0;
+                if (of_rows && x >= 0 && x < rows) tiles = (doc.seen((int)((float)(x + kAttRows < rows ? x + kAttRows - 1 : rows - 1) * by_group), a.causal) >> 6) + 1;
+                if (!of_rows && x >= 0 && x < doc.keys) tiles = ((doc.rows - first_row(a, doc, x)) >> 6) + 1;
+                f(b, tiles);
+            }
+        }
+        __syncthreads();
+    };
+    each([&](long long, int tiles) { atomicMax(&largest, tiles); });
+    const float by_most = (kBins - 1) / (float)largest;
+    auto bin_of = [&](int tiles) { return kBins - 1 - (int)((float)tiles * by_most); };
+    each([&](long long, int tiles) { atomicAdd(&bins[bin_of(tiles)], 1u); });
+    if (wave == 0) {  // how many lie before a class
+        unsigned mine[kBins / 64], sum = 0;
+#pragma unroll
+        for (int i = 0; i < kBins / 64; i++) mine[i] = sum, sum += bins[lane * (kBins / 64) + i];
+        unsigned before = sum;
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) {
+            const unsigned x = __shfl_up(before, s);
+            if (lane >= s) before += x;
+        }
+#pragma unroll
+        for (int i = 0; i < kBins / 64; i++) bins[lane * (kBins / 64) + i] = before - sum + mine[i];
+    }
+    __syncthreads();
+    each([&](long long b, int tiles) {
+        const unsigned at = atomicAdd(&bins[bin_of(tiles)], 1u);
+        if (at < n) order[at] = (int)b;
+    });
+}
+
 // ---------------------------------------------------------------- dQ
 // One block: 128 rows as in the forward, keys in tiles of 64: K through a ring of four buffers (read by rows for the next
 // tile's scores, by columns for the last tile's dQ), V through two.  Heads above 64 have registers for one wavefront a
@@ -118,7 +182,8 @@ __global__ __launch_bounds__(kAttThreads, DP == 64 ? 2 : 1) void k_att_dq(AttArg
     const int M = a.score.max_distance, G = a.group;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
     const int head = blockIdx.x % a.kv_heads;
-    const long long block = a.row_blocks - 1 - blockIdx.x / a.kv_heads;
+    const unsigned turn = blockIdx.x / a.kv_heads;  // (the last rows of a document see most)
+    const long long block = a.row_order ? a.row_order[turn] : a.row_blocks - 1 - turn;
     const int d = document_of(a.q_off, a.num_docs, a.num_rows, G, kAttRowsShift, block, lane);
     const AttDoc doc = att_doc(a, d);
     const long long first = (block - first_block(a.q_off, d, a.num_rows, G, kAttRowsShift)) << kAttRowsShift;
@@ -336,8 +401,7 @@ __global__ __launch_bounds__(kAttThreads, DP == 64 ? 2 : 1) void k_att_dq(AttArg
 //
 // dK, dV, K, V and the products fill both halves of the registers: one wavefront a unit, and what it waits for is its own
 // time.  The batch of k_att_dq: 1,130 us, 425 TFLOP/s of its four products; matrix units busy for 24 % of the time, vector units for
-// half, LDS for half.  Key blocks of the longest document come first, but 592 blocks of very different length leave units
-// idle at the end (a fifth of the time, by their lengths).
+// half, LDS for half.  It takes as long as the longest document's first key blocks, which see all 4,096 rows of four heads.
 template <class E, int DP, bool CAP, bool BIAS>
 __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -354,7 +418,8 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
     float *table = (float *)(column + (BIAS ? places_n : 0));  // [group][places_n]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
     const int head = blockIdx.x % a.kv_heads;
-    const long long block = blockIdx.x / a.kv_heads;  // the first keys of a document are seen by most rows: first
+    const unsigned turn = blockIdx.x / a.kv_heads;  // the first keys of a document are seen by most rows: first
+    const long long block = a.key_order ? a.key_order[turn] : turn;
     const int d = document_of(a.k_off, a.num_docs, a.num_keys, 1, kAttRowsShift, block, lane);
     const AttDoc doc = att_doc(a, d);
     const long long kb = (block - first_block(a.k_off, d, a.num_keys, 1, kAttRowsShift)) << kAttRowsShift;
@@ -415,11 +480,7 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
     float size = 0.f;
 
     const int kend = doc.keys < kb + kAttRows ? doc.keys : (int)kb + kAttRows;
-    int from = 0;  // first row that sees one of the keys
-    if (a.causal && kb >= doc.prefix) {
-        long long i = kb - ((long long)doc.keys - doc.rows);
-        from = i < 0 ? 0 : i > doc.rows ? doc.rows : (int)i;
-    }
+    const int from = first_row(a, doc, kb);
     const int per = (doc.rows - from + kGradTile - 1) / kGradTile, tiles_n = per * G;  // tiles of a head, of all
 
     TileLoad<kGradTile, DP> qload, oload;
@@ -698,9 +759,17 @@ template <class E> __global__ __launch_bounds__(1024) void k_att_dbias(AttArgs a
     ((E *)a.dbias)[h * nb + b] = (E)sum;
 }
 
+// Ordered where the blocks of either kernel are more than the units and the documents more than a few, whose blocks come
+// most first by themselves and share caches.  Forward and backward of documents of uneven lengths, us without / with (16 / 4 heads
+// of 128, up to 700 tokens and 1,500 entities): 4 documents (176 blocks) 390 / 391, 8 (456) 618 / 567, 16 (840) 861 / 733, 64
+// (3,276) 2,837 / 2,681; text and entities attending to each other, 2,000: 4 (564) 739 / 743, 8 (1,104) 866 / 882, 16 (2,236) 1,373 /
+// 1,210; up to 400: 16 (188 blocks) 147 / 147, 32 (348) 207 / 179.
+static bool ordered(const AttArgs &a) {
+    return a.num_docs >= 8 && a.num_rows && a.num_keys && (a.row_blocks > a.key_blocks ? a.row_blocks : a.key_blocks) * a.kv_heads > 256;
+}
 static int64_t delta_bytes(const AttArgs &a) { return (a.num_rows * a.heads * 4 + 15) / 16 * 16; }
 static int64_t backward_bytes(const AttArgs &a) {
-    return delta_bytes(a) + (a.score.bias ? a.key_blocks * a.heads * (int64_t)a.score.num_buckets * 4 : 0);
+    return delta_bytes(a) + (a.score.bias ? a.key_blocks * a.heads * (int64_t)a.score.num_buckets * 4 : 0) + (ordered(a) ? (a.row_blocks + a.key_blocks) * 4 : 0);
 }
 
 template <class E, int DP, bool CAP, bool BIAS> static logoskg_status launch_backward(const AttArgs &a, hipStream_t st) {
@@ -726,6 +795,10 @@ template <class E, int DP, bool CAP, bool BIAS> static logoskg_status launch_bac
 }
 
 template <class E> static logoskg_status backward(const AttArgs &a, hipStream_t st) {
+    if (a.key_order) {
+        k_att_order<<<dim3(2), 1024, 0, st>>>(a);
+        LKG_HIP(hipGetLastError());
+    }
     const bool cap = a.score.c > 0, bias = a.score.bias != nullptr, wide = a.dim > 64;
     if (wide) LKG_TRY((cap ? bias ? launch_backward<E, 128, true, true>(a, st) : launch_backward<E, 128, true, false>(a, st)
                            : bias ? launch_backward<E, 128, false, true>(a, st) : launch_backward<E, 128, false, false>(a, st)));
@@ -766,6 +839,7 @@ extern "C" logoskg_status logoskg_attend_backward(const logoskg_attention *in, c
     a.bias_part = (float *)((char *)g->workspace + delta_bytes(a));
     if (a.key_blocks * a.kv_heads >= (1ll << 31)) { set_error("logoskg_attend_backward: too many rows"); return LOGOSKG_EINVAL; }
     if (a.num_keys == 0) a.key_blocks = 0;
+    if (ordered(a)) a.key_order = (int *)(a.bias_part + (a.score.bias ? a.key_blocks * a.heads * (int64_t)a.score.num_buckets : 0)), a.row_order = a.key_order + a.key_blocks;
     LKG_HIP(hipSetDevice(in->device));
     return in->dtype == LOGOSKG_BF16 ? backward<bf16>(a, (hipStream_t)in->stream) : backward<fp16>(a, (hipStream_t)in->stream);
 }

@@ -242,3 +242,17 @@ def test_many_heads_large_scores():
     res, _ = oracle.attention(**a)
     got = lkg.attend(**{k: _gpu(x) for k, x in a.items()})
     assert torch.allclose(got[1].cpu().double(), res["lse"], rtol=2e-5)  # (as with few heads)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("docs", [7, 8, 40])
+def test_documents_of_very_different_lengths(docs, causal):
+    # blocks enough to be put in order from eight documents on; some documents have no rows, some no keys
+    rows = [(97 * i) % 260 if i % 5 else 0 for i in range(docs)]
+    keys = [(61 * i * i) % 390 if i % 7 else 0 for i in range(docs)]
+    a, dout = _inputs(23, torch.bfloat16, rows, keys, 64, 32, 16, bias=True)
+    if causal:
+        a["prefix"] = torch.tensor([(13 * i) % 90 for i in range(docs)], dtype=torch.int32)
+    got = _check({**a, "causal": causal}, dout)
+    again = _attend({**a, "causal": causal}, dout)
+    assert all(torch.equal(got[n], again[n]) for n in got)
