@@ -276,6 +276,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
     }
     l = halves_sum(l);
     if (!mine) return;
+    if (sees_nothing(m) && l == l) l = 0.f;
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;  // (a NaN stays one)
     const long long place = (doc.row0 + row) * a.heads + h;
     write_row<E, DP>(o, inv, (E *)a.out + place * a.dim, a.dim, half);
@@ -405,9 +406,9 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend_few(AttArgs a) {
     const Joined all = join_wavefronts<DP>(o, m, l, lds, wave_m, wave_l, wave, lane);
     if (wave != 0 || !mine) return;
     const long long place = (doc.row0 + row) * a.heads + h;
-    const float inv = all.sum > 0.f || all.sum != all.sum ? 1.f / all.sum : 0.f;
+    const float sum = sees_nothing(all.top) && all.sum == all.sum ? 0.f : all.sum, inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
     write_row<E, DP>(o, inv, (E *)a.out + place * a.dim, a.dim, half);
-    if (half == 0) a.lse[place] = all.sum == 0.f ? -INFINITY : (all.top + __log2f(all.sum)) * kLn2;
+    if (half == 0) a.lse[place] = sum == 0.f ? -INFINITY : (all.top + __log2f(sum)) * kLn2;
 }
 
 const char *bad_heads(int dtype, int heads, int kv_heads, int dim) {

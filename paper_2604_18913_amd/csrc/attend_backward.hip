@@ -98,7 +98,6 @@ template <bool CAP> __device__ __forceinline__ void exact_score(const AttArgs &a
         slope = a.scale;
     }
 }
-constexpr float kHidden = -1e15f;      // 2^this is 0, and its square finite
 constexpr float kHiddenLse = 1e15f;    // of a row that sees nothing, or is none: p = 0 the same way
 
 // the first row that sees one of the keys from kb on

@@ -162,9 +162,10 @@ __global__ __launch_bounds__(256, 2) void k_read(ReadArgs a) {
         wave_sync();
     }
     const Joined all = join_wavefronts<DP>(o, m, l, lds, wave_m, wave_l, wave, lane);
-    const float top = all.top, sum = all.sum;
+    const float top = all.top;
     if (wave != 0 || !mine) return;
     if (alone) {
+        const float sum = sees_nothing(top) && all.sum == all.sum ? 0.f : all.sum;
         const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
         write_row<E, DP>(o, inv, (E *)a.out + place * a.dim, a.dim, half);
         if (half == 0) a.lse[place] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * kLn2;
@@ -178,7 +179,7 @@ __global__ __launch_bounds__(256, 2) void k_read(ReadArgs a) {
                 int c = 32 * i + 8 * r + 4 * half;
                 if (c < a.dim) *(f32x4 *)(a.part_o + at * a.dim + c) = f32x4{o[i][4 * r], o[i][4 * r + 1], o[i][4 * r + 2], o[i][4 * r + 3]};
             }
-        if (half == 0) a.part_ml[2 * at] = top, a.part_ml[2 * at + 1] = sum;
+        if (half == 0) a.part_ml[2 * at] = top, a.part_ml[2 * at + 1] = all.sum;
     }
 }
 
@@ -213,6 +214,7 @@ template <class E> __global__ __launch_bounds__(256) void k_read_join(ReadArgs a
 #pragma unroll
     for (int e = 0; e < 4; e++) o[e] = halves_sum(o[e]);
     if (lane >= 32 || c >= a.dim) return;
+    if (sees_nothing(top) && sum == sum) sum = 0.f;
     const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
     typename Vec4<E>::type x;
 #pragma unroll

@@ -215,14 +215,20 @@ __device__ __forceinline__ int wave_max(int x) {
     return x;
 }
 
+// A bias of -infinity, or so low that it can only be meant to hide (the type's lowest value in bfloat16), stands as this: 2^this is 0,
+// and its square finite, where that of an infinity is not.  A row whose maximum is no higher sees nothing.
+constexpr float kHidden = -1e15f;
+__device__ __forceinline__ bool sees_nothing(float top) { return top < 0.5f * kHidden; }
+
 // Biases of the heads h0 .. h0 + group - 1 by distance, times log2 e, in LDS: [group][2 M + 1]
 template <class E> __device__ __forceinline__ void bias_to_lds(float *table, const ScoreArgs &s, int h0, int group, int tid, int threads) {
     const E *bias = (const E *)s.bias;
     int places = 2 * s.max_distance + 1;
+    auto lowest = [](float x) { return x < kHidden ? kHidden : x; };
     for (int i = tid; i < places; i += threads) {
         int b = s.buckets[i];
         b = b < 0 ? 0 : b >= s.num_buckets ? s.num_buckets - 1 : b;
-        for (int g = 0; g < group; g++) table[g * places + i] = (float)bias[(long long)(h0 + g) * s.num_buckets + b] * kLog2e;
+        for (int g = 0; g < group; g++) table[g * places + i] = lowest((float)bias[(long long)(h0 + g) * s.num_buckets + b] * kLog2e);
     }
 }
 

@@ -256,3 +256,60 @@ def test_documents_of_very_different_lengths(docs, causal):
     got = _check({**a, "causal": causal}, dout)
     again = _attend({**a, "causal": causal}, dout)
     assert all(torch.equal(got[n], again[n]) for n in got)
+
+
+# ------------------------------------------------------------------------- biases that hide
+def _hiding(dtype, low, kv_heads, heads, cap):
+    """Keys at distance 5 and beyond read a bucket whose bias is `low`; the case without them, and which they are."""
+    a, dout = _inputs(24, dtype, [70], [300], heads, kv_heads, 64)
+    g = torch.Generator().manual_seed(3)
+    hidden = torch.rand(300, generator=g) < 0.4
+    hidden[64:130] = True  # (a whole tile of them)
+    near = torch.randint(0, 3, (300,), generator=g, dtype=torch.int32)
+    buckets = torch.tensor([0, 0, 0, 0, 0, 0, 1, 0, 2, 2, 3], dtype=torch.int32)  # distances -5 .. 5
+    bias = torch.randn(heads, 4, generator=g).to(dtype)
+    bias[:, 3] = low
+    a |= dict(bias=bias, buckets=buckets, cap=cap, q_pos=torch.zeros(70, dtype=torch.int32), k_pos=torch.where(hidden, 9 + near, near))
+    seen = {**a, "k": a["k"][~hidden], "v": a["v"][~hidden], "k_pos": a["k_pos"][~hidden], "k_off": torch.tensor([0, int((~hidden).sum())])}
+    return a, seen, hidden, dout
+
+
+@pytest.mark.parametrize("heads, kv_heads", [(4, 2), (260, 260)])
+@pytest.mark.parametrize("cap", [0.0, 6.0])
+@pytest.mark.parametrize("dtype, low", [(torch.bfloat16, -math.inf), (torch.bfloat16, torch.finfo(torch.bfloat16).min), (torch.float16, -math.inf), (torch.float16, -65504.0)])
+def test_biases_that_hide_keys(dtype, low, cap, heads, kv_heads):
+    a, seen, hidden, dout = _hiding(dtype, low, kv_heads, heads, cap)
+    got = _attend(a, dout)
+    res, tol = oracle.attention(**{**seen, "bias": seen["bias"].clone().clamp(min=-9.0)}, dout=dout)  # (no key is left that reads it)
+    for n in ("out", "lse", "dq"):
+        oracle.check(got[n], res[n], tol[n], n)
+    for n in ("dk", "dv"):
+        oracle.check(got[n].cpu()[~hidden], res[n], tol[n], n)
+        assert (got[n].cpu()[hidden] == 0).all()
+    oracle.check(got["dbias"].cpu()[:, :3], res["dbias"][:, :3], tol["dbias"][:, :3], "dbias")
+    assert (got["dbias"][:, 3] == 0).all()
+
+
+@pytest.mark.parametrize("heads, kv_heads", [(4, 2), (260, 260)])
+@pytest.mark.parametrize("cap", [0.0, 6.0])
+def test_biases_that_hide_everything(cap, heads, kv_heads):
+    a, seen, hidden, dout = _hiding(torch.bfloat16, -math.inf, kv_heads, heads, cap)
+    a["bias"][:] = -math.inf
+    got = _attend(a, dout)
+    assert all((got[n] == 0).all() for n in ("out", "dq", "dk", "dv", "dbias")) and (got["lse"] == -math.inf).all()
+
+
+@pytest.mark.parametrize("length", [40, 3000])
+@pytest.mark.parametrize("cap", [0.0, 6.0])
+def test_read_biases_that_hide(cap, length):
+    a = _read(25, torch.bfloat16, [length, 90], 2, 4, 2, 64, cap=cap)
+    a["buckets"] = torch.tensor([0, 0, 0, 0, 1, 2, 3], dtype=torch.int32)  # hops 0 .. 3
+    a["bias"][:, 3] = -math.inf
+    a["hop"][length:] = 3  # nothing left of the second list
+    got = lkg.read_entities(**{k: _gpu(x) for k, x in a.items()})
+    keep = a["hop"] != 3
+    seen = {**a, "entity": a["entity"][keep], "hop": a["hop"][keep], "off": torch.tensor([0, int(keep.sum()), int(keep.sum())]), "bias": a["bias"].clone().clamp(min=-9.0)}
+    res, tol = oracle.read(**seen)
+    for n in ("out", "lse"):
+        oracle.check(got[n], res[n], tol[n], n)
+    assert (got["out"][1] == 0).all() and (got["lse"][1] == -math.inf).all()
