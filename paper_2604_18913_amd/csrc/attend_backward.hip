@@ -281,6 +281,22 @@ __global__ __launch_bounds__(kAttThreads, DP == 64 ? 2 : 1) void k_att_dq(AttArg
 #pragma unroll
         for (int r = 0; r < 32; r++) size = fmaxf(size, __builtin_fabsf(s[r / 16][r % 16]));
         if (BIAS) look_at(kpos[lane]);
+        if (tiles_n == 1) {
+            // Few keys: their dy nearly cancel (one key's is 0), and what delta lacks would be most of it.  It is added up first.
+            float lack = 0.f;
+#pragma unroll
+            for (int u = 0; u < 2; u++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) {
+                    const int at = 32 * u + 8 * (r / 4) + 4 * half + r % 4;
+                    float y, slope;
+                    exact_score<CAP>(a, s[u][r], y, slope);
+                    if (BIAS) y += float_at(place_of_key(places, kpos[at]));
+                    if (at < seen) lack = __builtin_fmaf(exp2_fast(y - lse), dp[u][r] - delta, lack);
+                    if (r % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+                }
+            delta += halves_sum(lack);
+        }
         __syncthreads();
     }
     for (int t = 0; t < tiles_n; t++) {

@@ -313,3 +313,18 @@ def test_read_biases_that_hide(cap, length):
     for n in ("out", "lse"):
         oracle.check(got[n], res[n], tol[n], n)
     assert (got["out"][1] == 0).all() and (got["lse"][1] == -math.inf).all()
+
+
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+@pytest.mark.parametrize("dim, heads, kv_heads", [(64, 4, 2), (96, 12, 4)])
+def test_gradients_of_rows_with_few_keys(dim, heads, kv_heads, cap):
+    # dy = p (dP - delta) cancels where keys are few: with one it is 0.  delta from the rounded output would be off by 2^-9 of
+    # sums of `dim` products (some 1e-2); in 32 bits by 2^-22 of p, that is 1e-5 of the same
+    a, dout = _inputs(26, torch.bfloat16, [50, 130, 7], [1, 1, 1], heads, kv_heads, dim, bias=True)
+    got = _attend({**a, "cap": cap}, dout)
+    assert got["dq"].abs().max() < 2e-4
+    # two and three keys: the roundings of dz and of the result, 0.0017 of the norm each
+    a, dout = _inputs(27, torch.bfloat16, [50, 130, 64], [2, 3, 2], heads, kv_heads, dim, bias=True)
+    got = _check({**a, "cap": cap}, dout)
+    want = oracle.attention(**a, cap=cap, dout=dout)[0]["dq"]
+    assert (got["dq"].cpu().double() - want).norm() < 0.0035 * want.norm()
