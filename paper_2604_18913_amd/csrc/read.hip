@@ -49,7 +49,7 @@ __global__ __launch_bounds__(256, 2) void k_read(ReadArgs a) {
     const long long b0 = first_block(a.off, d, a.num_entries, 1, a.shift);
     const long long e0 = taken_into(a.off[d], a.num_entries), e1 = taken_into(a.off[d + 1], a.num_entries);
     const long long len = e1 > e0 ? e1 - e0 : 0, from = (block - b0) << a.shift;
-    if (from > 0 && from >= len) return;  // (the first block of an empty list writes its zeros)
+    if (from < 0 || (from > 0 && from >= len)) return;  // before the first list, or behind one (an empty list's first block writes its zeros)
     const bool alone = len <= (1ll << a.shift);
     const int n = (int)(len - from < (1ll << a.shift) ? len - from : 1ll << a.shift);
     const int32_t *entity = a.entity ? a.entity + e0 + from : nullptr;
