@@ -12,8 +12,8 @@ namespace lkg {
 // products of the next tile's scores and of the last tile's values are issued between the exponentials of this one, one
 // matrix instruction a step, and a tile is spared what costs most when nothing special is asked of it: all its keys are visible, all
 // its distances read one bias (text far from the row, which is most of a long document), the scores are in the range of the
-// tanh's polynomial, and the maximum does not move by more than 2^8.  m need not be the true maximum: p stays below 2^8 and
-// is summed in 32 bits.  Other tiles get their y - m first, with m the maximum again, which takes them twice as long.
+// tanh's polynomial, and the maximum does not move by more than 8.  m need not be the true maximum: p stays below 2^8 and
+// is summed in 32 bits.  (The test takes b - m: against m + 8 it would lose the scores beside a bias of large size.)  Other tiles get their y - m first, with m the maximum again, which takes them twice as long.
 //
 // 4 documents of up to 8,192 rows and keys (32 / 8 heads of 128, bfloat16, cap, bias; two fifths of the pairs are between
 // entities, whose distances vary): 2,135 us, 680 TFLOP/s of the 1,370 that a product of 16,384^3 reaches here; text alone, whose
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
     for (int t = 0; t < tiles_n; t++) {
         const bool edge = (t + 1) * kKeys > least;  // some row does not see all of the tile
         const bool far = wave_any(size > a.score.most);
-        const bool plain = !edge && !far && !varied && !wave_any(__builtin_fmaf(size, a.score.slope, b) > m + 8.f);
+        const bool plain = !edge && !far && !varied && !wave_any(__builtin_fmaf(size, a.score.slope, b - m) > 8.f);
         // p = 2^(w + shift), w = z times the polynomial of `near` (CAP) or z near[0]; the other way leaves y - m in z
         float shift = b - m, near0 = CAP ? a.score.near[0] : a.score.k, near1 = a.score.near[1], near2 = a.score.near[2], near3 = a.score.near[3];
         float shrink = 1.f;
@@ -276,7 +276,6 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
     }
     l = halves_sum(l);
     if (!mine) return;
-    if (sees_nothing(m) && l == l) l = 0.f;
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;  // (a NaN stays one)
     const long long place = (doc.row0 + row) * a.heads + h;
     write_row<E, DP>(o, inv, (E *)a.out + place * a.dim, a.dim, half);
@@ -406,7 +405,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend_few(AttArgs a) {
     const Joined all = join_wavefronts<DP>(o, m, l, lds, wave_m, wave_l, wave, lane);
     if (wave != 0 || !mine) return;
     const long long place = (doc.row0 + row) * a.heads + h;
-    const float sum = sees_nothing(all.top) && all.sum == all.sum ? 0.f : all.sum, inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+    const float sum = all.sum, inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
     write_row<E, DP>(o, inv, (E *)a.out + place * a.dim, a.dim, half);
     if (half == 0) a.lse[place] = sum == 0.f ? -INFINITY : (all.top + __log2f(sum)) * kLn2;
 }

@@ -165,7 +165,7 @@ __global__ __launch_bounds__(256, 2) void k_read(ReadArgs a) {
     const float top = all.top;
     if (wave != 0 || !mine) return;
     if (alone) {
-        const float sum = sees_nothing(top) && all.sum == all.sum ? 0.f : all.sum;
+        const float sum = all.sum;
         const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
         write_row<E, DP>(o, inv, (E *)a.out + place * a.dim, a.dim, half);
         if (half == 0) a.lse[place] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * kLn2;
@@ -214,7 +214,6 @@ template <class E> __global__ __launch_bounds__(256) void k_read_join(ReadArgs a
 #pragma unroll
     for (int e = 0; e < 4; e++) o[e] = halves_sum(o[e]);
     if (lane >= 32 || c >= a.dim) return;
-    if (sees_nothing(top) && sum == sum) sum = 0.f;
     const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
     typename Vec4<E>::type x;
 #pragma unroll

@@ -14,7 +14,11 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kLowest = -1e30f;  // running maximum of a row that has seen nothing: below any score, and no infinity
+
+// A bias of -infinity, or so low that it can only be meant to hide (the type's lowest value in bfloat16), stands as kHidden: 2^this
+// is 0, and its square finite, where that of an infinity is not.  kLowest is the running maximum of a row that has seen nothing,
+// below any other score and above the hidden ones: those weigh 0 from the first tile on, and a sum of 0 tells that nothing was seen.
+constexpr float kHidden = -1e15f, kLowest = 0.5f * kHidden;
 
 // The two 16-bit types: eight values as a matrix instruction takes them, and that instruction on 32 x 32 x 16.
 // Lane l holds A[l % 32][8 (l / 32) ..] and B[8 (l / 32) ..][l % 32]; C's element r is row 8 (r / 4) + 4 (l / 32) + r % 4
@@ -214,11 +218,6 @@ __device__ __forceinline__ int wave_max(int x) {
     }
     return x;
 }
-
-// A bias of -infinity, or so low that it can only be meant to hide (the type's lowest value in bfloat16), stands as this: 2^this is 0,
-// and its square finite, where that of an infinity is not.  A row whose maximum is no higher sees nothing.
-constexpr float kHidden = -1e15f;
-__device__ __forceinline__ bool sees_nothing(float top) { return top < 0.5f * kHidden; }
 
 // Biases of the heads h0 .. h0 + group - 1 by distance, times log2 e, in LDS: [group][2 M + 1]
 template <class E> __device__ __forceinline__ void bias_to_lds(float *table, const ScoreArgs &s, int h0, int group, int tid, int threads) {

@@ -1,0 +1,49 @@
+"""Scores that the attention's kernels take apart (bounds: reading_oracle)."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_reading import _check, _inputs
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------- biases that hide the first tiles of a row
+@pytest.mark.parametrize("heads, kv_heads", [(4, 2), (260, 260)])  # (few rows, many)
+@pytest.mark.parametrize("dtype, cap, size", [(torch.float16, 0.0, 3.0), (torch.float16, 50.0, 3.0), (torch.bfloat16, 0.0, 40.0), (torch.bfloat16, 50.0, 3.0)])
+@pytest.mark.parametrize("low", [-math.inf, -1e10])  # (-1e10 hides by its size alone: beside it, 32 bits hold scores to 512)
+def test_first_tiles_hidden_by_their_bias(low, dtype, cap, size, heads, kv_heads):
+    # four whole tiles that read a hiding bucket, under scores of which 16 bits could not hold the exponential, then keys that
+    # are seen; the second document has hidden keys only
+    if dtype is torch.float16 and low > -math.inf:
+        low = -65504.0
+    a, dout = _inputs(41, dtype, [70, 40], [300, 200], heads, kv_heads, 64, spread=1.5)
+    g = torch.Generator().manual_seed(41)
+    k_pos = torch.randint(0, 3, (500,), generator=g, dtype=torch.int32)
+    k_pos[:256], k_pos[300:] = 9, 9
+    a["k"][:256] *= size
+    a["k"][300:] *= size
+    bias = torch.randn(heads, 4, generator=g).to(dtype)
+    bias[:, 3] = low
+    a |= dict(bias=bias, buckets=torch.tensor([0, 0, 0, 0, 0, 0, 1, 0, 2, 2, 3], dtype=torch.int32), cap=cap,
+              q_pos=torch.zeros(110, dtype=torch.int32), k_pos=k_pos)
+    if low > -math.inf:  # (keys that all read a finite bias share their row's weight: no such document here)
+        a |= dict(q=a["q"][:70], q_off=torch.tensor([0, 70]), k=a["k"][:300], v=a["v"][:300], k_off=torch.tensor([0, 300]), q_pos=a["q_pos"][:70], k_pos=k_pos[:300])
+        _check(a, dout[:70])
+    else:
+        got = _check(a, dout)
+        assert all((got[n][70:] == 0).all() for n in ("out", "dq")) and (got["lse"][70:] == -math.inf).all()
+        assert all((got[n][300:] == 0).all() and (got[n][:256] == 0).all() for n in ("dk", "dv")) and (got["dbias"][:, 3] == 0).all()
+
+
+@pytest.mark.parametrize("heads, kv_heads", [(4, 2), (132, 132)])
+@pytest.mark.parametrize("dtype, cap", [(torch.float16, 0.0), (torch.float16, 50.0), (torch.bfloat16, 20.0)])
+def test_a_window_made_by_a_hiding_bucket(dtype, cap, heads, kv_heads):
+    # causal text whose keys 60 or more places back are hidden: the last rows' first tiles hold nothing else
+    a, dout = _inputs(42, dtype, [420], [420], heads, kv_heads, 64, spread=2.0)
+    buckets = torch.zeros(2 * 60 + 1, dtype=torch.int32)
+    buckets[0], buckets[1:30] = 2, 1
+    bias = torch.zeros(heads, 3, dtype=dtype)
+    bias[:, 1], bias[:, 2] = 0.5, -math.inf
+    _check({**a, "causal": True, "cap": cap, "bias": bias, "buckets": buckets}, dout)
