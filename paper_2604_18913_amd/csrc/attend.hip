@@ -159,12 +159,13 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
             } else {
 #pragma unroll
                 for (int u = 0; u < 2; u++)
+                    if (CAP) cap_scores<true>(a.score, s[u]);
+#pragma unroll
+                for (int u = 0; u < 2; u++)
 #pragma unroll
                     for (int r = 0; r < 16; r++) {
                         const int at = 32 * u + 8 * (r / 4) + 4 * half + r % 4;
-                        float y;
-                        if (CAP) y = __builtin_fmaf(-2.f * a.score.c, rcp_fast(exp2_fast(s[u][r] * a.score.k) + 1.f), a.score.c);
-                        else y = s[u][r] * a.score.k;
+                        float y = CAP ? s[u][r] : s[u][r] * a.score.k;
                         if (BIAS) y += float_at(place_of_key(places, kpt[at]));
                         y = t * kKeys + at < seen ? y : -INFINITY;
                         s[u][r] = y;
@@ -365,6 +366,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend_few(AttArgs a) {
         wave_sync();
         if (t + 4 < tiles_n) fetch(t + 4);
         const bool edge = (t + 1) * kFewKeys > least;
+        if (CAP) cap_scores<DP == 64>(a.score, s);
         float top = kLowest;
 #pragma unroll
         for (int j = 0; j < 4; j++) {
@@ -372,9 +374,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend_few(AttArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; e++) {
                 const int r = 4 * j + e;
-                float y;
-                if (CAP) y = __builtin_fmaf(-2.f * a.score.c, rcp_fast(exp2_fast(s[r] * a.score.k) + 1.f), a.score.c);
-                else y = s[r] * a.score.k;
+                float y = CAP ? s[r] : s[r] * a.score.k;
                 if (BIAS) y += float_at(place_of_key(places, (int)p4[e]));
                 if (edge) y = t * kFewKeys + 8 * j + 4 * half + e < seen ? y : -INFINITY;
                 s[r] = y;
@@ -456,7 +456,7 @@ logoskg_status attend_args(const logoskg_attention *a, AttArgs *o, const char *c
     o->few_blocks = (a->num_rows * o->group >> kFewShift) + a->num_docs;
     o->key_blocks = (a->num_keys >> kAttRowsShift) + a->num_docs;
     o->scale = a->score.scale;
-    o->curve = o->score.c > 0 ? -a->score.scale / (o->score.c * o->score.c) : 0.f;
+    o->curve = o->score.c > 0 ? (float)(-(double)a->score.scale / ((double)o->score.c * o->score.c)) : 0.f;
     o->slope = 4.f * a->score.scale;
     if (o->row_blocks * a->kv_heads >= (1ll << 31)) { set_error("%s: too many rows", call); return LOGOSKG_EINVAL; }
     return LOGOSKG_OK;

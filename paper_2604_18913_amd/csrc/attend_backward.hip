@@ -87,17 +87,23 @@ template <class E> __device__ __forceinline__ typename Vec8<E>::type chunk_of(co
     return as8<E>(u32x4{pairs[0], pairs[1], pairs[2], pairs[3]});
 }
 
-// A special element: y and its slope from the product, by the exact tanh
-template <bool CAP> __device__ __forceinline__ void exact_score(const AttArgs &a, float z, float &y, float &slope) {
-    if (CAP) {
-        const float w = rcp_fast(exp2_fast(z * a.score.k) + 1.f);
-        y = __builtin_fmaf(-2.f * a.score.c, w, a.score.c);
-        slope = a.slope * (w * (1.f - w));
+// A special element: y and its slope from the product; `far`: which may be of any size
+template <bool CAP> __device__ __forceinline__ void score_of(const AttArgs &a, const Steps &x, bool far, float z, float &y, float &slope) {
+    if (!CAP) {
+        y = z * x.near0;
+        slope = x.slope;
+    } else if (far) {
+        float share;
+        y = any_capped(a.score, z, share);
+        slope = a.slope * (share * (1.f - share));
     } else {
-        y = z * a.score.k;
-        slope = a.scale;
+        y = element_w<CAP>(x, z);
+        slope = __builtin_fmaf(y * y, x.curve, x.slope);
     }
 }
+// What is special about a tile, each kind with its own elements: varied biases alone, hidden keys (or either where there are no
+// biases), products that are not near
+enum { kVaried, kEdge, kFar };
 constexpr float kHiddenLse = 1e15f;    // of a row that sees nothing, or is none: p = 0 the same way
 
 // the first row that sees one of the keys from kb on
@@ -284,13 +290,14 @@ __global__ __launch_bounds__(kAttThreads, DP == 64 ? 2 : 1) void k_att_dq(AttArg
         if (tiles_n == 1) {
             // Few keys: their dy nearly cancel (one key's is 0), and what delta lacks would be most of it.  It is added up first.
             float lack = 0.f;
+            const Steps x = plain_steps<CAP>(a, 0.f);
 #pragma unroll
             for (int u = 0; u < 2; u++)
 #pragma unroll
                 for (int r = 0; r < 16; r++) {
                     const int at = 32 * u + 8 * (r / 4) + 4 * half + r % 4;
                     float y, slope;
-                    exact_score<CAP>(a, s[u][r], y, slope);
+                    score_of<CAP>(a, x, true, s[u][r], y, slope);
                     if (BIAS) y += float_at(place_of_key(places, kpos[at]));
                     if (at < seen) lack = __builtin_fmaf(exp2_fast(y - lse), dp[u][r] - delta, lack);
                     if (r % 8 == 7) __builtin_amdgcn_sched_barrier(0);
@@ -302,7 +309,7 @@ __global__ __launch_bounds__(kAttThreads, DP == 64 ? 2 : 1) void k_att_dq(AttArg
     for (int t = 0; t < tiles_n; t++) {
         const bool edge = (t + 1) * kGradTile > least, far = wave_any(size > a.score.most), plain = !edge && !far && !varied;
         Steps x = plain_steps<CAP>(a, b);
-        auto special = [&](auto exact) __attribute__((always_inline)) {
+        auto special = [&](auto kind) __attribute__((always_inline)) {
 #pragma unroll
             for (int u = 0; u < 2; u++) {
                 float bias[16];
@@ -316,7 +323,7 @@ __global__ __launch_bounds__(kAttThreads, DP == 64 ? 2 : 1) void k_att_dq(AttArg
 #pragma unroll
                 for (int r = 0; r < 16; r++) {
                     float away = dp[u][r] - delta;
-                    if (!decltype(exact)::value) {
+                    if (decltype(kind)::value == kVaried) {
                         const float w = element_w<CAP>(x, s[u][r]);
                         float y = bias[r] - lse;
                         y = CAP ? y + w : __builtin_fmaf(w, x.near0, y);
@@ -324,7 +331,7 @@ __global__ __launch_bounds__(kAttThreads, DP == 64 ? 2 : 1) void k_att_dq(AttArg
                         dp[u][r] = element_dz<CAP>(x, away, w);
                     } else {
                         float y, slope;
-                        exact_score<CAP>(a, s[u][r], y, slope);
+                        score_of<CAP>(a, x, decltype(kind)::value == kFar, s[u][r], y, slope);
                         y += bias[r] - lse;
                         if (t * kGradTile + 32 * u + 8 * (r / 4) + 4 * half + r % 4 >= seen) y = kHidden, away = 0.f;
                         s[u][r] = y < kHidden ? kHidden : y;
@@ -336,8 +343,9 @@ __global__ __launch_bounds__(kAttThreads, DP == 64 ? 2 : 1) void k_att_dq(AttArg
             }
         };
         if (!plain) {
-            if (!BIAS || edge || far) special(std::true_type{});
-            else special(std::false_type{});
+            if (CAP && (!BIAS || far)) special(std::integral_constant<int, kFar>{});
+            else if (!BIAS || edge) special(std::integral_constant<int, kEdge>{});
+            else special(std::integral_constant<int, kVaried>{});
             x = special_steps();
         }
         const unsigned kt = my_rows + k_buffer(t + 1), vt = my_rows + v_buffer(t + 1), ct = my_columns + k_buffer(t - 1);
@@ -598,7 +606,7 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
         const float *lse = lses + (t & 3) * kGradTile, *delta = deltas + (t & 3) * kGradTile;
         const int bucket_now = bucket;
         Steps x = plain_steps<CAP>(a, b);
-        auto special = [&](auto exact) __attribute__((always_inline)) {
+        auto special = [&](auto kind) __attribute__((always_inline)) {
             const unsigned to_head = to_table + g * places_n * 4;
 #pragma unroll
             for (int part = 0; part < 4; part++) {
@@ -620,6 +628,16 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
                     if (BIAS) bucket_of[i] = int_at(place[i]);
                 }
                 __builtin_amdgcn_sched_barrier(0);
+                float ys[8], slopes[8];
+                if (decltype(kind)::value != kVaried) {
+                    if (CAP && (!BIAS || far)) {
+#pragma unroll
+                        for (int i = 0; i < 8; i++) score_of<CAP>(a, x, true, s[u][4 * j0 + i], ys[i], slopes[i]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; i++) score_of<CAP>(a, x, false, s[u][4 * j0 + i], ys[i], slopes[i]);
+                    }
+                }
 #pragma unroll
                 for (int j = 0; j < 2; j++) {
                     const int at = 32 * u + 8 * (j0 + j) + 4 * half;
@@ -628,7 +646,7 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
                     for (int e = 0; e < 4; e++) {
                         const int r = 4 * (j0 + j) + e;
                         float away = dp[u][r] - delta4[e];
-                        if (!decltype(exact)::value) {
+                        if (decltype(kind)::value == kVaried) {
                             const float w = element_w<CAP>(x, s[u][r]);
                             float y = bias[4 * j + e] - lse4[e];
                             y = CAP ? y + w : __builtin_fmaf(w, x.near0, y);
@@ -636,7 +654,7 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
                             dp[u][r] = element_dz<CAP>(x, away, w);
                         } else {
                             float y, slope;
-                            exact_score<CAP>(a, s[u][r], y, slope);
+                            y = ys[4 * j + e], slope = slopes[4 * j + e];
                             y += bias[4 * j + e] - lse4[e];
                             if (key >= doc.seen(r0 + at + e, a.causal)) y = kHidden, away = 0.f;
                             s[u][r] = y < kHidden ? kHidden : y;
@@ -653,8 +671,8 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
             }
         };
         if (!plain) {
-            if (!BIAS || edge || far) special(std::true_type{});
-            else special(std::false_type{});
+            if (!BIAS || edge || far) special(std::integral_constant<int, kEdge>{});
+            else special(std::integral_constant<int, kVaried>{});
             x = special_steps();
         }
         const unsigned rt = my_rows + after, ct = my_columns + last;

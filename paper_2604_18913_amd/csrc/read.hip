@@ -128,12 +128,11 @@ __global__ __launch_bounds__(256, 2) void k_read(ReadArgs a) {
         if (t + 4 < tiles_n) fetch(id);
         next_id = id_of(t + 8);
         if (BIAS) next_hop = hop_of(t + 8);
+        if (CAP) cap_scores<DP == 64>(a.score, s);
         float top = kLowest;
 #pragma unroll
         for (int r = 0; r < 16; r++) {
-            float y;
-            if (CAP) y = __builtin_fmaf(-2.f * a.score.c, rcp_fast(exp2_fast(s[r] * a.score.k) + 1.f), a.score.c);
-            else y = s[r] * a.score.k;
+            float y = CAP ? s[r] : s[r] * a.score.k;
             const int at = 8 * (r / 4) + 4 * half + r % 4;
             if (BIAS) y += my_table[distance_place(hops[wave][at], q_pos, M)];
             if (seen != ~0u) y = seen >> at & 1 ? y : -INFINITY;

@@ -170,12 +170,13 @@ __device__ __forceinline__ int document_of(const int64_t *off, int n, long long 
 // ---------------------------------------------------------------- scores
 // What the kernels make of logoskg_score, in units of log 2.  Without a cap y = z k, k = scale log2 e.  With one
 // y = c - 2 c / (2^(z k) + 1), c = cap log2 e, which is c tanh(z scale / cap) for k = 2 log2 e scale / cap (2^.. may be
-// infinite or 0: +c or -c); for products up to `most`, where tanh's argument is below 1/2, also y = z times a polynomial in
-// z^2 (near), which costs five instructions instead of an exponential, a reciprocal and three, and is as exact.
+// infinite or 0: +c or -c).  That form's error is c 2^-23 whatever y is, so it is for products above `most` alone, where tanh's
+// argument is 1/2 or more; up to there y = z times a polynomial in z^2 (near), exact to 5.5e-7 of y under any cap, which also
+// costs five instructions instead of an exponential, a reciprocal and three.
 struct ScoreArgs {
     float k, c;
     float slope;    // |y| <= |z| slope
-    float most;     // largest |z| that the near form holds for (no cap: any)
+    float most;     // largest |z| that the near form holds for (no cap: any; below 0: none)
     float near[4];
     const void *bias;
     const int32_t *buckets;
@@ -185,21 +186,63 @@ struct ScoreArgs {
 inline ScoreArgs score_args(const logoskg_score &s) {
     ScoreArgs a;
     const float lin = s.scale * kLog2e;
-    a.k = s.cap > 0 ? 2.f * kLog2e * s.scale / s.cap : lin;
-    a.c = s.cap > 0 ? s.cap * kLog2e : 0.f;
+    const double w = s.cap > 0 ? (double)s.scale / s.cap : 0.0, steep = 2.0 * kLog2e * w;
+    a.k = s.cap > 0 ? (float)(steep > 3e38 ? 3e38 : steep < -3e38 ? -3e38 : steep) : lin;
+    a.c = s.cap > 0 ? (s.cap > 1e37f ? 1e37f : s.cap) * kLog2e : 0.f;  // (twice it is finite; products under such caps are near)
     a.slope = lin < 0 ? -lin : lin;
     a.most = INFINITY;
     // tanh(x) / x on |x| <= 1/2 as a polynomial in x^2: smallest largest relative error, 5.5e-7 (Remez exchange on [0, 1/4])
     const double fit[4] = {0.999999463558197, -0.33326318860054016, 0.13190296292304993, -0.04440222680568695};
-    const double w = s.cap > 0 ? (double)s.scale / s.cap : 0.0;
     double f = lin;
     for (int i = 0; i < 4; i++, f *= w * w) a.near[i] = (float)(fit[i] * f);
-    if (s.cap > 0 && w != 0.0) a.most = (float)(0.5 / (w < 0 ? -w : w));
+    if (s.cap > 0 && w != 0.0) {
+        const double most = 0.5 / (w < 0 ? -w : w);
+        a.most = most < 1e18 ? (float)most : 1e18f;  // (z^2 is finite)
+        if (!(f > -1e30 && f < 1e30)) {  // a cap so small that the coefficients leave 32 bits: products that are near are 0
+            a.most = -1.f;
+            for (float &x : a.near) x = 0.f;
+        }
+    }
     a.bias = s.bias;
     a.buckets = s.buckets;
     a.num_buckets = s.num_buckets;
     a.max_distance = s.max_distance;
     return a;
+}
+
+// A score under a cap, of a product that is near
+__device__ __forceinline__ float near_capped(const ScoreArgs &s, float z) {
+    const float zz = z * z;
+    float w = __builtin_fmaf(zz, s.near[3], s.near[2]);
+    w = __builtin_fmaf(zz, w, s.near[1]);
+    w = __builtin_fmaf(zz, w, s.near[0]);
+    return z * w;
+}
+// .. of any; `share`: 1 / (2^(z k) + 1), of which the backward makes the slope
+__device__ __forceinline__ float any_capped(const ScoreArgs &s, float z, float &share) {
+    share = rcp_fast(exp2_fast(z * s.k) + 1.f);
+    const float far = __builtin_fmaf(-2.f * s.c, share, s.c), near = near_capped(s, z);
+    return __builtin_fabsf(z) <= s.most ? near : far;
+}
+__device__ __forceinline__ float any_capped(const ScoreArgs &s, float z) {
+    float share;
+    return any_capped(s, z, share);
+}
+// Sixteen products of a wavefront's lanes to scores, in place; with ROOM in the registers for two ways, by the near form alone where
+// all of them are near, which is cheaper
+template <bool ROOM> __device__ __forceinline__ void cap_scores(const ScoreArgs &s, f32x16 &z) {
+    float size = 0.f;
+    if (ROOM) {
+#pragma unroll
+        for (int r = 0; r < 16; r++) size = fmaxf(size, __builtin_fabsf(z[r]));
+    }
+    if (!ROOM || wave_any(size > s.most)) {
+#pragma unroll
+        for (int r = 0; r < 16; r++) z[r] = any_capped(s, z[r]);
+    } else {
+#pragma unroll
+        for (int r = 0; r < 16; r++) z[r] = near_capped(s, z[r]);
+    }
 }
 
 __device__ __forceinline__ int wave_min(int x) {

@@ -1,10 +1,11 @@
-"""Scores that the attention's kernels take apart (bounds: reading_oracle)."""
+"""Scores that the attention's kernels take apart: biases that hide the first tiles of a row, caps of any size (bounds:
+reading_oracle)."""
 import math
 
 import pytest
 import torch
 
-from test_gpu_reading import _check, _inputs
+from test_gpu_reading import _check, _check_read, _inputs, _read
 
 pytestmark = pytest.mark.gpu
 
@@ -47,3 +48,25 @@ def test_a_window_made_by_a_hiding_bucket(dtype, cap, heads, kv_heads):
     bias = torch.zeros(heads, 3, dtype=dtype)
     bias[:, 1], bias[:, 2] = 0.5, -math.inf
     _check({**a, "causal": True, "cap": cap, "bias": bias, "buckets": buckets}, dout)
+
+
+# ------------------------------------------------------------------------- caps of any size
+CAPS = [1e-30, 1e-9, 1e3, 1e4, 1e6, 1e8, 1e30]
+
+
+@pytest.mark.parametrize("heads, kv_heads, dim", [(4, 2, 64), (4, 2, 128), (264, 264, 16)])
+@pytest.mark.parametrize("cap", CAPS)
+def test_attention_under_any_cap(cap, heads, kv_heads, dim):
+    # causal, so that most tiles have hidden keys; a row and a key of zeros, whose products are 0
+    a, dout = _inputs(43, torch.float16, [90, 30], [90, 140], heads, kv_heads, dim, bias=True)
+    a["q"][7], a["k"][11] = 0, 0
+    _check({**a, "causal": True, "cap": cap}, dout)
+    _check({**a, "causal": False, "cap": cap}, dout)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("cap", CAPS)
+def test_read_under_any_cap(cap, dim):
+    a = _read(44, torch.float16, [40, 0, 700], 2, 4, 2, dim, cap=cap)
+    a["q"][0, 0] = 0
+    _check_read(a)
