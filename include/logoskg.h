@@ -525,7 +525,8 @@ typedef struct {
  * Attention of a ragged batch.  Row i of a document with R rows and K keys sees
  * all K keys, or with `causal` the keys j < prefix and those j <= i + K - R (the
  * retrieved entities in front, then the text up to the row itself).  A row that
- * sees nothing gets zeros and lse = -inf.  Other documents' values never matter;
+ * sees nothing, or that no document holds (before q_off[0], from the last offset
+ * on: buffers may be longer than the batch), gets zeros and lse = -inf.  Other documents' values never matter;
  * keys of its own document that a row does not see are weighted with 0, so that an
  * infinity or NaN there may still reach it.
  */
@@ -545,8 +546,8 @@ typedef struct {
 
 /*
  * Gradients of logoskg_attend with respect to q, k, v and the bias, for out and
- * lse as that call has left them.  Sums are taken in a fixed order: the same
- * inputs give the same bits.
+ * lse as that call has left them; zeros for rows and keys that no document
+ * holds.  Sums are taken in a fixed order: the same inputs give the same bits.
  */
 int64_t logoskg_attend_backward_bytes(const logoskg_attention *a);
 logoskg_status logoskg_attend_backward(const logoskg_attention *a, const logoskg_attention_grad *g);

@@ -61,6 +61,27 @@ __device__ __forceinline__ AttDoc att_doc(const AttArgs &a, int d) {
     return o;
 }
 
+// Rows or keys that no document holds lie before the first document and behind the last, and get zeros.  A block has N places (of
+// row x head of the group, or of a key), the first of them at `first` from its document's begin; f(place in the array) for those that
+// nobody holds.  All of them fall on some block: what begins before the first document's own blocks on the blocks before those,
+// but for the places before the first of these, which block 0 takes too; what lies behind the last document on its blocks.
+template <int N, class F> __device__ __forceinline__ void each_spare(long long begin, long long held, long long total, int d, int num_docs, long long block, long long first, int tid, F f) {
+    const bool front = d == 0 && first < 0, behind = d + 1 == num_docs && first + N > held;
+    if (front || behind)
+#pragma unroll 1
+        for (int i = tid; i < N; i += kAttThreads) {
+            const long long x = first + i;
+            if (((front && x < 0) || (behind && x >= held)) && begin + x < total) f(begin + x);
+        }
+    if (block == 0)
+#pragma unroll 1
+        for (int i = tid; i < (int)(begin & (N - 1)); i += kAttThreads) f(i);
+}
+template <class E> __device__ __forceinline__ void clear_row(E *row, int dim) {
+#pragma unroll 1
+    for (int c = 0; c < dim; c += 8) *(u32x4 *)(row + c) = u32x4{0, 0, 0, 0};
+}
+
 // A window of memory from `base` on: reads behind `bytes` give zeros (and touch nothing).
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t window(const void *base, long long bytes) {
     bytes = bytes < 0 ? 0 : bytes > 0x7ffffff0 ? 0x7ffffff0 : bytes;

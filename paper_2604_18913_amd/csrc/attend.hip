@@ -37,6 +37,11 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
     const AttDoc doc = att_doc(a, d);
     const long long first = (block - first_block(a.q_off, d, a.num_rows, a.group, kAttRowsShift)) << kAttRowsShift;
     const long long vrows = (long long)doc.rows * a.group;
+    each_spare<kAttRows>(doc.row0 * a.group, vrows, a.num_rows * a.group, d, a.num_docs, block, first, tid, [&](long long at) {
+        const long long spare = at / a.group * a.heads + head * a.group + at % a.group;
+        clear_row((E *)a.out + spare * a.dim, a.dim);
+        a.lse[spare] = -INFINITY;
+    });
     if (first >= vrows || first < 0) return;
 
     const long long vr = first + wave * 32 + (lane & 31);
@@ -303,6 +308,11 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend_few(AttArgs a) {
     const AttDoc doc = att_doc(a, d);
     const long long first = (block - first_block(a.q_off, d, a.num_rows, a.group, kFewShift)) << kFewShift;
     const long long vrows = (long long)doc.rows * a.group;
+    each_spare<1 << kFewShift>(doc.row0 * a.group, vrows, a.num_rows * a.group, d, a.num_docs, block, first, tid, [&](long long at) {
+        const long long spare = at / a.group * a.heads + head * a.group + at % a.group;
+        clear_row((E *)a.out + spare * a.dim, a.dim);
+        a.lse[spare] = -INFINITY;
+    });
     if (first >= vrows || first < 0) return;
 
     const long long vr = first + (lane & 31);

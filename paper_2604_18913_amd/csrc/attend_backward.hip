@@ -193,6 +193,10 @@ __global__ __launch_bounds__(kAttThreads, DP == 64 ? 2 : 1) void k_att_dq(AttArg
     const AttDoc doc = att_doc(a, d);
     const long long first = (block - first_block(a.q_off, d, a.num_rows, G, kAttRowsShift)) << kAttRowsShift;
     const long long vrows = (long long)doc.rows * G;
+    each_spare<kAttRows>(doc.row0 * a.group, vrows, a.num_rows * a.group, d, a.num_docs, block, first, tid, [&](long long at) {
+        const long long spare = at / a.group * a.heads + head * a.group + at % a.group;
+        clear_row((E *)a.dq + spare * a.dim, a.dim);
+    });
     if (first >= vrows || first < 0) return;
 
     const long long vr = first + wave * 32 + (lane & 31);
@@ -447,6 +451,10 @@ __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {
     const AttDoc doc = att_doc(a, d);
     const long long kb = (block - first_block(a.k_off, d, a.num_keys, 1, kAttRowsShift)) << kAttRowsShift;
     float *part = BIAS ? a.bias_part + (block * a.heads + head * G) * nb : nullptr;
+    each_spare<kAttRows>(doc.key0, doc.keys, a.num_keys, d, a.num_docs, block, kb, tid, [&](long long at) {
+        clear_row((E *)a.dk + (at * a.kv_heads + head) * a.dim, a.dim);
+        clear_row((E *)a.dv + (at * a.kv_heads + head) * a.dim, a.dim);
+    });
     if (kb >= doc.keys || kb < 0) {
         if (BIAS)
             for (int i = tid; i < G * nb; i += kAttThreads) part[i] = 0.f;

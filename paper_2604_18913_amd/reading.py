@@ -185,7 +185,7 @@ def attend(q, k, v, q_off, k_off, *, scale=None, cap=0.0, causal=False, prefix=N
     """``logoskg_attend``: attention of a ragged batch, as (out [rows, heads, dim], lse float32 [rows, heads]).
 
     ``q`` [rows, heads, dim], ``k`` and ``v`` [keys, kv_heads, dim] in bfloat16 or float16, documents one behind the
-    other at ``q_off`` / ``k_off`` (int64, on the device).  ``causal``: row i of R sees the keys up to i + K - R, and
+    other at ``q_off`` / ``k_off`` (int64, on the device); rows that none holds get zeros and -inf.  ``causal``: row i of R sees the keys up to i + K - R, and
     the document's first ``prefix`` (int32, one per document) besides; else every row sees all keys.  ``cap``: scores
     become cap tanh(score / cap).  ``bias`` [heads, buckets] is learned, ``buckets`` (``distance_buckets``) says which
     column the distance ``k_pos - q_pos`` reads (positions: int32, by default the places, aligned at the end)."""

@@ -1,5 +1,7 @@
 """The calls that read a retrieval on a part of a batch: offsets that begin behind the first entry and end before the last, as
 a slice of a batch's offsets with its whole arrays gives them (bounds: reading_oracle)."""
+import math
+
 import pytest
 import torch
 
@@ -80,3 +82,57 @@ def test_attention_of_documents_that_begin_behind_the_first_row(heads, kv_heads,
     for n in ("dk", "dv"):
         oracle.check(got[n][k_off[0]:k_off[-1]], res[n][k_off[0]:k_off[-1]], tol[n][k_off[0]:k_off[-1]], n)
     oracle.check(got["dbias"], res["dbias"], tol["dbias"], "dbias")
+
+
+def _stale():
+    """Leaves NaN in the memory that the next tensors take."""
+    junk = [torch.full((1 << n,), math.nan, device="cuda") for n in range(8, 24) for _ in range(3)]
+    torch.cuda.synchronize()
+    del junk
+
+
+def _check_spare(got, q_off, k_off):
+    for n, (a, b) in {"out": (q_off[0], q_off[-1]), "dq": (q_off[0], q_off[-1]), "dk": (k_off[0], k_off[-1]), "dv": (k_off[0], k_off[-1])}.items():
+        assert (got[n][:a] == 0).all() and (got[n][b:] == 0).all(), n
+    assert (got["lse"][:q_off[0]] == -math.inf).all() and (got["lse"][q_off[-1]:] == -math.inf).all()
+
+
+@pytest.mark.parametrize("part", PARTS + [([0, 0], 200, [0, 0], 300), ([700, 700], 700, [900, 900], 900), ([500, 500, 500], 900, [0, 300, 300], 300)],
+                         ids=lambda x: "-".join(map(str, x[0])))
+@pytest.mark.parametrize("heads, kv_heads, dim", [(4, 2, 64), (6, 2, 80), (264, 264, 16), (35, 1, 24)])
+def test_rows_and_keys_that_no_document_holds(heads, kv_heads, dim, part):
+    a, dout = _part(36, torch.bfloat16, *part, heads, kv_heads, dim)
+    _stale()
+    _check_spare(_attend(a, dout), part[0], part[2])
+
+
+@pytest.mark.parametrize("heads, kv_heads", [(8, 2), (64, 32)])  # (the second batch's blocks are put in order)
+def test_a_batch_in_longer_buffers_under_a_graph(heads, kv_heads):
+    # buffers for 900 rows and 1,500 keys, offsets that change from replay to replay
+    a, dout = _inputs(37, torch.bfloat16, [100] * 9, [150] * 10, heads, kv_heads, 32, bias=True)
+    a["q_off"], a["k_off"] = (torch.cat([torch.zeros(1, dtype=torch.int64), x.sort().values]) for x in (a["q_off"][1:10], a["k_off"][1:10]))
+    b, d = {k: _gpu(x) for k, x in a.items()}, _gpu(dout)
+    pos = [b.pop(n) for n in ("q", "k", "v", "q_off", "k_off")]
+
+    def call():
+        out, lse = lkg.attend(*pos, causal=True, **b)
+        return dict(zip(("out", "lse", "dq", "dk", "dv", "dbias"), (out, lse, *lkg.attend_backward(d, *pos[:3], out, lse, *pos[3:], causal=True, **b))))
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        call()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = call()
+    for docs in (9, 4, 1, 6):
+        q_off, k_off = a["q_off"].clamp(max=100 * docs - 13), a["k_off"].clamp(max=150 * docs - 20)
+        pos[3].copy_(q_off)
+        pos[4].copy_(k_off)
+        for x in got.values():
+            x.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = call()
+        assert all(torch.equal(got[n], want[n]) for n in got)
+        _check_spare(got, q_off.tolist(), k_off.tolist())
