@@ -510,7 +510,7 @@ typedef struct {
     const int64_t *q_off, *k_off;    /* device int64[num_docs + 1]                           */
     const void *q, *k, *v;           /* device, rows of heads of dim consecutive elements    */
     int64_t q_row, q_head, k_row, k_head, v_row, v_head; /* strides, in elements: multiples of 8
-                                        (the arrays are 16-byte aligned)                     */
+                                        (the arrays are 16-byte aligned); those of rows not negative */
     const int32_t *prefix;    /* device int32[num_docs] or NULL (no prefix)                  */
     const int32_t *q_pos;     /* device int32[num_rows] or NULL: row i stands at i + keys - rows
                                  of its document                                             */

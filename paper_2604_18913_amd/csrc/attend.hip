@@ -450,7 +450,7 @@ logoskg_status attend_args(const logoskg_attention *a, AttArgs *o, const char *c
     if (!why && a->num_docs > 0 && (!a->q_off || !a->k_off)) why = "offsets are NULL";
     if (!why && a->num_rows && (!a->q || !a->out || !a->lse)) why = "q, out or lse is NULL";
     if (!why && a->num_keys && (!a->k || !a->v)) why = "k or v is NULL";
-    if (!why && (a->k_row < 0 || a->v_row < 0 || a->k_row >= kMostStride || a->v_row >= kMostStride || a->q_row >= kMostStride)) why = "a row stride is negative or too large";
+    if (!why && (a->q_row < 0 || a->k_row < 0 || a->v_row < 0 || a->k_row >= kMostStride || a->v_row >= kMostStride || a->q_row >= kMostStride)) why = "a row stride is negative or too large";
     if (!why && (odd_place(a->q, a->q_row, a->q_head) || odd_place(a->k, a->k_row, a->k_head) || odd_place(a->v, a->v_row, a->v_head) || odd_place(a->out, 0, 0)))
         why = "an array is not 16-byte aligned, or a stride no multiple of 8";
     if (why) { set_error("%s: %s", call, why); return LOGOSKG_EINVAL; }

@@ -302,7 +302,7 @@ template <class F> logoskg_status allow_lds(F *kernel, size_t bytes) {
     return LOGOSKG_OK;
 }
 
-const char *bad_score(const logoskg_score &s, int heads, int kv_heads);  // read.hip: why a call refuses it, or NULL
+const char *bad_score(const logoskg_score &s, int heads, int kv_heads);  // attend.hip: why a call refuses it, or NULL
 const char *bad_heads(int dtype, int heads, int kv_heads, int dim);
 
 }  // namespace lkg
