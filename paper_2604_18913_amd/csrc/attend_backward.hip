@@ -176,6 +176,7 @@ __global__ __launch_bounds__(1024) void k_att_order(AttArgs a) {
 // unit, whose matrix instructions follow from four chains; smaller ones for two.  4 documents of up to 4,096 rows and keys (32 / 8
 // heads of 128, bfloat16, cap, bias): 690 us, 520 TFLOP/s of its three products.
 constexpr int kGradTile = 64;
+constexpr int kFewSeen = 16;  // with n keys what delta lacks is some 1 / sqrt n of the roundings of dz and dQ
 
 template <class E, int DP, bool CAP, bool BIAS>
 __global__ __launch_bounds__(kAttThreads, DP == 64 ? 2 : 1) void k_att_dq(AttArgs a) {
@@ -291,22 +292,34 @@ __global__ __launch_bounds__(kAttThreads, DP == 64 ? 2 : 1) void k_att_dq(AttArg
 #pragma unroll
         for (int r = 0; r < 32; r++) size = fmaxf(size, __builtin_fabsf(s[r / 16][r % 16]));
         if (BIAS) look_at(kpos[lane]);
-        if (tiles_n == 1) {
-            // Few keys: their dy nearly cancel (one key's is 0), and what delta lacks would be most of it.  It is added up first.
+        if (tiles_n == 1 || least <= kFewSeen) {
+            // The dy of few keys nearly cancel (one key's is 0), and what delta lacks would be most of them.  It is added up first
+            // for the rows that see no keys behind this tile, in blocks that have some with few.
             float lack = 0.f;
             const Steps x = plain_steps<CAP>(a, 0.f);
+            auto add_up = [&](auto far) __attribute__((always_inline)) {
 #pragma unroll
-            for (int u = 0; u < 2; u++)
+                for (int j = 0; j < 8; j++) {
+                    const int at = 8 * j + 4 * half;
+                    const u32x4 p4 = BIAS ? *(const u32x4 *)(kpos + at) : u32x4{0, 0, 0, 0};
+                    float bias[4];
 #pragma unroll
-                for (int r = 0; r < 16; r++) {
-                    const int at = 32 * u + 8 * (r / 4) + 4 * half + r % 4;
-                    float y, slope;
-                    score_of<CAP>(a, x, true, s[u][r], y, slope);
-                    if (BIAS) y += float_at(place_of_key(places, kpos[at]));
-                    if (at < seen) lack = __builtin_fmaf(exp2_fast(y - lse), dp[u][r] - delta, lack);
-                    if (r % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+                    for (int e = 0; e < 4; e++) bias[e] = BIAS ? float_at(place_of_key(places, (int)p4[e])) : 0.f;
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        const int u = j / 4, r = 4 * (j % 4) + e;
+                        float y, slope;
+                        score_of<CAP>(a, x, decltype(far)::value, s[u][r], y, slope);
+                        y += bias[e] - lse;
+                        if (at + e < seen) lack = __builtin_fmaf(exp2_fast(y), dp[u][r] - delta, lack);
+                    }
+                    if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                 }
-            delta += halves_sum(lack);
+            };
+            if (CAP && wave_any(size > a.score.most)) add_up(std::true_type{});
+            else add_up(std::false_type{});
+            lack = halves_sum(lack);
+            if (seen <= kGradTile) delta += lack;
         }
         __syncthreads();
     }

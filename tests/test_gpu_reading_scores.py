@@ -1,10 +1,11 @@
-"""Scores that the attention's kernels take apart: biases that hide the first tiles of a row, caps of any size (bounds:
-reading_oracle)."""
+"""Scores that the attention's kernels take apart: biases that hide the first tiles of a row, caps of any size, rows whose few
+keys leave little of their gradient (bounds: reading_oracle)."""
 import math
 
 import pytest
 import torch
 
+import reading_oracle as oracle
 from test_gpu_reading import _check, _check_read, _inputs, _read
 
 pytestmark = pytest.mark.gpu
@@ -70,3 +71,20 @@ def test_read_under_any_cap(cap, dim):
     a = _read(44, torch.float16, [40, 0, 700], 2, 4, 2, dim, cap=cap)
     a["q"][0, 0] = 0
     _check_read(a)
+
+
+# ------------------------------------------------------------------------- rows with few keys among others
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+@pytest.mark.parametrize("rows, prefix", [(100, 0), (300, 0), (200, 2)])
+@pytest.mark.parametrize("heads, kv_heads, dim", [(4, 4, 64), (2, 2, 128), (4, 2, 64)])
+def test_gradients_of_the_first_rows_of_causal_text(heads, kv_heads, dim, rows, prefix, cap):
+    # row 0 sees one key: its dq is 0, and delta in 32 bits leaves 1e-5 of sums of `dim` products; the next rows see a few: the
+    # roundings of dz and of the result, 0.0017 of the norm each
+    a, dout = _inputs(45, torch.bfloat16, [rows], [rows], heads, kv_heads, dim, bias=True)
+    a |= dict(causal=True, cap=cap, prefix=torch.tensor([prefix], dtype=torch.int32))
+    got = _check(a, dout)
+    want = oracle.attention(**a, dout=dout)[0]["dq"]
+    if prefix == 0:
+        assert got["dq"][0].abs().max() < 2e-4
+    few = slice(1, 6)
+    assert (got["dq"][few].cpu().double() - want[few]).norm() < 0.0035 * want[few].norm()
