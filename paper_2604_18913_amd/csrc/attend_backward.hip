@@ -813,13 +813,17 @@ template <class E> __global__ __launch_bounds__(1024) void k_att_dbias(AttArgs a
     ((E *)a.dbias)[h * nb + b] = (E)sum;
 }
 
-// Ordered where the blocks of either kernel are more than the units and the documents more than a few, whose blocks come
-// most first by themselves and share caches.  Forward and backward of documents of uneven lengths, us without / with (16 / 4 heads
-// of 128, up to 700 tokens and 1,500 entities): 4 documents (176 blocks) 390 / 391, 8 (456) 618 / 567, 16 (840) 861 / 733, 64
-// (3,276) 2,837 / 2,681; text and entities attending to each other, 2,000: 4 (564) 739 / 743, 8 (1,104) 866 / 882, 16 (2,236) 1,373 /
-// 1,210; up to 400: 16 (188 blocks) 147 / 147, 32 (348) 207 / 179.
+// Ordered where the blocks of either kernel are more than the units, the documents more than a few, whose blocks come most
+// first by themselves and share caches, and most of them longer than a block: the order is made by one block per side, document by
+// document, and blocks that are all alike have none.  Forward and backward, us without / with:
+//   documents of uneven lengths (16 / 4 heads of 128, up to 700 tokens and 1,500 entities): 4 (176 blocks) 390 / 391, 8 (456)
+//   618 / 567, 16 (840) 861 / 733, 64 (3,276) 2,837 / 2,681; text and entities attending to each other, 2,000: 4 (564) 739 / 743,
+//   8 (1,104) 866 / 882, 16 (2,236) 1,373 / 1,210; up to 400: 16 (188 blocks) 147 / 147, 32 (348) 207 / 179
+//   1,024 documents by the blocks of both kernels to a document: 2.2 987 / 1,084, 3.0 1,349 / 1,304, 3.4 1,746 / 1,722, 5.3
+//   3,803 / 3,567; of 8 / 8 heads of 64: 2.2 780 / 934, 3.0 1,410 / 1,464, 3.7 1,906 / 1,922, 4.0 2,310 / 2,273, 5.7 4,344 / 4,252
 static bool ordered(const AttArgs &a) {
-    return a.num_docs >= 8 && a.num_rows && a.num_keys && (a.row_blocks > a.key_blocks ? a.row_blocks : a.key_blocks) * a.kv_heads > 256;
+    return a.num_docs >= 8 && a.num_rows && a.num_keys && 3 * (a.row_blocks + a.key_blocks) >= 10ll * a.num_docs &&
+           (a.row_blocks > a.key_blocks ? a.row_blocks : a.key_blocks) * a.kv_heads > 256;
 }
 static int64_t delta_bytes(const AttArgs &a) { return (a.num_rows * a.heads * 4 + 15) / 16 * 16; }
 static int64_t backward_bytes(const AttArgs &a) {

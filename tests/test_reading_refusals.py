@@ -1,4 +1,4 @@
-"""What the reading calls refuse before they touch a GPU, beside the list in test_reading_oracle (no GPU needed)."""
+"""What the reading calls refuse and ask for before they touch a GPU, beside the list in test_reading_oracle (no GPU needed)."""
 import ctypes
 
 import pytest
@@ -18,3 +18,11 @@ def test_row_strides_outside_their_range(name, stride):
     rc, text = _status("logoskg_attend_backward", a, grad)
     assert rc == 1 and "row stride" in text
     assert reading._load().logoskg_attend_backward_bytes(ctypes.addressof(a)) == -1
+
+
+@pytest.mark.parametrize("docs, rows, keys, ordered", [(100_000, 30, 70, False), (1024, 18, 78, False), (8, 500, 500, True), (1024, 120, 300, True), (7, 500, 500, False)])
+def test_blocks_are_ordered_where_documents_are_many_and_long(docs, rows, keys, ordered):
+    # the room for the order is what tells: a block is 128 rows or keys, and each document has one more than it fills
+    a = _attention(num_docs=docs, num_rows=docs * rows, num_keys=docs * keys, heads=32, kv_heads=32, q_row=2048, k_row=2048, v_row=2048)
+    blocks = (docs * rows >> 7) + (docs * keys >> 7) + 2 * docs
+    assert reading._load().logoskg_attend_backward_bytes(ctypes.addressof(a)) == docs * rows * 32 * 4 + (blocks * 4 if ordered else 0)
