@@ -119,8 +119,8 @@ def _score(scale, cap, bias, buckets, heads, dim, dtype, device):
         return scale, cap or 0.0, 0, 0, 0, 0
     if buckets is None or buckets.dim() != 1 or buckets.numel() % 2 != 1:
         raise ValueError("a bias needs buckets, one per distance -M .. M")
-    if bias.dim() != 2 or bias.shape[0] != heads:
-        raise ValueError("bias must be [heads, buckets]")
+    if bias.dim() != 2 or bias.shape[0] != heads or bias.shape[1] < 1:
+        raise ValueError("bias must be [heads, buckets], with a bucket at least")
     return (scale, cap or 0.0, _plain(bias, "bias", dtype, device), _plain(buckets, "buckets", _torch().int32, device),
             bias.shape[1], buckets.numel() // 2)
 

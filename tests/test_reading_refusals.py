@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 from paper_2604_18913_amd import reading
 from test_reading_oracle import _attention, _status
@@ -26,3 +27,10 @@ def test_blocks_are_ordered_where_documents_are_many_and_long(docs, rows, keys, 
     a = _attention(num_docs=docs, num_rows=docs * rows, num_keys=docs * keys, heads=32, kv_heads=32, q_row=2048, k_row=2048, v_row=2048)
     blocks = (docs * rows >> 7) + (docs * keys >> 7) + 2 * docs
     assert reading._load().logoskg_attend_backward_bytes(ctypes.addressof(a)) == docs * rows * 32 * 4 + (blocks * 4 if ordered else 0)
+
+
+def test_a_bias_without_buckets_is_refused():
+    # (its tensor has no memory, and no place is what the library takes for no bias)
+    with pytest.raises(ValueError, match="a bucket at least"):
+        reading._score(None, 0.0, torch.zeros(2, 0), torch.zeros(9, dtype=torch.int32), 2, 64, torch.float32, -1)
+    assert reading._score(None, 0.0, torch.zeros(2, 1), torch.zeros(9, dtype=torch.int32), 2, 64, torch.float32, -1)[4:] == (1, 4)
