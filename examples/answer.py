@@ -18,22 +18,6 @@ HEADS, KV_HEADS, DIM, TOKENS, HOPS, BUCKETS, FAR, CAP = 8, 2, 64, 6, 2, 12, 32, 
 TEXT_AT = HOPS + 1  # entities stand at their hop, the text behind them
 
 
-class Attend(torch.autograd.Function):
-    """``lkg.attend`` with ``lkg.attend_backward`` as its gradient."""
-
-    @staticmethod
-    def forward(ctx, q, k, v, bias, q_off, k_off, kw):
-        out, lse = lkg.attend(q, k, v, q_off, k_off, bias=bias, **kw)
-        ctx.save_for_backward(q, k, v, bias, out, lse, q_off, k_off)
-        ctx.kw = kw
-        return out
-
-    @staticmethod
-    def backward(ctx, dout):
-        q, k, v, bias, out, lse, q_off, k_off = ctx.saved_tensors
-        return (*lkg.attend_backward(dout.contiguous(), q, k, v, out, lse, q_off, k_off, bias=bias, **ctx.kw), None, None, None)
-
-
 def main(steps=40, questions=32):
     gen = torch.Generator().manual_seed(1)
     w = kggen.config1()
@@ -70,7 +54,7 @@ def main(steps=40, questions=32):
     def attention():
         read = torch.cat([table[entity.long()], words])[order]
         k, v = ((read @ m).view(-1, KV_HEADS, DIM).to(half) for m in (to_k, to_v))
-        return Attend.apply((words @ to_q).view(-1, HEADS, DIM).to(half), k, v, bias.to(half), q_off, k_off, kw)[last]
+        return lkg.attend((words @ to_q).view(-1, HEADS, DIM).to(half), k, v, q_off, k_off, bias=bias.to(half), **kw)[0][last]
 
     losses = []
     for _ in range(steps):

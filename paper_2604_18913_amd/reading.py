@@ -179,6 +179,34 @@ def _new(t):
     return _torch().empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
 
 
+@functools.lru_cache(None)
+def _differentiable():
+    torch = _torch()
+
+    class Attend(torch.autograd.Function):
+        """``attend`` for inputs that require gradients."""
+
+        @staticmethod
+        def forward(ctx, q, k, v, bias, q_off, k_off, kw):
+            out, lse = attend(q, k, v, q_off, k_off, bias=bias, **kw)
+            ctx.set_materialize_grads(False)
+            ctx.save_for_backward(q, k, v, bias, out, lse, q_off, k_off)
+            ctx.kw = kw
+            return out, lse
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, dout, dlse):
+            if dlse is not None:
+                raise RuntimeError("attend: lse has no gradient (parts that are joined by it cannot be trained)")
+            if dout is None:
+                return (None,) * 7
+            q, k, v, bias, out, lse, q_off, k_off = ctx.saved_tensors
+            return (*attend_backward(dout.contiguous(), q, k, v, out, lse, q_off, k_off, bias=bias, **ctx.kw), None, None, None)
+
+    return Attend
+
+
 @_on_stream
 def attend(q, k, v, q_off, k_off, *, scale=None, cap=0.0, causal=False, prefix=None, bias=None, buckets=None, q_pos=None,
            k_pos=None):
@@ -188,7 +216,13 @@ def attend(q, k, v, q_off, k_off, *, scale=None, cap=0.0, causal=False, prefix=N
     other at ``q_off`` / ``k_off`` (int64, on the device); rows that none holds get zeros and -inf.  ``causal``: row i of R sees the keys up to i + K - R, and
     the document's first ``prefix`` (int32, one per document) besides; else every row sees all keys.  ``cap``: scores
     become cap tanh(score / cap).  ``bias`` [heads, buckets] is learned, ``buckets`` (``distance_buckets``) says which
-    column the distance ``k_pos - q_pos`` reads (positions: int32, by default the places, aligned at the end)."""
+    column the distance ``k_pos - q_pos`` reads (positions: int32, by default the places, aligned at the end).
+
+    Where ``q``, ``k``, ``v`` or ``bias`` requires a gradient, ``out`` has one by ``attend_backward``; ``lse`` has none, and
+    asking for it raises."""
+    if (q.requires_grad or k.requires_grad or v.requires_grad or bias is not None and bias.requires_grad) and _torch().is_grad_enabled():
+        kw = dict(scale=scale, cap=cap, causal=causal, prefix=prefix, buckets=buckets, q_pos=q_pos, k_pos=k_pos)
+        return _differentiable().apply(q, k, v, bias, q_off, k_off, kw)
     out, lse = _new(q), q.new_empty(q.shape[:2], dtype=_torch().float32)
     _check(_load().logoskg_attend(_attention(q, k, v, q_off, k_off, scale, cap, causal, prefix, bias, buckets, q_pos, k_pos, out, lse, None)))
     return out, lse
@@ -218,7 +252,8 @@ def attend_backward(dout, q, k, v, out, lse, q_off, k_off, *, scale=None, cap=0.
 @_on_stream
 def read_entities(q, keys, values, off, entity=None, *, scale=None, cap=0.0, bias=None, buckets=None, hop=None, q_pos=None):
     """``logoskg_read_entities``: the tokens of every query attend to its entity list, as {"out": like q, "lse":
-    float32 [queries, tokens, heads]} (with its lse, the answer can be joined with attention over the text).
+    float32 [queries, tokens, heads]} (with its lse, the answer can be joined with attention over the text).  A serving call: it
+    has no gradient.
 
     ``q`` [queries, tokens, heads, dim]; ``keys`` / ``values`` [entities, kv_heads, dim] by entity; ``off`` (int64),
     ``entity`` (int32) and ``hop`` (uint8) as ``Result.offsets`` and ``Result.fetch`` give them, on the device.  An entity
@@ -271,7 +306,7 @@ def constrain_logits(logits, *, history=None, history_off=None, repetition=None,
     row's ``history`` penalised (``repetition`` divides or multiplies, ``presence`` and count times ``frequency`` are taken
     off; float32 per row), biases added, and every id whose bit of ``mask`` (``entity_mask``'s layout) is 0 at -infinity.
     Lists are ragged: ``history`` int32 at ``history_off``, ``bias_id`` int32 and ``bias_value`` float32 at ``bias_off``.
-    ``out`` may be ``logits``."""
+    ``out`` may be ``logits``.  A serving call: it has no gradient."""
     torch = _torch()
     if logits.dim() != 2:
         raise ValueError("logits must be [rows, vocab] with contiguous rows")
