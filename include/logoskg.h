@@ -489,7 +489,8 @@ typedef enum { LOGOSKG_F32 = 0, LOGOSKG_BF16 = 1, LOGOSKG_F16 = 2 } logoskg_dtyp
  *     u = cap tanh(z / cap)   (cap = 0: u = z)
  *     y = u + bias[head][buckets[clamp(k_pos - q_pos, -M, M) + M]],  M = max_distance
  * and the softmax over the visible keys' y.  bias has the type of q; NULL = none.
- * A bias of -inf (or below -6e14, as bfloat16's lowest value) hides its keys.
+ * A bias of -inf, or below -7e4 (which is meant to: beside it 32 bits do not hold
+ * the scores), hides its keys.
  */
 typedef struct {
     float scale, cap;

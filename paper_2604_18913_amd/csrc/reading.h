@@ -15,10 +15,11 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// A bias of -infinity, or so low that it can only be meant to hide (the type's lowest value in bfloat16), stands as kHidden: 2^this
-// is 0, and its square finite, where that of an infinity is not.  kLowest is the running maximum of a row that has seen nothing,
+// A bias of -infinity, or so low that it can only be meant to hide, stands as kHidden: 2^this is 0, and its square finite, where
+// that of an infinity is not.  Low is what is below kLeastBias (float16's lowest value is not, bfloat16's is): 32 bits hold scores to
+// 2^-8 beside that, and beside -1e9 not at all, so that p of a row that sees nothing else, made of y - lse, would be anything.  kLowest is the running maximum of a row that has seen nothing,
 // below any other score and above the hidden ones: those weigh 0 from the first tile on, and a sum of 0 tells that nothing was seen.
-constexpr float kHidden = -1e15f, kLowest = 0.5f * kHidden;
+constexpr float kHidden = -1e15f, kLowest = 0.5f * kHidden, kLeastBias = -7e4f * kLog2e;
 
 // The two 16-bit types: eight values as a matrix instruction takes them, and that instruction on 32 x 32 x 16.
 // Lane l holds A[l % 32][8 (l / 32) ..] and B[8 (l / 32) ..][l % 32]; C's element r is row 8 (r / 4) + 4 (l / 32) + r % 4
@@ -266,7 +267,7 @@ __device__ __forceinline__ int wave_max(int x) {
 template <class E> __device__ __forceinline__ void bias_to_lds(float *table, const ScoreArgs &s, int h0, int group, int tid, int threads) {
     const E *bias = (const E *)s.bias;
     int places = 2 * s.max_distance + 1;
-    auto lowest = [](float x) { return x < kHidden ? kHidden : x; };
+    auto lowest = [](float x) { return x < kLeastBias ? kHidden : x; };
     for (int i = tid; i < places; i += threads) {
         int b = s.buckets[i];
         b = b < 0 ? 0 : b >= s.num_buckets ? s.num_buckets - 1 : b;

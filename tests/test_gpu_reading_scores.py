@@ -5,8 +5,9 @@ import math
 import pytest
 import torch
 
+import paper_2604_18913_amd as lkg
 import reading_oracle as oracle
-from test_gpu_reading import _check, _check_read, _inputs, _read
+from test_gpu_reading import _attend, _check, _check_read, _gpu, _inputs, _read
 
 pytestmark = pytest.mark.gpu
 
@@ -49,6 +50,34 @@ def test_a_window_made_by_a_hiding_bucket(dtype, cap, heads, kv_heads):
     bias = torch.zeros(heads, 3, dtype=dtype)
     bias[:, 1], bias[:, 2] = 0.5, -math.inf
     _check({**a, "causal": True, "cap": cap, "bias": bias, "buckets": buckets}, dout)
+
+
+def _low(dtype, low, heads, kv_heads):
+    a, dout = _inputs(46, dtype, [70], [200], heads, kv_heads, 64, spread=1.5)
+    return {**a, "bias": torch.full((heads, 4), low, dtype=dtype), "buckets": torch.tensor([0, 1, 2, 3, 0], dtype=torch.int32)}, dout
+
+
+@pytest.mark.parametrize("heads, kv_heads", [(4, 2), (260, 260)])
+@pytest.mark.parametrize("low", [-7.2e4, -1e6, -1e9, -1e14, -6e14, -1e30, -math.inf])
+def test_rows_that_see_low_biases_alone(low, heads, kv_heads):
+    a, dout = _low(torch.bfloat16, low, heads, kv_heads)
+    got = _attend(a, dout)
+    assert all((got[n] == 0).all() for n in ("out", "dq", "dk", "dv", "dbias")) and (got["lse"] == -math.inf).all()
+    r = _read(46, torch.bfloat16, [300, 40], 1, heads, kv_heads, 64)
+    r["bias"][:] = low
+    got = lkg.read_entities(**{k: _gpu(x) for k, x in r.items()})
+    assert (got["out"] == 0).all() and (got["lse"] == -math.inf).all()
+
+
+@pytest.mark.parametrize("heads, kv_heads", [(4, 2), (260, 260)])
+@pytest.mark.parametrize("dtype, low", [(torch.float16, -65504.0), (torch.bfloat16, -65536.0)])
+def test_rows_that_see_the_least_biases_alone(dtype, low, heads, kv_heads):
+    # float16's lowest value is a number yet: beside 94,500 (in units of log 2) 32 bits hold scores to 2^-8, weights to 0.003, and
+    # lse to as much; with the roundings to 16 bits below a hundredth of the norm
+    a, dout = _low(dtype, low, heads, kv_heads)
+    got, (want, _) = _attend(a, dout), oracle.attention(**a, dout=dout)
+    for n in want:
+        assert (got[n].cpu().double() - want[n]).norm() < 0.01 * want[n].norm(), n
 
 
 # ------------------------------------------------------------------------- caps of any size
