@@ -164,7 +164,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend(AttArgs a) {
             } else {
 #pragma unroll
                 for (int u = 0; u < 2; u++)
-                    if (CAP) cap_scores<true>(a.score, s[u]);
+                    if (CAP) cap_scores<1>(a.score, s[u]);
 #pragma unroll
                 for (int u = 0; u < 2; u++)
 #pragma unroll
@@ -376,7 +376,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void k_attend_few(AttArgs a) {
         wave_sync();
         if (t + 4 < tiles_n) fetch(t + 4);
         const bool edge = (t + 1) * kFewKeys > least;
-        if (CAP) cap_scores<DP == 64>(a.score, s);
+        if (CAP) cap_scores<4>(a.score, s);
         float top = kLowest;
 #pragma unroll
         for (int j = 0; j < 4; j++) {

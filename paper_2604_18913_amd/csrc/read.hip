@@ -128,7 +128,7 @@ __global__ __launch_bounds__(256, 2) void k_read(ReadArgs a) {
         if (t + 4 < tiles_n) fetch(id);
         next_id = id_of(t + 8);
         if (BIAS) next_hop = hop_of(t + 8);
-        if (CAP) cap_scores<DP == 64>(a.score, s);
+        if (CAP) cap_scores<4>(a.score, s);
         float top = kLowest;
 #pragma unroll
         for (int r = 0; r < 16; r++) {

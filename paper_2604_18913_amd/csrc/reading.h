@@ -229,20 +229,31 @@ __device__ __forceinline__ float any_capped(const ScoreArgs &s, float z) {
     float share;
     return any_capped(s, z, share);
 }
-// Sixteen products of a wavefront's lanes to scores, in place; with ROOM in the registers for two ways, by the near form alone where
-// all of them are near, which is cheaper
-template <bool ROOM> __device__ __forceinline__ void cap_scores(const ScoreArgs &s, f32x16 &z) {
+// Sixteen products of a wavefront's lanes to scores, in place: by the near form, which is cheaper, where all of them are near.  PARTS
+// of them at a time: both forms of all sixteen take more registers than the kernels for few rows have; with four at a time 33 rows
+// before 5,000 keys (32 / 8 heads of 128) take 77 us, with both forms of each 85.
+template <int PARTS> __device__ __forceinline__ void cap_scores(const ScoreArgs &s, f32x16 &z) {
+    constexpr int N = 16 / PARTS;
     float size = 0.f;
-    if (ROOM) {
 #pragma unroll
-        for (int r = 0; r < 16; r++) size = fmaxf(size, __builtin_fabsf(z[r]));
-    }
-    if (!ROOM || wave_any(size > s.most)) {
+    for (int r = 0; r < 16; r++) size = fmaxf(size, __builtin_fabsf(z[r]));
+    const bool far = wave_any(size > s.most);
 #pragma unroll
-        for (int r = 0; r < 16; r++) z[r] = any_capped(s, z[r]);
-    } else {
+    for (int j = 0; j < PARTS; j++) {
+        float y[N];
+        if (PARTS == 1 && far) {
 #pragma unroll
-        for (int r = 0; r < 16; r++) z[r] = near_capped(s, z[r]);
+            for (int e = 0; e < N; e++) y[e] = any_capped(s, z[N * j + e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; e++) y[e] = near_capped(s, z[N * j + e]);
+        }
+        if (PARTS > 1 && far) {
+#pragma unroll
+            for (int e = 0; e < N; e++) y[e] = any_capped(s, z[N * j + e]);
+        }
+#pragma unroll
+        for (int e = 0; e < N; e++) z[N * j + e] = y[e];
     }
 }
 
