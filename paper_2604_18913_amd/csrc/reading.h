@@ -170,8 +170,8 @@ __device__ __forceinline__ int document_of(const int64_t *off, int n, long long 
 
 // ---------------------------------------------------------------- scores
 // What the kernels make of logoskg_score, in units of log 2.  Without a cap y = z k, k = scale log2 e.  With one
-// y = c - 2 c / (2^(z k) + 1), c = cap log2 e, which is c tanh(z scale / cap) for k = 2 log2 e scale / cap (2^.. may be
-// infinite or 0: +c or -c).  That form's error is c 2^-23 whatever y is, so it is for products above `most` alone, where tanh's
+// y = c - 2 c / (2^(z k) + 1), c = cap log2 e, which is c tanh(z scale / cap) for k = 2 log2 e scale / cap (with the sign of z k taken
+// off first and put back: 2^.. may be infinite, and is y = c then).  That form's error is c 2^-23 whatever y is, so it is for products above `most` alone, where tanh's
 // argument is 1/2 or more; up to there y = z times a polynomial in z^2 (near), exact to 5.5e-7 of y under any cap, which also
 // costs five instructions instead of an exponential, a reciprocal and three.
 struct ScoreArgs {
@@ -219,10 +219,12 @@ __device__ __forceinline__ float near_capped(const ScoreArgs &s, float z) {
     w = __builtin_fmaf(zz, w, s.near[0]);
     return z * w;
 }
-// .. of any; `share`: 1 / (2^(z k) + 1), of which the backward makes the slope
+// .. of any; `share`: 1 / (2^|z k| + 1), of which the backward makes the slope (of -z k it would be near 1, and 1 - share, which the
+// slope has as a factor, the rounding error of that)
 __device__ __forceinline__ float any_capped(const ScoreArgs &s, float z, float &share) {
-    share = rcp_fast(exp2_fast(z * s.k) + 1.f);
-    const float far = __builtin_fmaf(-2.f * s.c, share, s.c), near = near_capped(s, z);
+    const float zk = z * s.k;
+    share = rcp_fast(exp2_fast(__builtin_fabsf(zk)) + 1.f);
+    const float far = __builtin_copysignf(__builtin_fmaf(-2.f * s.c, share, s.c), zk), near = near_capped(s, z);
     return __builtin_fabsf(z) <= s.most ? near : far;
 }
 __device__ __forceinline__ float any_capped(const ScoreArgs &s, float z) {

@@ -7,7 +7,7 @@ import torch
 
 import paper_2604_18913_amd as lkg
 import reading_oracle as oracle
-from test_gpu_reading import _attend, _check, _check_read, _gpu, _inputs, _read
+from test_gpu_reading import HALVES, _attend, _check, _check_read, _gpu, _inputs, _read
 
 pytestmark = pytest.mark.gpu
 
@@ -92,6 +92,15 @@ def test_attention_under_any_cap(cap, heads, kv_heads, dim):
     a["q"][7], a["k"][11] = 0, 0
     _check({**a, "causal": True, "cap": cap}, dout)
     _check({**a, "causal": False, "cap": cap}, dout)
+
+
+@pytest.mark.parametrize("cap", [0.25, 0.5])
+@pytest.mark.parametrize("dtype", HALVES, ids=["bf16", "fp16"])
+@pytest.mark.parametrize("heads, kv_heads, dim, rows, keys", [(260, 260, 72, [5], [80]), (132, 132, 16, [1, 85, 3], [13, 473, 104]), (12, 3, 80, [33, 12, 50], [22, 67, 200]), (6, 3, 128, [196], [9])])
+def test_gradients_of_scores_near_their_cap(heads, kv_heads, dim, rows, keys, dtype, cap):
+    # slopes from 1 down to 1e-8 of the scale, of either sign of the score, each known to the roundings of its own size
+    a, dout = _inputs(47, dtype, rows, keys, heads, kv_heads, dim, bias=True)
+    _check({**a, "cap": cap}, dout)
 
 
 @pytest.mark.parametrize("dim", [64, 128])
