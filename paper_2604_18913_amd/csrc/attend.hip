@@ -16,7 +16,7 @@ namespace lkg {
 // is summed in 32 bits.  (The test takes b - m: against m + 8 it would lose the scores beside a bias of large size.)  Other tiles get their y - m first, with m the maximum again, which takes them twice as long.
 //
 // 4 documents of up to 8,192 rows and keys (32 / 8 heads of 128, bfloat16, cap, bias; two fifths of the pairs are between
-// entities, whose distances vary): 2,135 us, 680 TFLOP/s of the 1,370 that a product of 16,384^3 reaches here; text alone, whose
+// entities, whose distances vary): 2,130 us, 680 TFLOP/s of the 1,370 that a product of 16,384^3 reaches here; text alone, whose
 // tiles are plain, without a cap: 860.  By the counters the matrix units are busy for 36 % of the time (4 x 4,096 rows),
 // LDS banks collide for 2 %.  p is rounded to 16 bits as the matrix instruction takes it, the sum l is of the unrounded ones.
 //
@@ -473,10 +473,10 @@ logoskg_status attend_args(const logoskg_attention *a, AttArgs *o, const char *c
 }
 
 // Blocks of 128 rows x key heads up to which rows are few (k_attend / k_attend_few, us, with cap and bias and without):
-//   heads of 128   16 blocks: 33 rows before 300 entities 24.4 / 12.8 and 14.3 / 10.5, before 5,000 198 / 74 and 94 / 59
-//                  128: 500 rows before 300 entities 34 / 26 and 23.6 / 23.2, before 2,000 92 / 63 and 54 / 58
-//                  168: 16 documents of 24 rows before 1,000 48 / 31 and 26.0 / 28.7; 256: 1,000 rows before 2,000 98 / 119, 70 / 107
-//   heads of 64    192: 3,000 rows before 300 entities 74 / 61 and 49 / 42; 432: 32 documents of 200 rows 31 / 25 and 17.2 / 18.4
+//   heads of 128   16 blocks: 33 rows before 300 entities 24.4 / 13.5 and 14.7 / 10.5, before 5,000 204 / 77 and 98 / 60
+//                  128: 500 rows before 300 entities 34 / 27 and 23.7 / 23.1, before 2,000 94 / 62 and 54 / 57
+//                  168: 16 documents of 24 rows before 1,000 50 / 32 and 26.5 / 28.6; 256: 1,000 rows before 2,000 96 / 120, 66 / 106
+//   heads of 64    192: 3,000 rows before 300 entities 74 / 49 and 51 / 41; 432: 32 documents of 200 rows 31 / 23 and 17.2 / 18.5
 constexpr long long few_blocks_most(int DP) { return DP == 64 ? 256 : 128; }
 
 template <class E, int DP, bool CAP, bool BIAS> static logoskg_status launch_attend(const AttArgs &a, hipStream_t st) {

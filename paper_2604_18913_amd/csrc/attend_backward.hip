@@ -7,7 +7,8 @@
 // in return no sum depends on the order in which blocks arrive, and none is kept in memory in between.
 //
 // O comes in 16 bits, and dO . O carries its rounding: the first kernel, which begins with dO . O of its rows, adds up a row's
-// dy, which is what delta lacks, and leaves delta with it to the second (a bucket's sum of many dy would show it most).
+// dy, which is what delta lacks, and leaves delta with it to the second (a bucket's sum of many dy would show it most).  Its own dQ
+// has it where rows see few keys (kFewSeen); a row whose biases hide all but a few keys of several tiles is not told from others.
 // p and dz are rounded to the 16 bits that the matrix instructions take, sums are held in 32: dQ, dK and dV carry two
 // roundings, this one of every term and their own, sqrt 2 of what rounding the exact gradient alone gives (bfloat16: 0.0025 for
 // 0.0017 of the norm).  In float16 a dz below 2^-14 loses bits and one below 2^-25 all: losses are scaled, as that type asks.
@@ -101,8 +102,8 @@ template <bool CAP> __device__ __forceinline__ void score_of(const AttArgs &a, c
         slope = __builtin_fmaf(y * y, x.curve, x.slope);
     }
 }
-// What is special about a tile, each kind with its own elements: varied biases alone, hidden keys (or either where there are no
-// biases), products that are not near
+// What is special about a tile: varied biases alone, whose elements need no look at what a row sees; hidden keys; products that
+// are not near (in dK, dV kEdge takes these too, eight elements at a time, for want of registers).  Without biases one kind is for all.
 enum { kVaried, kEdge, kFar };
 constexpr float kHiddenLse = 1e15f;    // of a row that sees nothing, or is none: p = 0 the same way
 
@@ -440,7 +441,7 @@ __global__ __launch_bounds__(kAttThreads, DP == 64 ? 2 : 1) void k_att_dq(AttArg
 // columns are added up when its rows are through.
 //
 // dK, dV, K, V and the products fill both halves of the registers: one wavefront a unit, and what it waits for is its own
-// time.  The batch of k_att_dq: 1,130 us, 425 TFLOP/s of its four products; matrix units busy for 24 % of the time, vector units for
+// time.  The batch of k_att_dq: 1,145 us, 420 TFLOP/s of its four products; matrix units busy for 24 % of the time, vector units for
 // half, LDS for half.  It takes as long as the longest document's first key blocks, which see all 4,096 rows of four heads.
 template <class E, int DP, bool CAP, bool BIAS>
 __global__ __launch_bounds__(kAttThreads, 1) void k_att_dkdv(AttArgs a) {

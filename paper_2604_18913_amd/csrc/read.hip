@@ -27,7 +27,7 @@ constexpr int kReadLeastShift = 7;  // four wavefronts, a tile each
 // own piece of LDS, where they are read by columns; no wavefront waits for another.
 //
 // Memory bounds it: 64 lists of up to 20,000 entities of a table of 407,000 (8 key heads of 128, float16) 597 us, 4.5 TB/s of the
-// rows read, a copy's rate 4.85; 1,024 lists of up to 3,000 of 3 M (8 of 64, four tokens) 812 us, 3.9 TB/s: a key head's piece
+// rows read, a copy's rate 4.85; 1,024 lists of up to 3,000 of 3 M (8 of 64, four tokens) 820 us, 3.9 TB/s: a key head's piece
 // of a row is one line of 128 bytes.  One list of 900: 10 us and 4 for the join, both chains of loads.
 template <class E, int DP, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_read(ReadArgs a) {
