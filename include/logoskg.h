@@ -626,6 +626,159 @@ typedef struct {
  */
 logoskg_status logoskg_constrain_logits(const logoskg_logits *l);
 
+/* ------------------------------------------------- around the reading: rows of a table, training */
+
+/*
+ * Rows of a table by the ids of retrieved lists, for a model to read: row i of
+ * `out` is scale x row ids[i] of `table` in 32 bits, rounded once; zeros where
+ * ids[i] is outside [0, num_entities).
+ */
+typedef struct {
+    uint32_t struct_size;     /* sizeof(logoskg_embedding)                                   */
+    int32_t device;
+    int32_t dtype;            /* of table and out                                            */
+    float scale;
+    int64_t num_ids, num_entities, dim;
+    int64_t row;              /* stride of the table's rows, in elements: not negative       */
+    const int32_t *ids;       /* device int32[num_ids], any order, repeats and all           */
+    const void *table;        /* device, rows of dim consecutive elements                    */
+    void *out;                /* device [num_ids][dim]                                       */
+    void *stream;
+} logoskg_embedding;
+logoskg_status logoskg_embed_entities(const logoskg_embedding *e);
+
+/*
+ * Its gradient: row e of `dtable` is scale x the sum of the rows i of `dout` with
+ * ids[i] = e, in 32 bits and in an order that only the ids decide (the same inputs give
+ * the same bits), rounded once.  With `accumulate` it is added to what stands
+ * there, and rows that no id names are not touched; else those become zeros.
+ */
+typedef struct {
+    uint32_t struct_size;     /* sizeof(logoskg_embedding_grad)                              */
+    int32_t device;
+    int32_t dtype;            /* of dout                                                     */
+    int32_t table_dtype;      /* of dtable: dtype or LOGOSKG_F32                             */
+    float scale;
+    int32_t accumulate;
+    int64_t num_ids, num_entities, dim;  /* num_ids, num_entities below 2^31                 */
+    int64_t row;              /* stride of dtable's rows, in elements: dim at least          */
+    const int32_t *ids;       /* device int32[num_ids]                                       */
+    const void *dout;         /* device [num_ids][dim]                                       */
+    void *dtable;             /* device, rows of dim consecutive elements                    */
+    void *workspace;          /* device, logoskg_embed_entities_backward_bytes bytes, 16-byte aligned */
+    int64_t workspace_bytes;
+    void *stream;
+} logoskg_embedding_grad;
+int64_t logoskg_embed_entities_backward_bytes(const logoskg_embedding_grad *e);
+logoskg_status logoskg_embed_entities_backward(const logoskg_embedding_grad *e);
+
+/*
+ * The tokens of sampled answers, row by row of their logits.  With x = scale
+ * logits over the ids that the row's mask allows (what logoskg_constrain_logits
+ * held the samples to), t the row's target:
+ *     lse = log sum exp(x),   logp = x[t] - lse
+ * A target outside [0, vocab) pads: logp 0.  One that is hidden, or whose logit is -inf: logp -inf.
+ * The clipped policy loss, with r = exp(logp - old) and A the advantage:
+ *     l = -min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A) + kl (exp(ref - logp) - (ref - logp) - 1)
+ *     loss = sum of weight l over the rows that neither pad nor have a logp of -inf
+ *     dlogits[v] = dloss weight dl/dlogp scale ([v = t] - exp(x[v] - lse)),  0 for ids that the mask hides
+ * where dl/dlogp has the first term of l where r A is the smaller of the two or both are alike.
+ */
+typedef struct {
+    uint32_t struct_size;     /* sizeof(logoskg_policy)                                      */
+    int32_t device;
+    int32_t dtype;            /* of logits and dlogits                                       */
+    int32_t num_rows;
+    int64_t vocab;
+    int64_t row;              /* stride of the rows of logits, in elements                   */
+    const void *logits;       /* device                                                      */
+    const int32_t *target;    /* device int32[num_rows]                                      */
+    const uint64_t *mask;     /* device uint64[num_masks][ceil(vocab / 64)], as logoskg_entity_mask writes it; NULL: all allowed */
+    const int32_t *mask_row;  /* device int32[num_rows]: row i's mask (one outside [0, num_masks) allows nothing);
+                                 NULL: mask i, num_masks >= num_rows                         */
+    int64_t num_masks;
+    float scale;              /* 1 / temperature: above 0                                    */
+    float kl;                 /* not negative; 0: ref is not read and may be NULL            */
+    float clip_low, clip_high; /* not negative                                               */
+    const float *advantage;   /* device float[num_rows]                                      */
+    const float *old;         /* device float[num_rows]: logp of the policy that sampled; NULL: this one (r = 1) */
+    const float *ref;         /* device float[num_rows]: logp of the policy that is kept near */
+    const float *weight;      /* device float[num_rows]; NULL: 1 each                        */
+    float *logp, *lse;        /* device float[num_rows] each; lse is an input of the backward */
+    float *loss;              /* device float                                                */
+    void *dlogits;            /* device [num_rows][vocab]; logoskg_policy_loss: NULL, or the gradient for dloss = 1, in the
+                                 same pass (it may be `logits` where row = vocab)            */
+    const float *dloss;       /* device float: of the backward; NULL: 1                      */
+    void *workspace;          /* device, logoskg_policy_loss_bytes bytes, 16-byte aligned    */
+    int64_t workspace_bytes;
+    void *stream;
+} logoskg_policy;
+logoskg_status logoskg_token_logp(const logoskg_policy *p);      /* logp and lse alone */
+int64_t logoskg_policy_loss_bytes(const logoskg_policy *p);
+logoskg_status logoskg_policy_loss(const logoskg_policy *p);     /* loss, logp, lse and perhaps dlogits */
+logoskg_status logoskg_policy_loss_backward(const logoskg_policy *p); /* dlogits of lse */
+
+/*
+ * The norm of all gradients of a step together, and the gradients brought to it:
+ *     norm = |scale| sqrt(sum of grad^2),   out = grad scale min(1, max_norm / norm)
+ * summed in 64 bits, so that no size overflows, in a fixed order.  `out` may be
+ * `grad` (of the same type); otherwise no two arrays that are written, or one
+ * written and one read, may share memory.  A norm that is infinite gives zeros (NaN where the gradient is
+ * infinite), one that is NaN gives NaN; *norm tells.
+ */
+typedef struct {
+    const void *grad;         /* device                                                      */
+    void *out;                /* device                                                      */
+    int64_t n;                /* elements                                                    */
+    int32_t dtype, out_dtype;
+} logoskg_gradient;
+int64_t logoskg_clip_gradients_bytes(const logoskg_gradient *list, int64_t count);
+logoskg_status logoskg_clip_gradients(int32_t device, const logoskg_gradient *list, int64_t count, float max_norm, float scale,
+                                      float *norm, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------- around the reading: tables in 4 bits */
+
+/*
+ * Keys and values by entity, in 4 bits an element and a scale and base (bfloat16
+ * each) per head and group of 32 elements: value = base + scale x code.  With
+ * ng = ceil(dim / 32), a row of logoskg_packed_row_bytes bytes holds
+ *   - the keys' codes: per head 4 ng words of 32 bits; word c ng + g (c = 0 .. 3) holds the elements
+ *     32 g + 8 c .. + 7, four bits each from the lowest on;
+ *   - the values' codes: per head 4 ng words; word w holds the elements 8 w .. + 7;
+ *   - per head and group the keys' scale, the keys' base, the values' scale, the values' base;
+ * and zeros up to a multiple of 16 bytes.  Rows are rows: they may be copied, gathered and
+ * replaced one by one.
+ *
+ * base is the group's smallest element and scale a fifteenth of its range, rounded to bfloat16;
+ * code = (element - base) / scale, rounded to the nearest even, in 0 .. 15 (0 where scale is 0).  A group with an
+ * infinity or NaN, or a range above 32 bits, becomes NaN.
+ */
+int64_t logoskg_packed_row_bytes(int32_t kv_heads, int32_t dim);  /* 0 for sizes that are refused */
+
+typedef struct {
+    uint32_t struct_size;     /* sizeof(logoskg_pack)                                        */
+    int32_t device;
+    int32_t dtype;            /* of keys and values                                          */
+    int32_t kv_heads, dim;    /* dim: a multiple of 8, at most 128                           */
+    int32_t reserved;
+    int64_t num_rows;
+    void *keys, *values;      /* device, rows of kv_heads x dim: read by logoskg_pack_entities, written by
+                                 logoskg_unpack_entities                                     */
+    int64_t key_row, key_head, value_row, value_head; /* strides, in elements: not negative   */
+    void *packed;             /* device, 16-byte aligned                                     */
+    int64_t packed_row;       /* stride of its rows, in bytes: a multiple of 16              */
+    void *stream;
+} logoskg_pack;
+logoskg_status logoskg_pack_entities(const logoskg_pack *p);
+logoskg_status logoskg_unpack_entities(const logoskg_pack *p);
+
+/*
+ * logoskg_read_entities of a packed table: keys is the table, key_row the stride of its rows in
+ * bytes (a multiple of 16), and values, key_head, value_row and value_head are 0.
+ */
+int64_t logoskg_read_packed_bytes(const logoskg_entity_read *r);
+logoskg_status logoskg_read_packed(const logoskg_entity_read *r);
+
 const char *logoskg_last_error(void);
 const char *logoskg_version(void);
 

@@ -7,7 +7,10 @@ names.  PyTorch is used only for device buffers and the stream handle.
 from .binding import (Graph, Result, LogosKGError, logoskg_build, logoskg_khop, logoskg_paths,
                       library_path, version)
 from .reading import (attend, attend_backward, constrain_logits, distance_buckets, entity_mask, read_entities)
+from .packed import pack_entities, packed_row_bytes, read_packed, unpack_entities
+from .training import (clip_gradients, embed_entities, embed_entities_backward, policy_loss, policy_loss_backward, token_logp)
 
 __all__ = ["Graph", "Result", "LogosKGError", "logoskg_build", "logoskg_khop", "logoskg_paths",
            "library_path", "version", "attend", "attend_backward", "constrain_logits", "distance_buckets",
-           "entity_mask", "read_entities"]
+           "entity_mask", "read_entities", "pack_entities", "packed_row_bytes", "read_packed", "unpack_entities", "clip_gradients",
+           "embed_entities", "embed_entities_backward", "policy_loss", "policy_loss_backward", "token_logp"]

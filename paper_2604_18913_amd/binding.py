@@ -156,6 +156,19 @@ def _load():
     lib.logoskg_read_entities_bytes.argtypes = [P]
     lib.logoskg_entity_mask.argtypes = [I32, P, P, I64, I32, I64, P, P]
     lib.logoskg_constrain_logits.argtypes = [P]
+    for name in ("embed_entities", "embed_entities_backward", "token_logp", "policy_loss", "policy_loss_backward", "pack_entities",
+                 "unpack_entities", "read_packed"):
+        getattr(lib, "logoskg_" + name).restype = ctypes.c_int
+        getattr(lib, "logoskg_" + name).argtypes = [P]
+    for name in ("embed_entities_backward_bytes", "policy_loss_bytes", "read_packed_bytes"):
+        getattr(lib, "logoskg_" + name).restype = I64
+        getattr(lib, "logoskg_" + name).argtypes = [P]
+    lib.logoskg_packed_row_bytes.restype = I64
+    lib.logoskg_packed_row_bytes.argtypes = [I32, I32]
+    lib.logoskg_clip_gradients_bytes.restype = I64
+    lib.logoskg_clip_gradients_bytes.argtypes = [P, I64]
+    lib.logoskg_clip_gradients.restype = ctypes.c_int
+    lib.logoskg_clip_gradients.argtypes = [I32, P, I64, ctypes.c_float, ctypes.c_float, P, P, I64, P]
     lib.logoskg_last_error.restype = ctypes.c_char_p
     lib.logoskg_version.restype = ctypes.c_char_p
     _lib = lib

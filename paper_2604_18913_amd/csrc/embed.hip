@@ -1,0 +1,486 @@
+// Rows of a table by the ids of retrieved lists, and their gradient summed by entity (logoskg_embed_entities,
+// logoskg_embed_entities_backward).
+#include "training.h"
+
+namespace lkg {
+
+static_assert(sizeof(logoskg_embedding) == 80 && sizeof(logoskg_embedding_grad) == 104, "the ctypes binding mirrors these layouts");
+
+struct EmbedArgs {
+    long long num_ids, num_entities, dim, row;
+    float scale;
+    const int32_t *ids;
+    const void *table;
+    void *out;
+};
+
+constexpr int kEmbedRows = 4;  // of a group of lanes at a time
+
+// LG lanes move a row, 16 bytes each at a time; several rows of a group are in flight.
+template <class T, int LG> __global__ __launch_bounds__(256) void k_embed(EmbedArgs a) {
+    constexpr int V = 16 / sizeof(T);
+    const int lane = threadIdx.x % LG;
+    const long long first = ((long long)blockIdx.x * (256 / LG) + threadIdx.x / LG) * kEmbedRows;
+    if (first >= a.num_ids) return;
+    long long id[kEmbedRows];
+#pragma unroll
+    for (int r = 0; r < kEmbedRows; r++) id[r] = first + r < a.num_ids ? a.ids[first + r] : -1;
+    for (long long c = (long long)lane * V; c < a.dim; c += LG * V) {
+        const int count = a.dim - c < V ? (int)(a.dim - c) : V;
+        Some<T> x[kEmbedRows];
+#pragma unroll
+        for (int r = 0; r < kEmbedRows; r++) {
+            const bool in = id[r] >= 0 && id[r] < a.num_entities;
+            x[r] = in ? load_some<T>((const T *)a.table + id[r] * a.row + c, count) : Some<T>{};
+        }
+#pragma unroll
+        for (int r = 0; r < kEmbedRows; r++) {
+            if (first + r >= a.num_ids) continue;
+            const bool in = id[r] >= 0 && id[r] < a.num_entities;
+            Some<T> y;
+#pragma unroll
+            for (int e = 0; e < V; e++) y[e] = in ? (T)((float)x[r][e] * a.scale) : (T)0.f;
+            store_some<T>((T *)a.out + (first + r) * a.dim + c, y, count);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- gradient
+// The ids are sorted with their places (a stable radix sort, so that equal ids keep the order of the list); ids outside the
+// table become num_entities and come last.  Then every run of equal ids is a sum of rows of dout: chunks of the sorted
+// list are added up by groups of lanes, and runs that cross chunks are joined from the chunks' parts, in their order.
+struct GradArgs {
+    long long num_ids, num_entities, dim, row, chunks;
+    int accumulate, chunk, tiles, bits;
+    float scale;
+    const int32_t *ids;
+    const void *dout;
+    void *dtable;
+    unsigned *key[2], *place[2];  // of the sort: from one to the other and back
+    unsigned *count, *total;      // [digits][tiles], [digits]
+    float *part;                  // [chunks][2][dim]: of the run that comes in from the chunk before, and of the one that goes on
+};
+
+constexpr int kSortTile = 4096, kMostDigitBits = 11;
+
+__device__ __forceinline__ unsigned key_of(const GradArgs &a, long long i) {
+    const int id = a.ids[i];
+    return (unsigned)id < a.num_entities ? (unsigned)id : (unsigned)a.num_entities;
+}
+
+// Lanes of the wavefront that have this lane's digit.
+__device__ __forceinline__ unsigned long long alike(unsigned digit, int bits, bool in) {
+    unsigned long long m = __ballot(in);
+    for (int b = 0; b < bits; b++) {
+        const unsigned long long set = __ballot(digit >> b & 1);
+        m &= digit >> b & 1 ? set : ~set;
+    }
+    return m;
+}
+
+// Exclusive sums over a block's threads; `all`: the sum of all.  `box`: THREADS / 64 words of LDS.
+template <int THREADS> __device__ __forceinline__ unsigned block_before(unsigned x, unsigned *box, unsigned &all) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    unsigned y = x;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        const unsigned z = __shfl_up(y, s);
+        if (lane >= s) y += z;
+    }
+    __syncthreads();
+    if (lane == 63) box[wave] = y;
+    __syncthreads();
+    unsigned before = 0;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; w++) {
+        if (w == wave) before = all;
+        all += box[w];
+    }
+    return before + y - x;
+}
+
+// Lists of up to kSortTile ids: one block sorts them in LDS.
+__global__ __launch_bounds__(1024) void k_sort_few(GradArgs a) {
+    __shared__ unsigned key[2][kSortTile];
+    __shared__ unsigned short place[2][kSortTile];
+    __shared__ unsigned count[16][256], box[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = (int)a.num_ids, rounds = (n + 1023) / 1024;
+    for (int i = tid; i < n; i += 1024) key[0][i] = key_of(a, i), place[0][i] = (unsigned short)i;
+    int from = 0;
+    for (int shift = 0; shift < a.bits; shift += 8, from ^= 1) {
+        const int bits = a.bits - shift < 8 ? a.bits - shift : 8;
+        for (int i = tid; i < 16 * 256; i += 1024) ((unsigned *)count)[i] = 0;
+        __syncthreads();
+        unsigned rank[4], digit[4];
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+            if (r >= rounds) break;
+            const int i = wave * rounds * 64 + r * 64 + lane;
+            const bool in = i < n;
+            digit[r] = in ? key[from][i] >> shift & ((1u << bits) - 1) : 0;
+            const unsigned long long m = alike(digit[r], bits, in);
+            const unsigned long long below = m & ((1ull << lane) - 1);
+            if (in) rank[r] = count[wave][digit[r]] + __popcll(below);
+            wave_sync();
+            if (in && below == 0) count[wave][digit[r]] += __popcll(m);
+            wave_sync();
+        }
+        __syncthreads();
+        unsigned sum = 0, all;
+        if (tid < 256)
+            for (int w = 0; w < 16; w++) {
+                const unsigned c = count[w][tid];
+                count[w][tid] = sum;
+                sum += c;
+            }
+        const unsigned before = block_before<1024>(tid < 256 ? sum : 0, box, all);
+        if (tid < 256)
+            for (int w = 0; w < 16; w++) count[w][tid] += before;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+            if (r >= rounds) break;
+            const int i = wave * rounds * 64 + r * 64 + lane;
+            if (i >= n) continue;
+            const unsigned to = count[wave][digit[r]] + rank[r];
+            key[from ^ 1][to] = key[from][i];
+            place[from ^ 1][to] = place[from][i];
+        }
+        __syncthreads();
+    }
+    for (int i = tid; i < n; i += 1024) a.key[0][i] = key[from][i], a.place[0][i] = place[from][i];
+}
+
+// A pass of the sort over tiles: how often a digit occurs in each tile ..
+__global__ __launch_bounds__(256) void k_sort_count(GradArgs a, int pass, int shift, int bits) {
+    extern __shared__ unsigned found[];
+    const int tid = threadIdx.x, digits = 1 << bits;
+    for (int i = tid; i < digits; i += 256) found[i] = 0;
+    __syncthreads();
+    const long long from = (long long)blockIdx.x * kSortTile;
+    for (int i = tid; i < kSortTile; i += 256) {
+        if (from + i >= a.num_ids) break;
+        const unsigned key = pass == 0 ? key_of(a, from + i) : a.key[pass & 1][from + i];
+        atomicAdd(&found[key >> shift & (digits - 1)], 1u);
+    }
+    __syncthreads();
+    for (int i = tid; i < digits; i += 256) a.count[(long long)i * a.tiles + blockIdx.x] = found[i];
+}
+
+// .. how often before each tile, and in all (a block per digit) ..
+__global__ __launch_bounds__(256) void k_sort_before(GradArgs a) {
+    __shared__ unsigned box[4];
+    unsigned *count = a.count + (long long)blockIdx.x * a.tiles;
+    unsigned sum = 0;
+    for (int at = 0; at < a.tiles; at += 256) {
+        const int i = at + threadIdx.x;
+        unsigned all, x = i < a.tiles ? count[i] : 0;
+        const unsigned before = block_before<256>(x, box, all);
+        if (i < a.tiles) count[i] = sum + before;
+        sum += all;
+    }
+    if (threadIdx.x == 0) a.total[blockIdx.x] = sum;
+}
+
+// .. and every id to its place: behind the smaller digits, those of the tiles before, the wavefronts before and the lanes before.
+__global__ __launch_bounds__(256) void k_sort_move(GradArgs a, int pass, int shift, int bits) {
+    constexpr int kRounds = kSortTile / 256;
+    extern __shared__ unsigned count[];  // [4][digits]
+    __shared__ unsigned box[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, digits = 1 << bits;
+    unsigned *mine = count + wave * digits;
+    for (int i = tid; i < 4 * digits; i += 256) count[i] = 0;
+    __syncthreads();
+    const long long from = (long long)blockIdx.x * kSortTile + wave * (kSortTile / 4);
+    unsigned key[kRounds], rank[kRounds];
+#pragma unroll
+    for (int r = 0; r < kRounds; r++) {
+        const long long i = from + r * 64 + lane;
+        key[r] = i < a.num_ids ? pass == 0 ? key_of(a, i) : a.key[pass & 1][i] : 0;
+    }
+#pragma unroll
+    for (int r = 0; r < kRounds; r++) {
+        const bool in = from + r * 64 + lane < a.num_ids;
+        const unsigned digit = key[r] >> shift & (digits - 1);
+        const unsigned long long m = alike(digit, bits, in), below = m & ((1ull << lane) - 1);
+        rank[r] = mine[digit] + __popcll(below);
+        wave_sync();
+        if (in && below == 0) mine[digit] += __popcll(m);
+        wave_sync();
+    }
+    __syncthreads();
+    unsigned sum = 0;  // of the digits before this round's
+    for (int d0 = 0; d0 < digits; d0 += 256) {
+        const int d = d0 + tid;
+        unsigned all;
+        const unsigned before = block_before<256>(d < digits ? a.total[d] : 0, box, all);
+        if (d < digits) {
+            unsigned at = sum + before + a.count[(long long)d * a.tiles + blockIdx.x];
+            for (int w = 0; w < 4; w++) {
+                const unsigned c = count[w * digits + d];
+                count[w * digits + d] = at;
+                at += c;
+            }
+        }
+        sum += all;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kRounds; r++) {
+        const long long i = from + r * 64 + lane;
+        if (i >= a.num_ids) continue;
+        const unsigned to = mine[key[r] >> shift & (digits - 1)] + rank[r];
+        a.key[~pass & 1][to] = key[r];
+        a.place[~pass & 1][to] = pass == 0 ? (unsigned)i : a.place[pass & 1][i];
+    }
+}
+
+template <class O> __global__ __launch_bounds__(256) void k_clear_rows(GradArgs a) {
+    constexpr int V = 16 / sizeof(O);
+    const long long per = (a.dim + V - 1) / V, all = per * a.num_entities;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
+        const long long e = i / per, c = i % per * V;
+        store_some<O>((O *)a.dtable + e * a.row + c, Some<O>{}, a.dim - c < V ? (int)(a.dim - c) : V);
+    }
+}
+
+template <class O, int V> __device__ __forceinline__ void write_sum(const GradArgs &a, unsigned id, long long c, int count, const float (&x)[V]) {
+    O *to = (O *)a.dtable + (long long)id * a.row + c;
+    for (int e = 0; e < V; e++) {
+        if (e >= count) break;
+        const float y = x[e] * a.scale;
+        to[e] = (O)(a.accumulate ? (float)to[e] + y : y);
+    }
+}
+
+// A group of LG lanes adds up a chunk of the sorted list, each lane 16 bytes of a row; blockIdx.y: further columns.
+template <class T, class O, int LG> __global__ __launch_bounds__(256) void k_embed_sum(GradArgs a) {
+    constexpr int V = 16 / sizeof(T), kAhead = 4;
+    const long long g = (long long)blockIdx.x * (256 / LG) + threadIdx.x / LG, c = ((long long)blockIdx.y * LG + threadIdx.x % LG) * V;
+    if (g >= a.chunks || c >= a.dim) return;
+    const int count = a.dim - c < V ? (int)(a.dim - c) : V;
+    const long long from = g * a.chunk, to = from + a.chunk < a.num_ids ? from + a.chunk : a.num_ids;
+    const unsigned none = (unsigned)a.num_entities;
+    const unsigned *key = a.key[0], *place = a.place[0];
+    unsigned id = key[from];
+    if (id >= none) return;
+    const unsigned before = from > 0 ? key[from - 1] : none, behind = to < a.num_ids ? key[to] : none;
+    bool came = before == id;  // the run began before this chunk
+    float sum[V];
+    for (int e = 0; e < V; e++) sum[e] = 0.f;
+    float *part = a.part + g * 2 * a.dim + c;
+    for (long long i = from; i < to; i += kAhead) {
+        unsigned k[kAhead];
+        Some<T> x[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) {
+            k[u] = i + u < to ? key[i + u] : none;
+            if (k[u] < none) x[u] = load_some<T>((const T *)a.dout + place[i + u] * a.dim + c, count);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) {
+            if (k[u] >= none) continue;
+            if (k[u] != id) {
+                if (came) {
+                    for (int e = 0; e < count; e++) part[e] = sum[e];
+                } else {
+                    write_sum<O, V>(a, id, c, count, sum);
+                }
+                for (int e = 0; e < V; e++) sum[e] = 0.f;
+                came = false;
+                id = k[u];
+            }
+#pragma unroll
+            for (int e = 0; e < V; e++) sum[e] += (float)x[u][e];
+        }
+    }
+    const bool goes_on = behind == id;
+    if (came || goes_on) {
+        if (!came) part += a.dim;
+        for (int e = 0; e < count; e++) part[e] = sum[e];
+    } else {
+        write_sum<O, V>(a, id, c, count, sum);
+    }
+}
+
+// Runs that cross chunks: the block of the chunk that one begins in adds up its parts, 16 groups of 16 lanes a share each.
+template <class O> __global__ __launch_bounds__(256) void k_embed_join(GradArgs a) {
+    constexpr int V = 4, LG = 16, kGroups = 16;
+    __shared__ float box[kGroups][LG * V];
+    const long long g = blockIdx.x, last = (g + 1) * a.chunk - 1;
+    if (last + 1 >= a.num_ids) return;
+    const unsigned *key = a.key[0];
+    const unsigned id = key[last];
+    if (id >= a.num_entities || key[last + 1] != id) return;
+    if (key[g * a.chunk] == id && g > 0 && key[g * a.chunk - 1] == id) return;  // came in
+    long long lo = g + 1, hi = a.chunks;  // the last chunk that begins with the run: lo .. hi - 1
+    while (hi - lo > 1) {
+        const long long mid = (lo + hi) / 2;
+        if (key[mid * a.chunk] == id) lo = mid;
+        else hi = mid;
+    }
+    const long long parts = lo - g + 1;  // the first is this chunk's second
+    const int lane = threadIdx.x % LG, group = threadIdx.x / LG;
+    const long long c = ((long long)blockIdx.y * LG + lane) * V, share = (parts + kGroups - 1) / kGroups;
+    const int count = c >= a.dim ? 0 : a.dim - c < V ? (int)(a.dim - c) : V;
+    float sum[V] = {0.f, 0.f, 0.f, 0.f};
+    if (count > 0)
+        for (long long p = group * share; p < parts && p < (group + 1) * share; p++) {
+            const Some<float> x = load_some<float>(a.part + ((g + p) * 2 + (p == 0)) * a.dim + c, count);
+#pragma unroll
+            for (int e = 0; e < V; e++) sum[e] += x[e];
+        }
+    for (int e = 0; e < V; e++) box[group][lane * V + e] = sum[e];
+    __syncthreads();
+    if (group > 0 || count == 0) return;
+    const int used = parts < kGroups ? (int)parts : kGroups;
+    for (int i = 1; i < used; i++)
+        for (int e = 0; e < V; e++) sum[e] += box[i][lane * V + e];
+    write_sum<O, V>(a, id, c, count, sum);
+}
+
+static const char *bad_type(int dtype) { return dtype < LOGOSKG_F32 || dtype > LOGOSKG_F16 ? "unknown type" : nullptr; }
+
+template <class T> static logoskg_status launch_embed(const EmbedArgs &a, hipStream_t st) {
+    const long long chunks = (a.dim * (long long)sizeof(T) + 15) / 16;
+    const int LG = chunks <= 4 ? 4 : chunks <= 16 ? 16 : 64;
+    const long long per = 256 / LG * kEmbedRows, blocks = (a.num_ids + per - 1) / per;
+    if (blocks >= (1ll << 31)) { set_error("logoskg_embed_entities: too many ids"); return LOGOSKG_EINVAL; }
+    if (LG == 4) k_embed<T, 4><<<dim3((unsigned)blocks), 256, 0, st>>>(a);
+    else if (LG == 16) k_embed<T, 16><<<dim3((unsigned)blocks), 256, 0, st>>>(a);
+    else k_embed<T, 64><<<dim3((unsigned)blocks), 256, 0, st>>>(a);
+    LKG_HIP(hipGetLastError());
+    return LOGOSKG_OK;
+}
+
+static long long up(long long x) { return (x + 255) / 256 * 256; }
+
+// Sizes of the sort and places in the workspace; its size.
+static long long plan_grad(GradArgs &a, char *w) {
+    a.bits = 1;
+    while (a.num_entities >> a.bits) a.bits++;  // (num_entities itself is a key)
+    a.tiles = (int)((a.num_ids + kSortTile - 1) / kSortTile);
+    a.chunk = a.num_ids < 65536 ? 8 : 32;
+    a.chunks = (a.num_ids + a.chunk - 1) / a.chunk;
+    long long at = 0;
+    auto take = [&](long long bytes) {
+        char *p = w + at;
+        at += up(bytes);
+        return p;
+    };
+    const bool few = a.num_ids <= kSortTile;
+    for (int i = 0; i < 2; i++) {
+        a.key[i] = (unsigned *)take(few && i ? 0 : a.num_ids * 4);
+        a.place[i] = (unsigned *)take(few && i ? 0 : a.num_ids * 4);
+    }
+    a.count = (unsigned *)take(few ? 0 : ((long long)a.tiles << kMostDigitBits) * 4);
+    a.total = (unsigned *)take(few ? 0 : 4 << kMostDigitBits);
+    a.part = (float *)take(a.chunks * 2 * a.dim * 4);
+    return at;
+}
+
+static const char *grad_args(const logoskg_embedding_grad *e, GradArgs *a) {
+    if (!e || e->struct_size != sizeof(logoskg_embedding_grad)) return "struct_size";
+    if (bad_type(e->dtype)) return "unknown type";
+    if (e->table_dtype != e->dtype && e->table_dtype != LOGOSKG_F32) return "dtable is neither of dout's type nor float32";
+    if (!(e->scale - e->scale == 0.f)) return "scale is not finite";
+    if (e->num_ids < 0 || e->num_ids >= (1ll << 31) || e->num_entities < 0 || e->num_entities >= (1ll << 31) - 1 || e->dim < 0 || e->dim > (1ll << 24)) return "a count is out of range";
+    if (e->row < e->dim && e->num_entities > 1) return "rows overlap";
+    if (e->num_ids && e->dim && (!e->ids || !e->dout)) return "ids or dout is NULL";
+    if (e->num_entities && e->dim && !e->dtable) return "dtable is NULL";
+    if ((uintptr_t)e->workspace & 15) return "the workspace is not 16-byte aligned";
+    memset(a, 0, sizeof *a);
+    a->num_ids = e->num_ids; a->num_entities = e->num_entities; a->dim = e->dim; a->row = e->row;
+    a->accumulate = e->accumulate != 0; a->scale = e->scale;
+    a->ids = e->ids; a->dout = e->dout; a->dtable = e->dtable;
+    return nullptr;
+}
+
+template <class T, class O> static logoskg_status launch_grad(GradArgs &a, hipStream_t st) {
+    if (!a.accumulate) {
+        const long long all = (a.dim * (long long)sizeof(O) + 15) / 16 * a.num_entities, blocks = (all + 255) / 256;
+        k_clear_rows<O><<<dim3((unsigned)(blocks > 8192 ? 8192 : blocks)), 256, 0, st>>>(a);
+        LKG_HIP(hipGetLastError());
+    }
+    if (a.num_ids == 0) return LOGOSKG_OK;
+    if (a.num_ids <= kSortTile) {
+        k_sort_few<<<1, 1024, 0, st>>>(a);
+        LKG_HIP(hipGetLastError());
+    } else {
+        const int passes = (a.bits + kMostDigitBits - 1) / kMostDigitBits;
+        for (int pass = 0, shift = 0; pass < passes; pass++) {
+            const int bits = (a.bits - shift + passes - pass - 1) / (passes - pass);
+            k_sort_count<<<dim3(a.tiles), 256, 4 << bits, st>>>(a, pass, shift, bits);
+            LKG_HIP(hipGetLastError());
+            k_sort_before<<<dim3(1 << bits), 256, 0, st>>>(a);
+            LKG_HIP(hipGetLastError());
+            k_sort_move<<<dim3(a.tiles), 256, 16 << bits, st>>>(a, pass, shift, bits);
+            LKG_HIP(hipGetLastError());
+            shift += bits;
+        }
+        if (passes & 1) a.key[0] = a.key[1], a.place[0] = a.place[1];
+    }
+    const long long lanes = (a.dim * (long long)sizeof(T) + 15) / 16;
+    const int LG = lanes <= 4 ? 4 : lanes <= 16 ? 16 : 64;
+    const dim3 grid((unsigned)((a.chunks + 256 / LG - 1) / (256 / LG)), (unsigned)((lanes + LG - 1) / LG));
+    const dim3 join((unsigned)a.chunks, (unsigned)((a.dim + 63) / 64));
+    if (grid.y > 65535 || join.y > 65535) { set_error("logoskg_embed_entities_backward: rows of %lld elements", a.dim); return LOGOSKG_EINVAL; }
+    if (LG == 4) k_embed_sum<T, O, 4><<<grid, 256, 0, st>>>(a);
+    else if (LG == 16) k_embed_sum<T, O, 16><<<grid, 256, 0, st>>>(a);
+    else k_embed_sum<T, O, 64><<<grid, 256, 0, st>>>(a);
+    LKG_HIP(hipGetLastError());
+    if (a.chunks > 1) {
+        k_embed_join<O><<<join, 256, 0, st>>>(a);
+        LKG_HIP(hipGetLastError());
+    }
+    return LOGOSKG_OK;
+}
+
+}  // namespace lkg
+
+using namespace lkg;
+
+extern "C" logoskg_status logoskg_embed_entities(const logoskg_embedding *e) {
+    const char *why = nullptr;
+    if (!e || e->struct_size != sizeof(logoskg_embedding)) why = "struct_size";
+    else if (bad_type(e->dtype)) why = "unknown type";
+    else if (!(e->scale - e->scale == 0.f)) why = "scale is not finite";
+    else if (e->num_ids < 0 || e->num_ids >= (1ll << 40) || e->num_entities < 0 || e->dim < 0 || e->dim > (1ll << 24) || e->row < 0 || e->row > (1ll << 40)) why = "a count is out of range";
+    else if (e->num_ids && e->dim && (!e->ids || !e->out)) why = "ids or out is NULL";
+    else if (e->num_ids && e->dim && e->num_entities && !e->table) why = "table is NULL";
+    if (why) { set_error("logoskg_embed_entities: %s", why); return LOGOSKG_EINVAL; }
+    if (e->num_ids == 0 || e->dim == 0) return LOGOSKG_OK;
+    const EmbedArgs a = {e->num_ids, e->num_entities, e->dim, e->row, e->scale, e->ids, e->table, e->out};
+    OnDevice on;
+    LKG_TRY(on.go(e->device));
+    hipStream_t st = (hipStream_t)e->stream;
+    if (e->dtype == LOGOSKG_F32) return launch_embed<float>(a, st);
+    return e->dtype == LOGOSKG_BF16 ? launch_embed<bf16>(a, st) : launch_embed<fp16>(a, st);
+}
+
+extern "C" int64_t logoskg_embed_entities_backward_bytes(const logoskg_embedding_grad *e) {
+    GradArgs a;
+    if (const char *why = grad_args(e, &a)) { set_error("logoskg_embed_entities_backward_bytes: %s", why); return -1; }
+    return a.num_ids && a.dim && a.num_entities ? plan_grad(a, nullptr) : 0;
+}
+
+extern "C" logoskg_status logoskg_embed_entities_backward(const logoskg_embedding_grad *e) {
+    GradArgs a;
+    if (const char *why = grad_args(e, &a)) { set_error("logoskg_embed_entities_backward: %s", why); return LOGOSKG_EINVAL; }
+    if (a.dim == 0 || a.num_entities == 0) return LOGOSKG_OK;
+    if (a.num_ids) {
+        const long long need = plan_grad(a, (char *)e->workspace);
+        if (e->workspace_bytes < need || !e->workspace) {
+            set_error("logoskg_embed_entities_backward: the workspace has %lld of %lld bytes", (long long)e->workspace_bytes, need);
+            return LOGOSKG_ERANGE;
+        }
+    }
+    OnDevice on;
+    LKG_TRY(on.go(e->device));
+    hipStream_t st = (hipStream_t)e->stream;
+    const bool wide = e->table_dtype == LOGOSKG_F32;
+    if (e->dtype == LOGOSKG_F32) return launch_grad<float, float>(a, st);
+    if (e->dtype == LOGOSKG_BF16) return wide ? launch_grad<bf16, float>(a, st) : launch_grad<bf16, bf16>(a, st);
+    return wide ? launch_grad<fp16, float>(a, st) : launch_grad<fp16, fp16>(a, st);
+}

@@ -1,0 +1,550 @@
+// Keys and values by entity in 4 bits: into that form and back, and few tokens of every query attending to a list of such rows
+// (logoskg_pack_entities, logoskg_unpack_entities, logoskg_read_packed).
+#include "read.h"
+#include "training.h"
+
+namespace lkg {
+
+static_assert(sizeof(logoskg_pack) == 104, "the ctypes binding mirrors this layout");
+
+typedef unsigned long long u64;
+
+// ---------------------------------------------------------------- rows
+struct PackArgs {
+    int kv_heads, dim, groups, pad;  // groups: of a head; pad: bytes behind the last group
+    long long num_rows;
+    void *keys, *values;
+    long long key_row, key_head, value_row, value_head;
+    char *packed;
+    long long packed_row;
+};
+
+__host__ __device__ __forceinline__ int row_bytes_of(int kv_heads, int groups) { return (40 * kv_heads * groups + 15) / 16 * 16; }
+
+template <class T> struct Eight { typedef T type __attribute__((ext_vector_type(8), aligned(sizeof(T)))); };
+
+// Four lanes' codes of a group of 32 elements, eight each (x: those of this lane, `in`: whether there are any), and its scale and base.
+struct Codes { unsigned word, scale_base; };
+__device__ __forceinline__ Codes codes_of(const float (&x)[8], bool in) {
+    float lo = INFINITY, hi = -INFINITY, odd = 0.f;
+    if (in) {
+#pragma unroll
+        for (int e = 0; e < 8; e++) lo = fminf(lo, x[e]), hi = fmaxf(hi, x[e]), odd += x[e] - x[e];
+    }
+#pragma unroll
+    for (int d = 1; d < 4; d <<= 1) lo = fminf(lo, __shfl_xor(lo, d)), hi = fmaxf(hi, __shfl_xor(hi, d)), odd += __shfl_xor(odd, d);
+    // both rounded to the nearest bfloat16: 2^-9 of the base and of the range, a 30th of a step's half
+    const bf16 scale = (bf16)((hi - lo) / 15.f), base = (bf16)lo;
+    const float s = (float)scale, b = (float)base;
+    Codes got = {0, (unsigned)__builtin_bit_cast(unsigned short, scale) | (unsigned)__builtin_bit_cast(unsigned short, base) << 16};
+    if (!(odd + (s - s) + (b - b) == 0.f)) {
+        got.scale_base = 0x7fc07fc0u;  // NaN
+        return got;
+    }
+    if (in && s > 0.f) {
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const float c = __builtin_rintf((x[e] - b) / s);
+            got.word |= (unsigned)fminf(fmaxf(c, 0.f), 15.f) << (4 * e);
+        }
+    }
+    return got;
+}
+
+// Four lanes per group of 32 elements of a head of a row: its keys, then its values.
+template <class T> __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
+    const long long items = a.num_rows * a.kv_heads * a.groups;
+    const int c = threadIdx.x & 3;
+    for (long long i = (long long)blockIdx.x * 64 + threadIdx.x / 4; i < items; i += (long long)gridDim.x * 64) {
+        const int g = (int)(i % a.groups);
+        const long long rh = i / a.groups;
+        const int h = (int)(rh % a.kv_heads);
+        const long long r = rh / a.kv_heads;
+        const int at = 32 * g + 8 * c;
+        const bool in = at < a.dim;
+        typename Eight<T>::type k = {}, v = {};
+        if (in) {
+            k = *(const typename Eight<T>::type *)((const T *)a.keys + r * a.key_row + h * a.key_head + at);
+            v = *(const typename Eight<T>::type *)((const T *)a.values + r * a.value_row + h * a.value_head + at);
+        }
+        float x[8], y[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) x[e] = (float)k[e], y[e] = (float)v[e];
+        const Codes kc = codes_of(x, in), vc = codes_of(y, in);
+        char *row = a.packed + r * a.packed_row;
+        const int all = a.kv_heads * a.groups;
+        ((unsigned *)row)[h * 4 * a.groups + c * a.groups + g] = kc.word;
+        ((unsigned *)row)[4 * all + (h * a.groups + g) * 4 + c] = vc.word;
+        if (c < 2) ((unsigned *)row)[8 * all + (h * a.groups + g) * 2 + c] = c == 0 ? kc.scale_base : vc.scale_base;
+        if (a.pad && c < 2 && h == a.kv_heads - 1 && g == a.groups - 1) ((unsigned *)row)[10 * all + c] = 0;
+    }
+}
+
+__device__ __forceinline__ float low_half(unsigned x) { return __builtin_bit_cast(float, x << 16); }         // a bfloat16 in 32 bits
+__device__ __forceinline__ float high_half(unsigned x) { return __builtin_bit_cast(float, x & 0xffff0000u); }
+
+template <class T> __global__ __launch_bounds__(256) void k_unpack(PackArgs a) {
+    const long long items = a.num_rows * a.kv_heads * a.groups;
+    const int c = threadIdx.x & 3;
+    for (long long i = (long long)blockIdx.x * 64 + threadIdx.x / 4; i < items; i += (long long)gridDim.x * 64) {
+        const int g = (int)(i % a.groups);
+        const long long rh = i / a.groups;
+        const int h = (int)(rh % a.kv_heads);
+        const long long r = rh / a.kv_heads;
+        const int at = 32 * g + 8 * c, all = a.kv_heads * a.groups;
+        if (at >= a.dim) continue;
+        const unsigned *row = (const unsigned *)(a.packed + r * a.packed_row);
+        const unsigned kw = row[h * 4 * a.groups + c * a.groups + g], vw = row[4 * all + (h * a.groups + g) * 4 + c];
+        const unsigned kp = row[8 * all + (h * a.groups + g) * 2], vp = row[8 * all + (h * a.groups + g) * 2 + 1];
+        typename Eight<T>::type k, v;
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            k[e] = (T)__builtin_fmaf(low_half(kp), (float)(kw >> (4 * e) & 15), high_half(kp));
+            v[e] = (T)__builtin_fmaf(low_half(vp), (float)(vw >> (4 * e) & 15), high_half(vp));
+        }
+        *(typename Eight<T>::type *)((T *)a.keys + r * a.key_row + h * a.key_head + at) = k;
+        *(typename Eight<T>::type *)((T *)a.values + r * a.value_row + h * a.value_head + at) = v;
+    }
+}
+
+// ---------------------------------------------------------------- attention
+__device__ __forceinline__ f32x4 mfma16(Vec8<bf16>::type a, Vec8<bf16>::type b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mfma16(Vec8<fp16>::type a, Vec8<fp16>::type b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// Eight codes c of a word as 16 + c in 16 bits: a code's four bits become the highest of the mantissa of 16.  Codes 0 and 4,
+// 1 and 5, .. stand side by side.
+template <class E> __device__ __forceinline__ typename Vec8<E>::type codes8(unsigned w);
+template <> __device__ __forceinline__ Vec8<bf16>::type codes8<bf16>(unsigned w) {
+    const unsigned m = 0x00780078u, one = 0x41804180u;
+    return as8<bf16>(u32x4{(w << 3 & m) | one, (w >> 1 & m) | one, (w >> 5 & m) | one, (w >> 9 & m) | one});
+}
+template <> __device__ __forceinline__ Vec8<fp16>::type codes8<fp16>(unsigned w) {
+    const unsigned m = 0x03c003c0u, one = 0x4c004c00u;
+    return as8<fp16>(u32x4{(w << 6 & m) | one, (w << 2 & m) | one, (w >> 2 & m) | one, (w >> 6 & m) | one});
+}
+
+__device__ __forceinline__ float quarters_max(float x) { x = fmaxf(x, __shfl_xor(x, 16)); return fmaxf(x, __shfl_xor(x, 32)); }
+__device__ __forceinline__ float quarters_sum(float x) { x += __shfl_xor(x, 16); return x + __shfl_xor(x, 32); }
+
+struct PackedArgs {
+    ReadArgs r;
+    long long row_bytes;              // stride
+    int heads_in, rows_in, streams;   // of a block: key heads, groups of 16 rows, wavefronts that share a head's tiles
+    int row_groups;
+    int table_words;                  // of biases, per key head
+};
+
+constexpr int kPackedTile = 64;  // entries of a wavefront at a time
+
+// Bytes of a wavefront's piece of LDS: values' codes, scales and bases, ids and places of biases.
+constexpr int piece_bytes(int groups) { return kPackedTile * (16 * groups + 16 * groups + 4); }
+
+// One block: 2^shift entries of a list, some key heads and groups of 16 rows (token, head of the group); a wavefront has one
+// of each, and every so manieth tile of 64 entries.  With x = base + scale c (a group of 32 elements),
+//     q.k = sum over groups of scale (q . c) + base (sum of q),      out = sum of (p scale) c + p base :
+// the matrix instructions take the codes as they are, as 16 + c (see codes8), and the scales stay in 32 bits: those of the keys
+// are factors of a group's product, those of the values go into the weights, which are rounded to 16 bits for the second product
+// (as p itself is elsewhere).  16 + c would let that rounding weigh as much as the code is large: a third product, of the weights
+// and -23.5, makes it c - 7.5, and 7.5 scale goes to the base.
+//
+// Keys go from memory into the registers that the instruction reads; values' codes lie in LDS as they come, and the transposing
+// 4-bit read gives a lane one element of 16 entries.  Tile row p = 16 a + 4 b + c holds entry 16 b + 4 a + c, so that these
+// are the entries whose scores the lane has.
+template <class E, int NG, bool CAP, bool BIAS>
+__global__ __launch_bounds__(512) void k_read_packed(PackedArgs pa) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const ReadArgs &a = pa.r;
+    constexpr int kBytes = 16 * NG, kOut = 2 * NG, kPiece = piece_bytes(NG);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, quarter = lane >> 4;
+    const int units = pa.heads_in * pa.rows_in, unit = wave % units, stream = wave / units;
+    char *codes = lds + wave * kPiece;
+    float *params = (float *)(codes + kPackedTile * kBytes);  // [NG][key scale, key base, value scale, value base][64]
+    int *places = (int *)(params + 4 * NG * kPackedTile);
+    float *tables = (float *)(lds + pa.streams * units * kPiece);
+    const int head_groups = a.kv_heads / pa.heads_in;
+    // the key heads of a block's entries one behind the other on one of the card's eight dies, which blocks take turns with
+    const unsigned turn = blockIdx.x >> 3;
+    const int first_head = (int)(turn % head_groups) * pa.heads_in, head = first_head + unit % pa.heads_in;
+    const long long block = (long long)(turn / head_groups) * 8 + (blockIdx.x & 7);
+    if (block >= a.blocks) return;
+    const int d = document_of(a.off, a.num_queries, a.num_entries, 1, a.shift, block, lane);
+    const long long b0 = first_block(a.off, d, a.num_entries, 1, a.shift);
+    const long long e0 = taken_into(a.off[d], a.num_entries), e1 = taken_into(a.off[d + 1], a.num_entries);
+    const long long len = e1 > e0 ? e1 - e0 : 0, from = (block - b0) << a.shift;
+    if (from < 0 || (from > 0 && from >= len)) return;
+    const bool alone = len <= (1ll << a.shift);
+    const int n = (int)(len - from < (1ll << a.shift) ? len - from : 1ll << a.shift);
+    const int32_t *entity = a.entity ? a.entity + e0 + from : nullptr;
+    const uint8_t *hop = a.hop ? a.hop + e0 + from : nullptr;
+
+    const int row_group = blockIdx.y * pa.rows_in + unit / pa.heads_in, vr = row_group * 16 + col;
+    const bool mine = vr < a.rows;
+    const int token = mine ? vr / a.group : 0, g = mine ? vr % a.group : 0;
+    const long long place = ((long long)d * a.tokens + token) * a.heads + head * a.group + g;
+    typename Vec8<E>::type q[NG];
+    float q_sum[NG];  // of a group's elements
+#pragma unroll
+    for (int i = 0; i < NG; i++) {
+        const int c = 32 * i + 8 * quarter;
+        u32x4 x = {0, 0, 0, 0};
+        if (mine && c < a.dim) x = *(const u32x4 *)((const E *)a.q + place * a.dim + c);
+        const typename Vec8<E>::type y = as8<E>(x);
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; e++) sum += (float)y[e];
+        q_sum[i] = quarters_sum(sum);
+        q[i] = __builtin_shufflevector(y, y, 0, 4, 1, 5, 2, 6, 3, 7);
+    }
+    const int q_pos = a.q_pos ? a.q_pos[d] : 0, M = a.score.max_distance;
+    const float *my_table = tables + (unit % pa.heads_in) * pa.table_words + g * (2 * M + 1);
+    if (BIAS) {
+        for (int h = 0; h < pa.heads_in; h++) bias_to_lds<E>(tables + h * pa.table_words, a.score, (first_head + h) * a.group, a.group, tid, blockDim.x);
+        __syncthreads();
+    }
+    f32x4 o[kOut], shift_sum[NG];
+    float base_sum[NG];
+#pragma unroll
+    for (int i = 0; i < kOut; i++) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NG; i++) shift_sum[i] = f32x4{0.f, 0.f, 0.f, 0.f}, base_sum[i] = 0.f;
+    float m = kLowest, l = 0.f;
+    float unit_scale = sizeof(E) == 2 && !std::is_same<E, bf16>::value ? 0.f : 1.f;  // of the weights: see below
+    typename Vec8<E>::type shift_by;
+#pragma unroll
+    for (int e = 0; e < 8; e++) shift_by[e] = (E)-23.5f;
+
+    const char *rows = (const char *)a.keys;
+    const int all = a.kv_heads * NG;
+    auto id_of = [&](int t) {
+        const int at = t * kPackedTile + lane;
+        if (at >= n) return -1;
+        const long long id = entity ? entity[at] : e0 + from + at;
+        return id >= 0 && id < a.num_entities ? (int)id : -1;
+    };
+    auto hop_of = [&](int t) {
+        const int at = t * kPackedTile + lane;
+        return hop && at < n ? (int)hop[at] : 0;
+    };
+    unsigned k[4][NG];
+    u32x4 v[NG];
+    u64 param[NG];
+    auto fetch = [&](int id) {
+#pragma unroll
+        for (int t = 0; t < 4; t++) {
+            const int of = __shfl(id, 16 * t + col);
+            const unsigned *at = (const unsigned *)(rows + (long long)of * pa.row_bytes) + head * 4 * NG + quarter * NG;
+#pragma unroll
+            for (int i = 0; i < NG; i++) k[t][i] = of >= 0 ? at[i] : 0u;
+        }
+#pragma unroll
+        for (int i = 0; i < NG; i++) {
+            const int chunk = i * 64 + lane, p = chunk / NG, part = chunk % NG;
+            const int of = __shfl(id, 16 * ((p >> 2) & 3) + 4 * (p >> 4) + (p & 3));
+            v[i] = of >= 0 ? *(const u32x4 *)(rows + (long long)of * pa.row_bytes + 16 * all + head * kBytes + part * 16) : u32x4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int i = 0; i < NG; i++) param[i] = id >= 0 ? *(const u64 *)(rows + (long long)id * pa.row_bytes + 32 * all + (head * NG + i) * 8) : 0;
+    };
+    const int tiles = (n + kPackedTile - 1) / kPackedTile;
+    int id = id_of(stream), next_id = id_of(stream + pa.streams), now_hop = 0, next_hop = 0;
+    if (BIAS) now_hop = hop_of(stream), next_hop = hop_of(stream + pa.streams);
+    if (stream < tiles) fetch(id);
+    for (int t = stream; t < tiles; t += pa.streams) {
+        const u64 seen = __ballot(id >= 0);
+        if (!std::is_same<E, bf16>::value) {
+            // float16 holds weights down to 2^-24 only: they are multiplied by a power of two by which the values' largest scale so far
+            // is about 1
+            float top = 0.f;
+#pragma unroll
+            for (int i = 0; i < NG; i++) top = fmaxf(top, __builtin_fabsf(low_half((unsigned)(param[i] >> 32))));
+            if (wave_any(top * unit_scale > 1024.f || (unit_scale == 0.f && top > 0.f))) {
+#pragma unroll
+                for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
+                int power = 127 - (int)(__builtin_bit_cast(unsigned, top) >> 23 & 255);
+                power = power < -100 ? -100 : power > 100 ? 100 : power;
+                const float now = __builtin_bit_cast(float, (unsigned)(power + 127) << 23), change = unit_scale > 0.f ? now / unit_scale : 1.f;
+#pragma unroll
+                for (int i = 0; i < kOut; i++) o[i] *= change;
+#pragma unroll
+                for (int i = 0; i < NG; i++) shift_sum[i] *= change;
+                unit_scale = now;
+            }
+        }
+        // the tile's products, one per group of the elements
+        f32x4 z[4][NG];
+#pragma unroll
+        for (int b = 0; b < 4; b++)
+#pragma unroll
+            for (int i = 0; i < NG; i++) z[b][i] = mfma16(codes8<E>(k[b][i]), q[i], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+        for (int i = 0; i < NG; i++) *(u32x4 *)(codes + (i * 64 + lane) * 16) = v[i];
+#pragma unroll
+        for (int i = 0; i < NG; i++) {
+            const unsigned kp = (unsigned)param[i], vp = (unsigned)(param[i] >> 32);
+            const float ks = low_half(kp), vs = low_half(vp);
+            params[(4 * i + 0) * 64 + lane] = ks;
+            params[(4 * i + 1) * 64 + lane] = __builtin_fmaf(-16.f, ks, high_half(kp));
+            params[(4 * i + 2) * 64 + lane] = vs * unit_scale;
+            params[(4 * i + 3) * 64 + lane] = __builtin_fmaf(7.5f, vs, high_half(vp));
+        }
+        if (BIAS) places[lane] = distance_place(now_hop, q_pos, M);
+        wave_sync();
+        id = next_id;
+        now_hop = next_hop;
+        if (t + pa.streams < tiles) fetch(id);
+        next_id = id_of(t + 2 * pa.streams);
+        if (BIAS) next_hop = hop_of(t + 2 * pa.streams);
+        f32x16 s;
+#pragma unroll
+        for (int b = 0; b < 4; b++) {
+            float y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < NG; i++) {
+                const f32x4 ks = *(const f32x4 *)(params + (4 * i + 0) * 64 + 16 * b + 4 * quarter);
+                const f32x4 kb = *(const f32x4 *)(params + (4 * i + 1) * 64 + 16 * b + 4 * quarter);
+#pragma unroll
+                for (int e = 0; e < 4; e++) y[e] = __builtin_fmaf(ks[e], z[b][i][e], __builtin_fmaf(kb[e], q_sum[i], y[e]));
+            }
+#pragma unroll
+            for (int e = 0; e < 4; e++) s[4 * b + e] = y[e];
+        }
+        if (CAP) cap_scores<4>(a.score, s);
+        float top = kLowest;
+#pragma unroll
+        for (int b = 0; b < 4; b++) {
+            int4 at = {0, 0, 0, 0};
+            if (BIAS) at = *(const int4 *)(places + 16 * b + 4 * quarter);
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                float y = CAP ? s[4 * b + e] : s[4 * b + e] * a.score.k;
+                if (BIAS) y += my_table[e == 0 ? at.x : e == 1 ? at.y : e == 2 ? at.z : at.w];
+                if (seen != ~0ull) y = seen >> (16 * b + 4 * quarter + e) & 1 ? y : -INFINITY;
+                s[4 * b + e] = y;
+                top = fmaxf(top, y);
+            }
+        }
+        top = quarters_max(top);
+        if (wave_any(top > m)) {
+            const float up = fmaxf(m, top), shrink = exp2_fast(m - up);
+            m = up;
+            l *= shrink;
+#pragma unroll
+            for (int i = 0; i < kOut; i++) o[i] *= shrink;
+#pragma unroll
+            for (int i = 0; i < NG; i++) shift_sum[i] *= shrink, base_sum[i] *= shrink;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+            s[r] = exp2_fast(s[r] - m);
+            l += s[r];
+        }
+        typedef int v2i __attribute__((ext_vector_type(2)));
+        typedef __attribute__((address_space(3))) v2i lds2;
+#pragma unroll
+        for (int i = 0; i < NG; i++) {
+            typename Vec8<E>::type w[2];
+#pragma unroll
+            for (int b = 0; b < 4; b++) {
+                const f32x4 vs = *(const f32x4 *)(params + (4 * i + 2) * 64 + 16 * b + 4 * quarter);
+                const f32x4 vb = *(const f32x4 *)(params + (4 * i + 3) * 64 + 16 * b + 4 * quarter);
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    base_sum[i] = __builtin_fmaf(s[4 * b + e], vb[e], base_sum[i]);
+                    w[b >> 1][2 * e + (b & 1)] = (E)(s[4 * b + e] * vs[e]);
+                }
+            }
+            shift_sum[i] = mfma16(shift_by, w[0], shift_sum[i]);
+            shift_sum[i] = mfma16(shift_by, w[1], shift_sum[i]);
+#pragma unroll
+            for (int j = 2 * i; j < 2 * i + 2; j++) {
+                const v2i x = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds2 *)(uintptr_t)(lds_place(codes) + (16 * quarter + col) * kBytes + 8 * j));
+                o[j] = mfma16(codes8<E>((unsigned)x[0]), w[0], o[j]);
+                o[j] = mfma16(codes8<E>((unsigned)x[1]), w[1], o[j]);
+            }
+        }
+        wave_sync();
+    }
+    // the output of this wavefront's entries: element 16 j + 4 quarter + e of the lane's row
+    const float back = unit_scale > 0.f ? 1.f / unit_scale : 1.f;
+    l = quarters_sum(l);
+#pragma unroll
+    for (int i = 0; i < NG; i++) base_sum[i] = quarters_sum(base_sum[i]);
+#pragma unroll
+    for (int j = 0; j < kOut; j++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) o[j][e] = __builtin_fmaf(o[j][e] + shift_sum[j / 2][e], back, base_sum[j / 2]);
+    if (pa.streams > 1) {  // joined with the others that have the same rows, in their order
+        __syncthreads();
+        float *box = (float *)(lds + wave * kPiece);
+        if (stream > 0) {
+#pragma unroll
+            for (int j = 0; j < kOut; j++) *(f32x4 *)(box + (j * 64 + lane) * 4) = o[j];
+            if (quarter == 0) box[kOut * 256 + col] = m, box[kOut * 256 + 16 + col] = l;
+        }
+        __syncthreads();
+        if (stream > 0) return;
+        for (int w = 1; w < pa.streams; w++) {
+            const float *other = (const float *)(lds + (wave + w * units) * kPiece);
+            const float om = other[kOut * 256 + col], ol = other[kOut * 256 + 16 + col];
+            const float up = fmaxf(m, om), mine_by = exp2_fast(m - up), other_by = exp2_fast(om - up);
+            m = up;
+            l = l * mine_by + ol * other_by;
+#pragma unroll
+            for (int j = 0; j < kOut; j++) o[j] = o[j] * mine_by + *(const f32x4 *)(other + (j * 64 + lane) * 4) * other_by;
+        }
+    }
+    if (!mine) return;
+    if (alone) {
+        const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+#pragma unroll
+        for (int j = 0; j < kOut; j++) {
+            const int c = 16 * j + 4 * quarter;
+            if (c >= a.dim) continue;
+            typename Vec4<E>::type x;
+#pragma unroll
+            for (int e = 0; e < 4; e++) x[e] = (E)(o[j][e] * inv);
+            *(typename Vec4<E>::type *)((E *)a.out + place * a.dim + c) = x;
+        }
+        if (quarter == 0) a.lse[place] = l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2;
+    } else {
+        const long long at = (block * a.tokens + token) * a.heads + head * a.group + g;
+#pragma unroll
+        for (int j = 0; j < kOut; j++) {
+            const int c = 16 * j + 4 * quarter;
+            if (c < a.dim) *(f32x4 *)(a.part_o + at * a.dim + c) = o[j];
+        }
+        if (quarter == 0) a.part_ml[2 * at] = m, a.part_ml[2 * at + 1] = l;
+    }
+}
+
+static logoskg_status packed_args(const logoskg_entity_read *r, PackedArgs *pa, const char *call) {
+    if (!r || r->struct_size != sizeof(logoskg_entity_read)) { set_error("%s: struct_size", call); return LOGOSKG_EINVAL; }
+    const char *why = bad_heads(r->dtype, r->heads, r->kv_heads, r->dim);
+    if (!why) why = bad_score(r->score, r->heads, r->kv_heads);
+    if (!why && (r->num_queries < 0 || r->tokens < 1 || r->tokens > 65535 || r->num_entries < 0 || r->num_entities < 0)) why = "a count is out of range";
+    if (!why && r->num_entities >= (1ll << 31)) why = "num_entities is 2^31 or more";
+    if (!why && !r->entity && r->num_entities < r->num_entries) why = "fewer rows than entries";
+    if (!why && r->num_queries && (!r->off || !r->q || !r->out || !r->lse)) why = "off, q, out or lse is NULL";
+    if (!why && r->num_entries && r->num_entities && !r->keys) why = "the table is NULL";
+    if (!why && (r->values || r->key_head || r->value_row || r->value_head)) why = "values or strides beside a packed table";
+    if (!why && (((uintptr_t)r->q | (uintptr_t)r->keys | (uintptr_t)r->out | (uintptr_t)r->workspace) & 15)) why = "an array is not 16-byte aligned";
+    if (!why && (r->key_row & 15 || r->key_row < 0 || r->key_row > (1ll << 31) || (r->num_entities > 1 && r->key_row < row_bytes_of(r->kv_heads, (r->dim + 31) / 32)))) why = "the rows' stride is no multiple of 16, or rows overlap";
+    if (why) { set_error("%s: %s", call, why); return LOGOSKG_EINVAL; }
+    memset(pa, 0, sizeof *pa);
+    ReadArgs *a = &pa->r;
+    a->num_queries = r->num_queries; a->tokens = r->tokens; a->heads = r->heads; a->kv_heads = r->kv_heads;
+    a->group = r->heads / r->kv_heads; a->dim = r->dim; a->rows = a->tokens * a->group;
+    a->num_entries = r->num_entries; a->num_entities = r->num_entities;
+    a->off = r->off; a->entity = r->entity; a->q_pos = r->q_pos; a->hop = r->hop;
+    a->q = r->q; a->keys = r->keys; pa->row_bytes = r->key_row;
+    a->score = score_args(r->score);
+    a->out = r->out; a->lse = r->lse;
+    // A block's eight wavefronts: as many key heads as divide theirs (whose rows lie side by side) and have room for their biases,
+    // then groups of 16 rows, then streams of tiles.
+    pa->row_groups = (a->rows + 15) / 16;
+    pa->table_words = a->score.bias ? a->group * (2 * a->score.max_distance + 1) : 0;
+    const int piece = piece_bytes((a->dim + 31) / 32);
+    pa->heads_in = 1;
+    for (int h = 8; h > 1; h--)
+        if (a->kv_heads % h == 0 && 8 * piece + h * pa->table_words * 4 <= 80 << 10) { pa->heads_in = h; break; }
+    pa->rows_in = 8 / pa->heads_in < pa->row_groups ? 8 / pa->heads_in : pa->row_groups;
+    pa->streams = 8 / (pa->heads_in * pa->rows_in);
+    const long long each = (a->kv_heads / pa->heads_in) * (long long)((pa->row_groups + pa->rows_in - 1) / pa->rows_in);
+    a->shift = 6;
+    while (a->shift < 12 && ((1 << a->shift) < kPackedTile * pa->streams || (a->num_entries >> a->shift) * each > 2048)) a->shift++;
+    a->blocks = (a->num_entries >> a->shift) + a->num_queries;
+    if ((a->blocks + 8) * (a->kv_heads / pa->heads_in) >= (1ll << 31) || pa->row_groups > 65535 || (long long)a->num_queries * a->tokens * a->heads >= (1ll << 32)) { set_error("%s: too many rows", call); return LOGOSKG_EINVAL; }
+    return LOGOSKG_OK;
+}
+
+template <class E, int NG, bool CAP, bool BIAS> static logoskg_status launch_packed(const PackedArgs &pa, hipStream_t st) {
+    const ReadArgs &a = pa.r;
+    const int waves = pa.heads_in * pa.rows_in * pa.streams;
+    const size_t bytes = (size_t)waves * piece_bytes(NG) + (size_t)pa.heads_in * pa.table_words * 4;
+    LKG_TRY(allow_lds(k_read_packed<E, NG, CAP, BIAS>, bytes));
+    k_read_packed<E, NG, CAP, BIAS><<<dim3((unsigned)((a.blocks + 7) / 8 * 8 * (a.kv_heads / pa.heads_in)), (unsigned)((pa.row_groups + pa.rows_in - 1) / pa.rows_in)), waves * 64, bytes, st>>>(pa);
+    LKG_HIP(hipGetLastError());
+    return LOGOSKG_OK;
+}
+template <class E, int NG> static logoskg_status read_packed(const PackedArgs &pa, hipStream_t st) {
+    const bool cap = pa.r.score.c > 0, bias = pa.r.score.bias != nullptr;
+    return cap ? bias ? launch_packed<E, NG, true, true>(pa, st) : launch_packed<E, NG, true, false>(pa, st)
+               : bias ? launch_packed<E, NG, false, true>(pa, st) : launch_packed<E, NG, false, false>(pa, st);
+}
+template <class E> static logoskg_status read_packed(const PackedArgs &pa, hipStream_t st) {
+    const ReadArgs &a = pa.r;
+    const int groups = (a.dim + 31) / 32;
+    LKG_TRY((groups == 1 ? read_packed<E, 1>(pa, st) : groups == 2 ? read_packed<E, 2>(pa, st) : groups == 3 ? read_packed<E, 3>(pa, st) : read_packed<E, 4>(pa, st)));
+    if (part_bytes(a)) {
+        const long long n = (long long)a.num_queries * a.tokens * a.heads;
+        k_read_join<E><<<dim3((unsigned)((n + 3) / 4)), 256, 0, st>>>(a);
+        LKG_HIP(hipGetLastError());
+    }
+    return LOGOSKG_OK;
+}
+
+static const char *pack_args(const logoskg_pack *p, PackArgs *a) {
+    if (!p || p->struct_size != sizeof(logoskg_pack)) return "struct_size";
+    if (p->dtype < LOGOSKG_F32 || p->dtype > LOGOSKG_F16) return "unknown type";
+    if (logoskg_packed_row_bytes(p->kv_heads, p->dim) == 0) return "dim is no multiple of 8 up to 128, or kv_heads out of range";
+    if (p->num_rows < 0 || p->num_rows > (1ll << 31)) return "a count is out of range";
+    if (p->num_rows && (!p->keys || !p->values || !p->packed)) return "keys, values or packed is NULL";
+    if (p->key_row < 0 || p->key_head < 0 || p->value_row < 0 || p->value_head < 0) return "a stride is negative";
+    if (((uintptr_t)p->packed & 15) || p->packed_row & 15 || p->packed_row < 0 || (p->num_rows > 1 && p->packed_row < logoskg_packed_row_bytes(p->kv_heads, p->dim)))
+        return "packed is not 16-byte aligned, its stride no multiple of 16, or its rows overlap";
+    memset(a, 0, sizeof *a);
+    a->kv_heads = p->kv_heads; a->dim = p->dim; a->groups = (p->dim + 31) / 32;
+    a->pad = row_bytes_of(a->kv_heads, a->groups) - 40 * a->kv_heads * a->groups;
+    a->num_rows = p->num_rows; a->keys = p->keys; a->values = p->values;
+    a->key_row = p->key_row; a->key_head = p->key_head; a->value_row = p->value_row; a->value_head = p->value_head;
+    a->packed = (char *)p->packed; a->packed_row = p->packed_row;
+    return nullptr;
+}
+
+static logoskg_status pack(const logoskg_pack *p, bool back, const char *call) {
+    PackArgs a;
+    if (const char *why = pack_args(p, &a)) { set_error("%s: %s", call, why); return LOGOSKG_EINVAL; }
+    if (a.num_rows == 0) return LOGOSKG_OK;
+    OnDevice on;
+    LKG_TRY(on.go(p->device));
+    hipStream_t st = (hipStream_t)p->stream;
+    const long long blocks = (a.num_rows * a.kv_heads * a.groups + 63) / 64;
+    const dim3 grid((unsigned)(blocks > 16384 ? 16384 : blocks));
+    if (p->dtype == LOGOSKG_F32) back ? k_unpack<float><<<grid, 256, 0, st>>>(a) : k_pack<float><<<grid, 256, 0, st>>>(a);
+    else if (p->dtype == LOGOSKG_BF16) back ? k_unpack<bf16><<<grid, 256, 0, st>>>(a) : k_pack<bf16><<<grid, 256, 0, st>>>(a);
+    else back ? k_unpack<fp16><<<grid, 256, 0, st>>>(a) : k_pack<fp16><<<grid, 256, 0, st>>>(a);
+    LKG_HIP(hipGetLastError());
+    return LOGOSKG_OK;
+}
+
+}  // namespace lkg
+
+using namespace lkg;
+
+extern "C" int64_t logoskg_packed_row_bytes(int32_t kv_heads, int32_t dim) {
+    return kv_heads < 1 || kv_heads > 65536 || dim < 8 || dim > 128 || dim % 8 ? 0 : row_bytes_of(kv_heads, (dim + 31) / 32);
+}
+
+extern "C" logoskg_status logoskg_pack_entities(const logoskg_pack *p) { return pack(p, false, "logoskg_pack_entities"); }
+extern "C" logoskg_status logoskg_unpack_entities(const logoskg_pack *p) { return pack(p, true, "logoskg_unpack_entities"); }
+
+extern "C" int64_t logoskg_read_packed_bytes(const logoskg_entity_read *r) {
+    PackedArgs pa;
+    return packed_args(r, &pa, "logoskg_read_packed_bytes") == LOGOSKG_OK ? part_bytes(pa.r) : -1;
+}
+
+extern "C" logoskg_status logoskg_read_packed(const logoskg_entity_read *r) {
+    PackedArgs pa;
+    LKG_TRY(packed_args(r, &pa, "logoskg_read_packed"));
+    ReadArgs &a = pa.r;
+    if (r->workspace_bytes < part_bytes(a) || (part_bytes(a) && !r->workspace)) {
+        set_error("logoskg_read_packed: the workspace has %lld of %lld bytes", (long long)r->workspace_bytes, (long long)part_bytes(a));
+        return LOGOSKG_ERANGE;
+    }
+    if (a.num_queries == 0) return LOGOSKG_OK;
+    a.part_o = (float *)r->workspace;
+    a.part_ml = a.part_o + (part_bytes(a) ? a.blocks * a.tokens * a.heads * a.dim : 0);
+    OnDevice on;
+    LKG_TRY(on.go(r->device));
+    return r->dtype == LOGOSKG_BF16 ? read_packed<bf16>(pa, (hipStream_t)r->stream) : read_packed<fp16>(pa, (hipStream_t)r->stream);
+}
