@@ -116,8 +116,6 @@ __global__ __launch_bounds__(256) void k_clip_scale(ClipArgs a) {
     }
 }
 
-static int size_of(int dtype) { return dtype == LOGOSKG_F32 ? 4 : 2; }
-
 static const char *bad_gradients(const logoskg_gradient *list, int64_t count) {
     if (count < 0 || count > (1 << 24) || (count && !list)) return "list is NULL, or a count is out of range";
     for (int64_t i = 0; i < count; i++) {
@@ -125,7 +123,7 @@ static const char *bad_gradients(const logoskg_gradient *list, int64_t count) {
         if (g.dtype < LOGOSKG_F32 || g.dtype > LOGOSKG_F16 || g.out_dtype < LOGOSKG_F32 || g.out_dtype > LOGOSKG_F16) return "unknown type";
         if (g.n < 0 || g.n > (1ll << 42)) return "a count is out of range";
         if (g.n && (!g.grad || !g.out)) return "grad or out is NULL";
-        if (g.n && (((uintptr_t)g.grad & (size_of(g.dtype) - 1)) || ((uintptr_t)g.out & (size_of(g.out_dtype) - 1)))) return "an array is not aligned to its elements";
+        if (g.n && (!aligned_to(g.grad, g.dtype) || !aligned_to(g.out, g.out_dtype))) return kUnaligned;
     }
     return nullptr;
 }

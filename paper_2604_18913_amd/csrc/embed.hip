@@ -389,6 +389,7 @@ static const char *grad_args(const logoskg_embedding_grad *e, GradArgs *a) {
     if (e->row < e->dim && e->num_entities > 1) return "rows overlap";
     if (e->num_ids && e->dim && (!e->ids || !e->dout)) return "ids or dout is NULL";
     if (e->num_entities && e->dim && !e->dtable) return "dtable is NULL";
+    if (!aligned_to(e->dout, e->dtype) || !aligned_to(e->dtable, e->table_dtype) || !aligned_to(e->ids, LOGOSKG_F32)) return kUnaligned;
     if ((uintptr_t)e->workspace & 15) return "the workspace is not 16-byte aligned";
     memset(a, 0, sizeof *a);
     a->num_ids = e->num_ids; a->num_entities = e->num_entities; a->dim = e->dim; a->row = e->row;
@@ -449,6 +450,7 @@ extern "C" logoskg_status logoskg_embed_entities(const logoskg_embedding *e) {
     else if (e->num_ids < 0 || e->num_ids >= (1ll << 40) || e->num_entities < 0 || e->dim < 0 || e->dim > (1ll << 24) || e->row < 0 || e->row > (1ll << 40)) why = "a count is out of range";
     else if (e->num_ids && e->dim && (!e->ids || !e->out)) why = "ids or out is NULL";
     else if (e->num_ids && e->dim && e->num_entities && !e->table) why = "table is NULL";
+    else if (!aligned_to(e->table, e->dtype) || !aligned_to(e->out, e->dtype) || !aligned_to(e->ids, LOGOSKG_F32)) why = kUnaligned;
     if (why) { set_error("logoskg_embed_entities: %s", why); return LOGOSKG_EINVAL; }
     if (e->num_ids == 0 || e->dim == 0) return LOGOSKG_OK;
     const EmbedArgs a = {e->num_ids, e->num_entities, e->dim, e->row, e->scale, e->ids, e->table, e->out};

@@ -489,6 +489,7 @@ static const char *pack_args(const logoskg_pack *p, PackArgs *a) {
     if (logoskg_packed_row_bytes(p->kv_heads, p->dim) == 0) return "dim is no multiple of 8 up to 128, or kv_heads out of range";
     if (p->num_rows < 0 || p->num_rows > (1ll << 31)) return "a count is out of range";
     if (p->num_rows && (!p->keys || !p->values || !p->packed)) return "keys, values or packed is NULL";
+    if (!aligned_to(p->keys, p->dtype) || !aligned_to(p->values, p->dtype)) return kUnaligned;
     if (p->key_row < 0 || p->key_head < 0 || p->value_row < 0 || p->value_head < 0) return "a stride is negative";
     if (((uintptr_t)p->packed & 15) || p->packed_row & 15 || p->packed_row < 0 || (p->num_rows > 1 && p->packed_row < logoskg_packed_row_bytes(p->kv_heads, p->dim)))
         return "packed is not 16-byte aligned, its stride no multiple of 16, or its rows overlap";

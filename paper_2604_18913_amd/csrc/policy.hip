@@ -201,6 +201,7 @@ static const char *policy_args(const logoskg_policy *p, int mode, PolicyArgs *a)
     if (p->num_rows < 0 || p->vocab < 0 || p->vocab >= (1ll << 31) || p->num_masks < 0 || p->num_masks >= (1ll << 31)) return "a count is out of range";
     if (p->row < 0 || (p->row < p->vocab && p->num_rows > 1)) return "rows overlap";
     if (p->num_rows && ((p->vocab && !p->logits) || !p->target || !p->lse)) return "logits, target or lse is NULL";
+    if (!aligned_to(p->logits, p->dtype) || !aligned_to(p->dlogits, p->dtype)) return kUnaligned;
     if (mode != kBackward && p->num_rows && !p->logp) return "logp is NULL";
     if (p->mask && !p->mask_row && p->num_masks < p->num_rows) return "fewer masks than rows";
     if (!(p->scale > 0.f) || p->scale - p->scale != 0.f) return "scale is not above 0";

@@ -30,6 +30,11 @@ template <class T> __device__ __forceinline__ void store_some(T *p, const Some<T
         if (e < count) p[e] = x[e];
 }
 
+inline int size_of(int dtype) { return dtype == LOGOSKG_F32 ? 4 : 2; }
+// Whether a place is one of whole elements: what the chunks above ask for, and the least that a caller's tensors have.
+inline bool aligned_to(const void *p, int dtype) { return ((uintptr_t)p & (size_of(dtype) - 1)) == 0; }
+inline const char *const kUnaligned = "an array is not aligned to its elements";
+
 // A call works on the device that it is told; the caller's stays the current one behind it.
 struct OnDevice {
     int before = -1;

@@ -1,0 +1,147 @@
+"""clip_gradients against its 64-bit definition (bounds: around_oracle)."""
+import math
+
+import pytest
+import torch
+
+import around_oracle as oracle
+import paper_2604_18913_amd as lkg
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+TYPE_NAMES = ["fp32", "bf16", "fp16"]
+
+
+def _grads(seed, shapes, dtypes=TYPES[:1], size=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return [(torch.randn(s, generator=g) * size).to(dtypes[i % len(dtypes)]) for i, s in enumerate(shapes)]
+
+
+def _check(grads, max_norm, scale=1.0, to=None):
+    want, tol, each = oracle.clip(grads, max_norm, scale, to)
+    on = [g.cuda() for g in grads]
+    if to is not None:
+        out = [torch.full_like(g, 3.0, dtype=t) for g, t in zip(on, to)]
+        norm = lkg.clip_gradients(on, max_norm, scale=scale, out=out)
+        assert all(torch.equal(a.cpu(), b) for a, b in zip(on, grads))
+    else:
+        out, norm = on, lkg.clip_gradients(on, max_norm, scale=scale)
+    assert norm.shape == () and norm.dtype is torch.float32
+    oracle.check(norm, want, tol, "norm")
+    for i, (x, (y, t)) in enumerate(zip(out, each)):
+        oracle.check(x, y, t, f"gradient {i}")
+
+
+SHAPES = [(), (1,), (7,), (0, 5), (8,), (33, 65), (257,), (8191,), (8192,), (8193,), (3, 5, 7), (100_003,)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=TYPE_NAMES)
+@pytest.mark.parametrize("max_norm, scale", [(1.0, 1.0), (1e6, 1.0), (3.0, 0.25), (0.0, 1.0), (5.0, -2.0), (math.inf, 0.5), (2.0, 0.0)])
+def test_types_norms_and_scales(max_norm, scale, dtype):
+    _check(_grads(1, SHAPES, [dtype]), max_norm, scale)
+
+
+@pytest.mark.parametrize("to", TYPES, ids=TYPE_NAMES)
+def test_mixed_types_into_others(to):
+    grads = _grads(2, SHAPES, TYPES)
+    _check(grads, 2.0, 0.5)
+    _check(grads, 2.0, 0.5, [to] * len(grads))
+
+
+@pytest.mark.parametrize("count", [1, 63, 64, 65, 128, 200])
+def test_many_tensors(count):
+    _check(_grads(3, [(1 + 37 * i % 900,) for i in range(count)], TYPES), 1.0)
+
+
+@pytest.mark.parametrize("shapes", [[(5_000_000,)], [(3_000_001,), (9,), (2_222_222,)], [(20_000_000,)]])
+def test_more_chunks_than_blocks(shapes):
+    _check(_grads(4, shapes, [torch.bfloat16]), 10.0)
+
+
+def test_one_nothing_and_none():
+    _check(_grads(5, [(1,)]), 0.1)
+    for empty in ([torch.zeros(0, device="cuda")], [torch.zeros(4, 4, device="cuda")], [None, torch.zeros(3, device="cuda"), None]):
+        assert lkg.clip_gradients(empty, 1.0) == 0 and all(g is None or (g == 0).all() for g in empty)
+
+
+@pytest.mark.parametrize("size", [1e30, 1e-30, 3e38])
+def test_sizes_whose_squares_leave_32_bits(size):
+    g = torch.Generator().manual_seed(6)
+    grads = [(torch.rand(1000, generator=g) * 0.2 + 0.8) * size * 0.01, torch.tensor([size])]
+    want = math.sqrt(sum(float((x.double() ** 2).sum()) for x in grads))
+    on = [x.cuda() for x in grads]
+    norm = lkg.clip_gradients(on, 1.0)
+    assert (norm == math.inf) if want > 3.4e38 else abs(float(norm) / want - 1) < 1e-6
+    if size > 1:  # (scaled by less than 32 bits can hold, a factor is 0 or has fewer bits)
+        got = math.sqrt(sum(float((x.cpu().double() ** 2).sum()) for x in on))
+        assert abs(got - 1) < 1e-5
+    else:
+        assert torch.equal(on[0].cpu(), grads[0])
+
+
+def test_norms_that_are_not_finite():
+    grads = [torch.ones(5, device="cuda"), torch.tensor([1.0, math.inf], device="cuda")]
+    assert lkg.clip_gradients(grads, 1.0) == math.inf
+    assert (grads[0] == 0).all() and grads[1][0] == 0 and grads[1][1].isnan()
+    grads = [torch.ones(5, device="cuda"), torch.tensor([1.0, math.nan], device="cuda")]
+    assert lkg.clip_gradients(grads, 1.0).isnan() and all(g.isnan().all() for g in grads)
+
+
+def test_layouts():
+    wide = _grads(7, [(40, 50)])[0]
+    want, _, each = oracle.clip([wide], 1.0)
+    for on in (wide.cuda().t().contiguous().t(), wide.cuda().t()):  # a transpose, of its own memory or not
+        norm = lkg.clip_gradients([on], 1.0)
+        oracle.check(norm, want, 2 * oracle.E32 * want)
+        oracle.check(on if on.shape == (40, 50) else on.t(), *each[0])
+    for lead in (1, 3):  # not at a multiple of 16 bytes
+        flat = torch.full((2000 + lead,), 9.0).to(torch.bfloat16)
+        flat[lead:] = wide.reshape(-1).to(torch.bfloat16)
+        _, _, each = oracle.clip([flat[lead:]], 1.0)
+        on = flat.cuda()
+        lkg.clip_gradients([on[lead:]], 1.0)
+        oracle.check(on[lead:], *each[0])
+        assert (on[:lead] == 9).all()
+    out = [torch.empty(40, 50, device="cuda").t()]
+    with pytest.raises(ValueError, match="laid out"):
+        lkg.clip_gradients([wide.cuda()], 1.0, out=out)
+    for bad, says in [(wide.cuda()[:, ::2], "contiguous"), (wide.cuda()[:, :9], "contiguous"), (wide.cuda().double(), "not supported"), (wide, "on the GPU")]:
+        with pytest.raises(ValueError, match=says):
+            lkg.clip_gradients([bad], 1.0)
+    on = wide.cuda()
+    with pytest.raises(lkg.LogosKGError, match="share"):
+        lkg.clip_gradients([on, on], 1.0)
+    with pytest.raises(lkg.LogosKGError, match="share"):
+        lkg.clip_gradients([on, on[:3]], 1.0)
+    assert torch.equal(on.cpu(), wide)
+
+
+def test_the_same_bits_streams_and_graphs():
+    grads = [g.cuda() for g in _grads(8, [(500, 300), (70_000,), (11,)], TYPES)]
+    out = [torch.empty_like(g, dtype=torch.float32) for g in grads]
+    norm = lkg.clip_gradients(grads, 1.0, out=out).clone()
+    want = [o.clone() for o in out]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    other = [torch.empty_like(o) for o in out]
+    side_norm = lkg.clip_gradients(grads, 1.0, out=other, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(side_norm, norm) and all(torch.equal(a, b) for a, b in zip(other, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = lkg.clip_gradients(grads, 1.0, out=out)
+    for seed in range(4):
+        for g, x in zip(grads, _grads(20 + seed, [g.shape for g in grads], [g.dtype for g in grads], 1e-3 if seed == 2 else 1.0)):
+            g.copy_(x)
+        graph.replay()
+        torch.cuda.synchronize()
+        norm = lkg.clip_gradients(grads, 1.0, out=other)
+        assert torch.equal(held, norm) and all(torch.equal(a, b) for a, b in zip(out, other))
+
+
+def test_tensors_beyond_32_bits():
+    n = (1 << 32) + 5
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g[0], g[1 << 31], g[n - 1] = 3.0, 4.0, 12.0
+    assert abs(float(lkg.clip_gradients([g], 1.0)) - 13) < 1e-5
+    assert torch.allclose(g[[0, 1 << 31, n - 1]].float().cpu(), torch.tensor([3.0, 4.0, 12.0]) / 13, rtol=2 ** -8)
