@@ -52,6 +52,7 @@ template <class T, int LG> __global__ __launch_bounds__(256) void k_embed(EmbedA
 struct GradArgs {
     long long num_ids, num_entities, dim, row, chunks;
     int accumulate, chunk, tiles, bits;
+    int clears, clear_blocks;  // launches among which the rows that become zeros are divided, and blocks of each for it
     float scale;
     const int32_t *ids;
     const void *dout;
@@ -59,6 +60,7 @@ struct GradArgs {
     unsigned *key[2], *place[2];  // of the sort: from one to the other and back
     unsigned *count, *total;      // [digits][tiles], [digits]
     float *part;                  // [chunks][2][dim]: of the run that comes in from the chunk before, and of the one that goes on
+    unsigned *crossings, *crossing;  // how many runs go on from the chunk that they begin in, and those chunks, in any order
 };
 
 constexpr int kSortTile = 4096, kMostDigitBits = 11;
@@ -100,12 +102,42 @@ template <int THREADS> __device__ __forceinline__ unsigned block_before(unsigned
     return before + y - x;
 }
 
+// Rows [from, to) of the table become zeros, `blocks` blocks of THREADS threads side by side.  Rows that are written again later are
+// few where it costs much (a large table), and the sort beside which this runs leaves the memory idle.
+template <class O, int THREADS> __device__ __forceinline__ void clear_rows(const GradArgs &a, long long from, long long to, long long block, long long blocks) {
+    constexpr int V = 16 / sizeof(O);
+    O *table = (O *)a.dtable;
+    if (a.row == a.dim) {  // one run of elements, whole chunks from the first aligned one on
+        O *p = table + from * a.dim, *end = table + to * a.dim;
+        const long long lead0 = ((16 - ((uintptr_t)p & 15)) & 15) / sizeof(O), lead = lead0 < end - p ? lead0 : end - p;
+        const long long chunks = (end - p - lead) / V, tail = lead + chunks * V;
+        if (block == 0) {
+            if (threadIdx.x < lead) p[threadIdx.x] = (O)0.f;
+            if (tail + threadIdx.x < end - p) p[tail + threadIdx.x] = (O)0.f;
+        }
+        Some<O> *whole = (Some<O> *)(p + lead);
+        for (long long i = block * THREADS + threadIdx.x; i < chunks; i += blocks * THREADS) whole[i] = Some<O>{};
+        return;
+    }
+    const long long per = (a.dim + V - 1) / V;
+    for (long long i = from * per + block * THREADS + threadIdx.x; i < to * per; i += blocks * THREADS) {
+        const long long e = i / per, c = i % per * V;
+        store_some<O>(table + e * a.row + c, Some<O>{}, a.dim - c < V ? (int)(a.dim - c) : V);
+    }
+}
+// .. the share of them that launch `at` of a.clears has (clear_blocks of its blocks, behind the others)
+template <class O, int THREADS> __device__ __forceinline__ void clear_share(const GradArgs &a, int at, long long block) {
+    clear_rows<O, THREADS>(a, a.num_entities * at / a.clears, a.num_entities * (at + 1) / a.clears, block, a.clear_blocks);
+}
+
 // Lists of up to kSortTile ids: one block sorts them in LDS.
-__global__ __launch_bounds__(1024) void k_sort_few(GradArgs a) {
+template <class O> __global__ __launch_bounds__(1024) void k_sort_few(GradArgs a) {
     __shared__ unsigned key[2][kSortTile];
     __shared__ unsigned short place[2][kSortTile];
     __shared__ unsigned count[16][256], box[16];
+    if (blockIdx.x > 0) return clear_share<O, 1024>(a, 0, blockIdx.x - 1);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = (int)a.num_ids, rounds = (n + 1023) / 1024;
+    if (tid == 0) *a.crossings = 0;
     for (int i = tid; i < n; i += 1024) key[0][i] = key_of(a, i), place[0][i] = (unsigned short)i;
     int from = 0;
     for (int shift = 0; shift < a.bits; shift += 8, from ^= 1) {
@@ -153,9 +185,11 @@ __global__ __launch_bounds__(1024) void k_sort_few(GradArgs a) {
 }
 
 // A pass of the sort over tiles: how often a digit occurs in each tile ..
-__global__ __launch_bounds__(256) void k_sort_count(GradArgs a, int pass, int shift, int bits) {
+template <class O> __global__ __launch_bounds__(256) void k_sort_count(GradArgs a, int pass, int shift, int bits) {
     extern __shared__ unsigned found[];
+    if ((int)blockIdx.x >= a.tiles) return clear_share<O, 256>(a, 2 * pass, blockIdx.x - a.tiles);
     const int tid = threadIdx.x, digits = 1 << bits;
+    if (blockIdx.x == 0 && tid == 0) *a.crossings = 0;
     for (int i = tid; i < digits; i += 256) found[i] = 0;
     __syncthreads();
     const long long from = (long long)blockIdx.x * kSortTile;
@@ -184,9 +218,10 @@ __global__ __launch_bounds__(256) void k_sort_before(GradArgs a) {
 }
 
 // .. and every id to its place: behind the smaller digits, those of the tiles before, the wavefronts before and the lanes before.
-__global__ __launch_bounds__(256) void k_sort_move(GradArgs a, int pass, int shift, int bits) {
+template <class O> __global__ __launch_bounds__(256) void k_sort_move(GradArgs a, int pass, int shift, int bits) {
     constexpr int kRounds = kSortTile / 256;
     extern __shared__ unsigned count[];  // [4][digits]
+    if ((int)blockIdx.x >= a.tiles) return clear_share<O, 256>(a, 2 * pass + 1, blockIdx.x - a.tiles);
     __shared__ unsigned box[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, digits = 1 << bits;
     unsigned *mine = count + wave * digits;
@@ -236,108 +271,167 @@ __global__ __launch_bounds__(256) void k_sort_move(GradArgs a, int pass, int shi
     }
 }
 
-template <class O> __global__ __launch_bounds__(256) void k_clear_rows(GradArgs a) {
-    constexpr int V = 16 / sizeof(O);
-    const long long per = (a.dim + V - 1) / V, all = per * a.num_entities;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
-        const long long e = i / per, c = i % per * V;
-        store_some<O>((O *)a.dtable + e * a.row + c, Some<O>{}, a.dim - c < V ? (int)(a.dim - c) : V);
+// `count` of a lane's V sums, whole chunks of O at a time where all of them count
+template <class O, int V> __device__ __forceinline__ void store_sums(O *to, const O (&y)[V], int count) {
+    constexpr int N = 16 / sizeof(O) < V ? 16 / sizeof(O) : V;
+    typedef O chunk __attribute__((ext_vector_type(N), aligned(sizeof(O))));
+    if (count >= V) {
+#pragma unroll
+        for (int i = 0; i < V; i += N) {
+            chunk x;
+#pragma unroll
+            for (int e = 0; e < N; e++) x[e] = y[i + e];
+            *(chunk *)(to + i) = x;
+        }
+        return;
     }
+#pragma unroll
+    for (int e = 0; e < V - 1; e++)
+        if (e < count) to[e] = y[e];
 }
 
 template <class O, int V> __device__ __forceinline__ void write_sum(const GradArgs &a, unsigned id, long long c, int count, const float (&x)[V]) {
     O *to = (O *)a.dtable + (long long)id * a.row + c;
-    for (int e = 0; e < V; e++) {
-        if (e >= count) break;
-        const float y = x[e] * a.scale;
-        to[e] = (O)(a.accumulate ? (float)to[e] + y : y);
+    O y[V];
+#pragma unroll
+    for (int e = 0; e < V; e++) y[e] = (O)(x[e] * a.scale);
+    if (a.accumulate) {
+#pragma unroll
+        for (int e = 0; e < V; e++)
+            if (e < count) y[e] = (O)((float)to[e] + x[e] * a.scale);
     }
+    store_sums<O, V>(to, y, count);
 }
 
-// A group of LG lanes adds up a chunk of the sorted list, each lane 16 bytes of a row; blockIdx.y: further columns.
+// A group of LG lanes adds up a chunk of the sorted list, each lane 16 bytes of a row; blockIdx.y: further columns.  The list of a
+// block's groups goes through LDS first, so that rows are asked for without a wait in between.
+constexpr int kMostChunk = 32;
 template <class T, class O, int LG> __global__ __launch_bounds__(256) void k_embed_sum(GradArgs a) {
-    constexpr int V = 16 / sizeof(T), kAhead = 4;
-    const long long g = (long long)blockIdx.x * (256 / LG) + threadIdx.x / LG, c = ((long long)blockIdx.y * LG + threadIdx.x % LG) * V;
+    constexpr int V = 16 / sizeof(T), kAhead = 8, kGroups = 256 / LG;
+    __shared__ unsigned keys[kGroups * kMostChunk + 2], places[kGroups * kMostChunk];
+    const int tid = threadIdx.x, group = tid / LG;
+    const unsigned none = (unsigned)a.num_entities;
+    const long long first = (long long)blockIdx.x * kGroups * a.chunk;
+    for (int i = tid; i < kGroups * a.chunk + 2; i += 256) {  // the one before and the one behind, too
+        const long long at = first + i - 1;
+        keys[i] = at >= 0 && at < a.num_ids ? a.key[0][at] : none;
+        if (i > 0 && i <= kGroups * a.chunk) places[i - 1] = at < a.num_ids ? a.place[0][at] : 0;
+    }
+    __syncthreads();
+    const long long g = (long long)blockIdx.x * kGroups + group, c = ((long long)blockIdx.y * LG + tid % LG) * V;
     if (g >= a.chunks || c >= a.dim) return;
     const int count = a.dim - c < V ? (int)(a.dim - c) : V;
-    const long long from = g * a.chunk, to = from + a.chunk < a.num_ids ? from + a.chunk : a.num_ids;
-    const unsigned none = (unsigned)a.num_entities;
-    const unsigned *key = a.key[0], *place = a.place[0];
-    unsigned id = key[from];
+    const unsigned *key = keys + 1 + group * a.chunk, *place = places + group * a.chunk;
+    unsigned id = key[0];
     if (id >= none) return;
-    const unsigned before = from > 0 ? key[from - 1] : none, behind = to < a.num_ids ? key[to] : none;
-    bool came = before == id;  // the run began before this chunk
+    bool came = key[-1] == id;  // the run began before this chunk
     float sum[V];
+#pragma unroll
     for (int e = 0; e < V; e++) sum[e] = 0.f;
     float *part = a.part + g * 2 * a.dim + c;
-    for (long long i = from; i < to; i += kAhead) {
-        unsigned k[kAhead];
+    const T *dout = (const T *)a.dout + c;
+#pragma unroll 1
+    for (int i = 0; i < a.chunk; i += kAhead) {
         Some<T> x[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; u++) {
-            k[u] = i + u < to ? key[i + u] : none;
-            if (k[u] < none) x[u] = load_some<T>((const T *)a.dout + place[i + u] * a.dim + c, count);
-        }
+        for (int u = 0; u < kAhead; u++)
+            if (key[i + u] < none) x[u] = load_some<T>(dout + place[i + u] * a.dim, count);
 #pragma unroll
         for (int u = 0; u < kAhead; u++) {
-            if (k[u] >= none) continue;
-            if (k[u] != id) {
+            const unsigned k = key[i + u];
+            if (k >= none) continue;
+            if (k != id) {
                 if (came) {
-                    for (int e = 0; e < count; e++) part[e] = sum[e];
+                    store_sums<float, V>(part, sum, count);
                 } else {
                     write_sum<O, V>(a, id, c, count, sum);
                 }
+#pragma unroll
                 for (int e = 0; e < V; e++) sum[e] = 0.f;
                 came = false;
-                id = k[u];
+                id = k;
             }
 #pragma unroll
             for (int e = 0; e < V; e++) sum[e] += (float)x[u][e];
         }
     }
-    const bool goes_on = behind == id;
+    const bool goes_on = key[a.chunk] == id;
     if (came || goes_on) {
-        if (!came) part += a.dim;
-        for (int e = 0; e < count; e++) part[e] = sum[e];
+        if (!came) {
+            part += a.dim;
+            if (blockIdx.y == 0 && tid % LG == 0) a.crossing[atomicAdd(a.crossings, 1u)] = (unsigned)g;
+        }
+        store_sums<float, V>(part, sum, count);
     } else {
         write_sum<O, V>(a, id, c, count, sum);
     }
 }
 
-// Runs that cross chunks: the block of the chunk that one begins in adds up its parts, 16 groups of 16 lanes a share each.
+// Runs that cross chunks: blocks go through the list of them.  (Its order does not matter: each is a sum of its own.)  Runs of few
+// parts are added up by the blocks of the first column (blockIdx.y), a thread per four elements; those of many by 16 groups of 16
+// lanes, a share of the parts each, 64 elements per blockIdx.y.
 template <class O> __global__ __launch_bounds__(256) void k_embed_join(GradArgs a) {
-    constexpr int V = 4, LG = 16, kGroups = 16;
+    constexpr int V = 4, LG = 16, kGroups = 16, kAhead = 4, kFew = 16;
     __shared__ float box[kGroups][LG * V];
-    const long long g = blockIdx.x, last = (g + 1) * a.chunk - 1;
-    if (last + 1 >= a.num_ids) return;
     const unsigned *key = a.key[0];
-    const unsigned id = key[last];
-    if (id >= a.num_entities || key[last + 1] != id) return;
-    if (key[g * a.chunk] == id && g > 0 && key[g * a.chunk - 1] == id) return;  // came in
-    long long lo = g + 1, hi = a.chunks;  // the last chunk that begins with the run: lo .. hi - 1
-    while (hi - lo > 1) {
-        const long long mid = (lo + hi) / 2;
-        if (key[mid * a.chunk] == id) lo = mid;
-        else hi = mid;
-    }
-    const long long parts = lo - g + 1;  // the first is this chunk's second
+    const unsigned items = *a.crossings;
     const int lane = threadIdx.x % LG, group = threadIdx.x / LG;
-    const long long c = ((long long)blockIdx.y * LG + lane) * V, share = (parts + kGroups - 1) / kGroups;
-    const int count = c >= a.dim ? 0 : a.dim - c < V ? (int)(a.dim - c) : V;
-    float sum[V] = {0.f, 0.f, 0.f, 0.f};
-    if (count > 0)
-        for (long long p = group * share; p < parts && p < (group + 1) * share; p++) {
-            const Some<float> x = load_some<float>(a.part + ((g + p) * 2 + (p == 0)) * a.dim + c, count);
+    // parts p .. end - 1 of the run of chunk g, whose first is that chunk's second, from column c on
+    auto add = [&](float (&sum)[V], long long g, long long p, long long end, long long c, int count) {
+        for (; p < end; p += kAhead) {
+            Some<float> x[kAhead];
 #pragma unroll
-            for (int e = 0; e < V; e++) sum[e] += x[e];
+            for (int u = 0; u < kAhead; u++)
+                x[u] = p + u < end ? load_some<float>(a.part + ((g + p + u) * 2 + (p + u == 0)) * a.dim + c, count) : Some<float>{};
+#pragma unroll
+            for (int u = 0; u < kAhead; u++)
+#pragma unroll
+                for (int e = 0; e < V; e++) sum[e] += x[u][e];
         }
-    for (int e = 0; e < V; e++) box[group][lane * V + e] = sum[e];
-    __syncthreads();
-    if (group > 0 || count == 0) return;
-    const int used = parts < kGroups ? (int)parts : kGroups;
-    for (int i = 1; i < used; i++)
-        for (int e = 0; e < V; e++) sum[e] += box[i][lane * V + e];
-    write_sum<O, V>(a, id, c, count, sum);
+    };
+    for (unsigned item = blockIdx.x; item < items; item += gridDim.x) {
+        const long long g = a.crossing[item];
+        const unsigned id = key[(g + 1) * a.chunk - 1];
+        long long lo = g + 1, hi = g + 2;  // the last chunk that begins with the run: lo .. hi - 1
+        while (hi < a.chunks && key[hi * a.chunk] == id) {
+            lo = hi;
+            hi = g + 2 * (hi - g);
+        }
+        if (hi > a.chunks) hi = a.chunks;
+        while (hi - lo > 1) {
+            const long long mid = (lo + hi) / 2;
+            if (key[mid * a.chunk] == id) lo = mid;
+            else hi = mid;
+        }
+        const long long parts = lo - g + 1;
+        if (parts <= kFew) {
+            if (blockIdx.y > 0) continue;
+            for (long long c = threadIdx.x * V; c < a.dim; c += 256 * V) {
+                const int count = a.dim - c < V ? (int)(a.dim - c) : V;
+                float sum[V] = {0.f, 0.f, 0.f, 0.f};
+                add(sum, g, 0, parts, c, count);
+                write_sum<O, V>(a, id, c, count, sum);
+            }
+            continue;
+        }
+        const long long share = (parts + kGroups - 1) / kGroups;
+        for (long long slab = blockIdx.y; slab * LG * V < a.dim; slab += gridDim.y) {
+            const long long c = (slab * LG + lane) * V;
+            const int count = c >= a.dim ? 0 : a.dim - c < V ? (int)(a.dim - c) : V;
+            float sum[V] = {0.f, 0.f, 0.f, 0.f};
+            if (count > 0) add(sum, g, group * share, (group + 1) * share < parts ? (group + 1) * share : parts, c, count);
+#pragma unroll
+            for (int e = 0; e < V; e++) box[group][lane * V + e] = sum[e];
+            __syncthreads();
+            if (group == 0 && count > 0) {
+                for (int i = 1; i < kGroups; i++)
+#pragma unroll
+                    for (int e = 0; e < V; e++) sum[e] += box[i][lane * V + e];
+                write_sum<O, V>(a, id, c, count, sum);
+            }
+            __syncthreads();
+        }
+    }
 }
 
 static const char *bad_type(int dtype) { return dtype < LOGOSKG_F32 || dtype > LOGOSKG_F16 ? "unknown type" : nullptr; }
@@ -377,6 +471,8 @@ static long long plan_grad(GradArgs &a, char *w) {
     a.count = (unsigned *)take(few ? 0 : ((long long)a.tiles << kMostDigitBits) * 4);
     a.total = (unsigned *)take(few ? 0 : 4 << kMostDigitBits);
     a.part = (float *)take(a.chunks * 2 * a.dim * 4);
+    a.crossings = (unsigned *)take(4);
+    a.crossing = (unsigned *)take(a.chunks * 4);
     return at;
 }
 
@@ -398,25 +494,35 @@ static const char *grad_args(const logoskg_embedding_grad *e, GradArgs *a) {
     return nullptr;
 }
 
+template <class O> __global__ __launch_bounds__(256) void k_clear_table(GradArgs a) { clear_share<O, 256>(a, 0, blockIdx.x); }
+
 template <class T, class O> static logoskg_status launch_grad(GradArgs &a, hipStream_t st) {
-    if (!a.accumulate) {
-        const long long all = (a.dim * (long long)sizeof(O) + 15) / 16 * a.num_entities, blocks = (all + 255) / 256;
-        k_clear_rows<O><<<dim3((unsigned)(blocks > 8192 ? 8192 : blocks)), 256, 0, st>>>(a);
+    const long long bytes = a.accumulate ? 0 : a.num_entities * a.dim * (long long)sizeof(O);
+    auto clear_blocks = [&](int clears, int threads) {  // eight chunks a thread, up to eight blocks of 256 threads a compute unit
+        const long long blocks = (bytes / clears + threads * 128 - 1) / (threads * 128), most = 2048 * 256 / threads;
+        a.clears = clears;
+        a.clear_blocks = (int)(blocks < most ? blocks : most);
+    };
+    if (a.num_ids == 0) {
+        clear_blocks(1, 256);
+        if (a.clear_blocks) k_clear_table<O><<<dim3(a.clear_blocks), 256, 0, st>>>(a);
         LKG_HIP(hipGetLastError());
+        return LOGOSKG_OK;
     }
-    if (a.num_ids == 0) return LOGOSKG_OK;
     if (a.num_ids <= kSortTile) {
-        k_sort_few<<<1, 1024, 0, st>>>(a);
+        clear_blocks(1, 1024);
+        k_sort_few<O><<<dim3(1 + a.clear_blocks), 1024, 0, st>>>(a);
         LKG_HIP(hipGetLastError());
     } else {
         const int passes = (a.bits + kMostDigitBits - 1) / kMostDigitBits;
+        clear_blocks(2 * passes, 256);
         for (int pass = 0, shift = 0; pass < passes; pass++) {
             const int bits = (a.bits - shift + passes - pass - 1) / (passes - pass);
-            k_sort_count<<<dim3(a.tiles), 256, 4 << bits, st>>>(a, pass, shift, bits);
+            k_sort_count<O><<<dim3(a.tiles + a.clear_blocks), 256, 4 << bits, st>>>(a, pass, shift, bits);
             LKG_HIP(hipGetLastError());
             k_sort_before<<<dim3(1 << bits), 256, 0, st>>>(a);
             LKG_HIP(hipGetLastError());
-            k_sort_move<<<dim3(a.tiles), 256, 16 << bits, st>>>(a, pass, shift, bits);
+            k_sort_move<O><<<dim3(a.tiles + a.clear_blocks), 256, 16 << bits, st>>>(a, pass, shift, bits);
             LKG_HIP(hipGetLastError());
             shift += bits;
         }
@@ -425,8 +531,9 @@ template <class T, class O> static logoskg_status launch_grad(GradArgs &a, hipSt
     const long long lanes = (a.dim * (long long)sizeof(T) + 15) / 16;
     const int LG = lanes <= 4 ? 4 : lanes <= 16 ? 16 : 64;
     const dim3 grid((unsigned)((a.chunks + 256 / LG - 1) / (256 / LG)), (unsigned)((lanes + LG - 1) / LG));
-    const dim3 join((unsigned)a.chunks, (unsigned)((a.dim + 63) / 64));
-    if (grid.y > 65535 || join.y > 65535) { set_error("logoskg_embed_entities_backward: rows of %lld elements", a.dim); return LOGOSKG_EINVAL; }
+    const long long slabs = (a.dim + 63) / 64;
+    const dim3 join((unsigned)(a.chunks < 1024 ? a.chunks : 1024), (unsigned)(slabs < 16 ? slabs : 16));
+    if (grid.y > 65535) { set_error("logoskg_embed_entities_backward: rows of %lld elements", a.dim); return LOGOSKG_EINVAL; }
     if (LG == 4) k_embed_sum<T, O, 4><<<grid, 256, 0, st>>>(a);
     else if (LG == 16) k_embed_sum<T, O, 16><<<grid, 256, 0, st>>>(a);
     else k_embed_sum<T, O, 64><<<grid, 256, 0, st>>>(a);

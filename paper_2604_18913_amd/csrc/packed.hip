@@ -113,15 +113,20 @@ __device__ __forceinline__ f32x4 mfma16(Vec8<fp16>::type a, Vec8<fp16>::type b, 
 
 // Eight codes c of a word as 16 + c in 16 bits: a code's four bits become the highest of the mantissa of 16.  Codes 0 and 4,
 // 1 and 5, .. stand side by side.
-template <class E> __device__ __forceinline__ typename Vec8<E>::type codes8(unsigned w);
-template <> __device__ __forceinline__ Vec8<bf16>::type codes8<bf16>(unsigned w) {
-    const unsigned m = 0x00780078u, one = 0x41804180u;
-    return as8<bf16>(u32x4{(w << 3 & m) | one, (w >> 1 & m) | one, (w >> 5 & m) | one, (w >> 9 & m) | one});
+// (`sixteens`: twice 16, in a vector register, so that "and" and "or" are one instruction, which takes one constant.)
+template <class E> constexpr unsigned kSixteens = std::is_same<E, bf16>::value ? 0x41804180u : 0x4c004c00u;
+template <class E> __device__ __forceinline__ typename Vec8<E>::type codes8(unsigned w, unsigned sixteens) {
+    if (std::is_same<E, bf16>::value) {
+        const unsigned m = 0x00780078u;
+        return as8<E>(u32x4{(w << 3 & m) | sixteens, (w >> 1 & m) | sixteens, (w >> 5 & m) | sixteens, (w >> 9 & m) | sixteens});
+    }
+    const unsigned m = 0x03c003c0u;
+    return as8<E>(u32x4{(w << 6 & m) | sixteens, (w << 2 & m) | sixteens, (w >> 2 & m) | sixteens, (w >> 6 & m) | sixteens});
 }
-template <> __device__ __forceinline__ Vec8<fp16>::type codes8<fp16>(unsigned w) {
-    const unsigned m = 0x03c003c0u, one = 0x4c004c00u;
-    return as8<fp16>(u32x4{(w << 6 & m) | one, (w << 2 & m) | one, (w >> 2 & m) | one, (w >> 6 & m) | one});
-}
+
+// acc + the sum of two neighbours
+__device__ __forceinline__ float both_added(Pair<bf16>::type x, float acc) { return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(Pair<short>::type, x), Pair<short>::type{0x3f80, 0x3f80}, acc, false); }
+__device__ __forceinline__ float both_added(Pair<fp16>::type x, float acc) { return __builtin_amdgcn_fdot2(x, Pair<fp16>::type{(fp16)1.f, (fp16)1.f}, acc, false); }
 
 __device__ __forceinline__ float quarters_max(float x) { x = fmaxf(x, __shfl_xor(x, 16)); return fmaxf(x, __shfl_xor(x, 32)); }
 __device__ __forceinline__ float quarters_sum(float x) { x += __shfl_xor(x, 16); return x + __shfl_xor(x, 32); }
@@ -130,7 +135,7 @@ struct PackedArgs {
     ReadArgs r;
     long long row_bytes;              // stride
     int heads_in, rows_in, streams;   // of a block: key heads, groups of 16 rows, wavefronts that share a head's tiles
-    int row_groups;
+    int row_groups, ways;             // of 16 / ways rows
     int table_words;                  // of biases, per key head
 };
 
@@ -139,23 +144,48 @@ constexpr int kPackedTile = 64;  // entries of a wavefront at a time
 // Bytes of a wavefront's piece of LDS: values' codes, scales and bases, ids and places of biases.
 constexpr int piece_bytes(int groups) { return kPackedTile * (16 * groups + 16 * groups + 4); }
 
-// One block: 2^shift entries of a list, some key heads and groups of 16 rows (token, head of the group); a wavefront has one
-// of each, and every so manieth tile of 64 entries.  With x = base + scale c (a group of 32 elements),
+// N scores of a lane under a cap, in place: by the near form where all of the wavefront's are near, as cap_scores.
+template <int N> __device__ __forceinline__ void cap_some(const ScoreArgs &s, float (&z)[N]) {
+    float size = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; e++) size = fmaxf(size, __builtin_fabsf(z[e]));
+    const bool far = wave_any(size > s.most);
+#pragma unroll
+    for (int j = 0; j < N; j += 4) {
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) y[e] = near_capped(s, z[j + e]);
+        if (far) {
+#pragma unroll
+            for (int e = 0; e < 4; e++) y[e] = any_capped(s, z[j + e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; e++) z[j + e] = y[e];
+    }
+}
+
+// One block: 2^shift entries of a list, some key heads and groups of 16 / WAYS rows (token, head of the group); a wavefront has
+// one of each, and every so manieth tile of 64 entries.  With x = base + scale c (a group of 32 elements),
 //     q.k = sum over groups of scale (q . c) + base (sum of q),      out = sum of (p scale) c + p base :
 // the matrix instructions take the codes as they are, as 16 + c (see codes8), and the scales stay in 32 bits: those of the keys
-// are factors of a group's product, those of the values go into the weights, which are rounded to 16 bits for the second product
-// (as p itself is elsewhere).  16 + c would let that rounding weigh as much as the code is large: a third product, of the weights
-// and -23.5, makes it c - 7.5, and 7.5 scale goes to the base.
+// are factors of a group's product (which begins at -16 times the sum of q), those of the values go into the weights, which are
+// rounded to 16 bits for the second product (as p itself is elsewhere).  16 + c would let that rounding weigh as much as the
+// code is large: the sum of the rounded weights times 23.5 is taken off, which makes it c - 7.5, and 7.5 scale goes to the base.
 //
 // Keys go from memory into the registers that the instruction reads; values' codes lie in LDS as they come, and the transposing
-// 4-bit read gives a lane one element of 16 entries.  Tile row p = 16 a + 4 b + c holds entry 16 b + 4 a + c, so that these
-// are the entries whose scores the lane has.
-template <class E, int NG, bool CAP, bool BIAS>
-__global__ __launch_bounds__(512) void k_read_packed(PackedArgs pa) {
+// 4-bit read gives a lane one element of 16 entries.
+//
+// The instructions' 16 columns are rows of q.  Eight rows or fewer leave columns empty, and with them most of the lanes' work
+// between the two products: then the columns stand WAYS times for the rows, each time for other entries of the tile (16
+// neighbours of every 16 WAYS).  A lane keeps of the first product what is its own entries', its weights stand in the
+// second one's operand beside zeros, and the ways' sums are joined at the end.
+template <class E, int NG, int WAYS, bool CAP, bool BIAS>
+__global__ __launch_bounds__(512, NG <= 2 ? 4 : 2) void k_read_packed(PackedArgs pa) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const ReadArgs &a = pa.r;
-    constexpr int kBytes = 16 * NG, kOut = 2 * NG, kPiece = piece_bytes(NG);
+    constexpr int kBytes = 16 * NG, kOut = 2 * NG, kPiece = piece_bytes(NG), kRows = 16 / WAYS, kTiles = 4 / WAYS, kMine = 16 / WAYS;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, quarter = lane >> 4;
+    const int way = col / kRows, my = 16 * way + 4 * quarter;  // a lane's entries of a tile: my .. my + 3 of every 16 WAYS
     const int units = pa.heads_in * pa.rows_in, unit = wave % units, stream = wave / units;
     char *codes = lds + wave * kPiece;
     float *params = (float *)(codes + kPackedTile * kBytes);  // [NG][key scale, key base, value scale, value base][64]
@@ -177,7 +207,51 @@ __global__ __launch_bounds__(512) void k_read_packed(PackedArgs pa) {
     const int32_t *entity = a.entity ? a.entity + e0 + from : nullptr;
     const uint8_t *hop = a.hop ? a.hop + e0 + from : nullptr;
 
-    const int row_group = blockIdx.y * pa.rows_in + unit / pa.heads_in, vr = row_group * 16 + col;
+    const char *rows = (const char *)a.keys;
+    const int all = a.kv_heads * NG;
+    const unsigned row_bytes = (unsigned)pa.row_bytes;
+    auto id_of = [&](int t) {
+        const int at = t * kPackedTile + lane;
+        if (at >= n) return -1;
+        const long long id = entity ? entity[at] : e0 + from + at;
+        return id >= 0 && id < a.num_entities ? (int)id : -1;
+    };
+    auto hop_of = [&](int t) {
+        const int at = t * kPackedTile + lane;
+        return hop && at < n ? (int)hop[at] : 0;
+    };
+    // Rows of the tile of codes: row 16 h + j holds the entry whose weight is element j of quarter h in the second product's
+    // operands (two steps of eight, see below).
+    auto entry_of = [](int p) {
+        const int h = p >> 4, j = p & 15, r = j & 3, sub = WAYS == 2 ? 2 * (j >> 2 & 1) + (j >> 3) : j >> 2;
+        return 16 * sub + 4 * h + r;
+    };
+    unsigned k[4][NG];
+    u32x4 v[NG];
+    u64 param[NG];
+    auto row_of = [&](int id) { return rows + (u64)(unsigned)id * row_bytes; };
+    auto fetch = [&](int id) {  // (the first row stands in for entries that are left out: their scales, bases and weights are 0)
+        const int in = id < 0 ? 0 : id;
+#pragma unroll
+        for (int t = 0; t < 4; t++) {
+            const unsigned *at = (const unsigned *)(row_of(__shfl(in, 16 * t + col)) + head * kBytes) + quarter * NG;
+#pragma unroll
+            for (int i = 0; i < NG; i++) k[t][i] = at[i];
+        }
+#pragma unroll
+        for (int i = 0; i < NG; i++) {
+            const int chunk = i * 64 + lane;
+            v[i] = *(const u32x4 *)(row_of(__shfl(in, entry_of(chunk / NG))) + 16 * all + head * kBytes + chunk % NG * 16);
+        }
+#pragma unroll
+        for (int i = 0; i < NG; i++) param[i] = *(const u64 *)(row_of(in) + 32 * all + (head * NG + i) * 8);
+    };
+    const int tiles = a.num_entities > 0 ? (n + kPackedTile - 1) / kPackedTile : 0;
+    int id = id_of(stream), next_id = id_of(stream + pa.streams), now_hop = 0, next_hop = 0;
+    if (BIAS) now_hop = hop_of(stream), next_hop = hop_of(stream + pa.streams);
+    if (stream < tiles) fetch(id);
+
+    const int row_group = blockIdx.y * pa.rows_in + unit / pa.heads_in, vr = row_group * kRows + col % kRows;
     const bool mine = vr < a.rows;
     const int token = mine ? vr / a.group : 0, g = mine ? vr % a.group : 0;
     const long long place = ((long long)d * a.tokens + token) * a.heads + head * a.group + g;
@@ -201,54 +275,24 @@ __global__ __launch_bounds__(512) void k_read_packed(PackedArgs pa) {
         for (int h = 0; h < pa.heads_in; h++) bias_to_lds<E>(tables + h * pa.table_words, a.score, (first_head + h) * a.group, a.group, tid, blockDim.x);
         __syncthreads();
     }
-    f32x4 o[kOut], shift_sum[NG];
-    float base_sum[NG];
+    f32x4 o[kOut];
+    float base_sum[NG], weight_sum[NG];
 #pragma unroll
     for (int i = 0; i < kOut; i++) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < NG; i++) shift_sum[i] = f32x4{0.f, 0.f, 0.f, 0.f}, base_sum[i] = 0.f;
+    for (int i = 0; i < NG; i++) base_sum[i] = weight_sum[i] = 0.f;
     float m = kLowest, l = 0.f;
-    float unit_scale = sizeof(E) == 2 && !std::is_same<E, bf16>::value ? 0.f : 1.f;  // of the weights: see below
-    typename Vec8<E>::type shift_by;
-#pragma unroll
-    for (int e = 0; e < 8; e++) shift_by[e] = (E)-23.5f;
+    float unit_scale = std::is_same<E, bf16>::value ? 1.f : 0.f;  // of the weights: see below
+    unsigned sixteens = kSixteens<E>;
+    here(sixteens);
+    // of the second product's two steps, the lanes and halves of registers that a weight stands in
+    const unsigned keep[2] = {WAYS == 1 ? ~0u : WAYS == 2 ? (way == 0 ? ~0u : 0u) : way == 0 ? 0xffffu : way == 1 ? 0xffff0000u : 0u,
+                              WAYS == 1 ? ~0u : WAYS == 2 ? (way == 1 ? ~0u : 0u) : way == 2 ? 0xffffu : way == 3 ? 0xffff0000u : 0u};
+    // chunks of a row of the tile of codes change places, so that the 16 rows that a read goes down lie in different banks
+    constexpr int kTurn = NG == 4 ? 3 : NG == 2 ? 1 : 0;
+    const unsigned codes_at = lds_place(codes) + (16 * quarter + col) * kBytes + ((NG == 4 ? col >> 2 : col >> 3) & kTurn) * 16;
+    char *codes_to = codes + lane / NG * kBytes + ((lane % NG) ^ ((lane >> 4) & kTurn)) * 16;
 
-    const char *rows = (const char *)a.keys;
-    const int all = a.kv_heads * NG;
-    auto id_of = [&](int t) {
-        const int at = t * kPackedTile + lane;
-        if (at >= n) return -1;
-        const long long id = entity ? entity[at] : e0 + from + at;
-        return id >= 0 && id < a.num_entities ? (int)id : -1;
-    };
-    auto hop_of = [&](int t) {
-        const int at = t * kPackedTile + lane;
-        return hop && at < n ? (int)hop[at] : 0;
-    };
-    unsigned k[4][NG];
-    u32x4 v[NG];
-    u64 param[NG];
-    auto fetch = [&](int id) {
-#pragma unroll
-        for (int t = 0; t < 4; t++) {
-            const int of = __shfl(id, 16 * t + col);
-            const unsigned *at = (const unsigned *)(rows + (long long)of * pa.row_bytes) + head * 4 * NG + quarter * NG;
-#pragma unroll
-            for (int i = 0; i < NG; i++) k[t][i] = of >= 0 ? at[i] : 0u;
-        }
-#pragma unroll
-        for (int i = 0; i < NG; i++) {
-            const int chunk = i * 64 + lane, p = chunk / NG, part = chunk % NG;
-            const int of = __shfl(id, 16 * ((p >> 2) & 3) + 4 * (p >> 4) + (p & 3));
-            v[i] = of >= 0 ? *(const u32x4 *)(rows + (long long)of * pa.row_bytes + 16 * all + head * kBytes + part * 16) : u32x4{0, 0, 0, 0};
-        }
-#pragma unroll
-        for (int i = 0; i < NG; i++) param[i] = id >= 0 ? *(const u64 *)(rows + (long long)id * pa.row_bytes + 32 * all + (head * NG + i) * 8) : 0;
-    };
-    const int tiles = (n + kPackedTile - 1) / kPackedTile;
-    int id = id_of(stream), next_id = id_of(stream + pa.streams), now_hop = 0, next_hop = 0;
-    if (BIAS) now_hop = hop_of(stream), next_hop = hop_of(stream + pa.streams);
-    if (stream < tiles) fetch(id);
     for (int t = stream; t < tiles; t += pa.streams) {
         const u64 seen = __ballot(id >= 0);
         if (!std::is_same<E, bf16>::value) {
@@ -256,7 +300,7 @@ __global__ __launch_bounds__(512) void k_read_packed(PackedArgs pa) {
             // is about 1
             float top = 0.f;
 #pragma unroll
-            for (int i = 0; i < NG; i++) top = fmaxf(top, __builtin_fabsf(low_half((unsigned)(param[i] >> 32))));
+            for (int i = 0; i < NG; i++) top = id < 0 ? 0.f : fmaxf(top, __builtin_fabsf(low_half((unsigned)(param[i] >> 32))));
             if (wave_any(top * unit_scale > 1024.f || (unit_scale == 0.f && top > 0.f))) {
 #pragma unroll
                 for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
@@ -266,63 +310,75 @@ __global__ __launch_bounds__(512) void k_read_packed(PackedArgs pa) {
 #pragma unroll
                 for (int i = 0; i < kOut; i++) o[i] *= change;
 #pragma unroll
-                for (int i = 0; i < NG; i++) shift_sum[i] *= change;
+                for (int i = 0; i < NG; i++) weight_sum[i] *= change;
                 unit_scale = now;
             }
         }
-        // the tile's products, one per group of the elements
-        f32x4 z[4][NG];
 #pragma unroll
-        for (int b = 0; b < 4; b++)
-#pragma unroll
-            for (int i = 0; i < NG; i++) z[b][i] = mfma16(codes8<E>(k[b][i]), q[i], f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-        for (int i = 0; i < NG; i++) *(u32x4 *)(codes + (i * 64 + lane) * 16) = v[i];
+        for (int i = 0; i < NG; i++) *(u32x4 *)(NG == 3 ? codes + (i * 64 + lane) * 16 : codes_to + i * 1024) = v[i];
 #pragma unroll
         for (int i = 0; i < NG; i++) {
-            const unsigned kp = (unsigned)param[i], vp = (unsigned)(param[i] >> 32);
-            const float ks = low_half(kp), vs = low_half(vp);
-            params[(4 * i + 0) * 64 + lane] = ks;
-            params[(4 * i + 1) * 64 + lane] = __builtin_fmaf(-16.f, ks, high_half(kp));
+            const unsigned kp = id < 0 ? 0u : (unsigned)param[i], vp = id < 0 ? 0u : (unsigned)(param[i] >> 32);
+            const float vs = low_half(vp);
+            params[(4 * i + 0) * 64 + lane] = low_half(kp);
+            params[(4 * i + 1) * 64 + lane] = high_half(kp);
             params[(4 * i + 2) * 64 + lane] = vs * unit_scale;
             params[(4 * i + 3) * 64 + lane] = __builtin_fmaf(7.5f, vs, high_half(vp));
         }
         if (BIAS) places[lane] = distance_place(now_hop, q_pos, M);
         wave_sync();
+        float s[kMine];
+#pragma unroll
+        for (int b = 0; b < kTiles; b++) {
+            float y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < NG; i++) {  // a group's product, and its scale and base
+                const float begin = -16.f * q_sum[i];
+                f32x4 z = mfma16(codes8<E>(k[WAYS * b][i], sixteens), q[i], f32x4{begin, begin, begin, begin});
+#pragma unroll
+                for (int x = 1; x < WAYS; x++) {
+                    const f32x4 other = mfma16(codes8<E>(k[WAYS * b + x][i], sixteens), q[i], f32x4{begin, begin, begin, begin});
+#pragma unroll
+                    for (int e = 0; e < 4; e++) z[e] = way == x ? other[e] : z[e];
+                }
+                const f32x4 ks = *(const f32x4 *)(params + (4 * i + 0) * 64 + 16 * WAYS * b + my);
+                const f32x4 kb = *(const f32x4 *)(params + (4 * i + 1) * 64 + 16 * WAYS * b + my);
+#pragma unroll
+                for (int e = 0; e < 4; e++) y[e] = __builtin_fmaf(ks[e], z[e], __builtin_fmaf(kb[e], q_sum[i], y[e]));
+            }
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                here(y[e]);  // (else the compiler makes all scores behind the next branch, with what they are made of in registers until then)
+                s[4 * b + e] = y[e];
+            }
+        }
         id = next_id;
         now_hop = next_hop;
         if (t + pa.streams < tiles) fetch(id);
         next_id = id_of(t + 2 * pa.streams);
         if (BIAS) next_hop = hop_of(t + 2 * pa.streams);
-        f32x16 s;
+        if (CAP) cap_some(a.score, s);
 #pragma unroll
-        for (int b = 0; b < 4; b++) {
-            float y[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < NG; i++) {
-                const f32x4 ks = *(const f32x4 *)(params + (4 * i + 0) * 64 + 16 * b + 4 * quarter);
-                const f32x4 kb = *(const f32x4 *)(params + (4 * i + 1) * 64 + 16 * b + 4 * quarter);
-#pragma unroll
-                for (int e = 0; e < 4; e++) y[e] = __builtin_fmaf(ks[e], z[b][i][e], __builtin_fmaf(kb[e], q_sum[i], y[e]));
-            }
-#pragma unroll
-            for (int e = 0; e < 4; e++) s[4 * b + e] = y[e];
-        }
-        if (CAP) cap_scores<4>(a.score, s);
-        float top = kLowest;
-#pragma unroll
-        for (int b = 0; b < 4; b++) {
+        for (int b = 0; b < kTiles; b++) {
             int4 at = {0, 0, 0, 0};
-            if (BIAS) at = *(const int4 *)(places + 16 * b + 4 * quarter);
+            if (BIAS) at = *(const int4 *)(places + 16 * WAYS * b + my);
 #pragma unroll
             for (int e = 0; e < 4; e++) {
-                float y = CAP ? s[4 * b + e] : s[4 * b + e] * a.score.k;
-                if (BIAS) y += my_table[e == 0 ? at.x : e == 1 ? at.y : e == 2 ? at.z : at.w];
-                if (seen != ~0ull) y = seen >> (16 * b + 4 * quarter + e) & 1 ? y : -INFINITY;
-                s[4 * b + e] = y;
-                top = fmaxf(top, y);
+                if (!CAP) s[4 * b + e] *= a.score.k;
+                if (BIAS) s[4 * b + e] += my_table[e == 0 ? at.x : e == 1 ? at.y : e == 2 ? at.z : at.w];
             }
         }
+        if (seen != ~0ull) {
+#pragma unroll
+            for (int b = 0; b < kTiles; b++) {
+                const unsigned open = (unsigned)(seen >> (16 * WAYS * b + my));
+#pragma unroll
+                for (int e = 0; e < 4; e++) s[4 * b + e] = open >> e & 1 ? s[4 * b + e] : -INFINITY;
+            }
+        }
+        float top = kLowest;
+#pragma unroll
+        for (int e = 0; e < kMine; e++) top = fmaxf(top, s[e]);
         top = quarters_max(top);
         if (wave_any(top > m)) {
             const float up = fmaxf(m, top), shrink = exp2_fast(m - up);
@@ -331,35 +387,51 @@ __global__ __launch_bounds__(512) void k_read_packed(PackedArgs pa) {
 #pragma unroll
             for (int i = 0; i < kOut; i++) o[i] *= shrink;
 #pragma unroll
-            for (int i = 0; i < NG; i++) shift_sum[i] *= shrink, base_sum[i] *= shrink;
+            for (int i = 0; i < NG; i++) weight_sum[i] *= shrink, base_sum[i] *= shrink;
         }
 #pragma unroll
-        for (int r = 0; r < 16; r++) {
-            s[r] = exp2_fast(s[r] - m);
-            l += s[r];
+        for (int e = 0; e < kMine; e++) {
+            s[e] = exp2_fast(s[e] - m);
+            l += s[e];
         }
         typedef int v2i __attribute__((ext_vector_type(2)));
         typedef __attribute__((address_space(3))) v2i lds2;
 #pragma unroll
         for (int i = 0; i < NG; i++) {
-            typename Vec8<E>::type w[2];
+            u32x4 w[2];  // of the second product's two steps; element 2 r (+ 1) is entry r of a neighbourhood of 16 (of the next)
+            f32x4 ws[kTiles];
 #pragma unroll
-            for (int b = 0; b < 4; b++) {
-                const f32x4 vs = *(const f32x4 *)(params + (4 * i + 2) * 64 + 16 * b + 4 * quarter);
-                const f32x4 vb = *(const f32x4 *)(params + (4 * i + 3) * 64 + 16 * b + 4 * quarter);
+            for (int b = 0; b < kTiles; b++) {
+                const f32x4 vs = *(const f32x4 *)(params + (4 * i + 2) * 64 + 16 * WAYS * b + my);
+                const f32x4 vb = *(const f32x4 *)(params + (4 * i + 3) * 64 + 16 * WAYS * b + my);
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
                     base_sum[i] = __builtin_fmaf(s[4 * b + e], vb[e], base_sum[i]);
-                    w[b >> 1][2 * e + (b & 1)] = (E)(s[4 * b + e] * vs[e]);
+                    ws[b][e] = s[4 * b + e] * vs[e];
                 }
             }
-            shift_sum[i] = mfma16(shift_by, w[0], shift_sum[i]);
-            shift_sum[i] = mfma16(shift_by, w[1], shift_sum[i]);
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                if (WAYS == 1) {
+#pragma unroll
+                    for (int j = 0; j < 2; j++) {
+                        const unsigned x = rounded2<E>(ws[2 * j % kTiles][e], ws[(2 * j + 1) % kTiles][e]);
+                        weight_sum[i] = both_added(__builtin_bit_cast(typename Pair<E>::type, x), weight_sum[i]);  // (of w[j][e] it would take w[j][0])
+                        w[j][e] = x;
+                    }
+                } else {
+                    const unsigned x = rounded2<E>(ws[0][e], ws[kTiles - 1][e]);
+                    const unsigned once = WAYS == 2 ? x : x & 0xffffu;
+                    weight_sum[i] = both_added(__builtin_bit_cast(typename Pair<E>::type, once), weight_sum[i]);
+                    w[0][e] = x & keep[0];
+                    w[1][e] = x & keep[1];
+                }
+            }
 #pragma unroll
             for (int j = 2 * i; j < 2 * i + 2; j++) {
-                const v2i x = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds2 *)(uintptr_t)(lds_place(codes) + (16 * quarter + col) * kBytes + 8 * j));
-                o[j] = mfma16(codes8<E>((unsigned)x[0]), w[0], o[j]);
-                o[j] = mfma16(codes8<E>((unsigned)x[1]), w[1], o[j]);
+                const v2i x = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds2 *)(uintptr_t)((codes_at ^ (NG == 3 ? 0 : i << 4)) + (NG == 3 ? i << 4 : 0) + (j & 1) * 8));
+                o[j] = mfma16(codes8<E>((unsigned)x[0], sixteens), as8<E>(w[0]), o[j]);
+                o[j] = mfma16(codes8<E>((unsigned)x[1], sixteens), as8<E>(w[1]), o[j]);
             }
         }
         wave_sync();
@@ -368,11 +440,21 @@ __global__ __launch_bounds__(512) void k_read_packed(PackedArgs pa) {
     const float back = unit_scale > 0.f ? 1.f / unit_scale : 1.f;
     l = quarters_sum(l);
 #pragma unroll
-    for (int i = 0; i < NG; i++) base_sum[i] = quarters_sum(base_sum[i]);
+    for (int i = 0; i < NG; i++) base_sum[i] = quarters_sum(base_sum[i]), weight_sum[i] = -23.5f * quarters_sum(weight_sum[i]);
 #pragma unroll
     for (int j = 0; j < kOut; j++)
 #pragma unroll
-        for (int e = 0; e < 4; e++) o[j][e] = __builtin_fmaf(o[j][e] + shift_sum[j / 2][e], back, base_sum[j / 2]);
+        for (int e = 0; e < 4; e++) o[j][e] = __builtin_fmaf(o[j][e] + weight_sum[j / 2], back, base_sum[j / 2]);
+#pragma unroll
+    for (int x = kRows; x < 16; x <<= 1) {  // the ways' sums together
+        const float om = __shfl_xor(m, x), ol = __shfl_xor(l, x), up = fmaxf(m, om), mine_by = exp2_fast(m - up), other_by = exp2_fast(om - up);
+        l = l * mine_by + ol * other_by;
+#pragma unroll
+        for (int j = 0; j < kOut; j++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) o[j][e] = o[j][e] * mine_by + __shfl_xor(o[j][e], x) * other_by;
+        m = up;
+    }
     if (pa.streams > 1) {  // joined with the others that have the same rows, in their order
         __syncthreads();
         float *box = (float *)(lds + wave * kPiece);
@@ -393,7 +475,7 @@ __global__ __launch_bounds__(512) void k_read_packed(PackedArgs pa) {
             for (int j = 0; j < kOut; j++) o[j] = o[j] * mine_by + *(const f32x4 *)(other + (j * 64 + lane) * 4) * other_by;
         }
     }
-    if (!mine) return;
+    if (!mine || way > 0) return;
     if (alone) {
         const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
 #pragma unroll
@@ -441,7 +523,8 @@ static logoskg_status packed_args(const logoskg_entity_read *r, PackedArgs *pa, 
     a->out = r->out; a->lse = r->lse;
     // A block's eight wavefronts: as many key heads as divide theirs (whose rows lie side by side) and have room for their biases,
     // then groups of 16 rows, then streams of tiles.
-    pa->row_groups = (a->rows + 15) / 16;
+    pa->ways = a->rows <= 4 ? 4 : a->rows <= 8 ? 2 : 1;
+    pa->row_groups = (a->rows * pa->ways + 15) / 16;
     pa->table_words = a->score.bias ? a->group * (2 * a->score.max_distance + 1) : 0;
     const int piece = piece_bytes((a->dim + 31) / 32);
     pa->heads_in = 1;
@@ -457,19 +540,22 @@ static logoskg_status packed_args(const logoskg_entity_read *r, PackedArgs *pa, 
     return LOGOSKG_OK;
 }
 
-template <class E, int NG, bool CAP, bool BIAS> static logoskg_status launch_packed(const PackedArgs &pa, hipStream_t st) {
+template <class E, int NG, int WAYS, bool CAP, bool BIAS> static logoskg_status launch_packed(const PackedArgs &pa, hipStream_t st) {
     const ReadArgs &a = pa.r;
     const int waves = pa.heads_in * pa.rows_in * pa.streams;
     const size_t bytes = (size_t)waves * piece_bytes(NG) + (size_t)pa.heads_in * pa.table_words * 4;
-    LKG_TRY(allow_lds(k_read_packed<E, NG, CAP, BIAS>, bytes));
-    k_read_packed<E, NG, CAP, BIAS><<<dim3((unsigned)((a.blocks + 7) / 8 * 8 * (a.kv_heads / pa.heads_in)), (unsigned)((pa.row_groups + pa.rows_in - 1) / pa.rows_in)), waves * 64, bytes, st>>>(pa);
+    LKG_TRY(allow_lds(k_read_packed<E, NG, WAYS, CAP, BIAS>, bytes));
+    k_read_packed<E, NG, WAYS, CAP, BIAS><<<dim3((unsigned)((a.blocks + 7) / 8 * 8 * (a.kv_heads / pa.heads_in)), (unsigned)((pa.row_groups + pa.rows_in - 1) / pa.rows_in)), waves * 64, bytes, st>>>(pa);
     LKG_HIP(hipGetLastError());
     return LOGOSKG_OK;
 }
-template <class E, int NG> static logoskg_status read_packed(const PackedArgs &pa, hipStream_t st) {
+template <class E, int NG, int WAYS> static logoskg_status launch_packed(const PackedArgs &pa, hipStream_t st) {
     const bool cap = pa.r.score.c > 0, bias = pa.r.score.bias != nullptr;
-    return cap ? bias ? launch_packed<E, NG, true, true>(pa, st) : launch_packed<E, NG, true, false>(pa, st)
-               : bias ? launch_packed<E, NG, false, true>(pa, st) : launch_packed<E, NG, false, false>(pa, st);
+    return cap ? bias ? launch_packed<E, NG, WAYS, true, true>(pa, st) : launch_packed<E, NG, WAYS, true, false>(pa, st)
+               : bias ? launch_packed<E, NG, WAYS, false, true>(pa, st) : launch_packed<E, NG, WAYS, false, false>(pa, st);
+}
+template <class E, int NG> static logoskg_status read_packed(const PackedArgs &pa, hipStream_t st) {
+    return pa.ways == 4 ? launch_packed<E, NG, 4>(pa, st) : pa.ways == 2 ? launch_packed<E, NG, 2>(pa, st) : launch_packed<E, NG, 1>(pa, st);
 }
 template <class E> static logoskg_status read_packed(const PackedArgs &pa, hipStream_t st) {
     const ReadArgs &a = pa.r;
