@@ -6,6 +6,7 @@ library is missing this module raises; there is no CPU fallback.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import weakref
 from typing import Optional, Sequence
@@ -184,6 +185,7 @@ def _check(rc: int):
         raise LogosKGError(rc, _load().logoskg_last_error().decode())
 
 
+@functools.lru_cache(None)
 def _torch():
     import torch
     return torch

@@ -12,6 +12,7 @@ static_assert(sizeof(logoskg_gradient) == 32, "the ctypes binding mirrors this l
 constexpr int kClipList = 64;           // tensors of a launch: they travel in its arguments
 constexpr long long kClipChunk = 8192;  // elements
 constexpr int kClipBlocks = 2048;       // of a launch, at most
+constexpr int kClipEach = 4096;         // sums that every block adds up again, which spares a launch
 constexpr int kClipTop = 2;             // doubles in front of the blocks' sums: the factor
 
 struct ClipArgs {
@@ -70,15 +71,17 @@ __global__ __launch_bounds__(256) void k_clip_squares(ClipArgs a) {
     if (threadIdx.x == 0) a.sums[kClipTop + a.first + blockIdx.x] = sum;
 }
 
-__global__ __launch_bounds__(256) void k_clip_norm(double *sums, int n, float max_norm, float scale, float *norm) {
-    __shared__ double box[4];
+// The norm and the factor of the blocks' sums, in every thread.
+__device__ __forceinline__ double factor_of(const double *sums, int n, float max_norm, float scale, double *box, double &norm) {
     double sum = 0.0;
     for (int i = threadIdx.x; i < n; i += 256) sum += sums[kClipTop + i];
-    sum = block_sum(sum, box);
-    if (threadIdx.x) return;
-    const double got = sqrt(sum) * fabs((double)scale);
-    *norm = (float)got;
-    sums[0] = got <= (double)max_norm ? (double)scale : (double)scale * ((double)max_norm / got);
+    norm = sqrt(block_sum(sum, box)) * fabs((double)scale);
+    return norm <= (double)max_norm ? (double)scale : (double)scale * ((double)max_norm / norm);
+}
+__global__ __launch_bounds__(256) void k_clip_norm(double *sums, int n, float max_norm, float scale, float *norm) {
+    __shared__ double box[4];
+    double got, by = factor_of(sums, n, max_norm, scale, box, got);
+    if (threadIdx.x == 0) *norm = (float)got, sums[0] = by;
 }
 
 template <class T, class O> __device__ __forceinline__ void scaled(const T *g, O *out, long long n, float by, int tid) {
@@ -105,8 +108,12 @@ template <class T> __device__ __forceinline__ void scaled_to(const ClipArgs &a, 
     else scaled(g, (fp16 *)a.out[t] + from, n, by, threadIdx.x);
 }
 
-__global__ __launch_bounds__(256) void k_clip_scale(ClipArgs a) {
-    const float by = (float)a.sums[0];
+// (n: the number of sums that every block adds up itself, or 0: the factor is made)
+__global__ __launch_bounds__(256) void k_clip_scale(ClipArgs a, int n, float max_norm, float scale, float *norm) {
+    __shared__ double box[4];
+    double got, factor = n ? factor_of(a.sums, n, max_norm, scale, box, got) : a.sums[0];
+    if (n && blockIdx.x == 0 && a.first == 0 && threadIdx.x == 0) *norm = (float)got;
+    const float by = (float)factor;
     for (long long c = blockIdx.x; c < a.chunks; c += gridDim.x) {
         const int t = tensor_of(a, c);
         const long long from = (c - a.begin[t]) * kClipChunk, n = a.n[t] - from < kClipChunk ? a.n[t] - from : kClipChunk;
@@ -217,11 +224,14 @@ extern "C" logoskg_status logoskg_clip_gradients(int32_t device, const logoskg_g
         return (went = hipGetLastError()) == hipSuccess;
     });
     LKG_HIP(went);
-    k_clip_norm<<<1, 256, 0, st>>>(sums, (int)n, max_norm, scale, norm);
-    LKG_HIP(hipGetLastError());
+    const bool each = n > 0 && n <= kClipEach;
+    if (!each) {
+        k_clip_norm<<<1, 256, 0, st>>>(sums, (int)n, max_norm, scale, norm);
+        LKG_HIP(hipGetLastError());
+    }
     each_launch(list, count, [&](ClipArgs &a, int blocks) {
         a.sums = sums;
-        k_clip_scale<<<dim3(blocks), 256, 0, st>>>(a);
+        k_clip_scale<<<dim3(blocks), 256, 0, st>>>(a, each ? (int)n : 0, max_norm, scale, norm);
         return (went = hipGetLastError()) == hipSuccess;
     });
     LKG_HIP(went);

@@ -52,7 +52,7 @@ template <class T, int LG> __global__ __launch_bounds__(256) void k_embed(EmbedA
 struct GradArgs {
     long long num_ids, num_entities, dim, row, chunks;
     int accumulate, chunk, tiles, bits;
-    int clears, clear_blocks;  // launches among which the rows that become zeros are divided, and blocks of each for it
+    int gaps;  // whether rows without an id are still to be cleared behind the sort
     float scale;
     const int32_t *ids;
     const void *dout;
@@ -60,10 +60,15 @@ struct GradArgs {
     unsigned *key[2], *place[2];  // of the sort: from one to the other and back
     unsigned *count, *total;      // [digits][tiles], [digits]
     float *part;                  // [chunks][2][dim]: of the run that comes in from the chunk before, and of the one that goes on
-    unsigned *crossings, *crossing;  // how many runs go on from the chunk that they begin in, and those chunks, in any order
+    // what the sums leave for the joins, in any order; how many of each: [0] runs that go on from the chunk that they begin in, [1] those of
+    // many chunks, [2] pieces of long gaps between ids
+    unsigned *crossings, *crossing;  // chunks of the runs: from [0] and from [chunks] on
+    uint2 *gap;                      // first row and the one behind
 };
 
-constexpr int kSortTile = 4096, kMostDigitBits = 11;
+constexpr int kMostChunk = 32, kFewParts = 16;      // entries of the sorted list; parts of a run that one block joins
+constexpr int kGapRows = 32, kGapPiece = 512;  // rows without an id that the sums' kernel clears between two ids; rows of a piece of more
+constexpr int kFewIds = 4096, kSortTile = 2048, kMostDigitBits = 11;
 
 __device__ __forceinline__ unsigned key_of(const GradArgs &a, long long i) {
     const int id = a.ids[i];
@@ -102,42 +107,33 @@ template <int THREADS> __device__ __forceinline__ unsigned block_before(unsigned
     return before + y - x;
 }
 
-// Rows [from, to) of the table become zeros, `blocks` blocks of THREADS threads side by side.  Rows that are written again later are
-// few where it costs much (a large table), and the sort beside which this runs leaves the memory idle.
-template <class O, int THREADS> __device__ __forceinline__ void clear_rows(const GradArgs &a, long long from, long long to, long long block, long long blocks) {
+// Rows [from, to) of the table become zeros, by a block.
+template <class O, int THREADS> __device__ __forceinline__ void clear_rows(const GradArgs &a, long long from, long long to) {
     constexpr int V = 16 / sizeof(O);
-    O *table = (O *)a.dtable;
-    if (a.row == a.dim) {  // one run of elements, whole chunks from the first aligned one on
-        O *p = table + from * a.dim, *end = table + to * a.dim;
-        const long long lead0 = ((16 - ((uintptr_t)p & 15)) & 15) / sizeof(O), lead = lead0 < end - p ? lead0 : end - p;
-        const long long chunks = (end - p - lead) / V, tail = lead + chunks * V;
-        if (block == 0) {
-            if (threadIdx.x < lead) p[threadIdx.x] = (O)0.f;
-            if (tail + threadIdx.x < end - p) p[tail + threadIdx.x] = (O)0.f;
-        }
-        Some<O> *whole = (Some<O> *)(p + lead);
-        for (long long i = block * THREADS + threadIdx.x; i < chunks; i += blocks * THREADS) whole[i] = Some<O>{};
+    const long long chunks = (a.dim + V - 1) / V;
+    if (a.row == a.dim && a.dim % V == 0) {  // one run of whole chunks
+        typename Loose<O>::type *p = (typename Loose<O>::type *)((O *)a.dtable + from * a.row);
+        for (long long i = threadIdx.x; i < (to - from) * chunks; i += THREADS) p[i] = Some<O>{};
         return;
     }
-    const long long per = (a.dim + V - 1) / V;
-    for (long long i = from * per + block * THREADS + threadIdx.x; i < to * per; i += blocks * THREADS) {
-        const long long e = i / per, c = i % per * V;
-        store_some<O>(table + e * a.row + c, Some<O>{}, a.dim - c < V ? (int)(a.dim - c) : V);
-    }
-}
-// .. the share of them that launch `at` of a.clears has (clear_blocks of its blocks, behind the others)
-template <class O, int THREADS> __device__ __forceinline__ void clear_share(const GradArgs &a, int at, long long block) {
-    clear_rows<O, THREADS>(a, a.num_entities * at / a.clears, a.num_entities * (at + 1) / a.clears, block, a.clear_blocks);
+    const int LG = chunks <= 4 ? 4 : chunks <= 16 ? 16 : 64, lane = threadIdx.x % LG;
+    for (long long e = from + threadIdx.x / LG; e < to; e += THREADS / LG)
+        for (long long c = (long long)lane * V; c < a.dim; c += LG * V) store_some<O>((O *)a.dtable + e * a.row + c, Some<O>{}, a.dim - c < V ? (int)(a.dim - c) : V);
 }
 
-// Lists of up to kSortTile ids: one block sorts them in LDS.
+// .. all of them, by `blocks` blocks
+template <class O, int THREADS> __device__ __forceinline__ void clear_table(const GradArgs &a, long long block, long long blocks) {
+    clear_rows<O, THREADS>(a, a.num_entities * block / blocks, a.num_entities * (block + 1) / blocks);
+}
+
+// Lists of up to kFewIds ids: one block sorts them in LDS, the others clear the table.
 template <class O> __global__ __launch_bounds__(1024) void k_sort_few(GradArgs a) {
-    __shared__ unsigned key[2][kSortTile];
-    __shared__ unsigned short place[2][kSortTile];
+    __shared__ unsigned key[2][kFewIds];
+    __shared__ unsigned short place[2][kFewIds];
     __shared__ unsigned count[16][256], box[16];
-    if (blockIdx.x > 0) return clear_share<O, 1024>(a, 0, blockIdx.x - 1);
+    if (blockIdx.x > 0) return clear_table<O, 1024>(a, blockIdx.x - 1, gridDim.x - 1);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = (int)a.num_ids, rounds = (n + 1023) / 1024;
-    if (tid == 0) *a.crossings = 0;
+    if (tid < 3) a.crossings[tid] = 0;
     for (int i = tid; i < n; i += 1024) key[0][i] = key_of(a, i), place[0][i] = (unsigned short)i;
     int from = 0;
     for (int shift = 0; shift < a.bits; shift += 8, from ^= 1) {
@@ -185,11 +181,10 @@ template <class O> __global__ __launch_bounds__(1024) void k_sort_few(GradArgs a
 }
 
 // A pass of the sort over tiles: how often a digit occurs in each tile ..
-template <class O> __global__ __launch_bounds__(256) void k_sort_count(GradArgs a, int pass, int shift, int bits) {
+__global__ __launch_bounds__(256) void k_sort_count(GradArgs a, int pass, int shift, int bits) {
     extern __shared__ unsigned found[];
-    if ((int)blockIdx.x >= a.tiles) return clear_share<O, 256>(a, 2 * pass, blockIdx.x - a.tiles);
     const int tid = threadIdx.x, digits = 1 << bits;
-    if (blockIdx.x == 0 && tid == 0) *a.crossings = 0;
+    if (pass == 0 && blockIdx.x == 0 && tid < 3) a.crossings[tid] = 0;
     for (int i = tid; i < digits; i += 256) found[i] = 0;
     __syncthreads();
     const long long from = (long long)blockIdx.x * kSortTile;
@@ -218,10 +213,9 @@ __global__ __launch_bounds__(256) void k_sort_before(GradArgs a) {
 }
 
 // .. and every id to its place: behind the smaller digits, those of the tiles before, the wavefronts before and the lanes before.
-template <class O> __global__ __launch_bounds__(256) void k_sort_move(GradArgs a, int pass, int shift, int bits) {
+__global__ __launch_bounds__(256) void k_sort_move(GradArgs a, int pass, int shift, int bits) {
     constexpr int kRounds = kSortTile / 256;
     extern __shared__ unsigned count[];  // [4][digits]
-    if ((int)blockIdx.x >= a.tiles) return clear_share<O, 256>(a, 2 * pass + 1, blockIdx.x - a.tiles);
     __shared__ unsigned box[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, digits = 1 << bits;
     unsigned *mine = count + wave * digits;
@@ -305,7 +299,6 @@ template <class O, int V> __device__ __forceinline__ void write_sum(const GradAr
 
 // A group of LG lanes adds up a chunk of the sorted list, each lane 16 bytes of a row; blockIdx.y: further columns.  The list of a
 // block's groups goes through LDS first, so that rows are asked for without a wait in between.
-constexpr int kMostChunk = 32;
 template <class T, class O, int LG> __global__ __launch_bounds__(256) void k_embed_sum(GradArgs a) {
     constexpr int V = 16 / sizeof(T), kAhead = 8, kGroups = 256 / LG;
     __shared__ unsigned keys[kGroups * kMostChunk + 2], places[kGroups * kMostChunk];
@@ -314,7 +307,7 @@ template <class T, class O, int LG> __global__ __launch_bounds__(256) void k_emb
     const long long first = (long long)blockIdx.x * kGroups * a.chunk;
     for (int i = tid; i < kGroups * a.chunk + 2; i += 256) {  // the one before and the one behind, too
         const long long at = first + i - 1;
-        keys[i] = at >= 0 && at < a.num_ids ? a.key[0][at] : none;
+        keys[i] = at < 0 ? ~0u : at < a.num_ids ? a.key[0][at] : none;
         if (i > 0 && i <= kGroups * a.chunk) places[i - 1] = at < a.num_ids ? a.place[0][at] : 0;
     }
     __syncthreads();
@@ -322,14 +315,29 @@ template <class T, class O, int LG> __global__ __launch_bounds__(256) void k_emb
     if (g >= a.chunks || c >= a.dim) return;
     const int count = a.dim - c < V ? (int)(a.dim - c) : V;
     const unsigned *key = keys + 1 + group * a.chunk, *place = places + group * a.chunk;
-    unsigned id = key[0];
-    if (id >= none) return;
-    bool came = key[-1] == id;  // the run began before this chunk
+    unsigned id = key[-1];  // (before the list: -1, behind which the first row comes)
+    bool came = id < none;  // the run began before this chunk
     float sum[V];
 #pragma unroll
     for (int e = 0; e < V; e++) sum[e] = 0.f;
     float *part = a.part + g * 2 * a.dim + c;
     const T *dout = (const T *)a.dout + c;
+    // rows between two ids, which no id names: zeros, here or, where there are many, by the next kernel
+    auto gap = [&](unsigned from, unsigned to) __attribute__((always_inline)) {
+        if (!a.gaps || from >= to) return;
+        if (to - from <= kGapRows) {
+            const O zeros[V] = {};
+            for (unsigned e = from; e < to; e++) store_sums<O, V>((O *)a.dtable + (long long)e * a.row + c, zeros, count);
+        } else if (blockIdx.y == 0) {
+            const int lanes = a.dim >= LG * V ? LG : (int)((a.dim + V - 1) / V);  // (of the group, those that are here)
+            const unsigned pieces = (to - from + kGapPiece - 1) / kGapPiece;
+            for (unsigned i = tid % LG; i < pieces; i += lanes) {
+                const unsigned begin = from + i * kGapPiece;
+                a.gap[atomicAdd(a.crossings + 2, 1u)] = uint2{begin, to - begin < kGapPiece ? to : begin + kGapPiece};
+            }
+        }
+    };
+    bool any = false;  // whether sum holds something: rows of this chunk's
 #pragma unroll 1
     for (int i = 0; i < a.chunk; i += kAhead) {
         Some<T> x[kAhead];
@@ -339,42 +347,55 @@ template <class T, class O, int LG> __global__ __launch_bounds__(256) void k_emb
 #pragma unroll
         for (int u = 0; u < kAhead; u++) {
             const unsigned k = key[i + u];
-            if (k >= none) continue;
             if (k != id) {
-                if (came) {
-                    store_sums<float, V>(part, sum, count);
-                } else {
-                    write_sum<O, V>(a, id, c, count, sum);
-                }
+                if (any) {
+                    if (came) {
+                        store_sums<float, V>(part, sum, count);
+                    } else {
+                        write_sum<O, V>(a, id, c, count, sum);
+                    }
 #pragma unroll
-                for (int e = 0; e < V; e++) sum[e] = 0.f;
+                    for (int e = 0; e < V; e++) sum[e] = 0.f;
+                    any = false;
+                }
+                gap(id + 1, k);
                 came = false;
                 id = k;
             }
+            if (k >= none) continue;
+            any = true;
 #pragma unroll
             for (int e = 0; e < V; e++) sum[e] += (float)x[u][e];
         }
     }
-    const bool goes_on = key[a.chunk] == id;
-    if (came || goes_on) {
-        if (!came) {
-            part += a.dim;
-            if (blockIdx.y == 0 && tid % LG == 0) a.crossing[atomicAdd(a.crossings, 1u)] = (unsigned)g;
+    if (any) {
+        const bool goes_on = key[a.chunk] == id;
+        if (came || goes_on) {
+            if (!came) {
+                part += a.dim;
+                if (blockIdx.y == 0 && tid % LG == 0) {
+                    const long long far = (g + kFewParts) * a.chunk;
+                    const bool many = far < a.num_ids && a.key[0][far] == id;
+                    a.crossing[(many ? a.chunks : 0) + atomicAdd(a.crossings + many, 1u)] = (unsigned)g;
+                }
+            }
+            store_sums<float, V>(part, sum, count);
+        } else {
+            write_sum<O, V>(a, id, c, count, sum);
         }
-        store_sums<float, V>(part, sum, count);
-    } else {
-        write_sum<O, V>(a, id, c, count, sum);
     }
+    if (g == a.chunks - 1 && id < none) gap(id + 1, none);
 }
 
-// Runs that cross chunks: blocks go through the list of them.  (Its order does not matter: each is a sum of its own.)  Runs of few
-// parts are added up by the blocks of the first column (blockIdx.y), a thread per four elements; those of many by 16 groups of 16
-// lanes, a share of the parts each, 64 elements per blockIdx.y.
+// Runs that cross chunks: blocks go through the lists of them.  (Their order does not matter: each is a sum of its own.)  Runs of up to
+// kFewParts parts are added up by a block each, a thread per four elements; longer ones by 16 groups of 16 lanes, a share of the parts
+// each, a block per 64 elements.  Then the long gaps.
 template <class O> __global__ __launch_bounds__(256) void k_embed_join(GradArgs a) {
-    constexpr int V = 4, LG = 16, kGroups = 16, kAhead = 4, kFew = 16;
+    constexpr int V = 4, LG = 16, kGroups = 16, kAhead = 4;
     __shared__ float box[kGroups][LG * V];
     const unsigned *key = a.key[0];
-    const unsigned items = *a.crossings;
+    const long long few = a.crossings[0], slabs = (a.dim + LG * V - 1) / (LG * V), runs = few + a.crossings[1] * slabs;
+    const long long items = runs + (a.gaps ? a.crossings[2] : 0);
     const int lane = threadIdx.x % LG, group = threadIdx.x / LG;
     // parts p .. end - 1 of the run of chunk g, whose first is that chunk's second, from column c on
     auto add = [&](float (&sum)[V], long long g, long long p, long long end, long long c, int count) {
@@ -389,8 +410,13 @@ template <class O> __global__ __launch_bounds__(256) void k_embed_join(GradArgs 
                 for (int e = 0; e < V; e++) sum[e] += x[u][e];
         }
     };
-    for (unsigned item = blockIdx.x; item < items; item += gridDim.x) {
-        const long long g = a.crossing[item];
+    for (long long item = blockIdx.x; item < items; item += gridDim.x) {
+        if (item >= runs) {  // rows that become zeros
+            const uint2 rows = a.gap[item - runs];
+            clear_rows<O, 256>(a, rows.x, rows.y);
+            continue;
+        }
+        const long long g = a.crossing[item < few ? item : a.chunks + (item - few) / slabs], slab = item < few ? 0 : (item - few) % slabs;
         const unsigned id = key[(g + 1) * a.chunk - 1];
         long long lo = g + 1, hi = g + 2;  // the last chunk that begins with the run: lo .. hi - 1
         while (hi < a.chunks && key[hi * a.chunk] == id) {
@@ -404,8 +430,7 @@ template <class O> __global__ __launch_bounds__(256) void k_embed_join(GradArgs 
             else hi = mid;
         }
         const long long parts = lo - g + 1;
-        if (parts <= kFew) {
-            if (blockIdx.y > 0) continue;
+        if (item < few) {
             for (long long c = threadIdx.x * V; c < a.dim; c += 256 * V) {
                 const int count = a.dim - c < V ? (int)(a.dim - c) : V;
                 float sum[V] = {0.f, 0.f, 0.f, 0.f};
@@ -414,23 +439,20 @@ template <class O> __global__ __launch_bounds__(256) void k_embed_join(GradArgs 
             }
             continue;
         }
-        const long long share = (parts + kGroups - 1) / kGroups;
-        for (long long slab = blockIdx.y; slab * LG * V < a.dim; slab += gridDim.y) {
-            const long long c = (slab * LG + lane) * V;
-            const int count = c >= a.dim ? 0 : a.dim - c < V ? (int)(a.dim - c) : V;
-            float sum[V] = {0.f, 0.f, 0.f, 0.f};
-            if (count > 0) add(sum, g, group * share, (group + 1) * share < parts ? (group + 1) * share : parts, c, count);
+        const long long c = (slab * LG + lane) * V, share = (parts + kGroups - 1) / kGroups;
+        const int count = c >= a.dim ? 0 : a.dim - c < V ? (int)(a.dim - c) : V;
+        float sum[V] = {0.f, 0.f, 0.f, 0.f};
+        if (count > 0) add(sum, g, group * share, (group + 1) * share < parts ? (group + 1) * share : parts, c, count);
 #pragma unroll
-            for (int e = 0; e < V; e++) box[group][lane * V + e] = sum[e];
-            __syncthreads();
-            if (group == 0 && count > 0) {
-                for (int i = 1; i < kGroups; i++)
+        for (int e = 0; e < V; e++) box[group][lane * V + e] = sum[e];
+        __syncthreads();
+        if (group == 0 && count > 0) {
+            for (int i = 1; i < kGroups; i++)
 #pragma unroll
-                    for (int e = 0; e < V; e++) sum[e] += box[i][lane * V + e];
-                write_sum<O, V>(a, id, c, count, sum);
-            }
-            __syncthreads();
+                for (int e = 0; e < V; e++) sum[e] += box[i][lane * V + e];
+            write_sum<O, V>(a, id, c, count, sum);
         }
+        __syncthreads();
     }
 }
 
@@ -463,16 +485,19 @@ static long long plan_grad(GradArgs &a, char *w) {
         at += up(bytes);
         return p;
     };
-    const bool few = a.num_ids <= kSortTile;
+    const bool few = a.num_ids <= kFewIds;
     for (int i = 0; i < 2; i++) {
         a.key[i] = (unsigned *)take(few && i ? 0 : a.num_ids * 4);
         a.place[i] = (unsigned *)take(few && i ? 0 : a.num_ids * 4);
     }
-    a.count = (unsigned *)take(few ? 0 : ((long long)a.tiles << kMostDigitBits) * 4);
+    const int passes = (a.bits + kMostDigitBits - 1) / kMostDigitBits;
+    a.count = (unsigned *)take(few ? 0 : ((long long)a.tiles << (a.bits + passes - 1) / passes) * 4);
     a.total = (unsigned *)take(few ? 0 : 4 << kMostDigitBits);
     a.part = (float *)take(a.chunks * 2 * a.dim * 4);
-    a.crossings = (unsigned *)take(4);
-    a.crossing = (unsigned *)take(a.chunks * 4);
+    a.crossings = (unsigned *)take(12);
+    a.crossing = (unsigned *)take(a.chunks * 8);
+    a.gaps = !few && !a.accumulate;
+    a.gap = (uint2 *)take(!a.gaps ? 0 : (a.num_ids + 1 + a.num_entities / kGapPiece + 1) * 8);
     return at;
 }
 
@@ -494,35 +519,29 @@ static const char *grad_args(const logoskg_embedding_grad *e, GradArgs *a) {
     return nullptr;
 }
 
-template <class O> __global__ __launch_bounds__(256) void k_clear_table(GradArgs a) { clear_share<O, 256>(a, 0, blockIdx.x); }
+template <class O> __global__ __launch_bounds__(256) void k_clear_table(GradArgs a) { clear_table<O, 256>(a, blockIdx.x, gridDim.x); }
 
 template <class T, class O> static logoskg_status launch_grad(GradArgs &a, hipStream_t st) {
-    const long long bytes = a.accumulate ? 0 : a.num_entities * a.dim * (long long)sizeof(O);
-    auto clear_blocks = [&](int clears, int threads) {  // eight chunks a thread, up to eight blocks of 256 threads a compute unit
-        const long long blocks = (bytes / clears + threads * 128 - 1) / (threads * 128), most = 2048 * 256 / threads;
-        a.clears = clears;
-        a.clear_blocks = (int)(blocks < most ? blocks : most);
-    };
+    const long long pieces = (a.num_entities + kGapPiece - 1) / kGapPiece;
+    // blocks that clear the whole table, for some 64 KB each
+    const long long some = a.num_entities * a.dim * (long long)sizeof(O) / (64 << 10) + 1, clears = a.accumulate ? 0 : some < 1024 ? some : 1024;
     if (a.num_ids == 0) {
-        clear_blocks(1, 256);
-        if (a.clear_blocks) k_clear_table<O><<<dim3(a.clear_blocks), 256, 0, st>>>(a);
+        if (!a.accumulate) k_clear_table<O><<<dim3((unsigned)clears), 256, 0, st>>>(a);
         LKG_HIP(hipGetLastError());
         return LOGOSKG_OK;
     }
-    if (a.num_ids <= kSortTile) {
-        clear_blocks(1, 1024);
-        k_sort_few<O><<<dim3(1 + a.clear_blocks), 1024, 0, st>>>(a);
+    if (a.num_ids <= kFewIds) {
+        k_sort_few<O><<<dim3((unsigned)(1 + clears)), 1024, 0, st>>>(a);
         LKG_HIP(hipGetLastError());
     } else {
         const int passes = (a.bits + kMostDigitBits - 1) / kMostDigitBits;
-        clear_blocks(2 * passes, 256);
         for (int pass = 0, shift = 0; pass < passes; pass++) {
             const int bits = (a.bits - shift + passes - pass - 1) / (passes - pass);
-            k_sort_count<O><<<dim3(a.tiles + a.clear_blocks), 256, 4 << bits, st>>>(a, pass, shift, bits);
+            k_sort_count<<<dim3(a.tiles), 256, 4 << bits, st>>>(a, pass, shift, bits);
             LKG_HIP(hipGetLastError());
             k_sort_before<<<dim3(1 << bits), 256, 0, st>>>(a);
             LKG_HIP(hipGetLastError());
-            k_sort_move<O><<<dim3(a.tiles + a.clear_blocks), 256, 16 << bits, st>>>(a, pass, shift, bits);
+            k_sort_move<<<dim3(a.tiles), 256, 16 << bits, st>>>(a, pass, shift, bits);
             LKG_HIP(hipGetLastError());
             shift += bits;
         }
@@ -531,15 +550,14 @@ template <class T, class O> static logoskg_status launch_grad(GradArgs &a, hipSt
     const long long lanes = (a.dim * (long long)sizeof(T) + 15) / 16;
     const int LG = lanes <= 4 ? 4 : lanes <= 16 ? 16 : 64;
     const dim3 grid((unsigned)((a.chunks + 256 / LG - 1) / (256 / LG)), (unsigned)((lanes + LG - 1) / LG));
-    const long long slabs = (a.dim + 63) / 64;
-    const dim3 join((unsigned)(a.chunks < 1024 ? a.chunks : 1024), (unsigned)(slabs < 16 ? slabs : 16));
+    const long long joins = a.chunks * ((a.dim + 63) / 64) + (a.gaps ? pieces : 0);
     if (grid.y > 65535) { set_error("logoskg_embed_entities_backward: rows of %lld elements", a.dim); return LOGOSKG_EINVAL; }
     if (LG == 4) k_embed_sum<T, O, 4><<<grid, 256, 0, st>>>(a);
     else if (LG == 16) k_embed_sum<T, O, 16><<<grid, 256, 0, st>>>(a);
     else k_embed_sum<T, O, 64><<<grid, 256, 0, st>>>(a);
     LKG_HIP(hipGetLastError());
-    if (a.chunks > 1) {
-        k_embed_join<O><<<join, 256, 0, st>>>(a);
+    if (a.chunks > 1 || a.gaps) {
+        k_embed_join<O><<<dim3((unsigned)(joins < 2048 ? joins : 2048)), 256, 0, st>>>(a);
         LKG_HIP(hipGetLastError());
     }
     return LOGOSKG_OK;

@@ -230,7 +230,8 @@ __global__ __launch_bounds__(512, NG <= 2 ? 4 : 2) void k_read_packed(PackedArgs
     u32x4 v[NG];
     u64 param[NG];
     auto row_of = [&](int id) { return rows + (u64)(unsigned)id * row_bytes; };
-    auto fetch = [&](int id) {  // (the first row stands in for entries that are left out: their scales, bases and weights are 0)
+    // (the first row stands in for entries that are left out: their scales, bases and weights are 0)
+    auto fetch_keys = [&](int id) {
         const int in = id < 0 ? 0 : id;
 #pragma unroll
         for (int t = 0; t < 4; t++) {
@@ -238,6 +239,9 @@ __global__ __launch_bounds__(512, NG <= 2 ? 4 : 2) void k_read_packed(PackedArgs
 #pragma unroll
             for (int i = 0; i < NG; i++) k[t][i] = at[i];
         }
+    };
+    auto fetch = [&](int id) {
+        const int in = id < 0 ? 0 : id;
 #pragma unroll
         for (int i = 0; i < NG; i++) {
             const int chunk = i * 64 + lane;
@@ -249,7 +253,7 @@ __global__ __launch_bounds__(512, NG <= 2 ? 4 : 2) void k_read_packed(PackedArgs
     const int tiles = a.num_entities > 0 ? (n + kPackedTile - 1) / kPackedTile : 0;
     int id = id_of(stream), next_id = id_of(stream + pa.streams), now_hop = 0, next_hop = 0;
     if (BIAS) now_hop = hop_of(stream), next_hop = hop_of(stream + pa.streams);
-    if (stream < tiles) fetch(id);
+    if (stream < tiles) fetch(id), fetch_keys(id);
 
     const int row_group = blockIdx.y * pa.rows_in + unit / pa.heads_in, vr = row_group * kRows + col % kRows;
     const bool mine = vr < a.rows;
@@ -271,8 +275,8 @@ __global__ __launch_bounds__(512, NG <= 2 ? 4 : 2) void k_read_packed(PackedArgs
     }
     const int q_pos = a.q_pos ? a.q_pos[d] : 0, M = a.score.max_distance;
     const float *my_table = tables + (unit % pa.heads_in) * pa.table_words + g * (2 * M + 1);
-    if (BIAS) {
-        for (int h = 0; h < pa.heads_in; h++) bias_to_lds<E>(tables + h * pa.table_words, a.score, (first_head + h) * a.group, a.group, tid, blockDim.x);
+    if (BIAS) {  // of the block's heads, one behind the other
+        bias_to_lds<E>(tables, a.score, first_head * a.group, pa.heads_in * a.group, tid, blockDim.x);
         __syncthreads();
     }
     f32x4 o[kOut];
@@ -327,6 +331,11 @@ __global__ __launch_bounds__(512, NG <= 2 ? 4 : 2) void k_read_packed(PackedArgs
         }
         if (BIAS) places[lane] = distance_place(now_hop, q_pos, M);
         wave_sync();
+        id = next_id;
+        now_hop = next_hop;
+        if (t + pa.streams < tiles) fetch(id);
+        next_id = id_of(t + 2 * pa.streams);
+        if (BIAS) next_hop = hop_of(t + 2 * pa.streams);
         float s[kMine];
 #pragma unroll
         for (int b = 0; b < kTiles; b++) {
@@ -352,11 +361,7 @@ __global__ __launch_bounds__(512, NG <= 2 ? 4 : 2) void k_read_packed(PackedArgs
                 s[4 * b + e] = y[e];
             }
         }
-        id = next_id;
-        now_hop = next_hop;
-        if (t + pa.streams < tiles) fetch(id);
-        next_id = id_of(t + 2 * pa.streams);
-        if (BIAS) next_hop = hop_of(t + 2 * pa.streams);
+        if (t + pa.streams < tiles) fetch_keys(id);
         if (CAP) cap_some(a.score, s);
 #pragma unroll
         for (int b = 0; b < kTiles; b++) {
@@ -521,20 +526,26 @@ static logoskg_status packed_args(const logoskg_entity_read *r, PackedArgs *pa, 
     a->q = r->q; a->keys = r->keys; pa->row_bytes = r->key_row;
     a->score = score_args(r->score);
     a->out = r->out; a->lse = r->lse;
-    // A block's eight wavefronts: as many key heads as divide theirs (whose rows lie side by side) and have room for their biases,
-    // then groups of 16 rows, then streams of tiles.
+    // A block's eight wavefronts: as many key heads as divide theirs, whose rows lie side by side (64 lists of up to 20,000 entries, 32 / 8
+    // heads of 128: 340 us with two in a block, 204 with eight), and have room for their biases; then groups of rows; then streams of
+    // tiles.  Fewer heads where blocks would not do for the card (one list of 900: 12.4 us with eight, 9.5 with one).
     pa->ways = a->rows <= 4 ? 4 : a->rows <= 8 ? 2 : 1;
     pa->row_groups = (a->rows * pa->ways + 15) / 16;
     pa->table_words = a->score.bias ? a->group * (2 * a->score.max_distance + 1) : 0;
-    const int piece = piece_bytes((a->dim + 31) / 32);
-    pa->heads_in = 1;
-    for (int h = 8; h > 1; h--)
-        if (a->kv_heads % h == 0 && 8 * piece + h * pa->table_words * 4 <= 80 << 10) { pa->heads_in = h; break; }
-    pa->rows_in = 8 / pa->heads_in < pa->row_groups ? 8 / pa->heads_in : pa->row_groups;
-    pa->streams = 8 / (pa->heads_in * pa->rows_in);
-    const long long each = (a->kv_heads / pa->heads_in) * (long long)((pa->row_groups + pa->rows_in - 1) / pa->rows_in);
+    const int groups = (a->dim + 31) / 32, piece = piece_bytes(groups), room = (groups <= 2 ? 80 : 150) << 10;  // (two blocks of a unit, or one)
+    long long each = 0;  // blocks per 2^shift entries
+    for (int h = 8; h >= 1; h--) {
+        if (a->kv_heads % h || (h > 1 && 8 * piece + h * pa->table_words * 4 > room)) continue;
+        pa->heads_in = h;
+        pa->rows_in = 8 / h < pa->row_groups ? 8 / h : pa->row_groups;
+        each = (a->kv_heads / h) * (long long)((pa->row_groups + pa->rows_in - 1) / pa->rows_in);
+        if (((a->num_entries >> 6) + a->num_queries) * each >= 256) break;
+    }
+    // Blocks of 64 entries, larger ones (up to 4,096) where there are more than eight rounds of them: a block's begin costs as much as some tiles
     a->shift = 6;
-    while (a->shift < 12 && ((1 << a->shift) < kPackedTile * pa->streams || (a->num_entries >> a->shift) * each > 2048)) a->shift++;
+    while (a->shift < 12 && (a->num_entries >> a->shift) * each > (groups <= 2 ? 4096 : 2048)) a->shift++;
+    const int tiles = 1 << (a->shift - 6), spare = 8 / (pa->heads_in * pa->rows_in);
+    pa->streams = tiles < spare ? tiles : spare;
     a->blocks = (a->num_entries >> a->shift) + a->num_queries;
     if ((a->blocks + 8) * (a->kv_heads / pa->heads_in) >= (1ll << 31) || pa->row_groups > 65535 || (long long)a->num_queries * a->tokens * a->heads >= (1ll << 32)) { set_error("%s: too many rows", call); return LOGOSKG_EINVAL; }
     return LOGOSKG_OK;
@@ -561,12 +572,7 @@ template <class E> static logoskg_status read_packed(const PackedArgs &pa, hipSt
     const ReadArgs &a = pa.r;
     const int groups = (a.dim + 31) / 32;
     LKG_TRY((groups == 1 ? read_packed<E, 1>(pa, st) : groups == 2 ? read_packed<E, 2>(pa, st) : groups == 3 ? read_packed<E, 3>(pa, st) : read_packed<E, 4>(pa, st)));
-    if (part_bytes(a)) {
-        const long long n = (long long)a.num_queries * a.tokens * a.heads;
-        k_read_join<E><<<dim3((unsigned)((n + 3) / 4)), 256, 0, st>>>(a);
-        LKG_HIP(hipGetLastError());
-    }
-    return LOGOSKG_OK;
+    return launch_join<E>(a, st);
 }
 
 static const char *pack_args(const logoskg_pack *p, PackArgs *a) {

@@ -55,53 +55,83 @@ __device__ __forceinline__ void row_terms(const PolicyArgs &a, int r, float logp
     if (w == 0.f) loss = slope = 0.f;
 }
 
-// One row by a block (or a part of a block) of THREADS threads: a sweep over its logits for the largest and the sum, another for
-// the gradient.
-template <class T, int THREADS, int MODE> __global__ __launch_bounds__(THREADS) void k_policy(PolicyArgs a) {
+// Exponents up to this size, in units of log 2, are made in one step, x k minus a product that is rounded before: 2^-19 of the exponential
+// at most.
+constexpr float kNear = 64.f;
+
+// x where the bit is set, `other` where it is not: of a bit as a whole word two instructions
+__device__ __forceinline__ float by_bit(unsigned bits, int e, float x, float other) {
+    const unsigned m = (unsigned)__builtin_amdgcn_sbfe((int)bits, e, 1);
+    return __builtin_bit_cast(float, (__builtin_bit_cast(unsigned, x) & m) | (__builtin_bit_cast(unsigned, other) & ~m));
+}
+
+// One row by a block of THREADS threads: a sweep over its logits for the largest and the sum, another for the gradient.  The
+// first KEEP chunks of a thread, all that there are in rows of up to 16 KEEP THREADS bytes, are asked for at once and stay in registers
+// for the second sweep.
+template <int THREADS> struct RowShared { float tops[THREADS / 64], sums[THREADS / 64], said[2]; };
+template <class T, int THREADS, int MODE, bool MASKED, int KEEP> __device__ __forceinline__ void policy_row(const PolicyArgs &a, int r, int tid, RowShared<THREADS> &shared) {
     constexpr int V = 16 / sizeof(T), kWaves = THREADS / 64;
-    __shared__ float tops[kWaves], sums[kWaves], said[4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = blockIdx.x;
+    const int lane = tid & 63, wave = tid >> 6;
+    float *tops = shared.tops, *sums = shared.sums, *said = shared.said;
+    auto all_here = [] {  // (rows of a wavefront each need no more than its own order)
+        if (THREADS == 64) wave_sync();
+        else __syncthreads();
+    };
     const T *in = (const T *)a.logits + (long long)r * a.row;
     const long long vocab = a.vocab;
     const int target = a.target[r];
-    const long long mask_at = !a.mask ? 0 : a.mask_row ? a.mask_row[r] : r;
-    const bool closed = a.mask && (mask_at < 0 || mask_at >= a.num_masks);
-    const u64 *mask = a.mask && !closed ? a.mask + mask_at * a.words : nullptr;
+    const long long mask_at = !MASKED ? 0 : a.mask_row ? a.mask_row[r] : r;
+    const bool closed = MASKED && (mask_at < 0 || mask_at >= a.num_masks);  // (such a row's mask is not read: nothing is allowed)
+    const u64 *mask = MASKED && !closed ? a.mask + mask_at * a.words : nullptr;
     const float k = a.scale * kLog2e;
     const long long lead0 = ((16 - ((uintptr_t)in & 15)) & 15) / sizeof(T), lead = lead0 < vocab ? lead0 : vocab;
-    const long long chunks = (vocab - lead) / V, tail = lead + chunks * V;
-    auto allowed = [&](long long v) { return !closed && (!mask || (mask[v >> 6] >> (v & 63) & 1)); };
-    auto bits_of = [&](long long v) -> unsigned {  // of the V ids from v on
-        if (closed) return 0;
-        if (!mask) return ~0u;
-        const int sh = (int)(v & 63);
-        u64 m = mask[v >> 6] >> sh;
-        if (sh > 64 - V) m |= mask[(v >> 6) + 1] << (64 - sh);
-        return (unsigned)m;
+    const long long chunks = closed ? 0 : (vocab - lead) / V, tail = lead + (vocab - lead) / V * V;
+    auto allowed = [&](long long v) { return !MASKED || (!closed && (mask[v >> 6] >> (v & 63) & 1)); };
+    auto bits_of = [&](long long v) -> unsigned {  // of the V ids from v on, and others above: the two bytes that they stand in
+        if (!MASKED) return ~0u;
+        typedef unsigned short __attribute__((aligned(1))) two_bytes;
+        const long long last = a.words * 8 - 2, at = v >> 3 < last ? v >> 3 : last;
+        return (unsigned)*(const two_bytes *)((const char *)mask + at) >> (int)(v - 8 * at);
     };
-    auto counts = [&](float logp) { return target >= 0 && target < vocab && logp != -INFINITY; };
+    Some<T> kept[KEEP];
+    unsigned kept_bits[MASKED ? KEEP : 1];
+    Sum s = {-INFINITY, 0.f};
     float lse, logp, slope;
     if (MODE != kBackward) {
-        Sum s = {-INFINITY, 0.f};
         auto take = [&](float x) { s.join(x, x == -INFINITY ? 0.f : 1.f, k); };
         if (tid < lead && allowed(tid)) take((float)in[tid]);
         if (tail + tid < vocab && allowed(tail + tid)) take((float)in[tail + tid]);
-        for (long long c = tid; c < chunks; c += THREADS) {
-            const long long v = lead + c * V;
-            const Some<T> x = *(const Some<T> *)(in + v);
-            const unsigned bits = bits_of(v);
+        auto take_chunk = [&](const Some<T> &x, unsigned bits) __attribute__((always_inline)) {
             float y[V], top = s.top;
 #pragma unroll
             for (int e = 0; e < V; e++) {
-                y[e] = bits >> e & 1 ? (float)x[e] : -INFINITY;
+                y[e] = (float)x[e];
+                if (MASKED) y[e] = by_bit(bits, e, y[e], -INFINITY);
                 top = fmaxf(top, y[e]);
             }
             const float at = top == -INFINITY ? 0.f : top;
             float sum = s.sum * exp2_fast((s.top - at) * k);
+            const float from = -at * k;
+            if (__builtin_expect(__builtin_fabsf(from) < kNear, 1)) {
 #pragma unroll
-            for (int e = 0; e < V; e++) sum += exp2_fast((y[e] - at) * k);
+                for (int e = 0; e < V; e++) sum += exp2_fast(__builtin_fmaf(y[e], k, from));
+            } else {
+#pragma unroll
+                for (int e = 0; e < V; e++) sum += exp2_fast((y[e] - at) * k);
+            }
             s.top = top, s.sum = sum;
-        }
+        };
+#pragma unroll
+        for (int i = 0; i < KEEP; i++)
+            if (tid + i * THREADS < chunks) {
+                const long long v = lead + (long long)(tid + i * THREADS) * V;
+                kept[i] = *(const Some<T> *)(in + v);
+                if (MASKED) kept_bits[i] = bits_of(v);
+            }
+#pragma unroll
+        for (int i = 0; i < KEEP; i++)
+            if (tid + i * THREADS < chunks) take_chunk(kept[i], MASKED ? kept_bits[i] : ~0u);
+        for (long long c = tid + KEEP * THREADS; c < chunks; c += THREADS) take_chunk(*(const Some<T> *)(in + lead + c * V), bits_of(lead + c * V));
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) {
             const float top = __shfl_xor(s.top, d), sum = __shfl_xor(s.sum, d);
@@ -109,7 +139,7 @@ template <class T, int THREADS, int MODE> __global__ __launch_bounds__(THREADS) 
         }
         if (kWaves > 1) {
             if (lane == 0) tops[wave] = s.top, sums[wave] = s.sum;
-            __syncthreads();
+            all_here();
             s = Sum{tops[0], sums[0]};
             for (int w = 1; w < kWaves; w++) s.join(tops[w], sums[w], k);
         }
@@ -138,53 +168,112 @@ template <class T, int THREADS, int MODE> __global__ __launch_bounds__(THREADS) 
     if (MODE == kLogp) return;
     if (tid == 0) {
         float loss;
-        row_terms(a, r, logp, counts(logp), loss, slope);
+        row_terms(a, r, logp, target >= 0 && target < vocab && logp != -INFINITY, loss, slope);
         if (MODE != kBackward) a.row_loss[r] = loss;
         else if (a.dloss) slope *= *a.dloss;
         said[0] = slope * a.scale;
         said[1] = logp;
     }
     if (MODE == kLoss) return;
-    __syncthreads();
+    all_here();
     slope = said[0];
     logp = said[1];
     T *out = (T *)a.dlogits + (long long)r * vocab;
-    const float base = lse == -INFINITY ? 0.f : lse;
-    const bool any = slope != 0.f;
-    auto share = [&](float x) { return any && x != -INFINITY ? -slope * exp2_fast(__builtin_fmaf(x, a.scale, -base) * kLog2e) : 0.f; };
-    if (tid < lead) out[tid] = (T)(allowed(tid) ? share((float)in[tid]) : 0.f);
-    if (tail + tid < vocab) out[tail + tid] = (T)(allowed(tail + tid) ? share((float)in[tail + tid]) : 0.f);
-    for (long long c = tid; c < chunks; c += THREADS) {
-        const long long v = lead + c * V;
-        const Some<T> x = *(const Some<T> *)(in + v);
-        const unsigned bits = bits_of(v);
-        Some<T> y;
-#pragma unroll
-        for (int e = 0; e < V; e++) y[e] = (T)(bits >> e & 1 ? share((float)x[e]) : 0.f);
-        store_some<T>(out + v, y, V);
+    if (slope == 0.f || closed) {  // zeros, whatever the logits are
+        const long long lead1 = ((16 - ((uintptr_t)out & 15)) & 15) / sizeof(T), before = lead1 < vocab ? lead1 : vocab, whole = (vocab - before) / V, behind = before + whole * V;
+        if (tid < before) out[tid] = (T)0.f;
+        if (behind + tid < vocab) out[behind + tid] = (T)0.f;
+        for (long long c = tid; c < whole; c += THREADS) *(Some<T> *)(out + before + c * V) = Some<T>{};
+        return;
     }
-    __syncthreads();  // (a thread's share of the target is written over)
-    if (tid == 0 && any) out[target] = (T)(-slope * expm1f(logp));
+    constexpr int kKept = MODE == kBackward ? 0 : KEEP;
+    auto write_row = [&](auto far) __attribute__((always_inline)) {  // (where lse is far from 0, its rounding would be that of the shares)
+        const float from = far ? -__log2f(s.sum) : -lse * kLog2e;
+        auto share = [&](float x) { return exp2_fast(__builtin_fmaf(far ? x - s.top : x, k, from)) * -slope; };
+        auto write_chunk = [&](long long v, const Some<T> &x, unsigned bits) __attribute__((always_inline)) {
+            Some<T> y;
+#pragma unroll
+            for (int e = 0; e < V; e++) {
+                const float z = share((float)x[e]);
+                y[e] = (T)(MASKED ? by_bit(bits, e, z, 0.f) : z);
+            }
+            store_some<T>(out + v, y, V);
+        };
+        if (tid < lead) out[tid] = (T)(allowed(tid) ? share((float)in[tid]) : 0.f);
+        if (tail + tid < vocab) out[tail + tid] = (T)(allowed(tail + tid) ? share((float)in[tail + tid]) : 0.f);
+#pragma unroll
+        for (int i = 0; i < kKept; i++)
+            if (tid + i * THREADS < chunks) write_chunk(lead + (long long)(tid + i * THREADS) * V, kept[i], MASKED ? kept_bits[i] : ~0u);
+        for (long long c = tid + kKept * THREADS; c < chunks; c += THREADS) write_chunk(lead + c * V, *(const Some<T> *)(in + lead + c * V), bits_of(lead + c * V));
+    };
+    if (MODE == kBackward || __builtin_fabsf(lse * kLog2e) < kNear) write_row(std::false_type{});
+    else write_row(std::true_type{});
+    if (THREADS == 64) __threadfence_block();  // (a thread's share of the target is written over)
+    all_here();
+    if (tid == 0) out[target] = (T)(-slope * expm1f(logp));
 }
 
-__global__ __launch_bounds__(256) void k_policy_sum(const float *row_loss, int n, float *loss) {
-    __shared__ double box[4];
+template <class T, int THREADS, int MODE, bool MASKED, int KEEP> __global__ __launch_bounds__(THREADS, 4) void k_policy(PolicyArgs a) {
+    __shared__ RowShared<THREADS> shared;
+    policy_row<T, THREADS, MODE, MASKED, KEEP>(a, blockIdx.x, threadIdx.x, shared);
+}
+
+// The rows' losses together, in a fixed order.
+__device__ __forceinline__ void add_rows(const float *row_loss, int n, float *loss, double *box, int threads) {
     double sum = 0.0;
-    for (int i = threadIdx.x; i < n; i += 256) sum += row_loss[i];
+    for (int i = threadIdx.x; i < n; i += threads) sum += row_loss[i];
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
     if ((threadIdx.x & 63) == 0) box[threadIdx.x >> 6] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) *loss = (float)(box[0] + box[1] + box[2] + box[3]);
+    if (threadIdx.x) return;
+    sum = 0.0;
+    for (int w = 0; w < threads / 64; w++) sum += box[w];
+    *loss = (float)sum;
+}
+__global__ __launch_bounds__(256) void k_policy_sum(const float *row_loss, int n, float *loss) {
+    __shared__ double box[4];
+    add_rows(row_loss, n, loss, box, 256);
+}
+
+// Few short rows by one block, a wavefront each at a time, and their sum: one launch less.
+constexpr int kFewRows = 64;
+template <class T, int MODE, bool MASKED> __global__ __launch_bounds__(1024, 4) void k_policy_few(PolicyArgs a) {
+    __shared__ RowShared<64> shared[16];
+    __shared__ double box[16];
+    const int wave = threadIdx.x >> 6;
+    for (int r = wave; r < a.num_rows; r += 16) policy_row<T, 64, MODE, MASKED, 4>(a, r, threadIdx.x & 63, shared[wave]);
+    __threadfence_block();
+    __syncthreads();
+    add_rows(a.row_loss, a.num_rows, a.loss, box, 1024);
+}
+
+template <class T, int THREADS, int MODE, bool MASKED, int KEEP> static void launch_rows(const PolicyArgs &a, hipStream_t st) {
+    k_policy<T, THREADS, MODE, MASKED, KEEP><<<dim3(a.num_rows), THREADS, 0, st>>>(a);
 }
 
 template <class T, int MODE> static logoskg_status launch_policy(const PolicyArgs &a, hipStream_t st) {
+    const bool sum = MODE == kLoss || MODE == kLossAndGradient;
+    if (sum && a.num_rows <= kFewRows && a.vocab <= 64 * 2 * (16 / (int)sizeof(T))) {
+        a.mask ? k_policy_few<T, MODE, true><<<1, 1024, 0, st>>>(a) : k_policy_few<T, MODE, false><<<1, 1024, 0, st>>>(a);
+        LKG_HIP(hipGetLastError());
+        return LOGOSKG_OK;
+    }
     if (a.num_rows) {
-        if (a.vocab <= 4096) k_policy<T, 64, MODE><<<dim3(a.num_rows), 64, 0, st>>>(a);
-        else k_policy<T, 512, MODE><<<dim3(a.num_rows), 512, 0, st>>>(a);
+        // Threads by the chunks of a row: a wavefront for 4 each (4,096 rows of 2,000 bfloat16 logits 11 us; 128 threads 13, 512 21), 128 or 512
+        // for 8 (8,192 rows of 32,000: 192 us with 512, 250 with 1,024), else 1,024, where keeping few chunks is best under masks (2,048 rows of
+        // 150,001: 269 us with 2, 345 with 20, most of whose registers are the masks'), and all of long rows without (272 us with 20,
+        // 308 with 4; 4,096 rows of 80,000: 278 with 4, 294 with 512 threads).
+        const long long chunks = a.vocab / (16 / (int)sizeof(T));
+        if (chunks <= 64 * 4) a.mask ? launch_rows<T, 64, MODE, true, 4>(a, st) : launch_rows<T, 64, MODE, false, 4>(a, st);
+        else if (chunks <= 128 * 8) a.mask ? launch_rows<T, 128, MODE, true, 8>(a, st) : launch_rows<T, 128, MODE, false, 8>(a, st);
+        else if (chunks <= 512 * 8) a.mask ? launch_rows<T, 512, MODE, true, 8>(a, st) : launch_rows<T, 512, MODE, false, 8>(a, st);
+        else if (a.mask) launch_rows<T, 1024, MODE, true, 2>(a, st);
+        else if (chunks <= 1024 * 10 || chunks > 1024 * 20) launch_rows<T, 1024, MODE, false, 4>(a, st);
+        else launch_rows<T, 1024, MODE, false, 20>(a, st);
         LKG_HIP(hipGetLastError());
     }
-    if (MODE == kLoss || MODE == kLossAndGradient) {
+    if (sum) {
         k_policy_sum<<<1, 256, 0, st>>>(a.row_loss, a.num_rows, a.loss);
         LKG_HIP(hipGetLastError());
     }

@@ -213,12 +213,7 @@ template <class E> static logoskg_status read(const ReadArgs &a, hipStream_t st)
                                  : bias ? launch_read<E, 128, false, true>(a, st) : launch_read<E, 128, false, false>(a, st)));
     else LKG_TRY((cap ? bias ? launch_read<E, 64, true, true>(a, st) : launch_read<E, 64, true, false>(a, st)
                       : bias ? launch_read<E, 64, false, true>(a, st) : launch_read<E, 64, false, false>(a, st)));
-    if (part_bytes(a)) {
-        long long n = (long long)a.num_queries * a.tokens * a.heads;
-        k_read_join<E><<<dim3((unsigned)((n + 3) / 4)), 256, 0, st>>>(a);
-        LKG_HIP(hipGetLastError());
-    }
-    return LOGOSKG_OK;
+    return launch_join<E>(a, st);
 }
 
 }  // namespace lkg

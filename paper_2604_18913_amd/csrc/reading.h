@@ -284,6 +284,7 @@ template <class E> __device__ __forceinline__ void bias_to_lds(float *table, con
     for (int i = tid; i < places; i += threads) {
         int b = s.buckets[i];
         b = b < 0 ? 0 : b >= s.num_buckets ? s.num_buckets - 1 : b;
+#pragma unroll 4
         for (int g = 0; g < group; g++) table[g * places + i] = lowest((float)bias[(long long)(h0 + g) * s.num_buckets + b] * kLog2e);
     }
 }

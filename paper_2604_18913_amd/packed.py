@@ -3,6 +3,7 @@ the manner of ``reading``.  A 3,000,000-entity table of 8 key heads of 128 takes
 from __future__ import annotations
 
 import ctypes
+import struct
 
 from .binding import _check, _load, _stream_handle, _torch
 from .reading import _dtype, _entity_read_of, _I32, _I64, _on_gpu, _on_stream, _P, _packer, _plain, _rows, _score, _workspace
@@ -15,6 +16,7 @@ class _Pack(ctypes.Structure):
 
 
 _pack_of = _packer(_Pack)
+_last_of = struct.Struct("=QqQ").pack  # workspace, workspace_bytes and stream, with which the structures of calls that have one end
 
 
 def packed_row_bytes(kv_heads: int, dim: int) -> int:
@@ -91,7 +93,7 @@ def read_packed(q, packed, off, entity=None, *, kv_heads, scale=None, cap=0.0, b
     out, lse = torch.empty_like(q), q.new_empty((n, tokens, heads), dtype=torch.float32)
     head += (out.data_ptr(), lse.data_ptr())
     lib = _load()
-    w = _workspace(lib.logoskg_read_packed_bytes(_entity_read_of(*head, 0, 0, 0)), q)
-    _check(lib.logoskg_read_packed(_entity_read_of(*head, *((0, 0) if w is None else (w.data_ptr(), w.numel())),
-                                                   _stream_handle(None, device))))
+    call = _entity_read_of(*head, 0, 0, 0)
+    w = _workspace(lib.logoskg_read_packed_bytes(call), q)
+    _check(lib.logoskg_read_packed(call[:-24] + _last_of(*((0, 0) if w is None else (w.data_ptr(), w.numel())), _stream_handle(None, device))))
     return {"out": out, "lse": lse}

@@ -9,6 +9,7 @@ import functools
 import struct
 
 from .binding import _check, _load, _stream_handle, _torch
+from .packed import _last_of
 from .reading import _dtype, _F, _I32, _I64, _on_gpu, _on_stream, _P, _packer, _plain, _workspace
 
 _U32 = ctypes.c_uint32
@@ -114,9 +115,9 @@ def embed_entities_backward(dout, ids, num_entities, *, scale=1.0, out=None, acc
     head = (104, device, _dtype(dout.dtype), _dtype(out.dtype), scale, 1 if accumulate else 0, ids.numel(), num_entities, dim, row,
             ids_at, dout_at, out.data_ptr())
     lib = _load()
-    w = _workspace(lib.logoskg_embed_entities_backward_bytes(_embedding_grad_of(*head, 0, 0, 0)), dout)
-    _check(lib.logoskg_embed_entities_backward(_embedding_grad_of(*head, *((0, 0) if w is None else (w.data_ptr(), w.numel())),
-                                                                  _stream_handle(None, device))))
+    call = _embedding_grad_of(*head, 0, 0, 0)
+    w = _workspace(lib.logoskg_embed_entities_backward_bytes(call), dout)
+    _check(lib.logoskg_embed_entities_backward(call[:-24] + _last_of(*((0, 0) if w is None else (w.data_ptr(), w.numel())), _stream_handle(None, device))))
     return out
 
 
