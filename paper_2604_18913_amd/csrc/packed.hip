@@ -23,16 +23,21 @@ __host__ __device__ __forceinline__ int row_bytes_of(int kv_heads, int groups) {
 
 template <class T> struct Eight { typedef T type __attribute__((ext_vector_type(8), aligned(sizeof(T)))); };
 
+// of this lane and the one beside it, and of those two and the other two of four
+template <int PERM> __device__ __forceinline__ float quad(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), PERM, 0xf, 0xf, true)); }
+__device__ __forceinline__ float quad_min(float x) { x = fminf(x, quad<0xb1>(x)); return fminf(x, quad<0x4e>(x)); }
+__device__ __forceinline__ float quad_max(float x) { x = fmaxf(x, quad<0xb1>(x)); return fmaxf(x, quad<0x4e>(x)); }
+__device__ __forceinline__ float quad_sum(float x) { x += quad<0xb1>(x); return x + quad<0x4e>(x); }
+
 // Four lanes' codes of a group of 32 elements, eight each (x: those of this lane, `in`: whether there are any), and its scale and base.
 struct Codes { unsigned word, scale_base; };
 __device__ __forceinline__ Codes codes_of(const float (&x)[8], bool in) {
     float lo = INFINITY, hi = -INFINITY, odd = 0.f;
     if (in) {
 #pragma unroll
-        for (int e = 0; e < 8; e++) lo = fminf(lo, x[e]), hi = fmaxf(hi, x[e]), odd += x[e] - x[e];
+        for (int e = 0; e < 8; e++) lo = fminf(lo, x[e]), hi = fmaxf(hi, x[e]), odd = __builtin_fmaf(x[e], 0.f, odd);
     }
-#pragma unroll
-    for (int d = 1; d < 4; d <<= 1) lo = fminf(lo, __shfl_xor(lo, d)), hi = fmaxf(hi, __shfl_xor(hi, d)), odd += __shfl_xor(odd, d);
+    lo = quad_min(lo), hi = quad_max(hi), odd = quad_sum(odd);
     // both rounded to the nearest bfloat16: 2^-9 of the base and of the range, a 30th of a step's half
     const bf16 scale = (bf16)((hi - lo) / 15.f), base = (bf16)lo;
     const float s = (float)scale, b = (float)base;
@@ -41,25 +46,53 @@ __device__ __forceinline__ Codes codes_of(const float (&x)[8], bool in) {
         got.scale_base = 0x7fc07fc0u;  // NaN
         return got;
     }
-    if (in && s > 0.f) {
+    // (x - b) / s to the nearest whole number, halves to even ones, without a division: by a reciprocal, whose error matters next to
+    // halves alone, where the rest x - b - c s (c s has 12 bits, so that the rest is exact there) says on which side it is.  Scales that
+    // have no normal reciprocal are divided by.
+    float c[8], rest = 0.f;
+    if (s > 1e-37f && s < 1e37f) {
+        const float inv = 1.f / s, half = 0.5f * s;
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-            const float c = __builtin_rintf((x[e] - b) / s);
-            got.word |= (unsigned)fminf(fmaxf(c, 0.f), 15.f) << (4 * e);
+            const float d = x[e] - b;
+            c[e] = __builtin_rintf(d * inv);
+            rest = fmaxf(rest, __builtin_fabsf(__builtin_fmaf(-c[e], s, d)));
         }
+        if (wave_any(rest >= half)) {
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                const float d = x[e] - b, r = __builtin_fmaf(-c[e], s, d), size = __builtin_fabsf(r);
+                if (size > half || (size == half && ((int)c[e] & 1))) c[e] += r > 0.f ? 1.f : -1.f;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) c[e] = s > 0.f ? __builtin_rintf((x[e] - b) / s) : 0.f;
+    }
+    if (in) {  // four codes a time as a whole number of 16 bits, which 32-bit floats hold
+        float two[2] = {0.f, 0.f};
+#pragma unroll
+        for (int e = 7; e >= 0; e--) two[e >> 2] = __builtin_fmaf(two[e >> 2], 16.f, __builtin_amdgcn_fmed3f(c[e], 0.f, 15.f));
+        got.word = (unsigned)two[0] | (unsigned)two[1] << 16;
     }
     return got;
 }
 
-// Four lanes per group of 32 elements of a head of a row: its keys, then its values.
+// What a thread of k_pack and k_unpack does: four lanes per group of 32 elements, blocks of whole rows (or of a part of a long one's
+// groups at a time).  f(row, head, group, lane of the four)
+template <class F> __device__ __forceinline__ void each_group(const PackArgs &a, F f) {
+    const int items = a.kv_heads * a.groups, q = threadIdx.x >> 2, c = threadIdx.x & 3;
+    const int rows = items < 64 ? 64 / items : 1, sub = items < 64 ? q / items : 0;
+    if (sub >= rows) return;
+    for (int item = items < 64 ? q % items : q; item < items; item += 64) {
+        const int h = item / a.groups, g = item % a.groups;
+        for (long long r = (long long)blockIdx.x * rows + sub; r < a.num_rows; r += (long long)gridDim.x * rows) f(r, h, g, c);
+    }
+}
+
+// A row's keys, then its values, of a group.  Memory bounds it: 407,000 rows of 8 heads of 128 in bfloat16 (2.2 GB) PACK_US us.
 template <class T> __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
-    const long long items = a.num_rows * a.kv_heads * a.groups;
-    const int c = threadIdx.x & 3;
-    for (long long i = (long long)blockIdx.x * 64 + threadIdx.x / 4; i < items; i += (long long)gridDim.x * 64) {
-        const int g = (int)(i % a.groups);
-        const long long rh = i / a.groups;
-        const int h = (int)(rh % a.kv_heads);
-        const long long r = rh / a.kv_heads;
+    each_group(a, [&](long long r, int h, int g, int c) __attribute__((always_inline)) {
         const int at = 32 * g + 8 * c;
         const bool in = at < a.dim;
         typename Eight<T>::type k = {}, v = {};
@@ -77,22 +110,17 @@ template <class T> __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
         ((unsigned *)row)[4 * all + (h * a.groups + g) * 4 + c] = vc.word;
         if (c < 2) ((unsigned *)row)[8 * all + (h * a.groups + g) * 2 + c] = c == 0 ? kc.scale_base : vc.scale_base;
         if (a.pad && c < 2 && h == a.kv_heads - 1 && g == a.groups - 1) ((unsigned *)row)[10 * all + c] = 0;
-    }
+    });
 }
 
 __device__ __forceinline__ float low_half(unsigned x) { return __builtin_bit_cast(float, x << 16); }         // a bfloat16 in 32 bits
 __device__ __forceinline__ float high_half(unsigned x) { return __builtin_bit_cast(float, x & 0xffff0000u); }
 
+// (the same rows UNPACK_US us)
 template <class T> __global__ __launch_bounds__(256) void k_unpack(PackArgs a) {
-    const long long items = a.num_rows * a.kv_heads * a.groups;
-    const int c = threadIdx.x & 3;
-    for (long long i = (long long)blockIdx.x * 64 + threadIdx.x / 4; i < items; i += (long long)gridDim.x * 64) {
-        const int g = (int)(i % a.groups);
-        const long long rh = i / a.groups;
-        const int h = (int)(rh % a.kv_heads);
-        const long long r = rh / a.kv_heads;
+    each_group(a, [&](long long r, int h, int g, int c) __attribute__((always_inline)) {
         const int at = 32 * g + 8 * c, all = a.kv_heads * a.groups;
-        if (at >= a.dim) continue;
+        if (at >= a.dim) return;
         const unsigned *row = (const unsigned *)(a.packed + r * a.packed_row);
         const unsigned kw = row[h * 4 * a.groups + c * a.groups + g], vw = row[4 * all + (h * a.groups + g) * 4 + c];
         const unsigned kp = row[8 * all + (h * a.groups + g) * 2], vp = row[8 * all + (h * a.groups + g) * 2 + 1];
@@ -104,7 +132,7 @@ template <class T> __global__ __launch_bounds__(256) void k_unpack(PackArgs a) {
         }
         *(typename Eight<T>::type *)((T *)a.keys + r * a.key_row + h * a.key_head + at) = k;
         *(typename Eight<T>::type *)((T *)a.values + r * a.value_row + h * a.value_head + at) = v;
-    }
+    });
 }
 
 // ---------------------------------------------------------------- attention
@@ -601,8 +629,9 @@ static logoskg_status pack(const logoskg_pack *p, bool back, const char *call) {
     OnDevice on;
     LKG_TRY(on.go(p->device));
     hipStream_t st = (hipStream_t)p->stream;
-    const long long blocks = (a.num_rows * a.kv_heads * a.groups + 63) / 64;
-    const dim3 grid((unsigned)(blocks > 16384 ? 16384 : blocks));
+    const int items = a.kv_heads * a.groups, rows = items < 64 ? 64 / items : 1;
+    const long long blocks = (a.num_rows + rows - 1) / rows;
+    const dim3 grid((unsigned)(blocks > (1 << 20) ? 1 << 20 : blocks));
     if (p->dtype == LOGOSKG_F32) back ? k_unpack<float><<<grid, 256, 0, st>>>(a) : k_pack<float><<<grid, 256, 0, st>>>(a);
     else if (p->dtype == LOGOSKG_BF16) back ? k_unpack<bf16><<<grid, 256, 0, st>>>(a) : k_pack<bf16><<<grid, 256, 0, st>>>(a);
     else back ? k_unpack<fp16><<<grid, 256, 0, st>>>(a) : k_pack<fp16><<<grid, 256, 0, st>>>(a);
