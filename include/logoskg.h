@@ -689,7 +689,7 @@ typedef struct {
     int32_t device;
     int32_t dtype;            /* of logits and dlogits                                       */
     int32_t num_rows;
-    int64_t vocab;
+    int64_t vocab;            /* a row takes less than 2^32 - 2^20 bytes                     */
     int64_t row;              /* stride of the rows of logits, in elements                   */
     const void *logits;       /* device                                                      */
     const int32_t *target;    /* device int32[num_rows]                                      */
@@ -709,12 +709,9 @@ typedef struct {
     void *dlogits;            /* device [num_rows][vocab]; logoskg_policy_loss: NULL, or the gradient for dloss = 1, in the
                                  same pass (it may be `logits` where row = vocab)            */
     const float *dloss;       /* device float: of the backward; NULL: 1                      */
-    void *workspace;          /* device, logoskg_policy_loss_bytes bytes, 16-byte aligned    */
-    int64_t workspace_bytes;
     void *stream;
 } logoskg_policy;
 logoskg_status logoskg_token_logp(const logoskg_policy *p);      /* logp and lse alone */
-int64_t logoskg_policy_loss_bytes(const logoskg_policy *p);
 logoskg_status logoskg_policy_loss(const logoskg_policy *p);     /* loss, logp, lse and perhaps dlogits */
 logoskg_status logoskg_policy_loss_backward(const logoskg_policy *p); /* dlogits of lse */
 

@@ -161,7 +161,7 @@ def _load():
                  "unpack_entities", "read_packed"):
         getattr(lib, "logoskg_" + name).restype = ctypes.c_int
         getattr(lib, "logoskg_" + name).argtypes = [P]
-    for name in ("embed_entities_backward_bytes", "policy_loss_bytes", "read_packed_bytes"):
+    for name in ("embed_entities_backward_bytes", "read_packed_bytes"):
         getattr(lib, "logoskg_" + name).restype = I64
         getattr(lib, "logoskg_" + name).argtypes = [P]
     lib.logoskg_packed_row_bytes.restype = I64

@@ -66,7 +66,7 @@ struct GradArgs {
     uint2 *gap;                      // first row and the one behind
 };
 
-constexpr int kMostChunk = 32, kFewParts = 16;      // entries of the sorted list; parts of a run that one block joins
+constexpr int kMostChunk = 64, kFewParts = 16;      // entries of the sorted list; parts of a run that one block joins
 constexpr int kGapRows = 32, kGapPiece = 512;  // rows without an id that the sums' kernel clears between two ids; rows of a piece of more
 constexpr int kFewIds = 4096, kSortTile = 2048, kMostDigitBits = 11;
 
@@ -219,6 +219,16 @@ __global__ __launch_bounds__(256) void k_sort_move(GradArgs a, int pass, int shi
     __shared__ unsigned box[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, digits = 1 << bits;
     unsigned *mine = count + wave * digits;
+    // how often this thread's digits occur, in all and in the tiles before
+    constexpr int kPer = (1 << kMostDigitBits) / 256;
+    const int per = digits < 256 ? 1 : digits / 256, first = tid * per;
+    unsigned total[kPer], tile[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; j++) {
+        const bool in = j < per && first + j < digits;
+        total[j] = in ? a.total[first + j] : 0;
+        tile[j] = in ? a.count[(long long)(first + j) * a.tiles + blockIdx.x] : 0;
+    }
     for (int i = tid; i < 4 * digits; i += 256) count[i] = 0;
     __syncthreads();
     const long long from = (long long)blockIdx.x * kSortTile + wave * (kSortTile / 4);
@@ -239,20 +249,23 @@ __global__ __launch_bounds__(256) void k_sort_move(GradArgs a, int pass, int shi
         wave_sync();
     }
     __syncthreads();
-    unsigned sum = 0;  // of the digits before this round's
-    for (int d0 = 0; d0 < digits; d0 += 256) {
-        const int d = d0 + tid;
-        unsigned all;
-        const unsigned before = block_before<256>(d < digits ? a.total[d] : 0, box, all);
-        if (d < digits) {
-            unsigned at = sum + before + a.count[(long long)d * a.tiles + blockIdx.x];
+    // (up to eight digits a thread)
+    unsigned all, sum = 0;
+#pragma unroll
+    for (int j = 0; j < kPer; j++) sum += total[j];
+    unsigned before = block_before<256>(sum, box, all);
+#pragma unroll
+    for (int j = 0; j < kPer; j++) {
+        const int d = first + j;
+        if (j < per && d < digits) {
+            unsigned at = before + tile[j];
             for (int w = 0; w < 4; w++) {
                 const unsigned c = count[w * digits + d];
                 count[w * digits + d] = at;
                 at += c;
             }
         }
-        sum += all;
+        before += total[j];
     }
     __syncthreads();
 #pragma unroll
@@ -477,7 +490,7 @@ static long long plan_grad(GradArgs &a, char *w) {
     a.bits = 1;
     while (a.num_entities >> a.bits) a.bits++;  // (num_entities itself is a key)
     a.tiles = (int)((a.num_ids + kSortTile - 1) / kSortTile);
-    a.chunk = a.num_ids < 65536 ? 8 : 32;
+    a.chunk = a.num_ids < 65536 ? 8 : a.num_ids < 262144 ? 32 : 64;
     a.chunks = (a.num_ids + a.chunk - 1) / a.chunk;
     long long at = 0;
     auto take = [&](long long bytes) {

@@ -257,31 +257,35 @@ __global__ __launch_bounds__(512, NG <= 2 ? 4 : 2) void k_read_packed(PackedArgs
     unsigned k[4][NG];
     u32x4 v[NG];
     u64 param[NG];
-    auto row_of = [&](int id) { return rows + (u64)(unsigned)id * row_bytes; };
-    // (the first row stands in for entries that are left out: their scales, bases and weights are 0)
-    auto fetch_keys = [&](int id) {
-        const int in = id < 0 ? 0 : id;
+    // A lane makes the place of its own entry's row; the others get it by shuffles.  (The first row stands in for entries that are left
+    // out: their scales, bases and weights are 0.)
+    auto row_of = [&](u64 own, int entry) {
+        const unsigned lo = (unsigned)__shfl((int)(unsigned)own, entry), hi = (unsigned)__shfl((int)(unsigned)(own >> 32), entry);
+        return (const char *)((u64)hi << 32 | lo);
+    };
+    auto own_row = [&](int id) { return (u64)(uintptr_t)rows + (u64)(unsigned)(id < 0 ? 0 : id) * row_bytes; };
+    auto fetch_keys = [&](u64 own) {
 #pragma unroll
         for (int t = 0; t < 4; t++) {
-            const unsigned *at = (const unsigned *)(row_of(__shfl(in, 16 * t + col)) + head * kBytes) + quarter * NG;
+            const unsigned *at = (const unsigned *)(row_of(own, 16 * t + col) + head * kBytes) + quarter * NG;
 #pragma unroll
             for (int i = 0; i < NG; i++) k[t][i] = at[i];
         }
     };
-    auto fetch = [&](int id) {
-        const int in = id < 0 ? 0 : id;
+    auto fetch = [&](u64 own) {
 #pragma unroll
         for (int i = 0; i < NG; i++) {
             const int chunk = i * 64 + lane;
-            v[i] = *(const u32x4 *)(row_of(__shfl(in, entry_of(chunk / NG))) + 16 * all + head * kBytes + chunk % NG * 16);
+            v[i] = *(const u32x4 *)(row_of(own, entry_of(chunk / NG)) + 16 * all + head * kBytes + chunk % NG * 16);
         }
 #pragma unroll
-        for (int i = 0; i < NG; i++) param[i] = *(const u64 *)(row_of(in) + 32 * all + (head * NG + i) * 8);
+        for (int i = 0; i < NG; i++) param[i] = *(const u64 *)((const char *)(uintptr_t)own + 32 * all + (head * NG + i) * 8);
     };
     const int tiles = a.num_entities > 0 ? (n + kPackedTile - 1) / kPackedTile : 0;
     int id = id_of(stream), next_id = id_of(stream + pa.streams), now_hop = 0, next_hop = 0;
     if (BIAS) now_hop = hop_of(stream), next_hop = hop_of(stream + pa.streams);
-    if (stream < tiles) fetch(id), fetch_keys(id);
+    u64 own = own_row(id);
+    if (stream < tiles) fetch(own), fetch_keys(own);
 
     const int row_group = blockIdx.y * pa.rows_in + unit / pa.heads_in, vr = row_group * kRows + col % kRows;
     const bool mine = vr < a.rows;
@@ -361,7 +365,8 @@ __global__ __launch_bounds__(512, NG <= 2 ? 4 : 2) void k_read_packed(PackedArgs
         wave_sync();
         id = next_id;
         now_hop = next_hop;
-        if (t + pa.streams < tiles) fetch(id);
+        own = own_row(id);
+        if (t + pa.streams < tiles) fetch(own);
         next_id = id_of(t + 2 * pa.streams);
         if (BIAS) next_hop = hop_of(t + 2 * pa.streams);
         float s[kMine];
@@ -389,7 +394,7 @@ __global__ __launch_bounds__(512, NG <= 2 ? 4 : 2) void k_read_packed(PackedArgs
                 s[4 * b + e] = y[e];
             }
         }
-        if (t + pa.streams < tiles) fetch_keys(id);
+        if (t + pa.streams < tiles) fetch_keys(own);
         if (CAP) cap_some(a.score, s);
 #pragma unroll
         for (int b = 0; b < kTiles; b++) {
@@ -631,7 +636,8 @@ static logoskg_status pack(const logoskg_pack *p, bool back, const char *call) {
     hipStream_t st = (hipStream_t)p->stream;
     const int items = a.kv_heads * a.groups, rows = items < 64 ? 64 / items : 1;
     const long long blocks = (a.num_rows + rows - 1) / rows;
-    const dim3 grid((unsigned)(blocks > (1 << 20) ? 1 << 20 : blocks));
+    const long long most = back ? 1 << 20 : 1 << 14;  // (packing 407,000 rows: 527 us with 16,384 blocks, 554 with 4,096, 632 with one a row; back 200, 220 and 195)
+    const dim3 grid((unsigned)(blocks > most ? most : blocks));
     if (p->dtype == LOGOSKG_F32) back ? k_unpack<float><<<grid, 256, 0, st>>>(a) : k_pack<float><<<grid, 256, 0, st>>>(a);
     else if (p->dtype == LOGOSKG_BF16) back ? k_unpack<bf16><<<grid, 256, 0, st>>>(a) : k_pack<bf16><<<grid, 256, 0, st>>>(a);
     else back ? k_unpack<fp16><<<grid, 256, 0, st>>>(a) : k_pack<fp16><<<grid, 256, 0, st>>>(a);

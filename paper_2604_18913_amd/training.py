@@ -30,7 +30,7 @@ class _Policy(ctypes.Structure):
     _fields_ = [("struct_size", _U32), ("device", _I32), ("dtype", _I32), ("num_rows", _I32), ("vocab", _I64), ("row", _I64),
                 ("logits", _P), ("target", _P), ("mask", _P), ("mask_row", _P), ("num_masks", _I64), ("scale", _F), ("kl", _F),
                 ("clip_low", _F), ("clip_high", _F), ("advantage", _P), ("old", _P), ("ref", _P), ("weight", _P), ("logp", _P),
-                ("lse", _P), ("loss", _P), ("dlogits", _P), ("dloss", _P), ("workspace", _P), ("workspace_bytes", _I64), ("stream", _P)]
+                ("lse", _P), ("loss", _P), ("dlogits", _P), ("dloss", _P), ("stream", _P)]
 
 
 class _Gradient(ctypes.Structure):
@@ -138,7 +138,7 @@ def _answers(logits, target, mask, mask_row):
     else:
         masks = mask.shape[0] if mask.dim() == 2 else -1
         _plain(mask, "mask", torch.int64, device, (masks if mask_row is not None else rows, words))
-    head = (184, device, _dtype(logits.dtype), rows, vocab, row if rows > 1 else vocab, logits.data_ptr(),
+    head = (168, device, _dtype(logits.dtype), rows, vocab, row if rows > 1 else vocab, logits.data_ptr(),
             _plain(target, "target", torch.int32, device, (rows,)), 0 if mask is None else mask.data_ptr(),
             _plain(mask_row, "mask_row", torch.int32, device, (rows,)), masks)
     return head, device, rows
@@ -155,7 +155,7 @@ def token_logp(logits, target, *, scale=1.0, mask=None, mask_row=None):
     torch = _torch()
     head, device, rows = _answers(logits, target, mask, mask_row)
     logp, lse = (logits.new_empty((rows,), dtype=torch.float32) for _ in range(2))
-    _check(_load().logoskg_token_logp(_policy_of(*head, scale, 0.0, 0.0, 0.0, 0, 0, 0, 0, logp.data_ptr(), lse.data_ptr(), 0, 0, 0, 0, 0,
+    _check(_load().logoskg_token_logp(_policy_of(*head, scale, 0.0, 0.0, 0.0, 0, 0, 0, 0, logp.data_ptr(), lse.data_ptr(), 0, 0, 0,
                                                  _stream_handle(None, device))))
     return {"logp": logp, "lse": lse}
 
@@ -220,10 +220,8 @@ def policy_loss(logits, target, advantage, *, old=None, ref=None, weight=None, c
     terms = _terms(advantage, old, ref, weight, clip, kl, scale, rows, device)
     loss, logp, lse = (logits.new_empty(shape, dtype=torch.float32) for shape in ((), (rows,), (rows,)))
     dlogits = logits.new_empty(logits.shape) if gradient else None
-    w = _workspace(4 * rows, logits)
     _check(_load().logoskg_policy_loss(_policy_of(*head, *terms, logp.data_ptr(), lse.data_ptr(), loss.data_ptr(),
-                                                  0 if dlogits is None else dlogits.data_ptr(), 0, 0 if w is None else w.data_ptr(), 4 * rows,
-                                                  _stream_handle(None, device))))
+                                                  0 if dlogits is None else dlogits.data_ptr(), 0, _stream_handle(None, device))))
     got = {"loss": loss, "logp": logp, "lse": lse}
     return got if dlogits is None else got | {"dlogits": dlogits}
 
@@ -238,7 +236,7 @@ def policy_loss_backward(dloss, logits, target, advantage, lse, *, old=None, ref
     terms = _terms(advantage, old, ref, weight, clip, kl, scale, rows, device)
     lse_at, dloss_at = _plain(lse, "lse", torch.float32, device, (rows,)), _plain(dloss, "dloss", torch.float32, device, ())
     dlogits = logits.new_empty(logits.shape)
-    _check(_load().logoskg_policy_loss_backward(_policy_of(*head, *terms, 0, lse_at, 0, dlogits.data_ptr(), dloss_at, 0, 0,
+    _check(_load().logoskg_policy_loss_backward(_policy_of(*head, *terms, 0, lse_at, 0, dlogits.data_ptr(), dloss_at,
                                                            _stream_handle(None, device))))
     return dlogits
 

@@ -119,7 +119,7 @@ def test_read_packed_is_the_reading_of_what_rows_stand_for():
 
 # ---------------------------------------------------------------- refusals
 def test_struct_sizes_match_the_header():
-    assert [ctypes.sizeof(s) for s in (training._Embedding, training._EmbeddingGrad, training._Policy, training._Gradient, packed._Pack)] == [80, 104, 184, 32, 104]
+    assert [ctypes.sizeof(s) for s in (training._Embedding, training._EmbeddingGrad, training._Policy, training._Gradient, packed._Pack)] == [80, 104, 168, 32, 104]
 
 
 def test_cpu_tensors_are_refused():
@@ -156,17 +156,16 @@ def test_embedding_gradient_refusals(wrong, rc, says):
     assert (nbytes == -1) == (rc == 1)
 
 
-_POLICY = dict(struct_size=184, dtype=0, num_rows=2, vocab=10, row=10, logits=64, target=64, scale=1.0, kl=0.1, clip_low=0.2, clip_high=0.2, advantage=64, ref=64,
-               logp=64, lse=64, loss=64, dlogits=64, workspace=64, workspace_bytes=64)
+_POLICY = dict(struct_size=168, dtype=0, num_rows=2, vocab=10, row=10, logits=64, target=64, scale=1.0, kl=0.1, clip_low=0.2, clip_high=0.2, advantage=64, ref=64,
+               logp=64, lse=64, loss=64, dlogits=64)
 
 
 @pytest.mark.parametrize("wrong, rc, says", [
-    (dict(struct_size=0), 1, "struct_size"), (dict(dtype=9), 1, "type"), (dict(num_rows=-1), 1, "count"), (dict(vocab=1 << 31), 1, "count"), (dict(num_masks=-1), 1, "count"),
+    (dict(struct_size=0), 1, "struct_size"), (dict(dtype=9), 1, "type"), (dict(vocab=1 << 30, row=1 << 30), 1, "count"), (dict(num_rows=-1), 1, "count"), (dict(vocab=1 << 31), 1, "count"), (dict(num_masks=-1), 1, "count"),
     (dict(row=9), 1, "overlap"), (dict(logits=None), 1, "NULL"), (dict(target=None), 1, "NULL"), (dict(lse=None), 1, "NULL"), (dict(mask=64, num_masks=1), 1, "fewer masks"),
     (dict(scale=0.0), 1, "scale"), (dict(scale=-1.0), 1, "scale"), (dict(scale=math.inf), 1, "scale"), (dict(scale=math.nan), 1, "scale"), (dict(logits=66), 1, "aligned"),
     (dict(kl=-0.1), 1, "kl"), (dict(kl=math.nan), 1, "kl"), (dict(clip_low=-1.0), 1, "clip"), (dict(clip_high=math.nan), 1, "clip"), (dict(advantage=None), 1, "advantage"),
-    (dict(ref=None), 1, "ref"), (dict(loss=None), 1, "loss"), (dict(logp=None), 1, "logp"), (dict(row=12, dlogits=64), 1, "in place"),
-    (dict(workspace_bytes=4), 4, "workspace"), (dict(workspace=None), 4, "workspace")])
+    (dict(ref=None), 1, "ref"), (dict(loss=None), 1, "loss"), (dict(logp=None), 1, "logp"), (dict(row=12, dlogits=64), 1, "in place")])
 def test_policy_refusals(wrong, rc, says):
     got, text = _status("logoskg_policy_loss", training._Policy(**{**_POLICY, **wrong}))
     assert got == rc and says in text and text.startswith("logoskg_policy_loss"), text
@@ -178,7 +177,6 @@ def test_further_policy_refusals():
         assert rc == 1 and says in text
     rc, text = _status("logoskg_token_logp", training._Policy(**{**_POLICY, "logp": None}))
     assert rc == 1 and "logp" in text
-    assert reading._load().logoskg_policy_loss_bytes(ctypes.addressof(training._Policy(**{**_POLICY, "vocab": -1}))) == -1
     x = torch.zeros(2, 3)
     with pytest.raises(ValueError, match="mask_row without"):
         training._answers(_Fake(x), torch.zeros(2, dtype=torch.int32), None, torch.zeros(2, dtype=torch.int32))
