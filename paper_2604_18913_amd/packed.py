@@ -3,6 +3,7 @@ the manner of ``reading``.  A 3,000,000-entity table of 8 key heads of 128 takes
 from __future__ import annotations
 
 import ctypes
+import functools
 import struct
 
 from .binding import _check, _load, _stream_handle, _torch
@@ -19,6 +20,7 @@ _pack_of = _packer(_Pack)
 _last_of = struct.Struct("=QqQ").pack  # workspace, workspace_bytes and stream, with which the structures of calls that have one end
 
 
+@functools.lru_cache(None)
 def packed_row_bytes(kv_heads: int, dim: int) -> int:
     """``logoskg_packed_row_bytes``: the bytes of a packed row, 40 for every head and 32 elements of ``dim``."""
     n = _load().logoskg_packed_row_bytes(kv_heads, dim)
@@ -43,7 +45,7 @@ def pack_entities(keys, values, *, out=None):
     uint8 [entities, packed_row_bytes(kv_heads, dim)] for ``read_packed``.  ``out`` may be rows of a larger table:
     ``pack_entities(k, v, out=table[a:b])``; single rows are replaced as any tensor's, ``table[ids] = pack_entities(k, v)``.
 
-    Groups of 32 elements of a head have a scale and a base in bfloat16, a sixteenth of the group's range being a step; the layout stands in
+    Groups of 32 elements of a head have a scale and a base in bfloat16, a fifteenth of the group's range being a step; the layout stands in
     ``include/logoskg.h``.  A group with an infinity or NaN becomes NaN.  There is no gradient."""
     torch = _torch()
     dtype, device = keys.dtype, _on_gpu(keys, "keys")
@@ -65,9 +67,11 @@ def pack_entities(keys, values, *, out=None):
 @_on_stream
 def unpack_entities(packed, kv_heads: int, dim: int, *, dtype):
     """``logoskg_unpack_entities``: the keys and values [rows, kv_heads, dim] that packed rows stand for, in ``dtype``."""
+    torch = _torch()
     device = _on_gpu(packed, "packed")
     n, row = _packed_rows(packed, "packed", packed_row_bytes(kv_heads, dim), device)
-    keys, values = (packed.new_empty((n, kv_heads, dim), dtype=dtype) for _ in range(2))
+    keys = packed.new_empty((n, kv_heads, dim), dtype=dtype)
+    values = torch.empty_like(keys)
     _check(_load().logoskg_unpack_entities(_pack_of(104, device, _dtype(dtype), kv_heads, dim, 0, n, keys.data_ptr(), values.data_ptr(),
                                                     kv_heads * dim, dim, kv_heads * dim, dim, packed.data_ptr(), row,
                                                     _stream_handle(None, device))))

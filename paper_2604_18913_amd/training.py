@@ -218,7 +218,7 @@ def policy_loss(logits, target, advantage, *, old=None, ref=None, weight=None, c
         return {"loss": loss, "logp": logp, "lse": lse}
     head, device, rows = _answers(logits, target, mask, mask_row)
     terms = _terms(advantage, old, ref, weight, clip, kl, scale, rows, device)
-    loss, logp, lse = (logits.new_empty(shape, dtype=torch.float32) for shape in ((), (rows,), (rows,)))
+    loss, logp, lse = logits.new_empty((), dtype=torch.float32), logits.new_empty((rows,), dtype=torch.float32), logits.new_empty((rows,), dtype=torch.float32)
     dlogits = logits.new_empty(logits.shape) if gradient else None
     _check(_load().logoskg_policy_loss(_policy_of(*head, *terms, logp.data_ptr(), lse.data_ptr(), loss.data_ptr(),
                                                   0 if dlogits is None else dlogits.data_ptr(), 0, _stream_handle(None, device))))
@@ -245,8 +245,8 @@ def policy_loss_backward(dloss, logits, target, advantage, lse, *, old=None, ref
 _gradient_of = struct.Struct("=QQqii").pack
 
 
-def _dense(t) -> bool:
-    return t.is_contiguous() or t.dim() == 2 and t.stride(0) == 1 and t.stride(1) == t.shape[0]
+def _transposed(t) -> bool:
+    return t.dim() == 2 and t.stride(0) == 1 and t.stride(1) == t.shape[0]
 
 
 @_on_stream
@@ -269,11 +269,16 @@ def clip_gradients(grads, max_norm, *, scale=1.0, out=None):
             continue
         if device < 0:
             device, like = _on_gpu(g, "a gradient"), g
-        if g.get_device() != device or not _dense(g):
+        whole, dtype = g.is_contiguous(), g.dtype
+        if g.get_device() != device or not (whole or _transposed(g)):
             raise ValueError(f"gradients must be contiguous tensors on cuda:{device}")
-        if o is not g and (o is None or o.get_device() != device or o.shape != g.shape or (o.stride() != g.stride() and not (o.is_contiguous() and g.is_contiguous()))):
-            raise ValueError("an output must be laid out as its gradient")
-        entries.append(_gradient_of(g.data_ptr(), o.data_ptr(), g.numel(), _dtype(g.dtype), _dtype(o.dtype)))
+        kind = to = _dtype(dtype)
+        if o is not g:
+            if o is None or o.get_device() != device or o.shape != g.shape or not (o.is_contiguous() if whole else o.stride() == g.stride()):
+                raise ValueError("an output must be laid out as its gradient")
+            if o.dtype is not dtype:
+                to = _dtype(o.dtype)
+        entries.append(_gradient_of(g.data_ptr(), o.data_ptr(), g.numel(), kind, to))
     if device < 0:
         raise ValueError("no gradients")
     packed = b"".join(entries)
