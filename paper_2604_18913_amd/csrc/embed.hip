@@ -51,8 +51,8 @@ template <class T, int LG> __global__ __launch_bounds__(256) void k_embed(EmbedA
 // list are added up by groups of lanes, and runs that cross chunks are joined from the chunks' parts, in their order.
 struct GradArgs {
     long long num_ids, num_entities, dim, row, chunks;
-    int accumulate, chunk, tiles, bits;
-    int gaps;  // whether rows without an id are still to be cleared behind the sort
+    int accumulate, chunk, tile, tiles, bits;
+    int gaps;  // whether rows without an id are cleared between the sums, and not before
     float scale;
     const int32_t *ids;
     const void *dout;
@@ -60,15 +60,13 @@ struct GradArgs {
     unsigned *key[2], *place[2];  // of the sort: from one to the other and back
     unsigned *count, *total;      // [digits][tiles], [digits]
     float *part;                  // [chunks][2][dim]: of the run that comes in from the chunk before, and of the one that goes on
-    // what the sums leave for the joins, in any order; how many of each: [0] runs that go on from the chunk that they begin in, [1] those of
-    // many chunks, [2] pieces of long gaps between ids
-    unsigned *crossings, *crossing;  // chunks of the runs: from [0] and from [chunks] on
-    uint2 *gap;                      // first row and the one behind
+    unsigned *gap_pieces;         // how many there are of ..
+    uint2 *gap;                   // .. pieces of long gaps: first row and the one behind
 };
 
-constexpr int kMostChunk = 64, kFewParts = 16;      // entries of the sorted list; parts of a run that one block joins
-constexpr int kGapRows = 32, kGapPiece = 512;  // rows without an id that the sums' kernel clears between two ids; rows of a piece of more
-constexpr int kFewIds = 4096, kSortTile = 2048, kMostDigitBits = 11;
+constexpr int kMostChunk = 64, kFewParts = 16;  // entries of the sorted list; parts of a run that 16 lanes join
+constexpr int kGapRows = 32, kGapPiece = 512, kGapBlocks = 1024;  // rows without an id that the sums' kernel clears between two ids; rows of a piece of more; blocks for those
+constexpr int kFewIds = 12288, kMostDigitBits = 11;
 
 __device__ __forceinline__ unsigned key_of(const GradArgs &a, long long i) {
     const int id = a.ids[i];
@@ -121,57 +119,77 @@ template <class O, int THREADS> __device__ __forceinline__ void clear_rows(const
         for (long long c = (long long)lane * V; c < a.dim; c += LG * V) store_some<O>((O *)a.dtable + e * a.row + c, Some<O>{}, a.dim - c < V ? (int)(a.dim - c) : V);
 }
 
-// .. all of them, by `blocks` blocks
-template <class O, int THREADS> __device__ __forceinline__ void clear_table(const GradArgs &a, long long block, long long blocks) {
-    clear_rows<O, THREADS>(a, a.num_entities * block / blocks, a.num_entities * (block + 1) / blocks);
+// The table is cleared before the sums, by blocks beside those of the sort, which is a chain of short waits: a part of it in each of
+// the sort's launches.  Rows that ids name are written twice then; where these can be more than kTwice bytes, the others are cleared
+// between the sums instead, where the sorted ids leave gaps.  (65,536 ids to 300,000 rows of 64 in 32 bits: 50 us a call with the table
+// cleared before, 78 between; to 300,000 rows of 512 in 16 bits 110 and 124; to 30,000 of 2,000 in 32 bits (240 MB) 247 and 220.  550,000 ids to
+// 407,000 rows of 1,024 in 16 bits (833 MB): 563 and 507.)
+constexpr long long kTwice = 192ll << 20;
+struct Rows {
+    long long from, to;
+    int blocks;
+};
+template <class O, int THREADS> __device__ __forceinline__ void clear_share(const GradArgs &a, const Rows &r, long long block) {
+    const long long n = r.to - r.from;
+    clear_rows<O, THREADS>(a, r.from + n * block / r.blocks, r.from + n * (block + 1) / r.blocks);
 }
 
-// Lists of up to kFewIds ids: an id's place is the number of ids before it in the order, counted over all of them, 2 instructions
-// each.  A block has 16 ids, whose 64 lanes of every four wavefronts count over a 64th of the list; the other blocks clear the table.
-// (1,984 ids, 10,000 rows of 512 in 32 bits to clear: RANK_US us; a radix sort by one block beside the clears 9.1.)
-constexpr int kRankIds = 16;
-template <class O> __global__ __launch_bounds__(1024) void k_sort_few(GradArgs a) {
-    __shared__ __attribute__((aligned(16))) unsigned key[kFewIds];
-    __shared__ unsigned box[16][kRankIds];
-    const int n = (int)a.num_ids, ranks = (n + kRankIds - 1) / kRankIds;
-    if ((int)blockIdx.x >= ranks) return clear_table<O, 1024>(a, blockIdx.x - ranks, gridDim.x - ranks);
+// Lists of up to kFewIds ids: an id's place is the number of ids before it in the order, counted over all of them, two instructions
+// each.  A block has 16 PER ids and splits the list among 64 lanes of each; the other blocks clear the table.
+// (1,984 ids, 10,000 rows of 512 in 32 bits to clear: 5.5 us; a radix sort by one block beside the clears 9.1.  12,288 ids to 30,000
+// rows of 64: 20 us, by the passes below 25 and two launches more.)
+template <class O, int PER, int MOST> __global__ __launch_bounds__(1024) void k_sort_few(GradArgs a, Rows rows) {
+    constexpr int L = 16, IDS = L * PER;
+    __shared__ __attribute__((aligned(16))) unsigned key[MOST];
+    __shared__ unsigned box[16][IDS];
+    const int n = (int)a.num_ids, ranks = (n + IDS - 1) / IDS;
+    if ((int)blockIdx.x >= ranks) return clear_share<O, 1024>(a, rows, blockIdx.x - ranks);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, quads = (n + 3) / 4;
-    if (blockIdx.x == 0 && tid < 3) a.crossings[tid] = 0;
     for (int i = tid; i < quads * 4; i += 1024) key[i] = i < n ? key_of(a, i) : ~0u;
     __syncthreads();
-    const int i = blockIdx.x * kRankIds + lane % kRankIds, first = i & ~3;
-    const unsigned mine = i < n ? key[i] : 0;
-    unsigned rank = 0;
+    const int begin = blockIdx.x * IDS + tid % L;
+    unsigned mine[PER], rank[PER];
+#pragma unroll
+    for (int p = 0; p < PER; p++) mine[p] = begin + p * L < n ? key[begin + p * L] : 0, rank[p] = 0;
 #pragma unroll 4
-    for (int j = (wave * 4 + lane / kRankIds) * 4; j < quads * 4; j += 256) {  // of four ids those that are smaller, or as large and before
+    for (int j = tid / L * 4; j < quads * 4; j += 256) {  // of four ids those that are smaller, or as large and before
         const u32x4 x = *(const u32x4 *)(key + j);
-        const unsigned most = mine + (j < first);
 #pragma unroll
-        for (int e = 0; e < 4; e++) rank += x[e] < most;
+        for (int p = 0; p < PER; p++) {
+            const unsigned most = mine[p] + (j < ((begin + p * L) & ~3));
+#pragma unroll
+            for (int e = 0; e < 4; e++) rank[p] += x[e] < most;
+        }
     }
-    if (tid < kRankIds && i < n)  // (of the id's own four)
 #pragma unroll
-        for (int e = 0; e < 3; e++) rank += first + e < i && key[first + e] == mine;
-    rank += __shfl_xor(rank, 16);
-    rank += __shfl_xor(rank, 32);
-    if (lane < kRankIds) box[wave][lane] = rank;
+    for (int p = 0; p < PER; p++) {
+        const int i = begin + p * L, first = i & ~3;
+        if (tid < L && i < n)  // (of the id's own four)
+#pragma unroll
+            for (int e = 0; e < 3; e++) rank[p] += first + e < i && key[first + e] == mine[p];
+        rank[p] += __shfl_xor(rank[p], 16);
+        rank[p] += __shfl_xor(rank[p], 32);
+        if (lane < L) box[wave][p * L + lane] = rank[p];
+    }
     __syncthreads();
-    if (tid >= kRankIds || i >= n) return;
-    rank = 0;
+    const int i = blockIdx.x * IDS + tid;
+    if (tid >= IDS || i >= n) return;
+    unsigned to = 0;
 #pragma unroll
-    for (int w = 0; w < 16; w++) rank += box[w][lane];
-    a.key[0][rank] = mine, a.place[0][rank] = i;
+    for (int w = 0; w < 16; w++) to += box[w][tid];
+    a.key[0][to] = key[i], a.place[0][to] = i;
 }
 
 // A pass of the sort over tiles: how often a digit occurs in each tile ..
-__global__ __launch_bounds__(256) void k_sort_count(GradArgs a, int pass, int shift, int bits) {
+template <class O> __global__ __launch_bounds__(256) void k_sort_count(GradArgs a, int pass, int shift, int bits, Rows rows) {
     extern __shared__ unsigned found[];
+    if ((int)blockIdx.x >= a.tiles) return clear_share<O, 256>(a, rows, blockIdx.x - a.tiles);
     const int tid = threadIdx.x, digits = 1 << bits;
-    if (pass == 0 && blockIdx.x == 0 && tid < 3) a.crossings[tid] = 0;
+    if (blockIdx.x == 0 && tid == 0) *a.gap_pieces = 0;
     for (int i = tid; i < digits; i += 256) found[i] = 0;
     __syncthreads();
-    const long long from = (long long)blockIdx.x * kSortTile;
-    for (int i = tid; i < kSortTile; i += 256) {
+    const long long from = (long long)blockIdx.x * a.tile;
+    for (int i = tid; i < a.tile; i += 256) {
         if (from + i >= a.num_ids) break;
         const unsigned key = pass == 0 ? key_of(a, from + i) : a.key[pass & 1][from + i];
         atomicAdd(&found[key >> shift & (digits - 1)], 1u);
@@ -181,8 +199,9 @@ __global__ __launch_bounds__(256) void k_sort_count(GradArgs a, int pass, int sh
 }
 
 // .. how often before each tile, and in all (a block per digit) ..
-__global__ __launch_bounds__(256) void k_sort_before(GradArgs a) {
+template <class O> __global__ __launch_bounds__(256) void k_sort_before(GradArgs a, int digits, Rows rows) {
     __shared__ unsigned box[4];
+    if ((int)blockIdx.x >= digits) return clear_share<O, 256>(a, rows, blockIdx.x - digits);
     unsigned *count = a.count + (long long)blockIdx.x * a.tiles;
     unsigned sum = 0;
     for (int at = 0; at < a.tiles; at += 256) {
@@ -196,10 +215,11 @@ __global__ __launch_bounds__(256) void k_sort_before(GradArgs a) {
 }
 
 // .. and every id to its place: behind the smaller digits, those of the tiles before, the wavefronts before and the lanes before.
-__global__ __launch_bounds__(256) void k_sort_move(GradArgs a, int pass, int shift, int bits) {
-    constexpr int kRounds = kSortTile / 256;
+template <class O, int TILE> __global__ __launch_bounds__(256) void k_sort_move(GradArgs a, int pass, int shift, int bits, Rows rows) {
+    constexpr int kRounds = TILE / 256;
     extern __shared__ unsigned count[];  // [4][digits]
     __shared__ unsigned box[4];
+    if ((int)blockIdx.x >= a.tiles) return clear_share<O, 256>(a, rows, blockIdx.x - a.tiles);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, digits = 1 << bits;
     unsigned *mine = count + wave * digits;
     // how often this thread's digits occur, in all and in the tiles before
@@ -214,7 +234,7 @@ __global__ __launch_bounds__(256) void k_sort_move(GradArgs a, int pass, int shi
     }
     for (int i = tid; i < 4 * digits; i += 256) count[i] = 0;
     __syncthreads();
-    const long long from = (long long)blockIdx.x * kSortTile + wave * (kSortTile / 4);
+    const long long from = (long long)blockIdx.x * TILE + wave * (TILE / 4);
     unsigned key[kRounds], rank[kRounds];
 #pragma unroll
     for (int r = 0; r < kRounds; r++) {
@@ -329,7 +349,7 @@ template <class T, class O, int LG> __global__ __launch_bounds__(256) void k_emb
             const unsigned pieces = (to - from + kGapPiece - 1) / kGapPiece;
             for (unsigned i = tid % LG; i < pieces; i += lanes) {
                 const unsigned begin = from + i * kGapPiece;
-                a.gap[atomicAdd(a.crossings + 2, 1u)] = uint2{begin, to - begin < kGapPiece ? to : begin + kGapPiece};
+                a.gap[atomicAdd(a.gap_pieces, 1u)] = uint2{begin, to - begin < kGapPiece ? to : begin + kGapPiece};
             }
         }
     };
@@ -367,14 +387,7 @@ template <class T, class O, int LG> __global__ __launch_bounds__(256) void k_emb
     if (any) {
         const bool goes_on = key[a.chunk] == id;
         if (came || goes_on) {
-            if (!came) {
-                part += a.dim;
-                if (blockIdx.y == 0 && tid % LG == 0) {
-                    const long long far = (g + kFewParts) * a.chunk;
-                    const bool many = far < a.num_ids && a.key[0][far] == id;
-                    a.crossing[(many ? a.chunks : 0) + atomicAdd(a.crossings + many, 1u)] = (unsigned)g;
-                }
-            }
+            if (!came) part += a.dim;
             store_sums<float, V>(part, sum, count);
         } else {
             write_sum<O, V>(a, id, c, count, sum);
@@ -383,18 +396,25 @@ template <class T, class O, int LG> __global__ __launch_bounds__(256) void k_emb
     if (g == a.chunks - 1 && id < none) gap(id + 1, none);
 }
 
-// Runs that cross chunks: blocks go through the lists of them.  (Their order does not matter: each is a sum of its own.)  Runs of up to
-// kFewParts parts are added up by a block each, a thread per four elements; longer ones by 16 groups of 16 lanes, a share of the parts
-// each, a block per 64 elements.  Then the long gaps.
+// Runs that cross chunks, by the chunks that they begin in: 16 lanes have such a chunk and 64 columns (blockIdx.y: further ones).  Runs of
+// up to kFewParts parts they add up alone; of the others the block's 16 groups take a share of the parts each.  Further blocks clear the
+// long gaps.
 template <class O> __global__ __launch_bounds__(256) void k_embed_join(GradArgs a) {
     constexpr int V = 4, LG = 16, kGroups = 16, kAhead = 4;
     __shared__ float box[kGroups][LG * V];
+    __shared__ unsigned many[kGroups];
     const unsigned *key = a.key[0];
-    const long long few = a.crossings[0], slabs = (a.dim + LG * V - 1) / (LG * V), runs = few + a.crossings[1] * slabs;
-    const long long items = runs + (a.gaps ? a.crossings[2] : 0);
     const int lane = threadIdx.x % LG, group = threadIdx.x / LG;
-    // parts p .. end - 1 of the run of chunk g, whose first is that chunk's second, from column c on
-    auto add = [&](float (&sum)[V], long long g, long long p, long long end, long long c, int count) {
+    const long long first = (long long)blockIdx.x * kGroups;
+    if (first >= a.chunks) {
+        const unsigned block = blockIdx.x - (unsigned)((a.chunks + kGroups - 1) / kGroups), pieces = blockIdx.y == 0 ? *a.gap_pieces : 0;
+        for (unsigned i = block; i < pieces; i += kGapBlocks) clear_rows<O, 256>(a, a.gap[i].x, a.gap[i].y);
+        return;
+    }
+    const long long c = ((long long)blockIdx.y * LG + lane) * V;
+    const int count = c >= a.dim ? 0 : a.dim - c < V ? (int)(a.dim - c) : V;
+    // parts p .. end - 1 of the run of chunk g, whose first is that chunk's second
+    auto add = [&](float (&sum)[V], long long g, long long p, long long end) {
         for (; p < end; p += kAhead) {
             Some<float> x[kAhead];
 #pragma unroll
@@ -406,47 +426,45 @@ template <class O> __global__ __launch_bounds__(256) void k_embed_join(GradArgs 
                 for (int e = 0; e < V; e++) sum[e] += x[u][e];
         }
     };
-    for (long long item = blockIdx.x; item < items; item += gridDim.x) {
-        if (item >= runs) {  // rows that become zeros
-            const uint2 rows = a.gap[item - runs];
-            clear_rows<O, 256>(a, rows.x, rows.y);
-            continue;
-        }
-        const long long g = a.crossing[item < few ? item : a.chunks + (item - few) / slabs], slab = item < few ? 0 : (item - few) % slabs;
-        const unsigned id = key[(g + 1) * a.chunk - 1];
-        long long lo = g + 1, hi = g + 2;  // the last chunk that begins with the run: lo .. hi - 1
-        while (hi < a.chunks && key[hi * a.chunk] == id) {
-            lo = hi;
-            hi = g + 2 * (hi - g);
-        }
-        if (hi > a.chunks) hi = a.chunks;
-        while (hi - lo > 1) {
-            const long long mid = (lo + hi) / 2;
-            if (key[mid * a.chunk] == id) lo = mid;
-            else hi = mid;
-        }
-        const long long parts = lo - g + 1;
-        if (item < few) {
-            for (long long c = threadIdx.x * V; c < a.dim; c += 256 * V) {
-                const int count = a.dim - c < V ? (int)(a.dim - c) : V;
+    const long long g = first + group;
+    long long parts = 0;
+    if (g + 1 < a.chunks) {
+        const unsigned id = key[(g + 1) * a.chunk - 1], before = g == 0 ? ~0u : key[g * a.chunk - 1];
+        if (id < a.num_entities && before != id && key[(g + 1) * a.chunk] == id) {
+            long long lo = g + 1, hi = g + 2;  // the last chunk that begins with the run: lo .. hi - 1
+            while (hi < a.chunks && key[hi * a.chunk] == id) {
+                lo = hi;
+                hi = g + 2 * (hi - g);
+            }
+            if (hi > a.chunks) hi = a.chunks;
+            while (hi - lo > 1) {
+                const long long mid = (lo + hi) / 2;
+                if (key[mid * a.chunk] == id) lo = mid;
+                else hi = mid;
+            }
+            parts = lo - g + 1;
+            if (parts <= kFewParts && count > 0) {
                 float sum[V] = {0.f, 0.f, 0.f, 0.f};
-                add(sum, g, 0, parts, c, count);
+                add(sum, g, 0, parts);
                 write_sum<O, V>(a, id, c, count, sum);
             }
-            continue;
         }
-        const long long c = (slab * LG + lane) * V, share = (parts + kGroups - 1) / kGroups;
-        const int count = c >= a.dim ? 0 : a.dim - c < V ? (int)(a.dim - c) : V;
+    }
+    if (lane == 0) many[group] = parts > kFewParts ? (unsigned)parts : 0;
+    __syncthreads();
+    for (int i = 0; i < kGroups; i++) {
+        if (many[i] == 0) continue;
+        const long long share = (many[i] + kGroups - 1) / kGroups, end = (group + 1) * share;
         float sum[V] = {0.f, 0.f, 0.f, 0.f};
-        if (count > 0) add(sum, g, group * share, (group + 1) * share < parts ? (group + 1) * share : parts, c, count);
+        if (count > 0) add(sum, first + i, group * share, end < many[i] ? end : many[i]);
 #pragma unroll
         for (int e = 0; e < V; e++) box[group][lane * V + e] = sum[e];
         __syncthreads();
         if (group == 0 && count > 0) {
-            for (int i = 1; i < kGroups; i++)
+            for (int w = 1; w < kGroups; w++)
 #pragma unroll
-                for (int e = 0; e < V; e++) sum[e] += box[i][lane * V + e];
-            write_sum<O, V>(a, id, c, count, sum);
+                for (int e = 0; e < V; e++) sum[e] += box[w][lane * V + e];
+            write_sum<O, V>(a, key[(first + i + 1) * a.chunk - 1], c, count, sum);
         }
         __syncthreads();
     }
@@ -468,11 +486,12 @@ template <class T> static logoskg_status launch_embed(const EmbedArgs &a, hipStr
 
 static long long up(long long x) { return (x + 255) / 256 * 256; }
 
-// Sizes of the sort and places in the workspace; its size.
-static long long plan_grad(GradArgs &a, char *w) {
+// Sizes of the sort and places in the workspace; its size.  (size: of an element of the table)
+static long long plan_grad(GradArgs &a, int size, char *w) {
     a.bits = 1;
     while (a.num_entities >> a.bits) a.bits++;  // (num_entities itself is a key)
-    a.tiles = (int)((a.num_ids + kSortTile - 1) / kSortTile);
+    a.tile = a.num_ids < 262144 ? 512 : 2048;
+    a.tiles = (int)((a.num_ids + a.tile - 1) / a.tile);
     a.chunk = a.num_ids < 65536 ? 8 : a.num_ids < 262144 ? 32 : 64;
     a.chunks = (a.num_ids + a.chunk - 1) / a.chunk;
     long long at = 0;
@@ -490,9 +509,8 @@ static long long plan_grad(GradArgs &a, char *w) {
     a.count = (unsigned *)take(few ? 0 : ((long long)a.tiles << (a.bits + passes - 1) / passes) * 4);
     a.total = (unsigned *)take(few ? 0 : 4 << kMostDigitBits);
     a.part = (float *)take(a.chunks * 2 * a.dim * 4);
-    a.crossings = (unsigned *)take(12);
-    a.crossing = (unsigned *)take(a.chunks * 8);
-    a.gaps = !few && !a.accumulate;
+    a.gaps = !few && !a.accumulate && (a.num_ids < a.num_entities ? a.num_ids : a.num_entities) * a.dim * size > kTwice;
+    a.gap_pieces = (unsigned *)take(few ? 0 : 4);
     a.gap = (uint2 *)take(!a.gaps ? 0 : (a.num_ids + 1 + a.num_entities / kGapPiece + 1) * 8);
     return at;
 }
@@ -502,7 +520,7 @@ static const char *grad_args(const logoskg_embedding_grad *e, GradArgs *a) {
     if (bad_type(e->dtype)) return "unknown type";
     if (e->table_dtype != e->dtype && e->table_dtype != LOGOSKG_F32) return "dtable is neither of dout's type nor float32";
     if (!(e->scale - e->scale == 0.f)) return "scale is not finite";
-    if (e->num_ids < 0 || e->num_ids >= (1ll << 31) || e->num_entities < 0 || e->num_entities >= (1ll << 31) - 1 || e->dim < 0 || e->dim > (1ll << 24)) return "a count is out of range";
+    if (e->num_ids < 0 || e->num_ids >= (1ll << 31) || e->num_entities < 0 || e->num_entities >= (1ll << 31) - 1 || e->dim < 0 || e->dim > 65535 * 64) return "a count is out of range";
     if (e->row < e->dim && e->num_entities > 1) return "rows overlap";
     if (e->num_ids && e->dim && (!e->ids || !e->dout)) return "ids or dout is NULL";
     if (e->num_entities && e->dim && !e->dtable) return "dtable is NULL";
@@ -515,29 +533,39 @@ static const char *grad_args(const logoskg_embedding_grad *e, GradArgs *a) {
     return nullptr;
 }
 
-template <class O> __global__ __launch_bounds__(256) void k_clear_table(GradArgs a) { clear_table<O, 256>(a, blockIdx.x, gridDim.x); }
+template <class O> __global__ __launch_bounds__(256) void k_clear_table(GradArgs a, Rows rows) { clear_share<O, 256>(a, rows, blockIdx.x); }
 
 template <class T, class O> static logoskg_status launch_grad(GradArgs &a, hipStream_t st) {
-    const long long pieces = (a.num_entities + kGapPiece - 1) / kGapPiece;
-    // blocks that clear the whole table, for some 64 KB each
-    const long long some = a.num_entities * a.dim * (long long)sizeof(O) / (64 << 10) + 1, clears = a.accumulate ? 0 : some < 1024 ? some : 1024;
+    // the table from `part` to `next` of `parts`, by blocks that clear some 64 KB each
+    auto share = [&](int part, int next, int parts) {
+        Rows r = {a.num_entities * part / parts, a.num_entities * next / parts, 0};
+        const long long some = (r.to - r.from) * a.dim * (long long)sizeof(O) / (64 << 10) + 1;
+        r.blocks = a.accumulate || a.gaps ? 0 : (int)(some < 1024 ? some : 1024);
+        return r;
+    };
+    const Rows all = share(0, 1, 1);
     if (a.num_ids == 0) {
-        if (!a.accumulate) k_clear_table<O><<<dim3((unsigned)clears), 256, 0, st>>>(a);
+        if (!a.accumulate) k_clear_table<O><<<dim3(all.blocks), 256, 0, st>>>(a, all);
         LKG_HIP(hipGetLastError());
         return LOGOSKG_OK;
     }
-    if (a.num_ids <= kFewIds) {
-        k_sort_few<O><<<dim3((unsigned)((a.num_ids + kRankIds - 1) / kRankIds + clears)), 1024, 0, st>>>(a);
+    if (a.num_ids <= 4096) {
+        k_sort_few<O, 1, 4096><<<dim3((unsigned)(a.num_ids + 15) / 16 + all.blocks), 1024, 0, st>>>(a, all);
+        LKG_HIP(hipGetLastError());
+    } else if (a.num_ids <= kFewIds) {
+        k_sort_few<O, 2, kFewIds><<<dim3((unsigned)(a.num_ids + 31) / 32 + all.blocks), 1024, 0, st>>>(a, all);
         LKG_HIP(hipGetLastError());
     } else {
         const int passes = (a.bits + kMostDigitBits - 1) / kMostDigitBits;
         for (int pass = 0, shift = 0; pass < passes; pass++) {
             const int bits = (a.bits - shift + passes - pass - 1) / (passes - pass);
-            k_sort_count<<<dim3(a.tiles), 256, 4 << bits, st>>>(a, pass, shift, bits);
+            const Rows one = share(4 * pass, 4 * pass + 1, 4 * passes), two = share(4 * pass + 1, 4 * pass + 2, 4 * passes), rest = share(4 * pass + 2, 4 * pass + 4, 4 * passes);
+            k_sort_count<O><<<dim3(a.tiles + one.blocks), 256, 4 << bits, st>>>(a, pass, shift, bits, one);
             LKG_HIP(hipGetLastError());
-            k_sort_before<<<dim3(1 << bits), 256, 0, st>>>(a);
+            k_sort_before<O><<<dim3((1 << bits) + two.blocks), 256, 0, st>>>(a, 1 << bits, two);
             LKG_HIP(hipGetLastError());
-            k_sort_move<<<dim3(a.tiles), 256, 16 << bits, st>>>(a, pass, shift, bits);
+            if (a.tile == 512) k_sort_move<O, 512><<<dim3(a.tiles + rest.blocks), 256, 16 << bits, st>>>(a, pass, shift, bits, rest);
+            else k_sort_move<O, 2048><<<dim3(a.tiles + rest.blocks), 256, 16 << bits, st>>>(a, pass, shift, bits, rest);
             LKG_HIP(hipGetLastError());
             shift += bits;
         }
@@ -546,14 +574,12 @@ template <class T, class O> static logoskg_status launch_grad(GradArgs &a, hipSt
     const long long lanes = (a.dim * (long long)sizeof(T) + 15) / 16;
     const int LG = lanes <= 4 ? 4 : lanes <= 16 ? 16 : 64;
     const dim3 grid((unsigned)((a.chunks + 256 / LG - 1) / (256 / LG)), (unsigned)((lanes + LG - 1) / LG));
-    const long long joins = a.chunks * ((a.dim + 63) / 64) + (a.gaps ? pieces : 0);
-    if (grid.y > 65535) { set_error("logoskg_embed_entities_backward: rows of %lld elements", a.dim); return LOGOSKG_EINVAL; }
     if (LG == 4) k_embed_sum<T, O, 4><<<grid, 256, 0, st>>>(a);
     else if (LG == 16) k_embed_sum<T, O, 16><<<grid, 256, 0, st>>>(a);
     else k_embed_sum<T, O, 64><<<grid, 256, 0, st>>>(a);
     LKG_HIP(hipGetLastError());
-    if (a.chunks > 1 || a.gaps) {
-        k_embed_join<O><<<dim3((unsigned)(joins < 2048 ? joins : 2048)), 256, 0, st>>>(a);
+    if (a.chunks > 1) {
+        k_embed_join<O><<<dim3((unsigned)((a.chunks + 15) / 16) + (a.gaps ? kGapBlocks : 0), (unsigned)((a.dim + 63) / 64)), 256, 0, st>>>(a);
         LKG_HIP(hipGetLastError());
     }
     return LOGOSKG_OK;
@@ -585,7 +611,7 @@ extern "C" logoskg_status logoskg_embed_entities(const logoskg_embedding *e) {
 extern "C" int64_t logoskg_embed_entities_backward_bytes(const logoskg_embedding_grad *e) {
     GradArgs a;
     if (const char *why = grad_args(e, &a)) { set_error("logoskg_embed_entities_backward_bytes: %s", why); return -1; }
-    return a.num_ids && a.dim && a.num_entities ? plan_grad(a, nullptr) : 0;
+    return a.num_ids && a.dim && a.num_entities ? plan_grad(a, size_of(e->table_dtype), nullptr) : 0;
 }
 
 extern "C" logoskg_status logoskg_embed_entities_backward(const logoskg_embedding_grad *e) {
@@ -593,7 +619,7 @@ extern "C" logoskg_status logoskg_embed_entities_backward(const logoskg_embeddin
     if (const char *why = grad_args(e, &a)) { set_error("logoskg_embed_entities_backward: %s", why); return LOGOSKG_EINVAL; }
     if (a.dim == 0 || a.num_entities == 0) return LOGOSKG_OK;
     if (a.num_ids) {
-        const long long need = plan_grad(a, (char *)e->workspace);
+        const long long need = plan_grad(a, size_of(e->table_dtype), (char *)e->workspace);
         if (e->workspace_bytes < need || !e->workspace) {
             set_error("logoskg_embed_entities_backward: the workspace has %lld of %lld bytes", (long long)e->workspace_bytes, need);
             return LOGOSKG_ERANGE;
