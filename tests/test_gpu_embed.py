@@ -132,6 +132,37 @@ def test_wide_gradients_and_accumulation(n, dtype):
         _backward(dout, ids, 400, 0.5, out=_table(20, 400, 48, to), accumulate=True)
 
 
+# (lanes at the end of such rows begin before their own columns)
+@pytest.mark.parametrize("dtype", TYPES, ids=TYPE_NAMES)
+@pytest.mark.parametrize("dim", [1, 3, 5, 9, 13, 67, 333])
+@pytest.mark.parametrize("n", [40, 13_000])
+def test_accumulation_into_rows_of_odd_sizes(n, dim, dtype):
+    dout, ids = _table(21, n, dim, dtype, 0.1), _ids(22, n, 300, 3)
+    for to in {dtype, torch.float32}:
+        _backward(dout, ids, 300, 0.5, out=_table(23, 300, dim, to), accumulate=True)
+
+
+@pytest.mark.parametrize("n", [12_288, 131_072, 262_143, 262_145])
+@pytest.mark.parametrize("entities, skew", [(3000, 4), (300_000, 1)])
+def test_long_lists(n, entities, skew):
+    _backward(_table(24, n, 4, torch.float32), _ids(25, n, entities, skew), entities)
+
+
+@pytest.mark.parametrize("dim, dtype", [(2048, torch.bfloat16), (1021, torch.float32)])
+def test_large_tables_whose_rows_are_mostly_named(dim, dtype):
+    """Cleared between the sums: gaps of no, few and many rows, and those at both ends.  Whole numbers: sums are exact."""
+    n, entities = 62_000, 64_000
+    g = torch.Generator().manual_seed(26)
+    ids = torch.cat([torch.arange(3, 30_000), torch.arange(30_000, 56_000, 2), torch.full((100,), 57_000), torch.tensor([63_998])])
+    ids = torch.cat([ids, ids[torch.randint(0, len(ids), (n - len(ids),), generator=g)]])[torch.randperm(n, generator=g)].int().cuda()
+    dout = torch.randint(-1, 2, (n, dim), generator=g).to(dtype).cuda()
+    want = torch.zeros(entities, dim, device="cuda").index_add_(0, ids.long(), dout.float())
+    assert want.abs().max() <= 256
+    for _ in range(2):
+        got = lkg.embed_entities_backward(dout, ids, entities, out=torch.full((entities, dim), 5.0, dtype=dtype, device="cuda"))
+        assert torch.equal(got.float(), want)
+
+
 def test_tables_beyond_32_bits():
     entities, dim = 600_000, 4096  # 2.4e9 elements
     table = torch.zeros(entities, dim, dtype=torch.bfloat16, device="cuda")
