@@ -660,11 +660,11 @@ typedef struct {
     int32_t table_dtype;      /* of dtable: dtype or LOGOSKG_F32                             */
     float scale;
     int32_t accumulate;
-    int64_t num_ids, num_entities, dim;  /* num_ids, num_entities below 2^31                 */
+    int64_t num_ids, num_entities, dim;  /* num_ids, num_entities below 2^31 - 1, dim at most 2^22 - 64 */
     int64_t row;              /* stride of dtable's rows, in elements: dim at least          */
     const int32_t *ids;       /* device int32[num_ids]                                       */
     const void *dout;         /* device [num_ids][dim]                                       */
-    void *dtable;             /* device, rows of dim consecutive elements                    */
+    void *dtable;             /* device, rows of dim consecutive elements; shares no memory with dout */
     void *workspace;          /* device, logoskg_embed_entities_backward_bytes bytes, 16-byte aligned */
     int64_t workspace_bytes;
     void *stream;
@@ -707,7 +707,7 @@ typedef struct {
     float *logp, *lse;        /* device float[num_rows] each; lse is an input of the backward */
     float *loss;              /* device float                                                */
     void *dlogits;            /* device [num_rows][vocab]; logoskg_policy_loss: NULL, or the gradient for dloss = 1, in the
-                                 same pass (it may be `logits` where row = vocab)            */
+                                 same pass (it may be `logits` where row = vocab, else it shares no memory with them) */
     const float *dloss;       /* device float: of the backward; NULL: 1                      */
     void *stream;
 } logoskg_policy;
@@ -762,7 +762,7 @@ typedef struct {
     void *keys, *values;      /* device, rows of kv_heads x dim: read by logoskg_pack_entities, written by
                                  logoskg_unpack_entities                                     */
     int64_t key_row, key_head, value_row, value_head; /* strides, in elements: not negative   */
-    void *packed;             /* device, 16-byte aligned                                     */
+    void *packed;             /* device, 16-byte aligned; what is written shares no memory with what is read */
     int64_t packed_row;       /* stride of its rows, in bytes: a multiple of 16              */
     void *stream;
 } logoskg_pack;

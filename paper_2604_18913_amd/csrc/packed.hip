@@ -90,7 +90,7 @@ template <class F> __device__ __forceinline__ void each_group(const PackArgs &a,
     }
 }
 
-// A row's keys, then its values, of a group.  Memory bounds it: 407,000 rows of 8 heads of 128 in bfloat16 (2.2 GB) PACK_US us.
+// A row's keys, then its values, of a group.  Memory bounds it: 407,000 rows of 8 heads of 128 in bfloat16 (2.2 GB) 518 us, 4.2 TB/s.
 template <class T> __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
     each_group(a, [&](long long r, int h, int g, int c) __attribute__((always_inline)) {
         const int at = 32 * g + 8 * c;
@@ -116,7 +116,7 @@ template <class T> __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
 __device__ __forceinline__ float low_half(unsigned x) { return __builtin_bit_cast(float, x << 16); }         // a bfloat16 in 32 bits
 __device__ __forceinline__ float high_half(unsigned x) { return __builtin_bit_cast(float, x & 0xffff0000u); }
 
-// (the same rows UNPACK_US us)
+// (the same rows 393 us, 5.6 TB/s)
 template <class T> __global__ __launch_bounds__(256) void k_unpack(PackArgs a) {
     each_group(a, [&](long long r, int h, int g, int c) __attribute__((always_inline)) {
         const int at = 32 * g + 8 * c, all = a.kv_heads * a.groups;
@@ -207,6 +207,12 @@ template <int N> __device__ __forceinline__ void cap_some(const ScoreArgs &s, fl
 // between the two products: then the columns stand WAYS times for the rows, each time for other entries of the tile (16
 // neighbours of every 16 WAYS).  A lane keeps of the first product what is its own entries', its weights stand in the
 // second one's operand beside zeros, and the ways' sums are joined at the end.
+//
+// 1,024 lists of up to 3,000 entries, four tokens, 16 / 8 heads of 64: 327 us, of which the loads alone take 292 and the lines that they bring
+// (0.8 GB) 166 at a copy's rate.  The eight heads of a row ask for its lines at eight times; vector instructions (450 for 64 entries of eight rows) and
+// matrix instructions take 60 % of the cycles, the rest are waits that four wavefronts leave.  Rows fetched by the block together, straight into
+// LDS, come in 163, but hold the wavefronts to one step (331 in all; 64 lists of up to 20,000, 32 / 8 heads of 128: 262, so 204); a barrier
+// before every fetch, so that heads share lines, 359; two heads a wavefront, with half as many lines asked for, the same.
 template <class E, int NG, int WAYS, bool CAP, bool BIAS>
 __global__ __launch_bounds__(512, NG <= 2 ? 4 : 2) void k_read_packed(PackedArgs pa) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -636,7 +642,7 @@ static logoskg_status pack(const logoskg_pack *p, bool back, const char *call) {
     hipStream_t st = (hipStream_t)p->stream;
     const int items = a.kv_heads * a.groups, rows = items < 64 ? 64 / items : 1;
     const long long blocks = (a.num_rows + rows - 1) / rows;
-    const long long most = back ? 1 << 20 : 1 << 14;  // (packing 407,000 rows: 527 us with 16,384 blocks, 554 with 4,096, 632 with one a row; back 200, 220 and 195)
+    const long long most = back ? 1 << 20 : 1 << 14;  // (packing 407,000 rows: 527 us with 16,384 blocks, 554 with 4,096, 632 with one a row; back 400, 440 and 390)
     const dim3 grid((unsigned)(blocks > most ? most : blocks));
     if (p->dtype == LOGOSKG_F32) back ? k_unpack<float><<<grid, 256, 0, st>>>(a) : k_pack<float><<<grid, 256, 0, st>>>(a);
     else if (p->dtype == LOGOSKG_BF16) back ? k_unpack<bf16><<<grid, 256, 0, st>>>(a) : k_pack<bf16><<<grid, 256, 0, st>>>(a);

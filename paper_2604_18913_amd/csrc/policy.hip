@@ -389,9 +389,9 @@ template <class T, int MODE> static logoskg_status launch_policy(const PolicyArg
     }
     if (a.num_rows) {
         // By the chunks of a row.  Whole rows in registers where they are short or no mask takes its share of instructions: 8,192 rows of
-        // 32,000 bfloat16 logits under masks 197 us (227 in two sweeps), 2,048 rows of 150,001 without 264 (313), 4,096 of 80,000 without
-        // 252 (284).  Long rows under masks in two sweeps over memory, two blocks of a unit in turn: 2,048 of 150,001 326 us (359 in
-        // registers, where one block fits and its loads, exponentials and stores take turns), 4,096 of 80,000 292 (308).
+        // 32,000 bfloat16 logits under masks 208 us (264 in two sweeps), 2,048 rows of 150,001 without 284 (317), 4,096 of 80,000 without
+        // 261 (272).  Long rows under masks in two sweeps over memory, two blocks of a unit in turn: 4,096 of 80,000 298 us (318 in registers,
+        // where one block fits and its loads, exponentials and stores take turns), 2,048 of 150,001 332 (334).
         if (chunks <= kShortLanes * kShortChunks) {
             const dim3 blocks((a.num_rows + 15) / 16);
             a.mask ? k_policy_short<T, MODE, true, 256, false><<<blocks, 256, 0, st>>>(a) : k_policy_short<T, MODE, false, 256, false><<<blocks, 256, 0, st>>>(a);

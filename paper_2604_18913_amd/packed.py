@@ -17,6 +17,17 @@ class _Pack(ctypes.Structure):
 
 
 _pack_of = _packer(_Pack)
+def _apart(written, name, *others):
+    """Refuses a tensor that is written where others that are read lie."""
+    def ends(t):
+        return t.data_ptr(), t.data_ptr() + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))) if t.numel() else t.data_ptr()
+    begin, end = ends(written)
+    for t in others:
+        first, last = ends(t)
+        if begin < last and first < end:
+            raise ValueError(f"{name} shares memory with an input")
+
+
 _last_of = struct.Struct("=QqQ").pack  # workspace, workspace_bytes and stream, with which the structures of calls that have one end
 
 
@@ -56,6 +67,8 @@ def pack_entities(keys, values, *, out=None):
     nbytes = packed_row_bytes(heads, dim)
     if out is None:
         out = keys.new_empty((n, nbytes), dtype=torch.uint8)
+    else:
+        _apart(out, "out", keys, values)
     rows, row = _packed_rows(out, "out", nbytes, device)
     if rows != n:
         raise ValueError(f"out has {rows} rows, not {n}")

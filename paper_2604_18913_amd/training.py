@@ -9,7 +9,7 @@ import functools
 import struct
 
 from .binding import _check, _load, _stream_handle, _torch
-from .packed import _last_of
+from .packed import _apart, _last_of
 from .reading import _dtype, _F, _I32, _I64, _on_gpu, _on_stream, _P, _packer, _plain, _workspace
 
 _U32 = ctypes.c_uint32
@@ -96,14 +96,15 @@ def embed_entities_backward(dout, ids, num_entities, *, scale=1.0, out=None, acc
     [*ids.shape, dim], that of its result; summed in 32 bits and rounded once; the same inputs give the same bits.
 
     ``out`` (of ``dout``'s type, or float32) takes it; with ``accumulate`` it is added to what stands there, and rows that no id
-    names are not touched."""
+    names are not touched.  It shares no memory with ``dout``."""
     torch = _torch()
     device = _on_gpu(dout, "dout")
     if dout.dim() != ids.dim() + 1 or dout.shape[:-1] != ids.shape:
         raise ValueError(f"dout has the shape {tuple(dout.shape)}, and ids {tuple(ids.shape)}")
     dout_at, ids_at = _plain(dout, "dout", dout.dtype, device), _plain(ids, "ids", torch.int32, device)
     dim = dout.shape[-1]
-    if out is None:
+    given = out is not None
+    if not given:
         if accumulate:
             raise ValueError("accumulate needs out")
         out = dout.new_empty((num_entities, dim))
@@ -112,6 +113,8 @@ def embed_entities_backward(dout, ids, num_entities, *, scale=1.0, out=None, acc
     n, wide, row = _table(out, "out", out.dtype, device)
     if n != num_entities or wide != dim:
         raise ValueError(f"out has the shape {tuple(out.shape)}, not {(num_entities, dim)}")
+    if given:
+        _apart(out, "out", dout, ids)
     head = (104, device, _dtype(dout.dtype), _dtype(out.dtype), scale, 1 if accumulate else 0, ids.numel(), num_entities, dim, row,
             ids_at, dout_at, out.data_ptr())
     lib = _load()
@@ -137,6 +140,8 @@ def _answers(logits, target, mask, mask_row):
             raise ValueError("mask_row without a mask")
     else:
         masks = mask.shape[0] if mask.dim() == 2 else -1
+        if masks == 0 and rows:
+            raise ValueError("a mask without rows")
         _plain(mask, "mask", torch.int64, device, (masks if mask_row is not None else rows, words))
     head = (168, device, _dtype(logits.dtype), rows, vocab, row if rows > 1 else vocab, logits.data_ptr(),
             _plain(target, "target", torch.int32, device, (rows,)), 0 if mask is None else mask.data_ptr(),

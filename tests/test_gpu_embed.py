@@ -235,8 +235,8 @@ def test_what_the_binding_refuses():
                       (lambda: lkg.embed_entities(table[0], ids), "entities, dim"), (lambda: lkg.embed_entities(table, ids[::2]), "contiguous"),
                       (lambda: lkg.embed_entities_backward(table, ids, 4), "shape"), (lambda: lkg.embed_entities_backward(table[:3], ids, 4, accumulate=True), "needs out"),
                       (lambda: lkg.embed_entities_backward(table[:3], ids, 5, out=table), "shape"), (lambda: lkg.embed_entities_backward(table[:3], ids, 4, out=table.half()), "float32"),
-                      (lambda: lkg.embed_entities_backward(table[:1].expand(3, 8), ids, 4), "contiguous")]:
+                      (lambda: lkg.embed_entities_backward(table[:1].expand(3, 8), ids, 4), "contiguous"), (lambda: lkg.embed_entities_backward(table[:3], ids, 4, out=table), "shares memory")]:
         with pytest.raises(ValueError, match=says):
             bad()
     with pytest.raises(lkg.LogosKGError, match="overlap"):
-        lkg.embed_entities_backward(table[:3], ids, 4, out=table[:1].expand(4, 8))
+        lkg.embed_entities_backward(table[:3].clone(), ids, 4, out=table[:1].expand(4, 8))

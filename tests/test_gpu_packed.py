@@ -258,7 +258,8 @@ def test_what_the_binding_refuses():
                       (lambda: lkg.read_packed(**{**a, "q": a["q"].float()[0]}), "q must be"), (lambda: lkg.read_packed(**{**a, "entity": a["entity"].long()}), "int32"),
                       (lambda: lkg.pack_entities(k, v[:5]), "one shape"), (lambda: lkg.pack_entities(k, v.half()), "bfloat16"), (lambda: lkg.pack_entities(k, v, out=a["packed"][:5]), "rows"),
                       (lambda: lkg.pack_entities(k[:, :, :12], v[:, :, :12]), "multiple of 8"), (lambda: lkg.unpack_entities(a["packed"], 2, 128, dtype=torch.float32), "uint8"),
-                      (lambda: lkg.unpack_entities(a["packed"], 2, 64, dtype=torch.float64), "not supported")]:
+                      (lambda: lkg.unpack_entities(a["packed"], 2, 64, dtype=torch.float64), "not supported"),
+                      (lambda: lkg.pack_entities(k, v, out=v.view(torch.uint8).view(9, 256)[:, :160]), "shares memory")]:
         with pytest.raises(ValueError, match=says):
             bad()
     with pytest.raises(lkg.LogosKGError, match="type"):

@@ -233,7 +233,8 @@ def test_what_the_binding_refuses():
     a = _gpu(_case(11, 4, 70, masks=2))
     for change, says in [(dict(target=a["target"].long()), "int32"), (dict(target=a["target"][:3]), "shape"), (dict(advantage=a["advantage"].double()), "float32"), (dict(mask=a["mask"][:, :1]), "mask"),
                          (dict(mask_row=None), "shape"), (dict(mask_row=a["mask_row"].long()), "int32"), (dict(mask=None), "mask_row without"), (dict(ref=None), "kl without ref"),
-                         (dict(logits=a["logits"].t()), "contiguous rows"), (dict(logits=a["logits"].double()), "not supported"), (dict(weight=a["weight"][:2]), "shape")]:
+                         (dict(logits=a["logits"].t()), "contiguous rows"), (dict(logits=a["logits"].double()), "not supported"), (dict(weight=a["weight"][:2]), "shape"),
+                         (dict(mask=a["mask"][:0]), "without rows")]:
         with pytest.raises(ValueError, match=says):
             lkg.policy_loss(**{**a, **change})
     with pytest.raises(ValueError, match="dloss"):
