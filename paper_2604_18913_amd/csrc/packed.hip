@@ -263,17 +263,22 @@ __global__ __launch_bounds__(512, NG <= 2 ? 4 : 2) void k_read_packed(PackedArgs
     unsigned k[4][NG];
     u32x4 v[NG];
     u64 param[NG];
+    // (of global memory: loads of a place that may be LDS too are waited for with every read of LDS)
+    typedef const __attribute__((address_space(1))) char global_bytes;
+    typedef const __attribute__((address_space(1))) unsigned global_words;
+    typedef const __attribute__((address_space(1))) u32x4 global_chunk;
+    typedef const __attribute__((address_space(1))) u64 global_pair;
     // A lane makes the place of its own entry's row; the others get it by shuffles.  (The first row stands in for entries that are left
     // out: their scales, bases and weights are 0.)
     auto row_of = [&](u64 own, int entry) {
         const unsigned lo = (unsigned)__shfl((int)(unsigned)own, entry), hi = (unsigned)__shfl((int)(unsigned)(own >> 32), entry);
-        return (const char *)((u64)hi << 32 | lo);
+        return (global_bytes *)((u64)hi << 32 | lo);
     };
     auto own_row = [&](int id) { return (u64)(uintptr_t)rows + (u64)(unsigned)(id < 0 ? 0 : id) * row_bytes; };
     auto fetch_keys = [&](u64 own) {
 #pragma unroll
         for (int t = 0; t < 4; t++) {
-            const unsigned *at = (const unsigned *)(row_of(own, 16 * t + col) + head * kBytes) + quarter * NG;
+            global_words *at = (global_words *)(row_of(own, 16 * t + col) + head * kBytes) + quarter * NG;
 #pragma unroll
             for (int i = 0; i < NG; i++) k[t][i] = at[i];
         }
@@ -282,10 +287,10 @@ __global__ __launch_bounds__(512, NG <= 2 ? 4 : 2) void k_read_packed(PackedArgs
 #pragma unroll
         for (int i = 0; i < NG; i++) {
             const int chunk = i * 64 + lane;
-            v[i] = *(const u32x4 *)(row_of(own, entry_of(chunk / NG)) + 16 * all + head * kBytes + chunk % NG * 16);
+            v[i] = *(global_chunk *)(row_of(own, entry_of(chunk / NG)) + 16 * all + head * kBytes + chunk % NG * 16);
         }
 #pragma unroll
-        for (int i = 0; i < NG; i++) param[i] = *(const u64 *)((const char *)(uintptr_t)own + 32 * all + (head * NG + i) * 8);
+        for (int i = 0; i < NG; i++) param[i] = *(global_pair *)((global_bytes *)(uintptr_t)own + 32 * all + (head * NG + i) * 8);
     };
     const int tiles = a.num_entities > 0 ? (n + kPackedTile - 1) / kPackedTile : 0;
     int id = id_of(stream), next_id = id_of(stream + pa.streams), now_hop = 0, next_hop = 0;
