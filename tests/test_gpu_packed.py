@@ -119,6 +119,20 @@ def test_lengths(lengths, kv_heads):
             assert (got["out"][i] == 0).all() and (got["lse"][i] == -math.inf).all()
 
 
+# lists that a block has alone, and that several share
+@pytest.mark.parametrize("dtype", HALVES, ids=["bf16", "fp16"])
+@pytest.mark.parametrize("heads, kv_heads, dim", [(4, 4, 128), (6, 2, 80), (5, 5, 40), (2, 2, 8), (12, 4, 96), (8, 1, 128), (16, 8, 64), (9, 9, 32)])
+@pytest.mark.parametrize("lengths, tokens", [([1100], 1), ([1030, 0, 2100, 3], 3), ([600], 5)], ids=str)
+def test_lists_of_several_blocks(lengths, tokens, heads, kv_heads, dim, dtype):
+    _check(_case(26, lengths, heads, kv_heads, dim, dtype, bias=True, cap=5.0, tokens=tokens))
+
+
+@pytest.mark.parametrize("lengths", [[512], [513], [1023], [1024], [1025], [4095, 1] + [0] * 9, [4096, 1] + [0] * 9, [0, 4096] + [0] * 8, [64] * 64, [64] * 63 + [65]], ids=lambda x: f"{len(x)}_{sum(x)}")
+@pytest.mark.parametrize("heads, kv_heads, dim", [(8, 1, 128), (4, 2, 64)])
+def test_where_lists_begin_to_share_blocks(lengths, heads, kv_heads, dim):
+    _check(_case(27, lengths, heads, kv_heads, dim))
+
+
 @pytest.mark.parametrize("tokens", [1, 2, 3, 4, 5, 9, 33, 70])
 @pytest.mark.parametrize("heads, kv_heads", [(8, 1), (4, 4), (20, 4)])
 def test_tokens(tokens, heads, kv_heads):
