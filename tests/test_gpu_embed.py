@@ -142,6 +142,16 @@ def test_accumulation_into_rows_of_odd_sizes(n, dim, dtype):
         _backward(dout, ids, 300, 0.5, out=_table(23, 300, dim, to), accumulate=True)
 
 
+@pytest.mark.parametrize("run", [7, 8, 9, 63, 64, 65, 66, 127, 1000, 4000])
+@pytest.mark.parametrize("before", [0, 1, 7, 8, 90])
+@pytest.mark.parametrize("dim, dtype", [(3, torch.float32), (40, torch.bfloat16), (333, torch.float16)])
+def test_runs_of_one_entity(before, run, dim, dtype):
+    ids = torch.cat([torch.arange(before), torch.full((run,), 100), torch.tensor([101, 103])]).int()[torch.randperm(before + run + 2, generator=torch.Generator().manual_seed(28))]
+    dout = _table(29, len(ids), dim, dtype, 0.1)
+    _backward(dout, ids, 110)
+    _backward(dout, ids, 110, 2.0, out=_table(30, 110, dim, dtype), accumulate=True)
+
+
 @pytest.mark.parametrize("n", [12_288, 131_072, 262_143, 262_145])
 @pytest.mark.parametrize("entities, skew", [(3000, 4), (300_000, 1)])
 def test_long_lists(n, entities, skew):
