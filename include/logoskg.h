@@ -678,6 +678,7 @@ logoskg_status logoskg_embed_entities_backward(const logoskg_embedding_grad *e);
  * held the samples to), t the row's target:
  *     lse = log sum exp(x),   logp = x[t] - lse
  * A target outside [0, vocab) pads: logp 0.  One that is hidden, or whose logit is -inf: logp -inf.
+ * An allowed NaN or +inf makes NaN of its row's lse, and of its logp where the target is allowed.
  * The clipped policy loss, with r = exp(logp - old) and A the advantage:
  *     l = -min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A) + kl (exp(ref - logp) - (ref - logp) - 1)
  *     loss = sum of weight l over the rows that neither pad nor have a logp of -inf

@@ -57,7 +57,7 @@ def policy(logits, target, advantage=None, old=None, ref=None, weight=None, clip
     """(results, bounds): "logp" and "lse", and with an advantage "loss" and "dlogits".
 
     An exponential's argument (x - top) scale is off by 2 roundings, the exponential by two more; a sum's terms go by 64 threads at
-    least, or V / 512 in turn; so each of exp's relative errors enters lse by its share p."""
+    least, or V / 512 in turn (rows of up to 1,024 by 16 threads, 64 terms each in four sums: 22 in turn); so each of exp's relative errors enters lse by its share p."""
     (R, V), dtype = logits.shape, logits.dtype
     x = logits.detach().cpu().double() * scale
     hidden = torch.zeros(R, V, dtype=torch.bool)
@@ -113,6 +113,9 @@ def policy(logits, target, advantage=None, old=None, ref=None, weight=None, clip
     res["dlogits"] = torch.where(counts[:, None], g * (hot - p), 0.0)
     tol["dlogits"] = g_tol * (hot - p).abs() + 1.1 * g.abs() * (share_tol + 4 * E32 * (hot - p).abs())
     tol["dlogits"] = torch.where(counts[:, None], tol["dlogits"] + UNIT[dtype] * (res["dlogits"].abs() + tol["dlogits"]) + LEAST[dtype], 0.0)
+    # what rounds to more than the type holds (float16: from 65,520 on, half a step above its largest) is infinite
+    over = res["dlogits"].abs() - tol["dlogits"] > torch.finfo(dtype).max * (1 + torch.finfo(dtype).eps / 4)
+    res["dlogits"] = torch.where(over, torch.sign(res["dlogits"]) * math.inf, res["dlogits"])
     return res, tol
 
 

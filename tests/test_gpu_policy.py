@@ -229,6 +229,23 @@ def test_logits_beyond_32_bits():
     assert abs(float(last[(rows - 1) % vocab]) + 1) < 0.01 and abs(float(last[5]) * vocab - 1) < 0.01
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=TYPE_NAMES)
+@pytest.mark.parametrize("rows, vocab", [(6, 300), (100, 300), (6, 5000), (6, 60_000)])
+def test_nan_and_infinity_among_allowed_logits(rows, vocab, dtype):
+    a = _case(13, rows, vocab, dtype)
+    a["logits"][0, 7], a["logits"][1, vocab - 1], a["logits"][2, 3] = math.nan, math.inf, math.inf
+    a["target"][:4] = torch.tensor([5, 6, 3, -1], dtype=torch.int32)
+    a["logits"][3, 0] = math.nan  # of a row that pads
+    a = a | dict(old=None, ref=torch.zeros(rows), kl=0.1)
+    got = lkg.policy_loss(**_gpu(a), gradient=True)
+    assert got["lse"][:4].isnan().all() and got["logp"][:3].isnan().all() and got["logp"][3] == 0 and got["loss"].isnan()
+    assert got["dlogits"][:3].isnan().all() and (got["dlogits"][3] == 0).all()
+    rest = {k: x[4:] if isinstance(x, torch.Tensor) else x for k, x in a.items()}
+    res, tol = oracle.policy(**rest)
+    for name in ("logp", "lse", "dlogits"):
+        oracle.check(got[name][4:], res[name], tol[name], name)
+
+
 def test_what_the_binding_refuses():
     a = _gpu(_case(11, 4, 70, masks=2))
     for change, says in [(dict(target=a["target"].long()), "int32"), (dict(target=a["target"][:3]), "shape"), (dict(advantage=a["advantage"].double()), "float32"), (dict(mask=a["mask"][:, :1]), "mask"),
