@@ -590,13 +590,14 @@ static logoskg_status packed_args(const logoskg_entity_read *r, PackedArgs *pa, 
     // Blocks of 64 entries, larger ones (up to 4,096) where there are more than eight rounds of them: a block's begin costs as much as some tiles
     a->shift = 6;
     // Few entries go to one block a list, whose wavefronts share it, and nothing is joined behind, a launch and a workspace less: up to 4,096, where an
-    // average list is a tile or two for each of eight wavefronts.  (One token, 32 / 8 heads of 128, a call and on the GPU: one list of 200 14.7
+    // average list is a tile or two for each of the wavefronts that share it (and where those are one or two, 512 each).  (One token, 32 / 8 heads of 128, a call and on the GPU: one list of 200 14.7
     // and 10.6 us, so 10.0 and 8.6; 16 of 250 14.8 and 12.8, so 11.6 and 11.3; one of 900 would be 14.8 and 12.6, 14.7 and 14.5, of 4,000 22 and 34.
     // Of heads of 64 one of 900 14.5 and 10.4, so 10.2 and 9.3.)
-    const long long few = std::min<long long>(4096, (long long)(groups <= 2 ? 1024 : 512) * a->num_queries);
+    const int spare = 8 / (pa->heads_in * pa->rows_in);  // wavefronts to a list
+    const long long few = std::min<long long>(spare >= 4 ? 4096 : 512 * spare, (long long)(groups <= 2 ? 128 : 64) * spare * a->num_queries);
     while (a->num_entries <= few && a->num_entries >> a->shift > 0) a->shift++;
     while (a->shift < 12 && (a->num_entries >> a->shift) * each > (groups <= 2 ? 4096 : 2048)) a->shift++;
-    const int tiles = 1 << (a->shift - 6), spare = 8 / (pa->heads_in * pa->rows_in);
+    const int tiles = 1 << (a->shift - 6);
     pa->streams = tiles < spare ? tiles : spare;
     a->blocks = (a->num_entries >> a->shift) + a->num_queries;
     if ((a->blocks + 8) * (a->kv_heads / pa->heads_in) >= (1ll << 31) || pa->row_groups > 65535 || (long long)a->num_queries * a->tokens * a->heads >= (1ll << 32)) { set_error("%s: too many rows", call); return LOGOSKG_EINVAL; }
