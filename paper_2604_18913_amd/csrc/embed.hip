@@ -69,7 +69,7 @@ struct GradArgs {
     const void *dout;
     void *dtable;
     unsigned *key[2], *place[2];  // of the sort: from one to the other and back
-    unsigned *count, *total;      // [digits][tiles], [digits]
+    unsigned *count, *total;      // [tiles][digits], [digits]
     float *part;                  // [chunks][2][dim]: of the run that comes in from the chunk before, and of the one that goes on
     unsigned *gap_pieces;         // how many there are of ..
     uint2 *gap;                   // .. pieces of long gaps: first row and the one behind
@@ -195,7 +195,8 @@ template <class O, int PER, int MOST> __global__ __launch_bounds__(1024) void k_
 }
 
 // A pass of the sort over tiles, of 512 ids, or 2,048 where those are enough for the card: how often a digit occurs in each tile ..  (A chain of
-// waits: 65,536 ids 5.8 us here, 4.5 and 8.4 in the two behind, with tiles of 2,048 5.6, 4.4 and 11; 550,000 ids 8.7, 4.8 and 18.)
+// waits: 65,536 ids 4.8 us here, 4.6 and 8.1 in the two behind, with tiles of 2,048 11 in the last; 550,000 ids 6.6, 4.9 and 18; counts by
+// digit, tile after tile, 8.7, 4.8 and 18; 6 million ids 16, 20 and 155.)
 template <class O> __global__ __launch_bounds__(256) void k_sort_count(GradArgs a, int pass, int shift, int bits, Rows rows) {
     extern __shared__ unsigned found[];
     if ((int)blockIdx.x >= a.tiles) return clear_share<O, 256>(a, rows, blockIdx.x - a.tiles);
@@ -210,23 +211,46 @@ template <class O> __global__ __launch_bounds__(256) void k_sort_count(GradArgs 
         atomicAdd(&found[key >> shift & (digits - 1)], 1u);
     }
     __syncthreads();
-    for (int i = tid; i < digits; i += 256) a.count[(long long)i * a.tiles + blockIdx.x] = found[i];
+    for (int i = tid; i < digits; i += 256) a.count[(long long)blockIdx.x * digits + i] = found[i];
 }
 
-// .. how often before each tile, and in all (a block per digit) ..
-template <class O> __global__ __launch_bounds__(256) void k_sort_before(GradArgs a, int digits, Rows rows) {
-    __shared__ unsigned box[4];
-    if ((int)blockIdx.x >= digits) return clear_share<O, 256>(a, rows, blockIdx.x - digits);
-    unsigned *count = a.count + (long long)blockIdx.x * a.tiles;
+// .. how often before each tile, and in all (a block per 16 digits, a 32nd of the tiles to 16 threads) ..
+template <class O> __global__ __launch_bounds__(512) void k_sort_before(GradArgs a, int digits, Rows rows) {
+    constexpr int kDigits = 16, kSlices = 32, kAhead = 8;
+    __shared__ unsigned box[kSlices][kDigits];
+    const int blocks = (digits + kDigits - 1) / kDigits;
+    if ((int)blockIdx.x >= blocks) return clear_share<O, 512>(a, rows, blockIdx.x - blocks);
+    const int d = blockIdx.x * kDigits + threadIdx.x % kDigits, slice = threadIdx.x / kDigits, each = (a.tiles + kSlices - 1) / kSlices;
+    const int from = slice * each, to = from + each < a.tiles ? from + each : a.tiles;
+    unsigned *count = a.count + d;
     unsigned sum = 0;
-    for (int at = 0; at < a.tiles; at += 256) {
-        const int i = at + threadIdx.x;
-        unsigned all, x = i < a.tiles ? count[i] : 0;
-        const unsigned before = block_before<256>(x, box, all);
-        if (i < a.tiles) count[i] = sum + before;
-        sum += all;
+    for (int t = from; t < to; t += kAhead) {
+        unsigned x[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) x[u] = t + u < to && d < digits ? count[(long long)(t + u) * digits] : 0;
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) sum += x[u];
     }
-    if (threadIdx.x == 0) a.total[blockIdx.x] = sum;
+    box[slice][threadIdx.x % kDigits] = sum;
+    __syncthreads();
+    unsigned before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kSlices; w++) {
+        if (w == slice) before = all;
+        all += box[w][threadIdx.x % kDigits];
+    }
+    if (d >= digits) return;
+    if (slice == 0) a.total[d] = all;
+    for (int t = from; t < to; t += kAhead) {
+        unsigned x[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) x[u] = t + u < to ? count[(long long)(t + u) * digits] : 0;
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) {
+            if (t + u < to) count[(long long)(t + u) * digits] = before;
+            before += x[u];
+        }
+    }
 }
 
 // .. and every id to its place: behind the smaller digits, those of the tiles before, the wavefronts before and the lanes before.
@@ -245,7 +269,7 @@ template <class O, int TILE> __global__ __launch_bounds__(256) void k_sort_move(
     for (int j = 0; j < kPer; j++) {
         const bool in = j < per && first + j < digits;
         total[j] = in ? a.total[first + j] : 0;
-        tile[j] = in ? a.count[(long long)(first + j) * a.tiles + blockIdx.x] : 0;
+        tile[j] = in ? a.count[(long long)blockIdx.x * digits + first + j] : 0;
     }
     for (int i = tid; i < 4 * digits; i += 256) count[i] = 0;
     __syncthreads();
@@ -581,7 +605,7 @@ template <class T, class O> static logoskg_status launch_grad(GradArgs &a, hipSt
             const Rows one = share(4 * pass, 4 * pass + 1, 4 * passes), two = share(4 * pass + 1, 4 * pass + 2, 4 * passes), rest = share(4 * pass + 2, 4 * pass + 4, 4 * passes);
             k_sort_count<O><<<dim3(a.tiles + one.blocks), 256, 4 << bits, st>>>(a, pass, shift, bits, one);
             LKG_HIP(hipGetLastError());
-            k_sort_before<O><<<dim3((1 << bits) + two.blocks), 256, 0, st>>>(a, 1 << bits, two);
+            k_sort_before<O><<<dim3(((1 << bits) + 15) / 16 + two.blocks), 512, 0, st>>>(a, 1 << bits, two);
             LKG_HIP(hipGetLastError());
             if (a.tile == 512) k_sort_move<O, 512><<<dim3(a.tiles + rest.blocks), 256, 16 << bits, st>>>(a, pass, shift, bits, rest);
             else k_sort_move<O, 2048><<<dim3(a.tiles + rest.blocks), 256, 16 << bits, st>>>(a, pass, shift, bits, rest);
