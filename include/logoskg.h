@@ -681,9 +681,10 @@ logoskg_status logoskg_embed_entities_backward(const logoskg_embedding_grad *e);
  * An allowed NaN or +inf makes NaN of its row's lse, and of its logp where the target is allowed.
  * The clipped policy loss, with r = exp(logp - old) and A the advantage:
  *     l = -min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A) + kl (exp(ref - logp) - (ref - logp) - 1)
- *     loss = sum of weight l over the rows that neither pad nor have a logp of -inf
+ *     loss = sum of weight l over the rows that count: that do not pad, have a logp above -inf and a weight other than 0
  *     dlogits[v] = dloss weight dl/dlogp scale ([v = t] - exp(x[v] - lse)),  0 for ids that the mask hides
- * where dl/dlogp has the first term of l where r A is the smaller of the two or both are alike.
+ * where dl/dlogp has the first term of l where r A is the smaller of the two or both are alike.  Rows that do not count
+ * have dlogits of 0, whatever stands in them and beside them and whatever dloss is.
  */
 typedef struct {
     uint32_t struct_size;     /* sizeof(logoskg_policy)                                      */

@@ -39,6 +39,10 @@ struct Beside { float advantage, old, ref, weight; };
 __device__ __forceinline__ Beside beside(const PolicyArgs &a, int r) {
     return Beside{a.advantage[r], a.old ? a.old[r] : 0.f, a.kl > 0.f ? a.ref[r] : 0.f, a.weight ? a.weight[r] : 1.f};
 }
+// Rows that pad, whose answer cannot be or that weigh nothing do not count: their loss and gradient are 0 whatever stands beside them.
+__device__ __forceinline__ bool row_counts(const PolicyArgs &a, const Beside &row, int target, float logp) {
+    return target >= 0 && target < a.vocab && logp != -INFINITY && row.weight != 0.f;
+}
 // A row's loss and what its logp's gradient is, weight included; 0 and 0 for rows that do not count.
 __device__ __forceinline__ void row_terms(const PolicyArgs &a, const Beside &row, float logp, bool counts, float &loss, float &slope) {
     loss = slope = 0.f;
@@ -57,7 +61,6 @@ __device__ __forceinline__ void row_terms(const PolicyArgs &a, const Beside &row
     }
     loss *= w;
     slope *= w;
-    if (w == 0.f) loss = slope = 0.f;
 }
 
 // Exponents up to this size, in units of log 2, are made in one step, x k minus a product that is rounded before: 2^-19 of the exponential
@@ -102,6 +105,7 @@ template <class T, int THREADS, int MODE, bool MASKED, int KEEP, bool WHOLE> str
     static constexpr int kStaged = MASKED && WHOLE ? THREADS * KEEP * (16 / (int)sizeof(T)) / 32 : 1;
     unsigned staged[kStaged];
     float tops[(THREADS + 63) / 64], sums[(THREADS + 63) / 64], said[2];
+    bool counts;
 };
 template <class T, int THREADS, int MODE, bool MASKED, int KEEP, bool WHOLE> __device__ __forceinline__ void policy_row(const PolicyArgs &a, int r, int tid, RowShared<T, THREADS, MODE, MASKED, KEEP, WHOLE> &shared) {
     constexpr int V = 16 / sizeof(T), kWaves = THREADS / 64;
@@ -267,17 +271,19 @@ template <class T, int THREADS, int MODE, bool MASKED, int KEEP, bool WHOLE> __d
     if (MODE == kLogp) return;
     if (tid == 0) {
         float loss;
-        row_terms(a, row, logp, (unsigned)target < vocab && logp != -INFINITY, loss, slope);
-        if (MODE == kBackward && a.dloss) slope *= *a.dloss;
+        const bool counts = row_counts(a, row, target, logp);
+        row_terms(a, row, logp, counts, loss, slope);
+        if (MODE == kBackward && a.dloss) slope *= *a.dloss;  // (it may be infinite or NaN, and this NaN of a row that does not count)
         said[0] = slope * a.scale;
         said[1] = logp;
+        shared.counts = counts;
     }
     if (MODE == kLoss) return;
     all_here();
     slope = said[0];
     logp = said[1];
     T *out = (T *)a.dlogits + (long long)r * vocab;
-    if (slope == 0.f || closed) {  // zeros, whatever the logits are
+    if (!shared.counts || slope == 0.f) {  // zeros, whatever the logits are; behind this the target is an id
         const unsigned lead1 = (unsigned)((16 - ((uintptr_t)out & 15)) & 15) / sizeof(T), before = lead1 < vocab ? lead1 : vocab, whole = (vocab - before) / V, behind = before + whole * V;
         if ((unsigned)tid < before) out[tid] = (T)0.f;
         if (behind + tid < vocab) out[behind + tid] = (T)0.f;
@@ -329,7 +335,7 @@ template <int THREADS> __device__ __forceinline__ void add_rows(const PolicyArgs
     double sum = 0.0;
     auto add = [&](int target, float logp, const Beside &row) {
         float loss, slope;
-        row_terms(a, row, logp, target >= 0 && target < a.vocab && logp != -INFINITY, loss, slope);
+        row_terms(a, row, logp, row_counts(a, row, target, logp), loss, slope);
         sum += loss;
     };
     int r = threadIdx.x;

@@ -258,3 +258,47 @@ def test_what_the_binding_refuses():
         lkg.policy_loss_backward(torch.ones(1, device="cuda"), a["logits"], a["target"], a["advantage"], a["weight"])
     with pytest.raises(lkg.LogosKGError, match="scale"):
         lkg.policy_loss(**{**a, "scale": 0.0})
+
+
+# A vocabulary for every kernel: by 16, 64, 256 (twice) and 1,024 lanes a row (under masks in two sweeps, else whole rows of two sizes, and two sweeps)
+KERNELS = [300, 1501, 6001, 20_001, 60_001, 120_001, 200_001]
+
+
+def _raw(call, a, dlogits, lse=None, dloss=None, logits=None):
+    """The C call on a gradient that the caller has; (loss, logp, lse) of a forward."""
+    from paper_2604_18913_amd import training
+    from paper_2604_18913_amd.binding import _check as check, _load, _stream_handle
+    x = a["logits"] if logits is None else logits
+    head, device, rows = training._answers(x, a["target"], a.get("mask"), a.get("mask_row"))
+    terms = training._terms(a["advantage"], a.get("old"), a.get("ref"), a.get("weight"), a.get("clip", (0.2, 0.2)), a.get("kl", 0.0), a.get("scale", 1.0), rows, device)
+    loss, logp = torch.empty((), device="cuda"), torch.empty(rows, device="cuda")
+    lse = torch.empty(rows, device="cuda") if lse is None else lse
+    check(getattr(_load(), call)(training._policy_of(*head, *terms, logp.data_ptr(), lse.data_ptr(), loss.data_ptr(), dlogits.data_ptr(), 0 if dloss is None else dloss.data_ptr(),
+                                                     _stream_handle(None, device))))
+    return loss, logp, lse
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=TYPE_NAMES)
+@pytest.mark.parametrize("masks", [None, 2], ids=["open", "masked"])
+@pytest.mark.parametrize("vocab", KERNELS)
+def test_rows_that_do_not_count_under_a_loss_that_is_not_finite(vocab, masks, dtype):
+    rows, pad = 9, 512
+    a = _case(30, rows, vocab, dtype, masks=masks)
+    idle = torch.tensor([True, True, False, True, True, False, True, masks is not None, True])
+    a["target"][[0, 1, 3, 4, 8]] = torch.tensor([-1, -100, vocab, 2 ** 31 - 1, -3], dtype=torch.int32)
+    a["weight"][6] = 0.0
+    if masks:
+        a["mask_row"] = torch.tensor([0, 1, 0, 1, 0, 0, 1, -1, 0], dtype=torch.int32)
+        for r in (2, 5):
+            a["mask"][0, int(a["target"][r]) // 64] |= -2 ** 63 if int(a["target"][r]) % 64 == 63 else 1 << int(a["target"][r]) % 64
+        hidden = ~((a["mask"][0][:, None] >> torch.arange(64)) & 1).reshape(-1)[:vocab].bool()
+    b = _gpu(a)
+    lse = lkg.token_logp(**{k: b[k] for k in ("logits", "target", "scale", "mask", "mask_row") if k in b})["lse"]
+    for dloss in (math.inf, -math.inf, math.nan):
+        flat = torch.full((pad + rows * vocab + pad,), 7.0, dtype=dtype, device="cuda")
+        got = flat[pad:pad + rows * vocab].view(rows, vocab)
+        _raw("logoskg_policy_loss_backward", b, got, lse, torch.tensor(dloss, device="cuda"))
+        assert (flat[:pad] == 7).all() and (flat[-pad:] == 7).all()
+        assert (got[idle] == 0).all() and not got[~idle].isfinite().all(1).any()
+        if masks:
+            assert (got[[2, 5]][:, hidden] == 0).all()
