@@ -105,7 +105,6 @@ template <class T, int THREADS, int MODE, bool MASKED, int KEEP, bool WHOLE> str
     static constexpr int kStaged = MASKED && WHOLE ? THREADS * KEEP * (16 / (int)sizeof(T)) / 32 : 1;
     unsigned staged[kStaged];
     float tops[(THREADS + 63) / 64], sums[(THREADS + 63) / 64], said[2];
-    bool counts;
 };
 template <class T, int THREADS, int MODE, bool MASKED, int KEEP, bool WHOLE> __device__ __forceinline__ void policy_row(const PolicyArgs &a, int r, int tid, RowShared<T, THREADS, MODE, MASKED, KEEP, WHOLE> &shared) {
     constexpr int V = 16 / sizeof(T), kWaves = THREADS / 64;
@@ -275,15 +274,14 @@ template <class T, int THREADS, int MODE, bool MASKED, int KEEP, bool WHOLE> __d
         row_terms(a, row, logp, counts, loss, slope);
         if (MODE == kBackward && a.dloss) slope *= *a.dloss;  // (it may be infinite or NaN, and this NaN of a row that does not count)
         said[0] = slope * a.scale;
-        said[1] = logp;
-        shared.counts = counts;
+        said[1] = counts ? logp : -INFINITY;
     }
     if (MODE == kLoss) return;
     all_here();
     slope = said[0];
     logp = said[1];
     T *out = (T *)a.dlogits + (long long)r * vocab;
-    if (!shared.counts || slope == 0.f) {  // zeros, whatever the logits are; behind this the target is an id
+    if (logp == -INFINITY || slope == 0.f) {  // zeros, whatever the logits are; behind this the target is an id
         const unsigned lead1 = (unsigned)((16 - ((uintptr_t)out & 15)) & 15) / sizeof(T), before = lead1 < vocab ? lead1 : vocab, whole = (vocab - before) / V, behind = before + whole * V;
         if ((unsigned)tid < before) out[tid] = (T)0.f;
         if (behind + tid < vocab) out[behind + tid] = (T)0.f;
