@@ -317,8 +317,16 @@ template <class T, int THREADS, int MODE, bool MASKED, int KEEP, bool WHOLE> __d
     };
     if (MODE == kBackward || __builtin_fabsf(lse * kLog2e) < kNear) write_row(std::false_type{});
     else write_row(std::true_type{});
-    if (THREADS <= 64) __threadfence_block();  // (a thread's share of the target is written over)
-    all_here();
+    auto written = [&] {  // before others write over it
+        if (THREADS <= 64) __threadfence_block();
+        all_here();
+    };
+    written();
+    if (MASKED && WHOLE && kKept > 0 && !(lse - lse == 0.f && slope - slope == 0.f)) {  // what is hidden has come through the products as NaN
+        for (unsigned v = tid; v < vocab; v += THREADS)
+            if (!allowed(v)) out[v] = (T)0.f;
+        written();
+    }
     if (tid == 0) out[target] = (T)(-slope * expm1f(logp));
 }
 

@@ -302,3 +302,24 @@ def test_rows_that_do_not_count_under_a_loss_that_is_not_finite(vocab, masks, dt
         assert (got[idle] == 0).all() and not got[~idle].isfinite().all(1).any()
         if masks:
             assert (got[[2, 5]][:, hidden] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=TYPE_NAMES)
+@pytest.mark.parametrize("rows, vocab", [(100, 300)] + [(6, v) for v in KERNELS])
+def test_hidden_ids_get_no_gradient_whatever_their_row_holds(rows, vocab, dtype):
+    a = _case(31, rows, vocab, dtype, masks=2)
+    a["mask_row"][:] = 0
+    a["target"][:] = 70
+    a["mask"][0, 0] |= 1 << 9
+    a["mask"][0, 1] |= 1 << 70 - 64
+    hidden = ~((a["mask"][0][:, None] >> torch.arange(64)) & 1).reshape(-1)[:vocab].bool()
+    a["logits"][0, 9], a["logits"][1, 9], a["logits"][2, 70] = math.nan, math.inf, math.nan
+    a["logits"][3, hidden.nonzero()[:2, 0]] = torch.tensor([math.nan, math.inf], dtype=dtype)
+    a["old"][4], a["advantage"][4] = -1000.0, -1.0  # a ratio above 32 bits
+    b = _gpu(a)
+    got = lkg.policy_loss(**b, gradient=True)
+    rest = {k: x for k, x in b.items() if k not in ("logits", "target", "advantage")}
+    back = lkg.policy_loss_backward(torch.tensor(1.0, device="cuda"), b["logits"], b["target"], b["advantage"], got["lse"], **rest)
+    for d in (got["dlogits"], back):
+        assert (d[:, hidden] == 0).all()
+        assert d[0, ~hidden].isnan().all() and d[1, ~hidden].isnan().all() and d[2, ~hidden].isnan().all() and d[4, 70] == math.inf and d[5].isfinite().all()
