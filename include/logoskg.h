@@ -690,7 +690,7 @@ typedef struct {
     uint32_t struct_size;     /* sizeof(logoskg_policy)                                      */
     int32_t device;
     int32_t dtype;            /* of logits and dlogits                                       */
-    int32_t num_rows;
+    int32_t num_rows;         /* below 2^31 - 2^16                                           */
     int64_t vocab;            /* a row takes less than 2^32 - 2^20 bytes                     */
     int64_t row;              /* stride of the rows of logits, in elements                   */
     const void *logits;       /* device                                                      */

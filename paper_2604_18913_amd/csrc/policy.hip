@@ -430,7 +430,8 @@ template <class T> static logoskg_status launch_policy(int mode, const PolicyArg
 static const char *policy_args(const logoskg_policy *p, int mode, PolicyArgs *a) {
     if (!p || p->struct_size != sizeof(logoskg_policy)) return "struct_size";
     if (p->dtype < LOGOSKG_F32 || p->dtype > LOGOSKG_F16) return "unknown type";
-    if (p->num_rows < 0 || p->vocab < 0 || p->vocab * size_of(p->dtype) >= (1ll << 32) - (1 << 20) || p->vocab >= (1ll << 31) - (1 << 16) || p->num_masks < 0 || p->num_masks >= (1ll << 31)) return "a count is out of range";
+    // (rows are counted in 32 bits, by steps of up to 2^13 behind the last)
+    if (p->num_rows < 0 || p->num_rows > INT32_MAX - (1 << 16) || p->vocab < 0 || p->vocab * size_of(p->dtype) >= (1ll << 32) - (1 << 20) || p->vocab >= (1ll << 31) - (1 << 16) || p->num_masks < 0 || p->num_masks >= (1ll << 31)) return "a count is out of range";
     if (p->row < 0 || (p->row < p->vocab && p->num_rows > 1)) return "rows overlap";
     if (p->num_rows && ((p->vocab && !p->logits) || !p->target || !p->lse)) return "logits, target or lse is NULL";
     if (!aligned_to(p->logits, p->dtype) || !aligned_to(p->dlogits, p->dtype)) return kUnaligned;

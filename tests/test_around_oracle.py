@@ -184,6 +184,13 @@ def test_further_policy_refusals():
         training._terms(x[:, 0], None, None, None, (0.2, 0.2), 0.1, 1.0, 2, 0)
 
 
+@pytest.mark.parametrize("call", ["logoskg_token_logp", "logoskg_policy_loss", "logoskg_policy_loss_backward"])
+def test_policy_rows_whose_numbers_leave_32_bits_are_refused(call):
+    for rows in (2 ** 31 - 1, 2 ** 31 - 2 ** 16):
+        rc, text = _status(call, training._Policy(**{**_POLICY, "num_rows": rows, "vocab": 1, "row": 1}))
+        assert rc == 1 and "count" in text, text
+
+
 class _Fake:
     """A tensor that says it is on the GPU."""
 
