@@ -9,7 +9,7 @@ static_assert(sizeof(logoskg_policy) == 168, "the ctypes binding mirrors this la
 typedef unsigned long long u64;
 
 struct PolicyArgs {
-    int num_rows, num_masks;
+    int num_rows, num_masks, first;  // first: row of a launch
     long long vocab, row, words;
     const void *logits;
     const int32_t *target, *mask_row;
@@ -332,7 +332,7 @@ template <class T, int THREADS, int MODE, bool MASKED, int KEEP, bool WHOLE> __d
 
 template <class T, int THREADS, int MODE, bool MASKED, int KEEP, bool WHOLE> __global__ __launch_bounds__(THREADS, 4) void k_policy(PolicyArgs a) {
     __shared__ RowShared<T, THREADS, MODE, MASKED, KEEP, WHOLE> shared;
-    policy_row<T, THREADS, MODE, MASKED, KEEP, WHOLE>(a, blockIdx.x, threadIdx.x, shared);
+    policy_row<T, THREADS, MODE, MASKED, KEEP, WHOLE>(a, a.first + blockIdx.x, threadIdx.x, shared);
 }
 
 // The rows' losses, made again of their logp, and their sum in a fixed order.  (One block's: 2 us, of 500,000 rows 165, and 325
@@ -378,7 +378,7 @@ template <class T, int MODE, bool MASKED, int THREADS, bool SUM> __global__ __la
     constexpr int L = kShortLanes;
     __shared__ RowShared<T, L, MODE, MASKED, kShortChunks, true> shared[THREADS / L];
     __shared__ double box[THREADS / 64];
-    const int r = blockIdx.x * (THREADS / L) + threadIdx.x / L;
+    const int r = a.first + blockIdx.x * (THREADS / L) + threadIdx.x / L;
     if (r < a.num_rows) policy_row<T, L, MODE, MASKED, kShortChunks, true>(a, r, threadIdx.x % L, shared[threadIdx.x / L]);
     if (!SUM) return;
     __threadfence_block();
@@ -386,9 +386,23 @@ template <class T, int MODE, bool MASKED, int THREADS, bool SUM> __global__ __la
     add_rows<THREADS>(a, box);
 }
 
-template <class T, int THREADS, int MODE, int KEEP, bool WHOLE> static void launch_rows(const PolicyArgs &a, hipStream_t st) {
-    if (a.mask) k_policy<T, THREADS, MODE, true, KEEP, WHOLE><<<dim3(a.num_rows), THREADS, 0, st>>>(a);
-    else k_policy<T, THREADS, MODE, false, KEEP, WHOLE><<<dim3(a.num_rows), THREADS, 0, st>>>(a);
+// A block a row, in launches of fewer than 2^32 threads.
+template <class T, int THREADS, int MODE, bool MASKED, int KEEP, bool WHOLE> static void launch_rows(PolicyArgs a, hipStream_t st) {
+    launch_ranges(a.num_rows, 1, [&](long long first, long long n) {
+        a.first = (int)first;
+        k_policy<T, THREADS, MODE, MASKED, KEEP, WHOLE><<<dim3((unsigned)n), THREADS, 0, st>>>(a);
+    }, (long long)UINT32_MAX / THREADS);
+}
+template <class T, int THREADS, int MODE, int KEEP> static void launch_rows(const PolicyArgs &a, hipStream_t st) {
+    a.mask ? launch_rows<T, THREADS, MODE, true, KEEP, true>(a, st) : launch_rows<T, THREADS, MODE, false, KEEP, true>(a, st);
+}
+template <class T, int MODE> static void launch_short_rows(PolicyArgs a, hipStream_t st) {
+    constexpr int kRows = 256 / kShortLanes;
+    launch_ranges(a.num_rows, kRows, [&](long long first, long long n) {
+        a.first = (int)first;
+        const dim3 blocks((unsigned)((n + kRows - 1) / kRows));
+        a.mask ? k_policy_short<T, MODE, true, 256, false><<<blocks, 256, 0, st>>>(a) : k_policy_short<T, MODE, false, 256, false><<<blocks, 256, 0, st>>>(a);
+    });
 }
 
 template <class T, int MODE> static logoskg_status launch_policy(const PolicyArgs &a, hipStream_t st) {
@@ -404,16 +418,14 @@ template <class T, int MODE> static logoskg_status launch_policy(const PolicyArg
         // 32,000 bfloat16 logits under masks 208 us (264 in two sweeps), 2,048 rows of 150,001 without 284 (317), 4,096 of 80,000 without
         // 261 (272).  Long rows under masks in two sweeps over memory, two blocks of a unit in turn: 4,096 of 80,000 298 us (318 in registers,
         // where one block fits and its loads, exponentials and stores take turns), 2,048 of 150,001 332 (334).
-        if (chunks <= kShortLanes * kShortChunks) {
-            const dim3 blocks((a.num_rows + 15) / 16);
-            a.mask ? k_policy_short<T, MODE, true, 256, false><<<blocks, 256, 0, st>>>(a) : k_policy_short<T, MODE, false, 256, false><<<blocks, 256, 0, st>>>(a);
-        } else if (chunks <= 64 * 4) launch_rows<T, 64, MODE, 4, true>(a, st);
-        else if (chunks <= 256 * 4) launch_rows<T, 256, MODE, 4, true>(a, st);
-        else if (chunks <= 256 * 16) launch_rows<T, 256, MODE, 16, true>(a, st);
-        else if (a.mask) k_policy<T, 1024, MODE, true, 2, false><<<dim3(a.num_rows), 1024, 0, st>>>(a);
-        else if (chunks <= 1024 * 10) k_policy<T, 1024, MODE, false, 10, true><<<dim3(a.num_rows), 1024, 0, st>>>(a);
-        else if (chunks <= 1024 * 20) k_policy<T, 1024, MODE, false, 20, true><<<dim3(a.num_rows), 1024, 0, st>>>(a);
-        else k_policy<T, 1024, MODE, false, 4, false><<<dim3(a.num_rows), 1024, 0, st>>>(a);
+        if (chunks <= kShortLanes * kShortChunks) launch_short_rows<T, MODE>(a, st);
+        else if (chunks <= 64 * 4) launch_rows<T, 64, MODE, 4>(a, st);
+        else if (chunks <= 256 * 4) launch_rows<T, 256, MODE, 4>(a, st);
+        else if (chunks <= 256 * 16) launch_rows<T, 256, MODE, 16>(a, st);
+        else if (a.mask) launch_rows<T, 1024, MODE, true, 2, false>(a, st);
+        else if (chunks <= 1024 * 10) launch_rows<T, 1024, MODE, false, 10, true>(a, st);
+        else if (chunks <= 1024 * 20) launch_rows<T, 1024, MODE, false, 20, true>(a, st);
+        else launch_rows<T, 1024, MODE, false, 4, false>(a, st);
         LKG_HIP(hipGetLastError());
     }
     if (sum) {

@@ -323,3 +323,21 @@ def test_hidden_ids_get_no_gradient_whatever_their_row_holds(rows, vocab, dtype)
     for d in (got["dlogits"], back):
         assert (d[:, hidden] == 0).all()
         assert d[0, ~hidden].isnan().all() and d[1, ~hidden].isnan().all() and d[2, ~hidden].isnan().all() and d[4, 70] == math.inf and d[5].isfinite().all()
+
+
+@pytest.mark.parametrize("rows, vocab, masked", [((1 << 28) + 40, 6, False), ((1 << 28) + 40, 6, True), ((1 << 24) + 40, 2050, False)])
+def test_more_rows_than_a_launch_takes(rows, vocab, masked):
+    """Rows of 16 lanes (2^28 and more), and of 256 (2^24 and more): 2^32 threads and more."""
+    logits = torch.zeros(rows, vocab, dtype=torch.bfloat16, device="cuda")
+    target = (torch.arange(rows, device="cuda") % 6).int()
+    kw = dict(mask=torch.tensor([[63]], device="cuda"), mask_row=torch.zeros(rows, dtype=torch.int32, device="cuda")) if masked else {}
+    logits[-1, 0] = 2.0
+    target[-1] = 0
+    logp = lkg.token_logp(logits, target, **kw)["logp"]
+    share = math.exp(2) / (math.exp(2) + vocab - 1)
+    assert abs(float(logp[:-1].min()) + math.log(vocab)) < 1e-5 and abs(float(logp[:-1].max()) + math.log(vocab)) < 1e-5 and abs(float(logp[-1]) - math.log(share)) < 1e-5
+    if vocab < 10:  # (the gradient too)
+        got = lkg.policy_loss(logits, target, torch.ones(rows, device="cuda"), gradient=True, **kw)
+        assert torch.equal(got["logp"], logp) and abs(float(got["loss"]) / -rows - 1) < 1e-6
+        one = got["dlogits"].abs().amax(1)  # of the target: 1 - its share
+        assert float((one[:-1].float() - 5 / 6).abs().max()) < 0.01 and abs(float(one[-1]) - (1 - share)) < 0.01
