@@ -519,10 +519,14 @@ template <class O> __global__ __launch_bounds__(256) void k_embed_join(GradArgs 
 
 static const char *bad_type(int dtype) { return dtype < LOGOSKG_F32 || dtype > LOGOSKG_F16 ? "unknown type" : nullptr; }
 
-template <class T> static logoskg_status launch_embed(const EmbedArgs &a, hipStream_t st) {
-    const long long pieces = (a.dim * (long long)sizeof(T) + 15) / 16, blocks = (a.num_ids * pieces + 256 * kEmbedPieces - 1) / (256 * kEmbedPieces);
-    if (blocks >= (1ll << 31)) { set_error("logoskg_embed_entities: too many ids"); return LOGOSKG_EINVAL; }
-    k_embed<T><<<dim3((unsigned)blocks), 256, 0, st>>>(a, (unsigned)pieces, (unsigned)(0xffffffffll / pieces));
+template <class T> static logoskg_status launch_embed(const EmbedArgs &all, hipStream_t st) {
+    constexpr long long kBlock = 256 * kEmbedPieces;  // pieces
+    const long long pieces = (all.dim * (long long)sizeof(T) + 15) / 16;
+    launch_ranges(all.num_ids, 1, [&](long long first, long long n) {
+        EmbedArgs a = all;
+        a.num_ids = n, a.ids += first, a.out = (T *)all.out + first * all.dim;
+        k_embed<T><<<dim3((unsigned)((n * pieces + kBlock - 1) / kBlock)), 256, 0, st>>>(a, (unsigned)pieces, (unsigned)(0xffffffffll / pieces));
+    }, kMaxBlocks * kBlock / pieces);
     LKG_HIP(hipGetLastError());
     return LOGOSKG_OK;
 }

@@ -250,3 +250,14 @@ def test_what_the_binding_refuses():
             bad()
     with pytest.raises(lkg.LogosKGError, match="overlap"):
         lkg.embed_entities_backward(table[:3].clone(), ids, 4, out=table[:1].expand(4, 8))
+
+
+def test_more_ids_than_a_launch_takes():
+    n = (1 << 34) + 3000  # four rows of one element a thread: 2^32 threads and some
+    table = torch.tensor([[1.0], [2.0], [3.0]], dtype=torch.bfloat16, device="cuda")
+    ids = torch.zeros(n, dtype=torch.int32, device="cuda")
+    ids[-2500:] = 2
+    ids[-1], ids[0] = 5, 1
+    got = lkg.embed_entities(table, ids)
+    assert got.shape == (n, 1) and got[0] == 2 and got[-1] == 0
+    assert bool((got[1:-2500] == 1).all()) and bool((got[-2500:-1] == 3).all())

@@ -325,7 +325,7 @@ def test_hidden_ids_get_no_gradient_whatever_their_row_holds(rows, vocab, dtype)
         assert d[0, ~hidden].isnan().all() and d[1, ~hidden].isnan().all() and d[2, ~hidden].isnan().all() and d[4, 70] == math.inf and d[5].isfinite().all()
 
 
-@pytest.mark.parametrize("rows, vocab, masked", [((1 << 28) + 40, 6, False), ((1 << 28) + 40, 6, True), ((1 << 24) + 40, 2050, False)])
+@pytest.mark.parametrize("rows, vocab, masked", [((1 << 28) + 40, 6, False), ((1 << 28) + 40, 6, True), ((1 << 24) + 40, 2064, False)])
 def test_more_rows_than_a_launch_takes(rows, vocab, masked):
     """Rows of 16 lanes (2^28 and more), and of 256 (2^24 and more): 2^32 threads and more."""
     logits = torch.zeros(rows, vocab, dtype=torch.bfloat16, device="cuda")
