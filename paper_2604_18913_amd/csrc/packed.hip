@@ -231,7 +231,7 @@ __global__ __launch_bounds__(512, NG <= 2 ? 4 : 2) void k_read_packed(PackedArgs
     // the key heads of a block's entries one behind the other on one of the card's eight dies, which blocks take turns with
     const unsigned turn = blockIdx.x >> 3;
     const int first_head = (int)(turn % head_groups) * pa.heads_in, head = first_head + unit % pa.heads_in;
-    const long long block = (long long)(turn / head_groups) * 8 + (blockIdx.x & 7);
+    const long long block = a.first + (long long)(turn / head_groups) * 8 + (blockIdx.x & 7);
     if (block >= a.blocks) return;
     const int d = document_of(a.off, a.num_queries, a.num_entries, 1, a.shift, block, lane);
     const long long b0 = first_block(a.off, d, a.num_entries, 1, a.shift);
@@ -604,12 +604,13 @@ static logoskg_status packed_args(const logoskg_entity_read *r, PackedArgs *pa, 
     return LOGOSKG_OK;
 }
 
-template <class E, int NG, int WAYS, bool CAP, bool BIAS> static logoskg_status launch_packed(const PackedArgs &pa, hipStream_t st) {
-    const ReadArgs &a = pa.r;
+template <class E, int NG, int WAYS, bool CAP, bool BIAS> static logoskg_status launch_packed(PackedArgs pa, hipStream_t st) {
+    ReadArgs &a = pa.r;
     const int waves = pa.heads_in * pa.rows_in * pa.streams;
     const size_t bytes = (size_t)waves * piece_bytes(NG) + (size_t)pa.heads_in * pa.table_words * 4;
     LKG_TRY(allow_lds(k_read_packed<E, NG, WAYS, CAP, BIAS>, bytes));
-    k_read_packed<E, NG, WAYS, CAP, BIAS><<<dim3((unsigned)((a.blocks + 7) / 8 * 8 * (a.kv_heads / pa.heads_in)), (unsigned)((pa.row_groups + pa.rows_in - 1) / pa.rows_in)), waves * 64, bytes, st>>>(pa);
+    const unsigned row_blocks = (unsigned)((pa.row_groups + pa.rows_in - 1) / pa.rows_in);
+    each_eight_blocks(a, a.kv_heads / pa.heads_in, waves * 64, [&](unsigned blocks) { k_read_packed<E, NG, WAYS, CAP, BIAS><<<dim3(blocks, row_blocks), waves * 64, bytes, st>>>(pa); });
     LKG_HIP(hipGetLastError());
     return LOGOSKG_OK;
 }

@@ -8,7 +8,7 @@ namespace lkg {
 
 struct ReadArgs {
     int num_queries, tokens, heads, kv_heads, group, dim, rows, shift;  // rows: tokens x group per key head; 2^shift entries per block
-    long long num_entries, num_entities, blocks;
+    long long num_entries, num_entities, blocks, first;  // first: block (of the join, row) that a launch begins with
     const int64_t *off;
     const int32_t *entity, *q_pos;
     const uint8_t *hop;
@@ -27,7 +27,7 @@ struct ReadArgs {
 template <class E, int LG, int SIDES> __global__ __launch_bounds__(256) void k_read_join(ReadArgs a) {
     constexpr int kHalf = LG / SIDES, kStep = 4 * SIDES;
     const int lane = threadIdx.x % LG, side = lane / kHalf;
-    const long long at = (long long)blockIdx.x * (256 / LG) + threadIdx.x / LG, per = (long long)a.tokens * a.heads;
+    const long long at = a.first + (long long)blockIdx.x * (256 / LG) + threadIdx.x / LG, per = (long long)a.tokens * a.heads;
     if (at >= a.num_queries * per) return;
     const int d = (int)(at / per), th = (int)(at % per);
     const long long e0 = taken_into(a.off[d], a.num_entries), e1 = taken_into(a.off[d + 1], a.num_entries);
@@ -81,14 +81,26 @@ inline int64_t part_bytes(const ReadArgs &a) {  // one block per list: nothing t
     return a.num_entries <= (1ll << a.shift) ? 0 : (int64_t)a.blocks * a.tokens * a.heads * (a.dim + 2) * 4;
 }
 
-template <class E> logoskg_status launch_join(const ReadArgs &a, hipStream_t st) {
+// The blocks of a call, each for `heads` groups of key heads, in launches of fewer than 2^32 threads: launch(the grid's x) for
+// whole eights of them, which the card's dies share.
+template <class F> void each_eight_blocks(ReadArgs &a, int heads, int threads, F launch) {
+    launch_ranges((a.blocks + 7) / 8, 1, [&](long long first, long long n) {
+        a.first = 8 * first;
+        launch((unsigned)(8 * n * heads));
+    }, (long long)UINT32_MAX / threads / heads / 8);
+}
+
+template <class E> logoskg_status launch_join(ReadArgs a, hipStream_t st) {
     if (!part_bytes(a)) return LOGOSKG_OK;
     const long long n = (long long)a.num_queries * a.tokens * a.heads;
     const bool many = a.num_entries >> a.shift > 8ll * a.num_queries;
     const int lanes = (a.dim <= 64 ? 16 : 32) * (many ? 2 : 1);
-    const dim3 grid((unsigned)((n * lanes + 255) / 256));
-    if (a.dim <= 64) many ? k_read_join<E, 32, 2><<<grid, 256, 0, st>>>(a) : k_read_join<E, 16, 1><<<grid, 256, 0, st>>>(a);
-    else many ? k_read_join<E, 64, 2><<<grid, 256, 0, st>>>(a) : k_read_join<E, 32, 1><<<grid, 256, 0, st>>>(a);
+    launch_ranges(n, 256 / lanes, [&](long long first, long long rows) {
+        a.first = first;
+        const dim3 grid((unsigned)((rows * lanes + 255) / 256));
+        if (a.dim <= 64) many ? k_read_join<E, 32, 2><<<grid, 256, 0, st>>>(a) : k_read_join<E, 16, 1><<<grid, 256, 0, st>>>(a);
+        else many ? k_read_join<E, 64, 2><<<grid, 256, 0, st>>>(a) : k_read_join<E, 32, 1><<<grid, 256, 0, st>>>(a);
+    });
     LKG_HIP(hipGetLastError());
     return LOGOSKG_OK;
 }

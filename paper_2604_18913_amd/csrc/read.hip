@@ -29,7 +29,7 @@ __global__ __launch_bounds__(256, 2) void k_read(ReadArgs a) {
     // their rows lie side by side
     const unsigned turn = blockIdx.x >> 3;
     const int head = turn % a.kv_heads;
-    const long long block = (long long)(turn / a.kv_heads) * 8 + (blockIdx.x & 7);
+    const long long block = a.first + (long long)(turn / a.kv_heads) * 8 + (blockIdx.x & 7);
     if (block >= a.blocks) return;
     const int d = document_of(a.off, a.num_queries, a.num_entries, 1, a.shift, block, lane);
     const long long b0 = first_block(a.off, d, a.num_entries, 1, a.shift);
@@ -200,10 +200,10 @@ static logoskg_status read_args(const logoskg_entity_read *r, ReadArgs *a, const
     return LOGOSKG_OK;
 }
 
-template <class E, int DP, bool CAP, bool BIAS> static logoskg_status launch_read(const ReadArgs &a, hipStream_t st) {
+template <class E, int DP, bool CAP, bool BIAS> static logoskg_status launch_read(ReadArgs a, hipStream_t st) {
     size_t bytes = 4 * kReadTile * DP * 2 + (BIAS ? (size_t)a.group * (2 * a.score.max_distance + 1) * 4 : 0);
     LKG_TRY(allow_lds(k_read<E, DP, CAP, BIAS>, bytes));
-    k_read<E, DP, CAP, BIAS><<<dim3((unsigned)((a.blocks + 7) / 8 * 8 * a.kv_heads), (unsigned)((a.rows + 31) / 32)), 256, bytes, st>>>(a);
+    each_eight_blocks(a, a.kv_heads, 256, [&](unsigned blocks) { k_read<E, DP, CAP, BIAS><<<dim3(blocks, (unsigned)((a.rows + 31) / 32)), 256, bytes, st>>>(a); });
     LKG_HIP(hipGetLastError());
     return LOGOSKG_OK;
 }

@@ -280,3 +280,23 @@ def test_what_the_binding_refuses():
         lkg.read_packed(**{**a, "q": a["q"].float()})
     with pytest.raises(lkg.LogosKGError, match="multiple"):
         lkg.read_packed(**{**a, "q": a["q"][:, :, :3].contiguous()})
+
+
+@pytest.mark.parametrize("packed", [False, True], ids=["16 bits", "4 bits"])
+def test_more_lists_than_a_launch_takes(packed):
+    """2^26 lists and some of one entry, the last one of 5,000, in four heads: 2^32 threads and more of the reading and of the join."""
+    lists, entities = (1 << 26) + 40, 6001
+    values = (torch.arange(entities, device="cuda") % 50).to(torch.bfloat16)[:, None, None].expand(-1, 4, 8).contiguous()
+    keys = torch.zeros_like(values)
+    off = torch.arange(lists + 1, device="cuda")
+    off[-1] = lists - 1 + 5000
+    entity = (torch.arange(lists - 1 + 5000, device="cuda") % entities).int()
+    q = torch.ones(lists, 1, 4, 8, dtype=torch.bfloat16, device="cuda")
+    got = lkg.read_packed(q, lkg.pack_entities(keys, values), off, entity, kv_heads=4) if packed else lkg.read_entities(q, keys, values, off, entity)
+    out, lse = got["out"], got["lse"]
+    want = (entity[:lists - 1] % 50).to(torch.bfloat16)
+    for h in range(4):
+        for c in (0, 7):
+            assert bool((out[:-1, 0, h, c] == want).all())
+    assert bool((lse[:-1] == 0).all())
+    assert float((out[-1].float() - float((entity[-5000:] % 50).double().mean())).abs().max()) < 25 * 2 ** -7 and float((lse[-1] - math.log(5000)).abs().max()) < 1e-4
