@@ -62,9 +62,9 @@ constexpr int kMaskEntries = 1024;  // of a block
 
 // One atomic "or" per run of neighbouring lanes whose ids share a word (lists ascend, so that most runs are whole words):
 // the first lane of a run takes the bits of the others.
-__global__ __launch_bounds__(256) void k_mask_set(const int64_t *off, const int32_t *ids, long long n, int Q, long long num_ids, long long words, u64 *mask) {
+__global__ __launch_bounds__(256) void k_mask_set(const int64_t *off, const int32_t *ids, long long n, int Q, long long num_ids, long long words, u64 *mask, long long first) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long base = (long long)blockIdx.x * kMaskEntries + wave * 256;
+    const long long base = (first + blockIdx.x) * kMaskEntries + wave * 256;
     if (base >= n) return;
     // the list of the wavefront's first entry; later ones move on from it
     int lo = 0, hi = Q;  // off[lo] <= base < off[hi]
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(256) void k_mask_set(const int64_t *off, const int3
 // ---------------------------------------------------------------- logits
 struct LogitArgs {
     int num_rows;
-    long long vocab, row, words, num_history, num_bias, pieces;  // pieces of a row
+    long long vocab, row, words, num_history, num_bias, pieces, first;  // pieces of a row; row that a launch begins with
     const void *logits;
     void *out;
     const int64_t *history_off, *bias_off;
@@ -132,7 +132,7 @@ template <class T, int THREADS> __global__ __launch_bounds__(THREADS) void k_log
     } few;
     __shared__ int hits;
     const int tid = threadIdx.x;
-    const long long b = blockIdx.x / a.pieces;
+    const long long b = a.first + blockIdx.x / a.pieces;
     const T *in = (const T *)a.logits + b * a.row;
     T *out = (T *)a.out + b * a.row;
     // ids of the row before its first whole chunk; pieces begin there, the first one with what lies before
@@ -305,8 +305,10 @@ template <class T> static logoskg_status launch_logits(LogitArgs a, hipStream_t 
     // (3.6 TB/s; a copy of the logits and masks 33), with next to no lists 29; pieces of 2,048 take 49 and 29, of 8,192
     // 48 and 29, of 16,384 73 and 45 us.  (256 rows of 32,000 float32 logits with 8,000 ids each: 26, 28, 24, 22 us.)
     a.pieces = (a.vocab + 4096 + 15) / 4096;
-    if (a.pieces * a.num_rows >= (1ll << 31)) { set_error("logoskg_constrain_logits: too many rows"); return LOGOSKG_EINVAL; }
-    k_logits<T, 256><<<dim3((unsigned)(a.pieces * a.num_rows)), 256, 0, st>>>(a);
+    launch_ranges(a.num_rows, 1, [&](long long first, long long n) {
+        a.first = first;
+        k_logits<T, 256><<<dim3((unsigned)(a.pieces * n)), 256, 0, st>>>(a);
+    }, kMaxBlocks / a.pieces);
     LKG_HIP(hipGetLastError());
     return LOGOSKG_OK;
 }
@@ -331,7 +333,7 @@ extern "C" logoskg_status logoskg_entity_mask(int32_t device, const int64_t *off
     int piece_words = 16384;
     while (piece_words > 512 && (words + piece_words - 1) / piece_words * num_queries < 512) piece_words /= 2;
     const long long pieces = (words + piece_words - 1) / piece_words;
-    if (pieces <= kMostMaskPieces && num_entries / num_queries <= kMostMaskList && pieces * num_queries < (1ll << 31)) {
+    if (pieces <= kMostMaskPieces && num_entries / num_queries <= kMostMaskList && pieces * num_queries <= kMaxBlocks / 4) {  // (blocks of 1,024: fewer than 2^32 threads)
         LKG_TRY(allow_lds(k_mask_piece, (size_t)piece_words * 8));
         k_mask_piece<<<dim3((unsigned)(pieces * num_queries)), 1024, piece_words * 8, st>>>(off, ids, num_entries, num_ids, words, (int)pieces, piece_words, (u64 *)mask);
         LKG_HIP(hipGetLastError());
@@ -341,7 +343,9 @@ extern "C" logoskg_status logoskg_entity_mask(int32_t device, const int64_t *off
     k_mask_clear<<<dim3((unsigned)(blocks < 1 ? 1 : blocks > 8192 ? 8192 : blocks)), 256, 0, st>>>((ulonglong2 *)mask, all / 2, all & 1 ? (u64 *)mask + all - 1 : nullptr);
     LKG_HIP(hipGetLastError());
     if (num_entries) {
-        k_mask_set<<<dim3((unsigned)((num_entries + kMaskEntries - 1) / kMaskEntries)), 256, 0, st>>>(off, ids, num_entries, num_queries, num_ids, words, (u64 *)mask);
+        launch_ranges((num_entries + kMaskEntries - 1) / kMaskEntries, 1, [&](long long first, long long n) {
+            k_mask_set<<<dim3((unsigned)n), 256, 0, st>>>(off, ids, num_entries, num_queries, num_ids, words, (u64 *)mask, first);
+        });
         LKG_HIP(hipGetLastError());
     }
     return LOGOSKG_OK;

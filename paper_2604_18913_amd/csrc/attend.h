@@ -5,7 +5,7 @@
 
 namespace lkg {
 
-constexpr int kAttThreads = 256;  // four wavefronts
+constexpr int kAttThreads = 256;  // four wavefronts (and what kMaxBlocks counts)
 constexpr int kAttRowsShift = 7;  // a block's rows: 4 x 32
 constexpr int kAttRows = 1 << kAttRowsShift;
 constexpr int kFewShift = 5;       // rows of a block where there are few: 32

@@ -468,7 +468,7 @@ logoskg_status attend_args(const logoskg_attention *a, AttArgs *o, const char *c
     o->scale = a->score.scale;
     o->curve = o->score.c > 0 ? (float)(-(double)a->score.scale / ((double)o->score.c * o->score.c)) : 0.f;
     o->slope = 4.f * a->score.scale;
-    if (o->row_blocks * a->kv_heads >= (1ll << 31)) { set_error("%s: too many rows", call); return LOGOSKG_EINVAL; }
+    if (o->row_blocks * a->kv_heads > kMaxBlocks) { set_error("%s: too many rows", call); return LOGOSKG_EINVAL; }
     return LOGOSKG_OK;
 }
 

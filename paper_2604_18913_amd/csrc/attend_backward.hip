@@ -896,7 +896,7 @@ extern "C" logoskg_status logoskg_attend_backward(const logoskg_attention *in, c
     a.dout = g->dout; a.dq = g->dq; a.dk = g->dk; a.dv = g->dv; a.dbias = g->dbias;
     a.delta = (float *)g->workspace;
     a.bias_part = (float *)((char *)g->workspace + delta_bytes(a));
-    if (a.key_blocks * a.kv_heads >= (1ll << 31)) { set_error("logoskg_attend_backward: too many rows"); return LOGOSKG_EINVAL; }
+    if (a.key_blocks * a.kv_heads > kMaxBlocks) { set_error("logoskg_attend_backward: too many rows"); return LOGOSKG_EINVAL; }
     if (a.num_keys == 0) a.key_blocks = 0;
     if (ordered(a)) a.key_order = (int *)(a.bias_part + (a.score.bias ? a.key_blocks * a.heads * (int64_t)a.score.num_buckets : 0)), a.row_order = a.key_order + a.key_blocks;
     LKG_HIP(hipSetDevice(in->device));

@@ -328,3 +328,22 @@ def test_gradients_of_rows_with_few_keys(dim, heads, kv_heads, cap):
     got = _check({**a, "cap": cap}, dout)
     want = oracle.attention(**a, cap=cap, dout=dout)[0]["dq"]
     assert (got["dq"].cpu().double() - want).norm() < 0.0035 * want.norm()
+
+
+def test_more_rows_of_logits_than_a_launch_takes():
+    rows = (1 << 24) + 40  # a block of 256 threads each
+    logits = torch.arange(20, device="cuda").to(torch.bfloat16).expand(rows, 20).contiguous()
+    mask = torch.full((rows, 1), 0b1010, device="cuda")
+    mask[-1] = 0b1
+    got = lkg.constrain_logits(logits, mask=mask)
+    want = torch.full((20,), -float("inf"), device="cuda", dtype=torch.bfloat16)
+    want[[1, 3]] = logits[0, [1, 3]]
+    assert bool((got[:-1] == want).all()) and got[-1].tolist() == [0.0] + [-float("inf")] * 19
+
+
+def test_more_masks_than_a_launch_takes():
+    rows = (1 << 22) + 40  # a block of 1,024 threads each, if one launch took them
+    off = torch.arange(rows + 1, device="cuda")
+    ids = (torch.arange(rows, device="cuda") % 60).int()
+    got = lkg.entity_mask(off, ids, 60)
+    assert got.shape == (rows, 1) and bool((got[:, 0] == (torch.ones((), dtype=torch.int64, device="cuda") << ids.long())).all())

@@ -34,3 +34,14 @@ def test_a_bias_without_buckets_is_refused():
     with pytest.raises(ValueError, match="a bucket at least"):
         reading._score(None, 0.0, torch.zeros(2, 0), torch.zeros(9, dtype=torch.int32), 2, 64, torch.float32, -1)
     assert reading._score(None, 0.0, torch.zeros(2, 1), torch.zeros(9, dtype=torch.int32), 2, 64, torch.float32, -1)[4:] == (1, 4)
+
+
+def test_more_blocks_than_a_launch_takes_are_refused():
+    # (256 threads each: 2^24 of them would be 2^32 threads)
+    a = _attention(num_docs=1 << 20, num_rows=1 << 20, num_keys=1 << 20, heads=16, kv_heads=16, q_row=1024, k_row=1024, v_row=1024)
+    rc, text = _status("logoskg_attend", a)
+    assert rc == 1 and "too many rows" in text
+    a = _attention(num_docs=1 << 19, num_rows=1 << 19, num_keys=1 << 26, heads=16, kv_heads=16, q_row=1024, k_row=1024, v_row=1024)
+    grad = reading._AttentionGrad(struct_size=64, dout=64, dq=64, dk=64, dv=64, workspace=64, workspace_bytes=1 << 40)
+    rc, text = _status("logoskg_attend_backward", a, grad)
+    assert rc == 1 and "too many rows" in text
