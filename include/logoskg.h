@@ -715,7 +715,8 @@ typedef struct {
 } logoskg_policy;
 logoskg_status logoskg_token_logp(const logoskg_policy *p);      /* logp and lse alone */
 logoskg_status logoskg_policy_loss(const logoskg_policy *p);     /* loss, logp, lse and perhaps dlogits */
-logoskg_status logoskg_policy_loss_backward(const logoskg_policy *p); /* dlogits of lse */
+logoskg_status logoskg_policy_loss_backward(const logoskg_policy *p); /* dlogits of lse; rows whose lse is 44 or more from 0 are
+                                                                         read for their sum again, whose bits lse does not hold */
 
 /*
  * The norm of all gradients of a step together, and the gradients brought to it:

@@ -170,7 +170,15 @@ template <class T, int THREADS, int MODE, bool MASKED, int KEEP, bool WHOLE> __d
     asm volatile("" : "+v"(said_x));
     Sum s = {-INFINITY, 0.f};
     float lse, logp, slope;
-    if (MODE != kBackward) {
+    // Where lse is far from 0, its rounding would be that of shares and of logp (2^-24 of 1,000: 6e-5 of a share): these are made of the
+    // largest and the sum, and the backward, which is given lse alone, makes those again.  (Such rows of 150,001 bfloat16 logits, 2,048 of
+    // them: 320 us, others 248; under masks 243 and 208; 8,192 of 32,000 255 and 205.)
+    bool far = false;
+    if (MODE == kBackward) {
+        lse = a.lse[r];
+        far = said_x != -INFINITY && !(__builtin_fabsf(lse * kLog2e) < kNear);
+    }
+    if (MODE != kBackward || far) {
         auto take = [&](float x) { s.join(x, x == -INFINITY ? 0.f : 1.f, k); };
         if ((unsigned)tid < lead && allowed(tid)) take((float)in[tid]);
         if (tail + tid < vocab && allowed(tail + tid)) take((float)in[tail + tid]);
@@ -195,7 +203,7 @@ template <class T, int THREADS, int MODE, bool MASKED, int KEEP, bool WHOLE> __d
             }
             s.top = top, s.sum = sum;
         };
-        if (WHOLE) {  // the largest of all first; what is hidden becomes -infinity in place, for the second sweep too
+        if (WHOLE && MODE != kBackward) {  // the largest of all first; what is hidden becomes -infinity in place, for the second sweep too
             float top = s.top;
 #pragma unroll
             for (int i = 0; i < KEEP; i++) {
@@ -222,7 +230,7 @@ template <class T, int THREADS, int MODE, bool MASKED, int KEEP, bool WHOLE> __d
                 }
             }
             s.top = top, s.sum = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        } else {
+        } else if (MODE != kBackward) {
 #pragma unroll
             for (int i = 0; i < KEEP; i++)
                 if (tid + i * THREADS < chunks) {
@@ -230,13 +238,14 @@ template <class T, int THREADS, int MODE, bool MASKED, int KEEP, bool WHOLE> __d
                     take_chunks(std::integral_constant<int, 1>{}, &kept[i], &bits);
                 }
         }
-        unsigned c = tid + KEEP * THREADS;
-        for (; !WHOLE && c + THREADS < chunks; c += 2 * THREADS) {
+        constexpr bool kRest = !WHOLE || MODE == kBackward;
+        unsigned c = tid + (MODE == kBackward ? 0 : KEEP * THREADS);
+        for (; kRest && c + THREADS < chunks; c += 2 * THREADS) {
             const Some<T> x[2] = {chunk_at(c), chunk_at(c + THREADS)};
             const unsigned bits[2] = {bits_at(c), bits_at(c + THREADS)};
             take_chunks(std::integral_constant<int, 2>{}, x, bits);
         }
-        if (!WHOLE && c < chunks) {
+        if (kRest && c < chunks) {
             const Some<T> x = chunk_at(c);
             const unsigned bits = bits_at(c);
             take_chunks(std::integral_constant<int, 1>{}, &x, &bits);
@@ -255,17 +264,17 @@ template <class T, int THREADS, int MODE, bool MASKED, int KEEP, bool WHOLE> __d
         const float total = logf(s.sum);
         lse = s.top * a.scale + total;
         if (s.sum == 0.f) lse = -INFINITY;
+        if (MODE != kBackward) far = !(__builtin_fabsf(lse * kLog2e) < kNear);
         if (tid == 0) {
             logp = 0.f;
             if ((unsigned)target < vocab) logp = said_x == -INFINITY ? -INFINITY : (said_x - s.top) * a.scale - total;
-            a.logp[r] = logp;
-            a.lse[r] = lse;
+            if (MODE != kBackward) {
+                a.logp[r] = logp;
+                a.lse[r] = lse;
+            }
         }
-    } else {
-        lse = a.lse[r];
-        if (tid == 0) {
-            logp = said_x == -INFINITY ? -INFINITY : __builtin_fmaf(said_x, a.scale, -lse);
-        }
+    } else if (tid == 0) {
+        logp = said_x == -INFINITY ? -INFINITY : __builtin_fmaf(said_x, a.scale, -lse);
     }
     if (MODE == kLogp) return;
     if (tid == 0) {
@@ -289,7 +298,7 @@ template <class T, int THREADS, int MODE, bool MASKED, int KEEP, bool WHOLE> __d
         return;
     }
     constexpr int kKept = MODE == kBackward ? 0 : KEEP;
-    auto write_row = [&](auto far) __attribute__((always_inline)) {  // (where lse is far from 0, its rounding would be that of the shares)
+    auto write_row = [&](auto far) __attribute__((always_inline)) {
         const float from = far ? -__log2f(s.sum) : -lse * kLog2e;
         auto share = [&](float x) { return exp2_fast(__builtin_fmaf(far ? x - s.top : x, k, from)) * -slope; };
         constexpr bool kHide = MASKED && !(WHOLE && kKept > 0);  // (else it is hidden already)
@@ -315,8 +324,8 @@ template <class T, int THREADS, int MODE, bool MASKED, int KEEP, bool WHOLE> __d
         }
         if ((!WHOLE || kKept == 0) && c < chunks) write_chunk(c, chunk_at(c));
     };
-    if (MODE == kBackward || __builtin_fabsf(lse * kLog2e) < kNear) write_row(std::false_type{});
-    else write_row(std::true_type{});
+    if (far) write_row(std::true_type{});
+    else write_row(std::false_type{});
     auto written = [&] {  // before others write over it
         if (THREADS <= 64) __threadfence_block();
         all_here();

@@ -235,7 +235,8 @@ def policy_loss(logits, target, advantage, *, old=None, ref=None, weight=None, c
 def policy_loss_backward(dloss, logits, target, advantage, lse, *, old=None, ref=None, weight=None, clip=(0.2, 0.2), kl=0.0, scale=1.0,
                          mask=None, mask_row=None):
     """``logoskg_policy_loss_backward``: the gradient of ``logits`` for ``dloss`` (float32 scalar on the device), that of
-    ``policy_loss``'s "loss"; the other arguments are that call's, and its "lse"."""
+    ``policy_loss``'s "loss"; the other arguments are that call's, and its "lse".  Rows whose lse is 44 or more from 0 are read once more
+    than others: what 32 bits of it do not hold is made again."""
     torch = _torch()
     head, device, rows = _answers(logits, target, mask, mask_row)
     terms = _terms(advantage, old, ref, weight, clip, kl, scale, rows, device)

@@ -341,3 +341,51 @@ def test_more_rows_than_a_launch_takes(rows, vocab, masked):
         assert torch.equal(got["logp"], logp) and abs(float(got["loss"]) / -rows - 1) < 1e-6
         one = got["dlogits"].abs().amax(1)  # of the target: 1 - its share
         assert float((one[:-1].float() - 5 / 6).abs().max()) < 0.01 and abs(float(one[-1]) - (1 - share)) < 0.01
+
+
+@pytest.mark.parametrize("dtype, size", [(torch.float32, 1e4), (torch.float32, -1e5), (torch.float16, 3000.0), (torch.bfloat16, -400.0), (torch.float32, 65.0)])
+@pytest.mark.parametrize("masks", [None, 3], ids=["open", "masked"])
+@pytest.mark.parametrize("rows, vocab", [(100, 300)] + [(6, v) for v in KERNELS])
+def test_rows_far_from_nothing(rows, vocab, masks, dtype, size):
+    """Rows whose logits stand far from 0 keep the bits of those near it, in one pass and from lse.
+
+    With b what an id is below its row's largest, in units of the exponent: its term is off by 2^-24 (4 b + 2), the sum by those and by up to
+    250 additions and scalings in turn (1,024 threads with 195 terms each, 256 with 128, in steps of 16), its logarithm by four of its own last places, and
+    logp by the four more of what it is."""
+    a = _case(32, rows, vocab, dtype, scale=0.5)
+    a["logits"] = (a["logits"].float() * 1.5 + size / 0.5).to(dtype)
+    few = dict(scale=0.5)
+    if masks:
+        a |= {k: x for k, x in _case(32, rows, vocab, dtype, masks=masks).items() if k in ("mask", "mask_row")}
+        few |= {k: a[k] for k in ("mask", "mask_row")}
+    lp = oracle.policy(a["logits"], a["target"], **few)[0]["logp"]
+    lp = torch.where(lp.isfinite(), lp, 0.0)
+    g = torch.Generator().manual_seed(33)
+    a["old"] = (lp - torch.randint(-8, 9, (rows,), generator=g) * 0.05 + 0.011).float()
+    a["ref"] = (lp + torch.randn(rows, generator=g) * 0.3).float()
+    res, _ = oracle.policy(**a)
+    x = a["logits"].double() * 0.5
+    if masks:
+        bits = ((a["mask"][:, :, None] >> torch.arange(64)) & 1).reshape(masks, -1)[:, :vocab].bool()
+        x = torch.where(bits[a["mask_row"].long()], x, -math.inf)
+    top = x.amax(1, keepdim=True)
+    b = torch.where(x == -math.inf, 0.0, top - x)
+    p, logsum = torch.softmax(x, 1), torch.logsumexp(x - top, 1, keepdim=True)
+    rest = oracle.E32 * (250 + 4 * (p * b).sum(1, keepdim=True) + 4 * logsum)
+    said = b.gather(1, a["target"].long()[:, None])
+    counts = res["logp"].isfinite()[:, None]
+    lp, old, ref, A, w = (t.double()[:, None] for t in (lp, a["old"], a["ref"], a["advantage"], a["weight"]))
+    lp_tol = rest + oracle.E32 * (4 * said + 4 * lp.abs())
+    near = lp_tol + 4 * oracle.E32 * (1 + lp.abs() + old.abs() + ref.abs())
+    steep = torch.exp(lp - old) * A.abs() + a["kl"] * torch.exp(ref - lp)
+    slope_tol = 0.5 * w * steep * (1.1 * near + 8 * oracle.E32)
+    hot = torch.zeros_like(p).scatter_(1, a["target"].long()[:, None], 1.0)
+    slope = 0.5 * w * steep  # at most
+    tol = slope_tol * (hot - p).abs() + 1.1 * slope * (p * (rest + 4 * oracle.E32 * (b + 1)) + hot * lp_tol * torch.exp(lp) + 4 * oracle.E32 * (hot - p).abs())
+    tol = torch.where(counts, tol + oracle.UNIT[dtype] * (res["dlogits"].abs() + tol) + oracle.LEAST[dtype], 0.0)
+    c = _gpu(a)
+    got = lkg.policy_loss(**c, gradient=True)
+    oracle.check(got["dlogits"], res["dlogits"], tol, "one pass")
+    oracle.check(got["logp"], res["logp"], torch.where(counts, lp_tol, 0.0).squeeze(1), "logp")
+    rest = {k: t for k, t in c.items() if k not in ("logits", "target", "advantage")}
+    oracle.check(lkg.policy_loss_backward(torch.tensor(1.0, device="cuda"), c["logits"], c["target"], c["advantage"], got["lse"], **rest), res["dlogits"], tol, "backward")
