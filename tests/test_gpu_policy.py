@@ -389,3 +389,27 @@ def test_rows_far_from_nothing(rows, vocab, masks, dtype, size):
     oracle.check(got["logp"], res["logp"], torch.where(counts, lp_tol, 0.0).squeeze(1), "logp")
     rest = {k: t for k, t in c.items() if k not in ("logits", "target", "advantage")}
     oracle.check(lkg.policy_loss_backward(torch.tensor(1.0, device="cuda"), c["logits"], c["target"], c["advantage"], got["lse"], **rest), res["dlogits"], tol, "backward")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=TYPE_NAMES)
+@pytest.mark.parametrize("masks", [None, 3], ids=["open", "masked"])
+@pytest.mark.parametrize("rows, vocab", [(9, 7), (100, 299), (100, 304)] + [(9, v) for v in KERNELS])
+def test_gradients_in_place_of_the_logits(rows, vocab, masks, dtype):
+    a = _case(34, rows, vocab, dtype, masks=masks)
+    a["target"][[2, 5]] = torch.tensor([-1, vocab], dtype=torch.int32)
+    a["logits"][3] += 200  # (its sum is made again by the backward)
+    b = _gpu(a)
+    want = lkg.policy_loss(**b, gradient=True)
+    x = b["logits"].clone()
+    loss, logp, lse = _raw("logoskg_policy_loss", b, x, logits=x)
+    assert torch.equal(x, want["dlogits"]) and torch.equal(loss, want["loss"]) and torch.equal(logp, want["logp"]) and torch.equal(lse, want["lse"])
+    rest = {k: t for k, t in b.items() if k not in ("logits", "target", "advantage")}
+    dloss = torch.tensor(-1.5, device="cuda")
+    back = lkg.policy_loss_backward(dloss, b["logits"], b["target"], b["advantage"], lse, **rest)
+    x = b["logits"].clone()
+    _raw("logoskg_policy_loss_backward", b, x, lse, dloss, logits=x)
+    assert torch.equal(x, back)
+    one = {k: t[3:4].clone() if k not in ("mask", "kl", "scale") else t for k, t in b.items()}  # of one row, whose stride does not matter
+    x = one["logits"].clone()
+    _raw("logoskg_policy_loss", one, x, logits=x)
+    assert torch.equal(x, lkg.policy_loss(**one, gradient=True)["dlogits"])
