@@ -80,6 +80,13 @@ def _on_stream(call):
     return on
 
 
+def _has_tangent(*tensors) -> bool:
+    """Whether differentiation in forward mode sends a tangent along with one of them.  Calls with a gradient go by their
+    autograd function then, which torch refuses: past it the tangent would be lost."""
+    forward = _torch().autograd.forward_ad
+    return forward._current_level >= 0 and any(t is not None and forward.unpack_dual(t).tangent is not None for t in tensors)  # (-1: no such mode)
+
+
 def _on_gpu(t, name) -> int:
     """The number of the tensor's GPU."""
     device = t.get_device()
@@ -220,7 +227,8 @@ def attend(q, k, v, q_off, k_off, *, scale=None, cap=0.0, causal=False, prefix=N
 
     Where ``q``, ``k``, ``v`` or ``bias`` requires a gradient, ``out`` has one by ``attend_backward``; ``lse`` has none, and
     asking for it raises."""
-    if (q.requires_grad or k.requires_grad or v.requires_grad or bias is not None and bias.requires_grad) and _torch().is_grad_enabled():
+    if ((q.requires_grad or k.requires_grad or v.requires_grad or bias is not None and bias.requires_grad) and _torch().is_grad_enabled()
+            or _has_tangent(q, k, v, bias)):
         kw = dict(scale=scale, cap=cap, causal=causal, prefix=prefix, buckets=buckets, q_pos=q_pos, k_pos=k_pos)
         return _differentiable().apply(q, k, v, bias, q_off, k_off, kw)
     out, lse = _new(q), q.new_empty(q.shape[:2], dtype=_torch().float32)

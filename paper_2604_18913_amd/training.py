@@ -10,7 +10,7 @@ import struct
 
 from .binding import _check, _load, _stream_handle, _torch
 from .packed import _apart, _last_of
-from .reading import _dtype, _F, _I32, _I64, _on_gpu, _on_stream, _P, _packer, _plain, _workspace
+from .reading import _dtype, _F, _has_tangent, _I32, _I64, _on_gpu, _on_stream, _P, _packer, _plain, _workspace
 
 _U32 = ctypes.c_uint32
 
@@ -79,7 +79,7 @@ def embed_entities(table, ids, *, scale=1.0):
     as ``Result.fetch`` gives them) times ``scale``, as [*ids.shape, dim] in the table's type.  Ids outside the table pad: their rows are
     zeros.  Where ``table`` requires a gradient, the result has one by ``embed_entities_backward``."""
     torch = _torch()
-    if table.requires_grad and torch.is_grad_enabled():
+    if table.requires_grad and torch.is_grad_enabled() or _has_tangent(table):
         return _differentiable_embedding().apply(table, ids, scale)
     device = _on_gpu(table, "table")
     entities, dim, row = _table(table, "table")
@@ -165,6 +165,13 @@ def token_logp(logits, target, *, scale=1.0, mask=None, mask_row=None):
     return {"logp": logp, "lse": lse}
 
 
+def _no_gradient(**tensors):
+    """Refuses tensors whose gradient would be lost: what stands beside the rows is taken as it is."""
+    for name, t in tensors.items():
+        if t is not None and (t.requires_grad or _has_tangent(t)):
+            raise ValueError(f"{name} requires a gradient, and policy_loss has none for it: detach it")
+
+
 def _terms(advantage, old, ref, weight, clip, kl, scale, rows, device):
     """The values of a _Policy from scale to weight."""
     if kl and ref is None:
@@ -211,13 +218,15 @@ def policy_loss(logits, target, advantage, *, old=None, ref=None, weight=None, c
     Row by row, with ``token_logp``'s logp (which has the other arguments) and r = exp(logp - ``old``): the loss is ``weight`` times
     -min(r A, clamp(r, 1 - clip[0], 1 + clip[1]) A) + ``kl`` (exp(ref - logp) - (ref - logp) - 1), A = ``advantage``, summed over the rows.
     All of them are float32 per row; without ``old`` r is 1 (the samples are this policy's), without ``weight`` it is 1.  Rows whose target
-    pads or is hidden do not count.
+    pads or is hidden, or whose weight is 0, do not count.  They are taken as they are: one that requires a gradient is refused (detach it).
 
     With ``gradient`` the same pass also returns "dlogits", the gradient of the loss with respect to ``logits`` in their type: for
     ``logits.backward(dlogits)``.  Without it, where ``logits`` requires a gradient, "loss" has one by ``policy_loss_backward``
     ("logp" and "lse" have none)."""
     torch = _torch()
-    if not gradient and logits.requires_grad and torch.is_grad_enabled():
+    if torch.is_grad_enabled() and not gradient:
+        _no_gradient(advantage=advantage, old=old, ref=ref, weight=weight)
+    if not gradient and (logits.requires_grad and torch.is_grad_enabled() or _has_tangent(logits)):
         tensors = {n: t for n, t in dict(old=old, ref=ref, weight=weight, mask=mask, mask_row=mask_row).items() if t is not None}
         loss, logp, lse = _differentiable_policy().apply(logits, target, advantage, tensors, dict(clip=clip, kl=kl, scale=scale))
         return {"loss": loss, "logp": logp, "lse": lse}

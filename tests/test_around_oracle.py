@@ -261,3 +261,23 @@ def test_read_packed_refusals(wrong, rc, says):
     got, text = _status("logoskg_read_packed", e)
     assert got == rc and says in text, text
     assert (reading._load().logoskg_read_packed_bytes(ctypes.addressof(e)) == -1) == (rc == 1)
+
+
+@pytest.mark.parametrize("name", ["advantage", "old", "ref", "weight"])
+def test_gradients_that_the_policy_loss_does_not_have_are_refused(name):
+    x = torch.zeros(2, 8)
+    kw = dict(advantage=torch.zeros(2), old=torch.zeros(2), ref=torch.zeros(2), weight=torch.zeros(2))
+    kw[name].requires_grad_()
+    call = lambda **more: lkg.policy_loss(x, torch.zeros(2, dtype=torch.int32), kl=0.1, **kw, **more)
+    with pytest.raises(ValueError, match=f"{name} requires a gradient"):
+        call()
+    for more in (torch.no_grad, torch.inference_mode):  # (nothing is asked for: refused for another reason)
+        with more(), pytest.raises(ValueError, match="on the GPU"):
+            call()
+    with pytest.raises(ValueError, match="on the GPU"):
+        call(gradient=True)
+    kw[name] = torch.zeros(2)
+    with torch.autograd.forward_ad.dual_level():
+        kw[name] = torch.autograd.forward_ad.make_dual(kw[name], torch.ones(2))
+        with pytest.raises(ValueError, match=f"{name} requires a gradient"):
+            call()

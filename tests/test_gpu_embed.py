@@ -261,3 +261,11 @@ def test_more_ids_than_a_launch_takes():
     got = lkg.embed_entities(table, ids)
     assert got.shape == (n, 1) and got[0] == 2 and got[-1] == 0
     assert bool((got[1:-2500] == 1).all()) and bool((got[-2500:-1] == 3).all())
+
+
+def test_tangents_are_not_lost():
+    table, ids = torch.ones(5, 8, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    with torch.autograd.forward_ad.dual_level():
+        assert lkg.embed_entities(table, ids).shape == (3, 8)
+        with pytest.raises(NotImplementedError, match="jvp"):
+            lkg.embed_entities(torch.autograd.forward_ad.make_dual(table, torch.ones_like(table)), ids)

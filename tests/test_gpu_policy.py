@@ -413,3 +413,11 @@ def test_gradients_in_place_of_the_logits(rows, vocab, masks, dtype):
     x = one["logits"].clone()
     _raw("logoskg_policy_loss", one, x, logits=x)
     assert torch.equal(x, lkg.policy_loss(**one, gradient=True)["dlogits"])
+
+
+def test_tangents_are_not_lost():
+    a = _gpu(_case(35, 4, 30))
+    with torch.autograd.forward_ad.dual_level():
+        a["logits"] = torch.autograd.forward_ad.make_dual(a["logits"], torch.ones_like(a["logits"]))
+        with pytest.raises(NotImplementedError, match="jvp"):
+            lkg.policy_loss(**a)

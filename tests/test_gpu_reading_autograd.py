@@ -67,3 +67,14 @@ def test_the_gradient_of_lse_is_refused():
     out, lse = lkg.attend(**b)
     out.float().sum().backward()
     assert b["k"].grad is not None
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v", "bias"])
+def test_tangents_are_not_lost(name):
+    a, _ = _case(65)
+    b = {k: _gpu(x) for k, x in a.items()}
+    with torch.autograd.forward_ad.dual_level():
+        assert lkg.attend(**b)[0].shape == b["q"].shape
+        b[name] = torch.autograd.forward_ad.make_dual(b[name], torch.ones_like(b[name]))
+        with pytest.raises(NotImplementedError, match="jvp"):
+            lkg.attend(**b)
