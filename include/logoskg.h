@@ -724,7 +724,8 @@ logoskg_status logoskg_policy_loss_backward(const logoskg_policy *p); /* dlogits
  * summed in 64 bits, so that no size overflows, in a fixed order.  `out` may be
  * `grad` (of the same type); otherwise no two arrays that are written, or one
  * written and one read, may share memory.  A norm that is infinite gives zeros (NaN where the gradient is
- * infinite), one that is NaN gives NaN; *norm tells.
+ * infinite), one that is NaN gives NaN; *norm tells.  (One of finite gradients that is above what 32 bits hold is told as
+ * infinite too; these are brought to max_norm as others.)
  */
 typedef struct {
     const void *grad;         /* device                                                      */

@@ -86,7 +86,10 @@ __global__ __launch_bounds__(256) void k_clip_norm(double *sums, int n, float ma
     if (threadIdx.x == 0) *norm = (float)got, sums[0] = by;
 }
 
-template <class T, class O> __device__ __forceinline__ void scaled(const T *g, O *out, long long n, float by, int tid) {
+// The factor in 32 bits: `by` alone, or where it is below the normal numbers, which would leave it few bits, 2^-100 and 2^100 times it in turn.
+// (Gradients below 2^-26 lose bits by 2^-100; their product is below 2^-152 and 0.)
+struct Factor { float first, by; };
+template <class T, class O> __device__ __forceinline__ void scaled(const T *g, O *out, long long n, Factor f, int tid) {
     constexpr int V = 16 / (sizeof(T) > sizeof(O) ? sizeof(T) : sizeof(O));  // elements at a time: 16 bytes of the wider type
     typedef T from __attribute__((ext_vector_type(V), aligned(sizeof(T))));
     typedef O to __attribute__((ext_vector_type(V), aligned(sizeof(O))));
@@ -95,19 +98,19 @@ template <class T, class O> __device__ __forceinline__ void scaled(const T *g, O
             const from x = *(const from *)(g + i);
             to y;
 #pragma unroll
-            for (int e = 0; e < V; e++) y[e] = (O)((float)x[e] * by);
+            for (int e = 0; e < V; e++) y[e] = (O)((float)x[e] * f.first * f.by);
             *(to *)(out + i) = y;
         } else {
-            for (int e = 0; e < n - i; e++) out[i + e] = (O)((float)g[i + e] * by);
+            for (int e = 0; e < n - i; e++) out[i + e] = (O)((float)g[i + e] * f.first * f.by);
         }
     }
 }
 
-template <class T> __device__ __forceinline__ void scaled_to(const ClipArgs &a, int t, long long from, long long n, float by) {
+template <class T> __device__ __forceinline__ void scaled_to(const ClipArgs &a, int t, long long from, long long n, Factor f) {
     const T *g = (const T *)a.grad[t] + from;
-    if (a.out_type[t] == LOGOSKG_F32) scaled(g, (float *)a.out[t] + from, n, by, threadIdx.x);
-    else if (a.out_type[t] == LOGOSKG_BF16) scaled(g, (bf16 *)a.out[t] + from, n, by, threadIdx.x);
-    else scaled(g, (fp16 *)a.out[t] + from, n, by, threadIdx.x);
+    if (a.out_type[t] == LOGOSKG_F32) scaled(g, (float *)a.out[t] + from, n, f, threadIdx.x);
+    else if (a.out_type[t] == LOGOSKG_BF16) scaled(g, (bf16 *)a.out[t] + from, n, f, threadIdx.x);
+    else scaled(g, (fp16 *)a.out[t] + from, n, f, threadIdx.x);
 }
 
 // (n: the number of sums that every block adds up itself, or 0: the factor is made)
@@ -115,14 +118,15 @@ __global__ __launch_bounds__(256) void k_clip_scale(ClipArgs a, int n, float max
     __shared__ double box[4];
     double got, factor = n ? factor_of(a.sums, n, max_norm, scale, box, got) : a.sums[0];
     if (n && blockIdx.x == 0 && a.first == 0 && threadIdx.x == 0) *norm = (float)got;
-    const float by = (float)factor;
+    const bool small = fabs(factor) < 0x1p-126 && factor != 0.0;
+    const Factor f = {small ? 0x1p-100f : 1.f, (float)(small ? factor * 0x1p100 : factor)};
     for (long long c = blockIdx.x; c < a.chunks; c += gridDim.x) {
         const int t = tensor_of(a, c);
-        if (by == 1.f && a.grad[t] == a.out[t] && a.type[t] == a.out_type[t]) continue;  // (they are what they become)
+        if (f.first * f.by == 1.f && a.grad[t] == a.out[t] && a.type[t] == a.out_type[t]) continue;  // (they are what they become)
         const long long from = (c - a.begin[t]) * kClipChunk, n = a.n[t] - from < kClipChunk ? a.n[t] - from : kClipChunk;
-        if (a.type[t] == LOGOSKG_F32) scaled_to<float>(a, t, from, n, by);
-        else if (a.type[t] == LOGOSKG_BF16) scaled_to<bf16>(a, t, from, n, by);
-        else scaled_to<fp16>(a, t, from, n, by);
+        if (a.type[t] == LOGOSKG_F32) scaled_to<float>(a, t, from, n, f);
+        else if (a.type[t] == LOGOSKG_BF16) scaled_to<bf16>(a, t, from, n, f);
+        else scaled_to<fp16>(a, t, from, n, f);
     }
 }
 

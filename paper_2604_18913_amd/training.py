@@ -272,7 +272,7 @@ def clip_gradients(grads, max_norm, *, scale=1.0, out=None):
 
     In place, or into ``out``, one tensor per gradient in any of the three types (float32 for an optimizer that keeps 32 bits, say).  Sums are
     64-bit, and the same inputs give the same bits.  A norm that is not finite shows in the result: infinite, it makes zeros of the finite
-    gradients; NaN, NaN of all.  Tensors may not share memory."""
+    gradients (where all are finite and their norm is above float32's range, it shows as infinite, and they are scaled as others); NaN, NaN of all.  Tensors may not share memory."""
     torch = _torch()
     grads = list(grads)
     out = grads if out is None else list(out)

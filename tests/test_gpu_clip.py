@@ -145,3 +145,18 @@ def test_tensors_beyond_32_bits():
     g[0], g[1 << 31], g[n - 1] = 3.0, 4.0, 12.0
     assert abs(float(lkg.clip_gradients([g], 1.0)) - 13) < 1e-5
     assert torch.allclose(g[[0, 1 << 31, n - 1]].float().cpu(), torch.tensor([3.0, 4.0, 12.0]) / 13, rtol=2 ** -8)
+
+
+@pytest.mark.parametrize("to", TYPES, ids=TYPE_NAMES)
+@pytest.mark.parametrize("size, max_norm, scale", [(3e38, 1.0, 1.0), (3e38, 1e-3, 1.0), (3e38, 1e-3, -0.5), (1e38, 1e-6, 1.0), (2e37, math.inf, 1e-41), (3e38, 1e30, 1.0)])
+def test_norms_above_32_bits_and_factors_below_them(size, max_norm, scale, to):
+    g = torch.Generator().manual_seed(40)
+    grads = [(torch.rand(1003, generator=g) * 0.5 + 0.5) * size, torch.tensor([size, -size, 1e-30, 0.0, 1.0]), torch.full((9,), 1e38 if size > 1e38 else 1e36).to(torch.bfloat16)]
+    want, _, each = oracle.clip(grads, max_norm, float(torch.tensor(scale)), [to] * 3)  # (the call's numbers are float32: of 1e-41 that is 13 bits)
+    on = [x.cuda() for x in grads]
+    out = [torch.empty_like(x, dtype=to) for x in on]
+    norm = float(lkg.clip_gradients(on, max_norm, scale=scale, out=out))
+    assert norm == math.inf if want > torch.finfo(torch.float32).max else abs(norm / float(want) - 1) < 1e-6
+    for x, (y, t) in zip(out, each):
+        over = y.abs() > torch.finfo(to).max * (1 + torch.finfo(to).eps / 4)
+        oracle.check(x, torch.where(over, y.sign() * math.inf, y), t, "gradient")
