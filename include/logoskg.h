@@ -752,7 +752,9 @@ logoskg_status logoskg_clip_gradients(int32_t device, const logoskg_gradient *li
  *
  * base is the group's smallest element and scale a fifteenth of its range, rounded to bfloat16;
  * code = (element - base) / scale, rounded to the nearest even, in 0 .. 15 (0 where scale is 0).  A group with an
- * infinity or NaN, or a range above 32 bits, becomes NaN (7fc0, codes 0).
+ * infinity or NaN, or a range above 32 bits, becomes NaN (7fc0, codes 0).  So an element comes back off by up to half
+ * a step, or by 2^-8 of the group's range and smallest element's size together where that is more: a group that stands far
+ * from 0 against its range loses accuracy by its base.
  */
 int64_t logoskg_packed_row_bytes(int32_t kv_heads, int32_t dim);  /* 0 for sizes that are refused */
 

@@ -40,7 +40,8 @@ __device__ __forceinline__ Codes codes_of(const float (&x)[8], bool in) {
         for (int e = 0; e < 8; e++) lo = fminf(lo, x[e]), hi = fmaxf(hi, x[e]), odd = __builtin_fmaf(x[e], 0.f, odd);
     }
     lo = quad_min(lo), hi = quad_max(hi), odd = quad_sum(odd);
-    // both rounded to the nearest bfloat16: 2^-9 of the base and of the range, a 30th of a step's half
+    // both rounded to the nearest bfloat16, off by up to 2^-8 of themselves: of the scale, over 15 steps, that is a ninth of half a step; of the
+    // base it is as much of the group's offset, which is more than a step where that is 17 times the range
     const bf16 scale = (bf16)((hi - lo) / 15.f), base = (bf16)lo;
     const float s = (float)scale, b = (float)base;
     Codes got = {0, (unsigned)__builtin_bit_cast(unsigned short, scale) | (unsigned)__builtin_bit_cast(unsigned short, base) << 16};

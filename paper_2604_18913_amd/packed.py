@@ -56,8 +56,8 @@ def pack_entities(keys, values, *, out=None):
     uint8 [entities, packed_row_bytes(kv_heads, dim)] for ``read_packed``.  ``out`` may be rows of a larger table:
     ``pack_entities(k, v, out=table[a:b])``; single rows are replaced as any tensor's, ``table[ids] = pack_entities(k, v)``.
 
-    Groups of 32 elements of a head have a scale and a base in bfloat16, a fifteenth of the group's range being a step; the layout stands in
-    ``include/logoskg.h``.  A group with an infinity or NaN becomes NaN.  There is no gradient."""
+    Groups of 32 elements of a head have a scale and a base in bfloat16, a fifteenth of the group's range being a step; the layout and
+    what it loses stand in ``include/logoskg.h`` (a group that stands far from 0 against its range loses most).  A group with an infinity or NaN becomes NaN.  There is no gradient."""
     torch = _torch()
     dtype, device = keys.dtype, _on_gpu(keys, "keys")
     n, heads, dim, k_row, k_head = _rows(keys, "keys", dtype, device)

@@ -300,3 +300,21 @@ def test_more_lists_than_a_launch_takes(packed):
             assert bool((out[:-1, 0, h, c] == want).all())
     assert bool((lse[:-1] == 0).all())
     assert float((out[-1].float() - float((entity[-5000:] % 50).double().mean())).abs().max()) < 25 * 2 ** -7 and float((lse[-1] - math.log(5000)).abs().max()) < 1e-4
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, *HALVES], ids=["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("offset, spread", [(0.0, 1.0), (1000.0, 1.0), (-1000.0, 1.0), (1000.0, 1e-3), (257.0, 30.0), (-3.0, 0.1), (5e4, 100.0)])
+def test_groups_that_stand_far_from_nothing(offset, spread, dtype):
+    """With lo and R a group's smallest element and range, u = 2^-8: its base is off by u |lo|, its step s by u of itself, so the
+    last code's place by u (|lo| + R).  An element between the first and the last code is off by s / 2, one outside by what
+    those places are; the value, a product and sum in 32 bits and a rounding to float32, by 2^-23 of its size."""
+    g = torch.Generator().manual_seed(50)
+    k, v = ((offset + torch.rand(200, 3, 64, generator=g) * spread).to(dtype) for _ in range(2))
+    rows = lkg.pack_entities(k.cuda(), v.cuda())
+    _check_rows(rows, k, v)
+    for x, y in zip((k, v), lkg.unpack_entities(rows, 3, 64, dtype=torch.float32)):
+        x, y = (t.cpu().double().view(200, 3, 2, 32) for t in (x, y))
+        lo, hi = x.amin(3, keepdim=True), x.amax(3, keepdim=True)
+        step = (hi - lo) / 15 * (1 + 2 ** -8)
+        bound = torch.maximum(step / 2, 2.0 ** -8 * (lo.abs() + hi - lo)) * (1 + 2 ** -20) + 2.0 ** -23 * (x.abs() + y.abs())
+        assert bool(((x - y).abs() <= bound).all())
