@@ -699,7 +699,7 @@ typedef struct {
     const int32_t *mask_row;  /* device int32[num_rows]: row i's mask (one outside [0, num_masks) allows nothing);
                                  NULL: mask i, num_masks >= num_rows                         */
     int64_t num_masks;
-    float scale;              /* 1 / temperature: above 0                                    */
+    float scale;              /* 1 / temperature: above 0, at most 2e38                      */
     float kl;                 /* not negative; 0: ref is not read and may be NULL            */
     float clip_low, clip_high; /* not negative                                               */
     const float *advantage;   /* device float[num_rows]                                      */

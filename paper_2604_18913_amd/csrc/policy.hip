@@ -459,6 +459,7 @@ static const char *policy_args(const logoskg_policy *p, int mode, PolicyArgs *a)
     if (mode != kBackward && p->num_rows && !p->logp) return "logp is NULL";
     if (p->mask && !p->mask_row && p->num_masks < p->num_rows) return "fewer masks than rows";
     if (!(p->scale > 0.f) || p->scale - p->scale != 0.f) return "scale is not above 0";
+    if (p->scale > 2e38f) return "scale is above 2e38";  // (times log2 e it is finite)
     if (mode != kLogp) {
         if (!(p->kl >= 0.f) || p->kl - p->kl != 0.f) return "kl is negative";
         if (!(p->clip_low >= 0.f) || !(p->clip_high >= 0.f)) return "a clip is negative";

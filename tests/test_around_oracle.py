@@ -281,3 +281,9 @@ def test_gradients_that_the_policy_loss_does_not_have_are_refused(name):
         kw[name] = torch.autograd.forward_ad.make_dual(kw[name], torch.ones(2))
         with pytest.raises(ValueError, match=f"{name} requires a gradient"):
             call()
+
+
+@pytest.mark.parametrize("call", ["logoskg_token_logp", "logoskg_policy_loss", "logoskg_policy_loss_backward"])
+def test_policy_scales_that_leave_32_bits_as_exponents_are_refused(call):
+    rc, text = _status(call, training._Policy(**{**_POLICY, "scale": 3e38}))
+    assert rc == 1 and "scale is above" in text, text

@@ -421,3 +421,10 @@ def test_tangents_are_not_lost():
         a["logits"] = torch.autograd.forward_ad.make_dual(a["logits"], torch.ones_like(a["logits"]))
         with pytest.raises(NotImplementedError, match="jvp"):
             lkg.policy_loss(**a)
+
+
+def test_the_largest_scale():
+    a = _gpu(dict(logits=torch.tensor([[1.0, 0.5, -2.0], [0.25, 0.25, 0.0]]), target=torch.tensor([0, 1], dtype=torch.int32), advantage=torch.ones(2), scale=2e38))
+    got = lkg.policy_loss(**a, gradient=True)
+    assert got["logp"][0] == 0 and abs(float(got["logp"][1]) + math.log(2)) < 1e-6
+    assert got["dlogits"][0].tolist() == [0, 0, 0] and torch.allclose(got["dlogits"][1], torch.tensor([1e38, -1e38, 0.0], device="cuda"))
