@@ -4,10 +4,9 @@ from __future__ import annotations
 
 import ctypes
 import functools
-import struct
 
 from .binding import _check, _load, _stream_handle, _torch
-from .reading import _dtype, _entity_read_of, _I32, _I64, _on_gpu, _on_stream, _P, _packer, _plain, _rows, _score, _workspace
+from .reading import _apart, _dtype, _entity_read_of, _I32, _I64, _last_of, _on_gpu, _on_stream, _P, _packer, _plain, _rows, _score, _workspace
 
 
 class _Pack(ctypes.Structure):
@@ -17,18 +16,6 @@ class _Pack(ctypes.Structure):
 
 
 _pack_of = _packer(_Pack)
-def _apart(written, name, *others):
-    """Refuses a tensor that is written where others that are read lie."""
-    def ends(t):
-        return t.data_ptr(), t.data_ptr() + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))) if t.numel() else t.data_ptr()
-    begin, end = ends(written)
-    for t in others:
-        first, last = ends(t)
-        if begin < last and first < end:
-            raise ValueError(f"{name} shares memory with an input")
-
-
-_last_of = struct.Struct("=QqQ").pack  # workspace, workspace_bytes and stream, with which the structures of calls that have one end
 
 
 @functools.lru_cache(None)

@@ -140,6 +140,21 @@ def _workspace(nbytes, like):
     return like.new_empty(nbytes, dtype=_torch().uint8)
 
 
+def _apart(written, name, *others):
+    """Refuses a tensor that is written where others that are read lie."""
+    def ends(t):
+        return t.data_ptr(), t.data_ptr() + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))) if t.numel() else t.data_ptr()
+
+    begin, end = ends(written)
+    for t in others:
+        first, last = ends(t)
+        if begin < last and first < end:
+            raise ValueError(f"{name} shares memory with an input")
+
+
+_last_of = struct.Struct("=QqQ").pack  # workspace, workspace_bytes and stream, with which the structures of calls that have one end
+
+
 def distance_buckets(num_buckets: int, max_distance: int, both_sides: bool = True, device="cuda"):
     """int32[2 M + 1]: a bucket for every distance -M .. M (M = max_distance; what is farther counts as M).
 

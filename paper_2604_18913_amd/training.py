@@ -9,8 +9,7 @@ import functools
 import struct
 
 from .binding import _check, _load, _stream_handle, _torch
-from .packed import _apart, _last_of
-from .reading import _dtype, _F, _has_tangent, _I32, _I64, _on_gpu, _on_stream, _P, _packer, _plain, _workspace
+from .reading import _apart, _dtype, _F, _has_tangent, _I32, _I64, _last_of, _on_gpu, _on_stream, _P, _packer, _plain, _workspace
 
 _U32 = ctypes.c_uint32
 
