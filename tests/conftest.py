@@ -29,3 +29,11 @@ def pytest_collection_modifyitems(config, items):
     for item in items:
         if "gpu" in item.keywords:
             item.add_marker(skip)
+
+
+@pytest.fixture
+def memory_given_back():
+    """Of a test whose tensors take much of the card: the library's own memory does not come from torch's cache."""
+    import torch
+    yield
+    torch.cuda.empty_cache()

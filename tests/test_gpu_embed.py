@@ -252,7 +252,7 @@ def test_what_the_binding_refuses():
         lkg.embed_entities_backward(table[:3].clone(), ids, 4, out=table[:1].expand(4, 8))
 
 
-def test_more_ids_than_a_launch_takes():
+def test_more_ids_than_a_launch_takes(memory_given_back):
     n = (1 << 34) + 3000  # four rows of one element a thread: 2^32 threads and some
     table = torch.tensor([[1.0], [2.0], [3.0]], dtype=torch.bfloat16, device="cuda")
     ids = torch.zeros(n, dtype=torch.int32, device="cuda")

@@ -283,7 +283,7 @@ def test_what_the_binding_refuses():
 
 
 @pytest.mark.parametrize("packed", [False, True], ids=["16 bits", "4 bits"])
-def test_more_lists_than_a_launch_takes(packed):
+def test_more_lists_than_a_launch_takes(packed, memory_given_back):
     """2^26 lists and some of one entry, the last one of 5,000, in four heads: 2^32 threads and more of the reading and of the join."""
     lists, entities = (1 << 26) + 40, 6001
     values = (torch.arange(entities, device="cuda") % 50).to(torch.bfloat16)[:, None, None].expand(-1, 4, 8).contiguous()

@@ -326,7 +326,7 @@ def test_hidden_ids_get_no_gradient_whatever_their_row_holds(rows, vocab, dtype)
 
 
 @pytest.mark.parametrize("rows, vocab, masked", [((1 << 28) + 40, 6, False), ((1 << 28) + 40, 6, True), ((1 << 24) + 40, 2064, False)])
-def test_more_rows_than_a_launch_takes(rows, vocab, masked):
+def test_more_rows_than_a_launch_takes(rows, vocab, masked, memory_given_back):
     """Rows of 16 lanes (2^28 and more), and of 256 (2^24 and more): 2^32 threads and more."""
     logits = torch.zeros(rows, vocab, dtype=torch.bfloat16, device="cuda")
     target = (torch.arange(rows, device="cuda") % 6).int()

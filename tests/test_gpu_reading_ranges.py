@@ -330,7 +330,7 @@ def test_gradients_of_rows_with_few_keys(dim, heads, kv_heads, cap):
     assert (got["dq"].cpu().double() - want).norm() < 0.0035 * want.norm()
 
 
-def test_more_rows_of_logits_than_a_launch_takes():
+def test_more_rows_of_logits_than_a_launch_takes(memory_given_back):
     rows = (1 << 24) + 40  # a block of 256 threads each
     logits = torch.arange(20, device="cuda").to(torch.bfloat16).expand(rows, 20).contiguous()
     mask = torch.full((rows, 1), 0b1010, device="cuda")
@@ -341,7 +341,7 @@ def test_more_rows_of_logits_than_a_launch_takes():
     assert bool((got[:-1] == want).all()) and got[-1].tolist() == [0.0] + [-float("inf")] * 19
 
 
-def test_more_masks_than_a_launch_takes():
+def test_more_masks_than_a_launch_takes(memory_given_back):
     rows = (1 << 22) + 40  # a block of 1,024 threads each, if one launch took them
     off = torch.arange(rows + 1, device="cuda")
     ids = (torch.arange(rows, device="cuda") % 60).int()
